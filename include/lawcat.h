@@ -333,6 +333,93 @@ int lawcat_layer_fwd_noalloc(const lawcat_params* p, const void* q, const void* 
                              const void* cache_k_in, const float* S0, const float* z0, void* o, void* cache_q_out,
                              void* cache_k_out, float* S_T, float* z_T, void* stream, int* dev_status);
 
+/*
+ * Softmax attention beside the layer: what the layer is distilled from (Eq. 1; the layer-wise stage of Section 5.1 compares the
+ * layer's output with the output of softmax attention) and what a hybrid model keeps in some layers (the sliding-window rows of
+ * the ablation). With i the position of a query and j that of a key, per query head h reading key-value head h / G:
+ *   u = scale q_i . k_j     s = u, or cap tanh(u / cap) when cap > 0     x = s - slopes[h] |i - j| when slopes are given
+ *   p = softmax over the keys that query i sees     o_i = sum_j p_j v_j     lse_i = ln sum_j exp(x_j)
+ * Keys that a query sees: all T_k of them; causal = 1: those with j <= i; window = w > 0: those with |i - j| < w. Query t has
+ * position i = t + T_k - T (a piece of a prompt behind T_k - T earlier tokens). A query that sees no key (T > T_k) has o = 0 and
+ * lse = -infinity, and no gradient.
+ */
+typedef struct {
+  int32_t B, T, T_k; /* T queries, T_k keys per sequence; the cache calls: T rows, caches of T_k slots */
+  int32_t H, H_kv, d; /* d in {16, 32, 64, 128}, keys and values alike */
+  int32_t dtype;     /* LAWCAT_F32 | LAWCAT_BF16 */
+  int32_t causal;    /* 0 | 1 */
+  int32_t window;    /* 0 = none */
+  int32_t exact;     /* 1 = the fp32 CUDA-core kernels whatever the shape */
+  float scale;       /* usually 1 / sqrt(d) */
+  float cap;         /* 0 = none */
+} lawcat_attn_params;
+
+enum { LAWCAT_OP_ATTN_FWD = 7, LAWCAT_OP_ATTN_BWD = 8, LAWCAT_OP_ATTN_DECODE = 9 };
+
+/* Scratch bytes of the attention entry points (LAWCAT_OP_ATTN_*; both decode steps share one); 0 on invalid parameters. */
+size_t lawcat_attn_workspace_bytes(const lawcat_attn_params* p, int op);
+
+/*
+ * Forward: q [B,T,H,d]  k, v [B,T_k,H_kv,d]  slopes [H] fp32 or NULL  ->  o [B,T,H,d], lse [B,T,H] fp32 (nullable; the backward
+ * needs it).
+ *   cu_seqlens: NULL, or a HOST array of nseq + 1 non-decreasing ints, cu_seqlens[0] = 0, cu_seqlens[nseq] = T: the tokens of nseq
+ *     documents packed along T (B = 1, T_k = T). No query sees a key of another document.
+ *   prefix: NULL, or a HOST array of nseq ints (nseq = B without cu_seqlens): the first prefix[i] keys of sequence i are seen by
+ *     every query of that sequence (causal = 1, no window).
+ *   nseq is 0 when both are NULL. The arrays are read during the call; a captured call keeps their values.
+ * fp32 accumulation, softmax statistics in fp32, one rounding of o.
+ * A key or value row that a query does not see does not reach its results, not even as a NaN.
+ */
+int lawcat_attn_fwd(const lawcat_attn_params* p, const int32_t* cu_seqlens, const int32_t* prefix, int32_t nseq, const void* q,
+                    const void* k, const void* v, const float* slopes, void* o, float* lse, void* ws, size_t ws_bytes, void* stream,
+                    int* dev_status);
+
+/*
+ * Backward for an upstream gradient dO [B,T,H,d], from the forward's inputs, its o and its lse:
+ *   dq [B,T,H,d], dk, dv [B,T_k,H_kv,d] in p->dtype, overwritten; dk and dv are summed over the query heads of a group in fp32
+ *   and rounded once. All are required. No gradient flows into the slopes and none is taken from lse. The sums have one order:
+ *   the same call gives the same bits.
+ */
+int lawcat_attn_bwd(const lawcat_attn_params* p, const int32_t* cu_seqlens, const int32_t* prefix, int32_t nseq, const void* q,
+                    const void* k, const void* v, const float* slopes, const void* o, const float* lse, const void* dO, void* dq,
+                    void* dk, void* dv, void* ws, size_t ws_bytes, void* stream, int* dev_status);
+
+/*
+ * One decode step for B sequences over caches of C = p->T_k slots (p->T and p->causal are ignored):
+ *   q_t [B,H,d]  k_t, v_t [B,H_kv,d]  K, V [B,C,H_kv,d]  pos [B] DEVICE ints: the position of the new token, i.e. the tokens so far
+ * The step writes k_t, v_t to slot pos mod C and attends to positions max(0, pos - C + 1) ... pos, under a window w to the last w
+ * of them (w <= C: a sliding-window layer needs a ring of w slots). pos is read on the device (a captured step is replayed at
+ * every length) and not advanced: several layers share it. A sequence with pos < 0 is not there: its cache stays and its o_t is 0.
+ * Slots that hold no token yet may hold anything.   out: o_t [B,H,d]
+ */
+int lawcat_attn_decode(const lawcat_attn_params* p, const void* q_t, const void* k_t, const void* v_t, void* K, void* V, const int32_t* pos,
+                       const float* slopes, void* o_t, void* ws, size_t ws_bytes, void* stream, int* dev_status);
+
+/*
+ * The cache held in 4 bits, by groups of 32 channels of a row (16 at d = 16):
+ *   kq, vq [B,H_kv,C,d/2] bytes: the codes of channels 2i (low half) and 2i+1;  kp, vp [B,H_kv,C,groups,2] bf16: scale, minimum
+ *   value = minimum + code * scale,  minimum = bf16(min x),  scale = bf16((max x - minimum) / 15),
+ *   code = round to even((x - minimum) / scale), limited to 0 ... 15 (0 when the scale is not positive)
+ * A group that holds a value that is not finite, or spans more than fp32 holds, reads back as NaN.
+ * lawcat_cache_quantize: rows t = 0 ... T-1 of k, v [B,T,H_kv,d] go to slots (pos + t) mod C, pos [B] DEVICE ints (of more than C
+ *   rows the last C are kept); nothing is written for a sequence with pos < 0.
+ * lawcat_cache_dequantize: the same slots as values, rounded to p->dtype (a piece of a prompt behind a cache takes its k, v for
+ *   lawcat_attn_fwd from here); zeros for a sequence with pos < 0.
+ * p->H is not used. No scratch: ws may be NULL.
+ */
+int lawcat_cache_quantize(const lawcat_attn_params* p, const void* k, const void* v, const int32_t* pos, void* kq, void* kp, void* vq,
+                          void* vp, void* ws, size_t ws_bytes, void* stream, int* dev_status);
+int lawcat_cache_dequantize(const lawcat_attn_params* p, const void* kq, const void* kp, const void* vq, const void* vp, const int32_t* pos,
+                            void* k, void* v, void* ws, size_t ws_bytes, void* stream, int* dev_status);
+
+/*
+ * lawcat_attn_decode over a cache in 4 bits: k_t, v_t are quantized into their slot, and the step attends to what the cache then
+ * holds, the new token's row included.
+ */
+int lawcat_attn_decode_quant(const lawcat_attn_params* p, const void* q_t, const void* k_t, const void* v_t, void* kq, void* kp, void* vq,
+                             void* vp, const int32_t* pos, const float* slopes, void* o_t, void* ws, size_t ws_bytes, void* stream,
+                             int* dev_status);
+
 #ifdef __cplusplus
 }
 #endif

@@ -20,13 +20,15 @@ F32, BF16 = 0, 1
 PHI_SOFTMAX, PHI_ELU1, PHI_IDENTITY = 0, 1, 2
 GATE_LOGITS, GATE_LOGDECAY = 0, 1
 OP_CONV_FWD, OP_CONV_BWD, OP_GLA_FWD, OP_GLA_BWD, OP_LAYER_FWD, OP_DECODE_STEP, OP_LAYER_BWD = range(7)
+OP_ATTN_FWD, OP_ATTN_BWD, OP_ATTN_DECODE = range(7, 10)
 
 EXPORTS = ["lawcat_workspace_bytes", "lawcat_status_string", "lawcat_version", "lawcat_launch_count",
            "lawcat_trace_begin", "lawcat_trace_end", "lawcat_test_set_wait_limit", "lawcat_conv_fwd", "lawcat_conv_bwd", "lawcat_gla_fwd",
            "lawcat_gla_bwd", "lawcat_layer_fwd", "lawcat_layer_fwd_varlen_workspace_bytes",
            "lawcat_layer_fwd_varlen", "lawcat_layer_bwd", "lawcat_decode_step", "lawcat_layer_fwd_host_arena_bytes",
            "lawcat_layer_fwd_host", "lawcat_noalloc_scratch_bytes", "lawcat_layer_fwd_noalloc", "lawcat_last_cuda_error", "lawcat_gate_fn_workspace_bytes",
-           "lawcat_gate_fn_fwd"]
+           "lawcat_gate_fn_fwd", "lawcat_attn_workspace_bytes", "lawcat_attn_fwd", "lawcat_attn_bwd", "lawcat_attn_decode",
+           "lawcat_cache_quantize", "lawcat_cache_dequantize", "lawcat_attn_decode_quant"]
 
 
 class LawcatError(RuntimeError):
@@ -57,6 +59,21 @@ def params(B, T, H, H_kv, d_k, d_v, conv_k=4, gate_dim=0, chunk=0, dtype=BF16, p
                   normalize, mix_unshared)
 
 
+class AttnParams(ctypes.Structure):
+    """Mirror of ``lawcat_attn_params``."""
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("T_k", ctypes.c_int32), ("H", ctypes.c_int32),
+                ("H_kv", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("exact", ctypes.c_int32), ("scale", ctypes.c_float), ("cap", ctypes.c_float)]
+
+
+def attn_params(B, T, H, H_kv, d, T_k=None, dtype=BF16, causal=1, window=0, exact=0, scale=None, cap=0.0) -> AttnParams:
+    """T_k defaults to T, scale to 1 / sqrt(d)."""
+    if isinstance(dtype, str):
+        dtype = {"f32": F32, "bf16": BF16}[dtype]
+    return AttnParams(B, T, T if T_k is None else T_k, H, H_kv, d, dtype, causal, window, exact,
+                      d ** -0.5 if scale is None else scale, cap)
+
+
 _lib = None
 
 
@@ -85,6 +102,19 @@ def lib() -> ctypes.CDLL:
         L.lawcat_trace_end.argtypes = [ctypes.c_char_p, ctypes.c_size_t]
         L.lawcat_gate_fn_workspace_bytes.restype = ctypes.c_size_t
         L.lawcat_gate_fn_workspace_bytes.argtypes = [ctypes.POINTER(Params), ctypes.c_int32, ctypes.c_int32]
+        L.lawcat_attn_workspace_bytes.restype = ctypes.c_size_t
+        L.lawcat_attn_workspace_bytes.argtypes = [ctypes.POINTER(AttnParams), ctypes.c_int]
+        for name, nptr in (("lawcat_attn_decode", 8), ("lawcat_cache_quantize", 7), ("lawcat_cache_dequantize", 7),
+                           ("lawcat_attn_decode_quant", 10)):
+            f = getattr(L, name)
+            f.restype = ctypes.c_int
+            f.argtypes = [ctypes.POINTER(AttnParams)] + [ctypes.c_void_p] * nptr + \
+                         [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p]
+        for name, nptr in (("lawcat_attn_fwd", 6), ("lawcat_attn_bwd", 10)):
+            f = getattr(L, name)
+            f.restype = ctypes.c_int
+            f.argtypes = [ctypes.POINTER(AttnParams), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32] + \
+                         [ctypes.c_void_p] * nptr + [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p]
         L.lawcat_layer_fwd_varlen_workspace_bytes.restype = ctypes.c_size_t
         L.lawcat_layer_fwd_varlen_workspace_bytes.argtypes = [ctypes.POINTER(Params), ctypes.c_void_p, ctypes.c_int]
         for name, nptr in (("lawcat_conv_fwd", 9), ("lawcat_conv_bwd", 14), ("lawcat_gla_fwd", 10),
@@ -291,6 +321,113 @@ def lawcat_decode_step(p: Params, q_t, k_t, v_t, gate_t, w_q, w_k, W, S, z, cach
         o_t = _empty(q_t, p.dtype, p.B, p.H, p.d_v)
     _call("lawcat_decode_step", p, OP_DECODE_STEP, (q_t, k_t, v_t, gate_t, w_q, w_k, W, S, z, cache_q, cache_k, o_t), ws, stream,
           dev_status)
+    return o_t
+
+
+def _attn_call(name, p, op, args, ws, stream, dev_status, nint=0):
+    """op: the call's LAWCAT_OP_ATTN (its scratch is taken from torch's allocator when ws is None), or None for no scratch."""
+    b = _binding or _bind()
+    st = b.call(_addr[name], ctypes.addressof(p), 0 if op is None else _addr["lawcat_attn_workspace_bytes"], -1 if op is None else op,
+                args, ws, stream and stream.cuda_stream, dev_status, nint)
+    if st != 0:
+        raise LawcatError(st, name)
+
+
+def _expect(p, **tensors):
+    """The kernels trust sizes and types: each named tensor (None is skipped) has to have the given shape and dtype."""
+    for name, (t, shape, dtype) in tensors.items():
+        if t is not None and (t.shape != shape or t.dtype != dtype):
+            raise ValueError(f"{name}: expected {tuple(shape)} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+
+
+def _sequences(cu_seqlens, prefix):
+    """HOST arrays of the packed documents and the prefixes -> (what keeps them alive, the three leading arguments)."""
+    arr = lambda x: None if x is None else (ctypes.c_int32 * max(1, len(x)))(*[int(i) for i in x])  # noqa: E731
+    cu, pre = arr(cu_seqlens), arr(prefix)
+    nseq = len(cu_seqlens) - 1 if cu is not None else len(prefix) if pre is not None else 0
+    if cu is not None and (nseq < 0 or (pre is not None and len(prefix) != nseq)):
+        raise ValueError("cu_seqlens holds nseq + 1 offsets, prefix nseq lengths")
+    return (cu, pre), (0 if cu is None else ctypes.addressof(cu), 0 if pre is None else ctypes.addressof(pre), nseq)
+
+
+def lawcat_attn_fwd(p: AttnParams, q, k, v, slopes=None, cu_seqlens=None, prefix=None, o=None, want_lse=True, ws=None, stream=None,
+                    dev_status=None):
+    """Softmax attention; cu_seqlens (packed documents, nseq + 1 offsets) and prefix (a length per sequence) are host sequences.
+    Returns dict(o, lse)."""
+    dt, qs, ks = torch_dtype(p), (p.B, p.T, p.H, p.d), (p.B, p.T_k, p.H_kv, p.d)
+    _expect(p, q=(q, qs, dt), k=(k, ks, dt), v=(v, ks, dt), o=(o, qs, dt), slopes=(slopes, (p.H,), torch.float32))
+    keep, seqs = _sequences(cu_seqlens, prefix)
+    if o is None:
+        o = _empty(q, p.dtype, *qs)
+    lse = _empty(q, F32, p.B, p.T, p.H) if want_lse else None
+    _attn_call("lawcat_attn_fwd", p, OP_ATTN_FWD, (*seqs, q, k, v, slopes, o, lse), ws, stream, dev_status, 3)
+    return dict(o=o, lse=lse)
+
+
+def lawcat_attn_bwd(p: AttnParams, q, k, v, o, lse, dO, slopes=None, cu_seqlens=None, prefix=None, ws=None, stream=None,
+                    dev_status=None):
+    """Gradients for the upstream gradient dO, from the forward's o and lse: dict(dq, dk, dv)."""
+    dt, qs, ks = torch_dtype(p), (p.B, p.T, p.H, p.d), (p.B, p.T_k, p.H_kv, p.d)
+    _expect(p, q=(q, qs, dt), k=(k, ks, dt), v=(v, ks, dt), o=(o, qs, dt), lse=(lse, qs[:3], torch.float32), dO=(dO, qs, dt),
+            slopes=(slopes, (p.H,), torch.float32))
+    keep, seqs = _sequences(cu_seqlens, prefix)
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    _attn_call("lawcat_attn_bwd", p, OP_ATTN_BWD, (*seqs, q, k, v, slopes, o, lse, dO, dq, dk, dv), ws, stream, dev_status, 3)
+    return dict(dq=dq, dk=dk, dv=dv)
+
+
+def lawcat_attn_decode(p: AttnParams, q_t, k_t, v_t, K, V, pos, slopes=None, o_t=None, ws=None, stream=None, dev_status=None):
+    """One token over caches of p.T_k slots; K, V are updated in place; returns o_t [B,H,d]."""
+    dt, qs, ks, cs = torch_dtype(p), (p.B, p.H, p.d), (p.B, p.H_kv, p.d), (p.B, p.T_k, p.H_kv, p.d)
+    _expect(p, q_t=(q_t, qs, dt), k_t=(k_t, ks, dt), v_t=(v_t, ks, dt), K=(K, cs, dt), V=(V, cs, dt),
+            pos=(pos, (p.B,), torch.int32), o_t=(o_t, qs, dt), slopes=(slopes, (p.H,), torch.float32))
+    if o_t is None:
+        o_t = _empty(q_t, p.dtype, *qs)
+    _attn_call("lawcat_attn_decode", p, OP_ATTN_DECODE, (q_t, k_t, v_t, K, V, pos, slopes, o_t), ws, stream, dev_status)
+    return o_t
+
+
+def quant_cache(p: AttnParams, device="cuda"):
+    """An empty cache in 4 bits for p.B sequences of p.T_k slots: (kq, kp, vq, vp), codes and (scale, minimum) pairs."""
+    q = lambda: torch.zeros(p.B, p.H_kv, p.T_k, p.d // 2, dtype=torch.uint8, device=device)  # noqa: E731
+    g = lambda: torch.zeros(p.B, p.H_kv, p.T_k, max(1, p.d // 32), 2, dtype=torch.bfloat16, device=device)  # noqa: E731
+    return q(), g(), q(), g()
+
+
+def _expect_cache(p, kq, kp, vq, vp, pos):
+    qs, gs = (p.B, p.H_kv, p.T_k, p.d // 2), (p.B, p.H_kv, p.T_k, max(1, p.d // 32), 2)
+    _expect(p, kq=(kq, qs, torch.uint8), kp=(kp, gs, torch.bfloat16), vq=(vq, qs, torch.uint8), vp=(vp, gs, torch.bfloat16),
+            pos=(pos, (p.B,), torch.int32))
+
+
+def lawcat_cache_quantize(p: AttnParams, k, v, pos, kq, kp, vq, vp, stream=None, dev_status=None):
+    """Rows of k, v [B,T,H_kv,d] into slots (pos + t) mod p.T_k of the 4-bit cache, in place."""
+    dt, ks = torch_dtype(p), (p.B, p.T, p.H_kv, p.d)
+    _expect(p, k=(k, ks, dt), v=(v, ks, dt))
+    _expect_cache(p, kq, kp, vq, vp, pos)
+    _attn_call("lawcat_cache_quantize", p, None, (k, v, pos, kq, kp, vq, vp), None, stream, dev_status)
+
+
+def lawcat_cache_dequantize(p: AttnParams, kq, kp, vq, vp, pos, k=None, v=None, stream=None, dev_status=None):
+    """The p.T rows from position pos on as values: dict(k, v) [B,T,H_kv,d]."""
+    dt, ks = torch_dtype(p), (p.B, p.T, p.H_kv, p.d)
+    _expect(p, k=(k, ks, dt), v=(v, ks, dt))
+    _expect_cache(p, kq, kp, vq, vp, pos)
+    k = _empty(kq, p.dtype, *ks) if k is None else k
+    v = _empty(kq, p.dtype, *ks) if v is None else v
+    _attn_call("lawcat_cache_dequantize", p, None, (kq, kp, vq, vp, pos, k, v), None, stream, dev_status)
+    return dict(k=k, v=v)
+
+
+def lawcat_attn_decode_quant(p: AttnParams, q_t, k_t, v_t, kq, kp, vq, vp, pos, slopes=None, o_t=None, ws=None, stream=None,
+                             dev_status=None):
+    """One token over a cache in 4 bits, which is updated in place; returns o_t [B,H,d]."""
+    dt, qs, ks = torch_dtype(p), (p.B, p.H, p.d), (p.B, p.H_kv, p.d)
+    _expect(p, q_t=(q_t, qs, dt), k_t=(k_t, ks, dt), v_t=(v_t, ks, dt), o_t=(o_t, qs, dt), slopes=(slopes, (p.H,), torch.float32))
+    _expect_cache(p, kq, kp, vq, vp, pos)
+    if o_t is None:
+        o_t = _empty(q_t, p.dtype, *qs)
+    _attn_call("lawcat_attn_decode_quant", p, OP_ATTN_DECODE, (q_t, k_t, v_t, kq, kp, vq, vp, pos, slopes, o_t), ws, stream, dev_status)
     return o_t
 
 

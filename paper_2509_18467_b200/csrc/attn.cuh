@@ -1,0 +1,92 @@
+// Softmax attention beside the linearized layer: what its kernels share.
+//   u = scale q.k,  s = cap tanh(u / cap) (cap > 0),  x = s - slope_h |i - j|,  p = softmax(x),  o = p v
+// Every mask offered (causal, window, documents, prefix, T != T_k) leaves a query ONE interval of keys [lo, hi), and both ends
+// grow with the query; the kernels know nothing else of masks.
+#pragma once
+#include "common.cuh"
+
+namespace lawcat {
+namespace attn {
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+
+struct Mask {
+  int T, T_k;
+  int off;           // position of query t: t + off  (T_k - T)
+  int causal, window;
+  const int2* rows;  // [B, T] (lo, hi) where documents or prefixes are given, else null
+};
+
+__host__ __device__ __forceinline__ int2 interval(const Mask& m, int b, int t) {
+#ifdef __CUDA_ARCH__
+  if (m.rows) return __ldg(m.rows + (size_t)b * m.T + t);
+#endif
+  const int pos = t + m.off;
+  int lo = 0, hi = m.T_k;
+  if (m.causal) hi = pos + 1 < m.T_k ? pos + 1 : m.T_k;
+  if (m.window) {
+    if (pos - m.window + 1 > 0) lo = pos - m.window + 1;
+    if (pos < m.T_k - m.window) hi = hi < pos + m.window ? hi : pos + m.window;
+  }
+  return make_int2(lo, hi > lo ? hi : lo);
+}
+
+// Queries that may see one of the keys [j0, j1): the first with hi > j0 up to the first with lo >= j1 (both ends of the
+// intervals grow with t). Called by all threads with the same arguments.
+__device__ __forceinline__ int2 queries_of(const Mask& m, int b, int j0, int j1) {
+  int l = 0, h = m.T;
+  while (l < h) {
+    const int mid = (l + h) >> 1;
+    if (interval(m, b, mid).y > j0) h = mid; else l = mid + 1;
+  }
+  const int first = l;
+  h = m.T;
+  while (l < h) {
+    const int mid = (l + h) >> 1;
+    if (interval(m, b, mid).x >= j1) h = mid; else l = mid + 1;
+  }
+  return make_int2(first, l);
+}
+
+struct Args {
+  const void *q, *k, *v, *dO;
+  const void* o_in;
+  void *o, *dq, *dk, *dv;
+  float* lse;           // [B, T, H] natural logarithm (forward: output; backward: input)
+  const float* slopes;  // [H] or null
+  float2* stat;         // backward: [B, H, T] (lse log2e, dO.o)
+  Mask mask;
+  int B, H, H_kv;
+  float scale, cap;
+  int* dev_status;
+};
+
+}  // namespace attn
+
+// which kernels serve a call (attn_tc.cu), their launchers and scratch
+struct AttnCall {
+  attn::Args a;
+  int d, dtype, exact;
+  cudaStream_t stream;
+};
+int launch_attn_fwd_exact(const AttnCall& c);
+int launch_attn_bwd_exact(const AttnCall& c);
+
+// one step over a cache, in the storage type (K, V) or in 4 bits (kq, kp, vq, vp); attn_decode.cu
+struct AttnDecode {
+  const void *q, *k_t, *v_t;
+  void *K, *V, *kq, *kp, *vq, *vp;
+  const int* pos;
+  const float* slopes;
+  void *o, *ws;
+  int B, H, H_kv, C, window, d, dtype, exact;
+  float scale, cap;
+  cudaStream_t stream;
+};
+size_t attn_decode_workspace_bytes(int B, int H, int H_kv, int C, int window, int d);
+int launch_attn_decode(const AttnDecode& c);
+// T rows per sequence of k_t, v_t into the 4-bit cache, or (write = false) out of it
+int launch_attn_quant(const AttnDecode& c, int T, bool write);
+
+}  // namespace lawcat

@@ -1,0 +1,384 @@
+// One step of softmax attention over a cache of keys and values, and the cache held in 4 bits. See attn.cuh for the formulas.
+//
+// A cache has C slots per sequence; the token at position i lives in slot i mod C, so a window of w tokens needs C >= w slots
+// and nothing else. The step writes the new token's key and value to its slot and attends to positions
+// max(0, pos - C + 1, pos - w + 1) ... pos. The slot that it overwrites held position pos - C, which it does not see.
+//
+// The general kernel: a block takes one (sequence, key-value head, eight query heads at most, part of the keys), walks its
+// part in tiles of 64 keys that it widens to fp32 in shared memory once for all its query heads, and keeps the running maximum
+// and sum of each head (one warp per head). The keys are cut into as many parts as fill the SMs; the parts' (maximum, sum,
+// weighted values) meet in a second kernel. The number of parts follows from the capacity alone, so that a captured step may
+// be replayed at every length.
+#include "attn.cuh"
+
+namespace lawcat {
+namespace attn {
+
+constexpr int TK = 64;       // keys per tile
+constexpr int HB = 8;        // query heads per block (one warp each)
+constexpr int DEC_THREADS = 32 * HB;
+
+struct DecArgs {
+  const void *q, *k_t, *v_t;    // [B, H, D], [B, H_kv, D]
+  void *K, *V;                  // [B, C, H_kv, D] in the storage type (not in the 4-bit form)
+  uint8_t *kq, *vq;             // [B, H_kv, C, D / 2]
+  bf16 *kp, *vp;                // [B, H_kv, C, groups, 2]
+  const int* pos;               // [B]
+  const float* slopes;
+  void* o;                      // [B, H, D]
+  float* part;                  // [B, H, parts, D + 2] (maximum in log2 units, sum, weighted values) where parts > 1
+  int B, H, H_kv, C, window, parts;
+  float scale, cap;
+};
+
+__host__ __device__ constexpr int quant_group(int d) { return d < 32 ? d : 32; }
+
+// scale and minimum of a group from its minimum and maximum, both rounded to bf16; a group that holds a value that is not
+// finite (or spans more than fp32 holds) reads back as NaN
+__device__ __forceinline__ void quant_params(float lo, float hi, bool finite, float& scale, float& low) {
+  low = __bfloat162float(__float2bfloat16_rn(lo));
+  const float s = __fdiv_rn(hi - low, 15.f);
+  scale = finite && isfinite(s) && isfinite(low) ? __bfloat162float(__float2bfloat16_rn(s)) : NAN;
+}
+// (in fp32 as in 64 bits: the difference of two bf16 values a few binades apart is exact, and no quotient of such numbers lies
+// closer to a border between two codes than fp32 tells apart)
+__device__ __forceinline__ uint32_t quant_code(float x, float scale, float low) {
+  return scale > 0.f ? (uint32_t)fminf(fmaxf(rintf(__fdiv_rn(x - low, scale)), 0.f), 15.f) : 0u;
+}
+
+// Eight channels of one row (c0 = 8 i), threads of a group side by side in a warp: codes as one word, parameters by the
+// group's first thread, and the values that they stand for in place of x.
+template <int D>
+__device__ __forceinline__ void quantize8(float (&x)[8], int c0, uint8_t* q_row, bf16* p_row, bool write) {
+  constexpr int GS = quant_group(D), TPG = GS / 8;
+  float lo = x[0], hi = x[0];
+  bool fin = true;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    lo = fminf(lo, x[i]);
+    hi = fmaxf(hi, x[i]);
+    fin = fin && isfinite(x[i]);
+  }
+  const unsigned lanes = ((1u << TPG) - 1) << (threadIdx.x & 31 & ~(TPG - 1));  // the group's threads
+#pragma unroll
+  for (int o = 1; o < TPG; o <<= 1) {
+    lo = fminf(lo, __shfl_xor_sync(lanes, lo, o));
+    hi = fmaxf(hi, __shfl_xor_sync(lanes, hi, o));
+    fin = __shfl_xor_sync(lanes, (int)fin, o) && fin;
+  }
+  float scale, low;
+  quant_params(lo, hi, fin, scale, low);
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t code = quant_code(x[i], scale, low);
+    w |= code << (4 * i);
+    x[i] = fmaf((float)code, scale, low);
+  }
+  if (write) {
+    *reinterpret_cast<uint32_t*>(q_row + c0 / 2) = w;
+    if (c0 % GS == 0)
+      reinterpret_cast<__nv_bfloat162*>(p_row)[c0 / GS] = __nv_bfloat162(__float2bfloat16_rn(scale), __float2bfloat16_rn(low));
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  } else {
+    const uint4 w = *reinterpret_cast<const uint4*>(p);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(u[i] << 16);
+      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) stf<T>(p + i, x[i]);
+}
+template <int D>
+__device__ __forceinline__ void load8q(const uint8_t* q_row, const bf16* p_row, int c0, float (&x)[8]) {
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(q_row + c0 / 2);
+  const __nv_bfloat162 p = reinterpret_cast<const __nv_bfloat162*>(p_row)[c0 / quant_group(D)];
+  const float scale = __bfloat162float(p.x), low = __bfloat162float(p.y);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = fmaf((float)(w >> (4 * i) & 15u), scale, low);
+}
+
+// T: storage type of the step's own tensors; QUANT: the cache holds 4-bit codes
+template <typename T, int D, bool QUANT>
+__global__ void __launch_bounds__(DEC_THREADS) attn_decode_kernel(const DecArgs a) {
+  constexpr int LD = D + 4, V8 = D / 8, NC = D / 32;
+  extern __shared__ __align__(16) float sm[];
+  float *K = sm, *V = K + TK * LD, *Q = V + TK * LD, *P = Q + HB * LD, *R = P + HB * TK;  // R: [HB] factor of the accumulators
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int G = a.H / a.H_kv, HG = (G + HB - 1) / HB;
+  const int part = blockIdx.x % a.parts, hg = blockIdx.x / a.parts % HG, bg = blockIdx.x / a.parts / HG;
+  const int b = bg / a.H_kv, g = bg % a.H_kv, h0 = g * G + hg * HB, nh = min(HB, G - hg * HB);
+  const int pos = a.pos[b];
+  int n = pos < 0 ? 0 : min(pos, a.C - 1) + 1;                         // keys that are seen: positions pos - n + 1 ... pos
+  if (a.window && n > a.window) n = a.window;
+  const int per = ((n + a.parts - 1) / a.parts + TK - 1) / TK * TK;     // keys of a part
+  const int i0 = min(n, part * per), i1 = min(n, i0 + per);
+  const T* q = (const T*)a.q + ((size_t)b * a.H + h0) * D;
+  for (int i = tid; i < HB * D; i += DEC_THREADS) Q[i / D * LD + i % D] = i / D < nh ? ldf<T>(q + i) : 0.f;
+  const T* k_t = (const T*)a.k_t + ((size_t)b * a.H_kv + g) * D;
+  const T* v_t = (const T*)a.v_t + ((size_t)b * a.H_kv + g) * D;
+  const float slope = a.slopes && warp < nh ? a.slopes[h0 + warp] : 0.f;
+  float m = -INFINITY, l = 0.f, acc[NC > 0 ? NC : 1];
+#pragma unroll
+  for (int c = 0; c < (NC > 0 ? NC : 1); ++c) acc[c] = 0.f;
+
+  for (int t0 = i0; t0 < i1; t0 += TK) {
+    __syncthreads();
+    for (int i = tid; i < TK * V8; i += DEC_THREADS) {
+      const int r = i / V8, c0 = i % V8 * 8, idx = t0 + r;
+      float x[8] = {}, y[8] = {};
+      if (idx < i1) {
+        const int at = pos - (n - 1 - idx);
+        const size_t slot = at % a.C;
+        const bool fresh = idx == n - 1;  // (the new token: its row comes from the step, and goes into the cache)
+        if constexpr (QUANT) {
+          const size_t row = ((size_t)b * a.H_kv + g) * a.C + slot;
+          constexpr int NG = D / quant_group(D);
+          if (fresh) {
+            load8(k_t + c0, x);
+            load8(v_t + c0, y);
+            quantize8<D>(x, c0, a.kq + row * (D / 2), a.kp + row * (2 * NG), hg == 0);
+            quantize8<D>(y, c0, a.vq + row * (D / 2), a.vp + row * (2 * NG), hg == 0);
+          } else {
+            load8q<D>(a.kq + row * (D / 2), a.kp + row * (2 * NG), c0, x);
+            load8q<D>(a.vq + row * (D / 2), a.vp + row * (2 * NG), c0, y);
+          }
+        } else {
+          const size_t row = (((size_t)b * a.C + slot) * a.H_kv + g) * D + c0;
+          load8(fresh ? k_t + c0 : (const T*)a.K + row, x);
+          load8(fresh ? v_t + c0 : (const T*)a.V + row, y);
+          if (fresh && hg == 0) {
+            store8((T*)a.K + row, x);
+            store8((T*)a.V + row, y);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        K[r * LD + c0 + j] = x[j];
+        V[r * LD + c0 + j] = y[j];
+      }
+    }
+    __syncthreads();
+    float s[2];
+    float mx = m;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int r = lane + 32 * j, idx = t0 + r;
+      float d = 0.f;
+#pragma unroll 8
+      for (int c = 0; c < D; c += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(Q + warp * LD + c), y = *reinterpret_cast<const float4*>(K + r * LD + c);
+        d = fmaf(x.w, y.w, fmaf(x.z, y.z, fmaf(x.y, y.y, fmaf(x.x, y.x, d))));
+      }
+      float x = d * a.scale;
+      if (a.cap > 0.f) x = a.cap * tanhf(x / a.cap);
+      x = (x - slope * (float)(n - 1 - idx)) * LOG2E;
+      s[j] = idx < i1 ? x : -INFINITY;
+      mx = fmaxf(mx, s[j]);
+    }
+    mx = warp_max(mx);
+    const float base = mx == -INFINITY ? 0.f : mx, corr = exp2f(m - base);
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float p = exp2f(s[j] - base);
+      P[warp * TK + lane + 32 * j] = p;
+      sum += p;
+    }
+    l = l * corr + warp_sum(sum);
+    m = mx;
+    __syncwarp();
+    if (NC > 0 || lane < D) {
+#pragma unroll
+      for (int c = 0; c < (NC > 0 ? NC : 1); ++c) {
+        float w = acc[c] * corr;
+        const int rows = min(TK, i1 - t0);
+#pragma unroll 8
+        for (int r = 0; r < rows; ++r) w = fmaf(P[warp * TK + r], V[r * LD + lane + 32 * c], w);
+        acc[c] = w;
+      }
+    }
+  }
+  if (warp >= nh) return;
+  const int h = h0 + warp;
+  if (a.parts == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (NC > 0 || lane < D)
+#pragma unroll
+      for (int c = 0; c < (NC > 0 ? NC : 1); ++c) stf<T>((T*)a.o + ((size_t)b * a.H + h) * D + lane + 32 * c, acc[c] * inv);
+  } else {
+    float* w = a.part + (((size_t)b * a.H + h) * a.parts + part) * (D + 2);
+    if (lane == 0) {
+      w[0] = m;
+      w[1] = l;
+    }
+    if (NC > 0 || lane < D)
+#pragma unroll
+      for (int c = 0; c < (NC > 0 ? NC : 1); ++c) w[2 + lane + 32 * c] = acc[c];
+  }
+}
+
+// the parts of a (sequence, head), one warp each: every part's sum and values at the common maximum
+template <typename T, int D>
+__global__ void attn_decode_join_kernel(const DecArgs a) {
+  const int bh = (blockIdx.x * blockDim.x + threadIdx.x) >> 5, lane = threadIdx.x & 31;
+  if (bh >= a.B * a.H) return;
+  const float* w = a.part + (size_t)bh * a.parts * (D + 2);
+  float m = -INFINITY;
+  for (int i = lane; i < a.parts; i += 32) m = fmaxf(m, w[(size_t)i * (D + 2)]);
+  m = warp_max(m);
+  const float base = m == -INFINITY ? 0.f : m;
+  constexpr int NC = D / 32 > 0 ? D / 32 : 1;
+  float l = 0.f, acc[NC] = {};
+  for (int i = 0; i < a.parts; ++i) {
+    const float* x = w + (size_t)i * (D + 2);
+    const float f = exp2f(x[0] - base);
+    if (x[1] == 0.f) continue;
+    l = fmaf(f, x[1], l);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      if (lane + 32 * c < D) acc[c] = fmaf(f, x[2 + lane + 32 * c], acc[c]);
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+    if (lane + 32 * c < D) stf<T>((T*)a.o + (size_t)bh * D + lane + 32 * c, acc[c] * inv);
+}
+
+// [B, T, H_kv, D] rows of k and v to and from the slots (pos + t) mod C; a thread has eight channels of one row
+struct QuantArgs {
+  void *k, *v;
+  const int* pos;
+  uint8_t *kq, *vq;
+  bf16 *kp, *vp;
+  int B, T, H_kv, C;
+};
+template <typename T, int D, bool WRITE>
+__global__ void __launch_bounds__(256) attn_quant_kernel(const QuantArgs a) {
+  constexpr int V8 = D / 8, NG = D / quant_group(D);
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, row = i / V8;  // row = ((b T + t) H_kv + g)
+  const int c0 = (int)(i % V8) * 8;
+  const bool is_v = blockIdx.y;
+  if (row >= (size_t)a.B * a.T * a.H_kv) return;
+  const int g = (int)(row % a.H_kv);
+  const size_t bt = row / a.H_kv;
+  const int t = (int)(bt % a.T), b = (int)(bt / a.T);
+  const int p0 = a.pos[b];
+  T* const x_row = (T*)(is_v ? a.v : a.k) + row * D + c0;
+  float x[8] = {};
+  if (p0 < 0) {                        // a sequence that is not there: its slots stay, what is read of them is zero
+    if (!WRITE) store8(x_row, x);
+    return;
+  }
+  if (WRITE && t < a.T - a.C) return;  // (a later token takes this slot)
+  const size_t slot = (size_t)(((long long)p0 + t) % a.C);
+  const size_t at = ((size_t)b * a.H_kv + g) * a.C + slot;
+  uint8_t* const q_row = (is_v ? a.vq : a.kq) + at * (D / 2);
+  bf16* const p_row = (is_v ? a.vp : a.kp) + at * (2 * NG);
+  if (WRITE) {
+    load8(x_row, x);
+    quantize8<D>(x, c0, q_row, p_row, true);
+  } else {
+    load8q<D>(q_row, p_row, c0, x);
+    store8(x_row, x);
+  }
+}
+
+// Parts of the keys: as many as give each SM two blocks, while a part keeps at least 256 keys.
+int decode_parts(int B, int H, int H_kv, int C, int window) {
+  const int G = H / H_kv;
+  const long long n = (long long)B * H_kv * ((G + HB - 1) / HB);
+  const int most = ((window && window < C ? window : C) + 255) / 256;
+  const long long want = (2LL * sm_count() + n - 1) / (n > 0 ? n : 1);
+  return (int)(want < 1 ? 1 : want < most ? want : most);
+}
+
+}  // namespace attn
+
+size_t attn_decode_workspace_bytes(int B, int H, int H_kv, int C, int window, int d) {
+  const int parts = attn::decode_parts(B, H, H_kv, C, window);
+  return parts == 1 ? 0 : sizeof(float) * (size_t)B * H * parts * (d + 2);
+}
+
+namespace {
+template <typename F>
+int by_width(int d, F f) {
+  switch (d) {
+    case 16: return f(std::integral_constant<int, 16>{});
+    case 32: return f(std::integral_constant<int, 32>{});
+    case 64: return f(std::integral_constant<int, 64>{});
+    default: return f(std::integral_constant<int, 128>{});
+  }
+}
+}  // namespace
+
+int launch_attn_decode(const AttnDecode& c) {
+  attn::DecArgs a{c.q, c.k_t, c.v_t, c.K, c.V, (uint8_t*)c.kq, (uint8_t*)c.vq, (bf16*)c.kp, (bf16*)c.vp, c.pos, c.slopes, c.o, (float*)c.ws,
+                  c.B, c.H, c.H_kv, c.C, c.window, attn::decode_parts(c.B, c.H, c.H_kv, c.C, c.window), c.scale, c.cap};
+  const int G = c.H / c.H_kv;
+  const long long blocks = (long long)c.B * c.H_kv * ((G + attn::HB - 1) / attn::HB) * a.parts;
+  if (blocks > 0x7fffffffLL) return LAWCAT_ERR_UNSUPPORTED;
+  return by_width(c.d, [&](auto dd) {
+    constexpr int D = decltype(dd)::value;
+    auto go = [&](auto t, auto quant) -> int {
+      using T = decltype(t);
+      constexpr bool Q4 = decltype(quant)::value;
+      const size_t sm = sizeof(float) * ((2 * attn::TK + attn::HB) * (D + 4) + attn::HB * attn::TK + attn::HB);
+      const cudaError_t e = cudaFuncSetAttribute(attn::attn_decode_kernel<T, D, Q4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm);
+      if (e != cudaSuccess) {
+        cudaGetLastError();
+        note_cuda_error(e, __FILE__, __LINE__);
+        return LAWCAT_ERR_CUDA;
+      }
+      LAWCAT_LAUNCH("attn_decode", c.stream,
+                    attn::attn_decode_kernel<T, D, Q4><<<(unsigned)blocks, attn::DEC_THREADS, sm, c.stream>>>(a));
+      LAWCAT_CHECK_LAUNCH();
+      if (a.parts > 1) {
+        LAWCAT_LAUNCH("attn_decode_join", c.stream,
+                      attn::attn_decode_join_kernel<T, D><<<(unsigned)(((long long)c.B * c.H + 3) / 4), 128, 0, c.stream>>>(a));
+        LAWCAT_CHECK_LAUNCH();
+      }
+      return LAWCAT_OK;
+    };
+    if (c.kq) return c.dtype == LAWCAT_F32 ? go(float{}, std::true_type{}) : go(bf16{}, std::true_type{});
+    return c.dtype == LAWCAT_F32 ? go(float{}, std::false_type{}) : go(bf16{}, std::false_type{});
+  });
+}
+
+int launch_attn_quant(const AttnDecode& c, int T, bool write) {
+  attn::QuantArgs a{const_cast<void*>(c.k_t), const_cast<void*>(c.v_t), c.pos, (uint8_t*)c.kq, (uint8_t*)c.vq, (bf16*)c.kp, (bf16*)c.vp,
+                    c.B, T, c.H_kv, c.C};
+  const unsigned long long n = ((unsigned long long)c.B * T * c.H_kv * (c.d / 8) + 255) / 256;
+  if (n > 0x7fffffffULL) return LAWCAT_ERR_UNSUPPORTED;
+  return by_width(c.d, [&](auto dd) {
+    constexpr int D = decltype(dd)::value;
+    auto go = [&](auto t) -> int {
+      using U = decltype(t);
+      const dim3 grid((unsigned)n, 2);
+      if (write) {
+        LAWCAT_LAUNCH("attn_quantize", c.stream, attn::attn_quant_kernel<U, D, true><<<grid, 256, 0, c.stream>>>(a));
+      } else {
+        LAWCAT_LAUNCH("attn_dequantize", c.stream, attn::attn_quant_kernel<U, D, false><<<grid, 256, 0, c.stream>>>(a));
+      }
+      LAWCAT_CHECK_LAUNCH();
+      return LAWCAT_OK;
+    };
+    return c.dtype == LAWCAT_F32 ? go(float{}) : go(bf16{});
+  });
+}
+
+}  // namespace lawcat
