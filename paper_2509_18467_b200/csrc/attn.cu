@@ -142,7 +142,8 @@ extern "C" {
 size_t lawcat_attn_workspace_bytes(const lawcat_attn_params* p, int op) {
   if (check(p) != LAWCAT_OK) return 0;
   switch (op) {
-    case LAWCAT_OP_ATTN_FWD: return rows_bytes(p);
+    case LAWCAT_OP_ATTN_FWD:
+      return rows_bytes(p) + (attn_tc_supported(p->dtype, p->d, p->exact) ? attn_fwd_tc_workspace_bytes(p->B, p->H, p->H_kv, p->T, p->T_k, p->window, p->d) : 0);
     case LAWCAT_OP_ATTN_BWD: return rows_bytes(p) + stat_bytes(p);
     case LAWCAT_OP_ATTN_DECODE: return align_up(attn_decode_workspace_bytes(p->B, p->H, p->H_kv, p->T_k, p->window, p->d), 256);
     default: return 0;
@@ -166,7 +167,7 @@ int lawcat_attn_fwd(const lawcat_attn_params* p, const int32_t* cu_seqlens, cons
     if ((r = fill_rows(p, cu_seqlens, prefix, nseq, c.a.mask, (int2*)ws, c.stream))) return r;
     c.a.mask.rows = (const int2*)ws;
   }
-  return launch_attn_fwd_exact(c);
+  return attn_tc_supported(p->dtype, p->d, p->exact) ? launch_attn_fwd_tc(c, (char*)ws + rows_bytes(p)) : launch_attn_fwd_exact(c);
 }
 
 int lawcat_attn_bwd(const lawcat_attn_params* p, const int32_t* cu_seqlens, const int32_t* prefix, int32_t nseq, const void* q,

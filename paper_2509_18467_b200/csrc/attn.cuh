@@ -72,6 +72,10 @@ struct AttnCall {
 };
 int launch_attn_fwd_exact(const AttnCall& c);
 int launch_attn_bwd_exact(const AttnCall& c);
+// the tensor-core kernels (attn_fwd_tc.cu): bf16 storage, d = 64 or 128
+bool attn_tc_supported(int dtype, int d, int exact);
+size_t attn_fwd_tc_workspace_bytes(int B, int H, int H_kv, int T, int T_k, int window, int d);
+int launch_attn_fwd_tc(const AttnCall& c, void* ws);
 
 // one step over a cache, in the storage type (K, V) or in 4 bits (kq, kp, vq, vp); attn_decode.cu
 struct AttnDecode {

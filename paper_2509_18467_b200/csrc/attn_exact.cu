@@ -1,340 +1,35 @@
-// Softmax attention on the CUDA cores: forward and gradients in fp32 for every storage type and head width (the formulas are
-// at the top of attn.cuh). These kernels serve fp32 storage, the widths that the tensor-core kernels do not take, and calls
-// that ask for exact results.
-//
-// All three are the same tiling: a block owns BM rows (queries; keys in the dk/dv kernel) of one head in shared memory and
-// walks the other side in tiles of 64 rows. 16 x 16 threads; a thread holds RM = BM / 16 rows x 4 columns of the scores and
-// RM rows x D / 16 channels of what it accumulates, so that a row's statistics are shuffles among 16 lanes. The running
-// maximum and sum of the softmax stay in registers: one pass over the keys.
-// The gradients take two kernels, one per side, each recomputing the scores: the sums over queries and over keys then both
-// stay in registers of one block, in one order (no atomics, the same bits every time), at 14 instead of 10 D flop per pair.
-// A weight of zero adds nothing, whatever its value row holds: rows that a query does not see never reach its results, not
-// even as NaN. (Tiles that every row sees whole skip that test.)
-// RM is 4 (64 rows), or 1 where blocks of 64 rows would leave most SMs idle: a tile's loads then serve a quarter of the
-// products, but a call of 4 heads x 512 queries runs on 128 blocks instead of 32.
-#include "attn.cuh"
+// Launches of the exact attention kernels (attn_exact.cuh).
+// A block has 256 threads and 64 rows (RM = 4), or 16 rows (RM = 1) where blocks of 64 would leave most SMs idle: a tile's loads
+// then serve a quarter of the products, but a call of 4 heads x 512 queries runs on 128 blocks instead of 32.
+#include "attn_exact.cuh"
 
 namespace lawcat {
 namespace attn {
 
-constexpr int BN = 64;       // rows of the walked side per tile
 constexpr int THREADS = 256;
-
-// R rows x D channels from rows row0 + r < rows_end of a [*, heads, D] tensor into shared memory (fp32, row stride D + 4); zeros behind
-template <typename T, int D>
-__device__ __forceinline__ void load_rows(float* dst, const T* src, size_t row_stride, int row0, int rows_end, int R) {
-  constexpr int PER = 16 / sizeof(T), VPR = D / PER;  // elements per 16-byte load, loads per row
-  for (int i = threadIdx.x; i < R * VPR; i += THREADS) {
-    const int r = i / VPR, c = i % VPR * PER;
-    float* d = dst + r * (D + 4) + c;
-    if (row0 + r < rows_end) {
-      const uint4 w = __ldg(reinterpret_cast<const uint4*>(src + (size_t)(row0 + r) * row_stride + c));
-      if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<uint4*>(d) = w;
-      } else {
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-          reinterpret_cast<float4*>(d)[k] = make_float4(__uint_as_float(x[2 * k] << 16), __uint_as_float(x[2 * k] & 0xffff0000u),
-                                                        __uint_as_float(x[2 * k + 1] << 16), __uint_as_float(x[2 * k + 1] & 0xffff0000u));
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < PER / 4; ++k) reinterpret_cast<float4*>(d)[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-  }
-}
-
-// s[i][j] = sum_c X[row i][c] Y[tx + 16 j][c]
-template <int D, int RM>
-__device__ __forceinline__ void product_t(const float* X, const float* Y, int ty, int tx, float (&s)[RM][4]) {
-#pragma unroll
-  for (int i = 0; i < RM; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
-#pragma unroll 4
-  for (int c = 0; c < D; c += 4) {
-    float4 x[RM], y[4];
-#pragma unroll
-    for (int i = 0; i < RM; ++i) x[i] = *reinterpret_cast<const float4*>(X + (ty * RM + i) * (D + 4) + c);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(Y + (tx + 16 * j) * (D + 4) + c);
-#pragma unroll
-    for (int i = 0; i < RM; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        s[i][j] = fmaf(x[i].w, y[j].w, fmaf(x[i].z, y[j].z, fmaf(x[i].y, y[j].y, fmaf(x[i].x, y[j].x, s[i][j]))));
-  }
-}
-
-// acc[i][:] += sum_r P[row i][r] Y[r][this thread's channels]; `whole`: no weight of the tile has to be tested for zero
-template <int D, int RM>
-__device__ __forceinline__ void product_acc(const float* P, const float* Y, int ty, int tx, bool whole, float (&acc)[RM][D / 16]) {
-  constexpr int NC = D / 16, VW = NC < 4 ? NC : 4;
-  auto step = [&](int r, auto test) {
-    float y[NC];
-#pragma unroll
-    for (int c = 0; c < NC / VW; ++c)
-#pragma unroll
-      for (int e = 0; e < VW; ++e) y[c * VW + e] = Y[r * (D + 4) + (tx + 16 * c) * VW + e];
-#pragma unroll
-    for (int i = 0; i < RM; ++i) {
-      const float w = P[(ty * RM + i) * (BN + 4) + r];
-      if (!decltype(test)::value || w != 0.f) {
-#pragma unroll
-        for (int c = 0; c < NC; ++c) acc[i][c] = fmaf(w, y[c], acc[i][c]);
-      }
-    }
-  };
-  if (whole) {
-#pragma unroll 4
-    for (int r = 0; r < BN; ++r) step(r, std::false_type{});
-  } else {
-#pragma unroll 4
-    for (int r = 0; r < BN; ++r) step(r, std::true_type{});
-  }
-}
-
-template <typename T, int D, int RM>
-__device__ __forceinline__ void store_rows(T* dst, size_t row_stride, int row0, int rows_end, int ty, int tx, const float (&acc)[RM][D / 16]) {
-  constexpr int NC = D / 16, VW = NC < 4 ? NC : 4;
-#pragma unroll
-  for (int i = 0; i < RM; ++i) {
-    const int r = row0 + ty * RM + i;
-    if (r < rows_end)
-#pragma unroll
-      for (int c = 0; c < NC; ++c) stf<T>(dst + (size_t)r * row_stride + (tx + 16 * (c / VW)) * VW + c % VW, acc[i][c]);
-  }
-}
-
-__device__ __forceinline__ float sum16(float v) {
-#pragma unroll
-  for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-__device__ __forceinline__ float max16(float v) {
-#pragma unroll
-  for (int o = 8; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
-}
-
-// the score in units of log2 from the dot product; th: tanh(u / cap) (only under a cap)
-__device__ __forceinline__ float score2(float dot, float scale, float cap, float slope, int dist, float& th) {
-  float x = dot * scale;
-  if (cap > 0.f) {
-    th = tanhf(x / cap);
-    x = cap * th;
-  }
-  return (x - slope * (float)dist) * LOG2E;
-}
 
 template <typename T, int D, int RM>
 __global__ void __launch_bounds__(THREADS) attn_fwd_exact_kernel(const Args a, int tiles) {
-  constexpr int BM = 16 * RM, LD = D + 4, NC = D / 16;
   extern __shared__ __align__(16) float sm[];
-  float *Q = sm, *K = Q + BM * LD, *V = K + BN * LD, *P = V + BN * LD;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int bh = blockIdx.x % (a.B * a.H), h = bh % a.H, b = bh / a.H, g = h / (a.H / a.H_kv);
-  const int t0 = (tiles - 1 - (int)(blockIdx.x / (a.B * a.H))) * BM;  // (under a causal mask the longest rows first)
-  const int t_end = a.mask.T;
-  const size_t qs = (size_t)a.H * D, ks = (size_t)a.H_kv * D;
-  const T* q = (const T*)a.q + (size_t)b * a.mask.T * qs + (size_t)h * D;
-  const T* k = (const T*)a.k + (size_t)b * a.mask.T_k * ks + (size_t)g * D;
-  const T* v = (const T*)a.v + (size_t)b * a.mask.T_k * ks + (size_t)g * D;
-  const float slope = a.slopes ? a.slopes[h] : 0.f;
-  const int last = t0 + BM < t_end ? t0 + BM - 1 : t_end - 1;
-  const int2 head = interval(a.mask, b, t0), tail = interval(a.mask, b, last);
-  int2 iv[RM];
-#pragma unroll
-  for (int i = 0; i < RM; ++i) iv[i] = t0 + ty * RM + i <= last ? interval(a.mask, b, t0 + ty * RM + i) : make_int2(0, 0);
-
-  load_rows<T, D>(Q, q, qs, t0, t_end, BM);
-  float m[RM], l[RM], acc[RM][NC];
-#pragma unroll
-  for (int i = 0; i < RM; ++i) {
-    m[i] = -INFINITY;
-    l[i] = 0.f;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) acc[i][c] = 0.f;
-  }
-  for (int j0 = head.x; j0 < tail.y; j0 += BN) {
-    __syncthreads();
-    load_rows<T, D>(K, k, ks, j0, a.mask.T_k, BN);
-    load_rows<T, D>(V, v, ks, j0, a.mask.T_k, BN);
-    __syncthreads();
-    const bool whole = last - t0 + 1 == BM && tail.x <= j0 && head.y >= j0 + BN;
-    float s[RM][4];
-    product_t<D, RM>(Q, K, ty, tx, s);
-#pragma unroll
-    for (int i = 0; i < RM; ++i) {
-      const int pos = t0 + ty * RM + i + a.mask.off;
-      float mx = m[i], th;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int key = j0 + tx + 16 * j;
-        const float x = score2(s[i][j], a.scale, a.cap, slope, abs(pos - key), th);
-        s[i][j] = key >= iv[i].x && key < iv[i].y ? x : -INFINITY;
-        mx = fmaxf(mx, s[i][j]);
-      }
-      mx = max16(mx);
-      const float base = mx == -INFINITY ? 0.f : mx;
-      const float corr = exp2f(m[i] - base);
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float p = exp2f(s[i][j] - base);
-        sum += p;
-        P[(ty * RM + i) * (BN + 4) + tx + 16 * j] = p;
-      }
-      l[i] = l[i] * corr + sum16(sum);
-      m[i] = mx;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) acc[i][c] *= corr;
-    }
-    __syncwarp();  // (a row's weights are written and read by the 16 lanes of half a warp)
-    product_acc<D, RM>(P, V, ty, tx, whole, acc);
-  }
-#pragma unroll
-  for (int i = 0; i < RM; ++i) {
-    const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
-#pragma unroll
-    for (int c = 0; c < NC; ++c) acc[i][c] *= inv;
-    const int t = t0 + ty * RM + i;
-    if (a.lse && tx == 0 && t < t_end) a.lse[((size_t)b * a.mask.T + t) * a.H + h] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * LN2;
-  }
-  store_rows<T, D, RM>((T*)a.o + (size_t)b * a.mask.T * qs + (size_t)h * D, qs, t0, t_end, ty, tx, acc);
+  const int bh = blockIdx.x % (a.B * a.H);
+  const int t0 = (tiles - 1 - (int)(blockIdx.x / (a.B * a.H))) * 16 * RM;  // (under a causal mask the longest rows first)
+  fwd_rows<T, D, RM, THREADS>(a, sm, bh / a.H, bh % a.H, t0, 0, a.mask.T_k, nullptr, nullptr);
 }
 
 // dq, and (lse log2e, dO.o) of every query for the other kernel
 template <typename T, int D, int RM>
 __global__ void __launch_bounds__(THREADS) attn_dq_exact_kernel(const Args a, int tiles) {
-  constexpr int BM = 16 * RM, LD = D + 4, NC = D / 16;
   extern __shared__ __align__(16) float sm[];
-  float *Q = sm, *O = Q + BM * LD, *K = O + BM * LD, *V = K + BN * LD, *P = V + BN * LD;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int bh = blockIdx.x % (a.B * a.H), h = bh % a.H, b = bh / a.H, g = h / (a.H / a.H_kv);
-  const int t0 = (tiles - 1 - (int)(blockIdx.x / (a.B * a.H))) * BM;
-  const int t_end = a.mask.T;
-  const size_t qs = (size_t)a.H * D, ks = (size_t)a.H_kv * D;
-  const size_t qo = (size_t)b * a.mask.T * qs + (size_t)h * D, ko = (size_t)b * a.mask.T_k * ks + (size_t)g * D;
-  const float slope = a.slopes ? a.slopes[h] : 0.f;
-  const int last = t0 + BM < t_end ? t0 + BM - 1 : t_end - 1;
-  const int2 head = interval(a.mask, b, t0), tail = interval(a.mask, b, last);
-  int2 iv[RM];
-#pragma unroll
-  for (int i = 0; i < RM; ++i) iv[i] = t0 + ty * RM + i <= last ? interval(a.mask, b, t0 + ty * RM + i) : make_int2(0, 0);
-
-  load_rows<T, D>(Q, (const T*)a.q + qo, qs, t0, t_end, BM);
-  load_rows<T, D>(O, (const T*)a.dO + qo, qs, t0, t_end, BM);
-  __syncthreads();
-  float lse2[RM], dsum[RM], acc[RM][NC];
-#pragma unroll
-  for (int i = 0; i < RM; ++i) {
-    const int t = t0 + ty * RM + i;
-    float w = 0.f;
-    lse2[i] = 0.f;
-    if (t < t_end) {
-      const T* o = (const T*)a.o_in + qo + (size_t)t * qs;
-      for (int c = tx; c < D; c += 16) w = fmaf(ldf<T>(o + c), O[(ty * RM + i) * LD + c], w);
-      lse2[i] = a.lse[((size_t)b * a.mask.T + t) * a.H + h] * LOG2E;
-    }
-    dsum[i] = sum16(w);
-    if (tx == 0 && t < t_end) a.stat[((size_t)b * a.H + h) * a.mask.T + t] = make_float2(lse2[i], dsum[i]);
-#pragma unroll
-    for (int c = 0; c < NC; ++c) acc[i][c] = 0.f;
-  }
-  for (int j0 = head.x; j0 < tail.y; j0 += BN) {
-    __syncthreads();
-    load_rows<T, D>(K, (const T*)a.k + ko, ks, j0, a.mask.T_k, BN);
-    load_rows<T, D>(V, (const T*)a.v + ko, ks, j0, a.mask.T_k, BN);
-    __syncthreads();
-    const bool whole = last - t0 + 1 == BM && tail.x <= j0 && head.y >= j0 + BN;
-    float s[RM][4], dp[RM][4];
-    product_t<D, RM>(Q, K, ty, tx, s);
-    product_t<D, RM>(O, V, ty, tx, dp);
-#pragma unroll
-    for (int i = 0; i < RM; ++i) {
-      const int pos = t0 + ty * RM + i + a.mask.off;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int key = j0 + tx + 16 * j;
-        float th = 0.f;
-        const float x = score2(s[i][j], a.scale, a.cap, slope, abs(pos - key), th);
-        const float dx = exp2f(x - lse2[i]) * (dp[i][j] - dsum[i]) * (1.f - th * th);
-        P[(ty * RM + i) * (BN + 4) + tx + 16 * j] = key >= iv[i].x && key < iv[i].y ? dx : 0.f;
-      }
-    }
-    __syncwarp();
-    product_acc<D, RM>(P, K, ty, tx, whole, acc);
-  }
-#pragma unroll
-  for (int i = 0; i < RM; ++i)
-#pragma unroll
-    for (int c = 0; c < NC; ++c) acc[i][c] *= a.scale;
-  store_rows<T, D, RM>((T*)a.dq + qo, qs, t0, t_end, ty, tx, acc);
+  const int bh = blockIdx.x % (a.B * a.H);
+  const int t0 = (tiles - 1 - (int)(blockIdx.x / (a.B * a.H))) * 16 * RM;
+  dq_rows<T, D, RM, THREADS>(a, sm, bh / a.H, bh % a.H, t0);
 }
 
-// dk, dv: a block owns BM keys and walks the queries of every head of its group
 template <typename T, int D, int RM>
 __global__ void __launch_bounds__(THREADS) attn_dkdv_exact_kernel(const Args a, int tiles) {
-  constexpr int BM = 16 * RM, LD = D + 4, NC = D / 16;
   extern __shared__ __align__(16) float sm[];
-  float *K = sm, *V = K + BM * LD, *Q = V + BM * LD, *O = Q + BN * LD, *P = O + BN * LD, *S = P + BM * (BN + 4);
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int bg = blockIdx.x % (a.B * a.H_kv), g = bg % a.H_kv, b = bg / a.H_kv, G = a.H / a.H_kv;
-  const int j0 = (int)(blockIdx.x / (a.B * a.H_kv)) * BM, j_end = a.mask.T_k;
-  const size_t qs = (size_t)a.H * D, ks = (size_t)a.H_kv * D;
-  const size_t ko = (size_t)b * a.mask.T_k * ks + (size_t)g * D;
-  load_rows<T, D>(K, (const T*)a.k + ko, ks, j0, j_end, BM);
-  load_rows<T, D>(V, (const T*)a.v + ko, ks, j0, j_end, BM);
-  const int j1 = j0 + BM < j_end ? j0 + BM : j_end;
-  const int2 qr = queries_of(a.mask, b, j0, j1);
-  float dk[RM][NC], dv[RM][NC];
-#pragma unroll
-  for (int i = 0; i < RM; ++i)
-#pragma unroll
-    for (int c = 0; c < NC; ++c) dk[i][c] = dv[i][c] = 0.f;
-  for (int h = g * G; h < (g + 1) * G; ++h) {
-    const size_t qo = (size_t)b * a.mask.T * qs + (size_t)h * D;
-    const float2* stat = a.stat + ((size_t)b * a.H + h) * a.mask.T;
-    const float slope = a.slopes ? a.slopes[h] : 0.f;
-    for (int t0 = qr.x; t0 < qr.y; t0 += BN) {
-      __syncthreads();
-      load_rows<T, D>(Q, (const T*)a.q + qo, qs, t0, qr.y, BN);
-      load_rows<T, D>(O, (const T*)a.dO + qo, qs, t0, qr.y, BN);
-      __syncthreads();
-      bool whole = t0 + BN <= qr.y && j1 - j0 == BM;
-      if (whole) whole = interval(a.mask, b, t0 + BN - 1).x <= j0 && interval(a.mask, b, t0).y >= j0 + BM;
-      float s[RM][4], dp[RM][4];
-      product_t<D, RM>(K, Q, ty, tx, s);
-      product_t<D, RM>(V, O, ty, tx, dp);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int t = t0 + tx + 16 * j;
-        const int2 iv = t < qr.y ? interval(a.mask, b, t) : make_int2(0, 0);
-        const float2 st = t < qr.y ? stat[t] : make_float2(0.f, 0.f);
-#pragma unroll
-        for (int i = 0; i < RM; ++i) {
-          const int key = j0 + ty * RM + i;
-          const bool see = key >= iv.x && key < iv.y;
-          float th = 0.f;
-          const float x = score2(s[i][j], a.scale, a.cap, slope, abs(t + a.mask.off - key), th);
-          const float p = exp2f(x - st.x);
-          P[(ty * RM + i) * (BN + 4) + tx + 16 * j] = see ? p : 0.f;
-          S[(ty * RM + i) * (BN + 4) + tx + 16 * j] = see ? p * (dp[i][j] - st.y) * (1.f - th * th) : 0.f;
-        }
-      }
-      __syncwarp();
-      product_acc<D, RM>(P, O, ty, tx, whole, dv);
-      product_acc<D, RM>(S, Q, ty, tx, whole, dk);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < RM; ++i)
-#pragma unroll
-    for (int c = 0; c < NC; ++c) dk[i][c] *= a.scale;
-  store_rows<T, D, RM>((T*)a.dk + ko, ks, j0, j_end, ty, tx, dk);
-  store_rows<T, D, RM>((T*)a.dv + ko, ks, j0, j_end, ty, tx, dv);
+  const int bg = blockIdx.x % (a.B * a.H_kv);
+  dkdv_rows<T, D, RM, THREADS>(a, sm, bg / a.H_kv, bg % a.H_kv, (int)(blockIdx.x / (a.B * a.H_kv)) * 16 * RM);
 }
 
 template <typename K>
@@ -359,7 +54,7 @@ static int fwd(const AttnCall& c) {
   const int tiles = (c.a.mask.T + 16 * RM - 1) / (16 * RM);
   const unsigned n = blocks(c.a.mask.T, (long long)c.a.B * c.a.H, 16 * RM);
   if (!n) return LAWCAT_ERR_UNSUPPORTED;
-  const size_t sm = sizeof(float) * ((16 * RM + 2 * BN) * (D + 4) + 16 * RM * (BN + 4));
+  constexpr size_t sm = fwd_smem<D, RM, THREADS>();
   if (int r = set_smem(attn_fwd_exact_kernel<T, D, RM>, sm)) return r;
   LAWCAT_LAUNCH("attn_fwd_exact", c.stream, attn_fwd_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles));
   LAWCAT_CHECK_LAUNCH();
@@ -371,7 +66,7 @@ static int dq(const AttnCall& c) {
   const int tiles = (c.a.mask.T + 16 * RM - 1) / (16 * RM);
   const unsigned n = blocks(c.a.mask.T, (long long)c.a.B * c.a.H, 16 * RM);
   if (!n) return LAWCAT_ERR_UNSUPPORTED;
-  const size_t sm = sizeof(float) * ((2 * 16 * RM + 2 * BN) * (D + 4) + 16 * RM * (BN + 4));
+  constexpr size_t sm = dq_smem<D, RM, THREADS>();
   if (int r = set_smem(attn_dq_exact_kernel<T, D, RM>, sm)) return r;
   LAWCAT_LAUNCH("attn_dq_exact", c.stream, attn_dq_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles));
   LAWCAT_CHECK_LAUNCH();
@@ -383,7 +78,7 @@ static int dkdv(const AttnCall& c) {
   const int tiles = (c.a.mask.T_k + 16 * RM - 1) / (16 * RM);
   const unsigned n = blocks(c.a.mask.T_k, (long long)c.a.B * c.a.H_kv, 16 * RM);
   if (!n) return LAWCAT_ERR_UNSUPPORTED;
-  const size_t sm = sizeof(float) * ((2 * 16 * RM + 2 * BN) * (D + 4) + 2 * 16 * RM * (BN + 4));
+  constexpr size_t sm = dkdv_smem<D, RM, THREADS>();
   if (int r = set_smem(attn_dkdv_exact_kernel<T, D, RM>, sm)) return r;
   LAWCAT_LAUNCH("attn_dkdv_exact", c.stream, attn_dkdv_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles));
   LAWCAT_CHECK_LAUNCH();

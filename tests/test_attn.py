@@ -130,23 +130,30 @@ def test_the_same_call_gives_the_same_bits(dtype, exact):
 @pytest.mark.parametrize("T", [70, 300])
 def test_rows_that_are_not_seen_stay_out(T, bad, dtype, exact):
     """A NaN or an infinity in keys and values that only later queries see, and in another document's rows, changes no bit of
-    the other queries' results."""
+    the other queries' results. (The tensor-core kernels compute the rows of a block that came out not finite again on the CUDA
+    cores, where the weights are not rounded to bf16: those stay within the tolerance instead.)"""
     d, H, H_kv, at = 64, 4, 2, T - 13
     q, k, v = draw((1, T, H, d), 1, dtype), draw((1, T, H_kv, d), 2, dtype), draw((1, T, H_kv, d), 3, dtype)
     dO = draw((1, T, H, d), 4, dtype)
+    coarse, out = U16 if dtype == "bf16" and not exact else 0.0, U16 if dtype == "bf16" else U32
     for kw in (dict(), dict(cu_seqlens=[0, at, T])):
         p = api.attn_params(1, T, H, H_kv, d, dtype=dtype, exact=exact)
         clean = api.lawcat_attn_fwd(p, q, k, v, **kw)
-        gc = api.lawcat_attn_bwd(p, q, k, v, clean["o"], clean["lse"], dO, **kw)
+        clean.update(api.lawcat_attn_bwd(p, q, k, v, clean["o"], clean["lse"], dO, **kw))
         k2, v2, q2, dO2 = k.clone(), v.clone(), q.clone(), dO.clone()
         for x in (k2, v2, q2, dO2):
             x[:, at:, :, 5] = bad
         r = api.lawcat_attn_fwd(p, q2, k2, v2, **kw)
-        assert torch.equal(r["o"][:, :at], clean["o"][:, :at]) and torch.equal(r["lse"][:, :at], clean["lse"][:, :at])
-        g = api.lawcat_attn_bwd(p, q2, k2, v2, r["o"], r["lse"], dO2, **kw)
-        assert torch.equal(g["dq"][:, :at], gc["dq"][:, :at])
-        if "cu_seqlens" in kw:
-            assert torch.equal(g["dk"][:, :at], gc["dk"][:, :at]) and torch.equal(g["dv"][:, :at], gc["dv"][:, :at])
+        r.update(api.lawcat_attn_bwd(p, q2, k2, v2, r["o"], r["lse"], dO2, **kw))
+        names = ["o", "lse", "dq"] + (["dk", "dv"] if "cu_seqlens" in kw else [])
+        if not coarse:
+            for n in names:
+                assert torch.equal(r[n][:, :at], clean[n][:, :at]), n
+            continue
+        ref = attention(q, k, v, visible(T, T, 1, 0, kw.get("cu_seqlens")), 0.125, 0.0, None, dO, r["o"].nan_to_num(0, 0, 0))
+        err = dict(ref["grad_err"](coarse, out), o=ref["o_sum"] + coarse * ref["o_mag"], lse=ref["lse_err"])
+        for n in names:
+            check(r[n][:, :at], ref[n][:, :at], err[n][:, :at], U32 if n == "lse" else out, n)
 
 
 @pytest.mark.gpu
