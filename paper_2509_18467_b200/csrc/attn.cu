@@ -49,8 +49,8 @@ struct Sequences {
   int start[TABLE + 1], prefix[TABLE];
 };
 
-// rows[b][t] = the interval of keys that query t sees
-__global__ void attn_rows_kernel(const __grid_constant__ Sequences s, const attn::Mask m, int2* rows) {
+// rows[b][t] = the keys that query t sees, and keys[b][j] = the queries that see key j
+__global__ void attn_rows_kernel(const __grid_constant__ Sequences s, const attn::Mask m, int2* rows, int2* keys) {
   const int i = blockIdx.x * blockDim.x + threadIdx.x;
   if (s.docs) {  // one packed batch: the launch's sequences cover tokens [start[0], start[n])
     const int t = s.start[0] + i;
@@ -66,16 +66,23 @@ __global__ void attn_rows_kernel(const __grid_constant__ Sequences s, const attn
     int2 iv = attn::interval(md, 0, t - s0);
     if (s.prefix[lo] > iv.y) iv.y = s.prefix[lo];
     rows[t] = make_int2(iv.x + s0, iv.y + s0);
+    if (keys) {
+      iv = attn::key_interval(md, 0, t - s0, s.prefix[lo]);
+      keys[t] = make_int2(iv.x + s0, iv.y + s0);
+    }
   } else {
     const int b = blockIdx.y;
-    if (i >= m.T) return;
-    int2 iv = attn::interval(m, 0, i);
-    if (s.prefix[b] > iv.y) iv.y = s.prefix[b];
-    rows[(size_t)(s.first_b + b) * m.T + i] = iv;
+    if (i < m.T) {
+      int2 iv = attn::interval(m, 0, i);
+      if (s.prefix[b] > iv.y) iv.y = s.prefix[b];
+      rows[(size_t)(s.first_b + b) * m.T + i] = iv;
+    }
+    if (keys && i < m.T_k) keys[(size_t)(s.first_b + b) * m.T_k + i] = attn::key_interval(m, 0, i, s.prefix[b]);
   }
 }
 
-int fill_rows(const lawcat_attn_params* p, const int32_t* cu, const int32_t* prefix, int nseq, attn::Mask m, int2* rows, cudaStream_t stream) {
+int fill_rows(const lawcat_attn_params* p, const int32_t* cu, const int32_t* prefix, int nseq, attn::Mask& m, int2* rows, int2* keys,
+              cudaStream_t stream) {
   Sequences s;
   s.docs = cu != nullptr;
   for (int f = 0; f < nseq; f += TABLE) {
@@ -86,17 +93,21 @@ int fill_rows(const lawcat_attn_params* p, const int32_t* cu, const int32_t* pre
       s.prefix[i] = prefix ? prefix[f + i] : 0;
     }
     s.start[s.n] = cu ? cu[f + s.n] : 0;
-    const int tokens = cu ? s.start[s.n] - s.start[0] : m.T;
+    const int tokens = cu ? s.start[s.n] - s.start[0] : keys && m.T_k > m.T ? m.T_k : m.T;
     if (!tokens) continue;
     const dim3 grid((unsigned)((tokens + 255) / 256), cu ? 1u : (unsigned)s.n);
-    LAWCAT_LAUNCH("attn_rows", stream, attn_rows_kernel<<<grid, 256, 0, stream>>>(s, m, rows));
+    LAWCAT_LAUNCH("attn_rows", stream, attn_rows_kernel<<<grid, 256, 0, stream>>>(s, m, rows, keys));
     LAWCAT_CHECK_LAUNCH();
   }
+  m.rows = rows;
+  m.keys = keys;
   return LAWCAT_OK;
 }
 
 size_t rows_bytes(const lawcat_attn_params* p) { return align_up(sizeof(int2) * (size_t)p->B * p->T, 256); }
-size_t stat_bytes(const lawcat_attn_params* p) { return align_up(sizeof(float2) * (size_t)p->B * p->T * p->H, 256); }
+size_t keys_bytes(const lawcat_attn_params* p) { return align_up(sizeof(int2) * (size_t)p->B * p->T_k, 256); }
+int stat_stride(const lawcat_attn_params* p) { return (p->T + 63) / 64 * 64; }
+size_t stat_bytes(const lawcat_attn_params* p) { return align_up(sizeof(float2) * (size_t)p->B * stat_stride(p) * p->H, 256); }
 
 AttnCall make_call(const lawcat_attn_params* p, const float* slopes, void* stream, int* dev_status) {
   AttnCall c{};
@@ -104,7 +115,9 @@ AttnCall make_call(const lawcat_attn_params* p, const float* slopes, void* strea
   c.a.scale = p->scale; c.a.cap = p->cap;
   c.a.slopes = slopes;
   c.a.dev_status = dev_status;
-  c.a.mask = attn::Mask{p->T, p->T_k, p->T_k - p->T, p->causal, p->window, nullptr};
+  // (a window that holds every distance is none: positions plus or minus a window then stay inside 32 bits)
+  const int window = p->window > (p->T > p->T_k ? p->T : p->T_k) ? 0 : p->window;
+  c.a.mask = attn::Mask{p->T, p->T_k, p->T_k - p->T, p->causal, window, nullptr, nullptr};
   c.d = p->d; c.dtype = p->dtype; c.exact = p->exact;
   c.stream = (cudaStream_t)stream;
   return c;
@@ -144,7 +157,7 @@ size_t lawcat_attn_workspace_bytes(const lawcat_attn_params* p, int op) {
   switch (op) {
     case LAWCAT_OP_ATTN_FWD:
       return rows_bytes(p) + (attn_tc_supported(p->dtype, p->d, p->exact) ? attn_fwd_tc_workspace_bytes(p->B, p->H, p->H_kv, p->T, p->T_k, p->window, p->d) : 0);
-    case LAWCAT_OP_ATTN_BWD: return rows_bytes(p) + stat_bytes(p);
+    case LAWCAT_OP_ATTN_BWD: return rows_bytes(p) + keys_bytes(p) + stat_bytes(p);
     case LAWCAT_OP_ATTN_DECODE: return align_up(attn_decode_workspace_bytes(p->B, p->H, p->H_kv, p->T_k, p->window, p->d), 256);
     default: return 0;
   }
@@ -164,8 +177,7 @@ int lawcat_attn_fwd(const lawcat_attn_params* p, const int32_t* cu_seqlens, cons
   AttnCall c = make_call(p, slopes, stream, dev_status);
   c.a.q = q; c.a.k = k; c.a.v = v; c.a.o = o; c.a.lse = lse;
   if (cu_seqlens || prefix) {
-    if ((r = fill_rows(p, cu_seqlens, prefix, nseq, c.a.mask, (int2*)ws, c.stream))) return r;
-    c.a.mask.rows = (const int2*)ws;
+    if ((r = fill_rows(p, cu_seqlens, prefix, nseq, c.a.mask, (int2*)ws, nullptr, c.stream))) return r;
   }
   return attn_tc_supported(p->dtype, p->d, p->exact) ? launch_attn_fwd_tc(c, (char*)ws + rows_bytes(p)) : launch_attn_fwd_exact(c);
 }
@@ -187,12 +199,13 @@ int lawcat_attn_bwd(const lawcat_attn_params* p, const int32_t* cu_seqlens, cons
   c.a.q = q; c.a.k = k; c.a.v = v; c.a.o_in = o; c.a.dO = dO;
   c.a.lse = const_cast<float*>(lse);
   c.a.dq = dq; c.a.dk = dk; c.a.dv = dv;
-  c.a.stat = (float2*)((char*)ws + rows_bytes(p));
+  int2* const keys = (int2*)((char*)ws + rows_bytes(p));
+  c.a.stat = (float2*)((char*)keys + keys_bytes(p));
+  c.a.stat_stride = stat_stride(p);
   if (cu_seqlens || prefix) {
-    if ((r = fill_rows(p, cu_seqlens, prefix, nseq, c.a.mask, (int2*)ws, c.stream))) return r;
-    c.a.mask.rows = (const int2*)ws;
+    if ((r = fill_rows(p, cu_seqlens, prefix, nseq, c.a.mask, (int2*)ws, keys, c.stream))) return r;
   }
-  return launch_attn_bwd_exact(c);
+  return attn_tc_supported(p->dtype, p->d, p->exact) ? launch_attn_bwd_tc(c) : launch_attn_bwd_exact(c);
 }
 
 int lawcat_attn_decode(const lawcat_attn_params* p, const void* q_t, const void* k_t, const void* v_t, void* K, void* V, const int32_t* pos,

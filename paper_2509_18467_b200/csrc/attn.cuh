@@ -16,6 +16,7 @@ struct Mask {
   int off;           // position of query t: t + off  (T_k - T)
   int causal, window;
   const int2* rows;  // [B, T] (lo, hi) where documents or prefixes are given, else null
+  const int2* keys;  // [B, T_k] the other way round, for the gradients (see key_interval)
 };
 
 __host__ __device__ __forceinline__ int2 interval(const Mask& m, int b, int t) {
@@ -30,6 +31,23 @@ __host__ __device__ __forceinline__ int2 interval(const Mask& m, int b, int t) {
     if (pos < m.T_k - m.window) hi = hi < pos + m.window ? hi : pos + m.window;
   }
   return make_int2(lo, hi > lo ? hi : lo);
+}
+
+// The other way round: the queries that see key j, one interval as well since both ends of the queries' intervals grow with the
+// query. prefix: the keys below it are seen by every query.
+__host__ __device__ __forceinline__ int2 key_interval(const Mask& m, int b, int j, int prefix = 0) {
+#ifdef __CUDA_ARCH__
+  if (m.keys) return __ldg(m.keys + (size_t)b * m.T_k + j);
+#endif
+  int first = 0, end = m.T;  // (query t has position t + off)
+  if (m.causal) {
+    if (j >= prefix) first = j - m.off;
+  } else if (m.window) {
+    first = j - m.off - m.window + 1;
+  }
+  if (m.window && j - m.off < m.T - m.window) end = j - m.off + m.window;
+  first = first < 0 ? 0 : first > m.T ? m.T : first;
+  return make_int2(first, end > first ? end : first);
 }
 
 // Queries that may see one of the keys [j0, j1): the first with hi > j0 up to the first with lo >= j1 (both ends of the
@@ -55,7 +73,8 @@ struct Args {
   void *o, *dq, *dk, *dv;
   float* lse;           // [B, T, H] natural logarithm (forward: output; backward: input)
   const float* slopes;  // [H] or null
-  float2* stat;         // backward: [B, H, T] (lse log2e, dO.o)
+  float2* stat;         // backward: [B, H, stat_stride] (lse log2e, dO.o)
+  int stat_stride;      // T rounded up to 64
   Mask mask;
   int B, H, H_kv;
   float scale, cap;
@@ -76,6 +95,7 @@ int launch_attn_bwd_exact(const AttnCall& c);
 bool attn_tc_supported(int dtype, int d, int exact);
 size_t attn_fwd_tc_workspace_bytes(int B, int H, int H_kv, int T, int T_k, int window, int d);
 int launch_attn_fwd_tc(const AttnCall& c, void* ws);
+int launch_attn_bwd_tc(const AttnCall& c);  // attn_bwd_tc.cu
 
 // one step over a cache, in the storage type (K, V) or in 4 bits (kq, kp, vq, vp); attn_decode.cu
 struct AttnDecode {

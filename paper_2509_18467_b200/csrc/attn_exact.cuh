@@ -259,7 +259,7 @@ __device__ __forceinline__ void dq_rows(const Args& a, float* sm, int b, int h, 
       lse2[i] = a.lse[((size_t)b * a.mask.T + t) * a.H + h] * LOG2E;
     }
     dsum[i] = sum16(w);
-    if (tx == 0 && t < t_end) a.stat[((size_t)b * a.H + h) * a.mask.T + t] = make_float2(lse2[i], dsum[i]);
+    if (tx == 0 && t < t_end) a.stat[((size_t)b * a.H + h) * a.stat_stride + t] = make_float2(lse2[i], dsum[i]);
 #pragma unroll
     for (int c = 0; c < NC; ++c) acc[i][c] = 0.f;
   }
@@ -315,7 +315,7 @@ __device__ __forceinline__ void dkdv_rows(const Args& a, float* sm, int b, int g
     for (int c = 0; c < NC; ++c) dk[i][c] = dv[i][c] = 0.f;
   for (int h = g * G; h < (g + 1) * G; ++h) {
     const size_t qo = (size_t)b * a.mask.T * qs + (size_t)h * D;
-    const float2* stat = a.stat + ((size_t)b * a.H + h) * a.mask.T;
+    const float2* stat = a.stat + ((size_t)b * a.H + h) * a.stat_stride;
     const float slope = a.slopes ? a.slopes[h] : 0.f;
     for (int t0 = qr.x; t0 < qr.y; t0 += BN) {
       sync_rows<NTHR>();

@@ -64,7 +64,7 @@ def test_heads_and_widths(H, H_kv, d, dtype, exact):
 
 MASKS = [
     dict(causal=0), dict(causal=0, cap=8.0, slopes=True), dict(window=1), dict(window=64), dict(window=7, causal=0), dict(window=1000),
-    dict(window=130, slopes=True), dict(cap=5.0), dict(slopes=True), dict(cap=30.0, slopes=True),
+    dict(window=130, slopes=True), dict(window=2 ** 31 - 1, causal=0), dict(cap=5.0), dict(slopes=True), dict(cap=30.0, slopes=True),
     dict(prefix=[0, 300]), dict(prefix=[129, 64], slopes=True, cap=20.0),
 ]
 
