@@ -123,8 +123,10 @@ AttnCall make_call(const lawcat_attn_params* p, const float* slopes, void* strea
   return c;
 }
 
-AttnDecode make_decode(const lawcat_attn_params* p, const void* q, const void* k, const void* v, const int* pos, const float* slopes, void* stream) {
+AttnDecode make_decode(const lawcat_attn_params* p, const void* q, const void* k, const void* v, const int* pos, const float* slopes, void* stream,
+                       int* dev_status) {
   AttnDecode c{};
+  c.dev_status = dev_status;
   c.q = q; c.k_t = k; c.v_t = v;
   c.pos = pos; c.slopes = slopes;
   c.B = p->B; c.H = p->H; c.H_kv = p->H_kv; c.C = p->T_k; c.window = p->window;
@@ -158,7 +160,7 @@ size_t lawcat_attn_workspace_bytes(const lawcat_attn_params* p, int op) {
     case LAWCAT_OP_ATTN_FWD:
       return rows_bytes(p) + (attn_tc_supported(p->dtype, p->d, p->exact) ? attn_fwd_tc_workspace_bytes(p->B, p->H, p->H_kv, p->T, p->T_k, p->window, p->d) : 0);
     case LAWCAT_OP_ATTN_BWD: return rows_bytes(p) + keys_bytes(p) + stat_bytes(p);
-    case LAWCAT_OP_ATTN_DECODE: return align_up(attn_decode_workspace_bytes(p->B, p->H, p->H_kv, p->T_k, p->window, p->d), 256);
+    case LAWCAT_OP_ATTN_DECODE: return align_up(attn_decode_workspace_bytes(make_decode(p, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr)), 256);
     default: return 0;
   }
 }
@@ -210,7 +212,6 @@ int lawcat_attn_bwd(const lawcat_attn_params* p, const int32_t* cu_seqlens, cons
 
 int lawcat_attn_decode(const lawcat_attn_params* p, const void* q_t, const void* k_t, const void* v_t, void* K, void* V, const int32_t* pos,
                        const float* slopes, void* o_t, void* ws, size_t ws_bytes, void* stream, int* dev_status) {
-  (void)dev_status;
   int r = check(p);
   if (r || (r = check_cache(p))) return r;
   if (p->B == 0) return LAWCAT_OK;
@@ -219,7 +220,7 @@ int lawcat_attn_decode(const lawcat_attn_params* p, const void* q_t, const void*
   if ((r = check_ptrs(req, opt, 2))) return r;
   const size_t need = lawcat_attn_workspace_bytes(p, LAWCAT_OP_ATTN_DECODE);
   if (need && (!ws || ws_bytes < need)) return LAWCAT_ERR_WORKSPACE_TOO_SMALL;
-  AttnDecode c = make_decode(p, q_t, k_t, v_t, pos, slopes, stream);
+  AttnDecode c = make_decode(p, q_t, k_t, v_t, pos, slopes, stream, dev_status);
   c.K = K; c.V = V; c.o = o_t; c.ws = ws;
   return launch_attn_decode(c);
 }
@@ -227,7 +228,6 @@ int lawcat_attn_decode(const lawcat_attn_params* p, const void* q_t, const void*
 int lawcat_attn_decode_quant(const lawcat_attn_params* p, const void* q_t, const void* k_t, const void* v_t, void* kq, void* kp, void* vq,
                              void* vp, const int32_t* pos, const float* slopes, void* o_t, void* ws, size_t ws_bytes, void* stream,
                              int* dev_status) {
-  (void)dev_status;
   int r = check(p);
   if (r || (r = check_cache(p))) return r;
   if (p->B == 0) return LAWCAT_OK;
@@ -236,7 +236,7 @@ int lawcat_attn_decode_quant(const lawcat_attn_params* p, const void* q_t, const
   if ((r = check_ptrs(req, opt, 2))) return r;
   const size_t need = lawcat_attn_workspace_bytes(p, LAWCAT_OP_ATTN_DECODE);
   if (need && (!ws || ws_bytes < need)) return LAWCAT_ERR_WORKSPACE_TOO_SMALL;
-  AttnDecode c = make_decode(p, q_t, k_t, v_t, pos, slopes, stream);
+  AttnDecode c = make_decode(p, q_t, k_t, v_t, pos, slopes, stream, dev_status);
   c.kq = kq; c.kp = kp; c.vq = vq; c.vp = vp; c.o = o_t; c.ws = ws;
   return launch_attn_decode(c);
 }
@@ -248,7 +248,7 @@ static int cache_rows(const lawcat_attn_params* p, const void* k, const void* v,
   if ((size_t)p->B * p->T == 0) return LAWCAT_OK;
   const void* const req[] = {k, v, kq, kp, vq, vp, pos};
   if ((r = check_ptrs(req, nullptr, 0))) return r;
-  AttnDecode c = make_decode(p, nullptr, k, v, pos, nullptr, stream);
+  AttnDecode c = make_decode(p, nullptr, k, v, pos, nullptr, stream, nullptr);
   c.kq = kq; c.kp = kp; c.vq = vq; c.vp = vp;
   return launch_attn_quant(c, p->T, write);
 }

@@ -106,9 +106,10 @@ struct AttnDecode {
   void *o, *ws;
   int B, H, H_kv, C, window, d, dtype, exact;
   float scale, cap;
+  int* dev_status;
   cudaStream_t stream;
 };
-size_t attn_decode_workspace_bytes(int B, int H, int H_kv, int C, int window, int d);
+size_t attn_decode_workspace_bytes(const AttnDecode& c);
 int launch_attn_decode(const AttnDecode& c);
 // T rows per sequence of k_t, v_t into the 4-bit cache, or (write = false) out of it
 int launch_attn_quant(const AttnDecode& c, int T, bool write);

@@ -9,7 +9,7 @@
 // and sum of each head (one warp per head). The keys are cut into as many parts as fill the SMs; the parts' (maximum, sum,
 // weighted values) meet in a second kernel. The number of parts follows from the capacity alone, so that a captured step may
 // be replayed at every length.
-#include "attn.cuh"
+#include "attn_decode.cuh"
 
 namespace lawcat {
 namespace attn {
@@ -17,34 +17,6 @@ namespace attn {
 constexpr int TK = 64;       // keys per tile
 constexpr int HB = 8;        // query heads per block (one warp each)
 constexpr int DEC_THREADS = 32 * HB;
-
-struct DecArgs {
-  const void *q, *k_t, *v_t;    // [B, H, D], [B, H_kv, D]
-  void *K, *V;                  // [B, C, H_kv, D] in the storage type (not in the 4-bit form)
-  uint8_t *kq, *vq;             // [B, H_kv, C, D / 2]
-  bf16 *kp, *vp;                // [B, H_kv, C, groups, 2]
-  const int* pos;               // [B]
-  const float* slopes;
-  void* o;                      // [B, H, D]
-  float* part;                  // [B, H, parts, D + 2] (maximum in log2 units, sum, weighted values) where parts > 1
-  int B, H, H_kv, C, window, parts;
-  float scale, cap;
-};
-
-__host__ __device__ constexpr int quant_group(int d) { return d < 32 ? d : 32; }
-
-// scale and minimum of a group from its minimum and maximum, both rounded to bf16; a group that holds a value that is not
-// finite (or spans more than fp32 holds) reads back as NaN
-__device__ __forceinline__ void quant_params(float lo, float hi, bool finite, float& scale, float& low) {
-  low = __bfloat162float(__float2bfloat16_rn(lo));
-  const float s = __fdiv_rn(hi - low, 15.f);
-  scale = finite && isfinite(s) && isfinite(low) ? __bfloat162float(__float2bfloat16_rn(s)) : NAN;
-}
-// (in fp32 as in 64 bits: the difference of two bf16 values a few binades apart is exact, and no quotient of such numbers lies
-// closer to a border between two codes than fp32 tells apart)
-__device__ __forceinline__ uint32_t quant_code(float x, float scale, float low) {
-  return scale > 0.f ? (uint32_t)fminf(fmaxf(rintf(__fdiv_rn(x - low, scale)), 0.f), 15.f) : 0u;
-}
 
 // Eight channels of one row (c0 = 8 i), threads of a group side by side in a warp: codes as one word, parameters by the
 // group's first thread, and the values that they stand for in place of x.
@@ -309,9 +281,16 @@ int decode_parts(int B, int H, int H_kv, int C, int window) {
 
 }  // namespace attn
 
-size_t attn_decode_workspace_bytes(int B, int H, int H_kv, int C, int window, int d) {
-  const int parts = attn::decode_parts(B, H, H_kv, C, window);
-  return parts == 1 ? 0 : sizeof(float) * (size_t)B * H * parts * (d + 2);
+size_t attn_decode_workspace_bytes(const AttnDecode& c) {  // (of the step in the storage type and of the 4-bit one: the larger need)
+  int parts = attn::decode_parts(c.B, c.H, c.H_kv, c.C, c.window);
+  if (attn_tc_supported(c.dtype, c.d, c.exact)) {
+    AttnDecode q = c;
+    q.kq = nullptr;
+    parts = attn_decode_tc_parts(q);
+    q.kq = &q;
+    parts = parts > attn_decode_tc_parts(q) ? parts : attn_decode_tc_parts(q);
+  }
+  return parts == 1 ? 0 : sizeof(float) * (size_t)c.B * c.H * parts * (c.d + 2);
 }
 
 namespace {
@@ -326,9 +305,23 @@ int by_width(int d, F f) {
 }
 }  // namespace
 
+int launch_attn_decode_join(const attn::DecArgs& a, int d, int dtype, cudaStream_t stream) {
+  return by_width(d, [&](auto dd) {
+    constexpr int D = decltype(dd)::value;
+    auto go = [&](auto t) -> int {
+      using T = decltype(t);
+      LAWCAT_LAUNCH("attn_decode_join", stream,
+                    attn::attn_decode_join_kernel<T, D><<<(unsigned)(((long long)a.B * a.H + 3) / 4), 128, 0, stream>>>(a));
+      LAWCAT_CHECK_LAUNCH();
+      return LAWCAT_OK;
+    };
+    return dtype == LAWCAT_F32 ? go(float{}) : go(bf16{});
+  });
+}
+
 int launch_attn_decode(const AttnDecode& c) {
-  attn::DecArgs a{c.q, c.k_t, c.v_t, c.K, c.V, (uint8_t*)c.kq, (uint8_t*)c.vq, (bf16*)c.kp, (bf16*)c.vp, c.pos, c.slopes, c.o, (float*)c.ws,
-                  c.B, c.H, c.H_kv, c.C, c.window, attn::decode_parts(c.B, c.H, c.H_kv, c.C, c.window), c.scale, c.cap};
+  if (attn_tc_supported(c.dtype, c.d, c.exact)) return launch_attn_decode_tc(c);
+  attn::DecArgs a = attn::decode_args(c, attn::decode_parts(c.B, c.H, c.H_kv, c.C, c.window));
   const int G = c.H / c.H_kv;
   const long long blocks = (long long)c.B * c.H_kv * ((G + attn::HB - 1) / attn::HB) * a.parts;
   if (blocks > 0x7fffffffLL) return LAWCAT_ERR_UNSUPPORTED;
@@ -347,12 +340,7 @@ int launch_attn_decode(const AttnDecode& c) {
       LAWCAT_LAUNCH("attn_decode", c.stream,
                     attn::attn_decode_kernel<T, D, Q4><<<(unsigned)blocks, attn::DEC_THREADS, sm, c.stream>>>(a));
       LAWCAT_CHECK_LAUNCH();
-      if (a.parts > 1) {
-        LAWCAT_LAUNCH("attn_decode_join", c.stream,
-                      attn::attn_decode_join_kernel<T, D><<<(unsigned)(((long long)c.B * c.H + 3) / 4), 128, 0, c.stream>>>(a));
-        LAWCAT_CHECK_LAUNCH();
-      }
-      return LAWCAT_OK;
+      return a.parts > 1 ? launch_attn_decode_join(a, c.d, c.dtype, c.stream) : (int)LAWCAT_OK;
     };
     if (c.kq) return c.dtype == LAWCAT_F32 ? go(float{}, std::true_type{}) : go(bf16{}, std::true_type{});
     return c.dtype == LAWCAT_F32 ? go(float{}, std::false_type{}) : go(bf16{}, std::false_type{});
