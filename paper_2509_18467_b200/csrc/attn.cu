@@ -107,7 +107,7 @@ int fill_rows(const lawcat_attn_params* p, const int32_t* cu, const int32_t* pre
 size_t rows_bytes(const lawcat_attn_params* p) { return align_up(sizeof(int2) * (size_t)p->B * p->T, 256); }
 size_t keys_bytes(const lawcat_attn_params* p) { return align_up(sizeof(int2) * (size_t)p->B * p->T_k, 256); }
 int stat_stride(const lawcat_attn_params* p) { return (p->T + 63) / 64 * 64; }
-size_t stat_bytes(const lawcat_attn_params* p) { return align_up(sizeof(float2) * (size_t)p->B * stat_stride(p) * p->H, 256); }
+size_t stat_bytes(const lawcat_attn_params* p) { return align_up(2 * sizeof(float) * (size_t)p->B * stat_stride(p) * p->H, 256); }
 
 AttnCall make_call(const lawcat_attn_params* p, const float* slopes, void* stream, int* dev_status) {
   AttnCall c{};
@@ -202,7 +202,7 @@ int lawcat_attn_bwd(const lawcat_attn_params* p, const int32_t* cu_seqlens, cons
   c.a.lse = const_cast<float*>(lse);
   c.a.dq = dq; c.a.dk = dk; c.a.dv = dv;
   int2* const keys = (int2*)((char*)ws + rows_bytes(p));
-  c.a.stat = (float2*)((char*)keys + keys_bytes(p));
+  c.a.stat = (float*)((char*)keys + keys_bytes(p));
   c.a.stat_stride = stat_stride(p);
   if (cu_seqlens || prefix) {
     if ((r = fill_rows(p, cu_seqlens, prefix, nseq, c.a.mask, (int2*)ws, keys, c.stream))) return r;

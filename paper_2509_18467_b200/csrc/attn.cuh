@@ -73,7 +73,7 @@ struct Args {
   void *o, *dq, *dk, *dv;
   float* lse;           // [B, T, H] natural logarithm (forward: output; backward: input)
   const float* slopes;  // [H] or null
-  float2* stat;         // backward: [B, H, stat_stride] (lse log2e, dO.o)
+  float* stat;          // backward: [2, B, H, stat_stride]: -lse log2e, then -D, D = sum_j p_j dO.v_j
   int stat_stride;      // T rounded up to 64
   Mask mask;
   int B, H, H_kv;

@@ -1,12 +1,15 @@
 // Gradients of softmax attention on the tensor cores: bf16 storage, d = 64 or 128. One kernel in two forms:
-//   KV = false   a block owns 128 queries of one head (Q, dO) and walks their keys (K, V) in tiles of 64:        dQ += dX K
+//   KV = false   a block owns 128 queries of one head (Q, dO) and walks their keys (K, V) in tiles of 64:  dQ += dX K, R += P f K
 //   KV = true    a block owns 128 keys of one key-value head (K, V) and walks the queries that see them, of every head of the
 //                group (Q, dO), in tiles of 64:                                             dK += dX^T Q,  dV += P^T dO
 // With A1, A2 the block's own tiles and B1, B2 the walked ones, both compute
-//   S = A1 B1^T, dP = A2 B2^T (shared memory), P = exp2(S scale - lse), dX = P (dP - D) (one thread per own row),
-//   acc1 += dX B1 and, for keys, acc2 += P B2 (dX and P as bf16 in tensor memory over dP and S).
+//   S = A1 B1^T, dP = A2 B2^T (shared memory), P = exp2(S scale - lse), dX = P (dP - D) f (one thread per own row; f = 1 - tanh^2
+//   under a cap, else 1), acc1 += dX B1, acc2 += P B2 (keys) or P f B1 (queries), dX and P as bf16 in tensor memory over dP and S.
 // Two warpgroups take the walked tiles in turn, each with an S and a dP of its own: one tile's exponentials run behind the other
-// tile's products. D = dO.o is computed by the first form, which also leaves (lse log2e, D) of every query for the second.
+// tile's products.
+// D = sum_j p_j dP_j comes out of the first form's own loop, in fp32: it starts from dO.o, whose o was rounded, and what that was off
+// by is put right at the end with R: dQ = acc1 + (dO.o - D) R. The second form reads (lse, D) of every query as the first left them.
+// (With dO.o for D the gradients of q and k were 2.6e-3 off 64 bits, of which 2.3e-3 are the roundings below.)
 // The sums over queries and over keys stay in tensor memory of one block each, in one order: no atomics, the same bits every time.
 // The price is S and dP computed twice (7 products of 128 x 128 x d per pair of tiles instead of 5).
 // Rounding: P and dX to bf16 as operands, the gradients once. All else is fp32.
@@ -24,10 +27,10 @@ struct BwdArgs {
 
 template <int D>
 struct BwdLay {
-  static constexpr uint32_t OWN = 128 * D * 2, WALK = 64 * D * 2, STAT = 512;
+  static constexpr uint32_t OWN = 128 * D * 2, WALK = 64 * D * 2, STAT = 512;   // (a tile's -lse log2e, then its -D)
   static constexpr int ST = 4;
   static constexpr uint32_t STAGE = 2 * WALK;
-  static constexpr uint32_t OFF_A = 0, OFF_RING = 2 * OWN, OFF_STAT = OFF_RING + ST * STAGE, OFF_BAR = OFF_STAT + ST * STAT;
+  static constexpr uint32_t OFF_A = 0, OFF_RING = 2 * OWN, OFF_STAT = OFF_RING + ST * STAGE, OFF_DEX = OFF_STAT + ST * STAT, OFF_BAR = OFF_DEX + 1024;
   static constexpr uint32_t BYTES0 = OFF_BAR + 256, E1 = (uint32_t)dq_smem<D, 4, 128>(), E2 = (uint32_t)dkdv_smem<D, 4, 128>();
   static constexpr uint32_t E = E1 > E2 ? E1 : E2, BYTES = BYTES0 > E ? BYTES0 : E;
   static constexpr int THREADS = 320;
@@ -122,7 +125,11 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
         mbar_arrive_expect_tx(bar(L::B_FULL + s), L::STAGE + (KV ? L::STAT : 0));
         load_tile<D, 64>(sb + L::OFF_RING + s * L::STAGE, &tm_b1, bar(L::B_FULL + s), h, w, b);
         load_tile<D, 64>(sb + L::OFF_RING + s * L::STAGE + L::WALK, &tm_b2, bar(L::B_FULL + s), h, w, b);
-        if (KV) bulk_load(sb + L::OFF_STAT + s * L::STAT, a.stat + ((size_t)b * a.H + h) * a.stat_stride + w, L::STAT, bar(L::B_FULL + s));
+        if (KV) {
+          const float* const nl = a.stat + ((size_t)b * a.H + h) * a.stat_stride + w;
+          bulk_load(sb + L::OFF_STAT + s * L::STAT, nl, 256, bar(L::B_FULL + s));
+          bulk_load(sb + L::OFF_STAT + s * L::STAT + 256, nl + (size_t)a.B * a.H * a.stat_stride, 256, bar(L::B_FULL + s));
+        }
       }
     }
   } else if (warp == 9) {
@@ -148,9 +155,8 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
         if (ok) ok = wait_bar(bar(L::B_P + (it & 1)), (it >> 1) & 1, s_abort, f.limit);
         if (!ok) break;
         tc_fence_after_sync();
-        if (KV)
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) mma_ts(acc2, s_col(it & 1) + kk * 8, mdesc<64>(b1(it) + L::WALK, kk), id_a, (it | kk) != 0);
+        for (int kk = 0; kk < 4; ++kk) mma_ts(acc2, s_col(it & 1) + kk * 8, mdesc<64>(b1(it) + (KV ? L::WALK : 0), kk), id_a, (it | kk) != 0);
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) mma_ts(acc1, p_col(it & 1) + kk * 8, mdesc<64>(b1(it), kk), id_a, (it | kk) != 0);
         mma_commit(bar(L::B_EMPTY + it % L::ST));
@@ -165,8 +171,9 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
     const uint32_t S = s_col(wg) + lanes, P = p_col(wg) + lanes;
     // the columns that this row meets: the keys that the query sees, or the queries that see the key
     const int2 iv = !valid ? make_int2(0, 0x7fffffff) : KV ? key_interval(a.mask, b, r) : interval(a.mask, b, r);
-    const float scale2 = a.scale * LOG2E, inv_cap = GENERAL && a.cap > 0.f ? 1.f / a.cap : 0.f;
-    float lse2 = 0.f, dsum = 0.f;
+    const float scale2 = a.scale * LOG2E, c2 = a.cap * LOG2E, inv_c2 = GENERAL && a.cap > 0.f ? 1.f / c2 : 0.f;
+    float nl = 0.f, nd = 0.f;   // -lse log2e and -dO.o of an own query
+    uint64_t dex = 0;           // sums of p dP
     if (!KV && valid) {
       const size_t row = ((size_t)b * a.mask.T + r) * a.H + own;
       const uint4 *o = reinterpret_cast<const uint4*>((const bf16*)a.o_in + row * D), *g = reinterpret_cast<const uint4*>((const bf16*)a.dO + row * D);
@@ -183,9 +190,8 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
         d0 = fmaf(bf16_lo(x.w), bf16_lo(y.w), d0);
         d1 = fmaf(bf16_hi(x.w), bf16_hi(y.w), d1);
       }
-      dsum = d0 + d1;
-      lse2 = a.lse[row] * LOG2E;
-      if (wg == 0) a.stat[((size_t)b * a.H + own) * a.stat_stride + r] = make_float2(lse2, dsum);
+      nd = -(d0 + d1);
+      nl = -a.lse[row] * LOG2E;
     }
     bool ok = true;
     for (int it = wg; it < n; it += 2) {
@@ -202,55 +208,74 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
       tmem_ld32(P, p);
       tmem_ld32(P + 32, p + 32);
       tmem_wait_ld();
-      const bool whole = __all_sync(0xffffffffu, iv.x <= c0 && iv.y >= c0 + 64);
-      const int rel = iv.x - c0;
-      const uint32_t len = (uint32_t)(iv.y - iv.x);
       // |i - j| = |dist0 - c|
       const float dist0 = (float)(KV ? r - c0 - a.mask.off : r + a.mask.off - c0);
-      const float k1 = 2.f * LOG2E * a.scale * inv_cap, c2 = a.cap * LOG2E;
       if (KV) mbar_wait(bar(L::B_FULL + st), (it / L::ST) & 1);   // (complete by now; makes the copied statistics visible here)
-#pragma unroll
-      for (int c = 0; c < 64; c += 2) {
-        float l0 = lse2, l1 = lse2, D0 = dsum, D1 = dsum;
-        if (KV) {
-          const float4 w = stat[c / 2];
-          l0 = w.x; D0 = w.y; l1 = w.z; D1 = w.w;
-        }
-        float x0, x1, f0 = 1.f, f1 = 1.f;
-        if (GENERAL) {
-          if (a.cap > 0.f) {
-            const float q0 = rcpf(1.f + ex2f(s[c] * k1)), q1 = rcpf(1.f + ex2f(s[c + 1] * k1));   // tanh = 1 - 2 q
-            x0 = c2 - 2.f * c2 * q0;
-            x1 = c2 - 2.f * c2 * q1;
-            f0 = 4.f * q0 * (1.f - q0);
-            f1 = 4.f * q1 * (1.f - q1);
-          } else {
-            x0 = s[c] * scale2;
-            x1 = s[c + 1] * scale2;
-          }
-          x0 = fmaf(-slope2, fabsf(dist0 - (float)c), x0) - l0;
-          x1 = fmaf(-slope2, fabsf(dist0 - (float)(c + 1)), x1) - l1;
+      if (GENERAL) {
+        if (a.cap > 0.f) {
+          cap_scores(s, a.scale / a.cap, c2);
         } else {
-          x0 = fmaf(s[c], scale2, -l0);
-          x1 = fmaf(s[c + 1], scale2, -l1);
+#pragma unroll
+          for (int c = 0; c < 64; ++c) s[c] *= scale2;
         }
-        float p0 = ex2f(x0), p1 = ex2f(x1);
-        float y0 = p0 * (p[c] - D0), y1 = p1 * (p[c + 1] - D1);
-        if (GENERAL) {
-          y0 *= f0;
-          y1 *= f1;
-        }
-        if (!whole) {
-          const bool v0 = (uint32_t)(c - rel) < len, v1 = (uint32_t)(c + 1 - rel) < len;
-          p0 = v0 ? p0 : 0.f;
-          y0 = v0 ? y0 : 0.f;
-          p1 = v1 ? p1 : 0.f;
-          y1 = v1 ? y1 : 0.f;
-        }
-        s[c / 2] = __uint_as_float(pack_bf16(p0, p1));
-        p[c / 2] = __uint_as_float(pack_bf16(y0, y1));
       }
-      if (KV) tmem_st32(S, s);
+      const uint64_t sc = f2_pack(scale2, scale2), one = f2_pack(1.f, 1.f), ic = f2_pack(inv_c2, inv_c2), nic = f2_pack(-inv_c2, -inv_c2);
+      // weights and their gradients over the scores, as bf16 pairs; `some`: not every column is met
+      auto weigh = [&](auto some) {
+        const int rel = iv.x - c0;
+        const uint32_t len = (uint32_t)(iv.y - iv.x);
+#pragma unroll
+        for (int q = 0; q < 64; q += 4) {
+          float4 l4 = make_float4(nl, nl, nl, nl), d4 = make_float4(nd, nd, nd, nd);
+          if (KV) {
+            l4 = stat[q / 4];
+            d4 = stat[16 + q / 4];
+          }
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            const int c = q + e;
+            const uint64_t x = f2_pack(s[c], s[c + 1]), l = e ? f2_pack(l4.z, l4.w) : f2_pack(l4.x, l4.y), d = e ? f2_pack(d4.z, d4.w) : f2_pack(d4.x, d4.y);
+            uint64_t y, fac = one;
+            if (GENERAL) {
+              float b0, b1;
+              f2_unpack(l, b0, b1);
+              b0 = fmaf(-slope2, fabsf(dist0 - (float)c), b0);
+              b1 = fmaf(-slope2, fabsf(dist0 - (float)(c + 1)), b1);
+              y = f2_add(x, f2_pack(b0, b1));
+              fac = f2_fma(f2_mul(x, ic), f2_mul(x, nic), one);   // 1 - tanh^2
+            } else {
+              y = f2_fma(x, sc, l);
+            }
+            float p0, p1;
+            f2_unpack(y, p0, p1);
+            p0 = ex2f(p0);
+            p1 = ex2f(p1);
+            float g0 = p[c], g1 = p[c + 1], f0 = 1.f, f1 = 1.f;
+            if (GENERAL) f2_unpack(fac, f0, f1);
+            if (decltype(some)::value) {
+              const bool v0 = (uint32_t)(c - rel) < len, v1 = (uint32_t)(c + 1 - rel) < len;
+              p0 = v0 ? p0 : 0.f;
+              g0 = v0 ? g0 : 0.f;
+              f0 = v0 ? f0 : 0.f;
+              p1 = v1 ? p1 : 0.f;
+              g1 = v1 ? g1 : 0.f;
+              f1 = v1 ? f1 : 0.f;
+            }
+            const uint64_t pp = f2_pack(p0, p1), gg = f2_pack(g0, g1);
+            if (!KV) dex = f2_fma(pp, gg, dex);
+            const uint64_t pf = GENERAL ? f2_mul(pp, f2_pack(f0, f1)) : pp;
+            const uint64_t dx = f2_mul(pf, f2_add(gg, d));
+            float y0, y1;
+            f2_unpack(KV ? pp : pf, y0, y1);
+            s[c / 2] = __uint_as_float(pack_bf16(y0, y1));
+            f2_unpack(dx, y0, y1);
+            p[c / 2] = __uint_as_float(pack_bf16(y0, y1));
+          }
+        }
+      };
+      if (__all_sync(0xffffffffu, iv.x <= c0 && iv.y >= c0 + 64)) weigh(std::false_type{});
+      else weigh(std::true_type{});
+      tmem_st32(S, s);
       tmem_st32(P, p);
       tmem_wait_st();
       tc_fence_before_sync();
@@ -258,8 +283,25 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
       if (KV) mbar_arrive(bar(L::B_EMPTY + st));
     }
     if (ok && n > 0) ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_DONE), 0, s_abort, f.limit));
+    float* const s_dex = reinterpret_cast<float*>(smem + L::OFF_DEX);
+    if (!KV) {
+      float d0, d1;
+      f2_unpack(dex, d0, d1);
+      s_dex[tid] = d0 + d1;
+      ok = !named_bar_or(2, 256, !ok);   // (all of them go on, or none)
+    }
     if (ok) {
       tc_fence_after_sync();
+      float fix = 0.f;   // dO.o - D
+      if (!KV) {
+        const float d = s_dex[tid & 127] + s_dex[128 + (tid & 127)];
+        fix = -nd - d;
+        if (valid && wg == 0) {
+          float* const w = a.stat + ((size_t)b * a.H + own) * a.stat_stride + r;
+          w[0] = nl;
+          w[(size_t)a.B * a.H * a.stat_stride] = -d;
+        }
+      }
       // keys: one group stores dv, the other dk; queries: half of dq's channels each
       const uint32_t acc = (KV ? (wg ? acc1 : acc2) : acc1) + lanes;
       bf16* const dst = KV ? (bf16*)(wg ? a.dk : a.dv) + (((size_t)b * a.mask.T_k + r) * a.H_kv + own) * D
@@ -271,6 +313,13 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
         float o[32];
         if (n > 0) {
           tmem_ld32(acc + c, o);
+          if (!KV) {
+            float w[32];
+            tmem_ld32(acc2 + lanes + c, w);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = fmaf(fix, w[e], o[e]);
+          }
           tmem_wait_ld();
         } else {
 #pragma unroll

@@ -259,7 +259,11 @@ __device__ __forceinline__ void dq_rows(const Args& a, float* sm, int b, int h, 
       lse2[i] = a.lse[((size_t)b * a.mask.T + t) * a.H + h] * LOG2E;
     }
     dsum[i] = sum16(w);
-    if (tx == 0 && t < t_end) a.stat[((size_t)b * a.H + h) * a.stat_stride + t] = make_float2(lse2[i], dsum[i]);
+    if (tx == 0 && t < t_end) {
+      float* const st = a.stat + ((size_t)b * a.H + h) * a.stat_stride + t;
+      st[0] = -lse2[i];
+      st[(size_t)a.B * a.H * a.stat_stride] = -dsum[i];
+    }
 #pragma unroll
     for (int c = 0; c < NC; ++c) acc[i][c] = 0.f;
   }
@@ -315,7 +319,7 @@ __device__ __forceinline__ void dkdv_rows(const Args& a, float* sm, int b, int g
     for (int c = 0; c < NC; ++c) dk[i][c] = dv[i][c] = 0.f;
   for (int h = g * G; h < (g + 1) * G; ++h) {
     const size_t qo = (size_t)b * a.mask.T * qs + (size_t)h * D;
-    const float2* stat = a.stat + ((size_t)b * a.H + h) * a.stat_stride;
+    const float *nl = a.stat + ((size_t)b * a.H + h) * a.stat_stride, *nd = nl + (size_t)a.B * a.H * a.stat_stride;
     const float slope = a.slopes ? a.slopes[h] : 0.f;
     for (int t0 = qr.x; t0 < qr.y; t0 += BN) {
       sync_rows<NTHR>();
@@ -331,16 +335,16 @@ __device__ __forceinline__ void dkdv_rows(const Args& a, float* sm, int b, int g
       for (int j = 0; j < 4; ++j) {
         const int t = t0 + tx + 16 * j;
         const int2 iv = t < qr.y ? interval(a.mask, b, t) : make_int2(0, 0);
-        const float2 st = t < qr.y ? stat[t] : make_float2(0.f, 0.f);
+        const float2 st = t < qr.y ? make_float2(nl[t], nd[t]) : make_float2(0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < RM; ++i) {
           const int key = j0 + ty * RM + i;
           const bool see = key >= iv.x && key < iv.y;
           float th = 0.f;
           const float x = score2(s[i][j], a.scale, a.cap, slope, abs(t + a.mask.off - key), th);
-          const float p = exp2f(x - st.x);
+          const float p = exp2f(x + st.x);
           P[(ty * RM + i) * (BN + 4) + tx + 16 * j] = see ? p : 0.f;
-          S[(ty * RM + i) * (BN + 4) + tx + 16 * j] = see ? p * (dp[i][j] - st.y) * (1.f - th * th) : 0.f;
+          S[(ty * RM + i) * (BN + 4) + tx + 16 * j] = see ? p * (dp[i][j] + st.y) * (1.f - th * th) : 0.f;
         }
       }
       __syncwarp();

@@ -190,9 +190,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       if constexpr (GENERAL) {
         const float dist0 = (float)(t + a.mask.off - j0);
         if (a.cap > 0.f) {
-          const float k1 = 2.f * LOG2E * a.scale * inv_cap, c2 = a.cap * LOG2E;
-#pragma unroll
-          for (int c = 0; c < 128; ++c) s[c] = c2 - 2.f * c2 * rcpf(1.f + ex2f(s[c] * k1));   // cap tanh(u / cap)
+          cap_scores(s, a.scale * inv_cap, a.cap * LOG2E);
         } else {
 #pragma unroll
           for (int c = 0; c < 128; ++c) s[c] *= scale2;

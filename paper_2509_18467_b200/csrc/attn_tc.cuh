@@ -52,7 +52,35 @@ __device__ __forceinline__ uint64_t mdesc(uint32_t tile, int kk) {
   return smem_desc(tile + (uint32_t)kk * 2048, ROWS * 128, 1024, LAYOUT_SW128);
 }
 
-__device__ __forceinline__ bool finite_bits(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+// s <- c2 tanh(s k) for N scores of a thread (all 32 lanes of a warp together). While no |s k| of the warp passes 0.8, tanh is y P(y^2)
+// with P of degree 5 on the FMA pipe (a least-maximum fit of tanh(y) / y over [0, 0.8], relative error 5e-8, 2e-7 with its fp32
+// arithmetic): the two special functions of the other form would be three times the whole softmax's load on their pipe.
+template <int N>
+__device__ __forceinline__ void cap_scores(float (&s)[N], float k, float c2) {
+  float big = 0.f;
+#pragma unroll
+  for (int c = 0; c < N; c += 2) big = fmaxf(big, fmaxf(fabsf(s[c]), fabsf(s[c + 1])));
+  if (__all_sync(0xffffffffu, big * fabsf(k) <= 0.8f)) {
+    const uint64_t kk = f2_pack(k, k), cc = f2_pack(c2, c2);
+    const uint64_t a0 = f2_pack(0.9999999403953552f, 0.9999999403953552f), a1 = f2_pack(-0.33332714438438416f, -0.33332714438438416f),
+                   a2 = f2_pack(0.13321532309055328f, 0.13321532309055328f), a3 = f2_pack(-0.05313541740179062f, -0.05313541740179062f),
+                   a4 = f2_pack(0.019130872562527657f, 0.019130872562527657f), a5 = f2_pack(-0.004378729499876499f, -0.004378729499876499f);
+#pragma unroll
+    for (int c = 0; c < N; c += 2) {
+      const uint64_t y = f2_mul(f2_pack(s[c], s[c + 1]), kk), z = f2_mul(y, y);
+      uint64_t r = f2_fma(a5, z, a4);
+      r = f2_fma(r, z, a3);
+      r = f2_fma(r, z, a2);
+      r = f2_fma(r, z, a1);
+      r = f2_fma(r, z, a0);
+      f2_unpack(f2_mul(f2_mul(y, cc), r), s[c], s[c + 1]);
+    }
+  } else {
+    const float k1 = 2.f * LOG2E * k;
+#pragma unroll
+    for (int c = 0; c < N; ++c) s[c] = c2 - 2.f * c2 * rcpf(1.f + ex2f(s[c] * k1));
+  }
+}
 
 }  // namespace attn
 }  // namespace lawcat
