@@ -1,7 +1,7 @@
 // Softmax attention forward on the tensor cores: bf16 storage, d = 64 or 128.
 //
-// A block owns NT tiles of 128 queries that read the same key-value head (two query heads of a group at the same tokens, or
-// two neighbouring tiles of one head) and walks their keys in tiles of 128:
+// An item is NT tiles of 128 queries that read the same key-value head (two query heads of a group at the same tokens, or
+// two neighbouring tiles of one head); a block walks their keys in tiles of 128:
 //   warpgroup i < NT   softmax of tile i: one thread per query; S_i from tensor memory, mask / cap / bias, running maximum and
 //                      sum in registers, P_i = exp2(x - m) rounded to bf16 over S_i in tensor memory
 //   copy warp          Q tiles once, K and V tiles in turn through a ring of stages (TMA, 128-byte swizzle)
@@ -9,6 +9,9 @@
 // While one tile's softmax runs, the other tile's products do. The accumulator O_i is rescaled only when a row's maximum has
 // grown by more than 2^8 since it was last scaled (the weights then stay within 2^8 in fp32 and bf16 alike), by the softmax
 // warps themselves: between a tile's S being there and its P being ready no product touches O_i.
+// One block per SM takes items in turn, the longest first: while an item's last tiles are weighed and its outputs stored, the next
+// one's queries and first keys are already on their way (a sequence of 1024 tokens has no more than eight key tiles per item, and
+// a block that starts and ends with each of them spent half its time so).
 // Few queries over many keys: the keys are shared out over `parts` blocks, whose (values, maximum, sum) a second kernel joins.
 // Rounding: weights to bf16 as an operand (the sum that divides them is of the unrounded ones), o once. All else is fp32.
 // A row that is not finite in a block is computed again on the CUDA cores (attn_exact.cuh): a weight of zero times a NaN that the
@@ -24,9 +27,10 @@ constexpr float RESCALE = 8.f;
 
 struct FwdArgs {
   Args a;
-  int pairs;          // blocks per (batch, query tile): H / 2 head pairs, or H
-  int tiles;          // query tiles of the grid
-  int two_heads;      // a block's two tiles are two heads (else two neighbouring tiles of one head)
+  int pairs;          // items per (batch, query tile): H / 2 head pairs, or H
+  int tiles;          // query tiles
+  int items;
+  int two_heads;      // an item's two tiles are two heads (else two neighbouring tiles of one head)
   int parts;
   float* part_o;      // [parts, B, H, T, D] where parts > 1
   float2* part_ml;    // [parts, B, H, T] (maximum in log2 units, sum)
@@ -36,16 +40,16 @@ struct FwdArgs {
 template <int D, int NT>
 struct FwdLay {
   static constexpr uint32_t TILE = 128 * D * 2;                  // a Q, K or V tile
-  static constexpr int ST = D == 128 ? 4 : (NT == 2 ? 8 : 4);    // stages of the ring (K and V tiles alternate)
-  static constexpr uint32_t OFF_Q = 0, OFF_RING = NT * TILE, OFF_BAR = OFF_RING + ST * TILE;
+  static constexpr int ST = D == 128 ? 4 : 8;                    // stages of the ring (K and V tiles alternate)
+  static constexpr uint32_t OFF_Q = 0, OFF_RING = NT * TILE, OFF_LIST = OFF_RING + ST * TILE, OFF_BAR = OFF_LIST + BAD_MAX * 4;
   static constexpr uint32_t BYTES0 = OFF_BAR + 256;
-  static constexpr uint32_t EXACT = (uint32_t)fwd_smem<D, 4, 128>();
-  static constexpr uint32_t BYTES = BYTES0 > EXACT ? BYTES0 : EXACT;
+  static constexpr uint32_t BYTES = BYTES0;
   static constexpr uint32_t COLS = NT * (128 + D) > 256 ? 512 : 256;
   static constexpr int THREADS = NT * 128 + 64;
   // mbarriers
-  static constexpr int B_Q = 0, B_FULL = 1, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + NT, B_O = B_P + NT, NBAR = B_O + NT;
-  static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 256, "shared memory");
+  static constexpr int B_Q = 0, B_QE = 1, B_FULL = 2, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + NT, B_O = B_P + NT, B_OE = B_O + NT,
+                       NBAR = B_OE + NT;
+  static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 256 && fwd_smem<D, 4, 128>() <= OFF_LIST, "shared memory");
 };
 
 template <int D>
@@ -67,26 +71,41 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   volatile int* const s_abort = s_flags + 1;
   auto bar = [&](int i) { return sb + L::OFF_BAR + 8 * (uint32_t)i; };
 
-  // what this block computes
-  const int part = blockIdx.x % f.parts, bp = blockIdx.x / f.parts % (a.B * f.pairs);
-  const int tile = f.tiles - 1 - (int)(blockIdx.x / f.parts / (a.B * f.pairs));   // (under a causal mask the longest rows first)
-  const int b = bp / f.pairs, h0 = bp % f.pairs * (f.two_heads ? 2 : 1), g = h0 / (a.H / a.H_kv);
-  const int tb = tile * (f.two_heads || NT == 1 ? 128 : 256);                     // first query
-  auto head_of = [&](int i) { return h0 + (f.two_heads ? i : 0); };
-  auto row_of = [&](int i) { return tb + (f.two_heads ? 0 : 128 * i); };
-  const int T = a.mask.T, t_last = min(T, row_of(NT - 1) + 128) - 1;
-  int j_first = interval(a.mask, b, tb).x, j_end = interval(a.mask, b, t_last).y;
-  int n = (j_end - j_first + 127) / 128;
-  if (j_end <= j_first) n = 0;
-  if (f.parts > 1) {
-    const int per = (n + f.parts - 1) / f.parts, i0 = min(n, part * per);
-    n = min(n - i0, per);
-    j_first += i0 * 128;
-    j_end = min(j_end, j_first + n * 128);
-  }
+  int* const s_list = reinterpret_cast<int*>(smem + L::OFF_LIST);
+
+  struct Item {
+    int part, b, h0, g, tb, j_first, j_end, n;
+  };
+  const int T = a.mask.T, per_tile = a.B * f.pairs * f.parts;
+  auto item_of = [&](int idx) {
+    Item w;
+    w.part = idx % f.parts;
+    const int bp = idx / f.parts % (a.B * f.pairs), tile = f.tiles - 1 - idx / per_tile;   // (under a causal mask the longest rows first)
+    w.b = bp / f.pairs;
+    w.h0 = bp % f.pairs * (f.two_heads ? 2 : 1);
+    w.g = w.h0 / (a.H / a.H_kv);
+    w.tb = tile * (f.two_heads || NT == 1 ? 128 : 256);                                    // first query
+    const int t_last = min(T, w.tb + (f.two_heads ? 128 : 128 * NT)) - 1;
+    w.j_first = interval(a.mask, w.b, w.tb).x;
+    w.j_end = interval(a.mask, w.b, t_last).y;
+    w.n = w.j_end > w.j_first ? (w.j_end - w.j_first + 127) / 128 : 0;
+    if (f.parts > 1) {
+      const int per = (w.n + f.parts - 1) / f.parts, i0 = min(w.n, w.part * per);
+      w.n = min(w.n - i0, per);
+      w.j_first += i0 * 128;
+      w.j_end = min(w.j_end, w.j_first + w.n * 128);
+    }
+    return w;
+  };
+  auto head_of = [&](const Item& w, int i) { return w.h0 + (f.two_heads ? i : 0); };
+  auto row_of = [&](const Item& w, int i) { return w.tb + (f.two_heads ? 0 : 128 * i); };
+  // this block's items: one of each round of gridDim.x, odd rounds from the other end (they are in falling order of length)
+  const int rounds = (f.items + (int)gridDim.x - 1) / (int)gridDim.x;
+  auto index_of = [&](int r) { return r * (int)gridDim.x + (r & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x); };
 
   if (tid == 0) {
     mbar_init(bar(L::B_Q), 1);
+    mbar_init(bar(L::B_QE), 1);
     for (int i = 0; i < L::ST; ++i) {
       mbar_init(bar(L::B_FULL + i), 1);
       mbar_init(bar(L::B_EMPTY + i), 1);
@@ -95,6 +114,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       mbar_init(bar(L::B_S + i), 1);
       mbar_init(bar(L::B_P + i), 128);
       mbar_init(bar(L::B_O + i), 1);
+      mbar_init(bar(L::B_OE + i), 128);
     }
     s_flags[1] = 0;
     s_flags[2] = 0;
@@ -116,157 +136,202 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 
   if (warp == NT * 4) {
     // ------------------------------------------------------------------------------------------------ copies
-    if (n > 0 && elect_one()) {
-      mbar_arrive_expect_tx(bar(L::B_Q), NT * L::TILE);
-      for (int i = 0; i < NT; ++i) load_tile<D, 128>(sb + L::OFF_Q + i * L::TILE, &tm_q, bar(L::B_Q), head_of(i), row_of(i), b);
-      for (int it = 0; it < 2 * n; ++it) {
-        const int s = it % L::ST;
-        if (it >= L::ST && !wait_bar(bar(L::B_EMPTY + s), (it / L::ST - 1) & 1, s_abort, f.limit)) break;
-        mbar_arrive_expect_tx(bar(L::B_FULL + s), L::TILE);
-        load_tile<D, 128>(sb + L::OFF_RING + s * L::TILE, it & 1 ? &tm_v : &tm_k, bar(L::B_FULL + s), g, j_first + it / 2 * 128, b);
+    if (elect_one()) {
+      int at = 0, seq = 0;   // tiles and items so far
+      bool ok = true;
+      for (int r = 0; r < rounds && ok; ++r) {
+        const int idx = index_of(r);
+        if (idx >= f.items) continue;
+        const Item w = item_of(idx);
+        if (w.n == 0) continue;
+        if (seq > 0) ok = wait_bar(bar(L::B_QE), (seq - 1) & 1, s_abort, f.limit);
+        if (!ok) break;
+        mbar_arrive_expect_tx(bar(L::B_Q), NT * L::TILE);
+        for (int i = 0; i < NT; ++i) load_tile<D, 128>(sb + L::OFF_Q + i * L::TILE, &tm_q, bar(L::B_Q), head_of(w, i), row_of(w, i), w.b);
+        for (int it = 0; it < 2 * w.n; ++it, ++at) {
+          const int s = at % L::ST;
+          if (at >= L::ST) ok = wait_bar(bar(L::B_EMPTY + s), (at / L::ST - 1) & 1, s_abort, f.limit);
+          if (!ok) break;
+          mbar_arrive_expect_tx(bar(L::B_FULL + s), L::TILE);
+          load_tile<D, 128>(sb + L::OFF_RING + s * L::TILE, it & 1 ? &tm_v : &tm_k, bar(L::B_FULL + s), w.g, w.j_first + it / 2 * 128, w.b);
+        }
+        ++seq;
       }
     }
   } else if (warp == NT * 4 + 1) {
     // ------------------------------------------------------------------------------------------------ products
-    if (n > 0 && elect_one()) {
+    if (elect_one()) {
       constexpr uint32_t id_s = instr_desc(128, 128, FMT_BF16, MAJOR_K, MAJOR_K);
       constexpr uint32_t id_o = instr_desc(128, D, FMT_BF16, MAJOR_K, MAJOR_MN);
-      auto stage = [&](int it) { return sb + L::OFF_RING + (uint32_t)(it % L::ST) * L::TILE; };
-      auto full = [&](int it) { return wait_bar(bar(L::B_FULL + it % L::ST), (it / L::ST) & 1, s_abort, f.limit); };
-      auto scores = [&](int i, int it) {
+      auto stage = [&](int at) { return sb + L::OFF_RING + (uint32_t)(at % L::ST) * L::TILE; };
+      auto full = [&](int at) { return wait_bar(bar(L::B_FULL + at % L::ST), (at / L::ST) & 1, s_abort, f.limit); };
+      // S_i of the tile whose keys are ring tile `at`; `last`: of the item
+      auto scores = [&](int i, int at, bool last) {
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
-          mma_f16(s_col(i), kdesc<128>(sb + L::OFF_Q + i * L::TILE, kk), kdesc<128>(stage(it), kk), id_s, kk != 0);
+          mma_f16(s_col(i), kdesc<128>(sb + L::OFF_Q + i * L::TILE, kk), kdesc<128>(stage(at), kk), id_s, kk != 0);
         mma_commit(bar(L::B_S + i));
-        if (i == NT - 1) mma_commit(bar(L::B_EMPTY + it % L::ST));
+        if (i == NT - 1) {
+          mma_commit(bar(L::B_EMPTY + at % L::ST));
+          if (last) mma_commit(bar(L::B_QE));
+        }
       };
-      bool ok = wait_bar(bar(L::B_Q), 0, s_abort, f.limit) && full(0);
-      if (ok) {
-        tc_fence_after_sync();
-        for (int i = 0; i < NT; ++i) scores(i, 0);
-      }
-      for (int it = 0; it < n && ok; ++it) {
-        for (int i = 0; i < NT && ok; ++i) {
-          if (i == 0) ok = full(2 * it + 1);
-          if (ok) ok = wait_bar(bar(L::B_P + i), it & 1, s_abort, f.limit);
-          if (!ok) break;
-          tc_fence_after_sync();
-#pragma unroll
-          for (int kk = 0; kk < 8; ++kk) mma_ts(o_col(i), s_col(i) + kk * 8, mdesc<128>(stage(2 * it + 1), kk), id_o, (it | kk) != 0);
-          if (i == NT - 1) mma_commit(bar(L::B_EMPTY + (2 * it + 1) % L::ST));
-          if (it + 1 < n) {
-            if (i == 0) {
-              ok = full(2 * it + 2);
-              if (!ok) break;
-              tc_fence_after_sync();
-            }
-            scores(i, 2 * it + 2);
-          } else {
-            mma_commit(bar(L::B_O + i));
+      auto next_item = [&](int& r) {   // tiles of the next item that has any; 0 behind the last
+        for (; r < rounds; ++r) {
+          const int idx = index_of(r);
+          if (idx >= f.items) continue;
+          const int n = item_of(idx).n;
+          if (n) {
+            ++r;
+            return n;
           }
         }
+        return 0;
+      };
+      int r = 0, n = next_item(r), seq = 0, step = 0;   // step: key tiles so far
+      bool ok = true;
+      if (n) {
+        ok = wait_bar(bar(L::B_Q), 0, s_abort, f.limit) && full(0);
+        if (ok) {
+          tc_fence_after_sync();
+          for (int i = 0; i < NT; ++i) scores(i, 0, n == 1);
+        }
+      }
+      while (n && ok) {
+        const int n_next = next_item(r);
+        for (int it = 0; it < n && ok; ++it, ++step) {
+          const bool more = it + 1 < n || n_next;
+          for (int i = 0; i < NT && ok; ++i) {
+            if (i == 0) ok = full(2 * step + 1);
+            if (ok && it == 0 && seq > 0) ok = wait_bar(bar(L::B_OE + i), (seq - 1) & 1, s_abort, f.limit);
+            if (ok) ok = wait_bar(bar(L::B_P + i), step & 1, s_abort, f.limit);
+            if (!ok) break;
+            tc_fence_after_sync();
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk) mma_ts(o_col(i), s_col(i) + kk * 8, mdesc<128>(stage(2 * step + 1), kk), id_o, (it | kk) != 0);
+            if (i == NT - 1) mma_commit(bar(L::B_EMPTY + (2 * step + 1) % L::ST));
+            if (it + 1 == n) mma_commit(bar(L::B_O + i));
+            if (more) {
+              if (i == 0) {
+                if (it + 1 == n) ok = wait_bar(bar(L::B_Q), (seq + 1) & 1, s_abort, f.limit);
+                if (ok) ok = full(2 * step + 2);
+                if (!ok) break;
+                tc_fence_after_sync();
+              }
+              scores(i, 2 * step + 2, it + 1 < n ? it + 2 == n : n_next == 1);
+            }
+          }
+        }
+        n = n_next;
+        ++seq;
       }
     }
   } else {
     // ------------------------------------------------------------------------------------------------ softmax
-    const int i = warp >> 2, h = head_of(i), t = row_of(i) + (tid & 127);
+    const int i = warp >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t S = s_col(i) + lanes, O = o_col(i) + lanes;
-    const bool valid = t < T;
-    const int2 iv = valid ? interval(a.mask, b, t) : make_int2(0, 0x7fffffff);   // (rows behind the last are never stored)
-    const float scale2 = a.scale * LOG2E, slope2 = GENERAL && a.slopes ? a.slopes[h] * LOG2E : 0.f;
-    const float inv_cap = GENERAL && a.cap > 0.f ? 1.f / a.cap : 0.f;
-    float m = -INFINITY, l = 0.f;
-    bool ok = true;
-    for (int it = 0; it < n; ++it) {
-      ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_S + i), it & 1, s_abort, f.limit));
+    const float scale2 = a.scale * LOG2E, inv_cap = GENERAL && a.cap > 0.f ? 1.f / a.cap : 0.f;
+    int step = 0, seq = 0;
+    for (int r = 0; r < rounds; ++r) {
+      const int idx = index_of(r);
+      if (idx >= f.items) continue;
+      const Item w = item_of(idx);
+      const int n = w.n, h = head_of(w, i), t = row_of(w, i) + (tid & 127);
+      const bool valid = t < T;
+      const int2 iv = valid ? interval(a.mask, w.b, t) : make_int2(0, 0x7fffffff);   // (rows behind the last are never stored)
+      const float slope2 = GENERAL && a.slopes ? a.slopes[h] * LOG2E : 0.f;
+      float m = -INFINITY, l = 0.f;
+      bool ok = true;
+      for (int it = 0; it < n; ++it, ++step) {
+        ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_S + i), step & 1, s_abort, f.limit));
+        if (!ok) break;
+        tc_fence_after_sync();
+        const int j0 = w.j_first + it * 128;
+        float s[128];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32(S + c * 32, s + c * 32);
+        tmem_wait_ld();
+        if constexpr (GENERAL) {
+          const float dist0 = (float)(t + a.mask.off - j0);
+          if (a.cap > 0.f) {
+            cap_scores(s, a.scale * inv_cap, a.cap * LOG2E);
+          } else {
+#pragma unroll
+            for (int c = 0; c < 128; ++c) s[c] *= scale2;
+          }
+          if (a.slopes) {
+#pragma unroll
+            for (int c = 0; c < 128; ++c) s[c] = fmaf(-slope2, fabsf(dist0 - (float)c), s[c]);
+          }
+        }
+        if (!__all_sync(0xffffffffu, iv.x <= j0 && iv.y >= j0 + 128)) {
+          const int rel = iv.x - j0;
+          const uint32_t len = (uint32_t)(iv.y - iv.x);
+#pragma unroll
+          for (int c = 0; c < 128; ++c)
+            if ((uint32_t)(c - rel) >= len) s[c] = -INFINITY;
+        }
+        float mx0 = s[0], mx1 = s[1], mx2 = s[2], mx3 = s[3];
+#pragma unroll
+        for (int c = 4; c < 128; c += 4) {
+          mx0 = fmaxf(mx0, s[c]);
+          mx1 = fmaxf(mx1, s[c + 1]);
+          mx2 = fmaxf(mx2, s[c + 2]);
+          mx3 = fmaxf(mx3, s[c + 3]);
+        }
+        float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
+        if constexpr (!GENERAL) mx *= scale2;
+        const bool grow = mx > m + RESCALE || (m == -INFINITY && mx > m);
+        if (__any_sync(0xffffffffu, grow)) {
+          const float base = grow ? mx : m, factor = m == -INFINITY ? 0.f : ex2f(m - base);
+          if (it > 0) {
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+              float o[32];
+              tmem_ld32(O + c, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] *= factor;
+              tmem_st32(O + c, o);
+            }
+            tmem_wait_st();
+          }
+          l *= factor;
+          m = base;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        const uint64_t sc = f2_pack(GENERAL ? 1.f : scale2, GENERAL ? 1.f : scale2), nb = f2_pack(-base, -base);
+        uint64_t sum0 = 0, sum1 = 0;
+#pragma unroll
+        for (int c = 0; c < 128; c += 64) {
+          float p[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            float x, y;
+            f2_unpack(f2_fma(f2_pack(s[c + 2 * e], s[c + 2 * e + 1]), sc, nb), x, y);
+            x = ex2f(x);
+            y = ex2f(y);
+            if (e & 1) sum1 = f2_add(sum1, f2_pack(x, y));
+            else sum0 = f2_add(sum0, f2_pack(x, y));
+            p[e] = __uint_as_float(pack_bf16(x, y));
+          }
+          tmem_st32(S + c / 2, p);
+        }
+        float x, y;
+        f2_unpack(f2_add(sum0, sum1), x, y);
+        l += x + y;
+        tmem_wait_st();
+        tc_fence_before_sync();
+        mbar_arrive(bar(L::B_P + i));
+      }
+      if (ok && n > 0) ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_O + i), seq & 1, s_abort, f.limit));
       if (!ok) break;
       tc_fence_after_sync();
-      const int j0 = j_first + it * 128;
-      float s[128];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32(S + c * 32, s + c * 32);
-      tmem_wait_ld();
-      if constexpr (GENERAL) {
-        const float dist0 = (float)(t + a.mask.off - j0);
-        if (a.cap > 0.f) {
-          cap_scores(s, a.scale * inv_cap, a.cap * LOG2E);
-        } else {
-#pragma unroll
-          for (int c = 0; c < 128; ++c) s[c] *= scale2;
-        }
-        if (a.slopes) {
-#pragma unroll
-          for (int c = 0; c < 128; ++c) s[c] = fmaf(-slope2, fabsf(dist0 - (float)c), s[c]);
-        }
-      }
-      if (!__all_sync(0xffffffffu, iv.x <= j0 && iv.y >= j0 + 128)) {
-        const int rel = iv.x - j0;
-        const uint32_t len = (uint32_t)(iv.y - iv.x);
-#pragma unroll
-        for (int c = 0; c < 128; ++c)
-          if ((uint32_t)(c - rel) >= len) s[c] = -INFINITY;
-      }
-      float mx0 = s[0], mx1 = s[1], mx2 = s[2], mx3 = s[3];
-#pragma unroll
-      for (int c = 4; c < 128; c += 4) {
-        mx0 = fmaxf(mx0, s[c]);
-        mx1 = fmaxf(mx1, s[c + 1]);
-        mx2 = fmaxf(mx2, s[c + 2]);
-        mx3 = fmaxf(mx3, s[c + 3]);
-      }
-      float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
-      if constexpr (!GENERAL) mx *= scale2;
-      const bool grow = mx > m + RESCALE || (m == -INFINITY && mx > m);
-      if (__any_sync(0xffffffffu, grow)) {
-        const float base = grow ? mx : m, factor = m == -INFINITY ? 0.f : ex2f(m - base);
-        if (it > 0) {
-#pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
-            float o[32];
-            tmem_ld32(O + c, o);
-            tmem_wait_ld();
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] *= factor;
-            tmem_st32(O + c, o);
-          }
-          tmem_wait_st();
-        }
-        l *= factor;
-        m = base;
-      }
-      const float base = m == -INFINITY ? 0.f : m;
-      const uint64_t sc = f2_pack(GENERAL ? 1.f : scale2, GENERAL ? 1.f : scale2), nb = f2_pack(-base, -base);
-      uint64_t sum0 = 0, sum1 = 0;
-#pragma unroll
-      for (int c = 0; c < 128; c += 64) {
-        float w[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          float x, y;
-          f2_unpack(f2_fma(f2_pack(s[c + 2 * e], s[c + 2 * e + 1]), sc, nb), x, y);
-          x = ex2f(x);
-          y = ex2f(y);
-          if (e & 1) sum1 = f2_add(sum1, f2_pack(x, y));
-          else sum0 = f2_add(sum0, f2_pack(x, y));
-          w[e] = __uint_as_float(pack_bf16(x, y));
-        }
-        tmem_st32(S + c / 2, w);
-      }
-      float x, y;
-      f2_unpack(f2_add(sum0, sum1), x, y);
-      l += x + y;
-      tmem_wait_st();
-      tc_fence_before_sync();
-      mbar_arrive(bar(L::B_P + i));
-    }
-    if (ok && n > 0) ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_O + i), 0, s_abort, f.limit));
-    if (ok) {
-      tc_fence_after_sync();
-      const size_t row = ((size_t)b * T + t) * a.H + h;                                           // of [B, T, H]
-      const size_t prow = (((size_t)part * a.B + b) * a.H + h) * (size_t)T + t;                   // of [parts, B, H, T]
+      const size_t row = ((size_t)w.b * T + t) * a.H + h;                                           // of [B, T, H]
+      const size_t prow = (((size_t)w.part * a.B + w.b) * a.H + h) * (size_t)T + t;                 // of [parts, B, H, T]
       const float inv = f.parts > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
-      bool bad = false;
+      float test = l * 0.f;
 #pragma unroll 1
       for (int c = 0; c < D; c += 32) {
         float o[32];
@@ -277,13 +342,15 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0.f;
         }
-        float test = 0.f;
+        if (c + 32 == D && n > 0) {
+          tc_fence_before_sync();
+          mbar_arrive(bar(L::B_OE + i));
+        }
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
           o[e] *= inv;
           test = fmaf(o[e], 0.f, test);
         }
-        bad |= !(test == 0.f);
         if (valid) {
           if (f.parts > 1) {
             float4* dst = reinterpret_cast<float4*>(f.part_o + prow * D + c);
@@ -301,8 +368,9 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       if (valid) {
         if (f.parts > 1) f.part_ml[prow] = make_float2(m, l);
         else if (a.lse) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
-        if (bad || !(l * 0.f == 0.f)) s_flags[2 + 0] = 1;
       }
+      if (__any_sync(0xffffffffu, valid && !(test == 0.f)) && lane == 0) note_bad(s_list, (int*)(s_flags + 2), idx);
+      if (n > 0) ++seq;
     }
   }
   __syncthreads();
@@ -313,13 +381,16 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   tc_fence_before_sync();
   __syncthreads();
   if (warp == NT * 4) tmem_dealloc(tmem, L::COLS);
-  const bool again = s_flags[2] && !*s_abort;
-  __syncthreads();                                     // (the flags lie in the shared memory that is used again)
-  if (again && tid < 128) {
-    const size_t pb = ((size_t)part * a.B + b) * a.H;
+  const int bad = *s_abort ? 0 : s_flags[2];
+  if (!bad || tid >= 128) return;
+  for (int r = 0; r < rounds; ++r) {
+    const int idx = index_of(r);
+    if (idx >= f.items || !is_bad(s_list, bad, idx)) continue;
+    const Item w = item_of(idx);
+    const size_t pb = ((size_t)w.part * a.B + w.b) * a.H;
     for (int i = 0; i < NT; ++i) {
-      const size_t at = (pb + head_of(i)) * (size_t)T;
-      fwd_again<D>(a, reinterpret_cast<float*>(smem), b, head_of(i), row_of(i), f.parts > 1 ? j_first : 0, f.parts > 1 ? j_end : a.mask.T_k,
+      const size_t at = (pb + head_of(w, i)) * (size_t)T;
+      fwd_again<D>(a, reinterpret_cast<float*>(smem), w.b, head_of(w, i), row_of(w, i), f.parts > 1 ? w.j_first : 0, f.parts > 1 ? w.j_end : a.mask.T_k,
                    f.parts > 1 ? f.part_o + at * D : nullptr, f.parts > 1 ? f.part_ml + at : nullptr);
     }
   }
@@ -360,9 +431,9 @@ struct FwdPlan {
   int nt, two_heads, tiles, pairs, parts;
   long long blocks;
 };
-static FwdPlan fwd_plan(int B, int H, int H_kv, int T, int T_k, int window, int d) {
+static FwdPlan fwd_plan(int B, int H, int H_kv, int T, int T_k, int window) {
   FwdPlan p;
-  p.nt = d == 128 ? 2 : 2;
+  p.nt = 2;
   p.two_heads = p.nt == 2 && (H / H_kv) % 2 == 0;
   const int rows = p.nt == 2 && !p.two_heads ? 256 : 128;
   p.tiles = (T + rows - 1) / rows;
@@ -384,7 +455,7 @@ static int fwd_tc(const AttnCall& c, const FwdPlan& pl, void* ws) {
   if (!tensor_map(&tq, a.q, false, a.H, a.mask.T, a.B, D, 64, 128, true) || !tensor_map(&tk, a.k, false, a.H_kv, a.mask.T_k, a.B, D, 64, 128, true) ||
       !tensor_map(&tv, a.v, false, a.H_kv, a.mask.T_k, a.B, D, 64, 128, true))
     return LAWCAT_ERR_CUDA;
-  FwdArgs f{a, pl.pairs, pl.tiles, pl.two_heads, pl.parts, nullptr, nullptr, wait_limit()};
+  FwdArgs f{a, pl.pairs, pl.tiles, (int)pl.blocks, pl.two_heads, pl.parts, nullptr, nullptr, wait_limit()};
   const size_t rows = (size_t)a.B * a.H * a.mask.T * pl.parts;
   if (pl.parts > 1) {
     f.part_o = (float*)ws;
@@ -397,7 +468,7 @@ static int fwd_tc(const AttnCall& c, const FwdPlan& pl, void* ws) {
     note_cuda_error(e, __FILE__, __LINE__);
     return LAWCAT_ERR_CUDA;
   }
-  LAWCAT_LAUNCH("attn_fwd_tc", c.stream, kernel<<<(unsigned)pl.blocks, L::THREADS, L::BYTES, c.stream>>>(tq, tk, tv, f));
+  LAWCAT_LAUNCH("attn_fwd_tc", c.stream, kernel<<<(unsigned)std::min<long long>(pl.blocks, sm_count()), L::THREADS, L::BYTES, c.stream>>>(tq, tk, tv, f));
   LAWCAT_CHECK_LAUNCH();
   if (pl.parts > 1) {
     const size_t n = (size_t)a.B * a.H * a.mask.T;
@@ -412,7 +483,7 @@ static int fwd_tc(const AttnCall& c, const FwdPlan& pl, void* ws) {
 bool attn_tc_supported(int dtype, int d, int exact) { return dtype == LAWCAT_BF16 && (d == 64 || d == 128) && !exact; }
 
 size_t attn_fwd_tc_workspace_bytes(int B, int H, int H_kv, int T, int T_k, int window, int d) {
-  const attn::FwdPlan p = attn::fwd_plan(B, H, H_kv, T, T_k, window, d);
+  const attn::FwdPlan p = attn::fwd_plan(B, H, H_kv, T, T_k, window);
   if (p.parts == 1) return 0;
   const size_t rows = (size_t)B * H * T * p.parts;
   return align_up(rows * d * sizeof(float), 256) + align_up(rows * sizeof(float2), 256);
@@ -421,7 +492,7 @@ size_t attn_fwd_tc_workspace_bytes(int B, int H, int H_kv, int T, int T_k, int w
 int launch_attn_fwd_tc(const AttnCall& c, void* ws) {
   const attn::Args& a = c.a;
   if (a.mask.T_k == 0) return launch_attn_fwd_exact(c);
-  const attn::FwdPlan p = attn::fwd_plan(a.B, a.H, a.H_kv, a.mask.T, a.mask.T_k, a.mask.window, c.d);
+  const attn::FwdPlan p = attn::fwd_plan(a.B, a.H, a.H_kv, a.mask.T, a.mask.T_k, a.mask.window);
   if (p.blocks > 0x7fffffffLL || (long long)a.B * a.H * a.mask.T / 8 >= 0x7fffffffLL) return LAWCAT_ERR_UNSUPPORTED;
   const bool general = a.cap > 0.f || a.slopes || !(a.scale > 0.f);
   if (c.d == 128) return general ? attn::fwd_tc<128, 2, true>(c, p, ws) : attn::fwd_tc<128, 2, false>(c, p, ws);

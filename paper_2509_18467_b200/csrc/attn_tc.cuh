@@ -52,6 +52,19 @@ __device__ __forceinline__ uint64_t mdesc(uint32_t tile, int kk) {
   return smem_desc(tile + (uint32_t)kk * 2048, ROWS * 128, 1024, LAYOUT_SW128);
 }
 
+// Items of a block that came out not finite, for a second computation behind everything else; more than the list holds: all of them.
+constexpr int BAD_MAX = 64;
+__device__ __forceinline__ void note_bad(int* list, int* count, int idx) {
+  const int at = atomicAdd(count, 1);
+  if (at < BAD_MAX) list[at] = idx;
+}
+__device__ __forceinline__ bool is_bad(const int* list, int count, int idx) {
+  if (count > BAD_MAX) return true;
+  for (int i = 0; i < count; ++i)
+    if (list[i] == idx) return true;
+  return false;
+}
+
 // s <- c2 tanh(s k) for N scores of a thread (all 32 lanes of a warp together). While no |s k| of the warp passes 0.8, tanh is y P(y^2)
 // with P of degree 5 on the FMA pipe (a least-maximum fit of tanh(y) / y over [0, 0.8], relative error 5e-8, 2e-7 with its fp32
 // arithmetic): the two special functions of the other form would be three times the whole softmax's load on their pipe.
