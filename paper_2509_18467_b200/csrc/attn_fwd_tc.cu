@@ -27,7 +27,8 @@ constexpr float RESCALE = 8.f;
 
 struct FwdArgs {
   Args a;
-  int pairs;          // items per (batch, query tile): H / 2 head pairs, or H
+  FastDiv pairs;      // items per (batch, query tile): H / 2 head pairs, or H
+  FastDiv bp, group, parts_d;   // B pairs, H / H_kv, parts
   int tiles;          // query tiles
   int items;
   int two_heads;      // an item's two tiles are two heads (else two neighbouring tiles of one head)
@@ -41,13 +42,14 @@ template <int D, int NT>
 struct FwdLay {
   static constexpr uint32_t TILE = 128 * D * 2;                  // a Q, K or V tile
   static constexpr int ST = D == 128 ? 4 : 8;                    // stages of the ring (K and V tiles alternate)
-  static constexpr uint32_t OFF_Q = 0, OFF_RING = NT * TILE, OFF_LIST = OFF_RING + ST * TILE, OFF_BAR = OFF_LIST + BAD_MAX * 4;
+  static constexpr uint32_t OUT = 128 * 128;                     // a warpgroup's outputs on their way: 64 channels (or 32 in fp32)
+  static constexpr uint32_t OFF_Q = 0, OFF_RING = NT * TILE, OFF_OUT = OFF_RING + ST * TILE, OFF_LIST = OFF_OUT + NT * OUT, OFF_BAR = OFF_LIST + BAD_MAX * 4;
   static constexpr uint32_t BYTES0 = OFF_BAR + 256;
   static constexpr uint32_t BYTES = BYTES0;
   static constexpr uint32_t COLS = NT * (128 + D) > 256 ? 512 : 256;
-  static constexpr int THREADS = NT * 128 + 64;
+  static constexpr int THREADS = NT * 128 + 128;
   // mbarriers
-  static constexpr int B_Q = 0, B_QE = 1, B_FULL = 2, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + NT, B_O = B_P + NT, B_OE = B_O + NT,
+  static constexpr int B_Q = 0, B_QE = 1, B_FULL = 2, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + NT, B_O = B_P + 2 * NT, B_OE = B_O + NT,
                        NBAR = B_OE + NT;
   static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 256 && fwd_smem<D, 4, 128>() <= OFF_LIST, "shared memory");
 };
@@ -61,7 +63,7 @@ __device__ __noinline__ void fwd_again(const Args& a, float* sm, int b, int h, i
 template <int D, int NT, bool GENERAL>
 __global__ void __launch_bounds__(FwdLay<D, NT>::THREADS, NT == 2 ? 1 : 2)
 attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                   const __grid_constant__ FwdArgs f) {
+                   const __grid_constant__ CUtensorMap tm_o, const __grid_constant__ FwdArgs f) {
   using L = FwdLay<D, NT>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const Args& a = f.a;
@@ -76,15 +78,15 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   struct Item {
     int part, b, h0, g, tb, j_first, j_end, n;
   };
-  const int T = a.mask.T, per_tile = a.B * f.pairs * f.parts;
+  const int T = a.mask.T;
   auto item_of = [&](int idx) {
     Item w;
-    w.part = idx % f.parts;
-    const int bp = idx / f.parts % (a.B * f.pairs), tile = f.tiles - 1 - idx / per_tile;   // (under a causal mask the longest rows first)
-    w.b = bp / f.pairs;
-    w.h0 = bp % f.pairs * (f.two_heads ? 2 : 1);
-    w.g = w.h0 / (a.H / a.H_kv);
-    w.tb = tile * (f.two_heads || NT == 1 ? 128 : 256);                                    // first query
+    const int q = quot(idx, f.parts_d), tile = quot(q, f.bp), bp = rest(q, tile, f.bp);
+    w.part = rest(idx, q, f.parts_d);
+    w.b = quot(bp, f.pairs);
+    w.h0 = rest(bp, w.b, f.pairs) * (f.two_heads ? 2 : 1);
+    w.g = quot(w.h0, f.group);
+    w.tb = (f.tiles - 1 - tile) * (f.two_heads || NT == 1 ? 128 : 256);                    // first query (under a causal mask the longest rows first)
     const int t_last = min(T, w.tb + (f.two_heads ? 128 : 128 * NT)) - 1;
     w.j_first = interval(a.mask, w.b, w.tb).x;
     w.j_end = interval(a.mask, w.b, t_last).y;
@@ -112,7 +114,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     }
     for (int i = 0; i < NT; ++i) {
       mbar_init(bar(L::B_S + i), 1);
-      mbar_init(bar(L::B_P + i), 128);
+      mbar_init(bar(L::B_P + 2 * i), 128);
+      mbar_init(bar(L::B_P + 2 * i + 1), 128);
       mbar_init(bar(L::B_O + i), 1);
       mbar_init(bar(L::B_OE + i), 128);
     }
@@ -134,7 +137,9 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   auto s_col = [&](int i) { return tmem + (uint32_t)i * 128u; };
   auto o_col = [&](int i) { return tmem + (uint32_t)(NT * 128 + i * D); };
 
-  if (warp == NT * 4) {
+  if (warp >= NT * 4) {
+    regs_few();
+    if (warp == NT * 4) {
     // ------------------------------------------------------------------------------------------------ copies
     if (elect_one()) {
       int at = 0, seq = 0;   // tiles and items so far
@@ -158,7 +163,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         ++seq;
       }
     }
-  } else if (warp == NT * 4 + 1) {
+    } else if (warp == NT * 4 + 1) {
     // ------------------------------------------------------------------------------------------------ products
     if (elect_one()) {
       constexpr uint32_t id_s = instr_desc(128, 128, FMT_BF16, MAJOR_K, MAJOR_K);
@@ -204,11 +209,15 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           for (int i = 0; i < NT && ok; ++i) {
             if (i == 0) ok = full(2 * step + 1);
             if (ok && it == 0 && seq > 0) ok = wait_bar(bar(L::B_OE + i), (seq - 1) & 1, s_abort, f.limit);
-            if (ok) ok = wait_bar(bar(L::B_P + i), step & 1, s_abort, f.limit);
-            if (!ok) break;
-            tc_fence_after_sync();
+            for (int u = 0; u < 2 && ok; ++u) {   // (the first half of the keys' weights come first)
+              ok = wait_bar(bar(L::B_P + 2 * i + u), step & 1, s_abort, f.limit);
+              if (!ok) break;
+              tc_fence_after_sync();
 #pragma unroll
-            for (int kk = 0; kk < 8; ++kk) mma_ts(o_col(i), s_col(i) + kk * 8, mdesc<128>(stage(2 * step + 1), kk), id_o, (it | kk) != 0);
+              for (int kk = 0; kk < 4; ++kk)
+                mma_ts(o_col(i), s_col(i) + u * 32 + kk * 8, mdesc<128>(stage(2 * step + 1), u * 4 + kk), id_o, (it | u | kk) != 0);
+            }
+            if (!ok) break;
             if (i == NT - 1) mma_commit(bar(L::B_EMPTY + (2 * step + 1) % L::ST));
             if (it + 1 == n) mma_commit(bar(L::B_O + i));
             if (more) {
@@ -226,7 +235,9 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         ++seq;
       }
     }
+    }
   } else {
+    regs_many();
     // ------------------------------------------------------------------------------------------------ softmax
     const int i = warp >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -239,7 +250,10 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       const Item w = item_of(idx);
       const int n = w.n, h = head_of(w, i), t = row_of(w, i) + (tid & 127);
       const bool valid = t < T;
-      const int2 iv = valid ? interval(a.mask, w.b, t) : make_int2(0, 0x7fffffff);   // (rows behind the last are never stored)
+      const int2 iv = interval(a.mask, w.b, valid ? t : T - 1);   // (rows behind the last are never stored)
+      // what the warp's rows see in all: [lo0, hi1), of which every row sees [lo1, hi0)
+      const int lo0 = __shfl_sync(0xffffffffu, iv.x, 0), lo1 = __shfl_sync(0xffffffffu, iv.x, 31);
+      const int hi0 = __shfl_sync(0xffffffffu, iv.y, 0), hi1 = __shfl_sync(0xffffffffu, iv.y, 31);
       const float slope2 = GENERAL && a.slopes ? a.slopes[h] * LOG2E : 0.f;
       float m = -INFINITY, l = 0.f;
       bool ok = true;
@@ -249,11 +263,13 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         tc_fence_after_sync();
         const int j0 = w.j_first + it * 128;
         float s[128];
+        // quarters of the tile that no row of the warp sees take no part: their weights are zero
+        auto met = [&](int c) { return j0 + c < hi1 && j0 + c + 32 > lo0; };
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(S + c * 32, s + c * 32);
+        for (int c = 0; c < 128; c += 32) tmem_ld32(S + c, s + c);
         tmem_wait_ld();
+        const bool low = lo1 > j0, high = hi0 < j0 + 128, whole = !low && !high;   // (the same for the warp)
         if constexpr (GENERAL) {
-          const float dist0 = (float)(t + a.mask.off - j0);
           if (a.cap > 0.f) {
             cap_scores(s, a.scale * inv_cap, a.cap * LOG2E);
           } else {
@@ -261,26 +277,37 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             for (int c = 0; c < 128; ++c) s[c] *= scale2;
           }
           if (a.slopes) {
+            const float dist0 = (float)(t + a.mask.off - j0);
 #pragma unroll
             for (int c = 0; c < 128; ++c) s[c] = fmaf(-slope2, fabsf(dist0 - (float)c), s[c]);
           }
         }
-        if (!__all_sync(0xffffffffu, iv.x <= j0 && iv.y >= j0 + 128)) {
-          const int rel = iv.x - j0;
-          const uint32_t len = (uint32_t)(iv.y - iv.x);
+        float mx0 = -INFINITY, mx1 = -INFINITY;
+        if (whole) {
 #pragma unroll
-          for (int c = 0; c < 128; ++c)
-            if ((uint32_t)(c - rel) >= len) s[c] = -INFINITY;
-        }
-        float mx0 = s[0], mx1 = s[1], mx2 = s[2], mx3 = s[3];
+          for (int c = 0; c < 128; c += 4) {
+            mx0 = fmaxf(fmaxf(mx0, s[c]), s[c + 1]);
+            mx1 = fmaxf(fmaxf(mx1, s[c + 2]), s[c + 3]);
+          }
+        } else {
+          const int rl = iv.x - j0, rh = iv.y - j0;
 #pragma unroll
-        for (int c = 4; c < 128; c += 4) {
-          mx0 = fmaxf(mx0, s[c]);
-          mx1 = fmaxf(mx1, s[c + 1]);
-          mx2 = fmaxf(mx2, s[c + 2]);
-          mx3 = fmaxf(mx3, s[c + 3]);
+          for (int c0 = 0; c0 < 128; c0 += 32) {
+            if (!met(c0)) continue;
+            if (low && lo1 > j0 + c0)
+#pragma unroll
+              for (int c = c0; c < c0 + 32; ++c) s[c] = c < rl ? -INFINITY : s[c];
+            if (high && hi0 < j0 + c0 + 32)
+#pragma unroll
+              for (int c = c0; c < c0 + 32; ++c) s[c] = c >= rh ? -INFINITY : s[c];
+#pragma unroll
+            for (int c = c0; c < c0 + 32; c += 4) {
+              mx0 = fmaxf(fmaxf(mx0, s[c]), s[c + 1]);
+              mx1 = fmaxf(fmaxf(mx1, s[c + 2]), s[c + 3]);
+            }
+          }
         }
-        float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
+        float mx = fmaxf(mx0, mx1);
         if constexpr (!GENERAL) mx *= scale2;
         const bool grow = mx > m + RESCALE || (m == -INFINITY && mx > m);
         if (__any_sync(0xffffffffu, grow)) {
@@ -303,35 +330,65 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const float base = m == -INFINITY ? 0.f : m;
         const uint64_t sc = f2_pack(GENERAL ? 1.f : scale2, GENERAL ? 1.f : scale2), nb = f2_pack(-base, -base);
         uint64_t sum0 = 0, sum1 = 0;
+        // every fourth pair of a tile that all rows see whole takes its exponentials on the FMA pipe: the special functions' pipe is
+        // what a tile waits for (below -126 and for -infinity the two differ, so not where keys are hidden)
+        auto quarter = [&](auto first, auto mixed) {   // 32 scores from column `first` on: the weights, two to a register, in their place
+          constexpr int c = decltype(first)::value;
 #pragma unroll
-        for (int c = 0; c < 128; c += 64) {
-          float p[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) {
+          for (int e = 0; e < 16; ++e) {
+            const uint64_t z = f2_fma(f2_pack(s[c + 2 * e], s[c + 2 * e + 1]), sc, nb);
             float x, y;
-            f2_unpack(f2_fma(f2_pack(s[c + 2 * e], s[c + 2 * e + 1]), sc, nb), x, y);
-            x = ex2f(x);
-            y = ex2f(y);
+            if (decltype(mixed)::value && (e & 3) == 3) {
+              ex2_pair(z, x, y);
+            } else {
+              f2_unpack(z, x, y);
+              x = ex2f(x);
+              y = ex2f(y);
+            }
             if (e & 1) sum1 = f2_add(sum1, f2_pack(x, y));
             else sum0 = f2_add(sum0, f2_pack(x, y));
-            p[e] = __uint_as_float(pack_bf16(x, y));
+            s[c / 64 * 64 + c % 64 / 2 + e] = __uint_as_float(pack_bf16(x, y));
           }
-          tmem_st32(S + c / 2, p);
-        }
-        float x, y;
-        f2_unpack(f2_add(sum0, sum1), x, y);
-        l += x + y;
-        tmem_wait_st();
-        tc_fence_before_sync();
-        mbar_arrive(bar(L::B_P + i));
+        };
+        auto hidden = [&](auto first) {
+          constexpr int c = decltype(first)::value;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[c / 64 * 64 + c % 64 / 2 + e] = 0.f;
+        };
+        auto half = [&](auto first) {
+          constexpr int c = decltype(first)::value;
+          using A = std::integral_constant<int, c>;
+          using B = std::integral_constant<int, c + 32>;
+          if (whole) {
+            quarter(A{}, std::true_type{});
+            quarter(B{}, std::true_type{});
+          } else {
+            if (met(c)) quarter(A{}, std::false_type{}); else hidden(A{});
+            if (met(c + 32)) quarter(B{}, std::false_type{}); else hidden(B{});
+          }
+          tmem_st32(S + c / 2, s + c);
+          if (c == 64) {
+            float x, y;
+            f2_unpack(f2_add(sum0, sum1), x, y);
+            l += x + y;
+          }
+          tmem_wait_st();
+          tc_fence_before_sync();
+          mbar_arrive(bar(L::B_P + 2 * i + c / 64));
+        };
+        half(std::integral_constant<int, 0>{});
+        half(std::integral_constant<int, 64>{});
       }
       if (ok && n > 0) ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_O + i), seq & 1, s_abort, f.limit));
-      if (!ok) break;
+      if (named_bar_or(2 + i, 128, !ok)) break;   // (all four warps go on, or none)
       tc_fence_after_sync();
-      const size_t row = ((size_t)w.b * T + t) * a.H + h;                                           // of [B, T, H]
-      const size_t prow = (((size_t)w.part * a.B + w.b) * a.H + h) * (size_t)T + t;                 // of [parts, B, H, T]
+      const size_t row = ((size_t)w.b * T + t) * a.H + h;                                                // of [B, T, H]
+      const size_t prow0 = (((size_t)w.part * a.B + w.b) * a.H + h) * (size_t)T + row_of(w, i), prow = prow0 + (tid & 127);  // of [parts, B, H, T]
       const float inv = f.parts > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
       float test = l * 0.f;
+      // outputs through shared memory: 64 channels at a time by the copy engine (which leaves out rows behind the last), or 32 in fp32
+      const uint32_t out = sb + L::OFF_OUT + i * L::OUT;
+      const int r128 = tid & 127, rows = min(128, T - row_of(w, i));
 #pragma unroll 1
       for (int c = 0; c < D; c += 32) {
         float o[32];
@@ -351,17 +408,33 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           o[e] *= inv;
           test = fmaf(o[e], 0.f, test);
         }
-        if (valid) {
-          if (f.parts > 1) {
-            float4* dst = reinterpret_cast<float4*>(f.part_o + prow * D + c);
+        if (f.parts > 1) {
+          named_bar_sync(2 + i, 128);   // (the last quarter is out of shared memory)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-          } else {
-            uint4* dst = reinterpret_cast<uint4*>((bf16*)a.o + row * D + c);
+          for (int e = 0; e < 8; ++e)
+            sts128(out + sw128(r128, e), make_uint4(__float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]), __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3])));
+          named_bar_sync(2 + i, 128);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              dst[e] = make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]), pack_bf16(o[8 * e + 4], o[8 * e + 5]),
-                                  pack_bf16(o[8 * e + 6], o[8 * e + 7]));
+          for (int e = 0; e < 8; ++e) {
+            const int k = e * 16 + (r128 >> 3);
+            if (k < rows) *reinterpret_cast<uint4*>(f.part_o + (prow0 + k) * D + c + (r128 & 7) * 4) = lds128(out + sw128(k, r128 & 7));
+          }
+        } else {
+          if (c % 64 == 0) {
+            if (r128 == 0) tma_store_wait_read();
+            named_bar_sync(2 + i, 128);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sts128(out + sw128(r128, c / 8 % 8 + e), make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]),
+                                                              pack_bf16(o[8 * e + 4], o[8 * e + 5]), pack_bf16(o[8 * e + 6], o[8 * e + 7])));
+          if (c % 64 == 32) {
+            fence_proxy_async();
+            named_bar_sync(2 + i, 128);
+            if (r128 == 0 && rows > 0) {
+              tma_store_4d(&tm_o, out, c - 32, h, row_of(w, i), w.b);
+              tma_store_commit();
+            }
           }
         }
       }
@@ -372,6 +445,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       if (__any_sync(0xffffffffu, valid && !(test == 0.f)) && lane == 0) note_bad(s_list, (int*)(s_flags + 2), idx);
       if (n > 0) ++seq;
     }
+    if ((tid & 127) == 0) tma_store_wait_all();
   }
   __syncthreads();
   if (*s_abort) {
@@ -451,11 +525,11 @@ template <int D, int NT, bool GENERAL>
 static int fwd_tc(const AttnCall& c, const FwdPlan& pl, void* ws) {
   using L = FwdLay<D, NT>;
   const Args& a = c.a;
-  CUtensorMap tq, tk, tv;
+  CUtensorMap tq, tk, tv, to;
   if (!tensor_map(&tq, a.q, false, a.H, a.mask.T, a.B, D, 64, 128, true) || !tensor_map(&tk, a.k, false, a.H_kv, a.mask.T_k, a.B, D, 64, 128, true) ||
-      !tensor_map(&tv, a.v, false, a.H_kv, a.mask.T_k, a.B, D, 64, 128, true))
+      !tensor_map(&tv, a.v, false, a.H_kv, a.mask.T_k, a.B, D, 64, 128, true) || !tensor_map(&to, a.o, false, a.H, a.mask.T, a.B, D, 64, 128, true))
     return LAWCAT_ERR_CUDA;
-  FwdArgs f{a, pl.pairs, pl.tiles, (int)pl.blocks, pl.two_heads, pl.parts, nullptr, nullptr, wait_limit()};
+  FwdArgs f{a, fast_div(pl.pairs), fast_div(a.B * pl.pairs), fast_div(a.H / a.H_kv), fast_div(pl.parts), pl.tiles, (int)pl.blocks, pl.two_heads, pl.parts, nullptr, nullptr, wait_limit()};
   const size_t rows = (size_t)a.B * a.H * a.mask.T * pl.parts;
   if (pl.parts > 1) {
     f.part_o = (float*)ws;
@@ -468,7 +542,7 @@ static int fwd_tc(const AttnCall& c, const FwdPlan& pl, void* ws) {
     note_cuda_error(e, __FILE__, __LINE__);
     return LAWCAT_ERR_CUDA;
   }
-  LAWCAT_LAUNCH("attn_fwd_tc", c.stream, kernel<<<(unsigned)std::min<long long>(pl.blocks, sm_count()), L::THREADS, L::BYTES, c.stream>>>(tq, tk, tv, f));
+  LAWCAT_LAUNCH("attn_fwd_tc", c.stream, kernel<<<(unsigned)std::min<long long>(pl.blocks, sm_count()), L::THREADS, L::BYTES, c.stream>>>(tq, tk, tv, to, f));
   LAWCAT_CHECK_LAUNCH();
   if (pl.parts > 1) {
     const size_t n = (size_t)a.B * a.H * a.mask.T;
