@@ -1,14 +1,16 @@
 // Softmax attention forward on the tensor cores: bf16 storage, d = 64 or 128.
 //
 // An item is NT tiles of 128 queries that read the same key-value head (two query heads of a group at the same tokens, or
-// two neighbouring tiles of one head); a block walks their keys in tiles of 128:
+// two neighbouring tiles of one head); a block walks their keys in tiles of 64:
 //   warpgroup i < NT   softmax of tile i: one thread per query; S_i from tensor memory, mask / cap / bias, running maximum and
 //                      sum in registers, P_i = exp2(x - m) rounded to bf16 over S_i in tensor memory
 //   copy warp          Q tiles once, K and V tiles in turn through a ring of stages (TMA, 128-byte swizzle)
 //   product warp       S_i = Q_i K^T (both operands in shared memory), O_i += P_i V (P_i from tensor memory); fp32 accumulation
-// While one tile's softmax runs, the other tile's products do. The accumulator O_i is rescaled only when a row's maximum has
-// grown by more than 2^8 since it was last scaled (the weights then stay within 2^8 in fp32 and bf16 alike), by the softmax
-// warps themselves: between a tile's S being there and its P being ready no product touches O_i.
+// S_i has two places in tensor memory: the products of the next tile's scores run while this one is weighed, and a warpgroup finds
+// its next scores there (with tiles of 128 keys and one place, a warpgroup's chain was scores, weights, both products, and a pair of
+// tiles took 3300 cycles; tensor memory holds no second place of 128 columns beside two O of 128).
+// The accumulator O_i is rescaled only when a row's maximum has grown by more than 2^8 since it was last scaled (the weights then
+// stay within 2^8 in fp32 and bf16 alike), by the softmax warps themselves, behind the product of the tile in front.
 // One block per SM takes items in turn, the longest first: while an item's last tiles are weighed and its outputs stored, the next
 // one's queries and first keys are already on their way (a sequence of 1024 tokens has no more than eight key tiles per item, and
 // a block that starts and ends with each of them spent half its time so).
@@ -24,6 +26,7 @@ namespace lawcat {
 namespace attn {
 
 constexpr float RESCALE = 8.f;
+constexpr int NT = 2;   // query tiles of an item
 
 struct FwdArgs {
   Args a;
@@ -38,20 +41,18 @@ struct FwdArgs {
   long long limit;
 };
 
-template <int D, int NT>
+template <int D>
 struct FwdLay {
-  static constexpr uint32_t TILE = 128 * D * 2;                  // a Q, K or V tile
-  static constexpr int ST = D == 128 ? 4 : 8;                    // stages of the ring (K and V tiles alternate)
+  static constexpr uint32_t TILE = 128 * D * 2, KT = 64 * D * 2; // a Q tile; a K or V tile
+  static constexpr int ST = 8;                                   // stages of the ring (K and V tiles alternate)
   static constexpr uint32_t OUT = 128 * 128;                     // a warpgroup's outputs on their way: 64 channels (or 32 in fp32)
-  static constexpr uint32_t OFF_Q = 0, OFF_RING = NT * TILE, OFF_OUT = OFF_RING + ST * TILE, OFF_LIST = OFF_OUT + NT * OUT, OFF_BAR = OFF_LIST + BAD_MAX * 4;
-  static constexpr uint32_t BYTES0 = OFF_BAR + 256;
-  static constexpr uint32_t BYTES = BYTES0;
-  static constexpr uint32_t COLS = NT * (128 + D) > 256 ? 512 : 256;
-  static constexpr int THREADS = NT * 128 + 128;
+  static constexpr uint32_t OFF_Q = 0, OFF_RING = NT * TILE, OFF_OUT = OFF_RING + ST * KT, OFF_LIST = OFF_OUT + NT * OUT, OFF_BAR = OFF_LIST + BAD_MAX * 4;
+  static constexpr uint32_t BYTES = OFF_BAR + 512;
+  static constexpr int THREADS = NT * 128 + 64;
   // mbarriers
-  static constexpr int B_Q = 0, B_QE = 1, B_FULL = 2, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + NT, B_O = B_P + 2 * NT, B_OE = B_O + NT,
+  static constexpr int B_Q = 0, B_QE = 1, B_FULL = 2, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + 2 * NT, B_O = B_P + 2 * NT, B_OE = B_O + 2 * NT,
                        NBAR = B_OE + NT;
-  static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 256 && fwd_smem<D, 4, 128>() <= OFF_LIST, "shared memory");
+  static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 512 && fwd_smem<D, 4, 128>() <= OFF_LIST && NT * (128 + D) <= 512, "shared memory, tensor memory");
 };
 
 template <int D>
@@ -60,11 +61,11 @@ __device__ __noinline__ void fwd_again(const Args& a, float* sm, int b, int h, i
 }
 
 // GENERAL: a cap, a bias, or a scale that is not positive
-template <int D, int NT, bool GENERAL>
-__global__ void __launch_bounds__(FwdLay<D, NT>::THREADS, NT == 2 ? 1 : 2)
+template <int D, bool GENERAL>
+__global__ void __launch_bounds__(FwdLay<D>::THREADS, 1)
 attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                    const __grid_constant__ CUtensorMap tm_o, const __grid_constant__ FwdArgs f) {
-  using L = FwdLay<D, NT>;
+  using L = FwdLay<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const Args& a = f.a;
   const uint32_t sb = smem_u32(smem);
@@ -86,16 +87,16 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     w.b = quot(bp, f.pairs);
     w.h0 = rest(bp, w.b, f.pairs) * (f.two_heads ? 2 : 1);
     w.g = quot(w.h0, f.group);
-    w.tb = (f.tiles - 1 - tile) * (f.two_heads || NT == 1 ? 128 : 256);                    // first query (under a causal mask the longest rows first)
+    w.tb = (f.tiles - 1 - tile) * (f.two_heads ? 128 : 256);                    // first query (under a causal mask the longest rows first)
     const int t_last = min(T, w.tb + (f.two_heads ? 128 : 128 * NT)) - 1;
     w.j_first = interval(a.mask, w.b, w.tb).x;
     w.j_end = interval(a.mask, w.b, t_last).y;
-    w.n = w.j_end > w.j_first ? (w.j_end - w.j_first + 127) / 128 : 0;
+    w.n = w.j_end > w.j_first ? (w.j_end - w.j_first + 63) / 64 : 0;
     if (f.parts > 1) {
       const int per = (w.n + f.parts - 1) / f.parts, i0 = min(w.n, w.part * per);
       w.n = min(w.n - i0, per);
-      w.j_first += i0 * 128;
-      w.j_end = min(w.j_end, w.j_first + w.n * 128);
+      w.j_first += i0 * 64;
+      w.j_end = min(w.j_end, w.j_first + w.n * 64);
     }
     return w;
   };
@@ -113,10 +114,11 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       mbar_init(bar(L::B_EMPTY + i), 1);
     }
     for (int i = 0; i < NT; ++i) {
-      mbar_init(bar(L::B_S + i), 1);
-      mbar_init(bar(L::B_P + 2 * i), 128);
-      mbar_init(bar(L::B_P + 2 * i + 1), 128);
-      mbar_init(bar(L::B_O + i), 1);
+      for (int u = 0; u < 2; ++u) {
+        mbar_init(bar(L::B_S + 2 * i + u), 1);
+        mbar_init(bar(L::B_P + 2 * i + u), 128);
+        mbar_init(bar(L::B_O + 2 * i + u), 1);   // (a softmax warp may be two products ahead: a barrier of one phase bit would mislead it)
+      }
       mbar_init(bar(L::B_OE + i), 128);
     }
     s_flags[1] = 0;
@@ -127,18 +129,17 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     tma_prefetch_desc(&tm_v);
   }
   if (warp == NT * 4) {
-    tmem_alloc(sb + L::OFF_BAR + 8 * L::NBAR, L::COLS);
+    tmem_alloc(sb + L::OFF_BAR + 8 * L::NBAR, 512);
     tmem_relinquish();
   }
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = (uint32_t)s_flags[0];
-  auto s_col = [&](int i) { return tmem + (uint32_t)i * 128u; };
+  auto s_col = [&](int i, int step) { return tmem + (uint32_t)(i * 128 + (step & 1) * 64); };
   auto o_col = [&](int i) { return tmem + (uint32_t)(NT * 128 + i * D); };
 
   if (warp >= NT * 4) {
-    regs_few();
     if (warp == NT * 4) {
     // ------------------------------------------------------------------------------------------------ copies
     if (elect_one()) {
@@ -157,8 +158,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           const int s = at % L::ST;
           if (at >= L::ST) ok = wait_bar(bar(L::B_EMPTY + s), (at / L::ST - 1) & 1, s_abort, f.limit);
           if (!ok) break;
-          mbar_arrive_expect_tx(bar(L::B_FULL + s), L::TILE);
-          load_tile<D, 128>(sb + L::OFF_RING + s * L::TILE, it & 1 ? &tm_v : &tm_k, bar(L::B_FULL + s), w.g, w.j_first + it / 2 * 128, w.b);
+          mbar_arrive_expect_tx(bar(L::B_FULL + s), L::KT);
+          load_tile<D, 64>(sb + L::OFF_RING + s * L::KT, it & 1 ? &tm_v : &tm_k, bar(L::B_FULL + s), w.g, w.j_first + it / 2 * 64, w.b);
         }
         ++seq;
       }
@@ -166,20 +167,24 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     } else if (warp == NT * 4 + 1) {
     // ------------------------------------------------------------------------------------------------ products
     if (elect_one()) {
-      constexpr uint32_t id_s = instr_desc(128, 128, FMT_BF16, MAJOR_K, MAJOR_K);
+      constexpr uint32_t id_s = instr_desc(128, 64, FMT_BF16, MAJOR_K, MAJOR_K);
       constexpr uint32_t id_o = instr_desc(128, D, FMT_BF16, MAJOR_K, MAJOR_MN);
-      auto stage = [&](int at) { return sb + L::OFF_RING + (uint32_t)(at % L::ST) * L::TILE; };
+      auto stage = [&](int at) { return sb + L::OFF_RING + (uint32_t)(at % L::ST) * L::KT; };
       auto full = [&](int at) { return wait_bar(bar(L::B_FULL + at % L::ST), (at / L::ST) & 1, s_abort, f.limit); };
-      // S_i of the tile whose keys are ring tile `at`; `last`: of the item
-      auto scores = [&](int i, int at, bool last) {
+      // the scores of a step; `last`: of the item
+      auto scores = [&](int step, bool last) {
+        if (!full(2 * step)) return false;
+        tc_fence_after_sync();
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk)
-          mma_f16(s_col(i), kdesc<128>(sb + L::OFF_Q + i * L::TILE, kk), kdesc<128>(stage(at), kk), id_s, kk != 0);
-        mma_commit(bar(L::B_S + i));
-        if (i == NT - 1) {
-          mma_commit(bar(L::B_EMPTY + at % L::ST));
-          if (last) mma_commit(bar(L::B_QE));
+        for (int i = 0; i < NT; ++i) {
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            mma_f16(s_col(i, step), kdesc<128>(sb + L::OFF_Q + i * L::TILE, kk), kdesc<64>(stage(2 * step), kk), id_s, kk != 0);
+          mma_commit(bar(L::B_S + 2 * i + (step & 1)));
         }
+        mma_commit(bar(L::B_EMPTY + 2 * step % L::ST));
+        if (last) mma_commit(bar(L::B_QE));
+        return true;
       };
       auto next_item = [&](int& r) {   // tiles of the next item that has any; 0 behind the last
         for (; r < rounds; ++r) {
@@ -194,42 +199,25 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         return 0;
       };
       int r = 0, n = next_item(r), seq = 0, step = 0;   // step: key tiles so far
-      bool ok = true;
-      if (n) {
-        ok = wait_bar(bar(L::B_Q), 0, s_abort, f.limit) && full(0);
-        if (ok) {
-          tc_fence_after_sync();
-          for (int i = 0; i < NT; ++i) scores(i, 0, n == 1);
-        }
-      }
+      bool ok = n && wait_bar(bar(L::B_Q), 0, s_abort, f.limit) && scores(0, n == 1);
       while (n && ok) {
         const int n_next = next_item(r);
         for (int it = 0; it < n && ok; ++it, ++step) {
-          const bool more = it + 1 < n || n_next;
-          for (int i = 0; i < NT && ok; ++i) {
-            if (i == 0) ok = full(2 * step + 1);
-            if (ok && it == 0 && seq > 0) ok = wait_bar(bar(L::B_OE + i), (seq - 1) & 1, s_abort, f.limit);
-            for (int u = 0; u < 2 && ok; ++u) {   // (the first half of the keys' weights come first)
-              ok = wait_bar(bar(L::B_P + 2 * i + u), step & 1, s_abort, f.limit);
-              if (!ok) break;
-              tc_fence_after_sync();
+          if (it + 1 < n) ok = scores(step + 1, it + 2 == n);
+          if (ok) ok = full(2 * step + 1);
 #pragma unroll
-              for (int kk = 0; kk < 4; ++kk)
-                mma_ts(o_col(i), s_col(i) + u * 32 + kk * 8, mdesc<128>(stage(2 * step + 1), u * 4 + kk), id_o, (it | u | kk) != 0);
-            }
+          for (int i = 0; i < NT; ++i) {
+            if (ok && it == 0 && seq > 0) ok = wait_bar(bar(L::B_OE + i), (seq - 1) & 1, s_abort, f.limit);
+            if (ok) ok = wait_bar(bar(L::B_P + 2 * i + (step & 1)), (step >> 1) & 1, s_abort, f.limit);
             if (!ok) break;
-            if (i == NT - 1) mma_commit(bar(L::B_EMPTY + (2 * step + 1) % L::ST));
-            if (it + 1 == n) mma_commit(bar(L::B_O + i));
-            if (more) {
-              if (i == 0) {
-                if (it + 1 == n) ok = wait_bar(bar(L::B_Q), (seq + 1) & 1, s_abort, f.limit);
-                if (ok) ok = full(2 * step + 2);
-                if (!ok) break;
-                tc_fence_after_sync();
-              }
-              scores(i, 2 * step + 2, it + 1 < n ? it + 2 == n : n_next == 1);
-            }
+            tc_fence_after_sync();
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) mma_ts(o_col(i), s_col(i, step) + kk * 8, mdesc<64>(stage(2 * step + 1), kk), id_o, (it | kk) != 0);
+            mma_commit(bar(L::B_O + 2 * i + (step & 1)));
           }
+          if (!ok) break;
+          mma_commit(bar(L::B_EMPTY + (2 * step + 1) % L::ST));
+          if (it + 1 == n && n_next) ok = wait_bar(bar(L::B_Q), (seq + 1) & 1, s_abort, f.limit) && scores(step + 1, n_next == 1);
         }
         n = n_next;
         ++seq;
@@ -237,11 +225,10 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     }
     }
   } else {
-    regs_many();
     // ------------------------------------------------------------------------------------------------ softmax
     const int i = warp >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t S = s_col(i) + lanes, O = o_col(i) + lanes;
+    const uint32_t O = o_col(i) + lanes;
     const float scale2 = a.scale * LOG2E, inv_cap = GENERAL && a.cap > 0.f ? 1.f / a.cap : 0.f;
     int step = 0, seq = 0;
     for (int r = 0; r < rounds; ++r) {
@@ -258,41 +245,42 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       float m = -INFINITY, l = 0.f;
       bool ok = true;
       for (int it = 0; it < n; ++it, ++step) {
-        ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_S + i), step & 1, s_abort, f.limit));
+        ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_S + 2 * i + (step & 1)), (step >> 1) & 1, s_abort, f.limit));
         if (!ok) break;
         tc_fence_after_sync();
-        const int j0 = w.j_first + it * 128;
-        float s[128];
-        // quarters of the tile that no row of the warp sees take no part: their weights are zero
+        const int j0 = w.j_first + it * 64;
+        const uint32_t S = s_col(i, step) + lanes;
+        float s[64];
+        // halves of the tile that no row of the warp sees take no part: their weights are zero
         auto met = [&](int c) { return j0 + c < hi1 && j0 + c + 32 > lo0; };
 #pragma unroll
-        for (int c = 0; c < 128; c += 32) tmem_ld32(S + c, s + c);
+        for (int c = 0; c < 64; c += 32) tmem_ld32(S + c, s + c);
         tmem_wait_ld();
-        const bool low = lo1 > j0, high = hi0 < j0 + 128, whole = !low && !high;   // (the same for the warp)
+        const bool low = lo1 > j0, high = hi0 < j0 + 64, whole = !low && !high;   // (the same for the warp)
         if constexpr (GENERAL) {
           if (a.cap > 0.f) {
             cap_scores(s, a.scale * inv_cap, a.cap * LOG2E);
           } else {
 #pragma unroll
-            for (int c = 0; c < 128; ++c) s[c] *= scale2;
+            for (int c = 0; c < 64; ++c) s[c] *= scale2;
           }
           if (a.slopes) {
             const float dist0 = (float)(t + a.mask.off - j0);
 #pragma unroll
-            for (int c = 0; c < 128; ++c) s[c] = fmaf(-slope2, fabsf(dist0 - (float)c), s[c]);
+            for (int c = 0; c < 64; ++c) s[c] = fmaf(-slope2, fabsf(dist0 - (float)c), s[c]);
           }
         }
         float mx0 = -INFINITY, mx1 = -INFINITY;
         if (whole) {
 #pragma unroll
-          for (int c = 0; c < 128; c += 4) {
+          for (int c = 0; c < 64; c += 4) {
             mx0 = fmaxf(fmaxf(mx0, s[c]), s[c + 1]);
             mx1 = fmaxf(fmaxf(mx1, s[c + 2]), s[c + 3]);
           }
         } else {
           const int rl = iv.x - j0, rh = iv.y - j0;
 #pragma unroll
-          for (int c0 = 0; c0 < 128; c0 += 32) {
+          for (int c0 = 0; c0 < 64; c0 += 32) {
             if (!met(c0)) continue;
             if (low && lo1 > j0 + c0)
 #pragma unroll
@@ -313,6 +301,9 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         if (__any_sync(0xffffffffu, grow)) {
           const float base = grow ? mx : m, factor = m == -INFINITY ? 0.f : ex2f(m - base);
           if (it > 0) {
+            ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_O + 2 * i + (step - 1 & 1)), (step - 1) >> 1 & 1, s_abort, f.limit));   // (the product in front)
+            if (!ok) break;
+            tc_fence_after_sync();
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
               float o[32];
@@ -332,7 +323,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         uint64_t sum0 = 0, sum1 = 0;
         // every fourth pair of a tile that all rows see whole takes its exponentials on the FMA pipe: the special functions' pipe is
         // what a tile waits for (below -126 and for -infinity the two differ, so not where keys are hidden)
-        auto quarter = [&](auto first, auto mixed) {   // 32 scores from column `first` on: the weights, two to a register, in their place
+        auto weigh = [&](auto first, auto mixed) {   // 32 scores from column `first` on: the weights, two to a register, in their place
           constexpr int c = decltype(first)::value;
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
@@ -347,39 +338,37 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             }
             if (e & 1) sum1 = f2_add(sum1, f2_pack(x, y));
             else sum0 = f2_add(sum0, f2_pack(x, y));
-            s[c / 64 * 64 + c % 64 / 2 + e] = __uint_as_float(pack_bf16(x, y));
+            s[c / 2 + e] = __uint_as_float(pack_bf16(x, y));
           }
         };
-        auto hidden = [&](auto first) {
-          constexpr int c = decltype(first)::value;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[c / 64 * 64 + c % 64 / 2 + e] = 0.f;
-        };
-        auto half = [&](auto first) {
-          constexpr int c = decltype(first)::value;
-          using A = std::integral_constant<int, c>;
-          using B = std::integral_constant<int, c + 32>;
-          if (whole) {
-            quarter(A{}, std::true_type{});
-            quarter(B{}, std::true_type{});
+        using C0 = std::integral_constant<int, 0>;
+        using C32 = std::integral_constant<int, 32>;
+        if (whole) {
+          weigh(C0{}, std::true_type{});
+          weigh(C32{}, std::true_type{});
+        } else {
+          if (met(0)) {
+            weigh(C0{}, std::false_type{});
           } else {
-            if (met(c)) quarter(A{}, std::false_type{}); else hidden(A{});
-            if (met(c + 32)) quarter(B{}, std::false_type{}); else hidden(B{});
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = 0.f;
           }
-          tmem_st32(S + c / 2, s + c);
-          if (c == 64) {
-            float x, y;
-            f2_unpack(f2_add(sum0, sum1), x, y);
-            l += x + y;
+          if (met(32)) {
+            weigh(C32{}, std::false_type{});
+          } else {
+#pragma unroll
+            for (int e = 16; e < 32; ++e) s[e] = 0.f;
           }
-          tmem_wait_st();
-          tc_fence_before_sync();
-          mbar_arrive(bar(L::B_P + 2 * i + c / 64));
-        };
-        half(std::integral_constant<int, 0>{});
-        half(std::integral_constant<int, 64>{});
+        }
+        tmem_st32(S, s);
+        float x, y;
+        f2_unpack(f2_add(sum0, sum1), x, y);
+        l += x + y;
+        tmem_wait_st();
+        tc_fence_before_sync();
+        mbar_arrive(bar(L::B_P + 2 * i + (step & 1)));
       }
-      if (ok && n > 0) ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_O + i), seq & 1, s_abort, f.limit));
+      if (ok && n > 0) ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_O + 2 * i + (step - 1 & 1)), (step - 1) >> 1 & 1, s_abort, f.limit));
       if (named_bar_or(2 + i, 128, !ok)) break;   // (all four warps go on, or none)
       tc_fence_after_sync();
       const size_t row = ((size_t)w.b * T + t) * a.H + h;                                                // of [B, T, H]
@@ -454,7 +443,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   }
   tc_fence_before_sync();
   __syncthreads();
-  if (warp == NT * 4) tmem_dealloc(tmem, L::COLS);
+  if (warp == NT * 4) tmem_dealloc(tmem, 512);
   const int bad = *s_abort ? 0 : s_flags[2];
   if (!bad || tid >= 128) return;
   for (int r = 0; r < rounds; ++r) {
@@ -502,14 +491,13 @@ __global__ void __launch_bounds__(256) attn_fwd_join_kernel(const FwdArgs f) {
 }
 
 struct FwdPlan {
-  int nt, two_heads, tiles, pairs, parts;
+  int two_heads, tiles, pairs, parts;
   long long blocks;
 };
 static FwdPlan fwd_plan(int B, int H, int H_kv, int T, int T_k, int window) {
   FwdPlan p;
-  p.nt = 2;
-  p.two_heads = p.nt == 2 && (H / H_kv) % 2 == 0;
-  const int rows = p.nt == 2 && !p.two_heads ? 256 : 128;
+  p.two_heads = (H / H_kv) % 2 == 0;
+  const int rows = p.two_heads ? 128 : 256;
   p.tiles = (T + rows - 1) / rows;
   p.pairs = p.two_heads ? H / 2 : H;
   const long long blocks = (long long)B * p.pairs * p.tiles;
@@ -521,13 +509,13 @@ static FwdPlan fwd_plan(int B, int H, int H_kv, int T, int T_k, int window) {
   return p;
 }
 
-template <int D, int NT, bool GENERAL>
+template <int D, bool GENERAL>
 static int fwd_tc(const AttnCall& c, const FwdPlan& pl, void* ws) {
-  using L = FwdLay<D, NT>;
+  using L = FwdLay<D>;
   const Args& a = c.a;
   CUtensorMap tq, tk, tv, to;
-  if (!tensor_map(&tq, a.q, false, a.H, a.mask.T, a.B, D, 64, 128, true) || !tensor_map(&tk, a.k, false, a.H_kv, a.mask.T_k, a.B, D, 64, 128, true) ||
-      !tensor_map(&tv, a.v, false, a.H_kv, a.mask.T_k, a.B, D, 64, 128, true) || !tensor_map(&to, a.o, false, a.H, a.mask.T, a.B, D, 64, 128, true))
+  if (!tensor_map(&tq, a.q, false, a.H, a.mask.T, a.B, D, 64, 128, true) || !tensor_map(&tk, a.k, false, a.H_kv, a.mask.T_k, a.B, D, 64, 64, true) ||
+      !tensor_map(&tv, a.v, false, a.H_kv, a.mask.T_k, a.B, D, 64, 64, true) || !tensor_map(&to, a.o, false, a.H, a.mask.T, a.B, D, 64, 128, true))
     return LAWCAT_ERR_CUDA;
   FwdArgs f{a, fast_div(pl.pairs), fast_div(a.B * pl.pairs), fast_div(a.H / a.H_kv), fast_div(pl.parts), pl.tiles, (int)pl.blocks, pl.two_heads, pl.parts, nullptr, nullptr, wait_limit()};
   const size_t rows = (size_t)a.B * a.H * a.mask.T * pl.parts;
@@ -535,7 +523,7 @@ static int fwd_tc(const AttnCall& c, const FwdPlan& pl, void* ws) {
     f.part_o = (float*)ws;
     f.part_ml = (float2*)((char*)ws + align_up(rows * D * sizeof(float), 256));
   }
-  auto kernel = attn_fwd_tc_kernel<D, NT, GENERAL>;
+  auto kernel = attn_fwd_tc_kernel<D, GENERAL>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::BYTES);
   if (e != cudaSuccess) {
     cudaGetLastError();
@@ -569,8 +557,8 @@ int launch_attn_fwd_tc(const AttnCall& c, void* ws) {
   const attn::FwdPlan p = attn::fwd_plan(a.B, a.H, a.H_kv, a.mask.T, a.mask.T_k, a.mask.window);
   if (p.blocks > 0x7fffffffLL || (long long)a.B * a.H * a.mask.T / 8 >= 0x7fffffffLL) return LAWCAT_ERR_UNSUPPORTED;
   const bool general = a.cap > 0.f || a.slopes || !(a.scale > 0.f);
-  if (c.d == 128) return general ? attn::fwd_tc<128, 2, true>(c, p, ws) : attn::fwd_tc<128, 2, false>(c, p, ws);
-  return general ? attn::fwd_tc<64, 2, true>(c, p, ws) : attn::fwd_tc<64, 2, false>(c, p, ws);
+  if (c.d == 128) return general ? attn::fwd_tc<128, true>(c, p, ws) : attn::fwd_tc<128, false>(c, p, ws);
+  return general ? attn::fwd_tc<64, true>(c, p, ws) : attn::fwd_tc<64, false>(c, p, ws);
 }
 
 }  // namespace lawcat

@@ -34,11 +34,6 @@ __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile
   }
 }
 
-// Registers per thread of a warpgroup (four warps, all of them here): the launch gave every thread 168; two warpgroups that hold score
-// rows take 224 and the third, with the copy and product warps, keeps 56 (2 x 224 + 56 = 3 x 168).
-__device__ __forceinline__ void regs_many() { asm volatile("setmaxnreg.inc.sync.aligned.u32 224;"); }
-__device__ __forceinline__ void regs_few() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
-
 // n / d for 0 <= n < 2^31: items are numbered, and their digits are run-time sizes (a division proper costs as much as an exponential
 // of a whole row).
 struct FastDiv {
