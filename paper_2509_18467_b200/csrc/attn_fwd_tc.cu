@@ -4,16 +4,21 @@
 // two neighbouring tiles of one head); a block walks their keys in tiles of 64:
 //   warpgroup i < NT   softmax of tile i: one thread per query; S_i from tensor memory, mask / cap / bias, running maximum and
 //                      sum in registers, P_i = exp2(x - m) rounded to bf16 over S_i in tensor memory
-//   copy warp          Q tiles once, K and V tiles in turn through a ring of stages (TMA, 128-byte swizzle)
+//   one warpgroup      outputs: O_i from tensor memory, divided, to memory by the copy engine, while the next item is being weighed
+//   copy warp          numbers and limits of the items; Q tiles once, K and V tiles in turn through a ring of stages (TMA, 128-byte swizzle)
 //   product warp       S_i = Q_i K^T (both operands in shared memory), O_i += P_i V (P_i from tensor memory); fp32 accumulation
 // S_i has two places in tensor memory: the products of the next tile's scores run while this one is weighed, and a warpgroup finds
 // its next scores there (with tiles of 128 keys and one place, a warpgroup's chain was scores, weights, both products, and a pair of
 // tiles took 3300 cycles; tensor memory holds no second place of 128 columns beside two O of 128).
 // The accumulator O_i is rescaled only when a row's maximum has grown by more than 2^8 since it was last scaled (the weights then
 // stay within 2^8 in fp32 and bf16 alike), by the softmax warps themselves, behind the product of the tile in front.
+// The products of the two tiles are issued in turn (S_0, O_0, S_1, O_1), which keeps the warpgroups half a step apart: weighing in
+// step, they meet at the pipe of the special functions and leave it idle together. Half of the exponentials of a tile that all rows
+// see whole are polynomials on the FMA pipe.
 // One block per SM takes items in turn, the longest first: while an item's last tiles are weighed and its outputs stored, the next
-// one's queries and first keys are already on their way (a sequence of 1024 tokens has no more than eight key tiles per item, and
-// a block that starts and ends with each of them spent half its time so).
+// one's queries and first keys are already on their way (a sequence of 1024 tokens has few key tiles per item, and a block that
+// starts and ends with each of them spent half its time so). Code that runs once per item is kept off the softmax warps: it comes
+// from the instruction caches' far end, at five cycles an instruction.
 // Few queries over many keys: the keys are shared out over `parts` blocks, whose (values, maximum, sum) a second kernel joins.
 // Rounding: weights to bf16 as an operand (the sum that divides them is of the unrounded ones), o once. All else is fp32.
 // A row that is not finite in a block is computed again on the CUDA cores (attn_exact.cuh): a weight of zero times a NaN that the
@@ -46,12 +51,14 @@ struct FwdLay {
   static constexpr uint32_t TILE = 128 * D * 2, KT = 64 * D * 2; // a Q tile; a K or V tile
   static constexpr int ST = 8;                                   // stages of the ring (K and V tiles alternate)
   static constexpr uint32_t OUT = 128 * 128;                     // a warpgroup's outputs on their way: 64 channels (or 32 in fp32)
-  static constexpr uint32_t OFF_Q = 0, OFF_RING = NT * TILE, OFF_OUT = OFF_RING + ST * KT, OFF_LIST = OFF_OUT + NT * OUT, OFF_BAR = OFF_LIST + BAD_MAX * 4;
+  static constexpr int SLOTS = 4;                                // items on their way
+  static constexpr uint32_t OFF_Q = 0, OFF_RING = NT * TILE, OFF_OUT = OFF_RING + ST * KT, OFF_ML = OFF_OUT + OUT, OFF_LIST = OFF_ML + 2 * NT * 128 * 8,
+                            OFF_ITEM = OFF_LIST + BAD_MAX * 4, OFF_BAR = OFF_ITEM + SLOTS * 64;
   static constexpr uint32_t BYTES = OFF_BAR + 512;
-  static constexpr int THREADS = NT * 128 + 64;
+  static constexpr int THREADS = NT * 128 + 192;                 // softmax, outputs, copies, products
   // mbarriers
   static constexpr int B_Q = 0, B_QE = 1, B_FULL = 2, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + 2 * NT, B_O = B_P + 2 * NT, B_OE = B_O + 2 * NT,
-                       NBAR = B_OE + NT;
+                       B_ML = B_OE + NT, B_ITEM = B_ML + NT, B_ITEME = B_ITEM + SLOTS, NBAR = B_ITEME + SLOTS;
   static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 512 && fwd_smem<D, 4, 128>() <= OFF_LIST && NT * (128 + D) <= 512, "shared memory, tensor memory");
 };
 
@@ -77,11 +84,12 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   int* const s_list = reinterpret_cast<int*>(smem + L::OFF_LIST);
 
   struct Item {
-    int part, b, h0, g, tb, j_first, j_end, n;
+    int part, b, h0, g, tb, j_first, j_end, n, idx;   // n: key tiles; < 0 behind the last item
   };
   const int T = a.mask.T;
   auto item_of = [&](int idx) {
     Item w;
+    w.idx = idx;
     const int q = quot(idx, f.parts_d), tile = quot(q, f.bp), bp = rest(q, tile, f.bp);
     w.part = rest(idx, q, f.parts_d);
     w.b = quot(bp, f.pairs);
@@ -120,6 +128,11 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         mbar_init(bar(L::B_O + 2 * i + u), 1);   // (a softmax warp may be two products ahead: a barrier of one phase bit would mislead it)
       }
       mbar_init(bar(L::B_OE + i), 128);
+      mbar_init(bar(L::B_ML + i), 128);
+    }
+    for (int i = 0; i < L::SLOTS; ++i) {
+      mbar_init(bar(L::B_ITEM + i), 1);
+      mbar_init(bar(L::B_ITEME + i), 13);   // (warps of softmax and outputs, and the product thread)
     }
     s_flags[1] = 0;
     s_flags[2] = 0;
@@ -128,7 +141,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
   }
-  if (warp == NT * 4) {
+  if (warp == NT * 4 + 4) {
     tmem_alloc(sb + L::OFF_BAR + 8 * L::NBAR, 512);
     tmem_relinquish();
   }
@@ -139,17 +152,31 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   auto s_col = [&](int i, int step) { return tmem + (uint32_t)(i * 128 + (step & 1) * 64); };
   auto o_col = [&](int i) { return tmem + (uint32_t)(NT * 128 + i * D); };
 
-  if (warp >= NT * 4) {
-    if (warp == NT * 4) {
+  // item k of this block, as the copy warp wrote it down
+  auto item_at = [&](int k, Item& w) {
+    const int u = k % L::SLOTS;
+    if (!wait_bar(bar(L::B_ITEM + u), (k / L::SLOTS) & 1, s_abort, f.limit)) return false;
+    w = *reinterpret_cast<const Item*>(smem + L::OFF_ITEM + u * 64);
+    return true;
+  };
+  auto item_read = [&](int k) { mbar_arrive(bar(L::B_ITEME + k % L::SLOTS)); };
+
+  if (warp == NT * 4 + 4) {
     // ------------------------------------------------------------------------------------------------ copies
     if (elect_one()) {
-      int at = 0, seq = 0;   // tiles and items so far
+      int at = 0, seq = 0, k = 0;   // tiles, items with tiles, and items so far
       bool ok = true;
-      for (int r = 0; r < rounds && ok; ++r) {
-        const int idx = index_of(r);
+      for (int r = 0; r <= rounds && ok; ++r) {
+        const int idx = r < rounds ? index_of(r) : 0;
         if (idx >= f.items) continue;
-        const Item w = item_of(idx);
-        if (w.n == 0) continue;
+        Item w = item_of(idx);
+        if (r == rounds) w.n = -1;
+        if (k >= L::SLOTS) ok = wait_bar(bar(L::B_ITEME + k % L::SLOTS), (k / L::SLOTS - 1) & 1, s_abort, f.limit);
+        if (!ok) break;
+        *reinterpret_cast<Item*>(smem + L::OFF_ITEM + k % L::SLOTS * 64) = w;
+        mbar_arrive(bar(L::B_ITEM + k % L::SLOTS));
+        ++k;
+        if (w.n <= 0) continue;
         if (seq > 0) ok = wait_bar(bar(L::B_QE), (seq - 1) & 1, s_abort, f.limit);
         if (!ok) break;
         mbar_arrive_expect_tx(bar(L::B_Q), NT * L::TILE);
@@ -164,7 +191,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         ++seq;
       }
     }
-    } else if (warp == NT * 4 + 1) {
+  } else if (warp == NT * 4 + 5) {
     // ------------------------------------------------------------------------------------------------ products
     if (elect_one()) {
       constexpr uint32_t id_s = instr_desc(128, 64, FMT_BF16, MAJOR_K, MAJOR_K);
@@ -172,41 +199,37 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       auto stage = [&](int at) { return sb + L::OFF_RING + (uint32_t)(at % L::ST) * L::KT; };
       auto full = [&](int at) { return wait_bar(bar(L::B_FULL + at % L::ST), (at / L::ST) & 1, s_abort, f.limit); };
       // the scores of a step; `last`: of the item
-      auto scores = [&](int step, bool last) {
-        if (!full(2 * step)) return false;
+      auto scores = [&](int i, int step, bool last) {
+        if (i == 0 && !full(2 * step)) return false;
         tc_fence_after_sync();
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk)
-            mma_f16(s_col(i, step), kdesc<128>(sb + L::OFF_Q + i * L::TILE, kk), kdesc<64>(stage(2 * step), kk), id_s, kk != 0);
-          mma_commit(bar(L::B_S + 2 * i + (step & 1)));
+        for (int kk = 0; kk < D / 16; ++kk)
+          mma_f16(s_col(i, step), kdesc<128>(sb + L::OFF_Q + i * L::TILE, kk), kdesc<64>(stage(2 * step), kk), id_s, kk != 0);
+        mma_commit(bar(L::B_S + 2 * i + (step & 1)));
+        if (i == NT - 1) {
+          mma_commit(bar(L::B_EMPTY + 2 * step % L::ST));
+          if (last) mma_commit(bar(L::B_QE));
         }
-        mma_commit(bar(L::B_EMPTY + 2 * step % L::ST));
-        if (last) mma_commit(bar(L::B_QE));
         return true;
       };
-      auto next_item = [&](int& r) {   // tiles of the next item that has any; 0 behind the last
-        for (; r < rounds; ++r) {
-          const int idx = index_of(r);
-          if (idx >= f.items) continue;
-          const int n = item_of(idx).n;
-          if (n) {
-            ++r;
-            return n;
-          }
-        }
-        return 0;
+      int k = 0, seq = 0, step = 0;   // items, items with tiles, key tiles so far
+      auto next_item = [&]() {   // tiles of the next item that has any; 0 behind the last
+        Item w;
+        w.n = -1;
+        do {
+          if (!item_at(k, w)) return -1;
+          item_read(k++);
+        } while (w.n == 0);
+        return max(w.n, 0);
       };
-      int r = 0, n = next_item(r), seq = 0, step = 0;   // step: key tiles so far
-      bool ok = n && wait_bar(bar(L::B_Q), 0, s_abort, f.limit) && scores(0, n == 1);
-      while (n && ok) {
-        const int n_next = next_item(r);
+      int n = next_item();
+      bool ok = n > 0 && wait_bar(bar(L::B_Q), 0, s_abort, f.limit) && scores(0, 0, n == 1) && scores(1, 0, n == 1);
+      while (n > 0 && ok) {
         for (int it = 0; it < n && ok; ++it, ++step) {
-          if (it + 1 < n) ok = scores(step + 1, it + 2 == n);
-          if (ok) ok = full(2 * step + 1);
 #pragma unroll
           for (int i = 0; i < NT; ++i) {
+            if (ok && it + 1 < n) ok = scores(i, step + 1, it + 2 == n);
+            if (ok && i == 0) ok = full(2 * step + 1);
             if (ok && it == 0 && seq > 0) ok = wait_bar(bar(L::B_OE + i), (seq - 1) & 1, s_abort, f.limit);
             if (ok) ok = wait_bar(bar(L::B_P + 2 * i + (step & 1)), (step >> 1) & 1, s_abort, f.limit);
             if (!ok) break;
@@ -217,37 +240,43 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           }
           if (!ok) break;
           mma_commit(bar(L::B_EMPTY + (2 * step + 1) % L::ST));
-          if (it + 1 == n && n_next) ok = wait_bar(bar(L::B_Q), (seq + 1) & 1, s_abort, f.limit) && scores(step + 1, n_next == 1);
         }
-        n = n_next;
+        // (asked for behind the item's last product: the other roles finish with it before the copy warp comes to write more down)
+        if (ok) n = next_item();
         ++seq;
+        if (ok && n > 0) ok = wait_bar(bar(L::B_Q), seq & 1, s_abort, f.limit) && scores(0, step, n == 1) && scores(1, step, n == 1);
       }
     }
-    }
-  } else {
+  } else if (warp < NT * 4) {
     // ------------------------------------------------------------------------------------------------ softmax
     const int i = warp >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t O = o_col(i) + lanes;
     const float scale2 = a.scale * LOG2E, inv_cap = GENERAL && a.cap > 0.f ? 1.f / a.cap : 0.f;
     int step = 0, seq = 0;
-    for (int r = 0; r < rounds; ++r) {
-      const int idx = index_of(r);
-      if (idx >= f.items) continue;
-      const Item w = item_of(idx);
+    for (int k = 0;; ++k) {
+      Item w;
+      w.n = -1;
+      bool ok = __all_sync(0xffffffffu, item_at(k, w));
+      if (!ok || w.n < 0) break;
+      if (lane == 0) item_read(k);
+      if (w.n == 0) continue;
       const int n = w.n, h = head_of(w, i), t = row_of(w, i) + (tid & 127);
-      const bool valid = t < T;
-      const int2 iv = interval(a.mask, w.b, valid ? t : T - 1);   // (rows behind the last are never stored)
-      // what the warp's rows see in all: [lo0, hi1), of which every row sees [lo1, hi0)
-      const int lo0 = __shfl_sync(0xffffffffu, iv.x, 0), lo1 = __shfl_sync(0xffffffffu, iv.x, 31);
-      const int hi0 = __shfl_sync(0xffffffffu, iv.y, 0), hi1 = __shfl_sync(0xffffffffu, iv.y, 31);
+      const int2 iv = interval(a.mask, w.b, min(t, T - 1));   // (rows behind the last are never stored)
       const float slope2 = GENERAL && a.slopes ? a.slopes[h] * LOG2E : 0.f;
+      // what the warp's rows see in all: [lo0, hi1), of which every row sees [lo1, hi0)
+      int lo0 = 0, lo1 = 0, hi0 = 0, hi1 = 0;
       float m = -INFINITY, l = 0.f;
-      bool ok = true;
       for (int it = 0; it < n; ++it, ++step) {
         ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_S + 2 * i + (step & 1)), (step >> 1) & 1, s_abort, f.limit));
         if (!ok) break;
         tc_fence_after_sync();
+        if (it == 0) {
+          lo0 = __shfl_sync(0xffffffffu, iv.x, 0);
+          lo1 = __shfl_sync(0xffffffffu, iv.x, 31);
+          hi0 = __shfl_sync(0xffffffffu, iv.y, 0);
+          hi1 = __shfl_sync(0xffffffffu, iv.y, 31);
+        }
         const int j0 = w.j_first + it * 64;
         const uint32_t S = s_col(i, step) + lanes;
         float s[64];
@@ -270,12 +299,14 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             for (int c = 0; c < 64; ++c) s[c] = fmaf(-slope2, fabsf(dist0 - (float)c), s[c]);
           }
         }
-        float mx0 = -INFINITY, mx1 = -INFINITY;
+        float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
         if (whole) {
 #pragma unroll
-          for (int c = 0; c < 64; c += 4) {
+          for (int c = 0; c < 64; c += 8) {
             mx0 = fmaxf(fmaxf(mx0, s[c]), s[c + 1]);
             mx1 = fmaxf(fmaxf(mx1, s[c + 2]), s[c + 3]);
+            mx2 = fmaxf(fmaxf(mx2, s[c + 4]), s[c + 5]);
+            mx3 = fmaxf(fmaxf(mx3, s[c + 6]), s[c + 7]);
           }
         } else {
           const int rl = iv.x - j0, rh = iv.y - j0;
@@ -295,7 +326,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             }
           }
         }
-        float mx = fmaxf(mx0, mx1);
+        float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
         if constexpr (!GENERAL) mx *= scale2;
         const bool grow = mx > m + RESCALE || (m == -INFINITY && mx > m);
         if (__any_sync(0xffffffffu, grow)) {
@@ -321,7 +352,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const float base = m == -INFINITY ? 0.f : m;
         const uint64_t sc = f2_pack(GENERAL ? 1.f : scale2, GENERAL ? 1.f : scale2), nb = f2_pack(-base, -base);
         uint64_t sum0 = 0, sum1 = 0;
-        // every fourth pair of a tile that all rows see whole takes its exponentials on the FMA pipe: the special functions' pipe is
+        // every other pair of a tile that all rows see whole takes its exponentials on the FMA pipe: the special functions' pipe is
         // what a tile waits for (below -126 and for -infinity the two differ, so not where keys are hidden)
         auto weigh = [&](auto first, auto mixed) {   // 32 scores from column `first` on: the weights, two to a register, in their place
           constexpr int c = decltype(first)::value;
@@ -329,7 +360,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           for (int e = 0; e < 16; ++e) {
             const uint64_t z = f2_fma(f2_pack(s[c + 2 * e], s[c + 2 * e + 1]), sc, nb);
             float x, y;
-            if (decltype(mixed)::value && (e & 3) == 3) {
+            if (decltype(mixed)::value && (e & 1)) {
               ex2_pair(z, x, y);
             } else {
               f2_unpack(z, x, y);
@@ -368,16 +399,46 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         tc_fence_before_sync();
         mbar_arrive(bar(L::B_P + 2 * i + (step & 1)));
       }
-      if (ok && n > 0) ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_O + 2 * i + (step - 1 & 1)), (step - 1) >> 1 & 1, s_abort, f.limit));
-      if (named_bar_or(2 + i, 128, !ok)) break;   // (all four warps go on, or none)
-      tc_fence_after_sync();
+      if (!ok) break;
+      reinterpret_cast<float2*>(smem + L::OFF_ML)[(seq & 1) * 256 + i * 128 + (tid & 127)] = make_float2(m, l);
+      mbar_arrive(bar(L::B_ML + i));
+      ++seq;
+    }
+  } else {
+    // ------------------------------------------------------------------------------------------------ outputs
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, out = sb + L::OFF_OUT;
+    const int r128 = tid & 127;
+    int step = 0, seq = 0;
+    bool fail = false;
+    for (int k = 0;; ++k) {
+      Item w;
+      w.n = -1;
+      fail = !item_at(k, w);
+      if (named_bar_or(2, 128, fail) || w.n < 0) break;
+      if (lane == 0) item_read(k);
+      const int n = w.n;
+      step += n;
+#pragma unroll 1
+      for (int i = 0; i < NT; ++i) {
+      const uint32_t O = o_col(i) + lanes;
+      const int h = head_of(w, i), t = row_of(w, i) + r128;
+      const bool valid = t < T;
+      float m = -INFINITY, l = 0.f;
+      if (n > 0) {
+        fail = !wait_bar(bar(L::B_ML + i), seq & 1, s_abort, f.limit) ||
+               !wait_bar(bar(L::B_O + 2 * i + (step - 1 & 1)), (step - 1) >> 1 & 1, s_abort, f.limit);
+        __syncwarp();
+        const float2 ml = reinterpret_cast<const float2*>(smem + L::OFF_ML)[(seq & 1) * 256 + i * 128 + r128];
+        m = ml.x;
+        l = ml.y;
+        tc_fence_after_sync();
+      }
       const size_t row = ((size_t)w.b * T + t) * a.H + h;                                                // of [B, T, H]
-      const size_t prow0 = (((size_t)w.part * a.B + w.b) * a.H + h) * (size_t)T + row_of(w, i), prow = prow0 + (tid & 127);  // of [parts, B, H, T]
+      const size_t prow0 = (((size_t)w.part * a.B + w.b) * a.H + h) * (size_t)T + row_of(w, i), prow = prow0 + r128;  // of [parts, B, H, T]
       const float inv = f.parts > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
       float test = l * 0.f;
       // outputs through shared memory: 64 channels at a time by the copy engine (which leaves out rows behind the last), or 32 in fp32
-      const uint32_t out = sb + L::OFF_OUT + i * L::OUT;
-      const int r128 = tid & 127, rows = min(128, T - row_of(w, i));
+      const int rows = min(128, T - row_of(w, i));
 #pragma unroll 1
       for (int c = 0; c < D; c += 32) {
         float o[32];
@@ -398,11 +459,11 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           test = fmaf(o[e], 0.f, test);
         }
         if (f.parts > 1) {
-          named_bar_sync(2 + i, 128);   // (the last quarter is out of shared memory)
+          named_bar_sync(2, 128);   // (the last quarter is out of shared memory)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             sts128(out + sw128(r128, e), make_uint4(__float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]), __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3])));
-          named_bar_sync(2 + i, 128);
+          named_bar_sync(2, 128);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const int k = e * 16 + (r128 >> 3);
@@ -411,7 +472,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         } else {
           if (c % 64 == 0) {
             if (r128 == 0) tma_store_wait_read();
-            named_bar_sync(2 + i, 128);
+            named_bar_sync(2, 128);
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -419,7 +480,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                                                               pack_bf16(o[8 * e + 4], o[8 * e + 5]), pack_bf16(o[8 * e + 6], o[8 * e + 7])));
           if (c % 64 == 32) {
             fence_proxy_async();
-            named_bar_sync(2 + i, 128);
+            named_bar_sync(2, 128);
             if (r128 == 0 && rows > 0) {
               tma_store_4d(&tm_o, out, c - 32, h, row_of(w, i), w.b);
               tma_store_commit();
@@ -431,10 +492,11 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         if (f.parts > 1) f.part_ml[prow] = make_float2(m, l);
         else if (a.lse) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
       }
-      if (__any_sync(0xffffffffu, valid && !(test == 0.f)) && lane == 0) note_bad(s_list, (int*)(s_flags + 2), idx);
+      if (__any_sync(0xffffffffu, valid && !(test == 0.f)) && lane == 0) note_bad(s_list, (int*)(s_flags + 2), w.idx);
+      }
       if (n > 0) ++seq;
     }
-    if ((tid & 127) == 0) tma_store_wait_all();
+    if (r128 == 0) tma_store_wait_all();
   }
   __syncthreads();
   if (*s_abort) {
@@ -443,7 +505,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   }
   tc_fence_before_sync();
   __syncthreads();
-  if (warp == NT * 4) tmem_dealloc(tmem, 512);
+  if (warp == NT * 4 + 4) tmem_dealloc(tmem, 512);
   const int bad = *s_abort ? 0 : s_flags[2];
   if (!bad || tid >= 128) return;
   for (int r = 0; r < rounds; ++r) {
