@@ -1,8 +1,8 @@
 // Gradients of softmax attention on the tensor cores: bf16 storage, d = 64 or 128. One kernel in two forms:
-//   KV = false   a block owns 128 queries of one head (Q, dO) and walks their keys (K, V) in tiles of 64:  dQ += dX K, R += P f K
-//   KV = true    a block owns 128 keys of one key-value head (K, V) and walks the queries that see them, of every head of the
+//   KV = false   an item is 128 queries of one head (Q, dO); a block walks their keys (K, V) in tiles of 64:  dQ += dX K, R += P f K
+//   KV = true    an item is 128 keys of one key-value head (K, V); a block walks the queries that see them, of every head of the
 //                group (Q, dO), in tiles of 64:                                             dK += dX^T Q,  dV += P^T dO
-// With A1, A2 the block's own tiles and B1, B2 the walked ones, both compute
+// With A1, A2 the item's own tiles and B1, B2 the walked ones, both compute
 //   S = A1 B1^T, dP = A2 B2^T (shared memory), P = exp2(S scale - lse), dX = P (dP - D) f (one thread per own row; f = 1 - tanh^2
 //   under a cap, else 1), acc1 += dX B1, acc2 += P B2 (keys) or P f B1 (queries), dX and P as bf16 in tensor memory over dP and S.
 // Two warpgroups take the walked tiles in turn, each with an S and a dP of its own: one tile's exponentials run behind the other
@@ -10,10 +10,15 @@
 // D = sum_j p_j dP_j comes out of the first form's own loop, in fp32: it starts from dO.o, whose o was rounded, and what that was off
 // by is put right at the end with R: dQ = acc1 + (dO.o - D) R. The second form reads (lse, D) of every query as the first left them.
 // (With dO.o for D the gradients of q and k were 2.6e-3 off 64 bits, of which 2.3e-3 are the roundings below.)
-// The sums over queries and over keys stay in tensor memory of one block each, in one order: no atomics, the same bits every time.
+// The sums over queries and over keys stay in tensor memory per item, in one order: no atomics, the same bits every time.
 // The price is S and dP computed twice (7 products of 128 x 128 x d per pair of tiles instead of 5).
+// One block per SM takes items in turn, the longest first, as in the forward: the next item's own tiles and first walked ones come in
+// while this one's last are weighed and its gradients leave through shared memory and the copy engine. dO.o is summed by two warps of
+// their own, an item ahead.
 // Rounding: P and dX to bf16 as operands, the gradients once. All else is fp32.
 // Rows that come out not finite are computed again on the CUDA cores, as in the forward.
+#include <algorithm>
+
 #include "attn_tc.cuh"
 
 namespace lawcat {
@@ -21,21 +26,23 @@ namespace attn {
 
 struct BwdArgs {
   Args a;
-  int tiles;
+  FastDiv bh, heads, group;   // B times the heads that own items, those heads, H / H_kv
+  int tiles, items;
   long long limit;
 };
 
 template <int D>
 struct BwdLay {
   static constexpr uint32_t OWN = 128 * D * 2, WALK = 64 * D * 2, STAT = 512;   // (a tile's -lse log2e, then its -D)
-  static constexpr int ST = 4;
-  static constexpr uint32_t STAGE = 2 * WALK;
-  static constexpr uint32_t OFF_A = 0, OFF_RING = 2 * OWN, OFF_STAT = OFF_RING + ST * STAGE, OFF_DEX = OFF_STAT + ST * STAT, OFF_BAR = OFF_DEX + 1024;
-  static constexpr uint32_t BYTES0 = OFF_BAR + 256, E1 = (uint32_t)dq_smem<D, 4, 128>(), E2 = (uint32_t)dkdv_smem<D, 4, 128>();
-  static constexpr uint32_t E = E1 > E2 ? E1 : E2, BYTES = BYTES0 > E ? BYTES0 : E;
-  static constexpr int THREADS = 320;
-  static constexpr int B_A = 0, B_FULL = 1, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + 2, B_DONE = B_P + 2, NBAR = B_DONE + 1;
-  static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 256, "shared memory");
+  static constexpr int ST = D == 128 ? 3 : 4, SLOTS = 4;
+  static constexpr uint32_t STAGE = 2 * WALK, OUT = 128 * 128;                  // a warpgroup's gradients on their way: 64 channels
+  static constexpr uint32_t OFF_A = 0, OFF_RING = 2 * OWN, OFF_OUT = OFF_RING + ST * STAGE, OFF_STAT = OFF_OUT + 2 * OUT, OFF_DEX = OFF_STAT + ST * STAT,
+                            OFF_OWN = OFF_DEX + 2048, OFF_LIST = OFF_OWN + 2048, OFF_ITEM = OFF_LIST + BAD_MAX * 4, OFF_BAR = OFF_ITEM + SLOTS * 64;
+  static constexpr uint32_t BYTES = OFF_BAR + 512, E1 = (uint32_t)dq_smem<D, 4, 128>(), E2 = (uint32_t)dkdv_smem<D, 4, 128>();
+  static constexpr int THREADS = 384;   // weights, copies, products, two warps for dO.o
+  static constexpr int B_A = 0, B_AE = 1, B_FULL = 2, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + 2, B_ACC = B_P + 2, B_ACCE = B_ACC + 1,
+                       B_OWN = B_ACCE + 1, B_OWNE = B_OWN + 2, B_ITEM = B_OWNE + 2, B_ITEME = B_ITEM + SLOTS, NBAR = B_ITEME + SLOTS;
+  static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 512 && E1 <= OFF_LIST && E2 <= OFF_LIST, "shared memory");
 };
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
@@ -55,7 +62,8 @@ __device__ __noinline__ void dkdv_again(const Args& a, float* sm, int b, int g, 
 template <int D, bool KV, bool GENERAL>
 __global__ void __launch_bounds__(BwdLay<D>::THREADS, 1)
 attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_constant__ CUtensorMap tm_a2, const __grid_constant__ CUtensorMap tm_b1,
-                   const __grid_constant__ CUtensorMap tm_b2, const __grid_constant__ BwdArgs f) {
+                   const __grid_constant__ CUtensorMap tm_b2, const __grid_constant__ CUtensorMap tm_o1, const __grid_constant__ CUtensorMap tm_o2,
+                   const __grid_constant__ BwdArgs f) {
   using L = BwdLay<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const Args& a = f.a;
@@ -65,24 +73,38 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
   volatile int* const s_abort = s_flags + 1;
   auto bar = [&](int i) { return sb + L::OFF_BAR + 8 * (uint32_t)i; };
 
-  const int heads = KV ? a.H_kv : a.H, G = a.H / a.H_kv;
-  const int bh = blockIdx.x % (a.B * heads), b = bh / heads, own = bh % heads;
-  const int tile = blockIdx.x / (a.B * heads);
-  const int r0 = (KV ? tile : f.tiles - 1 - tile) * 128;                       // (under a causal mask the longest rows first)
-  const int rows = KV ? a.mask.T_k : a.mask.T, r1 = min(r0 + 128, rows);
-  // the walked side: from w0 to w_end, 64 at a time; per head of the group where queries are walked
-  int w0, w_end;
-  if (KV) {
-    w0 = key_interval(a.mask, b, r0).x & ~63;                                  // (the statistics are copied from 16-byte places)
-    w_end = key_interval(a.mask, b, r1 - 1).y;
-  } else {
-    w0 = interval(a.mask, b, r0).x;
-    w_end = interval(a.mask, b, r1 - 1).y;
-  }
-  const int per = w_end > w0 ? (w_end - w0 + 63) / 64 : 0, n = KV ? per * G : per;
+  int* const s_list = reinterpret_cast<int*>(smem + L::OFF_LIST);
+
+  struct Item {
+    int b, own, r0, w0, per, n, idx;   // n walked tiles, `per` of them for each head; n < 0 behind the last item
+  };
+  const int G = a.H / a.H_kv, rows = KV ? a.mask.T_k : a.mask.T;
+  auto item_of = [&](int idx) {
+    Item w;
+    w.idx = idx;
+    const int tile = quot(idx, f.bh), bh = rest(idx, tile, f.bh);
+    w.b = quot(bh, f.heads);
+    w.own = rest(bh, w.b, f.heads);
+    w.r0 = (KV ? tile : f.tiles - 1 - tile) * 128;                               // (under a causal mask the longest first)
+    const int r1 = min(w.r0 + 128, rows);
+    int w_end;
+    if (KV) {
+      w.w0 = key_interval(a.mask, w.b, w.r0).x & ~63;                            // (the statistics are copied from 16-byte places)
+      w_end = key_interval(a.mask, w.b, r1 - 1).y;
+    } else {
+      w.w0 = interval(a.mask, w.b, w.r0).x;
+      w_end = interval(a.mask, w.b, r1 - 1).y;
+    }
+    w.per = w_end > w.w0 ? (w_end - w.w0 + 63) / 64 : 0;
+    w.n = KV ? w.per * G : w.per;
+    return w;
+  };
+  const int rounds = (f.items + (int)gridDim.x - 1) / (int)gridDim.x;
+  auto index_of = [&](int r) { return r * (int)gridDim.x + (r & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x); };
 
   if (tid == 0) {
     mbar_init(bar(L::B_A), 1);
+    mbar_init(bar(L::B_AE), 1);
     for (int i = 0; i < L::ST; ++i) {
       mbar_init(bar(L::B_FULL + i), 1);
       mbar_init(bar(L::B_EMPTY + i), KV ? 129 : 1);   // (the softmax threads read the statistics)
@@ -90,8 +112,15 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(L::B_S + i), 1);
       mbar_init(bar(L::B_P + i), 128);
+      mbar_init(bar(L::B_OWN + i), 64);
+      mbar_init(bar(L::B_OWNE + i), 256);
     }
-    mbar_init(bar(L::B_DONE), 1);
+    mbar_init(bar(L::B_ACC), 1);
+    mbar_init(bar(L::B_ACCE), 256);
+    for (int i = 0; i < L::SLOTS; ++i) {
+      mbar_init(bar(L::B_ITEM + i), 1);
+      mbar_init(bar(L::B_ITEME + i), KV ? 9 : 11);    // (warps of weights, the product thread, the two for dO.o)
+    }
     s_flags[1] = 0;
     s_flags[2] = 0;
     mbar_fence_init();
@@ -112,95 +141,209 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
   auto s_col = [&](int i) { return tmem + (uint32_t)(2 * D + i * 128); };
   auto p_col = [&](int i) { return s_col(i) + 64; };
   static_assert(2 * D + 256 <= 512, "tensor memory");
+  // item k of this block, as the copy warp wrote it down
+  auto item_at = [&](int k, Item& w) {
+    const int u = k % L::SLOTS;
+    if (!wait_bar(bar(L::B_ITEM + u), (k / L::SLOTS) & 1, s_abort, f.limit)) return false;
+    w = *reinterpret_cast<const Item*>(smem + L::OFF_ITEM + u * 64);
+    return true;
+  };
+  auto item_read = [&](int k) { mbar_arrive(bar(L::B_ITEME + k % L::SLOTS)); };
 
   if (warp == 8) {
     // ------------------------------------------------------------------------------------------------ copies
-    if (n > 0 && elect_one()) {
-      mbar_arrive_expect_tx(bar(L::B_A), 2 * L::OWN);
-      load_tile<D, 128>(sb + L::OFF_A, &tm_a1, bar(L::B_A), own, r0, b);
-      load_tile<D, 128>(sb + L::OFF_A + L::OWN, &tm_a2, bar(L::B_A), own, r0, b);
-      for (int it = 0; it < n; ++it) {
-        const int s = it % L::ST, h = KV ? own * G + it / per : own / G, w = w0 + (KV ? it % per : it) * 64;
-        if (it >= L::ST && !wait_bar(bar(L::B_EMPTY + s), (it / L::ST - 1) & 1, s_abort, f.limit)) break;
-        mbar_arrive_expect_tx(bar(L::B_FULL + s), L::STAGE + (KV ? L::STAT : 0));
-        load_tile<D, 64>(sb + L::OFF_RING + s * L::STAGE, &tm_b1, bar(L::B_FULL + s), h, w, b);
-        load_tile<D, 64>(sb + L::OFF_RING + s * L::STAGE + L::WALK, &tm_b2, bar(L::B_FULL + s), h, w, b);
-        if (KV) {
-          const float* const nl = a.stat + ((size_t)b * a.H + h) * a.stat_stride + w;
-          bulk_load(sb + L::OFF_STAT + s * L::STAT, nl, 256, bar(L::B_FULL + s));
-          bulk_load(sb + L::OFF_STAT + s * L::STAT + 256, nl + (size_t)a.B * a.H * a.stat_stride, 256, bar(L::B_FULL + s));
+    if (elect_one()) {
+      int step = 0, seq = 0, k = 0;   // walked tiles, items with tiles, items so far
+      bool ok = true;
+      for (int r = 0; r <= rounds && ok; ++r) {
+        const int idx = r < rounds ? index_of(r) : 0;
+        if (idx >= f.items) continue;
+        Item w = item_of(idx);
+        if (r == rounds) w.n = -1;
+        if (k >= L::SLOTS) ok = wait_bar(bar(L::B_ITEME + k % L::SLOTS), (k / L::SLOTS - 1) & 1, s_abort, f.limit);
+        if (!ok) break;
+        *reinterpret_cast<Item*>(smem + L::OFF_ITEM + k % L::SLOTS * 64) = w;
+        mbar_arrive(bar(L::B_ITEM + k % L::SLOTS));
+        ++k;
+        if (w.n <= 0) continue;
+        if (seq > 0) ok = wait_bar(bar(L::B_AE), (seq - 1) & 1, s_abort, f.limit);
+        if (!ok) break;
+        mbar_arrive_expect_tx(bar(L::B_A), 2 * L::OWN);
+        load_tile<D, 128>(sb + L::OFF_A, &tm_a1, bar(L::B_A), w.own, w.r0, w.b);
+        load_tile<D, 128>(sb + L::OFF_A + L::OWN, &tm_a2, bar(L::B_A), w.own, w.r0, w.b);
+        int h = KV ? w.own * G : quot(w.own, f.group), at = w.w0, left = w.per;
+        for (int it = 0; it < w.n; ++it, ++step) {
+          const int s = step % L::ST;
+          if (step >= L::ST) ok = wait_bar(bar(L::B_EMPTY + s), (step / L::ST - 1) & 1, s_abort, f.limit);
+          if (!ok) break;
+          mbar_arrive_expect_tx(bar(L::B_FULL + s), L::STAGE + (KV ? L::STAT : 0));
+          load_tile<D, 64>(sb + L::OFF_RING + s * L::STAGE, &tm_b1, bar(L::B_FULL + s), h, at, w.b);
+          load_tile<D, 64>(sb + L::OFF_RING + s * L::STAGE + L::WALK, &tm_b2, bar(L::B_FULL + s), h, at, w.b);
+          if (KV) {
+            const float* const nl = a.stat + ((size_t)w.b * a.H + h) * a.stat_stride + at;
+            bulk_load(sb + L::OFF_STAT + s * L::STAT, nl, 256, bar(L::B_FULL + s));
+            bulk_load(sb + L::OFF_STAT + s * L::STAT + 256, nl + (size_t)a.B * a.H * a.stat_stride, 256, bar(L::B_FULL + s));
+          }
+          at += 64;
+          if (--left == 0) {   // (the group's next head)
+            ++h;
+            at = w.w0;
+            left = w.per;
+          }
         }
+        ++seq;
       }
     }
   } else if (warp == 9) {
     // ------------------------------------------------------------------------------------------------ products
-    if (n > 0 && elect_one()) {
+    if (elect_one()) {
       constexpr uint32_t id_s = instr_desc(128, 64, FMT_BF16, MAJOR_K, MAJOR_K);
       constexpr uint32_t id_a = instr_desc(128, D, FMT_BF16, MAJOR_K, MAJOR_MN);
-      auto b1 = [&](int it) { return sb + L::OFF_RING + (uint32_t)(it % L::ST) * L::STAGE; };
-      auto scores = [&](int it) {
-        if (!wait_bar(bar(L::B_FULL + it % L::ST), (it / L::ST) & 1, s_abort, f.limit)) return false;
+      auto b1 = [&](int step) { return sb + L::OFF_RING + (uint32_t)(step % L::ST) * L::STAGE; };
+      auto scores = [&](int step, bool last) {
+        if (!wait_bar(bar(L::B_FULL + step % L::ST), (step / L::ST) & 1, s_abort, f.limit)) return false;
         tc_fence_after_sync();
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) mma_f16(s_col(it & 1), kdesc<128>(sb + L::OFF_A, kk), kdesc<64>(b1(it), kk), id_s, kk != 0);
+        for (int kk = 0; kk < D / 16; ++kk) mma_f16(s_col(step & 1), kdesc<128>(sb + L::OFF_A, kk), kdesc<64>(b1(step), kk), id_s, kk != 0);
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
-          mma_f16(p_col(it & 1), kdesc<128>(sb + L::OFF_A + L::OWN, kk), kdesc<64>(b1(it) + L::WALK, kk), id_s, kk != 0);
-        mma_commit(bar(L::B_S + (it & 1)));
+          mma_f16(p_col(step & 1), kdesc<128>(sb + L::OFF_A + L::OWN, kk), kdesc<64>(b1(step) + L::WALK, kk), id_s, kk != 0);
+        mma_commit(bar(L::B_S + (step & 1)));
+        if (last) mma_commit(bar(L::B_AE));
         return true;
       };
-      bool ok = wait_bar(bar(L::B_A), 0, s_abort, f.limit) && scores(0);
-      for (int it = 0; it < n && ok; ++it) {
-        if (it + 1 < n) ok = scores(it + 1);
-        if (ok) ok = wait_bar(bar(L::B_P + (it & 1)), (it >> 1) & 1, s_abort, f.limit);
+      int k = 0, seq = 0, step = 0;
+      auto next_item = [&]() {   // tiles of the next item that has any; 0 or less behind the last
+        Item w;
+        w.n = -1;
+        do {
+          if (!item_at(k, w)) return -1;
+          item_read(k++);
+        } while (w.n == 0);
+        return w.n;
+      };
+      int n = next_item();
+      bool ok = n > 0 && wait_bar(bar(L::B_A), 0, s_abort, f.limit) && scores(0, n == 1);
+      while (n > 0 && ok) {
+        for (int it = 0; it < n && ok; ++it, ++step) {
+          if (it + 1 < n) ok = scores(step + 1, it + 2 == n);
+          if (ok) ok = wait_bar(bar(L::B_P + (step & 1)), (step >> 1) & 1, s_abort, f.limit);
+          if (ok && it == 0 && seq > 0) ok = wait_bar(bar(L::B_ACCE), (seq - 1) & 1, s_abort, f.limit);
+          if (!ok) break;
+          tc_fence_after_sync();
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            mma_ts(acc2, s_col(step & 1) + kk * 8, mdesc<64>(b1(step) + (KV ? L::WALK : 0), kk), id_a, (it | kk) != 0);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) mma_ts(acc1, p_col(step & 1) + kk * 8, mdesc<64>(b1(step), kk), id_a, (it | kk) != 0);
+          mma_commit(bar(L::B_EMPTY + step % L::ST));
+        }
         if (!ok) break;
-        tc_fence_after_sync();
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) mma_ts(acc2, s_col(it & 1) + kk * 8, mdesc<64>(b1(it) + (KV ? L::WALK : 0), kk), id_a, (it | kk) != 0);
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) mma_ts(acc1, p_col(it & 1) + kk * 8, mdesc<64>(b1(it), kk), id_a, (it | kk) != 0);
-        mma_commit(bar(L::B_EMPTY + it % L::ST));
+        mma_commit(bar(L::B_ACC));
+        // (asked for behind the item's last product: the other roles finish with it before the copy warp comes to write more down)
+        n = next_item();
+        ++seq;
+        if (n > 0) ok = wait_bar(bar(L::B_A), seq & 1, s_abort, f.limit) && scores(step, n == 1);
       }
-      if (ok) mma_commit(bar(L::B_DONE));
+    }
+  } else if (warp >= 10) {
+    // ------------------------------------------------------------------------------------------------ -lse log2e and -dO.o of own queries
+    if (!KV) {
+      float* const s_own = reinterpret_cast<float*>(smem + L::OFF_OWN);
+      int seq = 0;
+      for (int k = 0;; ++k) {
+        Item w;
+        w.n = -1;
+        if (!__all_sync(0xffffffffu, item_at(k, w)) || w.n < 0) break;
+        if (lane == 0) item_read(k);
+        if (w.n == 0) continue;
+        float *const nl = s_own + (seq & 1) * 256, *const nd = nl + 128;
+        if (seq >= 2 && !__all_sync(0xffffffffu, wait_bar(bar(L::B_OWNE + (seq & 1)), ((seq >> 1) - 1) & 1, s_abort, f.limit))) break;
+        const int first = (warp - 10) * 64;
+        constexpr int LPR = D / 8, RP = 32 / LPR;   // lanes per row, rows at a time
+#pragma unroll 1
+        for (int i0 = first + lane / LPR; i0 < first + 64; i0 += 16 * RP) {   // (sixteen loads of each in flight: two warps have an item's time)
+          uint4 x[16], y[16];
+#pragma unroll
+          for (int u = 0; u < 16; ++u) {
+            const int t = w.r0 + i0 + u * RP;
+            const size_t at = (((size_t)w.b * a.mask.T + min(t, rows - 1)) * a.H + w.own) * D + lane % LPR * 8;
+            x[u] = __ldg(reinterpret_cast<const uint4*>((const bf16*)a.o_in + at));
+            y[u] = __ldg(reinterpret_cast<const uint4*>((const bf16*)a.dO + at));
+          }
+#pragma unroll
+          for (int u = 0; u < 16; ++u) {
+            float d = fmaf(bf16_lo(x[u].x), bf16_lo(y[u].x), bf16_hi(x[u].x) * bf16_hi(y[u].x));
+            d = fmaf(bf16_lo(x[u].y), bf16_lo(y[u].y), fmaf(bf16_hi(x[u].y), bf16_hi(y[u].y), d));
+            d = fmaf(bf16_lo(x[u].z), bf16_lo(y[u].z), fmaf(bf16_hi(x[u].z), bf16_hi(y[u].z), d));
+            d = fmaf(bf16_lo(x[u].w), bf16_lo(y[u].w), fmaf(bf16_hi(x[u].w), bf16_hi(y[u].w), d));
+#pragma unroll
+            for (int o = LPR / 2; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+            if (lane % LPR == 0) nd[i0 + u * RP] = -d;
+          }
+        }
+        for (int i = first + lane; i < first + 64; i += 32)
+          nl[i] = w.r0 + i < rows ? -a.lse[((size_t)w.b * a.mask.T + w.r0 + i) * a.H + w.own] * LOG2E : 0.f;
+        mbar_arrive(bar(L::B_OWN + (seq & 1)));
+        ++seq;
+      }
     }
   } else {
     // ------------------------------------------------------------------------------------------------ weights and their gradients
-    const int wg = warp >> 2, r = r0 + (tid & 127);
-    const bool valid = r < rows;
+    const int wg = warp >> 2, r128 = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t S = s_col(wg) + lanes, P = p_col(wg) + lanes;
-    // the columns that this row meets: the keys that the query sees, or the queries that see the key
-    const int2 iv = !valid ? make_int2(0, 0x7fffffff) : KV ? key_interval(a.mask, b, r) : interval(a.mask, b, r);
     const float scale2 = a.scale * LOG2E, c2 = a.cap * LOG2E, inv_c2 = GENERAL && a.cap > 0.f ? 1.f / c2 : 0.f;
+    int base = 0, seq = 0;   // walked tiles and items with tiles so far
+    for (int k = 0;; ++k) {
+    Item w;
+    w.n = -1;
+    bool ok = __all_sync(0xffffffffu, item_at(k, w));
+    if (KV ? named_bar_or(2 + wg, 128, !ok) : named_bar_or(2, 256, !ok)) break;   // (warps that meet at barriers leave together)
+    if (w.n < 0) break;
+    if (lane == 0) item_read(k);
+    const int n = w.n, r = w.r0 + r128;
+    const bool valid = r < rows;
+    // the columns that this row meets: the keys that the query sees, or the queries that see the key
+    const int2 iv = KV ? key_interval(a.mask, w.b, min(r, rows - 1)) : interval(a.mask, w.b, min(r, rows - 1));   // (rows behind the last are never stored)
+    int lo0 = 0, lo1 = 0, hi0 = 0, hi1 = 0;   // what the warp's rows meet in all: [lo0, hi1), every row: [lo1, hi0)
     float nl = 0.f, nd = 0.f;   // -lse log2e and -dO.o of an own query
     uint64_t dex = 0;           // sums of p dP
-    if (!KV && valid) {
-      const size_t row = ((size_t)b * a.mask.T + r) * a.H + own;
-      const uint4 *o = reinterpret_cast<const uint4*>((const bf16*)a.o_in + row * D), *g = reinterpret_cast<const uint4*>((const bf16*)a.dO + row * D);
-      float d0 = 0.f, d1 = 0.f;
-#pragma unroll 4
-      for (int c = 0; c < D / 8; ++c) {
-        const uint4 x = __ldg(o + c), y = __ldg(g + c);
-        d0 = fmaf(bf16_lo(x.x), bf16_lo(y.x), d0);
-        d1 = fmaf(bf16_hi(x.x), bf16_hi(y.x), d1);
-        d0 = fmaf(bf16_lo(x.y), bf16_lo(y.y), d0);
-        d1 = fmaf(bf16_hi(x.y), bf16_hi(y.y), d1);
-        d0 = fmaf(bf16_lo(x.z), bf16_lo(y.z), d0);
-        d1 = fmaf(bf16_hi(x.z), bf16_hi(y.z), d1);
-        d0 = fmaf(bf16_lo(x.w), bf16_lo(y.w), d0);
-        d1 = fmaf(bf16_hi(x.w), bf16_hi(y.w), d1);
-      }
-      nd = -(d0 + d1);
-      nl = -a.lse[row] * LOG2E;
+    if (!KV && n > 0) {
+      ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_OWN + (seq & 1)), (seq >> 1) & 1, s_abort, f.limit));
+      const float* const own = reinterpret_cast<const float*>(smem + L::OFF_OWN) + (seq & 1) * 256;
+      nl = own[r128];
+      nd = own[128 + r128];
+      mbar_arrive(bar(L::B_OWNE + (seq & 1)));
     }
-    bool ok = true;
-    for (int it = wg; it < n; it += 2) {
-      ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_S + wg), (it >> 1) & 1, s_abort, f.limit));
+    lo0 = __shfl_sync(0xffffffffu, iv.x, 0);
+    lo1 = __shfl_sync(0xffffffffu, iv.x, 31);
+    hi0 = __shfl_sync(0xffffffffu, iv.y, 0);
+    hi1 = __shfl_sync(0xffffffffu, iv.y, 31);
+    int h = KV ? w.own * G : w.own, col = (wg ^ base) & 1;   // of this group's next tile: the head, and its number within it
+    for (int it = col; it < n && ok; it += 2, col += 2) {
+      while (KV && col >= w.per) {
+        col -= w.per;
+        ++h;
+      }
+      const int step = base + it;
+      ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_S + wg), (step >> 1) & 1, s_abort, f.limit));
       if (!ok) break;
       tc_fence_after_sync();
-      const int c0 = w0 + (KV ? it % per : it) * 64, st = it % L::ST;
+      const int c0 = w.w0 + col * 64, st = step % L::ST;
+      if (c0 >= hi1 || c0 + 64 <= lo0) {   // (no row of the warp meets the tile)
+        float z[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) z[e] = 0.f;
+        tmem_st32(S, z);
+        tmem_st32(P, z);
+        tmem_wait_st();
+        tc_fence_before_sync();
+        mbar_arrive(bar(L::B_P + wg));
+        if (KV) mbar_arrive(bar(L::B_EMPTY + st));
+        continue;
+      }
       const float4* stat = reinterpret_cast<const float4*>(smem + L::OFF_STAT + st * L::STAT);
-      const int h = KV ? own * G + it / per : own;
       const float slope2 = GENERAL && a.slopes ? a.slopes[h] * LOG2E : 0.f;
       float s[64], p[64];
       tmem_ld32(S, s);
@@ -210,7 +353,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
       tmem_wait_ld();
       // |i - j| = |dist0 - c|
       const float dist0 = (float)(KV ? r - c0 - a.mask.off : r + a.mask.off - c0);
-      if (KV) mbar_wait(bar(L::B_FULL + st), (it / L::ST) & 1);   // (complete by now; makes the copied statistics visible here)
+      if (KV) mbar_wait(bar(L::B_FULL + st), (step / L::ST) & 1);   // (complete by now; makes the copied statistics visible here)
       if (GENERAL) {
         if (a.cap > 0.f) {
           cap_scores(s, a.scale / a.cap, c2);
@@ -273,7 +416,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
           }
         }
       };
-      if (__all_sync(0xffffffffu, iv.x <= c0 && iv.y >= c0 + 64)) weigh(std::false_type{});
+      if (lo1 <= c0 && hi0 >= c0 + 64) weigh(std::false_type{});
       else weigh(std::true_type{});
       tmem_st32(S, s);
       tmem_st32(P, p);
@@ -282,64 +425,83 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
       mbar_arrive(bar(L::B_P + wg));
       if (KV) mbar_arrive(bar(L::B_EMPTY + st));
     }
-    if (ok && n > 0) ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_DONE), 0, s_abort, f.limit));
-    float* const s_dex = reinterpret_cast<float*>(smem + L::OFF_DEX);
+    base += n;
+    if (ok && n > 0) ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_ACC), seq & 1, s_abort, f.limit));
+    float* const s_dex = reinterpret_cast<float*>(smem + L::OFF_DEX) + (k & 1) * 256;
     if (!KV) {
       float d0, d1;
       f2_unpack(dex, d0, d1);
       s_dex[tid] = d0 + d1;
-      ok = !named_bar_or(2, 256, !ok);   // (all of them go on, or none)
     }
-    if (ok) {
-      tc_fence_after_sync();
-      float fix = 0.f;   // dO.o - D
-      if (!KV) {
-        const float d = s_dex[tid & 127] + s_dex[128 + (tid & 127)];
-        fix = -nd - d;
-        if (valid && wg == 0) {
-          float* const w = a.stat + ((size_t)b * a.H + own) * a.stat_stride + r;
-          w[0] = nl;
-          w[(size_t)a.B * a.H * a.stat_stride] = -d;
-        }
+    if (KV ? named_bar_or(2 + wg, 128, !ok) : named_bar_or(2, 256, !ok)) break;   // (all of them go on, or none)
+    tc_fence_after_sync();
+    float fix = 0.f;   // dO.o - D
+    if (!KV) {
+      const float d = s_dex[r128] + s_dex[128 + r128];
+      fix = -nd - d;
+      if (valid && wg == 0 && n > 0) {
+        float* const st = a.stat + ((size_t)w.b * a.H + w.own) * a.stat_stride + r;
+        st[0] = nl;
+        st[(size_t)a.B * a.H * a.stat_stride] = -d;
       }
-      // keys: one group stores dv, the other dk; queries: half of dq's channels each
-      const uint32_t acc = (KV ? (wg ? acc1 : acc2) : acc1) + lanes;
-      bf16* const dst = KV ? (bf16*)(wg ? a.dk : a.dv) + (((size_t)b * a.mask.T_k + r) * a.H_kv + own) * D
-                           : (bf16*)a.dq + (((size_t)b * a.mask.T + r) * a.H + own) * D;
-      const float mul = KV && !wg ? 1.f : a.scale;
-      float test = 0.f;
+    }
+    // keys: one group stores dv, the other dk; queries: half of dq's channels each (all of them one group at D = 64); by 64 channels
+    // through shared memory and the copy engine, which leaves out rows behind the last
+    const uint32_t acc = (KV && !wg ? acc2 : acc1) + lanes, out = sb + L::OFF_OUT + wg * L::OUT;
+    const float mul = KV && !wg ? 1.f : a.scale;
+    const int c_first = KV ? 0 : wg * 64, c_end = KV ? D : min(D, c_first + 64);
+    float test = 0.f;
+    if (c_first >= c_end && n > 0) {
+      tc_fence_before_sync();
+      mbar_arrive(bar(L::B_ACCE));
+    }
 #pragma unroll 1
-      for (int c = KV ? 0 : wg * (D / 2); c < (KV ? D : (wg + 1) * (D / 2)); c += 32) {
-        float o[32];
-        if (n > 0) {
-          tmem_ld32(acc + c, o);
-          if (!KV) {
-            float w[32];
-            tmem_ld32(acc2 + lanes + c, w);
-            tmem_wait_ld();
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = fmaf(fix, w[e], o[e]);
-          }
+    for (int c = c_first; c < c_end; c += 32) {
+      float o[32];
+      if (n > 0) {
+        tmem_ld32(acc + c, o);
+        if (!KV) {
+          float u[32];
+          tmem_ld32(acc2 + lanes + c, u);
           tmem_wait_ld();
-        } else {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+          for (int e = 0; e < 32; ++e) o[e] = fmaf(fix, u[e], o[e]);
         }
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          o[e] *= mul;
-          test = fmaf(o[e], 0.f, test);
+        tmem_wait_ld();
+        if (c + 32 == c_end) {
+          tc_fence_before_sync();
+          mbar_arrive(bar(L::B_ACCE));
         }
-        if (valid) {
-          uint4* w = reinterpret_cast<uint4*>(dst + c);
+      } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            w[e] = make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]), pack_bf16(o[8 * e + 4], o[8 * e + 5]),
-                              pack_bf16(o[8 * e + 6], o[8 * e + 7]));
+        for (int e = 0; e < 32; ++e) o[e] = 0.f;
+      }
+      if (c % 64 == 0) {
+        if (r128 == 0) tma_store_wait_read();
+        named_bar_sync(4 + wg, 128);
+      }
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        o[e] *= mul;
+        test = fmaf(o[e], 0.f, test);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        sts128(out + sw128(r128, c / 8 % 8 + e), make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]),
+                                                          pack_bf16(o[8 * e + 4], o[8 * e + 5]), pack_bf16(o[8 * e + 6], o[8 * e + 7])));
+      if (c % 64 == 32) {
+        fence_proxy_async();
+        named_bar_sync(4 + wg, 128);
+        if (r128 == 0) {
+          tma_store_4d(KV && !wg ? &tm_o2 : &tm_o1, out, c - 32, w.own, w.r0, w.b);
+          tma_store_commit();
         }
       }
-      if (valid && !(test == 0.f)) s_flags[2] = 1;
     }
+    if (__any_sync(0xffffffffu, valid && !(test == 0.f)) && lane == 0) note_bad(s_list, (int*)(s_flags + 2), w.idx);
+    if (n > 0) ++seq;
+    }
+    if (r128 == 0) tma_store_wait_all();
   }
   __syncthreads();
   if (*s_abort) {
@@ -349,11 +511,14 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
   tc_fence_before_sync();
   __syncthreads();
   if (warp == 8) tmem_dealloc(tmem, 512);
-  const bool again = s_flags[2] && !*s_abort;
-  __syncthreads();                                     // (the flags lie in the shared memory that is used again)
-  if (again && tid < 128) {
-    if (KV) dkdv_again<D>(a, reinterpret_cast<float*>(smem), b, own, r0);
-    else dq_again<D>(a, reinterpret_cast<float*>(smem), b, own, r0);
+  const int bad = *s_abort ? 0 : s_flags[2];
+  if (!bad || tid >= 128) return;
+  for (int r = 0; r < rounds; ++r) {
+    const int idx = index_of(r);
+    if (idx >= f.items || !is_bad(s_list, bad, idx)) continue;
+    const Item w = item_of(idx);
+    if (KV) dkdv_again<D>(a, reinterpret_cast<float*>(smem), w.b, w.own, w.r0);
+    else dq_again<D>(a, reinterpret_cast<float*>(smem), w.b, w.own, w.r0);
   }
 }
 
@@ -362,10 +527,12 @@ static int bwd_tc(const AttnCall& c) {
   using L = BwdLay<D>;
   const Args& a = c.a;
   const int T = a.mask.T, T_k = a.mask.T_k;
-  CUtensorMap q, g, k, v;
+  CUtensorMap q, g, k, v, o1, o2;
   const int rq = KV ? 64 : 128, rk = KV ? 128 : 64;
   if (!tensor_map(&q, a.q, false, a.H, T, a.B, D, 64, rq, true) || !tensor_map(&g, a.dO, false, a.H, T, a.B, D, 64, rq, true) ||
-      !tensor_map(&k, a.k, false, a.H_kv, T_k, a.B, D, 64, rk, true) || !tensor_map(&v, a.v, false, a.H_kv, T_k, a.B, D, 64, rk, true))
+      !tensor_map(&k, a.k, false, a.H_kv, T_k, a.B, D, 64, rk, true) || !tensor_map(&v, a.v, false, a.H_kv, T_k, a.B, D, 64, rk, true) ||
+      !tensor_map(&o1, KV ? a.dk : a.dq, false, KV ? a.H_kv : a.H, KV ? T_k : T, a.B, D, 64, 128, true) ||
+      !tensor_map(&o2, KV ? a.dv : a.dq, false, KV ? a.H_kv : a.H, KV ? T_k : T, a.B, D, 64, 128, true))
     return LAWCAT_ERR_CUDA;
   const int tiles = ((KV ? T_k : T) + 127) / 128;
   const long long blocks = (long long)tiles * a.B * (KV ? a.H_kv : a.H);
@@ -377,9 +544,10 @@ static int bwd_tc(const AttnCall& c) {
     note_cuda_error(e, __FILE__, __LINE__);
     return LAWCAT_ERR_CUDA;
   }
-  const BwdArgs f{a, tiles, wait_limit()};
+  const int heads = KV ? a.H_kv : a.H;
+  const BwdArgs f{a, fast_div(a.B * heads), fast_div(heads), fast_div(a.H / a.H_kv), tiles, (int)blocks, wait_limit()};
   LAWCAT_LAUNCH(KV ? "attn_dkdv_tc" : "attn_dq_tc", c.stream,
-                kernel<<<(unsigned)blocks, L::THREADS, L::BYTES, c.stream>>>(KV ? k : q, KV ? v : g, KV ? q : k, KV ? g : v, f));
+                kernel<<<(unsigned)std::min<long long>(blocks, sm_count()), L::THREADS, L::BYTES, c.stream>>>(KV ? k : q, KV ? v : g, KV ? q : k, KV ? g : v, o1, o2, f));
   LAWCAT_CHECK_LAUNCH();
   return LAWCAT_OK;
 }

@@ -13,8 +13,8 @@
 // The accumulator O_i is rescaled only when a row's maximum has grown by more than 2^8 since it was last scaled (the weights then
 // stay within 2^8 in fp32 and bf16 alike), by the softmax warps themselves, behind the product of the tile in front.
 // The products of the two tiles are issued in turn (S_0, O_0, S_1, O_1), which keeps the warpgroups half a step apart: weighing in
-// step, they meet at the pipe of the special functions and leave it idle together. Half of the exponentials of a tile that all rows
-// see whole are polynomials on the FMA pipe.
+// step, they meet at the pipe of the special functions and leave it idle together. (Taking a quarter, three eighths or half of the
+// exponentials as polynomials on the FMA pipe made it slower, 440 us at 8192 tokens and 32/8 heads of 128 against 457, 479 and 487.)
 // One block per SM takes items in turn, the longest first: while an item's last tiles are weighed and its outputs stored, the next
 // one's queries and first keys are already on their way (a sequence of 1024 tokens has few key tiles per item, and a block that
 // starts and ends with each of them spent half its time so). Code that runs once per item is kept off the softmax warps: it comes
@@ -352,44 +352,45 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const float base = m == -INFINITY ? 0.f : m;
         const uint64_t sc = f2_pack(GENERAL ? 1.f : scale2, GENERAL ? 1.f : scale2), nb = f2_pack(-base, -base);
         uint64_t sum0 = 0, sum1 = 0;
-        // every other pair of a tile that all rows see whole takes its exponentials on the FMA pipe: the special functions' pipe is
-        // what a tile waits for (below -126 and for -infinity the two differ, so not where keys are hidden)
-        auto weigh = [&](auto first, auto mixed) {   // 32 scores from column `first` on: the weights, two to a register, in their place
+        auto weigh = [&](auto first) {   // 32 scores from column `first` on: the weights, two to a register, in their place
           constexpr int c = decltype(first)::value;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const uint64_t z = f2_fma(f2_pack(s[c + 2 * e], s[c + 2 * e + 1]), sc, nb);
-            float x, y;
-            if (decltype(mixed)::value && (e & 1)) {
-              ex2_pair(z, x, y);
-            } else {
-              f2_unpack(z, x, y);
-              x = ex2f(x);
-              y = ex2f(y);
+          for (int q = 0; q < 16; q += 8) {   // (step by step over eight pairs: what one warp has in flight is all that hides latencies)
+            uint64_t z[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = f2_fma(f2_pack(s[c + 2 * (q + e)], s[c + 2 * (q + e) + 1]), sc, nb);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              float u, v;
+              f2_unpack(z[e], u, v);
+              z[e] = f2_pack(ex2f(u), ex2f(v));
             }
-            if (e & 1) sum1 = f2_add(sum1, f2_pack(x, y));
-            else sum0 = f2_add(sum0, f2_pack(x, y));
-            s[c / 2 + e] = __uint_as_float(pack_bf16(x, y));
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+              sum0 = f2_add(sum0, z[e]);
+              sum1 = f2_add(sum1, z[e + 1]);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              float u, v;
+              f2_unpack(z[e], u, v);
+              s[c / 2 + q + e] = __uint_as_float(pack_bf16(u, v));
+            }
           }
         };
         using C0 = std::integral_constant<int, 0>;
         using C32 = std::integral_constant<int, 32>;
-        if (whole) {
-          weigh(C0{}, std::true_type{});
-          weigh(C32{}, std::true_type{});
+        if (whole || met(0)) {
+          weigh(C0{});
         } else {
-          if (met(0)) {
-            weigh(C0{}, std::false_type{});
-          } else {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = 0.f;
-          }
-          if (met(32)) {
-            weigh(C32{}, std::false_type{});
-          } else {
+          for (int e = 0; e < 16; ++e) s[e] = 0.f;
+        }
+        if (whole || met(32)) {
+          weigh(C32{});
+        } else {
 #pragma unroll
-            for (int e = 16; e < 32; ++e) s[e] = 0.f;
-          }
+          for (int e = 16; e < 32; ++e) s[e] = 0.f;
         }
         tmem_st32(S, s);
         float x, y;

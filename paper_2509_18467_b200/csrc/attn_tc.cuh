@@ -47,29 +47,6 @@ inline FastDiv fast_div(uint32_t d) {
 __device__ __forceinline__ int quot(int n, const FastDiv& f) { return (int)(((uint64_t)(uint32_t)n * f.mul) >> f.shift); }
 __device__ __forceinline__ int rest(int n, int q, const FastDiv& f) { return n - q * (int)f.d; }
 
-// 2^x for two numbers on the FMA pipe: x = n + f with n the nearest integer (by adding 1.5 2^23), 2^f a polynomial of degree 4 (least
-// maximum relative error on [-1/2, 1/2]: 2.6e-6, a fifteen-hundredth of the rounding to bf16 that follows), n added to the exponent.
-// x <= 127; below -126 the result is 2^-126 or so, as far below bf16's interest. A NaN comes out as a huge number: the row it belongs
-// to is not finite then, and is computed again.
-__device__ __forceinline__ void ex2_pair(uint64_t x, float& a, float& b) {
-  float x0, x1;
-  f2_unpack(x, x0, x1);
-  asm("max.NaN.f32 %0, %1, 0fC2FC0000;" : "=f"(x0) : "f"(x0));   // -126
-  asm("max.NaN.f32 %0, %1, 0fC2FC0000;" : "=f"(x1) : "f"(x1));
-  x = f2_pack(x0, x1);
-  const uint64_t magic = f2_pack(12582912.f, 12582912.f), t = f2_add(x, magic);
-  const uint64_t f = f2_fma(f2_add(t, f2_pack(-12582912.f, -12582912.f)), f2_pack(-1.f, -1.f), x);
-  uint64_t r = f2_fma(f2_pack(0.009570096619427204f, 0.009570096619427204f), f, f2_pack(0.05591785907745361f, 0.05591785907745361f));
-  r = f2_fma(r, f, f2_pack(0.240247443318367f, 0.240247443318367f));
-  r = f2_fma(r, f, f2_pack(0.6931217908859253f, 0.6931217908859253f));
-  r = f2_fma(r, f, f2_pack(0.9999992847442627f, 0.9999992847442627f));
-  float t0, t1;
-  f2_unpack(t, t0, t1);
-  f2_unpack(r, a, b);
-  a = __uint_as_float(__float_as_uint(a) + (__float_as_uint(t0) << 23));
-  b = __uint_as_float(__float_as_uint(b) + (__float_as_uint(t1) << 23));
-}
-
 // rows x D channels of one head at token t into slabs of 64 channels (rows x 128 bytes, swizzled)
 template <int D, int ROWS>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int t, int b) {
