@@ -12,13 +12,11 @@
 // (With dO.o for D the gradients of q and k were 2.6e-3 off 64 bits, of which 2.3e-3 are the roundings below.)
 // The sums over queries and over keys stay in tensor memory per item, in one order: no atomics, the same bits every time.
 // The price is S and dP computed twice (7 products of 128 x 128 x d per pair of tiles instead of 5).
-// One block per SM takes items in turn, the longest first, as in the forward: the next item's own tiles and first walked ones come in
+// A block takes items in turn, the longest first, as in the forward: the next item's own tiles and first walked ones come in
 // while this one's last are weighed and its gradients leave through shared memory and the copy engine. dO.o is summed by two warps of
 // their own, an item ahead.
 // Rounding: P and dX to bf16 as operands, the gradients once. All else is fp32.
 // Rows that come out not finite are computed again on the CUDA cores, as in the forward.
-#include <algorithm>
-
 #include "attn_tc.cuh"
 
 namespace lawcat {
@@ -27,7 +25,7 @@ namespace attn {
 struct BwdArgs {
   Args a;
   FastDiv bh, heads, group;   // B times the heads that own items, those heads, H / H_kv
-  int tiles, items;
+  int tiles;
   long long limit;
 };
 
@@ -37,11 +35,11 @@ struct BwdLay {
   static constexpr int ST = D == 128 ? 3 : 4, SLOTS = 4;
   static constexpr uint32_t STAGE = 2 * WALK, OUT = 128 * 128;                  // a warpgroup's gradients on their way: 64 channels
   static constexpr uint32_t OFF_A = 0, OFF_RING = 2 * OWN, OFF_OUT = OFF_RING + ST * STAGE, OFF_STAT = OFF_OUT + 2 * OUT, OFF_DEX = OFF_STAT + ST * STAT,
-                            OFF_OWN = OFF_DEX + 2048, OFF_LIST = OFF_OWN + 2048, OFF_ITEM = OFF_LIST + BAD_MAX * 4, OFF_BAR = OFF_ITEM + SLOTS * 64;
+                            OFF_OWN = OFF_DEX + 2048, OFF_LIST = OFF_OWN + 2048, OFF_ITEM = OFF_LIST + BAD_MAX * 4, OFF_ASK = OFF_ITEM + SLOTS * 64, OFF_BAR = OFF_ASK + 16;
   static constexpr uint32_t BYTES = OFF_BAR + 512, E1 = (uint32_t)dq_smem<D, 4, 128>(), E2 = (uint32_t)dkdv_smem<D, 4, 128>();
   static constexpr int THREADS = 384;   // weights, copies, products, two warps for dO.o
   static constexpr int B_A = 0, B_AE = 1, B_FULL = 2, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + 2, B_ACC = B_P + 2, B_ACCE = B_ACC + 1,
-                       B_OWN = B_ACCE + 1, B_OWNE = B_OWN + 2, B_ITEM = B_OWNE + 2, B_ITEME = B_ITEM + SLOTS, NBAR = B_ITEME + SLOTS;
+                       B_OWN = B_ACCE + 1, B_OWNE = B_OWN + 2, B_ITEM = B_OWNE + 2, B_ITEME = B_ITEM + SLOTS, B_ASK = B_ITEME + SLOTS, NBAR = B_ASK + 1;
   static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 512 && E1 <= OFF_LIST && E2 <= OFF_LIST, "shared memory");
 };
 
@@ -99,8 +97,6 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
     w.n = KV ? w.per * G : w.per;
     return w;
   };
-  const int rounds = (f.items + (int)gridDim.x - 1) / (int)gridDim.x;
-  auto index_of = [&](int r) { return r * (int)gridDim.x + (r & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x); };
 
   if (tid == 0) {
     mbar_init(bar(L::B_A), 1);
@@ -121,6 +117,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
       mbar_init(bar(L::B_ITEM + i), 1);
       mbar_init(bar(L::B_ITEME + i), KV ? 9 : 11);    // (warps of weights, the product thread, the two for dO.o)
     }
+    mbar_init(bar(L::B_ASK), 1);
     s_flags[1] = 0;
     s_flags[2] = 0;
     mbar_fence_init();
@@ -155,43 +152,53 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
     if (elect_one()) {
       int step = 0, seq = 0, k = 0;   // walked tiles, items with tiles, items so far
       bool ok = true;
-      for (int r = 0; r <= rounds && ok; ++r) {
-        const int idx = r < rounds ? index_of(r) : 0;
-        if (idx >= f.items) continue;
-        Item w = item_of(idx);
-        if (r == rounds) w.n = -1;
+      int idx = (int)blockIdx.x;
+      for (;;) {
+        Item w = item_of(max(idx, 0));
+        if (idx < 0) w.n = -1;
         if (k >= L::SLOTS) ok = wait_bar(bar(L::B_ITEME + k % L::SLOTS), (k / L::SLOTS - 1) & 1, s_abort, f.limit);
         if (!ok) break;
         *reinterpret_cast<Item*>(smem + L::OFF_ITEM + k % L::SLOTS * 64) = w;
         mbar_arrive(bar(L::B_ITEM + k % L::SLOTS));
         ++k;
-        if (w.n <= 0) continue;
-        if (seq > 0) ok = wait_bar(bar(L::B_AE), (seq - 1) & 1, s_abort, f.limit);
-        if (!ok) break;
-        mbar_arrive_expect_tx(bar(L::B_A), 2 * L::OWN);
-        load_tile<D, 128>(sb + L::OFF_A, &tm_a1, bar(L::B_A), w.own, w.r0, w.b);
-        load_tile<D, 128>(sb + L::OFF_A + L::OWN, &tm_a2, bar(L::B_A), w.own, w.r0, w.b);
-        int h = KV ? w.own * G : quot(w.own, f.group), at = w.w0, left = w.per;
-        for (int it = 0; it < w.n; ++it, ++step) {
-          const int s = step % L::ST;
-          if (step >= L::ST) ok = wait_bar(bar(L::B_EMPTY + s), (step / L::ST - 1) & 1, s_abort, f.limit);
+        if (idx < 0) break;
+        if (w.n > 0) {
+          if (seq > 0) ok = wait_bar(bar(L::B_AE), (seq - 1) & 1, s_abort, f.limit);
           if (!ok) break;
-          mbar_arrive_expect_tx(bar(L::B_FULL + s), L::STAGE + (KV ? L::STAT : 0));
-          load_tile<D, 64>(sb + L::OFF_RING + s * L::STAGE, &tm_b1, bar(L::B_FULL + s), h, at, w.b);
-          load_tile<D, 64>(sb + L::OFF_RING + s * L::STAGE + L::WALK, &tm_b2, bar(L::B_FULL + s), h, at, w.b);
-          if (KV) {
-            const float* const nl = a.stat + ((size_t)w.b * a.H + h) * a.stat_stride + at;
-            bulk_load(sb + L::OFF_STAT + s * L::STAT, nl, 256, bar(L::B_FULL + s));
-            bulk_load(sb + L::OFF_STAT + s * L::STAT + 256, nl + (size_t)a.B * a.H * a.stat_stride, 256, bar(L::B_FULL + s));
+          mbar_arrive_expect_tx(bar(L::B_A), 2 * L::OWN);
+          load_tile<D, 128>(sb + L::OFF_A, &tm_a1, bar(L::B_A), w.own, w.r0, w.b);
+          load_tile<D, 128>(sb + L::OFF_A + L::OWN, &tm_a2, bar(L::B_A), w.own, w.r0, w.b);
+          int h = KV ? w.own * G : quot(w.own, f.group), at = w.w0, left = w.per;
+          for (int it = 0; it < w.n; ++it, ++step) {
+            const int s = step % L::ST;
+            if (step >= L::ST) ok = wait_bar(bar(L::B_EMPTY + s), (step / L::ST - 1) & 1, s_abort, f.limit);
+            if (!ok) break;
+            mbar_arrive_expect_tx(bar(L::B_FULL + s), L::STAGE + (KV ? L::STAT : 0));
+            load_tile<D, 64>(sb + L::OFF_RING + s * L::STAGE, &tm_b1, bar(L::B_FULL + s), h, at, w.b);
+            load_tile<D, 64>(sb + L::OFF_RING + s * L::STAGE + L::WALK, &tm_b2, bar(L::B_FULL + s), h, at, w.b);
+            if (KV) {
+              const float* const nl = a.stat + ((size_t)w.b * a.H + h) * a.stat_stride + at;
+              bulk_load(sb + L::OFF_STAT + s * L::STAT, nl, 256, bar(L::B_FULL + s));
+              bulk_load(sb + L::OFF_STAT + s * L::STAT + 256, nl + (size_t)a.B * a.H * a.stat_stride, 256, bar(L::B_FULL + s));
+            }
+            at += 64;
+            if (--left == 0) {   // (the group's next head)
+              ++h;
+              at = w.w0;
+              left = w.per;
+            }
           }
-          at += 64;
-          if (--left == 0) {   // (the group's next head)
-            ++h;
-            at = w.w0;
-            left = w.per;
-          }
+          ++seq;
         }
-        ++seq;
+        // (asked for behind the item's loads, a ring of tiles before its end: asked for at its start, the next item often went to the
+        // block with the longest one in hand)
+        idx = -1;
+        if (s_flags[2] == 0) {
+          ask_item(sb + L::OFF_ASK, bar(L::B_ASK));
+          ok = ok && wait_bar(bar(L::B_ASK), (k - 1) & 1, s_abort, f.limit);
+          if (!ok) break;
+          idx = read_item(sb + L::OFF_ASK);
+        }
       }
     }
   } else if (warp == 9) {
@@ -511,12 +518,11 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
   tc_fence_before_sync();
   __syncthreads();
   if (warp == 8) tmem_dealloc(tmem, 512);
-  const int bad = *s_abort ? 0 : s_flags[2];
-  if (!bad || tid >= 128) return;
-  for (int r = 0; r < rounds; ++r) {
-    const int idx = index_of(r);
-    if (idx >= f.items || !is_bad(s_list, bad, idx)) continue;
-    const Item w = item_of(idx);
+  const int bad = *s_abort ? 0 : min(s_flags[2], BAD_MAX);
+  if (tid >= 128) return;
+  for (int e = 0; e < bad; ++e) {
+    if (noted_before(s_list, e)) continue;
+    const Item w = item_of(s_list[e]);
     if (KV) dkdv_again<D>(a, reinterpret_cast<float*>(smem), w.b, w.own, w.r0);
     else dq_again<D>(a, reinterpret_cast<float*>(smem), w.b, w.own, w.r0);
   }
@@ -545,9 +551,9 @@ static int bwd_tc(const AttnCall& c) {
     return LAWCAT_ERR_CUDA;
   }
   const int heads = KV ? a.H_kv : a.H;
-  const BwdArgs f{a, fast_div(a.B * heads), fast_div(heads), fast_div(a.H / a.H_kv), tiles, (int)blocks, wait_limit()};
+  const BwdArgs f{a, fast_div(a.B * heads), fast_div(heads), fast_div(a.H / a.H_kv), tiles, wait_limit()};
   LAWCAT_LAUNCH(KV ? "attn_dkdv_tc" : "attn_dq_tc", c.stream,
-                kernel<<<(unsigned)std::min<long long>(blocks, sm_count()), L::THREADS, L::BYTES, c.stream>>>(KV ? k : q, KV ? v : g, KV ? q : k, KV ? g : v, o1, o2, f));
+                kernel<<<(unsigned)blocks, L::THREADS, L::BYTES, c.stream>>>(KV ? k : q, KV ? v : g, KV ? q : k, KV ? g : v, o1, o2, f));
   LAWCAT_CHECK_LAUNCH();
   return LAWCAT_OK;
 }

@@ -15,7 +15,7 @@
 // The products of the two tiles are issued in turn (S_0, O_0, S_1, O_1), which keeps the warpgroups half a step apart: weighing in
 // step, they meet at the pipe of the special functions and leave it idle together. (Taking a quarter, three eighths or half of the
 // exponentials as polynomials on the FMA pipe made it slower, 440 us at 8192 tokens and 32/8 heads of 128 against 457, 479 and 487.)
-// One block per SM takes items in turn, the longest first: while an item's last tiles are weighed and its outputs stored, the next
+// A block takes items in turn, the longest first: while an item's last tiles are weighed and its outputs stored, the next
 // one's queries and first keys are already on their way (a sequence of 1024 tokens has few key tiles per item, and a block that
 // starts and ends with each of them spent half its time so). Code that runs once per item is kept off the softmax warps: it comes
 // from the instruction caches' far end, at five cycles an instruction.
@@ -38,7 +38,6 @@ struct FwdArgs {
   FastDiv pairs;      // items per (batch, query tile): H / 2 head pairs, or H
   FastDiv bp, group, parts_d;   // B pairs, H / H_kv, parts
   int tiles;          // query tiles
-  int items;
   int two_heads;      // an item's two tiles are two heads (else two neighbouring tiles of one head)
   int parts;
   float* part_o;      // [parts, B, H, T, D] where parts > 1
@@ -53,12 +52,12 @@ struct FwdLay {
   static constexpr uint32_t OUT = 128 * 128;                     // a warpgroup's outputs on their way: 64 channels (or 32 in fp32)
   static constexpr int SLOTS = 4;                                // items on their way
   static constexpr uint32_t OFF_Q = 0, OFF_RING = NT * TILE, OFF_OUT = OFF_RING + ST * KT, OFF_ML = OFF_OUT + OUT, OFF_LIST = OFF_ML + 2 * NT * 128 * 8,
-                            OFF_ITEM = OFF_LIST + BAD_MAX * 4, OFF_BAR = OFF_ITEM + SLOTS * 64;
+                            OFF_ITEM = OFF_LIST + BAD_MAX * 4, OFF_ASK = OFF_ITEM + SLOTS * 64, OFF_BAR = OFF_ASK + 16;
   static constexpr uint32_t BYTES = OFF_BAR + 512;
   static constexpr int THREADS = NT * 128 + 192;                 // softmax, outputs, copies, products
   // mbarriers
   static constexpr int B_Q = 0, B_QE = 1, B_FULL = 2, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + 2 * NT, B_O = B_P + 2 * NT, B_OE = B_O + 2 * NT,
-                       B_ML = B_OE + NT, B_ITEM = B_ML + NT, B_ITEME = B_ITEM + SLOTS, NBAR = B_ITEME + SLOTS;
+                       B_ML = B_OE + NT, B_ITEM = B_ML + NT, B_ITEME = B_ITEM + SLOTS, B_ASK = B_ITEME + SLOTS, NBAR = B_ASK + 1;
   static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 512 && fwd_smem<D, 4, 128>() <= OFF_LIST && NT * (128 + D) <= 512, "shared memory, tensor memory");
 };
 
@@ -110,9 +109,6 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   };
   auto head_of = [&](const Item& w, int i) { return w.h0 + (f.two_heads ? i : 0); };
   auto row_of = [&](const Item& w, int i) { return w.tb + (f.two_heads ? 0 : 128 * i); };
-  // this block's items: one of each round of gridDim.x, odd rounds from the other end (they are in falling order of length)
-  const int rounds = (f.items + (int)gridDim.x - 1) / (int)gridDim.x;
-  auto index_of = [&](int r) { return r * (int)gridDim.x + (r & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x); };
 
   if (tid == 0) {
     mbar_init(bar(L::B_Q), 1);
@@ -134,6 +130,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       mbar_init(bar(L::B_ITEM + i), 1);
       mbar_init(bar(L::B_ITEME + i), 13);   // (warps of softmax and outputs, and the product thread)
     }
+    mbar_init(bar(L::B_ASK), 1);
     s_flags[1] = 0;
     s_flags[2] = 0;
     mbar_fence_init();
@@ -166,29 +163,39 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     if (elect_one()) {
       int at = 0, seq = 0, k = 0;   // tiles, items with tiles, and items so far
       bool ok = true;
-      for (int r = 0; r <= rounds && ok; ++r) {
-        const int idx = r < rounds ? index_of(r) : 0;
-        if (idx >= f.items) continue;
-        Item w = item_of(idx);
-        if (r == rounds) w.n = -1;
+      int idx = (int)blockIdx.x;
+      for (;;) {
+        Item w = item_of(max(idx, 0));
+        if (idx < 0) w.n = -1;
         if (k >= L::SLOTS) ok = wait_bar(bar(L::B_ITEME + k % L::SLOTS), (k / L::SLOTS - 1) & 1, s_abort, f.limit);
         if (!ok) break;
         *reinterpret_cast<Item*>(smem + L::OFF_ITEM + k % L::SLOTS * 64) = w;
         mbar_arrive(bar(L::B_ITEM + k % L::SLOTS));
         ++k;
-        if (w.n <= 0) continue;
-        if (seq > 0) ok = wait_bar(bar(L::B_QE), (seq - 1) & 1, s_abort, f.limit);
-        if (!ok) break;
-        mbar_arrive_expect_tx(bar(L::B_Q), NT * L::TILE);
-        for (int i = 0; i < NT; ++i) load_tile<D, 128>(sb + L::OFF_Q + i * L::TILE, &tm_q, bar(L::B_Q), head_of(w, i), row_of(w, i), w.b);
-        for (int it = 0; it < 2 * w.n; ++it, ++at) {
-          const int s = at % L::ST;
-          if (at >= L::ST) ok = wait_bar(bar(L::B_EMPTY + s), (at / L::ST - 1) & 1, s_abort, f.limit);
+        if (idx < 0) break;
+        if (w.n > 0) {
+          if (seq > 0) ok = wait_bar(bar(L::B_QE), (seq - 1) & 1, s_abort, f.limit);
           if (!ok) break;
-          mbar_arrive_expect_tx(bar(L::B_FULL + s), L::KT);
-          load_tile<D, 64>(sb + L::OFF_RING + s * L::KT, it & 1 ? &tm_v : &tm_k, bar(L::B_FULL + s), w.g, w.j_first + it / 2 * 64, w.b);
+          mbar_arrive_expect_tx(bar(L::B_Q), NT * L::TILE);
+          for (int i = 0; i < NT; ++i) load_tile<D, 128>(sb + L::OFF_Q + i * L::TILE, &tm_q, bar(L::B_Q), head_of(w, i), row_of(w, i), w.b);
+          for (int it = 0; it < 2 * w.n; ++it, ++at) {
+            const int s = at % L::ST;
+            if (at >= L::ST) ok = wait_bar(bar(L::B_EMPTY + s), (at / L::ST - 1) & 1, s_abort, f.limit);
+            if (!ok) break;
+            mbar_arrive_expect_tx(bar(L::B_FULL + s), L::KT);
+            load_tile<D, 64>(sb + L::OFF_RING + s * L::KT, it & 1 ? &tm_v : &tm_k, bar(L::B_FULL + s), w.g, w.j_first + it / 2 * 64, w.b);
+          }
+          ++seq;
         }
-        ++seq;
+        // (asked for behind the item's loads, a ring of tiles before its end: asked for at its start, the next item often went to the
+        // block with the longest one in hand)
+        idx = -1;
+        if (s_flags[2] == 0) {
+          ask_item(sb + L::OFF_ASK, bar(L::B_ASK));
+          ok = ok && wait_bar(bar(L::B_ASK), (k - 1) & 1, s_abort, f.limit);
+          if (!ok) break;
+          idx = read_item(sb + L::OFF_ASK);
+        }
       }
     }
   } else if (warp == NT * 4 + 5) {
@@ -507,12 +514,11 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   tc_fence_before_sync();
   __syncthreads();
   if (warp == NT * 4 + 4) tmem_dealloc(tmem, 512);
-  const int bad = *s_abort ? 0 : s_flags[2];
-  if (!bad || tid >= 128) return;
-  for (int r = 0; r < rounds; ++r) {
-    const int idx = index_of(r);
-    if (idx >= f.items || !is_bad(s_list, bad, idx)) continue;
-    const Item w = item_of(idx);
+  const int bad = *s_abort ? 0 : min(s_flags[2], BAD_MAX);
+  if (tid >= 128) return;
+  for (int e = 0; e < bad; ++e) {
+    if (noted_before(s_list, e)) continue;
+    const Item w = item_of(s_list[e]);
     const size_t pb = ((size_t)w.part * a.B + w.b) * a.H;
     for (int i = 0; i < NT; ++i) {
       const size_t at = (pb + head_of(w, i)) * (size_t)T;
@@ -580,7 +586,7 @@ static int fwd_tc(const AttnCall& c, const FwdPlan& pl, void* ws) {
   if (!tensor_map(&tq, a.q, false, a.H, a.mask.T, a.B, D, 64, 128, true) || !tensor_map(&tk, a.k, false, a.H_kv, a.mask.T_k, a.B, D, 64, 64, true) ||
       !tensor_map(&tv, a.v, false, a.H_kv, a.mask.T_k, a.B, D, 64, 64, true) || !tensor_map(&to, a.o, false, a.H, a.mask.T, a.B, D, 64, 128, true))
     return LAWCAT_ERR_CUDA;
-  FwdArgs f{a, fast_div(pl.pairs), fast_div(a.B * pl.pairs), fast_div(a.H / a.H_kv), fast_div(pl.parts), pl.tiles, (int)pl.blocks, pl.two_heads, pl.parts, nullptr, nullptr, wait_limit()};
+  FwdArgs f{a, fast_div(pl.pairs), fast_div(a.B * pl.pairs), fast_div(a.H / a.H_kv), fast_div(pl.parts), pl.tiles, pl.two_heads, pl.parts, nullptr, nullptr, wait_limit()};
   const size_t rows = (size_t)a.B * a.H * a.mask.T * pl.parts;
   if (pl.parts > 1) {
     f.part_o = (float*)ws;
@@ -593,7 +599,7 @@ static int fwd_tc(const AttnCall& c, const FwdPlan& pl, void* ws) {
     note_cuda_error(e, __FILE__, __LINE__);
     return LAWCAT_ERR_CUDA;
   }
-  LAWCAT_LAUNCH("attn_fwd_tc", c.stream, kernel<<<(unsigned)std::min<long long>(pl.blocks, sm_count()), L::THREADS, L::BYTES, c.stream>>>(tq, tk, tv, to, f));
+  LAWCAT_LAUNCH("attn_fwd_tc", c.stream, kernel<<<(unsigned)pl.blocks, L::THREADS, L::BYTES, c.stream>>>(tq, tk, tv, to, f));
   LAWCAT_CHECK_LAUNCH();
   if (pl.parts > 1) {
     const size_t n = (size_t)a.B * a.H * a.mask.T;

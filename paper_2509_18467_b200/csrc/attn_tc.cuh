@@ -65,16 +65,39 @@ __device__ __forceinline__ uint64_t mdesc(uint32_t tile, int kk) {
   return smem_desc(tile + (uint32_t)kk * 2048, ROWS * 128, 1024, LAYOUT_SW128);
 }
 
-// Items of a block that came out not finite, for a second computation behind everything else; more than the list holds: all of them.
+// The launch has one block per item, and as many run as there are SMs: a running block takes over blocks that have not started
+// (cluster launch control), whoever is free first. Their numbers fall with the items' lengths where a mask makes them differ.
+__device__ __forceinline__ void ask_item(uint32_t answer, uint32_t bar) {
+  fence_proxy_async();   // (the last answer has been read)
+  mbar_arrive_expect_tx(bar, 16);
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer), "r"(bar) : "memory");
+}
+// the number of the block that was taken over, or -1: all have started
+__device__ __forceinline__ int read_item(uint32_t answer) {
+  uint32_t got, idx;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\t"
+      "ld.shared.b128 r, [%2];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "mov.u32 %1, 0;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n\t}"
+      : "=r"(got), "=r"(idx)
+      : "r"(answer)
+      : "memory");
+  return got ? (int)idx : -1;
+}
+
+// Items of a block that came out not finite (noted by any of eight warps), for a second computation behind everything else. A block
+// takes over no further items once it has one, so that the list holds those that are on their way then.
 constexpr int BAD_MAX = 64;
 __device__ __forceinline__ void note_bad(int* list, int* count, int idx) {
   const int at = atomicAdd(count, 1);
   if (at < BAD_MAX) list[at] = idx;
 }
-__device__ __forceinline__ bool is_bad(const int* list, int count, int idx) {
-  if (count > BAD_MAX) return true;
-  for (int i = 0; i < count; ++i)
-    if (list[i] == idx) return true;
+__device__ __forceinline__ bool noted_before(const int* list, int at) {
+  for (int i = 0; i < at; ++i)
+    if (list[i] == list[at]) return true;
   return false;
 }
 
