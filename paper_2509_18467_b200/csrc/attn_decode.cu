@@ -40,12 +40,13 @@ __device__ __forceinline__ void quantize8(float (&x)[8], int c0, uint8_t* q_row,
   }
   float scale, low;
   quant_params(lo, hi, fin, scale, low);
+  const float inv = __frcp_rn(scale);
   uint32_t w = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const uint32_t code = quant_code(x[i], scale, low);
-    w |= code << (4 * i);
-    x[i] = fmaf((float)code, scale, low);
+    const float code = quant_code(x[i], scale, low, inv);
+    w |= code_bits(code) << (4 * i);
+    x[i] = fmaf(code, scale, low);
   }
   if (write) {
     *reinterpret_cast<uint32_t*>(q_row + c0 / 2) = w;
@@ -71,8 +72,18 @@ __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
 }
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+    uint32_t w[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) stf<T>(p + i, x[i]);
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
 }
 template <int D>
 __device__ __forceinline__ void load8q(const uint8_t* q_row, const bf16* p_row, int c0, float (&x)[8]) {
@@ -204,69 +215,87 @@ __global__ void __launch_bounds__(DEC_THREADS) attn_decode_kernel(const DecArgs 
   }
 }
 
-// the parts of a (sequence, head), one warp each: every part's sum and values at the common maximum
+// The parts of a (sequence, head): four warps share them out, each at the common maximum, four parts' loads in flight.
 template <typename T, int D>
-__global__ void attn_decode_join_kernel(const DecArgs a) {
-  const int bh = (blockIdx.x * blockDim.x + threadIdx.x) >> 5, lane = threadIdx.x & 31;
-  if (bh >= a.B * a.H) return;
+__global__ void __launch_bounds__(128) attn_decode_join_kernel(const DecArgs a) {
+  constexpr int NC = D / 32 > 0 ? D / 32 : 1;
+  __shared__ float s_acc[4][D], s_l[4];
+  const int bh = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const float* w = a.part + (size_t)bh * a.parts * (D + 2);
   float m = -INFINITY;
   for (int i = lane; i < a.parts; i += 32) m = fmaxf(m, w[(size_t)i * (D + 2)]);
   m = warp_max(m);
   const float base = m == -INFINITY ? 0.f : m;
-  constexpr int NC = D / 32 > 0 ? D / 32 : 1;
   float l = 0.f, acc[NC] = {};
-  for (int i = 0; i < a.parts; ++i) {
+#pragma unroll 4
+  for (int i = warp; i < a.parts; i += 4) {
     const float* x = w + (size_t)i * (D + 2);
+    const bool some = x[1] != 0.f;               // (a part without keys has written nothing else)
     const float f = exp2f(x[0] - base);
-    if (x[1] == 0.f) continue;
-    l = fmaf(f, x[1], l);
+    l += some ? f * x[1] : 0.f;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
-      if (lane + 32 * c < D) acc[c] = fmaf(f, x[2 + lane + 32 * c], acc[c]);
+      if (lane + 32 * c < D) acc[c] += some ? f * x[2 + lane + 32 * c] : 0.f;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int c = 0; c < NC; ++c)
-    if (lane + 32 * c < D) stf<T>((T*)a.o + (size_t)bh * D + lane + 32 * c, acc[c] * inv);
+    if (lane + 32 * c < D) s_acc[warp][lane + 32 * c] = acc[c];
+  if (lane == 0) s_l[warp] = l;
+  __syncthreads();
+  l = s_l[0] + s_l[1] + s_l[2] + s_l[3];
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  for (int c = threadIdx.x; c < D; c += 128)
+    stf<T>((T*)a.o + (size_t)bh * D + c, (s_acc[0][c] + s_acc[1][c] + s_acc[2][c] + s_acc[3][c]) * inv);
 }
 
-// [B, T, H_kv, D] rows of k and v to and from the slots (pos + t) mod C; a thread has eight channels of one row
+// Rows of k and v [B, T, H_kv, D] to and from the slots (pos + t) mod C: memory-bound. A block has 8192 / D tokens of one (sequence,
+// head) of k or of v, a thread eight channels of four of them; a head's slots lie side by side, so that a block writes (reads) codes in
+// one piece. (With one thread per row piece numbered by 64-bit divisions: 8192 tokens, 8 heads of 128, 45 and 40 us.)
 struct QuantArgs {
   void *k, *v;
   const int* pos;
   uint8_t *kq, *vq;
   bf16 *kp, *vp;
-  int B, T, H_kv, C;
+  int T, H_kv, C, chunks;
 };
+constexpr int QUANT_ROWS = 4;   // rows of a thread
+__host__ __device__ constexpr int quant_tokens(int d) { return QUANT_ROWS * 256 / (d / 8); }
 template <typename T, int D, bool WRITE>
 __global__ void __launch_bounds__(256) attn_quant_kernel(const QuantArgs a) {
-  constexpr int V8 = D / 8, NG = D / quant_group(D);
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, row = i / V8;  // row = ((b T + t) H_kv + g)
-  const int c0 = (int)(i % V8) * 8;
+  constexpr int V8 = D / 8, NG = D / quant_group(D), ROWS = 256 / V8;
+  const int bg = blockIdx.x / a.chunks, t0 = (int)(blockIdx.x - bg * a.chunks) * quant_tokens(D), b = bg / a.H_kv, g = bg - b * a.H_kv;
+  const int c0 = threadIdx.x % V8 * 8;
   const bool is_v = blockIdx.y;
-  if (row >= (size_t)a.B * a.T * a.H_kv) return;
-  const int g = (int)(row % a.H_kv);
-  const size_t bt = row / a.H_kv;
-  const int t = (int)(bt % a.T), b = (int)(bt / a.T);
-  const int p0 = a.pos[b];
-  T* const x_row = (T*)(is_v ? a.v : a.k) + row * D + c0;
-  float x[8] = {};
-  if (p0 < 0) {                        // a sequence that is not there: its slots stay, what is read of them is zero
-    if (!WRITE) store8(x_row, x);
-    return;
+  const int p0 = a.pos[b], first = p0 < 0 ? 0 : p0 % a.C;
+  T* const rows = (T*)(is_v ? a.v : a.k) + (((size_t)b * a.T) * a.H_kv + g) * D + c0;
+  uint8_t* const q = is_v ? a.vq : a.kq;
+  bf16* const p = is_v ? a.vp : a.kp;
+  constexpr int N = QUANT_ROWS;
+  auto token = [&](int i) { return t0 + i * ROWS + (int)threadIdx.x / V8; };
+  auto slot_of = [&](int t) {
+    int slot = first + t % a.C;
+    if (slot >= a.C) slot -= a.C;
+    return (size_t)bg * a.C + slot;
+  };
+  float x[N][8];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {   // (all loads first)
+    const int t = token(i);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
+    if (t >= a.T || p0 < 0) continue;
+    if (WRITE) load8(rows + (size_t)t * a.H_kv * D, x[i]);
+    else load8q<D>(q + slot_of(t) * (D / 2), p + slot_of(t) * (2 * NG), c0, x[i]);
   }
-  if (WRITE && t < a.T - a.C) return;  // (a later token takes this slot)
-  const size_t slot = (size_t)(((long long)p0 + t) % a.C);
-  const size_t at = ((size_t)b * a.H_kv + g) * a.C + slot;
-  uint8_t* const q_row = (is_v ? a.vq : a.kq) + at * (D / 2);
-  bf16* const p_row = (is_v ? a.vp : a.kp) + at * (2 * NG);
-  if (WRITE) {
-    load8(x_row, x);
-    quantize8<D>(x, c0, q_row, p_row, true);
-  } else {
-    load8q<D>(q_row, p_row, c0, x);
-    store8(x_row, x);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int t = token(i);
+    if (WRITE) {   // (of more rows than slots the last stay)
+      const size_t at = slot_of(min(t, a.T - 1));
+      quantize8<D>(x[i], c0, q + at * (D / 2), p + at * (2 * NG), t < a.T && t >= a.T - a.C && p0 >= 0);
+    } else if (t < a.T) {
+      store8(rows + (size_t)t * a.H_kv * D, x[i]);   // (zeros for a sequence that is not there)
+    }
   }
 }
 
@@ -311,7 +340,7 @@ int launch_attn_decode_join(const attn::DecArgs& a, int d, int dtype, cudaStream
     auto go = [&](auto t) -> int {
       using T = decltype(t);
       LAWCAT_LAUNCH("attn_decode_join", stream,
-                    attn::attn_decode_join_kernel<T, D><<<(unsigned)(((long long)a.B * a.H + 3) / 4), 128, 0, stream>>>(a));
+                    attn::attn_decode_join_kernel<T, D><<<(unsigned)(a.B * a.H), 128, 0, stream>>>(a));
       LAWCAT_CHECK_LAUNCH();
       return LAWCAT_OK;
     };
@@ -349,8 +378,8 @@ int launch_attn_decode(const AttnDecode& c) {
 
 int launch_attn_quant(const AttnDecode& c, int T, bool write) {
   attn::QuantArgs a{const_cast<void*>(c.k_t), const_cast<void*>(c.v_t), c.pos, (uint8_t*)c.kq, (uint8_t*)c.vq, (bf16*)c.kp, (bf16*)c.vp,
-                    c.B, T, c.H_kv, c.C};
-  const unsigned long long n = ((unsigned long long)c.B * T * c.H_kv * (c.d / 8) + 255) / 256;
+                    T, c.H_kv, c.C, (T + attn::quant_tokens(c.d) - 1) / attn::quant_tokens(c.d)};
+  const unsigned long long n = (unsigned long long)c.B * c.H_kv * a.chunks;
   if (n > 0x7fffffffULL) return LAWCAT_ERR_UNSUPPORTED;
   return by_width(c.d, [&](auto dd) {
     constexpr int D = decltype(dd)::value;

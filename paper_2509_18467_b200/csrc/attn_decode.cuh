@@ -32,11 +32,18 @@ __device__ __forceinline__ void quant_params(float lo, float hi, bool finite, fl
   const float s = __fdiv_rn(hi - low, 15.f);
   scale = finite && isfinite(s) && isfinite(low) ? __bfloat162float(__float2bfloat16_rn(s)) : NAN;
 }
-// (in fp32 as in 64 bits: the difference of two bf16 values a few binades apart is exact, and no quotient of such numbers lies
-// closer to a border between two codes than fp32 tells apart)
-__device__ __forceinline__ uint32_t quant_code(float x, float scale, float low) {
-  return scale > 0.f ? (uint32_t)fminf(fmaxf(rintf(__fdiv_rn(x - low, scale)), 0.f), 15.f) : 0u;
+// The code of x as a float, from inv = 1 / scale: the integer k nearest to (x - low) inv (added to 1.5 2^23, whose last bit is then k's),
+// which near a border between two codes may be one off; the remainder x - low - k scale against half a scale (k scale is exact:
+// 5 bits times 8) puts that right, ties to the even code. (Exact where x - low is, as for bf16 values less than 16 binades apart.)
+__device__ __forceinline__ float quant_code(float x, float scale, float low, float inv) {
+  const float d = x - low, half = 0.5f * scale, t = fmaf(d, inv, 12582912.f);
+  float k = t - 12582912.f;
+  const float r = fmaf(-k, scale, d), e = fabsf(r);
+  if (e > half || (e == half && (__float_as_uint(t) & 1u))) k += copysignf(1.f, r);
+  if (!(scale > 1e-30f)) k = scale > 0.f ? rintf(__fdiv_rn(d, scale)) : 0.f;  // (no reciprocal, no half)
+  return fminf(fmaxf(k, 0.f), 15.f);
 }
+__device__ __forceinline__ uint32_t code_bits(float code) { return __float_as_uint(code + 12582912.f) & 15u; }
 
 // The slots that a step sees, as tiles of 128: an arc of n slots that ends at slot ps = pos mod C and may wrap.
 struct Arc {

@@ -416,7 +416,7 @@ attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, in
 #pragma unroll
       for (int o = 16; o; o >>= 1) lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
       quant_params(lo, warp_max(x), __all_sync(0xffffffffu, isfinite(x)), scale, low);
-      const uint32_t code = quant_code(x, scale, low), other = __shfl_down_sync(0xffffffffu, code, 1);
+      const uint32_t code = code_bits(quant_code(x, scale, low, __frcp_rn(scale))), other = __shfl_down_sync(0xffffffffu, code, 1);
       const uint8_t byte = (uint8_t)(code | other << 4);
       const __nv_bfloat162 pr(__float2bfloat16_rn(scale), __float2bfloat16_rn(low));
       if (!(tid & 1)) {
@@ -494,7 +494,6 @@ attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, in
       vs[i] = __bfloat162float(vp[i].x);
       vm[i] = fmaf(8.f, vs[i], __bfloat162float(vp[i].y));
     }
-    if (it + 1 < n) fetch(it + 1);
     tmem_wait_st();
     fence_proxy_async();
     tc_fence_before_sync();
@@ -515,6 +514,7 @@ attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, in
 #pragma unroll
     for (int c = 0; c < NCOL; c += 16) tmem_ld16(s_col + lanes + c, y + c);
     tmem_wait_ld();
+    if (it + 1 < n) fetch(it + 1);   // (the next tile's codes: behind this one's last wait for a load)
 #pragma unroll
     for (int h = 0; h < HPB; ++h) {
       x[h] = 0.f;

@@ -543,12 +543,12 @@ __global__ void __launch_bounds__(256) attn_fwd_join_kernel(const FwdArgs f) {
   for (int i = lane; i < f.parts; i += 32) m = fmaxf(m, f.part_ml[i * step + at].x);
   m = warp_max(m);
   const float base = m == -INFINITY ? 0.f : m;
-  for (int i = 0; i < f.parts; ++i) {
+#pragma unroll 4
+  for (int i = 0; i < f.parts; ++i) {   // (a part without keys: maximum -infinity, sum and values zero)
     const float2 ml = f.part_ml[i * step + at];
-    if (ml.y == 0.f) continue;
+    const float* x = f.part_o + (i * step + at) * D + lane * NC;
     const float w = exp2f(ml.x - base);
     l = fmaf(w, ml.y, l);
-    const float* x = f.part_o + (i * step + at) * D + lane * NC;
 #pragma unroll
     for (int c = 0; c < NC; ++c) acc[c] = fmaf(w, x[c], acc[c]);
   }
