@@ -348,30 +348,33 @@ attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, in
   // this thread's slot of a tile: codes and parameters; zeros for slots that are not seen (whatever they hold)
   uint32_t kc[WPR], vc[WPR];
   __nv_bfloat162 kp[NG], vp[NG];
-  auto fetch = [&](int it) {
-    const int slot = arc_tile(arc, k0 + it) * 128 + tid;
-    const int back = slot < a.C ? arc_back(arc, slot, a.C) : 0;
-    if (slot < a.C && back < arc.n && back > 0) {
-      const size_t row = row0 + slot;
+  auto load_slot = [&](size_t row) {
 #pragma unroll
-      for (int i = 0; i < WPR / 4; ++i) {
-        const uint4 x = __ldcs(reinterpret_cast<const uint4*>(a.kq + row * (D / 2)) + i), y = __ldcs(reinterpret_cast<const uint4*>(a.vq + row * (D / 2)) + i);
-        kc[4 * i] = x.x; kc[4 * i + 1] = x.y; kc[4 * i + 2] = x.z; kc[4 * i + 3] = x.w;
-        vc[4 * i] = y.x; vc[4 * i + 1] = y.y; vc[4 * i + 2] = y.z; vc[4 * i + 3] = y.w;
-      }
-      if constexpr (NG == 4) {
-        *reinterpret_cast<uint4*>(kp) = __ldcs(reinterpret_cast<const uint4*>(a.kp + row * (2 * NG)));
-        *reinterpret_cast<uint4*>(vp) = __ldcs(reinterpret_cast<const uint4*>(a.vp + row * (2 * NG)));
-      } else {
-        *reinterpret_cast<uint2*>(kp) = __ldcs(reinterpret_cast<const uint2*>(a.kp + row * (2 * NG)));
-        *reinterpret_cast<uint2*>(vp) = __ldcs(reinterpret_cast<const uint2*>(a.vp + row * (2 * NG)));
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < WPR; ++i) kc[i] = vc[i] = 0u;
-#pragma unroll
-      for (int i = 0; i < NG; ++i) kp[i] = vp[i] = __nv_bfloat162(__float2bfloat16_rn(0.f), __float2bfloat16_rn(0.f));
+    for (int i = 0; i < WPR / 4; ++i) {
+      const uint4 x = __ldcs(reinterpret_cast<const uint4*>(a.kq + row * (D / 2)) + i), y = __ldcs(reinterpret_cast<const uint4*>(a.vq + row * (D / 2)) + i);
+      kc[4 * i] = x.x; kc[4 * i + 1] = x.y; kc[4 * i + 2] = x.z; kc[4 * i + 3] = x.w;
+      vc[4 * i] = y.x; vc[4 * i + 1] = y.y; vc[4 * i + 2] = y.z; vc[4 * i + 3] = y.w;
     }
+    if constexpr (NG == 4) {
+      *reinterpret_cast<uint4*>(kp) = __ldcs(reinterpret_cast<const uint4*>(a.kp + row * (2 * NG)));
+      *reinterpret_cast<uint4*>(vp) = __ldcs(reinterpret_cast<const uint4*>(a.vp + row * (2 * NG)));
+    } else {
+      *reinterpret_cast<uint2*>(kp) = __ldcs(reinterpret_cast<const uint2*>(a.kp + row * (2 * NG)));
+      *reinterpret_cast<uint2*>(vp) = __ldcs(reinterpret_cast<const uint2*>(a.vp + row * (2 * NG)));
+    }
+  };
+  auto fetch = [&](int it) {
+    const int s0 = arc_tile(arc, k0 + it) * 128, slot = s0 + tid;
+    if (arc_whole(arc, s0, a.C)) {
+      load_slot(row0 + slot);
+      return;
+    }
+    const int back = slot < a.C ? arc_back(arc, slot, a.C) : 0;
+#pragma unroll
+    for (int i = 0; i < WPR; ++i) kc[i] = vc[i] = 0u;
+#pragma unroll
+    for (int i = 0; i < NG; ++i) kp[i] = vp[i] = __nv_bfloat162(__float2bfloat16_rn(0.f), __float2bfloat16_rn(0.f));
+    if (slot < a.C && back < arc.n && back > 0) load_slot(row0 + slot);
   };
   fetch(0);
 
@@ -445,6 +448,7 @@ attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, in
 #pragma unroll
     for (int i = 0; i < NG; ++i) mid[h * NG + i] = 0.f;
   }
+  const uint32_t v_row = sb + L::OFF_V + sw128(tid, 0);   // (chunk j of the row: its address with bits 4 ... 6 turned over by j)
   bool fail = false;
   for (int it = 0; it < n; ++it) {
     const int slot = arc_tile(arc, k0 + it) * 128 + tid;
@@ -484,7 +488,7 @@ attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, in
         const __nv_bfloat162 y = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), c136);
         w[i] = *reinterpret_cast<const uint32_t*>(&y);
       }
-      sts128(sb + L::OFF_V + (j >> 3) * 16384 + sw128(tid, j & 7), make_uint4(w[0], w[1], w[2], w[3]));
+      sts128((v_row ^ (uint32_t)((j & 7) << 4)) + (j >> 3) * 16384, make_uint4(w[0], w[1], w[2], w[3]));
     }
     float ks[NG], kl[NG], vs[NG], vm[NG];
 #pragma unroll
@@ -494,6 +498,7 @@ attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, in
       vs[i] = __bfloat162float(vp[i].x);
       vm[i] = fmaf(8.f, vs[i], __bfloat162float(vp[i].y));
     }
+    if (it + 1 < n) fetch(it + 1);
     tmem_wait_st();
     fence_proxy_async();
     tc_fence_before_sync();
@@ -514,7 +519,6 @@ attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, in
 #pragma unroll
     for (int c = 0; c < NCOL; c += 16) tmem_ld16(s_col + lanes + c, y + c);
     tmem_wait_ld();
-    if (it + 1 < n) fetch(it + 1);   // (the next tile's codes: behind this one's last wait for a load)
 #pragma unroll
     for (int h = 0; h < HPB; ++h) {
       x[h] = 0.f;
@@ -558,7 +562,7 @@ attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, in
             x[h] = ex2f(x[h] - (m[h] == -INFINITY ? 0.f : m[h]));
             l[h] += x[h];
           }
-          q[u] = seen ? x[h] * vs[i] : 0.f;
+          q[u] = x[h] * vs[i];   // (slots that are not seen: weights, scales and minima are zero)
           mid[h * NG + i] = fmaf(x[h], vm[i], mid[h * NG + i]);
         }
         w[e / 2] = pack_bf16(q[0], q[1]);
