@@ -57,7 +57,7 @@ __device__ __noinline__ void dkdv_again(const Args& a, float* sm, int b, int g, 
   for (int r = 0; r < 128 && j0 + r < a.mask.T_k; r += 32) dkdv_rows<bf16, D, 4, 128>(a, sm, b, g, j0 + r);
 }
 
-template <int D, bool KV, bool GENERAL>
+template <int D, bool KV, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(BwdLay<D>::THREADS, 1)
 attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_constant__ CUtensorMap tm_a2, const __grid_constant__ CUtensorMap tm_b1,
                    const __grid_constant__ CUtensorMap tm_b2, const __grid_constant__ CUtensorMap tm_o1, const __grid_constant__ CUtensorMap tm_o2,
@@ -300,7 +300,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
     const int wg = warp >> 2, r128 = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t S = s_col(wg) + lanes, P = p_col(wg) + lanes;
-    const float scale2 = a.scale * LOG2E, c2 = a.cap * LOG2E, inv_c2 = GENERAL && a.cap > 0.f ? 1.f / c2 : 0.f;
+    const float scale2 = a.scale * LOG2E, c2 = a.cap * LOG2E, nic2 = CAP ? -1.f / (c2 * c2) : 0.f;
     int base = 0, seq = 0;   // walked tiles and items with tiles so far
     for (int k = 0;; ++k) {
     Item w;
@@ -351,7 +351,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
         continue;
       }
       const float4* stat = reinterpret_cast<const float4*>(smem + L::OFF_STAT + st * L::STAT);
-      const float slope2 = GENERAL && a.slopes ? a.slopes[h] * LOG2E : 0.f;
+      const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f;
       float s[64], p[64];
       tmem_ld32(S, s);
       tmem_ld32(S + 32, s + 32);
@@ -361,16 +361,10 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
       // |i - j| = |dist0 - c|
       const float dist0 = (float)(KV ? r - c0 - a.mask.off : r + a.mask.off - c0);
       if (KV) mbar_wait(bar(L::B_FULL + st), (step / L::ST) & 1);   // (complete by now; makes the copied statistics visible here)
-      if (GENERAL) {
-        if (a.cap > 0.f) {
-          cap_scores(s, a.scale / a.cap, c2);
-        } else {
-#pragma unroll
-          for (int c = 0; c < 64; ++c) s[c] *= scale2;
-        }
-      }
-      const uint64_t sc = f2_pack(scale2, scale2), one = f2_pack(1.f, 1.f), ic = f2_pack(inv_c2, inv_c2), nic = f2_pack(-inv_c2, -inv_c2);
-      // weights and their gradients over the scores, as bf16 pairs; `some`: not every column is met
+      if (CAP) cap_scores(s, a.scale / a.cap, c2);
+      const uint64_t sc = f2_pack(CAP ? 1.f : scale2, CAP ? 1.f : scale2), one = f2_pack(1.f, 1.f), nic = f2_pack(nic2, nic2);
+      // weights and their gradients over the scores, as bf16 pairs; `some`: not every column is met, or not all lie on one side
+      const float slope_c = KV ? -slope2 : slope2, bias0 = -slope_c * dist0;   // (on one side: the bias is bias0 + slope_c c)
       auto weigh = [&](auto some) {
         const int rel = iv.x - c0;
         const uint32_t len = (uint32_t)(iv.y - iv.x);
@@ -385,23 +379,26 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
           for (int e = 0; e < 4; e += 2) {
             const int c = q + e;
             const uint64_t x = f2_pack(s[c], s[c + 1]), l = e ? f2_pack(l4.z, l4.w) : f2_pack(l4.x, l4.y), d = e ? f2_pack(d4.z, d4.w) : f2_pack(d4.x, d4.y);
-            uint64_t y, fac = one;
-            if (GENERAL) {
+            uint64_t add = l, fac = one;
+            if (BIAS) {
               float b0, b1;
-              f2_unpack(l, b0, b1);
-              b0 = fmaf(-slope2, fabsf(dist0 - (float)c), b0);
-              b1 = fmaf(-slope2, fabsf(dist0 - (float)(c + 1)), b1);
-              y = f2_add(x, f2_pack(b0, b1));
-              fac = f2_fma(f2_mul(x, ic), f2_mul(x, nic), one);   // 1 - tanh^2
-            } else {
-              y = f2_fma(x, sc, l);
+              if (decltype(some)::value) {
+                f2_unpack(l, b0, b1);
+                b0 = fmaf(-slope2, fabsf(dist0 - (float)c), b0);
+                b1 = fmaf(-slope2, fabsf(dist0 - (float)(c + 1)), b1);
+                add = f2_pack(b0, b1);
+              } else {
+                add = f2_add(l, f2_pack(fmaf(slope_c, (float)c, bias0), fmaf(slope_c, (float)(c + 1), bias0)));
+              }
             }
+            const uint64_t y = f2_fma(x, sc, add);
+            if (CAP) fac = f2_fma(f2_mul(x, x), nic, one);   // 1 - tanh^2
             float p0, p1;
             f2_unpack(y, p0, p1);
             p0 = ex2f(p0);
             p1 = ex2f(p1);
             float g0 = p[c], g1 = p[c + 1], f0 = 1.f, f1 = 1.f;
-            if (GENERAL) f2_unpack(fac, f0, f1);
+            if (CAP) f2_unpack(fac, f0, f1);
             if (decltype(some)::value) {
               const bool v0 = (uint32_t)(c - rel) < len, v1 = (uint32_t)(c + 1 - rel) < len;
               p0 = v0 ? p0 : 0.f;
@@ -413,7 +410,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
             }
             const uint64_t pp = f2_pack(p0, p1), gg = f2_pack(g0, g1);
             if (!KV) dex = f2_fma(pp, gg, dex);
-            const uint64_t pf = GENERAL ? f2_mul(pp, f2_pack(f0, f1)) : pp;
+            const uint64_t pf = CAP ? f2_mul(pp, f2_pack(f0, f1)) : pp;
             const uint64_t dx = f2_mul(pf, f2_add(gg, d));
             float y0, y1;
             f2_unpack(KV ? pp : pf, y0, y1);
@@ -423,7 +420,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
           }
         }
       };
-      if (lo1 <= c0 && hi0 >= c0 + 64) weigh(std::false_type{});
+      if (lo1 <= c0 && hi0 >= c0 + 64 && (!BIAS || __all_sync(0xffffffffu, KV ? dist0 <= 0.f : dist0 >= 63.f))) weigh(std::false_type{});
       else weigh(std::true_type{});
       tmem_st32(S, s);
       tmem_st32(P, p);
@@ -528,7 +525,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
   }
 }
 
-template <int D, bool KV, bool GENERAL>
+template <int D, bool KV, bool CAP, bool BIAS>
 static int bwd_tc(const AttnCall& c) {
   using L = BwdLay<D>;
   const Args& a = c.a;
@@ -543,7 +540,7 @@ static int bwd_tc(const AttnCall& c) {
   const int tiles = ((KV ? T_k : T) + 127) / 128;
   const long long blocks = (long long)tiles * a.B * (KV ? a.H_kv : a.H);
   if (blocks > 0x7fffffffLL) return LAWCAT_ERR_UNSUPPORTED;
-  auto kernel = attn_bwd_tc_kernel<D, KV, GENERAL>;
+  auto kernel = attn_bwd_tc_kernel<D, KV, CAP, BIAS>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::BYTES);
   if (e != cudaSuccess) {
     cudaGetLastError();
@@ -559,9 +556,16 @@ static int bwd_tc(const AttnCall& c) {
 }
 
 template <int D>
-static int bwd_both(const AttnCall& c, bool general) {
-  if (int r = general ? bwd_tc<D, false, true>(c) : bwd_tc<D, false, false>(c)) return r;
-  return general ? bwd_tc<D, true, true>(c) : bwd_tc<D, true, false>(c);
+static int bwd_both(const AttnCall& c) {
+  auto both = [&](auto cap, auto bias) {
+    constexpr bool CAP = decltype(cap)::value, BIAS = decltype(bias)::value;
+    const int r = bwd_tc<D, false, CAP, BIAS>(c);
+    return r ? r : bwd_tc<D, true, CAP, BIAS>(c);
+  };
+  const std::true_type yes{};
+  const std::false_type no{};
+  if (c.a.cap > 0.f) return c.a.slopes ? both(yes, yes) : both(yes, no);
+  return c.a.slopes ? both(no, yes) : both(no, no);
 }
 
 }  // namespace attn
@@ -569,8 +573,7 @@ static int bwd_both(const AttnCall& c, bool general) {
 int launch_attn_bwd_tc(const AttnCall& c) {
   const attn::Args& a = c.a;
   if (a.mask.T == 0 || a.mask.T_k == 0) return launch_attn_bwd_exact(c);
-  const bool general = a.cap > 0.f || a.slopes;
-  return c.d == 128 ? attn::bwd_both<128>(c, general) : attn::bwd_both<64>(c, general);
+  return c.d == 128 ? attn::bwd_both<128>(c) : attn::bwd_both<64>(c);
 }
 
 }  // namespace lawcat

@@ -66,8 +66,8 @@ __device__ __noinline__ void fwd_again(const Args& a, float* sm, int b, int h, i
   for (int r = 0; r < 128 && t0 + r < a.mask.T; r += 32) fwd_rows<bf16, D, 4, 128>(a, sm, b, h, t0 + r, k_first, k_end, part_o, part_ml);
 }
 
-// GENERAL: a cap, a bias, or a scale that is not positive
-template <int D, bool GENERAL>
+// BIAS also serves a scale that is not positive: the scores are scaled before anything else looks at them
+template <int D, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(FwdLay<D>::THREADS, 1)
 attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                    const __grid_constant__ CUtensorMap tm_o, const __grid_constant__ FwdArgs f) {
@@ -259,7 +259,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const int i = warp >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t O = o_col(i) + lanes;
-    const float scale2 = a.scale * LOG2E, inv_cap = GENERAL && a.cap > 0.f ? 1.f / a.cap : 0.f;
+    const float scale2 = a.scale * LOG2E, inv_cap = CAP ? 1.f / a.cap : 0.f;
     int step = 0, seq = 0;
     for (int k = 0;; ++k) {
       Item w;
@@ -270,7 +270,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       if (w.n == 0) continue;
       const int n = w.n, h = head_of(w, i), t = row_of(w, i) + (tid & 127);
       const int2 iv = interval(a.mask, w.b, min(t, T - 1));   // (rows behind the last are never stored)
-      const float slope2 = GENERAL && a.slopes ? a.slopes[h] * LOG2E : 0.f;
+      const float slope2 = BIAS && a.slopes ? a.slopes[h] * LOG2E : 0.f;
       // what the warp's rows see in all: [lo0, hi1), of which every row sees [lo1, hi0)
       int lo0 = 0, lo1 = 0, hi0 = 0, hi1 = 0;
       float m = -INFINITY, l = 0.f;
@@ -293,17 +293,16 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         for (int c = 0; c < 64; c += 32) tmem_ld32(S + c, s + c);
         tmem_wait_ld();
         const bool low = lo1 > j0, high = hi0 < j0 + 64, whole = !low && !high;   // (the same for the warp)
-        if constexpr (GENERAL) {
-          if (a.cap > 0.f) {
-            cap_scores(s, a.scale * inv_cap, a.cap * LOG2E);
+        if constexpr (CAP) cap_scores(s, a.scale * inv_cap, a.cap * LOG2E);
+        if constexpr (BIAS) {
+          const float by = CAP ? 1.f : scale2, dist0 = (float)(t + a.mask.off - j0);
+          if (__all_sync(0xffffffffu, dist0 >= 63.f)) {   // (all keys lie behind: the distance is linear in the column)
+            const float base = -slope2 * dist0;
+#pragma unroll
+            for (int c = 0; c < 64; ++c) s[c] = fmaf(s[c], by, fmaf(slope2, (float)c, base));
           } else {
 #pragma unroll
-            for (int c = 0; c < 64; ++c) s[c] *= scale2;
-          }
-          if (a.slopes) {
-            const float dist0 = (float)(t + a.mask.off - j0);
-#pragma unroll
-            for (int c = 0; c < 64; ++c) s[c] = fmaf(-slope2, fabsf(dist0 - (float)c), s[c]);
+            for (int c = 0; c < 64; ++c) s[c] = fmaf(s[c], by, -slope2 * fabsf(dist0 - (float)c));
           }
         }
         float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
@@ -334,7 +333,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           }
         }
         float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
-        if constexpr (!GENERAL) mx *= scale2;
+        if constexpr (!CAP && !BIAS) mx *= scale2;
         const bool grow = mx > m + RESCALE || (m == -INFINITY && mx > m);
         if (__any_sync(0xffffffffu, grow)) {
           const float base = grow ? mx : m, factor = m == -INFINITY ? 0.f : ex2f(m - base);
@@ -357,7 +356,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           m = base;
         }
         const float base = m == -INFINITY ? 0.f : m;
-        const uint64_t sc = f2_pack(GENERAL ? 1.f : scale2, GENERAL ? 1.f : scale2), nb = f2_pack(-base, -base);
+        const uint64_t sc = f2_pack(CAP || BIAS ? 1.f : scale2, CAP || BIAS ? 1.f : scale2), nb = f2_pack(-base, -base);
         uint64_t sum0 = 0, sum1 = 0;
         auto weigh = [&](auto first) {   // 32 scores from column `first` on: the weights, two to a register, in their place
           constexpr int c = decltype(first)::value;
@@ -578,7 +577,7 @@ static FwdPlan fwd_plan(int B, int H, int H_kv, int T, int T_k, int window) {
   return p;
 }
 
-template <int D, bool GENERAL>
+template <int D, bool CAP, bool BIAS>
 static int fwd_tc(const AttnCall& c, const FwdPlan& pl, void* ws) {
   using L = FwdLay<D>;
   const Args& a = c.a;
@@ -592,7 +591,7 @@ static int fwd_tc(const AttnCall& c, const FwdPlan& pl, void* ws) {
     f.part_o = (float*)ws;
     f.part_ml = (float2*)((char*)ws + align_up(rows * D * sizeof(float), 256));
   }
-  auto kernel = attn_fwd_tc_kernel<D, GENERAL>;
+  auto kernel = attn_fwd_tc_kernel<D, CAP, BIAS>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::BYTES);
   if (e != cudaSuccess) {
     cudaGetLastError();
@@ -625,9 +624,14 @@ int launch_attn_fwd_tc(const AttnCall& c, void* ws) {
   if (a.mask.T_k == 0) return launch_attn_fwd_exact(c);
   const attn::FwdPlan p = attn::fwd_plan(a.B, a.H, a.H_kv, a.mask.T, a.mask.T_k, a.mask.window);
   if (p.blocks > 0x7fffffffLL || (long long)a.B * a.H * a.mask.T / 8 >= 0x7fffffffLL) return LAWCAT_ERR_UNSUPPORTED;
-  const bool general = a.cap > 0.f || a.slopes || !(a.scale > 0.f);
-  if (c.d == 128) return general ? attn::fwd_tc<128, true>(c, p, ws) : attn::fwd_tc<128, false>(c, p, ws);
-  return general ? attn::fwd_tc<64, true>(c, p, ws) : attn::fwd_tc<64, false>(c, p, ws);
+  auto by_width = [&](auto cap, auto bias) {
+    constexpr bool CAP = decltype(cap)::value, BIAS = decltype(bias)::value;
+    return c.d == 128 ? attn::fwd_tc<128, CAP, BIAS>(c, p, ws) : attn::fwd_tc<64, CAP, BIAS>(c, p, ws);
+  };
+  const std::true_type yes{};
+  const std::false_type no{};
+  if (a.cap > 0.f) return a.slopes ? by_width(yes, yes) : by_width(yes, no);
+  return a.slopes || !(a.scale > 0.f) ? by_width(no, yes) : by_width(no, no);
 }
 
 }  // namespace lawcat

@@ -101,29 +101,43 @@ __device__ __forceinline__ bool noted_before(const int* list, int at) {
   return false;
 }
 
-// s <- c2 tanh(s k) for N scores of a thread (all 32 lanes of a warp together). While no |s k| of the warp passes 0.8, tanh is y P(y^2)
-// with P of degree 5 on the FMA pipe (a least-maximum fit of tanh(y) / y over [0, 0.8], relative error 5e-8, 2e-7 with its fp32
-// arithmetic): the two special functions of the other form would be three times the whole softmax's load on their pipe.
+// s <- c2 tanh(s k) for N scores of a thread (all 32 lanes of a warp together). While no |s k| of the warp passes 0.4 (0.8), tanh is
+// y P(y^2) with P of degree 3 (5) on the FMA pipe, k and c2 multiplied into its coefficients: least-maximum fits of tanh(y) / y over
+// the range, relative error 1e-7 (5e-8), 2e-7 with their fp32 arithmetic. The two special functions of the other form would be three
+// times the whole softmax's load on their pipe. Scores under a cap of 30 seldom pass 12.
+template <int N, int DEG>
+__device__ __forceinline__ void cap_poly(float (&s)[N], float k, float c2, const float (&coef)[DEG + 1]) {
+  uint64_t c[DEG + 1];
+  float f = k * c2;
+#pragma unroll
+  for (int i = 0; i <= DEG; ++i) {
+    c[i] = f2_pack(coef[i] * f, coef[i] * f);
+    f *= k * k;
+  }
+#pragma unroll
+  for (int i = 0; i < N; i += 2) {
+    const uint64_t x = f2_pack(s[i], s[i + 1]), z = f2_mul(x, x);
+    uint64_t r = f2_fma(c[DEG], z, c[DEG - 1]);
+#pragma unroll
+    for (int d = DEG - 2; d >= 0; --d) r = f2_fma(r, z, c[d]);
+    f2_unpack(f2_mul(x, r), s[i], s[i + 1]);
+  }
+}
 template <int N>
 __device__ __forceinline__ void cap_scores(float (&s)[N], float k, float c2) {
-  float big = 0.f;
+  float b0 = 0.f, b1 = 0.f;
 #pragma unroll
-  for (int c = 0; c < N; c += 2) big = fmaxf(big, fmaxf(fabsf(s[c]), fabsf(s[c + 1])));
-  if (__all_sync(0xffffffffu, big * fabsf(k) <= 0.8f)) {
-    const uint64_t kk = f2_pack(k, k), cc = f2_pack(c2, c2);
-    const uint64_t a0 = f2_pack(0.9999999403953552f, 0.9999999403953552f), a1 = f2_pack(-0.33332714438438416f, -0.33332714438438416f),
-                   a2 = f2_pack(0.13321532309055328f, 0.13321532309055328f), a3 = f2_pack(-0.05313541740179062f, -0.05313541740179062f),
-                   a4 = f2_pack(0.019130872562527657f, 0.019130872562527657f), a5 = f2_pack(-0.004378729499876499f, -0.004378729499876499f);
-#pragma unroll
-    for (int c = 0; c < N; c += 2) {
-      const uint64_t y = f2_mul(f2_pack(s[c], s[c + 1]), kk), z = f2_mul(y, y);
-      uint64_t r = f2_fma(a5, z, a4);
-      r = f2_fma(r, z, a3);
-      r = f2_fma(r, z, a2);
-      r = f2_fma(r, z, a1);
-      r = f2_fma(r, z, a0);
-      f2_unpack(f2_mul(f2_mul(y, cc), r), s[c], s[c + 1]);
-    }
+  for (int c = 0; c < N; c += 4) {
+    b0 = fmaxf(b0, fmaxf(fabsf(s[c]), fabsf(s[c + 1])));
+    b1 = fmaxf(b1, fmaxf(fabsf(s[c + 2]), fabsf(s[c + 3])));
+  }
+  const float y = fabsf(k) < 1e4f ? fmaxf(b0, b1) * fabsf(k) : 1.f;
+  if (__all_sync(0xffffffffu, y <= 0.4f)) {
+    const float coef[4] = {0.9999998807907104f, -0.333313912153244f, 0.1327143758535385f, -0.04757280275225639f};
+    cap_poly<N, 3>(s, k, c2, coef);
+  } else if (__all_sync(0xffffffffu, y <= 0.8f)) {
+    const float coef[6] = {0.9999999403953552f, -0.33332714438438416f, 0.13321532309055328f, -0.05313541740179062f, 0.019130872562527657f, -0.004378729499876499f};
+    cap_poly<N, 5>(s, k, c2, coef);
   } else {
     const float k1 = 2.f * LOG2E * k;
 #pragma unroll
