@@ -158,8 +158,12 @@ size_t lawcat_attn_workspace_bytes(const lawcat_attn_params* p, int op) {
   if (check(p) != LAWCAT_OK) return 0;
   switch (op) {
     case LAWCAT_OP_ATTN_FWD:
-      return rows_bytes(p) + (attn_tc_supported(p->dtype, p->d, p->exact) ? attn_fwd_tc_workspace_bytes(p->B, p->H, p->H_kv, p->T, p->T_k, p->window, p->d) : 0);
-    case LAWCAT_OP_ATTN_BWD: return rows_bytes(p) + keys_bytes(p) + stat_bytes(p);
+      return rows_bytes(p) + (attn_tc_supported(p->dtype, p->d, p->exact)
+                                  ? attn_fwd_tc_workspace_bytes(p->B, p->H, p->H_kv, p->T, p->T_k, p->window, p->d)
+                                  : attn_fwd_exact_workspace_bytes(make_call(p, nullptr, nullptr, nullptr)));
+    case LAWCAT_OP_ATTN_BWD:
+      return rows_bytes(p) + keys_bytes(p) + stat_bytes(p) +
+             (attn_tc_supported(p->dtype, p->d, p->exact) ? 0 : attn_bwd_exact_workspace_bytes(make_call(p, nullptr, nullptr, nullptr)));
     case LAWCAT_OP_ATTN_DECODE: return align_up(attn_decode_workspace_bytes(make_decode(p, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr)), 256);
     default: return 0;
   }
@@ -181,7 +185,7 @@ int lawcat_attn_fwd(const lawcat_attn_params* p, const int32_t* cu_seqlens, cons
   if (cu_seqlens || prefix) {
     if ((r = fill_rows(p, cu_seqlens, prefix, nseq, c.a.mask, (int2*)ws, nullptr, c.stream))) return r;
   }
-  return attn_tc_supported(p->dtype, p->d, p->exact) ? launch_attn_fwd_tc(c, (char*)ws + rows_bytes(p)) : launch_attn_fwd_exact(c);
+  return attn_tc_supported(p->dtype, p->d, p->exact) ? launch_attn_fwd_tc(c, (char*)ws + rows_bytes(p)) : launch_attn_fwd_exact(c, (char*)ws + rows_bytes(p));
 }
 
 int lawcat_attn_bwd(const lawcat_attn_params* p, const int32_t* cu_seqlens, const int32_t* prefix, int32_t nseq, const void* q,
@@ -207,7 +211,7 @@ int lawcat_attn_bwd(const lawcat_attn_params* p, const int32_t* cu_seqlens, cons
   if (cu_seqlens || prefix) {
     if ((r = fill_rows(p, cu_seqlens, prefix, nseq, c.a.mask, (int2*)ws, keys, c.stream))) return r;
   }
-  return attn_tc_supported(p->dtype, p->d, p->exact) ? launch_attn_bwd_tc(c) : launch_attn_bwd_exact(c);
+  return attn_tc_supported(p->dtype, p->d, p->exact) ? launch_attn_bwd_tc(c) : launch_attn_bwd_exact(c, (char*)c.a.stat + stat_bytes(p));
 }
 
 int lawcat_attn_decode(const lawcat_attn_params* p, const void* q_t, const void* k_t, const void* v_t, void* K, void* V, const int32_t* pos,

@@ -89,8 +89,13 @@ struct AttnCall {
   int d, dtype, exact;
   cudaStream_t stream;
 };
-int launch_attn_fwd_exact(const AttnCall& c);
-int launch_attn_bwd_exact(const AttnCall& c);
+// the exact kernels (attn_exact.cu); without scratch no row block's tiles are shared out
+size_t attn_fwd_exact_workspace_bytes(const AttnCall& c);
+size_t attn_bwd_exact_workspace_bytes(const AttnCall& c);
+int launch_attn_fwd_exact(const AttnCall& c, void* ws);
+int launch_attn_bwd_exact(const AttnCall& c, void* ws);
+// o and lse from [parts, B, H, T, d] weighted values and [parts, B, H, T] (maximum in log2 units, sum)
+int launch_attn_fwd_join(const AttnCall& c, int parts, const float* part_o, const float2* part_ml);
 // the tensor-core kernels (attn_fwd_tc.cu): bf16 storage, d = 64 or 128
 bool attn_tc_supported(int dtype, int d, int exact);
 size_t attn_fwd_tc_workspace_bytes(int B, int H, int H_kv, int T, int T_k, int window, int d);

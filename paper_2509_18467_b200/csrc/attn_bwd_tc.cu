@@ -50,11 +50,11 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 
 template <int D>
 __device__ __noinline__ void dq_again(const Args& a, float* sm, int b, int h, int t0) {
-  for (int r = 0; r < 128 && t0 + r < a.mask.T; r += 32) dq_rows<bf16, D, 4, 128>(a, sm, b, h, t0 + r);
+  for (int r = 0; r < 128 && t0 + r < a.mask.T; r += 32) dq_rows<bf16, D, 4, 128>(a, sm, b, h, t0 + r, 0, 1, nullptr);
 }
 template <int D>
 __device__ __noinline__ void dkdv_again(const Args& a, float* sm, int b, int g, int j0) {
-  for (int r = 0; r < 128 && j0 + r < a.mask.T_k; r += 32) dkdv_rows<bf16, D, 4, 128>(a, sm, b, g, j0 + r);
+  for (int r = 0; r < 128 && j0 + r < a.mask.T_k; r += 32) dkdv_rows<bf16, D, 4, 128>(a, sm, b, g, j0 + r, 0, 1, nullptr, nullptr);
 }
 
 template <int D, bool KV, bool CAP, bool BIAS>
@@ -572,7 +572,7 @@ static int bwd_both(const AttnCall& c) {
 
 int launch_attn_bwd_tc(const AttnCall& c) {
   const attn::Args& a = c.a;
-  if (a.mask.T == 0 || a.mask.T_k == 0) return launch_attn_bwd_exact(c);
+  if (a.mask.T == 0 || a.mask.T_k == 0) return launch_attn_bwd_exact(c, nullptr);
   return c.d == 128 ? attn::bwd_both<128>(c) : attn::bwd_both<64>(c);
 }
 

@@ -1,6 +1,10 @@
-// Launches of the exact attention kernels (attn_exact.cuh).
-// A block has 256 threads and 64 rows (RM = 4), or 16 rows (RM = 1) where blocks of 64 would leave most SMs idle: a tile's loads
-// then serve a quarter of the products, but a call of 4 heads x 512 queries runs on 128 blocks instead of 32.
+// Launches of the exact attention kernels (attn_exact.cuh), and the sums of what is shared out over several blocks.
+// A block has 256 threads and 64 rows (RM = 4: a tile's loads serve four products), or 16 (RM = 1) in calls of no more. Where the
+// blocks would leave SMs idle, each row block's tiles are shared out over several, whose results in fp32 a small kernel joins in a
+// fixed order (4 heads x 512 tokens of 64 in fp32, forward and gradients: 32 blocks of 64 rows, or 128 of 16 rows as it was before,
+// 163 us).
+#include <algorithm>
+
 #include "attn_exact.cuh"
 
 namespace lawcat {
@@ -8,28 +12,91 @@ namespace attn {
 
 constexpr int THREADS = 256;
 
+struct Parts {
+  int n;
+  float *x, *y;   // [n, heads, rows, D]: weighted values; dq; dk and dv
+  float2* ml;     // [n, B, H, T] (maximum in log2 units, sum)
+};
+
 template <typename T, int D, int RM>
-__global__ void __launch_bounds__(THREADS) attn_fwd_exact_kernel(const Args a, int tiles) {
+__global__ void __launch_bounds__(THREADS) attn_fwd_exact_kernel(const Args a, int tiles, const Parts p) {
   extern __shared__ __align__(16) float sm[];
-  const int bh = blockIdx.x % (a.B * a.H);
-  const int t0 = (tiles - 1 - (int)(blockIdx.x / (a.B * a.H))) * 16 * RM;  // (under a causal mask the longest rows first)
-  fwd_rows<T, D, RM, THREADS>(a, sm, bh / a.H, bh % a.H, t0, 0, a.mask.T_k, nullptr, nullptr);
+  const int part = blockIdx.x % p.n, x = blockIdx.x / p.n, bh = x % (a.B * a.H), b = bh / a.H;
+  const int t0 = (tiles - 1 - x / (a.B * a.H)) * 16 * RM;  // (under a causal mask the longest rows first)
+  if (p.n == 1) {
+    fwd_rows<T, D, RM, THREADS>(a, sm, b, bh % a.H, t0, 0, a.mask.T_k, nullptr, nullptr);
+    return;
+  }
+  const int lo = interval(a.mask, b, t0).x, hi = interval(a.mask, b, min(t0 + 16 * RM, a.mask.T) - 1).y;
+  const int per = ((hi - lo + BN - 1) / BN + p.n - 1) / p.n * BN;
+  const size_t at = ((size_t)part * a.B * a.H + bh) * a.mask.T;
+  fwd_rows<T, D, RM, THREADS>(a, sm, b, bh % a.H, t0, lo + part * per, lo + (part + 1) * per, p.x + at * D, p.ml + at);
 }
 
 // dq, and (lse log2e, dO.o) of every query for the other kernel
 template <typename T, int D, int RM>
-__global__ void __launch_bounds__(THREADS) attn_dq_exact_kernel(const Args a, int tiles) {
+__global__ void __launch_bounds__(THREADS) attn_dq_exact_kernel(const Args a, int tiles, const Parts p) {
   extern __shared__ __align__(16) float sm[];
-  const int bh = blockIdx.x % (a.B * a.H);
-  const int t0 = (tiles - 1 - (int)(blockIdx.x / (a.B * a.H))) * 16 * RM;
-  dq_rows<T, D, RM, THREADS>(a, sm, bh / a.H, bh % a.H, t0);
+  const int part = blockIdx.x % p.n, x = blockIdx.x / p.n, bh = x % (a.B * a.H);
+  const int t0 = (tiles - 1 - x / (a.B * a.H)) * 16 * RM;
+  dq_rows<T, D, RM, THREADS>(a, sm, bh / a.H, bh % a.H, t0, part, p.n, p.x + ((size_t)part * a.B * a.H + bh) * a.mask.T * D);
 }
 
 template <typename T, int D, int RM>
-__global__ void __launch_bounds__(THREADS) attn_dkdv_exact_kernel(const Args a, int tiles) {
+__global__ void __launch_bounds__(THREADS) attn_dkdv_exact_kernel(const Args a, int tiles, const Parts p) {
   extern __shared__ __align__(16) float sm[];
-  const int bg = blockIdx.x % (a.B * a.H_kv);
-  dkdv_rows<T, D, RM, THREADS>(a, sm, bg / a.H_kv, bg % a.H_kv, (int)(blockIdx.x / (a.B * a.H_kv)) * 16 * RM);
+  const int part = blockIdx.x % p.n, x = blockIdx.x / p.n, bg = x % (a.B * a.H_kv);
+  const size_t at = ((size_t)part * a.B * a.H_kv + bg) * a.mask.T_k * D;
+  dkdv_rows<T, D, RM, THREADS>(a, sm, bg / a.H_kv, bg % a.H_kv, x / (a.B * a.H_kv) * 16 * RM, part, p.n, p.x + at, p.y + at);
+}
+
+// o and lse of every query from its parts; one warp per (batch, token, head)
+template <typename T, int D>
+__global__ void __launch_bounds__(256) attn_fwd_join_kernel(const Args a, const Parts p) {
+  const size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) >> 5, rows = (size_t)a.B * a.mask.T * a.H;
+  const int lane = threadIdx.x & 31;
+  if (row >= rows) return;
+  const int h = (int)(row % a.H);
+  const size_t bt = row / a.H, b = bt / a.mask.T, t = bt % a.mask.T;
+  const size_t at = (b * a.H + h) * a.mask.T + t, step = (size_t)a.B * a.H * a.mask.T;
+  constexpr int NC = D / 32 > 0 ? D / 32 : 1;
+  const bool mine = lane * NC < D;
+  float m = -INFINITY, l = 0.f, acc[NC] = {};
+  for (int i = lane; i < p.n; i += 32) m = fmaxf(m, p.ml[i * step + at].x);
+  m = warp_max(m);
+  const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll 4
+  for (int i = 0; i < p.n; ++i) {   // (a part without keys: maximum -infinity, sum and values zero)
+    const float2 ml = p.ml[i * step + at];
+    const float* x = p.x + (i * step + at) * D + (mine ? lane * NC : 0);
+    const float w = exp2f(ml.x - base);
+    l = fmaf(w, ml.y, l);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[c] = fmaf(w, x[c], acc[c]);
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* o = (T*)a.o + row * D + lane * NC;
+  if (mine)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) stf<T>(o + c, acc[c] * inv);
+  if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+}
+
+// out [B, rows, heads, D] = the sum of the parts [n, B, heads, rows, D]; four channels per thread
+template <typename T, int D>
+__global__ void __launch_bounds__(256) attn_sum_kernel(const float* __restrict__ x, T* __restrict__ out, int n, int B, int heads, int rows) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, all = (size_t)B * heads * rows * (D / 4);
+  if (i >= all) return;
+  const int c = (int)(i % (D / 4));
+  const size_t r = i / (D / 4), t = r % rows, bh = r / rows;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int k = 0; k < n; ++k) {
+    const float4 v = reinterpret_cast<const float4*>(x)[k * all + i];
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  T* o = out + (((bh / heads) * rows + t) * heads + bh % heads) * D + c * 4;
+  stf<T>(o, s.x); stf<T>(o + 1, s.y); stf<T>(o + 2, s.z); stf<T>(o + 3, s.w);
 }
 
 template <typename K>
@@ -42,47 +109,72 @@ static int set_smem(K kernel, size_t bytes) {
 }
 
 // blocks for `rows` rows of n heads in blocks of bm; 0 where the grid would not hold them
-static unsigned blocks(long long rows, long long n, int bm) {
-  const long long x = (rows + bm - 1) / bm * n;
+static unsigned blocks(long long rows, long long n, int bm, int parts) {
+  const long long x = (rows + bm - 1) / bm * n * parts;
   return x <= 0x7fffffffLL ? (unsigned)x : 0;
 }
-// 64 rows per block, or 16 where that leaves more than half of the SMs without a block
-static int rows_per_thread(long long rows, long long n) { return (rows + 63) / 64 * n * 2 < sm_count() ? 1 : 4; }
+static int rows_per_thread(int rows) { return rows <= 16 ? 1 : 4; }
+// Parts that a row block's `tiles` tiles are shared out into: two blocks per SM where one of 64 rows each would leave SMs idle.
+static int parts_of(int rows, long long n, long long tiles) {
+  const long long x = (rows + 63) / 64 * n;
+  if (x == 0 || x >= sm_count()) return 1;
+  return (int)std::max(1LL, std::min(std::min((2LL * sm_count() + x - 1) / x, tiles), 16LL));
+}
+static int parts_q(const Mask& m, int B, int H) {
+  const long long keys = m.window && m.window < m.T_k ? std::min<long long>(m.T_k, (long long)m.window + 63) : m.T_k;
+  return parts_of(m.T, (long long)B * H, (keys + 63) / 64);
+}
+static int parts_k(const Mask& m, int B, int H, int H_kv) {
+  const long long queries = m.window && m.window < m.T ? std::min<long long>(m.T, (long long)m.window + 63) : m.T;
+  return parts_of(m.T_k, (long long)B * H_kv, (queries + 63) / 64 * (H / H_kv));
+}
+// one part's sums behind another's: forward, queries, keys
+static size_t part_bytes(int parts, size_t rows, int d) { return parts == 1 ? 0 : align_up(sizeof(float) * parts * rows * d, 256); }
 
 template <typename T, int D, int RM>
-static int fwd(const AttnCall& c) {
+static int fwd(const AttnCall& c, const Parts& p) {
   const int tiles = (c.a.mask.T + 16 * RM - 1) / (16 * RM);
-  const unsigned n = blocks(c.a.mask.T, (long long)c.a.B * c.a.H, 16 * RM);
+  const unsigned n = blocks(c.a.mask.T, (long long)c.a.B * c.a.H, 16 * RM, p.n);
   if (!n) return LAWCAT_ERR_UNSUPPORTED;
   constexpr size_t sm = fwd_smem<D, RM, THREADS>();
   if (int r = set_smem(attn_fwd_exact_kernel<T, D, RM>, sm)) return r;
-  LAWCAT_LAUNCH("attn_fwd_exact", c.stream, attn_fwd_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles));
+  LAWCAT_LAUNCH("attn_fwd_exact", c.stream, attn_fwd_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles, p));
+  LAWCAT_CHECK_LAUNCH();
+  return p.n > 1 ? launch_attn_fwd_join(c, p.n, p.x, p.ml) : (int)LAWCAT_OK;
+}
+
+template <typename T, int D>
+static int sum(const AttnCall& c, const float* x, void* out, int parts, int heads, int rows) {
+  const long long n = ((long long)c.a.B * heads * rows * (D / 4) + 255) / 256;
+  LAWCAT_LAUNCH("attn_sum", c.stream, attn_sum_kernel<T, D><<<(unsigned)n, 256, 0, c.stream>>>(x, (T*)out, parts, c.a.B, heads, rows));
   LAWCAT_CHECK_LAUNCH();
   return LAWCAT_OK;
 }
 
 template <typename T, int D, int RM>
-static int dq(const AttnCall& c) {
+static int dq(const AttnCall& c, const Parts& p) {
   const int tiles = (c.a.mask.T + 16 * RM - 1) / (16 * RM);
-  const unsigned n = blocks(c.a.mask.T, (long long)c.a.B * c.a.H, 16 * RM);
+  const unsigned n = blocks(c.a.mask.T, (long long)c.a.B * c.a.H, 16 * RM, p.n);
   if (!n) return LAWCAT_ERR_UNSUPPORTED;
   constexpr size_t sm = dq_smem<D, RM, THREADS>();
   if (int r = set_smem(attn_dq_exact_kernel<T, D, RM>, sm)) return r;
-  LAWCAT_LAUNCH("attn_dq_exact", c.stream, attn_dq_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles));
+  LAWCAT_LAUNCH("attn_dq_exact", c.stream, attn_dq_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles, p));
   LAWCAT_CHECK_LAUNCH();
-  return LAWCAT_OK;
+  return p.n > 1 ? sum<T, D>(c, p.x, c.a.dq, p.n, c.a.H, c.a.mask.T) : (int)LAWCAT_OK;
 }
 
 template <typename T, int D, int RM>
-static int dkdv(const AttnCall& c) {
+static int dkdv(const AttnCall& c, const Parts& p) {
   const int tiles = (c.a.mask.T_k + 16 * RM - 1) / (16 * RM);
-  const unsigned n = blocks(c.a.mask.T_k, (long long)c.a.B * c.a.H_kv, 16 * RM);
+  const unsigned n = blocks(c.a.mask.T_k, (long long)c.a.B * c.a.H_kv, 16 * RM, p.n);
   if (!n) return LAWCAT_ERR_UNSUPPORTED;
   constexpr size_t sm = dkdv_smem<D, RM, THREADS>();
   if (int r = set_smem(attn_dkdv_exact_kernel<T, D, RM>, sm)) return r;
-  LAWCAT_LAUNCH("attn_dkdv_exact", c.stream, attn_dkdv_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles));
+  LAWCAT_LAUNCH("attn_dkdv_exact", c.stream, attn_dkdv_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles, p));
   LAWCAT_CHECK_LAUNCH();
-  return LAWCAT_OK;
+  if (p.n == 1) return LAWCAT_OK;
+  const int r = sum<T, D>(c, p.x, c.a.dk, p.n, c.a.H_kv, c.a.mask.T_k);
+  return r ? r : sum<T, D>(c, p.y, c.a.dv, p.n, c.a.H_kv, c.a.mask.T_k);
 }
 
 template <typename F>
@@ -100,23 +192,51 @@ static int dispatch(const AttnCall& c, F f) {
 
 }  // namespace attn
 
-int launch_attn_fwd_exact(const AttnCall& c) {
-  return attn::dispatch(c, [&](auto t, auto d) {
+int launch_attn_fwd_join(const AttnCall& c, int parts, const float* part_o, const float2* part_ml) {
+  return attn::dispatch(c, [&](auto t, auto d) -> int {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
-    return attn::rows_per_thread(c.a.mask.T, (long long)c.a.B * c.a.H) == 1 ? attn::fwd<T, D, 1>(c) : attn::fwd<T, D, 4>(c);
+    const attn::Parts p{parts, const_cast<float*>(part_o), nullptr, const_cast<float2*>(part_ml)};
+    const size_t n = (size_t)c.a.B * c.a.H * c.a.mask.T;
+    LAWCAT_LAUNCH("attn_fwd_join", c.stream, attn::attn_fwd_join_kernel<T, D><<<(unsigned)((n + 7) / 8), 256, 0, c.stream>>>(c.a, p));
+    LAWCAT_CHECK_LAUNCH();
+    return LAWCAT_OK;
   });
 }
 
-int launch_attn_bwd_exact(const AttnCall& c) {
+size_t attn_fwd_exact_workspace_bytes(const AttnCall& c) {
+  const int parts = attn::parts_q(c.a.mask, c.a.B, c.a.H);
+  const size_t rows = (size_t)c.a.B * c.a.H * c.a.mask.T;
+  return parts == 1 ? 0 : attn::part_bytes(parts, rows, c.d) + align_up(sizeof(float2) * parts * rows, 256);
+}
+
+int launch_attn_fwd_exact(const AttnCall& c, void* ws) {
+  attn::Parts p{ws ? attn::parts_q(c.a.mask, c.a.B, c.a.H) : 1, (float*)ws, nullptr, nullptr};
+  if (p.n > 1) p.ml = (float2*)((char*)ws + attn::part_bytes(p.n, (size_t)c.a.B * c.a.H * c.a.mask.T, c.d));
+  return attn::dispatch(c, [&](auto t, auto d) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value;
+    return attn::rows_per_thread(c.a.mask.T) == 1 ? attn::fwd<T, D, 1>(c, p) : attn::fwd<T, D, 4>(c, p);
+  });
+}
+
+size_t attn_bwd_exact_workspace_bytes(const AttnCall& c) {
+  const size_t q = attn::part_bytes(attn::parts_q(c.a.mask, c.a.B, c.a.H), (size_t)c.a.B * c.a.H * c.a.mask.T, c.d);
+  const size_t k = attn::part_bytes(attn::parts_k(c.a.mask, c.a.B, c.a.H, c.a.H_kv), (size_t)c.a.B * c.a.H_kv * c.a.mask.T_k, c.d);
+  return std::max(q, 2 * k);
+}
+
+int launch_attn_bwd_exact(const AttnCall& c, void* ws) {
+  const attn::Parts pq{ws ? attn::parts_q(c.a.mask, c.a.B, c.a.H) : 1, (float*)ws, nullptr, nullptr};
+  attn::Parts pk{ws ? attn::parts_k(c.a.mask, c.a.B, c.a.H, c.a.H_kv) : 1, (float*)ws, nullptr, nullptr};
+  if (pk.n > 1) pk.y = (float*)((char*)ws + attn::part_bytes(pk.n, (size_t)c.a.B * c.a.H_kv * c.a.mask.T_k, c.d));
   return attn::dispatch(c, [&](auto t, auto d) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
     int r = LAWCAT_OK;
-    if (c.a.mask.T > 0)
-      r = attn::rows_per_thread(c.a.mask.T, (long long)c.a.B * c.a.H) == 1 ? attn::dq<T, D, 1>(c) : attn::dq<T, D, 4>(c);
+    if (c.a.mask.T > 0) r = attn::rows_per_thread(c.a.mask.T) == 1 ? attn::dq<T, D, 1>(c, pq) : attn::dq<T, D, 4>(c, pq);
     if (r || c.a.mask.T_k == 0) return r;
-    return attn::rows_per_thread(c.a.mask.T_k, (long long)c.a.B * c.a.H_kv) == 1 ? attn::dkdv<T, D, 1>(c) : attn::dkdv<T, D, 4>(c);
+    return attn::rows_per_thread(c.a.mask.T_k) == 1 ? attn::dkdv<T, D, 1>(c, pk) : attn::dkdv<T, D, 4>(c, pk);
   });
 }
 

@@ -226,9 +226,10 @@ __device__ __forceinline__ void fwd_rows(const Args& a, float* sm, int b, int h,
   store_rows<T, D, RM>((T*)a.o + (size_t)b * a.mask.T * qs + (size_t)h * D, qs, t0, t_end, ty, tx, acc);
 }
 
-// dq, and (lse log2e, dO.o) of every query for the other kernel
+// dq, and (lse log2e, dO.o) of every query for the other kernel. part of parts: this share of the row block's key tiles, the sums in
+// fp32 to part_o [T, D] of the head where parts > 1.
 template <typename T, int D, int RM, int NTHR>
-__device__ __forceinline__ void dq_rows(const Args& a, float* sm, int b, int h, int t0) {
+__device__ __forceinline__ void dq_rows(const Args& a, float* sm, int b, int h, int t0, int part, int parts, float* part_o) {
   constexpr int BM = NTHR / 16 * RM, LD = D + 4, NC = D / 16;
   float *Q = sm, *O = Q + BM * LD, *K = O + BM * LD, *V = K + BN * LD, *P = V + BN * LD;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
@@ -259,7 +260,7 @@ __device__ __forceinline__ void dq_rows(const Args& a, float* sm, int b, int h, 
       lse2[i] = a.lse[((size_t)b * a.mask.T + t) * a.H + h] * LOG2E;
     }
     dsum[i] = sum16(w);
-    if (tx == 0 && t < t_end) {
+    if (tx == 0 && t < t_end && part == 0) {
       float* const st = a.stat + ((size_t)b * a.H + h) * a.stat_stride + t;
       st[0] = -lse2[i];
       st[(size_t)a.B * a.H * a.stat_stride] = -dsum[i];
@@ -267,12 +268,14 @@ __device__ __forceinline__ void dq_rows(const Args& a, float* sm, int b, int h, 
 #pragma unroll
     for (int c = 0; c < NC; ++c) acc[i][c] = 0.f;
   }
-  for (int j0 = head.x; j0 < tail.y; j0 += BN) {
+  const int per = ((tail.y - head.x + BN - 1) / BN + parts - 1) / parts * BN;   // keys of a part
+  const int j_first = head.x + part * per, j_last = tail.y < j_first + per ? tail.y : j_first + per;
+  for (int j0 = j_first; j0 < j_last; j0 += BN) {
     sync_rows<NTHR>();
     load_rows<T, D, NTHR>(K, (const T*)a.k + ko, ks, j0, a.mask.T_k, BN);
     load_rows<T, D, NTHR>(V, (const T*)a.v + ko, ks, j0, a.mask.T_k, BN);
     sync_rows<NTHR>();
-    const bool whole = last - t0 + 1 == BM && tail.x <= j0 && head.y >= j0 + BN;
+    const bool whole = last - t0 + 1 == BM && tail.x <= j0 && head.y >= j0 + BN && j0 + BN <= j_last;
     float s[RM][4], dp[RM][4];
     product_t<D, RM>(Q, K, ty, tx, s);
     product_t<D, RM>(O, V, ty, tx, dp);
@@ -285,7 +288,7 @@ __device__ __forceinline__ void dq_rows(const Args& a, float* sm, int b, int h, 
         float th = 0.f;
         const float x = score2(s[i][j], a.scale, a.cap, slope, abs(pos - key), th);
         const float dx = exp2f(x - lse2[i]) * (dp[i][j] - dsum[i]) * (1.f - th * th);
-        P[(ty * RM + i) * (BN + 4) + tx + 16 * j] = key >= iv[i].x && key < iv[i].y ? dx : 0.f;
+        P[(ty * RM + i) * (BN + 4) + tx + 16 * j] = key >= iv[i].x && key < iv[i].y && key < j_last ? dx : 0.f;
       }
     }
     __syncwarp();
@@ -295,12 +298,14 @@ __device__ __forceinline__ void dq_rows(const Args& a, float* sm, int b, int h, 
   for (int i = 0; i < RM; ++i)
 #pragma unroll
     for (int c = 0; c < NC; ++c) acc[i][c] *= a.scale;
-  store_rows<T, D, RM>((T*)a.dq + qo, qs, t0, t_end, ty, tx, acc);
+  if (parts > 1) store_rows<float, D, RM>(part_o, D, t0, t_end, ty, tx, acc);
+  else store_rows<T, D, RM>((T*)a.dq + qo, qs, t0, t_end, ty, tx, acc);
 }
 
-// dk, dv: a block owns BM keys and walks the queries of every head of its group
+// dk, dv: a block owns BM keys and walks the queries of every head of its group. part of parts: this share of those tiles, the sums in
+// fp32 to part_k, part_v [T_k, D] of the head where parts > 1.
 template <typename T, int D, int RM, int NTHR>
-__device__ __forceinline__ void dkdv_rows(const Args& a, float* sm, int b, int g, int j0) {
+__device__ __forceinline__ void dkdv_rows(const Args& a, float* sm, int b, int g, int j0, int part, int parts, float* part_k, float* part_v) {
   constexpr int BM = NTHR / 16 * RM, LD = D + 4, NC = D / 16;
   float *K = sm, *V = K + BM * LD, *Q = V + BM * LD, *O = Q + BN * LD, *P = O + BN * LD, *S = P + BM * (BN + 4);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
@@ -317,47 +322,52 @@ __device__ __forceinline__ void dkdv_rows(const Args& a, float* sm, int b, int g
   for (int i = 0; i < RM; ++i)
 #pragma unroll
     for (int c = 0; c < NC; ++c) dk[i][c] = dv[i][c] = 0.f;
-  for (int h = g * G; h < (g + 1) * G; ++h) {
+  const int tiles = (qr.y - qr.x + BN - 1) / BN, per = (tiles * G + parts - 1) / parts;
+  for (int i = part * per; i < tiles * G && i < (part + 1) * per; ++i) {
+    const int h = g * G + i / tiles, t0 = qr.x + i % tiles * BN;
     const size_t qo = (size_t)b * a.mask.T * qs + (size_t)h * D;
     const float *nl = a.stat + ((size_t)b * a.H + h) * a.stat_stride, *nd = nl + (size_t)a.B * a.H * a.stat_stride;
     const float slope = a.slopes ? a.slopes[h] : 0.f;
-    for (int t0 = qr.x; t0 < qr.y; t0 += BN) {
-      sync_rows<NTHR>();
-      load_rows<T, D, NTHR>(Q, (const T*)a.q + qo, qs, t0, qr.y, BN);
-      load_rows<T, D, NTHR>(O, (const T*)a.dO + qo, qs, t0, qr.y, BN);
-      sync_rows<NTHR>();
-      bool whole = t0 + BN <= qr.y && j1 - j0 == BM;
-      if (whole) whole = interval(a.mask, b, t0 + BN - 1).x <= j0 && interval(a.mask, b, t0).y >= j0 + BM;
-      float s[RM][4], dp[RM][4];
-      product_t<D, RM>(K, Q, ty, tx, s);
-      product_t<D, RM>(V, O, ty, tx, dp);
+    sync_rows<NTHR>();
+    load_rows<T, D, NTHR>(Q, (const T*)a.q + qo, qs, t0, qr.y, BN);
+    load_rows<T, D, NTHR>(O, (const T*)a.dO + qo, qs, t0, qr.y, BN);
+    sync_rows<NTHR>();
+    bool whole = t0 + BN <= qr.y && j1 - j0 == BM;
+    if (whole) whole = interval(a.mask, b, t0 + BN - 1).x <= j0 && interval(a.mask, b, t0).y >= j0 + BM;
+    float s[RM][4], dp[RM][4];
+    product_t<D, RM>(K, Q, ty, tx, s);
+    product_t<D, RM>(V, O, ty, tx, dp);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int t = t0 + tx + 16 * j;
-        const int2 iv = t < qr.y ? interval(a.mask, b, t) : make_int2(0, 0);
-        const float2 st = t < qr.y ? make_float2(nl[t], nd[t]) : make_float2(0.f, 0.f);
+    for (int j = 0; j < 4; ++j) {
+      const int t = t0 + tx + 16 * j;
+      const int2 iv = t < qr.y ? interval(a.mask, b, t) : make_int2(0, 0);
+      const float2 st = t < qr.y ? make_float2(nl[t], nd[t]) : make_float2(0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < RM; ++i) {
-          const int key = j0 + ty * RM + i;
-          const bool see = key >= iv.x && key < iv.y;
-          float th = 0.f;
-          const float x = score2(s[i][j], a.scale, a.cap, slope, abs(t + a.mask.off - key), th);
-          const float p = exp2f(x + st.x);
-          P[(ty * RM + i) * (BN + 4) + tx + 16 * j] = see ? p : 0.f;
-          S[(ty * RM + i) * (BN + 4) + tx + 16 * j] = see ? p * (dp[i][j] + st.y) * (1.f - th * th) : 0.f;
-        }
+      for (int i = 0; i < RM; ++i) {
+        const int key = j0 + ty * RM + i;
+        const bool see = key >= iv.x && key < iv.y;
+        float th = 0.f;
+        const float x = score2(s[i][j], a.scale, a.cap, slope, abs(t + a.mask.off - key), th);
+        const float p = exp2f(x + st.x);
+        P[(ty * RM + i) * (BN + 4) + tx + 16 * j] = see ? p : 0.f;
+        S[(ty * RM + i) * (BN + 4) + tx + 16 * j] = see ? p * (dp[i][j] + st.y) * (1.f - th * th) : 0.f;
       }
-      __syncwarp();
-      product_acc<D, RM>(P, O, ty, tx, whole, dv);
-      product_acc<D, RM>(S, Q, ty, tx, whole, dk);
     }
+    __syncwarp();
+    product_acc<D, RM>(P, O, ty, tx, whole, dv);
+    product_acc<D, RM>(S, Q, ty, tx, whole, dk);
   }
 #pragma unroll
   for (int i = 0; i < RM; ++i)
 #pragma unroll
     for (int c = 0; c < NC; ++c) dk[i][c] *= a.scale;
-  store_rows<T, D, RM>((T*)a.dk + ko, ks, j0, j_end, ty, tx, dk);
-  store_rows<T, D, RM>((T*)a.dv + ko, ks, j0, j_end, ty, tx, dv);
+  if (parts > 1) {
+    store_rows<float, D, RM>(part_k, D, j0, j_end, ty, tx, dk);
+    store_rows<float, D, RM>(part_v, D, j0, j_end, ty, tx, dv);
+  } else {
+    store_rows<T, D, RM>((T*)a.dk + ko, ks, j0, j_end, ty, tx, dk);
+    store_rows<T, D, RM>((T*)a.dv + ko, ks, j0, j_end, ty, tx, dv);
+  }
 }
 
 }  // namespace attn

@@ -527,37 +527,6 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   }
 }
 
-// o and lse of every query from its parts; one warp per (batch, token, head)
-template <int D>
-__global__ void __launch_bounds__(256) attn_fwd_join_kernel(const FwdArgs f) {
-  const Args& a = f.a;
-  const size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) >> 5, rows = (size_t)a.B * a.mask.T * a.H;
-  const int lane = threadIdx.x & 31;
-  if (row >= rows) return;
-  const int h = (int)(row % a.H);
-  const size_t bt = row / a.H, b = bt / a.mask.T, t = bt % a.mask.T;
-  const size_t at = (b * a.H + h) * a.mask.T + t, step = (size_t)a.B * a.H * a.mask.T;
-  constexpr int NC = D / 32;
-  float m = -INFINITY, l = 0.f, acc[NC] = {};
-  for (int i = lane; i < f.parts; i += 32) m = fmaxf(m, f.part_ml[i * step + at].x);
-  m = warp_max(m);
-  const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll 4
-  for (int i = 0; i < f.parts; ++i) {   // (a part without keys: maximum -infinity, sum and values zero)
-    const float2 ml = f.part_ml[i * step + at];
-    const float* x = f.part_o + (i * step + at) * D + lane * NC;
-    const float w = exp2f(ml.x - base);
-    l = fmaf(w, ml.y, l);
-#pragma unroll
-    for (int c = 0; c < NC; ++c) acc[c] = fmaf(w, x[c], acc[c]);
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  bf16* o = (bf16*)a.o + row * D + lane * NC;
-#pragma unroll
-  for (int c = 0; c < NC; ++c) o[c] = __float2bfloat16_rn(acc[c] * inv);
-  if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
-}
-
 struct FwdPlan {
   int two_heads, tiles, pairs, parts;
   long long blocks;
@@ -600,12 +569,7 @@ static int fwd_tc(const AttnCall& c, const FwdPlan& pl, void* ws) {
   }
   LAWCAT_LAUNCH("attn_fwd_tc", c.stream, kernel<<<(unsigned)pl.blocks, L::THREADS, L::BYTES, c.stream>>>(tq, tk, tv, to, f));
   LAWCAT_CHECK_LAUNCH();
-  if (pl.parts > 1) {
-    const size_t n = (size_t)a.B * a.H * a.mask.T;
-    LAWCAT_LAUNCH("attn_fwd_join", c.stream, attn_fwd_join_kernel<D><<<(unsigned)((n + 7) / 8), 256, 0, c.stream>>>(f));
-    LAWCAT_CHECK_LAUNCH();
-  }
-  return LAWCAT_OK;
+  return pl.parts > 1 ? launch_attn_fwd_join(c, pl.parts, f.part_o, f.part_ml) : (int)LAWCAT_OK;
 }
 
 }  // namespace attn
@@ -621,7 +585,7 @@ size_t attn_fwd_tc_workspace_bytes(int B, int H, int H_kv, int T, int T_k, int w
 
 int launch_attn_fwd_tc(const AttnCall& c, void* ws) {
   const attn::Args& a = c.a;
-  if (a.mask.T_k == 0) return launch_attn_fwd_exact(c);
+  if (a.mask.T_k == 0) return launch_attn_fwd_exact(c, nullptr);
   const attn::FwdPlan p = attn::fwd_plan(a.B, a.H, a.H_kv, a.mask.T, a.mask.T_k, a.mask.window);
   if (p.blocks > 0x7fffffffLL || (long long)a.B * a.H * a.mask.T / 8 >= 0x7fffffffLL) return LAWCAT_ERR_UNSUPPORTED;
   auto by_width = [&](auto cap, auto bias) {
