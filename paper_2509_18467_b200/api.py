@@ -333,11 +333,12 @@ def _attn_call(name, p, op, args, ws, stream, dev_status, nint=0):
         raise LawcatError(st, name)
 
 
-def _expect(p, **tensors):
-    """The kernels trust sizes and types: each named tensor (None is skipped) has to have the given shape and dtype."""
-    for name, (t, shape, dtype) in tensors.items():
-        if t is not None and (t.shape != shape or t.dtype != dtype):
-            raise ValueError(f"{name}: expected {tuple(shape)} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+U8, I32 = 2, 3  # (beside F32 and BF16: the types that the native module's expect() knows)
+
+
+def _checked():
+    """The native module's expect(name, tensor, type, sizes...): the kernels trust sizes and types, None is skipped."""
+    return (_binding or _bind()).expect
 
 
 def _sequences(cu_seqlens, prefix):
@@ -354,12 +355,16 @@ def lawcat_attn_fwd(p: AttnParams, q, k, v, slopes=None, cu_seqlens=None, prefix
                     dev_status=None):
     """Softmax attention; cu_seqlens (packed documents, nseq + 1 offsets) and prefix (a length per sequence) are host sequences.
     Returns dict(o, lse)."""
-    dt, qs, ks = torch_dtype(p), (p.B, p.T, p.H, p.d), (p.B, p.T_k, p.H_kv, p.d)
-    _expect(p, q=(q, qs, dt), k=(k, ks, dt), v=(v, ks, dt), o=(o, qs, dt), slopes=(slopes, (p.H,), torch.float32))
+    B, T, T_k, H, H_kv, d, dt, check = p.B, p.T, p.T_k, p.H, p.H_kv, p.d, p.dtype, _checked()
+    check("q", q, dt, B, T, H, d)
+    check("k", k, dt, B, T_k, H_kv, d)
+    check("v", v, dt, B, T_k, H_kv, d)
+    check("o", o, dt, B, T, H, d)
+    check("slopes", slopes, F32, H)
     keep, seqs = _sequences(cu_seqlens, prefix)
     if o is None:
-        o = _empty(q, p.dtype, *qs)
-    lse = _empty(q, F32, p.B, p.T, p.H) if want_lse else None
+        o = _empty(q, dt, B, T, H, d)
+    lse = _empty(q, F32, B, T, H) if want_lse else None
     _attn_call("lawcat_attn_fwd", p, OP_ATTN_FWD, (*seqs, q, k, v, slopes, o, lse), ws, stream, dev_status, 3)
     return dict(o=o, lse=lse)
 
@@ -367,22 +372,38 @@ def lawcat_attn_fwd(p: AttnParams, q, k, v, slopes=None, cu_seqlens=None, prefix
 def lawcat_attn_bwd(p: AttnParams, q, k, v, o, lse, dO, slopes=None, cu_seqlens=None, prefix=None, ws=None, stream=None,
                     dev_status=None):
     """Gradients for the upstream gradient dO, from the forward's o and lse: dict(dq, dk, dv)."""
-    dt, qs, ks = torch_dtype(p), (p.B, p.T, p.H, p.d), (p.B, p.T_k, p.H_kv, p.d)
-    _expect(p, q=(q, qs, dt), k=(k, ks, dt), v=(v, ks, dt), o=(o, qs, dt), lse=(lse, qs[:3], torch.float32), dO=(dO, qs, dt),
-            slopes=(slopes, (p.H,), torch.float32))
+    B, T, T_k, H, H_kv, d, dt, check = p.B, p.T, p.T_k, p.H, p.H_kv, p.d, p.dtype, _checked()
+    for name, t in (("q", q), ("o", o), ("dO", dO)):
+        check(name, t, dt, B, T, H, d)
+    check("k", k, dt, B, T_k, H_kv, d)
+    check("v", v, dt, B, T_k, H_kv, d)
+    check("lse", lse, F32, B, T, H)
+    check("slopes", slopes, F32, H)
     keep, seqs = _sequences(cu_seqlens, prefix)
-    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    dq, dk, dv = _empty(q, dt, B, T, H, d), _empty(q, dt, B, T_k, H_kv, d), _empty(q, dt, B, T_k, H_kv, d)
     _attn_call("lawcat_attn_bwd", p, OP_ATTN_BWD, (*seqs, q, k, v, slopes, o, lse, dO, dq, dk, dv), ws, stream, dev_status, 3)
     return dict(dq=dq, dk=dk, dv=dv)
 
 
+def _check_step(p, q_t, k_t, v_t, pos, slopes, o_t):
+    B, H, H_kv, d, dt, check = p.B, p.H, p.H_kv, p.d, p.dtype, _checked()
+    check("q_t", q_t, dt, B, H, d)
+    check("k_t", k_t, dt, B, H_kv, d)
+    check("v_t", v_t, dt, B, H_kv, d)
+    check("pos", pos, I32, B)
+    check("slopes", slopes, F32, H)
+    if o_t is None:
+        return _empty(q_t, dt, B, H, d)
+    check("o_t", o_t, dt, B, H, d)
+    return o_t
+
+
 def lawcat_attn_decode(p: AttnParams, q_t, k_t, v_t, K, V, pos, slopes=None, o_t=None, ws=None, stream=None, dev_status=None):
     """One token over caches of p.T_k slots; K, V are updated in place; returns o_t [B,H,d]."""
-    dt, qs, ks, cs = torch_dtype(p), (p.B, p.H, p.d), (p.B, p.H_kv, p.d), (p.B, p.T_k, p.H_kv, p.d)
-    _expect(p, q_t=(q_t, qs, dt), k_t=(k_t, ks, dt), v_t=(v_t, ks, dt), K=(K, cs, dt), V=(V, cs, dt),
-            pos=(pos, (p.B,), torch.int32), o_t=(o_t, qs, dt), slopes=(slopes, (p.H,), torch.float32))
-    if o_t is None:
-        o_t = _empty(q_t, p.dtype, *qs)
+    o_t = _check_step(p, q_t, k_t, v_t, pos, slopes, o_t)
+    check, sizes = _checked(), (p.dtype, p.B, p.T_k, p.H_kv, p.d)
+    check("K", K, *sizes)
+    check("V", V, *sizes)
     _attn_call("lawcat_attn_decode", p, OP_ATTN_DECODE, (q_t, k_t, v_t, K, V, pos, slopes, o_t), ws, stream, dev_status)
     return o_t
 
@@ -394,27 +415,33 @@ def quant_cache(p: AttnParams, device="cuda"):
     return q(), g(), q(), g()
 
 
-def _expect_cache(p, kq, kp, vq, vp, pos):
-    qs, gs = (p.B, p.H_kv, p.T_k, p.d // 2), (p.B, p.H_kv, p.T_k, max(1, p.d // 32), 2)
-    _expect(p, kq=(kq, qs, torch.uint8), kp=(kp, gs, torch.bfloat16), vq=(vq, qs, torch.uint8), vp=(vp, gs, torch.bfloat16),
-            pos=(pos, (p.B,), torch.int32))
+def _check_cache(p, kq, kp, vq, vp):
+    check, B, H_kv, C, d = _checked(), p.B, p.H_kv, p.T_k, p.d
+    check("kq", kq, U8, B, H_kv, C, d // 2)
+    check("vq", vq, U8, B, H_kv, C, d // 2)
+    check("kp", kp, BF16, B, H_kv, C, max(1, d // 32), 2)
+    check("vp", vp, BF16, B, H_kv, C, max(1, d // 32), 2)
 
 
 def lawcat_cache_quantize(p: AttnParams, k, v, pos, kq, kp, vq, vp, stream=None, dev_status=None):
     """Rows of k, v [B,T,H_kv,d] into slots (pos + t) mod p.T_k of the 4-bit cache, in place."""
-    dt, ks = torch_dtype(p), (p.B, p.T, p.H_kv, p.d)
-    _expect(p, k=(k, ks, dt), v=(v, ks, dt))
-    _expect_cache(p, kq, kp, vq, vp, pos)
+    check, sizes = _checked(), (p.dtype, p.B, p.T, p.H_kv, p.d)
+    check("k", k, *sizes)
+    check("v", v, *sizes)
+    check("pos", pos, I32, p.B)
+    _check_cache(p, kq, kp, vq, vp)
     _attn_call("lawcat_cache_quantize", p, None, (k, v, pos, kq, kp, vq, vp), None, stream, dev_status)
 
 
 def lawcat_cache_dequantize(p: AttnParams, kq, kp, vq, vp, pos, k=None, v=None, stream=None, dev_status=None):
     """The p.T rows from position pos on as values: dict(k, v) [B,T,H_kv,d]."""
-    dt, ks = torch_dtype(p), (p.B, p.T, p.H_kv, p.d)
-    _expect(p, k=(k, ks, dt), v=(v, ks, dt))
-    _expect_cache(p, kq, kp, vq, vp, pos)
-    k = _empty(kq, p.dtype, *ks) if k is None else k
-    v = _empty(kq, p.dtype, *ks) if v is None else v
+    check, sizes = _checked(), (p.dtype, p.B, p.T, p.H_kv, p.d)
+    check("k", k, *sizes)
+    check("v", v, *sizes)
+    check("pos", pos, I32, p.B)
+    _check_cache(p, kq, kp, vq, vp)
+    k = _empty(kq, *sizes) if k is None else k
+    v = _empty(kq, *sizes) if v is None else v
     _attn_call("lawcat_cache_dequantize", p, None, (kq, kp, vq, vp, pos, k, v), None, stream, dev_status)
     return dict(k=k, v=v)
 
@@ -422,11 +449,8 @@ def lawcat_cache_dequantize(p: AttnParams, kq, kp, vq, vp, pos, k=None, v=None, 
 def lawcat_attn_decode_quant(p: AttnParams, q_t, k_t, v_t, kq, kp, vq, vp, pos, slopes=None, o_t=None, ws=None, stream=None,
                              dev_status=None):
     """One token over a cache in 4 bits, which is updated in place; returns o_t [B,H,d]."""
-    dt, qs, ks = torch_dtype(p), (p.B, p.H, p.d), (p.B, p.H_kv, p.d)
-    _expect(p, q_t=(q_t, qs, dt), k_t=(k_t, ks, dt), v_t=(v_t, ks, dt), o_t=(o_t, qs, dt), slopes=(slopes, (p.H,), torch.float32))
-    _expect_cache(p, kq, kp, vq, vp, pos)
-    if o_t is None:
-        o_t = _empty(q_t, p.dtype, *qs)
+    o_t = _check_step(p, q_t, k_t, v_t, pos, slopes, o_t)
+    _check_cache(p, kq, kp, vq, vp)
     _attn_call("lawcat_attn_decode_quant", p, OP_ATTN_DECODE, (q_t, k_t, v_t, kq, kp, vq, vp, pos, slopes, o_t), ws, stream, dev_status)
     return o_t
 

@@ -3,6 +3,8 @@
 // Every mask offered (causal, window, documents, prefix, T != T_k) leaves a query ONE interval of keys [lo, hi), and both ends
 // grow with the query; the kernels know nothing else of masks.
 #pragma once
+#include <atomic>
+
 #include "common.cuh"
 
 namespace lawcat {
@@ -83,7 +85,24 @@ struct Args {
 
 }  // namespace attn
 
-// which kernels serve a call (attn_tc.cu), their launchers and scratch
+// Dynamic shared memory of a kernel, granted once per device (the call costs a microsecond, a decode step's launch not many more).
+template <auto KERNEL>
+int grant_smem(size_t bytes) {
+  static std::atomic<unsigned long long> granted{0};
+  int dev = 0;
+  const bool known = cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64;
+  if (known && (granted.load(std::memory_order_relaxed) >> dev & 1)) return LAWCAT_OK;
+  const cudaError_t e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    note_cuda_error(e, __FILE__, __LINE__);
+    return LAWCAT_ERR_CUDA;
+  }
+  if (known) granted.fetch_or(1ull << dev, std::memory_order_relaxed);
+  return LAWCAT_OK;
+}
+
+// a call's arguments, its launchers and scratch
 struct AttnCall {
   attn::Args a;
   int d, dtype, exact;

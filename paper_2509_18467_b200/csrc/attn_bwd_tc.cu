@@ -540,13 +540,8 @@ static int bwd_tc(const AttnCall& c) {
   const int tiles = ((KV ? T_k : T) + 127) / 128;
   const long long blocks = (long long)tiles * a.B * (KV ? a.H_kv : a.H);
   if (blocks > 0x7fffffffLL) return LAWCAT_ERR_UNSUPPORTED;
-  auto kernel = attn_bwd_tc_kernel<D, KV, CAP, BIAS>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::BYTES);
-  if (e != cudaSuccess) {
-    cudaGetLastError();
-    note_cuda_error(e, __FILE__, __LINE__);
-    return LAWCAT_ERR_CUDA;
-  }
+  constexpr auto kernel = attn_bwd_tc_kernel<D, KV, CAP, BIAS>;
+  if (int r = grant_smem<kernel>(L::BYTES)) return r;
   const int heads = KV ? a.H_kv : a.H;
   const BwdArgs f{a, fast_div(a.B * heads), fast_div(heads), fast_div(a.H / a.H_kv), tiles, wait_limit()};
   LAWCAT_LAUNCH(KV ? "attn_dkdv_tc" : "attn_dq_tc", c.stream,

@@ -360,12 +360,7 @@ int launch_attn_decode(const AttnDecode& c) {
       using T = decltype(t);
       constexpr bool Q4 = decltype(quant)::value;
       const size_t sm = sizeof(float) * ((2 * attn::TK + attn::HB) * (D + 4) + attn::HB * attn::TK + attn::HB);
-      const cudaError_t e = cudaFuncSetAttribute(attn::attn_decode_kernel<T, D, Q4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm);
-      if (e != cudaSuccess) {
-        cudaGetLastError();
-        note_cuda_error(e, __FILE__, __LINE__);
-        return LAWCAT_ERR_CUDA;
-      }
+      if (int r = grant_smem<attn::attn_decode_kernel<T, D, Q4>>(sm)) return r;
       LAWCAT_LAUNCH("attn_decode", c.stream,
                     attn::attn_decode_kernel<T, D, Q4><<<(unsigned)blocks, attn::DEC_THREADS, sm, c.stream>>>(a));
       LAWCAT_CHECK_LAUNCH();

@@ -648,13 +648,8 @@ static int step_tc(const AttnDecode& c, const DecArgs& a, unsigned blocks) {
   CUtensorMap tk, tv;
   if (!tensor_map(&tk, c.K, false, c.H_kv, c.C, c.B, D, 64, 128, true) || !tensor_map(&tv, c.V, false, c.H_kv, c.C, c.B, D, 64, 128, true))
     return LAWCAT_ERR_CUDA;
-  auto kernel = attn_step_tc_kernel<D, HPB>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::BYTES);
-  if (e != cudaSuccess) {
-    cudaGetLastError();
-    note_cuda_error(e, __FILE__, __LINE__);
-    return LAWCAT_ERR_CUDA;
-  }
+  constexpr auto kernel = attn_step_tc_kernel<D, HPB>;
+  if (int r = grant_smem<kernel>(L::BYTES)) return r;
   LAWCAT_LAUNCH("attn_decode_tc", c.stream, kernel<<<blocks, L::THREADS, L::BYTES, c.stream>>>(tk, tv, a, wait_limit(), c.dev_status));
   LAWCAT_CHECK_LAUNCH();
   return a.parts > 1 ? launch_attn_decode_join(a, D, LAWCAT_BF16, c.stream) : (int)LAWCAT_OK;
@@ -663,13 +658,8 @@ static int step_tc(const AttnDecode& c, const DecArgs& a, unsigned blocks) {
 template <int D, int HPB>
 static int step_quant_tc(const AttnDecode& c, const DecArgs& a, unsigned blocks) {
   using L = QuantLay<D, HPB>;
-  auto kernel = attn_step_quant_tc_kernel<D, HPB>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::BYTES);
-  if (e != cudaSuccess) {
-    cudaGetLastError();
-    note_cuda_error(e, __FILE__, __LINE__);
-    return LAWCAT_ERR_CUDA;
-  }
+  constexpr auto kernel = attn_step_quant_tc_kernel<D, HPB>;
+  if (int r = grant_smem<kernel>(L::BYTES)) return r;
   LAWCAT_LAUNCH("attn_decode_quant_tc", c.stream, kernel<<<blocks, 128, L::BYTES, c.stream>>>(a, wait_limit(), c.dev_status));
   LAWCAT_CHECK_LAUNCH();
   return a.parts > 1 ? launch_attn_decode_join(a, D, LAWCAT_BF16, c.stream) : (int)LAWCAT_OK;

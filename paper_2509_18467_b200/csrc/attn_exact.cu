@@ -99,15 +99,6 @@ __global__ void __launch_bounds__(256) attn_sum_kernel(const float* __restrict__
   stf<T>(o, s.x); stf<T>(o + 1, s.y); stf<T>(o + 2, s.z); stf<T>(o + 3, s.w);
 }
 
-template <typename K>
-static int set_smem(K kernel, size_t bytes) {
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-  if (e == cudaSuccess) return LAWCAT_OK;
-  cudaGetLastError();
-  note_cuda_error(e, __FILE__, __LINE__);
-  return LAWCAT_ERR_CUDA;
-}
-
 // blocks for `rows` rows of n heads in blocks of bm; 0 where the grid would not hold them
 static unsigned blocks(long long rows, long long n, int bm, int parts) {
   const long long x = (rows + bm - 1) / bm * n * parts;
@@ -137,7 +128,7 @@ static int fwd(const AttnCall& c, const Parts& p) {
   const unsigned n = blocks(c.a.mask.T, (long long)c.a.B * c.a.H, 16 * RM, p.n);
   if (!n) return LAWCAT_ERR_UNSUPPORTED;
   constexpr size_t sm = fwd_smem<D, RM, THREADS>();
-  if (int r = set_smem(attn_fwd_exact_kernel<T, D, RM>, sm)) return r;
+  if (int r = grant_smem<attn_fwd_exact_kernel<T, D, RM>>(sm)) return r;
   LAWCAT_LAUNCH("attn_fwd_exact", c.stream, attn_fwd_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles, p));
   LAWCAT_CHECK_LAUNCH();
   return p.n > 1 ? launch_attn_fwd_join(c, p.n, p.x, p.ml) : (int)LAWCAT_OK;
@@ -157,7 +148,7 @@ static int dq(const AttnCall& c, const Parts& p) {
   const unsigned n = blocks(c.a.mask.T, (long long)c.a.B * c.a.H, 16 * RM, p.n);
   if (!n) return LAWCAT_ERR_UNSUPPORTED;
   constexpr size_t sm = dq_smem<D, RM, THREADS>();
-  if (int r = set_smem(attn_dq_exact_kernel<T, D, RM>, sm)) return r;
+  if (int r = grant_smem<attn_dq_exact_kernel<T, D, RM>>(sm)) return r;
   LAWCAT_LAUNCH("attn_dq_exact", c.stream, attn_dq_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles, p));
   LAWCAT_CHECK_LAUNCH();
   return p.n > 1 ? sum<T, D>(c, p.x, c.a.dq, p.n, c.a.H, c.a.mask.T) : (int)LAWCAT_OK;
@@ -169,7 +160,7 @@ static int dkdv(const AttnCall& c, const Parts& p) {
   const unsigned n = blocks(c.a.mask.T_k, (long long)c.a.B * c.a.H_kv, 16 * RM, p.n);
   if (!n) return LAWCAT_ERR_UNSUPPORTED;
   constexpr size_t sm = dkdv_smem<D, RM, THREADS>();
-  if (int r = set_smem(attn_dkdv_exact_kernel<T, D, RM>, sm)) return r;
+  if (int r = grant_smem<attn_dkdv_exact_kernel<T, D, RM>>(sm)) return r;
   LAWCAT_LAUNCH("attn_dkdv_exact", c.stream, attn_dkdv_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles, p));
   LAWCAT_CHECK_LAUNCH();
   if (p.n == 1) return LAWCAT_OK;

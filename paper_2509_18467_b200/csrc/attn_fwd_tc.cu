@@ -560,13 +560,8 @@ static int fwd_tc(const AttnCall& c, const FwdPlan& pl, void* ws) {
     f.part_o = (float*)ws;
     f.part_ml = (float2*)((char*)ws + align_up(rows * D * sizeof(float), 256));
   }
-  auto kernel = attn_fwd_tc_kernel<D, CAP, BIAS>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::BYTES);
-  if (e != cudaSuccess) {
-    cudaGetLastError();
-    note_cuda_error(e, __FILE__, __LINE__);
-    return LAWCAT_ERR_CUDA;
-  }
+  constexpr auto kernel = attn_fwd_tc_kernel<D, CAP, BIAS>;
+  if (int r = grant_smem<kernel>(L::BYTES)) return r;
   LAWCAT_LAUNCH("attn_fwd_tc", c.stream, kernel<<<(unsigned)pl.blocks, L::THREADS, L::BYTES, c.stream>>>(tq, tk, tv, to, f));
   LAWCAT_CHECK_LAUNCH();
   return pl.parts > 1 ? launch_attn_fwd_join(c, pl.parts, f.part_o, f.part_ml) : (int)LAWCAT_OK;

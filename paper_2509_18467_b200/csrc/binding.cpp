@@ -6,6 +6,7 @@
 #include <torch/torch.h>
 
 #include <cstdint>
+#include <string>
 
 namespace {
 
@@ -130,8 +131,38 @@ PyObject* empty(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   }
 }
 
+// expect(name, tensor, dtype, sizes...): ValueError unless the tensor (None passes) has these sizes and this type;
+// dtype: 0 fp32, 1 bf16, 2 uint8, 3 int32
+PyObject* expect(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  static constexpr at::ScalarType types[] = {at::kFloat, at::kBFloat16, at::kByte, at::kInt};
+  static const char* const names[] = {"float32", "bfloat16", "uint8", "int32"};
+  if (nargs < 3 || nargs > 8) {
+    PyErr_SetString(PyExc_TypeError, "expect(name, tensor, dtype, sizes...)");
+    return nullptr;
+  }
+  if (args[1] == Py_None) Py_RETURN_NONE;
+  const long dt = PyLong_AsLong(args[2]);
+  int64_t sz[5];
+  for (Py_ssize_t i = 3; i < nargs; ++i) sz[i - 3] = PyLong_AsLongLong(args[i]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!THPVariable_Check(args[1]) || dt < 0 || dt > 3) {
+    PyErr_SetString(PyExc_TypeError, "expected a tensor or None");
+    return nullptr;
+  }
+  const at::Tensor& t = THPVariable_Unpack(args[1]);
+  if (t.scalar_type() == types[dt] && t.sizes() == at::IntArrayRef(sz, (size_t)nargs - 3)) Py_RETURN_NONE;
+  std::string want, got;
+  for (Py_ssize_t i = 3; i < nargs; ++i) want += (i > 3 ? ", " : "") + std::to_string(sz[i - 3]);
+  for (int64_t i = 0; i < t.dim(); ++i) got += (i ? ", " : "") + std::to_string(t.size(i));
+  const char* name = PyUnicode_AsUTF8(args[0]);
+  PyErr_Format(PyExc_ValueError, "%s: expected [%s] of %s, got [%s] of %s", name ? name : "tensor", want.c_str(), names[dt], got.c_str(),
+               c10::toString(t.scalar_type()));
+  return nullptr;
+}
+
 PyMethodDef methods[] = {
     {"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, "call an entry point of the CUDA library"},
+    {"expect", (PyCFunction)(void (*)(void))expect, METH_FASTCALL, "check a tensor's sizes and type"},
     {"empty", (PyCFunction)(void (*)(void))empty, METH_FASTCALL, "uninitialised tensor"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods};
