@@ -6,15 +6,15 @@
 //   S = A1 B1^T, dP = A2 B2^T (shared memory), P = exp2(S scale - lse), dX = P (dP - D) f (one thread per own row; f = 1 - tanh^2
 //   under a cap, else 1), acc1 += dX B1, acc2 += P B2 (keys) or P f B1 (queries), dX and P as bf16 in tensor memory over dP and S.
 // Two warpgroups take the walked tiles in turn, each with an S and a dP of its own: one tile's exponentials run behind the other
-// tile's products.
+// tile's products. A third one takes the finished gradients out of tensor memory while they go on with the next item.
 // D = sum_j p_j dP_j comes out of the first form's own loop, in fp32: it starts from dO.o, whose o was rounded, and what that was off
 // by is put right at the end with R: dQ = acc1 + (dO.o - D) R. The second form reads (lse, D) of every query as the first left them.
 // (With dO.o for D the gradients of q and k were 2.6e-3 off 64 bits, of which 2.3e-3 are the roundings below.)
 // The sums over queries and over keys stay in tensor memory per item, in one order: no atomics, the same bits every time.
 // The price is S and dP computed twice (7 products of 128 x 128 x d per pair of tiles instead of 5).
 // A block takes items in turn, the longest first, as in the forward: the next item's own tiles and first walked ones come in
-// while this one's last are weighed and its gradients leave through shared memory and the copy engine. dO.o is summed by two warps of
-// their own, an item ahead.
+// while this one's last are weighed and its gradients leave through shared memory and the copy engine. dO.o is
+// summed from the item's tiles of dO and o in shared memory.
 // Rounding: P and dX to bf16 as operands, the gradients once. All else is fp32.
 // Rows that come out not finite are computed again on the CUDA cores, as in the forward.
 #include "attn_tc.cuh"
@@ -33,13 +33,14 @@ template <int D>
 struct BwdLay {
   static constexpr uint32_t OWN = 128 * D * 2, WALK = 64 * D * 2, STAT = 512;   // (a tile's -lse log2e, then its -D)
   static constexpr int ST = D == 128 ? 3 : 4, SLOTS = 4;
-  static constexpr uint32_t STAGE = 2 * WALK, OUT = 128 * 128;                  // a warpgroup's gradients on their way: 64 channels
-  static constexpr uint32_t OFF_A = 0, OFF_RING = 2 * OWN, OFF_OUT = OFF_RING + ST * STAGE, OFF_STAT = OFF_OUT + 2 * OUT, OFF_DEX = OFF_STAT + ST * STAT,
+  static constexpr int OUTS = D == 128 ? 1 : 2;                                 // places for gradients on their way, of 64 channels
+  static constexpr uint32_t STAGE = 2 * WALK, OUT = 128 * 128;
+  static constexpr uint32_t OFF_A = 0, OFF_RING = 3 * OWN, OFF_OUT = OFF_RING + ST * STAGE, OFF_STAT = OFF_OUT + OUTS * OUT, OFF_DEX = OFF_STAT + ST * STAT,
                             OFF_OWN = OFF_DEX + 2048, OFF_LIST = OFF_OWN + 2048, OFF_ITEM = OFF_LIST + BAD_MAX * 4, OFF_ASK = OFF_ITEM + SLOTS * 64, OFF_BAR = OFF_ASK + 16;
   static constexpr uint32_t BYTES = OFF_BAR + 512, E1 = (uint32_t)dq_smem<D, 4, 128>(), E2 = (uint32_t)dkdv_smem<D, 4, 128>();
-  static constexpr int THREADS = 384;   // weights, copies, products, two warps for dO.o
+  static constexpr int THREADS = 448;   // weights, outputs, copies, products
   static constexpr int B_A = 0, B_AE = 1, B_FULL = 2, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + 2, B_ACC = B_P + 2, B_ACCE = B_ACC + 1,
-                       B_OWN = B_ACCE + 1, B_OWNE = B_OWN + 2, B_ITEM = B_OWNE + 2, B_ITEME = B_ITEM + SLOTS, B_ASK = B_ITEME + SLOTS, NBAR = B_ASK + 1;
+                       B_DEX = B_ACCE + 1, B_ITEM = B_DEX + 2, B_ITEME = B_ITEM + SLOTS, B_ASK = B_ITEME + SLOTS, NBAR = B_ASK + 1;
   static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 512 && E1 <= OFF_LIST && E2 <= OFF_LIST, "shared memory");
 };
 
@@ -100,7 +101,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
 
   if (tid == 0) {
     mbar_init(bar(L::B_A), 1);
-    mbar_init(bar(L::B_AE), 1);
+    mbar_init(bar(L::B_AE), KV ? 1 : 257);                // (the threads of weights read dO and o)
     for (int i = 0; i < L::ST; ++i) {
       mbar_init(bar(L::B_FULL + i), 1);
       mbar_init(bar(L::B_EMPTY + i), KV ? 129 : 1);   // (the softmax threads read the statistics)
@@ -108,14 +109,13 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(L::B_S + i), 1);
       mbar_init(bar(L::B_P + i), 128);
-      mbar_init(bar(L::B_OWN + i), 64);
-      mbar_init(bar(L::B_OWNE + i), 256);
+      mbar_init(bar(L::B_DEX + i), 256);
     }
     mbar_init(bar(L::B_ACC), 1);
-    mbar_init(bar(L::B_ACCE), 256);
+    mbar_init(bar(L::B_ACCE), 128);
     for (int i = 0; i < L::SLOTS; ++i) {
       mbar_init(bar(L::B_ITEM + i), 1);
-      mbar_init(bar(L::B_ITEME + i), KV ? 9 : 11);    // (warps of weights, the product thread, the two for dO.o)
+      mbar_init(bar(L::B_ITEME + i), 13);                  // (warps of weights and outputs, and the product thread)
     }
     mbar_init(bar(L::B_ASK), 1);
     s_flags[1] = 0;
@@ -126,7 +126,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
     tma_prefetch_desc(&tm_b1);
     tma_prefetch_desc(&tm_b2);
   }
-  if (warp == 8) {
+  if (warp == 12) {
     tmem_alloc(sb + L::OFF_BAR + 8 * L::NBAR, 512);
     tmem_relinquish();
   }
@@ -147,7 +147,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
   };
   auto item_read = [&](int k) { mbar_arrive(bar(L::B_ITEME + k % L::SLOTS)); };
 
-  if (warp == 8) {
+  if (warp == 12) {
     // ------------------------------------------------------------------------------------------------ copies
     if (elect_one()) {
       int step = 0, seq = 0, k = 0;   // walked tiles, items with tiles, items so far
@@ -165,9 +165,10 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
         if (w.n > 0) {
           if (seq > 0) ok = wait_bar(bar(L::B_AE), (seq - 1) & 1, s_abort, f.limit);
           if (!ok) break;
-          mbar_arrive_expect_tx(bar(L::B_A), 2 * L::OWN);
+          mbar_arrive_expect_tx(bar(L::B_A), (KV ? 2 : 3) * L::OWN);
           load_tile<D, 128>(sb + L::OFF_A, &tm_a1, bar(L::B_A), w.own, w.r0, w.b);
           load_tile<D, 128>(sb + L::OFF_A + L::OWN, &tm_a2, bar(L::B_A), w.own, w.r0, w.b);
+          if (!KV) load_tile<D, 128>(sb + L::OFF_A + 2 * L::OWN, &tm_o2, bar(L::B_A), w.own, w.r0, w.b);   // (o)
           int h = KV ? w.own * G : quot(w.own, f.group), at = w.w0, left = w.per;
           for (int it = 0; it < w.n; ++it, ++step) {
             const int s = step % L::ST;
@@ -201,7 +202,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
         }
       }
     }
-  } else if (warp == 9) {
+  } else if (warp == 13) {
     // ------------------------------------------------------------------------------------------------ products
     if (elect_one()) {
       constexpr uint32_t id_s = instr_desc(128, 64, FMT_BF16, MAJOR_K, MAJOR_K);
@@ -253,49 +254,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
         if (n > 0) ok = wait_bar(bar(L::B_A), seq & 1, s_abort, f.limit) && scores(step, n == 1);
       }
     }
-  } else if (warp >= 10) {
-    // ------------------------------------------------------------------------------------------------ -lse log2e and -dO.o of own queries
-    if (!KV) {
-      float* const s_own = reinterpret_cast<float*>(smem + L::OFF_OWN);
-      int seq = 0;
-      for (int k = 0;; ++k) {
-        Item w;
-        w.n = -1;
-        if (!__all_sync(0xffffffffu, item_at(k, w)) || w.n < 0) break;
-        if (lane == 0) item_read(k);
-        if (w.n == 0) continue;
-        float *const nl = s_own + (seq & 1) * 256, *const nd = nl + 128;
-        if (seq >= 2 && !__all_sync(0xffffffffu, wait_bar(bar(L::B_OWNE + (seq & 1)), ((seq >> 1) - 1) & 1, s_abort, f.limit))) break;
-        const int first = (warp - 10) * 64;
-        constexpr int LPR = D / 8, RP = 32 / LPR;   // lanes per row, rows at a time
-#pragma unroll 1
-        for (int i0 = first + lane / LPR; i0 < first + 64; i0 += 16 * RP) {   // (sixteen loads of each in flight: two warps have an item's time)
-          uint4 x[16], y[16];
-#pragma unroll
-          for (int u = 0; u < 16; ++u) {
-            const int t = w.r0 + i0 + u * RP;
-            const size_t at = (((size_t)w.b * a.mask.T + min(t, rows - 1)) * a.H + w.own) * D + lane % LPR * 8;
-            x[u] = __ldg(reinterpret_cast<const uint4*>((const bf16*)a.o_in + at));
-            y[u] = __ldg(reinterpret_cast<const uint4*>((const bf16*)a.dO + at));
-          }
-#pragma unroll
-          for (int u = 0; u < 16; ++u) {
-            float d = fmaf(bf16_lo(x[u].x), bf16_lo(y[u].x), bf16_hi(x[u].x) * bf16_hi(y[u].x));
-            d = fmaf(bf16_lo(x[u].y), bf16_lo(y[u].y), fmaf(bf16_hi(x[u].y), bf16_hi(y[u].y), d));
-            d = fmaf(bf16_lo(x[u].z), bf16_lo(y[u].z), fmaf(bf16_hi(x[u].z), bf16_hi(y[u].z), d));
-            d = fmaf(bf16_lo(x[u].w), bf16_lo(y[u].w), fmaf(bf16_hi(x[u].w), bf16_hi(y[u].w), d));
-#pragma unroll
-            for (int o = LPR / 2; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-            if (lane % LPR == 0) nd[i0 + u * RP] = -d;
-          }
-        }
-        for (int i = first + lane; i < first + 64; i += 32)
-          nl[i] = w.r0 + i < rows ? -a.lse[((size_t)w.b * a.mask.T + w.r0 + i) * a.H + w.own] * LOG2E : 0.f;
-        mbar_arrive(bar(L::B_OWN + (seq & 1)));
-        ++seq;
-      }
-    }
-  } else {
+  } else if (warp < 8) {
     // ------------------------------------------------------------------------------------------------ weights and their gradients
     const int wg = warp >> 2, r128 = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -306,22 +265,38 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
     Item w;
     w.n = -1;
     bool ok = __all_sync(0xffffffffu, item_at(k, w));
-    if (KV ? named_bar_or(2 + wg, 128, !ok) : named_bar_or(2, 256, !ok)) break;   // (warps that meet at barriers leave together)
-    if (w.n < 0) break;
+    if (!ok || w.n < 0) break;
     if (lane == 0) item_read(k);
+    if (w.n == 0) continue;
     const int n = w.n, r = w.r0 + r128;
-    const bool valid = r < rows;
     // the columns that this row meets: the keys that the query sees, or the queries that see the key
     const int2 iv = KV ? key_interval(a.mask, w.b, min(r, rows - 1)) : interval(a.mask, w.b, min(r, rows - 1));   // (rows behind the last are never stored)
     int lo0 = 0, lo1 = 0, hi0 = 0, hi1 = 0;   // what the warp's rows meet in all: [lo0, hi1), every row: [lo1, hi0)
     float nl = 0.f, nd = 0.f;   // -lse log2e and -dO.o of an own query
     uint64_t dex = 0;           // sums of p dP
-    if (!KV && n > 0) {
-      ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_OWN + (seq & 1)), (seq >> 1) & 1, s_abort, f.limit));
-      const float* const own = reinterpret_cast<const float*>(smem + L::OFF_OWN) + (seq & 1) * 256;
-      nl = own[r128];
-      nd = own[128 + r128];
-      mbar_arrive(bar(L::B_OWNE + (seq & 1)));
+    if (!KV) {
+      const float lse = r < rows ? a.lse[((size_t)w.b * a.mask.T + r) * a.H + w.own] : 0.f;
+      ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_A), seq & 1, s_abort, f.limit));
+      if (!ok) break;
+      const uint32_t row = sb + L::OFF_A + L::OWN + sw128(r128, 0);   // (chunk j of a row: its address with bits 4 ... 6 turned over by j)
+      float d0 = 0.f, d1 = 0.f;
+#pragma unroll 4
+      for (int j = 0; j < D / 8; ++j) {
+        const uint32_t at = (row ^ (uint32_t)((j & 7) << 4)) + (j >> 3) * 16384;
+        const uint4 x = lds128(at), y = lds128(at + L::OWN);
+        d0 = fmaf(bf16_lo(x.x), bf16_lo(y.x), fmaf(bf16_lo(x.y), bf16_lo(y.y), d0));
+        d1 = fmaf(bf16_hi(x.x), bf16_hi(y.x), fmaf(bf16_hi(x.y), bf16_hi(y.y), d1));
+        d0 = fmaf(bf16_lo(x.z), bf16_lo(y.z), fmaf(bf16_lo(x.w), bf16_lo(y.w), d0));
+        d1 = fmaf(bf16_hi(x.z), bf16_hi(y.z), fmaf(bf16_hi(x.w), bf16_hi(y.w), d1));
+      }
+      mbar_arrive(bar(L::B_AE));
+      nd = -(d0 + d1);
+      nl = -lse * LOG2E;
+      if (wg == 0) {
+        float* const own = reinterpret_cast<float*>(smem + L::OFF_OWN) + (seq & 1) * 256;
+        own[r128] = nl;
+        own[128 + r128] = nd;
+      }
     }
     lo0 = __shfl_sync(0xffffffffu, iv.x, 0);
     lo1 = __shfl_sync(0xffffffffu, iv.x, 31);
@@ -338,42 +313,39 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
       if (!ok) break;
       tc_fence_after_sync();
       const int c0 = w.w0 + col * 64, st = step % L::ST;
-      if (c0 >= hi1 || c0 + 64 <= lo0) {   // (no row of the warp meets the tile)
-        float z[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) z[e] = 0.f;
-        tmem_st32(S, z);
-        tmem_st32(P, z);
-        tmem_wait_st();
-        tc_fence_before_sync();
-        mbar_arrive(bar(L::B_P + wg));
-        if (KV) mbar_arrive(bar(L::B_EMPTY + st));
-        continue;
-      }
       const float4* stat = reinterpret_cast<const float4*>(smem + L::OFF_STAT + st * L::STAT);
       const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f;
-      float s[64], p[64];
-      tmem_ld32(S, s);
-      tmem_ld32(S + 32, s + 32);
-      tmem_ld32(P, p);
-      tmem_ld32(P + 32, p + 32);
-      tmem_wait_ld();
-      // |i - j| = |dist0 - c|
-      const float dist0 = (float)(KV ? r - c0 - a.mask.off : r + a.mask.off - c0);
       if (KV) mbar_wait(bar(L::B_FULL + st), (step / L::ST) & 1);   // (complete by now; makes the copied statistics visible here)
-      if (CAP) cap_scores(s, a.scale / a.cap, c2);
       const uint64_t sc = f2_pack(CAP ? 1.f : scale2, CAP ? 1.f : scale2), one = f2_pack(1.f, 1.f), nic = f2_pack(nic2, nic2);
       // weights and their gradients over the scores, as bf16 pairs; `some`: not every column is met, or not all lie on one side
+#pragma unroll 1
+      for (int hf = 0; hf < 2; ++hf) {   // 32 columns at a time: what a thread holds of them has to fit beside the other warps' registers
+      const int c1 = c0 + hf * 32;
+      if (c1 >= hi1 || c1 + 32 <= lo0) {   // (no row of the warp meets them)
+        float z[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[e] = 0.f;
+        tmem_st16(S + hf * 16, z);
+        tmem_st16(P + hf * 16, z);
+        continue;
+      }
+      float s[32], p[32];
+      tmem_ld32(S + hf * 32, s);
+      tmem_ld32(P + hf * 32, p);
+      tmem_wait_ld();
+      if (CAP) cap_scores(s, a.scale / a.cap, c2);
+      // |i - j| = |dist0 - c|
+      const float dist0 = (float)(KV ? r - c1 - a.mask.off : r + a.mask.off - c1);
       const float slope_c = KV ? -slope2 : slope2, bias0 = -slope_c * dist0;   // (on one side: the bias is bias0 + slope_c c)
       auto weigh = [&](auto some) {
-        const int rel = iv.x - c0;
+        const int rel = iv.x - c1;
         const uint32_t len = (uint32_t)(iv.y - iv.x);
 #pragma unroll
-        for (int q = 0; q < 64; q += 4) {
+        for (int q = 0; q < 32; q += 4) {
           float4 l4 = make_float4(nl, nl, nl, nl), d4 = make_float4(nd, nd, nd, nd);
           if (KV) {
-            l4 = stat[q / 4];
-            d4 = stat[16 + q / 4];
+            l4 = stat[hf * 8 + q / 4];
+            d4 = stat[16 + hf * 8 + q / 4];
           }
 #pragma unroll
           for (int e = 0; e < 4; e += 2) {
@@ -420,59 +392,78 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
           }
         }
       };
-      if (lo1 <= c0 && hi0 >= c0 + 64 && (!BIAS || __all_sync(0xffffffffu, KV ? dist0 <= 0.f : dist0 >= 63.f))) weigh(std::false_type{});
+      if (lo1 <= c1 && hi0 >= c1 + 32 && (!BIAS || __all_sync(0xffffffffu, KV ? dist0 <= 0.f : dist0 >= 31.f))) weigh(std::false_type{});
       else weigh(std::true_type{});
-      tmem_st32(S, s);
-      tmem_st32(P, p);
+      tmem_st16(S + hf * 16, s);
+      tmem_st16(P + hf * 16, p);
+      }
       tmem_wait_st();
       tc_fence_before_sync();
       mbar_arrive(bar(L::B_P + wg));
       if (KV) mbar_arrive(bar(L::B_EMPTY + st));
     }
     base += n;
-    if (ok && n > 0) ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_ACC), seq & 1, s_abort, f.limit));
-    float* const s_dex = reinterpret_cast<float*>(smem + L::OFF_DEX) + (k & 1) * 256;
+    if (!ok) break;
     if (!KV) {
       float d0, d1;
       f2_unpack(dex, d0, d1);
-      s_dex[tid] = d0 + d1;
+      reinterpret_cast<float*>(smem + L::OFF_DEX)[(seq & 1) * 256 + tid] = d0 + d1;
+      mbar_arrive(bar(L::B_DEX + (seq & 1)));
     }
-    if (KV ? named_bar_or(2 + wg, 128, !ok) : named_bar_or(2, 256, !ok)) break;   // (all of them go on, or none)
-    tc_fence_after_sync();
+    ++seq;
+    }
+  } else {
+    // ------------------------------------------------------------------------------------------------ outputs
+    const int r128 = tid & 127;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    int seq = 0;
+    bool fail = false;
+    for (int k = 0;; ++k) {
+    Item w;
+    w.n = -1;
+    fail = !item_at(k, w);
+    if (named_bar_or(2, 128, fail) || w.n < 0) break;
+    if (lane == 0) item_read(k);
+    const int n = w.n, r = w.r0 + r128;
+    const bool valid = r < rows;
     float fix = 0.f;   // dO.o - D
-    if (!KV) {
-      const float d = s_dex[r128] + s_dex[128 + r128];
-      fix = -nd - d;
-      if (valid && wg == 0 && n > 0) {
-        float* const st = a.stat + ((size_t)w.b * a.H + w.own) * a.stat_stride + r;
-        st[0] = nl;
-        st[(size_t)a.B * a.H * a.stat_stride] = -d;
+    if (n > 0) {
+      fail = !wait_bar(bar(L::B_ACC), seq & 1, s_abort, f.limit);
+      if (!KV) {
+        if (!fail) fail = !wait_bar(bar(L::B_DEX + (seq & 1)), (seq >> 1) & 1, s_abort, f.limit);
+        const float* const dex = reinterpret_cast<const float*>(smem + L::OFF_DEX) + (seq & 1) * 256;
+        const float* const own = reinterpret_cast<const float*>(smem + L::OFF_OWN) + (seq & 1) * 256;
+        const float d = dex[r128] + dex[128 + r128], nl = own[r128];
+        fix = -own[128 + r128] - d;
+        if (valid) {
+          float* const st = a.stat + ((size_t)w.b * a.H + w.own) * a.stat_stride + r;
+          st[0] = nl;
+          st[(size_t)a.B * a.H * a.stat_stride] = -d;
+        }
       }
+      __syncwarp();
+      tc_fence_after_sync();
     }
-    // keys: one group stores dv, the other dk; queries: half of dq's channels each (all of them one group at D = 64); by 64 channels
-    // through shared memory and the copy engine, which leaves out rows behind the last
-    const uint32_t acc = (KV && !wg ? acc2 : acc1) + lanes, out = sb + L::OFF_OUT + wg * L::OUT;
-    const float mul = KV && !wg ? 1.f : a.scale;
-    const int c_first = KV ? 0 : wg * 64, c_end = KV ? D : min(D, c_first + 64);
+    // dq; or dk, then dv: by 64 channels through shared memory and the copy engine, which leaves out rows behind the last
     float test = 0.f;
-    if (c_first >= c_end && n > 0) {
-      tc_fence_before_sync();
-      mbar_arrive(bar(L::B_ACCE));
-    }
 #pragma unroll 1
-    for (int c = c_first; c < c_end; c += 32) {
+    for (int x = 0; x < (KV ? 2 * D : D); x += 32) {
+      const bool second = KV && x >= D;              // (dv)
+      const int c = second ? x - D : x;
+      const uint32_t out = sb + L::OFF_OUT + (L::OUTS == 2 ? (x / 64 & 1) : 0) * L::OUT;
+      const float mul = second ? 1.f : a.scale;
       float o[32];
       if (n > 0) {
-        tmem_ld32(acc + c, o);
+        tmem_ld32(acc1 + lanes + x, o);              // (acc2 lies behind acc1)
         if (!KV) {
           float u[32];
-          tmem_ld32(acc2 + lanes + c, u);
+          tmem_ld32(acc2 + lanes + x, u);
           tmem_wait_ld();
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = fmaf(fix, u[e], o[e]);
         }
         tmem_wait_ld();
-        if (c + 32 == c_end) {
+        if (x + 32 == (KV ? 2 * D : D)) {
           tc_fence_before_sync();
           mbar_arrive(bar(L::B_ACCE));
         }
@@ -481,8 +472,11 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
         for (int e = 0; e < 32; ++e) o[e] = 0.f;
       }
       if (c % 64 == 0) {
-        if (r128 == 0) tma_store_wait_read();
-        named_bar_sync(4 + wg, 128);
+        if (r128 == 0) {                             // (this place's last store has read it)
+          if (L::OUTS == 2) tma_store_wait_read_1();
+          else tma_store_wait_read();
+        }
+        named_bar_sync(2, 128);
       }
 #pragma unroll
       for (int e = 0; e < 32; ++e) {
@@ -495,9 +489,9 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
                                                           pack_bf16(o[8 * e + 4], o[8 * e + 5]), pack_bf16(o[8 * e + 6], o[8 * e + 7])));
       if (c % 64 == 32) {
         fence_proxy_async();
-        named_bar_sync(4 + wg, 128);
+        named_bar_sync(2, 128);
         if (r128 == 0) {
-          tma_store_4d(KV && !wg ? &tm_o2 : &tm_o1, out, c - 32, w.own, w.r0, w.b);
+          tma_store_4d(second ? &tm_o2 : &tm_o1, out, c - 32, w.own, w.r0, w.b);
           tma_store_commit();
         }
       }
@@ -514,7 +508,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
   }
   tc_fence_before_sync();
   __syncthreads();
-  if (warp == 8) tmem_dealloc(tmem, 512);
+  if (warp == 12) tmem_dealloc(tmem, 512);
   const int bad = *s_abort ? 0 : min(s_flags[2], BAD_MAX);
   if (tid >= 128) return;
   for (int e = 0; e < bad; ++e) {
@@ -535,7 +529,7 @@ static int bwd_tc(const AttnCall& c) {
   if (!tensor_map(&q, a.q, false, a.H, T, a.B, D, 64, rq, true) || !tensor_map(&g, a.dO, false, a.H, T, a.B, D, 64, rq, true) ||
       !tensor_map(&k, a.k, false, a.H_kv, T_k, a.B, D, 64, rk, true) || !tensor_map(&v, a.v, false, a.H_kv, T_k, a.B, D, 64, rk, true) ||
       !tensor_map(&o1, KV ? a.dk : a.dq, false, KV ? a.H_kv : a.H, KV ? T_k : T, a.B, D, 64, 128, true) ||
-      !tensor_map(&o2, KV ? a.dv : a.dq, false, KV ? a.H_kv : a.H, KV ? T_k : T, a.B, D, 64, 128, true))
+      !tensor_map(&o2, KV ? a.dv : a.o_in, false, KV ? a.H_kv : a.H, KV ? T_k : T, a.B, D, 64, 128, true))
     return LAWCAT_ERR_CUDA;
   const int tiles = ((KV ? T_k : T) + 127) / 128;
   const long long blocks = (long long)tiles * a.B * (KV ? a.H_kv : a.H);

@@ -47,6 +47,8 @@ inline FastDiv fast_div(uint32_t d) {
 __device__ __forceinline__ int quot(int n, const FastDiv& f) { return (int)(((uint64_t)(uint32_t)n * f.mul) >> f.shift); }
 __device__ __forceinline__ int rest(int n, int q, const FastDiv& f) { return n - q * (int)f.d; }
 
+__device__ __forceinline__ void tma_store_wait_read_1() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+
 // rows x D channels of one head at token t into slabs of 64 channels (rows x 128 bytes, swizzled)
 template <int D, int ROWS>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int t, int b) {
