@@ -49,14 +49,15 @@ template <int D>
 struct FwdLay {
   static constexpr uint32_t TILE = 128 * D * 2, KT = 64 * D * 2; // a Q tile; a K or V tile
   static constexpr int ST = 8;                                   // stages of the ring (K and V tiles alternate)
+  static constexpr int NQ = D == 64 ? 2 : 1;                     // items whose Q tiles fit
   static constexpr uint32_t OUT = 128 * 128;                     // a warpgroup's outputs on their way: 64 channels (or 32 in fp32)
   static constexpr int SLOTS = 4;                                // items on their way
-  static constexpr uint32_t OFF_Q = 0, OFF_RING = NT * TILE, OFF_OUT = OFF_RING + ST * KT, OFF_ML = OFF_OUT + OUT, OFF_LIST = OFF_ML + 2 * NT * 128 * 8,
+  static constexpr uint32_t OFF_Q = 0, OFF_RING = NQ * NT * TILE, OFF_OUT = OFF_RING + ST * KT, OFF_ML = OFF_OUT + OUT, OFF_LIST = OFF_ML + 2 * NT * 128 * 8,
                             OFF_ITEM = OFF_LIST + BAD_MAX * 4, OFF_ASK = OFF_ITEM + SLOTS * 64, OFF_BAR = OFF_ASK + 16;
   static constexpr uint32_t BYTES = OFF_BAR + 512;
   static constexpr int THREADS = NT * 128 + 192;                 // softmax, outputs, copies, products
   // mbarriers
-  static constexpr int B_Q = 0, B_QE = 1, B_FULL = 2, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + 2 * NT, B_O = B_P + 2 * NT, B_OE = B_O + 2 * NT,
+  static constexpr int B_Q = 0, B_QE = NQ, B_FULL = 2 * NQ, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + 2 * NT, B_O = B_P + 2 * NT, B_OE = B_O + 2 * NT,
                        B_ML = B_OE + NT, B_ITEM = B_ML + NT, B_ITEME = B_ITEM + SLOTS, B_ASK = B_ITEME + SLOTS, NBAR = B_ASK + 1;
   static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 512 && fwd_smem<D, 4, 128>() <= OFF_LIST && NT * (128 + D) <= 512, "shared memory, tensor memory");
 };
@@ -111,8 +112,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   auto row_of = [&](const Item& w, int i) { return w.tb + (f.two_heads ? 0 : 128 * i); };
 
   if (tid == 0) {
-    mbar_init(bar(L::B_Q), 1);
-    mbar_init(bar(L::B_QE), 1);
+    for (int i = 0; i < 2 * L::NQ; ++i) mbar_init(bar(L::B_Q + i), 1);
     for (int i = 0; i < L::ST; ++i) {
       mbar_init(bar(L::B_FULL + i), 1);
       mbar_init(bar(L::B_EMPTY + i), 1);
@@ -174,10 +174,12 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         ++k;
         if (idx < 0) break;
         if (w.n > 0) {
-          if (seq > 0) ok = wait_bar(bar(L::B_QE), (seq - 1) & 1, s_abort, f.limit);
+          const int qb = seq % L::NQ;
+          if (seq >= L::NQ) ok = wait_bar(bar(L::B_QE + qb), (seq / L::NQ - 1) & 1, s_abort, f.limit);
           if (!ok) break;
-          mbar_arrive_expect_tx(bar(L::B_Q), NT * L::TILE);
-          for (int i = 0; i < NT; ++i) load_tile<D, 128>(sb + L::OFF_Q + i * L::TILE, &tm_q, bar(L::B_Q), head_of(w, i), row_of(w, i), w.b);
+          mbar_arrive_expect_tx(bar(L::B_Q + qb), NT * L::TILE);
+          for (int i = 0; i < NT; ++i)
+            load_tile<D, 128>(sb + L::OFF_Q + (qb * NT + i) * L::TILE, &tm_q, bar(L::B_Q + qb), head_of(w, i), row_of(w, i), w.b);
           for (int it = 0; it < 2 * w.n; ++it, ++at) {
             const int s = at % L::ST;
             if (at >= L::ST) ok = wait_bar(bar(L::B_EMPTY + s), (at / L::ST - 1) & 1, s_abort, f.limit);
@@ -205,37 +207,54 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       constexpr uint32_t id_o = instr_desc(128, D, FMT_BF16, MAJOR_K, MAJOR_MN);
       auto stage = [&](int at) { return sb + L::OFF_RING + (uint32_t)(at % L::ST) * L::KT; };
       auto full = [&](int at) { return wait_bar(bar(L::B_FULL + at % L::ST), (at / L::ST) & 1, s_abort, f.limit); };
-      // the scores of a step; `last`: of the item
-      auto scores = [&](int i, int step, bool last) {
+      // the scores of a step of the seq-th item; `last`: of the item
+      auto scores = [&](int i, int seq, int step, bool last) {
         if (i == 0 && !full(2 * step)) return false;
         tc_fence_after_sync();
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
-          mma_f16(s_col(i, step), kdesc<128>(sb + L::OFF_Q + i * L::TILE, kk), kdesc<64>(stage(2 * step), kk), id_s, kk != 0);
+          mma_f16(s_col(i, step), kdesc<128>(sb + L::OFF_Q + (seq % L::NQ * NT + i) * L::TILE, kk), kdesc<64>(stage(2 * step), kk), id_s, kk != 0);
         mma_commit(bar(L::B_S + 2 * i + (step & 1)));
         if (i == NT - 1) {
           mma_commit(bar(L::B_EMPTY + 2 * step % L::ST));
-          if (last) mma_commit(bar(L::B_QE));
+          if (last) mma_commit(bar(L::B_QE + seq % L::NQ));
         }
         return true;
       };
+      auto q_bar = [&](int seq) { return bar(L::B_Q + seq % L::NQ); };
+      auto first_scores = [&](int seq, int step, int n) {
+        return wait_bar(q_bar(seq), (seq / L::NQ) & 1, s_abort, f.limit) && scores(0, seq, step, n == 1) && scores(1, seq, step, n == 1);
+      };
       int k = 0, seq = 0, step = 0;   // items, items with tiles, key tiles so far
-      auto next_item = [&]() {   // tiles of the next item that has any; 0 behind the last
+      // tiles of the next item that has any; less than 0 behind the last, 0 (only where it is not to be waited for) when it is not known yet
+      auto next_item = [&](bool wait) {
         Item w;
         w.n = -1;
         do {
+          if (!wait && !mbar_test_wait(bar(L::B_ITEM + k % L::SLOTS), (k / L::SLOTS) & 1)) return 0;
           if (!item_at(k, w)) return -1;
           item_read(k++);
         } while (w.n == 0);
-        return max(w.n, 0);
+        return w.n;
       };
-      int n = next_item();
-      bool ok = n > 0 && wait_bar(bar(L::B_Q), 0, s_abort, f.limit) && scores(0, 0, n == 1) && scores(1, 0, n == 1);
+      int n = next_item(true);
+      bool ok = n > 0 && first_scores(0, 0, n);
       while (n > 0 && ok) {
+        int n_next = 0;
+        bool ahead = false;   // the next item's first scores have been issued
         for (int it = 0; it < n && ok; ++it, ++step) {
+          // where the next item's queries are there already, its first scores go in front of this one's last product
+          if (L::NQ == 2 && it + 1 == n) {
+            n_next = next_item(false);
+            if (n_next > 0 && mbar_test_wait(q_bar(seq + 1), ((seq + 1) / L::NQ) & 1) &&
+                mbar_test_wait(bar(L::B_FULL + (2 * step + 2) % L::ST), ((2 * step + 2) / L::ST) & 1)) {
+              ok = first_scores(seq + 1, step + 1, n_next);
+              ahead = true;
+            }
+          }
 #pragma unroll
           for (int i = 0; i < NT; ++i) {
-            if (ok && it + 1 < n) ok = scores(i, step + 1, it + 2 == n);
+            if (ok && it + 1 < n) ok = scores(i, seq, step + 1, it + 2 == n);
             if (ok && i == 0) ok = full(2 * step + 1);
             if (ok && it == 0 && seq > 0) ok = wait_bar(bar(L::B_OE + i), (seq - 1) & 1, s_abort, f.limit);
             if (ok) ok = wait_bar(bar(L::B_P + 2 * i + (step & 1)), (step >> 1) & 1, s_abort, f.limit);
@@ -248,10 +267,11 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           if (!ok) break;
           mma_commit(bar(L::B_EMPTY + (2 * step + 1) % L::ST));
         }
-        // (asked for behind the item's last product: the other roles finish with it before the copy warp comes to write more down)
-        if (ok) n = next_item();
+        // (waited for behind the item's last product: the other roles finish with it before the copy warp comes to write more down)
+        if (ok && n_next == 0) n_next = next_item(true);
+        n = n_next;
         ++seq;
-        if (ok && n > 0) ok = wait_bar(bar(L::B_Q), seq & 1, s_abort, f.limit) && scores(0, step, n == 1) && scores(1, step, n == 1);
+        if (ok && n > 0 && !ahead) ok = first_scores(seq, step, n);
       }
     }
   } else if (warp < NT * 4) {
