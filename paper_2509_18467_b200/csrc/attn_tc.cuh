@@ -18,14 +18,20 @@ __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_
       : "memory");
 }
 
-// Bounded wait: false when the block has been told to give up or the limit (clock cycles) ran out, which tells the others.
+// Bounded wait: false when the block has been told to give up or the limit (clock cycles) ran out, which tells the others. (A
+// try_wait may take microseconds to come back: under a limit of less, which only a test sets, the barrier is looked at instead.)
 __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
-  if (mbar_try_wait(bar, parity)) return true;
+  const bool look = limit < 1000000LL;
+  if (look ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
   const long long t0 = clock64();
   for (;;) {
+    if (look) {
+      if (mbar_test_wait(bar, parity)) return true;
+    } else {
 #pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-      if (mbar_try_wait(bar, parity)) return true;
+      for (int i = 0; i < 64; ++i)
+        if (mbar_try_wait(bar, parity)) return true;
+    }
     if (*abort_flag) return false;
     if (clock64() - t0 > limit) {
       *abort_flag = 1;

@@ -272,6 +272,99 @@ def test_teacher_student_and_hybrid_together():
         pos += 1
 
 
+@pytest.mark.gpu
+def test_which_kernels_run():
+    """bf16 and widths 64 and 128 run on the tensor cores unless exact results are asked for."""
+    def names(**kw):
+        api.trace_begin()
+        case(T=70, seed=1, **kw)
+        return set(api.trace_end())
+    tc, exact = {"attn_fwd_tc", "attn_dq_tc", "attn_dkdv_tc"}, {"attn_fwd_exact", "attn_dq_exact", "attn_dkdv_exact"}
+    for d in (64, 128):
+        assert names(d=d) == tc
+        assert names(d=d, exact=1) >= exact and not names(d=d, exact=1) & tc
+    assert names(d=32) >= exact and names(d=64, dtype="f32") >= exact
+    assert "attn_rows" in names(cu=[0, 30, 70])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,kw", [(64, dict()), (128, dict(cap=25.0)), (64, dict(window=3000, slopes=True))])
+def test_long_sequence_on_its_last_rows(d, kw):
+    """70001 tokens: the last 200 queries (which see all of them, or the window), and the last 200 keys, which no other query sees."""
+    T, n, H = 70001, 200, 2
+    q, k, v, dO = [draw((1, T, h, d), i, "bf16", 1.5 if i == 0 else 1.0) for i, h in enumerate((H, 1, 1, H))]
+    sl = torch.tensor([0.01, 0.001], device="cuda") if kw.get("slopes") else None
+    p = api.attn_params(1, T, H, 1, d, window=kw.get("window", 0), cap=kw.get("cap", 0.0))
+    r = api.lawcat_attn_fwd(p, q, k, v, slopes=sl)
+    r.update(api.lawcat_attn_bwd(p, q, k, v, r["o"], r["lse"], dO, slopes=sl))
+    last = lambda x: x[:, -n:]  # noqa: E731
+    ref = attention(last(q), k, v, visible(n, T, 1, kw.get("window", 0)), float(torch.tensor(d ** -0.5)), kw.get("cap", 0.0), sl, last(dO), last(r["o"]))
+    err = dict(ref["grad_err"](U16, U16), o=ref["o_sum"] + U16 * ref["o_mag"], lse=ref["lse_err"])
+    for x in ("o", "lse", "dq", "dk", "dv"):
+        want, e = (ref[x], err[x]) if ref[x].shape[1] == n else (last(ref[x]), last(err[x]))
+        check(last(r[x]), want, e, U32 if x == "lse" else U16, x)
+
+
+@pytest.mark.gpu
+def test_two_calls_at_once():
+    """Different calls on two streams, many blocks each, over and over: the results of the calls one after the other."""
+    T, H, H_kv, d = 700, 8, 2, 64
+    p = api.attn_params(2, T, H, H_kv, d, cap=9.0)
+    sets = [[draw((2, T, h, d), 10 * s + i, "bf16") for i, h in enumerate((H, H_kv, H_kv, H))] for s in range(2)]
+
+    def run(x, stream=None):
+        r = api.lawcat_attn_fwd(p, *x[:3], stream=stream)
+        r.update(api.lawcat_attn_bwd(p, *x[:3], r["o"], r["lse"], x[3], stream=stream))
+        return r
+    want = [run(x) for x in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(6):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(run(sets[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for r in got[i]:
+            for n in want[i]:
+                assert torch.equal(r[n], want[i][n]), n
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_wait_that_runs_out_is_reported(d):
+    """With a bound of a few hundred clock cycles, less than any copy or product takes, the kernels' roles give up on one another: each
+    call ends and says so, and the next one, with the bound restored, is right."""
+    T, H, H_kv, B = 500, 4, 2, 2
+    x = [draw((B, T, h, d), i, "bf16") for i, h in enumerate((H, H_kv, H_kv, H))]
+    p, pd = api.attn_params(B, T, H, H_kv, d), api.attn_params(B, 1, H, H_kv, d, T_k=T)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    pos = torch.full((B,), T - 1, dtype=torch.int32, device="cuda")
+    cache = api.quant_cache(pd)
+    api.lawcat_cache_quantize(api.attn_params(B, T, H, H_kv, d, T_k=T), x[1], x[2], torch.zeros_like(pos), *cache)
+    step = [t[:, -1].contiguous() for t in x[:3]]
+    calls = dict(fwd=lambda: api.lawcat_attn_fwd(p, *x[:3], dev_status=status)["o"],
+                 bwd=lambda: api.lawcat_attn_bwd(p, *x[:3], good["o"], good["lse"], x[3], dev_status=status)["dk"],
+                 decode=lambda: api.lawcat_attn_decode(pd, *step, x[1].clone(), x[2].clone(), pos, dev_status=status),
+                 quant=lambda: api.lawcat_attn_decode_quant(pd, *step, *[t.clone() for t in cache], pos, dev_status=status))
+    good = api.lawcat_attn_fwd(p, *x[:3])
+    want = {n: f() for n, f in calls.items()}
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    for n, f in calls.items():
+        api.test_set_wait_limit(300)
+        try:
+            f()
+            torch.cuda.synchronize()
+        finally:
+            api.test_set_wait_limit(0)
+        assert int(status.item()) == 5, n
+        status.zero_()
+        assert torch.equal(f(), want[n]), n
+        assert int(status.item()) == 0
+
+
 # ------------------------------------------------------------------------------------------------ refusals (no GPU)
 @pytest.fixture(scope="module")
 def L():
