@@ -82,16 +82,18 @@ __global__ void __launch_bounds__(256) attn_fwd_join_kernel(const Args a, const 
   if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
 }
 
-// out [B, rows, heads, D] = the sum of the parts [n, B, heads, rows, D]; four channels per thread
+// out [B, rows, heads, D] = the sum of the parts [n, B, heads, rows, D], of x and (gridDim.y = 2) of y; four channels per thread
 template <typename T, int D>
-__global__ void __launch_bounds__(256) attn_sum_kernel(const float* __restrict__ x, T* __restrict__ out, int n, int B, int heads, int rows) {
+__global__ void __launch_bounds__(256) attn_sum_kernel(const Parts p, T* out_x, T* out_y, int B, int heads, int rows) {
+  const float* const x = blockIdx.y ? p.y : p.x;
+  T* const out = blockIdx.y ? out_y : out_x;
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, all = (size_t)B * heads * rows * (D / 4);
   if (i >= all) return;
   const int c = (int)(i % (D / 4));
   const size_t r = i / (D / 4), t = r % rows, bh = r / rows;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int k = 0; k < n; ++k) {
+  for (int k = 0; k < p.n; ++k) {
     const float4 v = reinterpret_cast<const float4*>(x)[k * all + i];
     s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
   }
@@ -105,11 +107,13 @@ static unsigned blocks(long long rows, long long n, int bm, int parts) {
   return x <= 0x7fffffffLL ? (unsigned)x : 0;
 }
 static int rows_per_thread(int rows) { return rows <= 16 ? 1 : 4; }
-// Parts that a row block's `tiles` tiles are shared out into: two blocks per SM where one of 64 rows each would leave SMs idle.
+// Parts that a row block's `tiles` tiles are shared out into: as many as give every SM two blocks, four where the blocks differ in length
+// and there are fewer than that (1500 tokens, 32/8 heads of 64 in fp32, 192 blocks of keys: the gradients of K and V take 636 + 9 us,
+// 888 us with a block each; 4 x 300 tokens, 8 heads: the three kernels within 3 % either way).
 static int parts_of(int rows, long long n, long long tiles) {
-  const long long x = (rows + 63) / 64 * n;
-  if (x == 0 || x >= sm_count()) return 1;
-  return (int)std::max(1LL, std::min(std::min((2LL * sm_count() + x - 1) / x, tiles), 16LL));
+  const long long x = (rows + 63) / 64 * n, sms = sm_count();
+  if (x == 0 || x >= 4 * sms) return 1;
+  return (int)std::max(1LL, std::min(std::min(((x < sms ? 2 : 4) * sms + x - 1) / x, tiles), 16LL));
 }
 static int parts_q(const Mask& m, int B, int H) {
   const long long keys = m.window && m.window < m.T_k ? std::min<long long>(m.T_k, (long long)m.window + 63) : m.T_k;
@@ -135,9 +139,10 @@ static int fwd(const AttnCall& c, const Parts& p) {
 }
 
 template <typename T, int D>
-static int sum(const AttnCall& c, const float* x, void* out, int parts, int heads, int rows) {
+static int sum(const AttnCall& c, const Parts& p, void* out_x, void* out_y, int heads, int rows) {
   const long long n = ((long long)c.a.B * heads * rows * (D / 4) + 255) / 256;
-  LAWCAT_LAUNCH("attn_sum", c.stream, attn_sum_kernel<T, D><<<(unsigned)n, 256, 0, c.stream>>>(x, (T*)out, parts, c.a.B, heads, rows));
+  LAWCAT_LAUNCH("attn_sum", c.stream,
+                attn_sum_kernel<T, D><<<dim3((unsigned)n, out_y ? 2 : 1), 256, 0, c.stream>>>(p, (T*)out_x, (T*)out_y, c.a.B, heads, rows));
   LAWCAT_CHECK_LAUNCH();
   return LAWCAT_OK;
 }
@@ -151,7 +156,7 @@ static int dq(const AttnCall& c, const Parts& p) {
   if (int r = grant_smem<attn_dq_exact_kernel<T, D, RM>>(sm)) return r;
   LAWCAT_LAUNCH("attn_dq_exact", c.stream, attn_dq_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles, p));
   LAWCAT_CHECK_LAUNCH();
-  return p.n > 1 ? sum<T, D>(c, p.x, c.a.dq, p.n, c.a.H, c.a.mask.T) : (int)LAWCAT_OK;
+  return p.n > 1 ? sum<T, D>(c, p, c.a.dq, nullptr, c.a.H, c.a.mask.T) : (int)LAWCAT_OK;
 }
 
 template <typename T, int D, int RM>
@@ -163,9 +168,7 @@ static int dkdv(const AttnCall& c, const Parts& p) {
   if (int r = grant_smem<attn_dkdv_exact_kernel<T, D, RM>>(sm)) return r;
   LAWCAT_LAUNCH("attn_dkdv_exact", c.stream, attn_dkdv_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles, p));
   LAWCAT_CHECK_LAUNCH();
-  if (p.n == 1) return LAWCAT_OK;
-  const int r = sum<T, D>(c, p.x, c.a.dk, p.n, c.a.H_kv, c.a.mask.T_k);
-  return r ? r : sum<T, D>(c, p.y, c.a.dv, p.n, c.a.H_kv, c.a.mask.T_k);
+  return p.n > 1 ? sum<T, D>(c, p, c.a.dk, c.a.dv, c.a.H_kv, c.a.mask.T_k) : (int)LAWCAT_OK;
 }
 
 template <typename F>

@@ -14,6 +14,7 @@
 #include <type_traits>
 
 #include "attn.cuh"
+#include "tc_common.cuh"
 
 namespace lawcat {
 namespace attn {
@@ -23,78 +24,115 @@ constexpr int BN = 64;       // rows of the walked side per tile
 template <int NTHR>
 __device__ __forceinline__ void sync_rows() { asm volatile("bar.sync 1, %0;" ::"n"(NTHR) : "memory"); }
 
-// R rows x D channels from rows row0 + r < rows_end of a [*, heads, D] tensor into shared memory (fp32, row stride D + 4); zeros behind
-template <typename T, int D, int NTHR>
-__device__ __forceinline__ void load_rows(float* dst, const T* src, size_t row_stride, int row0, int rows_end, int R) {
-  constexpr int PER = 16 / sizeof(T), VPR = D / PER;  // elements per 16-byte load, loads per row
-  for (int i = threadIdx.x; i < R * VPR; i += NTHR) {
-    const int r = i / VPR, c = i % VPR * PER;
-    float* d = dst + r * (D + 4) + c;
-    if (row0 + r < rows_end) {
-      const uint4 w = __ldg(reinterpret_cast<const uint4*>(src + (size_t)(row0 + r) * row_stride + c));
+// R rows x D channels from rows row0 + r < rows_end of a [*, heads, D] tensor into shared memory (fp32, row stride D + 4); zeros behind.
+// Four loads of a thread are in flight together.
+template <typename T, int D, int NTHR, int R>
+__device__ __forceinline__ void load_rows(float* dst, const T* src, size_t row_stride, int row0, int rows_end) {
+  constexpr int PER = 16 / sizeof(T), VPR = D / PER, N = R * VPR;  // elements per 16-byte load, loads per row, loads
+  constexpr int U = N >= 4 * NTHR ? 4 : N >= 2 * NTHR ? 2 : 1;
+#pragma unroll 1
+  for (int i0 = threadIdx.x; i0 < N; i0 += U * NTHR) {
+    uint4 w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * NTHR, r = i / VPR, c = i % VPR * PER;
+      w[u] = i < N && row0 + r < rows_end ? __ldg(reinterpret_cast<const uint4*>(src + (size_t)(row0 + r) * row_stride + c)) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * NTHR, r = i / VPR, c = i % VPR * PER;
+      if (i >= N) continue;
+      float* d = dst + r * (D + 4) + c;
       if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<uint4*>(d) = w;
+        *reinterpret_cast<uint4*>(d) = w[u];
       } else {
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+        const uint32_t x[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
 #pragma unroll
         for (int k = 0; k < 2; ++k)
           reinterpret_cast<float4*>(d)[k] = make_float4(__uint_as_float(x[2 * k] << 16), __uint_as_float(x[2 * k] & 0xffff0000u),
                                                         __uint_as_float(x[2 * k + 1] << 16), __uint_as_float(x[2 * k + 1] & 0xffff0000u));
       }
-    } else {
-#pragma unroll
-      for (int k = 0; k < PER / 4; ++k) reinterpret_cast<float4*>(d)[k] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
   }
 }
 
-// s[i][j] = sum_c X[row i][c] Y[tx + 16 j][c]
+// s[i][j] = sum_c X[row i][c] Y[tx + 16 j][c]; two channels per multiply-add
 template <int D, int RM>
 __device__ __forceinline__ void product_t(const float* X, const float* Y, int ty, int tx, float (&s)[RM][4]) {
+  uint64_t s2[RM][4];
 #pragma unroll
   for (int i = 0; i < RM; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+    for (int j = 0; j < 4; ++j) s2[i][j] = 0;
 #pragma unroll 4
   for (int c = 0; c < D; c += 4) {
-    float4 x[RM], y[4];
+    ulonglong2 x[RM], y[4];
 #pragma unroll
-    for (int i = 0; i < RM; ++i) x[i] = *reinterpret_cast<const float4*>(X + (ty * RM + i) * (D + 4) + c);
+    for (int i = 0; i < RM; ++i) x[i] = *reinterpret_cast<const ulonglong2*>(X + (ty * RM + i) * (D + 4) + c);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(Y + (tx + 16 * j) * (D + 4) + c);
+    for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const ulonglong2*>(Y + (tx + 16 * j) * (D + 4) + c);
 #pragma unroll
     for (int i = 0; i < RM; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        s[i][j] = fmaf(x[i].w, y[j].w, fmaf(x[i].z, y[j].z, fmaf(x[i].y, y[j].y, fmaf(x[i].x, y[j].x, s[i][j]))));
+      for (int j = 0; j < 4; ++j) s2[i][j] = tc::f2_fma(x[i].y, y[j].y, tc::f2_fma(x[i].x, y[j].x, s2[i][j]));
   }
+#pragma unroll
+  for (int i = 0; i < RM; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float lo, hi;
+      tc::f2_unpack(s2[i][j], lo, hi);
+      s[i][j] = lo + hi;
+    }
 }
 
 // acc[i][:] += sum_r P[row i][r] Y[r][this thread's channels]; `whole`: no weight of the tile has to be tested for zero
 template <int D, int RM>
 __device__ __forceinline__ void product_acc(const float* P, const float* Y, int ty, int tx, bool whole, float (&acc)[RM][D / 16]) {
   constexpr int NC = D / 16, VW = NC < 4 ? NC : 4;
-  auto step = [&](int r, auto test) {
-    float y[NC];
+  auto load_y = [&](int r, float (&y)[NC]) {
 #pragma unroll
     for (int c = 0; c < NC / VW; ++c)
 #pragma unroll
       for (int e = 0; e < VW; ++e) y[c * VW + e] = Y[r * (D + 4) + (tx + 16 * c) * VW + e];
-#pragma unroll
-    for (int i = 0; i < RM; ++i) {
-      const float w = P[(ty * RM + i) * (BN + 4) + r];
-      if (!decltype(test)::value || w != 0.f) {
-#pragma unroll
-        for (int c = 0; c < NC; ++c) acc[i][c] = fmaf(w, y[c], acc[i][c]);
-      }
-    }
   };
   if (whole) {
-#pragma unroll 4
-    for (int r = 0; r < BN; ++r) step(r, std::false_type{});
+#pragma unroll 2
+    for (int r0 = 0; r0 < BN; r0 += 4) {   // (four weights of a row with one load)
+      float4 w[RM];
+#pragma unroll
+      for (int i = 0; i < RM; ++i) w[i] = *reinterpret_cast<const float4*>(P + (ty * RM + i) * (BN + 4) + r0);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float y[NC];
+        load_y(r0 + u, y);
+#pragma unroll
+        for (int i = 0; i < RM; ++i) {
+          const float x = u == 0 ? w[i].x : u == 1 ? w[i].y : u == 2 ? w[i].z : w[i].w;
+          if constexpr (NC >= 2) {
+#pragma unroll
+            for (int c = 0; c < NC; c += 2)
+              tc::f2_unpack(tc::f2_fma(tc::f2_pack(x, x), tc::f2_pack(y[c], y[c + 1]), tc::f2_pack(acc[i][c], acc[i][c + 1])), acc[i][c], acc[i][c + 1]);
+          } else {
+            acc[i][0] = fmaf(x, y[0], acc[i][0]);
+          }
+        }
+      }
+    }
   } else {
 #pragma unroll 4
-    for (int r = 0; r < BN; ++r) step(r, std::true_type{});
+    for (int r = 0; r < BN; ++r) {
+      float y[NC];
+      load_y(r, y);
+#pragma unroll
+      for (int i = 0; i < RM; ++i) {
+        const float w = P[(ty * RM + i) * (BN + 4) + r];
+        if (w != 0.f) {
+#pragma unroll
+          for (int c = 0; c < NC; ++c) acc[i][c] = fmaf(w, y[c], acc[i][c]);
+        }
+      }
+    }
   }
 }
 
@@ -159,7 +197,7 @@ __device__ __forceinline__ void fwd_rows(const Args& a, float* sm, int b, int h,
   for (int i = 0; i < RM; ++i) iv[i] = t0 + ty * RM + i <= last ? interval(a.mask, b, t0 + ty * RM + i) : make_int2(0, 0);
 
   sync_rows<NTHR>();
-  load_rows<T, D, NTHR>(Q, q, qs, t0, t_end, BM);
+  load_rows<T, D, NTHR, BM>(Q, q, qs, t0, t_end);
   const int j_first = head.x > k_first ? head.x : k_first, j_last = tail.y < k_end ? tail.y : k_end;
   float m[RM], l[RM], acc[RM][NC];
 #pragma unroll
@@ -170,9 +208,9 @@ __device__ __forceinline__ void fwd_rows(const Args& a, float* sm, int b, int h,
     for (int c = 0; c < NC; ++c) acc[i][c] = 0.f;
   }
   for (int j0 = j_first; j0 < j_last; j0 += BN) {
-    sync_rows<NTHR>();
-    load_rows<T, D, NTHR>(K, k, ks, j0, a.mask.T_k, BN);
-    load_rows<T, D, NTHR>(V, v, ks, j0, a.mask.T_k, BN);
+    if (j0 > j_first) sync_rows<NTHR>();   // (the first tile comes with the block's own rows)
+    load_rows<T, D, NTHR, BN>(K, k, ks, j0, a.mask.T_k);
+    load_rows<T, D, NTHR, BN>(V, v, ks, j0, a.mask.T_k);
     sync_rows<NTHR>();
     const bool whole = last - t0 + 1 == BM && tail.x <= j0 && head.y >= j0 + BN && j0 + BN <= j_last;
     float s[RM][4];
@@ -245,8 +283,14 @@ __device__ __forceinline__ void dq_rows(const Args& a, float* sm, int b, int h, 
   for (int i = 0; i < RM; ++i) iv[i] = t0 + ty * RM + i <= last ? interval(a.mask, b, t0 + ty * RM + i) : make_int2(0, 0);
 
   sync_rows<NTHR>();
-  load_rows<T, D, NTHR>(Q, (const T*)a.q + qo, qs, t0, t_end, BM);
-  load_rows<T, D, NTHR>(O, (const T*)a.dO + qo, qs, t0, t_end, BM);
+  load_rows<T, D, NTHR, BM>(Q, (const T*)a.q + qo, qs, t0, t_end);
+  load_rows<T, D, NTHR, BM>(O, (const T*)a.dO + qo, qs, t0, t_end);
+  const int per = ((tail.y - head.x + BN - 1) / BN + parts - 1) / parts * BN;   // keys of a part
+  const int j_first = head.x + part * per, j_last = tail.y < j_first + per ? tail.y : j_first + per;
+  if (j_first < j_last) {   // (the first tile comes with the block's own rows)
+    load_rows<T, D, NTHR, BN>(K, (const T*)a.k + ko, ks, j_first, a.mask.T_k);
+    load_rows<T, D, NTHR, BN>(V, (const T*)a.v + ko, ks, j_first, a.mask.T_k);
+  }
   sync_rows<NTHR>();
   float lse2[RM], dsum[RM], acc[RM][NC];
 #pragma unroll
@@ -268,13 +312,13 @@ __device__ __forceinline__ void dq_rows(const Args& a, float* sm, int b, int h, 
 #pragma unroll
     for (int c = 0; c < NC; ++c) acc[i][c] = 0.f;
   }
-  const int per = ((tail.y - head.x + BN - 1) / BN + parts - 1) / parts * BN;   // keys of a part
-  const int j_first = head.x + part * per, j_last = tail.y < j_first + per ? tail.y : j_first + per;
   for (int j0 = j_first; j0 < j_last; j0 += BN) {
-    sync_rows<NTHR>();
-    load_rows<T, D, NTHR>(K, (const T*)a.k + ko, ks, j0, a.mask.T_k, BN);
-    load_rows<T, D, NTHR>(V, (const T*)a.v + ko, ks, j0, a.mask.T_k, BN);
-    sync_rows<NTHR>();
+    if (j0 > j_first) {
+      sync_rows<NTHR>();
+      load_rows<T, D, NTHR, BN>(K, (const T*)a.k + ko, ks, j0, a.mask.T_k);
+      load_rows<T, D, NTHR, BN>(V, (const T*)a.v + ko, ks, j0, a.mask.T_k);
+      sync_rows<NTHR>();
+    }
     const bool whole = last - t0 + 1 == BM && tail.x <= j0 && head.y >= j0 + BN && j0 + BN <= j_last;
     float s[RM][4], dp[RM][4];
     product_t<D, RM>(Q, K, ty, tx, s);
@@ -313,8 +357,8 @@ __device__ __forceinline__ void dkdv_rows(const Args& a, float* sm, int b, int g
   const size_t qs = (size_t)a.H * D, ks = (size_t)a.H_kv * D;
   const size_t ko = (size_t)b * a.mask.T_k * ks + (size_t)g * D;
   sync_rows<NTHR>();
-  load_rows<T, D, NTHR>(K, (const T*)a.k + ko, ks, j0, j_end, BM);
-  load_rows<T, D, NTHR>(V, (const T*)a.v + ko, ks, j0, j_end, BM);
+  load_rows<T, D, NTHR, BM>(K, (const T*)a.k + ko, ks, j0, j_end);
+  load_rows<T, D, NTHR, BM>(V, (const T*)a.v + ko, ks, j0, j_end);
   const int j1 = j0 + BM < j_end ? j0 + BM : j_end;
   const int2 qr = queries_of(a.mask, b, j0, j1);
   float dk[RM][NC], dv[RM][NC];
@@ -328,9 +372,9 @@ __device__ __forceinline__ void dkdv_rows(const Args& a, float* sm, int b, int g
     const size_t qo = (size_t)b * a.mask.T * qs + (size_t)h * D;
     const float *nl = a.stat + ((size_t)b * a.H + h) * a.stat_stride, *nd = nl + (size_t)a.B * a.H * a.stat_stride;
     const float slope = a.slopes ? a.slopes[h] : 0.f;
-    sync_rows<NTHR>();
-    load_rows<T, D, NTHR>(Q, (const T*)a.q + qo, qs, t0, qr.y, BN);
-    load_rows<T, D, NTHR>(O, (const T*)a.dO + qo, qs, t0, qr.y, BN);
+    if (i > part * per) sync_rows<NTHR>();   // (the first tile comes with the block's own rows)
+    load_rows<T, D, NTHR, BN>(Q, (const T*)a.q + qo, qs, t0, qr.y);
+    load_rows<T, D, NTHR, BN>(O, (const T*)a.dO + qo, qs, t0, qr.y);
     sync_rows<NTHR>();
     bool whole = t0 + BN <= qr.y && j1 - j0 == BM;
     if (whole) whole = interval(a.mask, b, t0 + BN - 1).x <= j0 && interval(a.mask, b, t0).y >= j0 + BM;
