@@ -208,6 +208,7 @@ int lawcat_attn_bwd(const lawcat_attn_params* p, const int32_t* cu_seqlens, cons
   int2* const keys = (int2*)((char*)ws + rows_bytes(p));
   c.a.stat = (float*)((char*)keys + keys_bytes(p));
   c.a.stat_stride = stat_stride(p);
+  c.cu = cu_seqlens; c.prefix = prefix; c.nseq = nseq;
   if (cu_seqlens || prefix) {
     if ((r = fill_rows(p, cu_seqlens, prefix, nseq, c.a.mask, (int2*)ws, keys, c.stream))) return r;
   }

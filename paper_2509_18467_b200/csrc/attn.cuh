@@ -105,6 +105,8 @@ int grant_smem(size_t bytes) {
 // a call's arguments, its launchers and scratch
 struct AttnCall {
   attn::Args a;
+  const int32_t *cu, *prefix;  // HOST arrays of the documents (or null), read during the call alone
+  int nseq;
   int d, dtype, exact;
   cudaStream_t stream;
 };
