@@ -10,6 +10,7 @@
 // weighted values) meet in a second kernel. The number of parts follows from the capacity alone, so that a captured step may
 // be replayed at every length.
 #include "attn_decode.cuh"
+#include "attn_tc.cuh"
 
 namespace lawcat {
 namespace attn {
@@ -18,36 +19,72 @@ constexpr int TK = 64;       // keys per tile
 constexpr int HB = 8;        // query heads per block (one warp each)
 constexpr int DEC_THREADS = 32 * HB;
 
+__device__ __forceinline__ float min_nan(float x, float y) {  // (NaN where either is)
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float x, float y) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ float rcp_about(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
 // Eight channels of one row (c0 = 8 i), threads of a group side by side in a warp: codes as one word, parameters by the
-// group's first thread, and the values that they stand for in place of x.
-template <int D>
-__device__ __forceinline__ void quantize8(float (&x)[8], int c0, uint8_t* q_row, bf16* p_row, bool write) {
+// group's first thread, and the values that they stand for in place of x. `lanes`: the lanes that call it, whole groups.
+// bf16 rows (EXACT: the minimum is one of the values, so that all quotients lie in 0 ... 15) take quant_code's steps two values at a
+// time: t = 1.5 2^23 + k, whose last bits are k; |r| > scale / 2, or equal to it and k odd, is one comparison of 2 |r| (the bits of r,
+// shifted) plus k's last bit with scale's bits; and the word is sum_i 16^i t_i less what the 1.5 2^23 add up to.
+template <int D, bool EXACT>
+__device__ __forceinline__ void quantize8(float (&x)[8], int c0, uint8_t* q_row, bf16* p_row, bool write, unsigned lanes) {
   constexpr int GS = quant_group(D), TPG = GS / 8;
   float lo = x[0], hi = x[0];
-  bool fin = true;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    lo = fminf(lo, x[i]);
-    hi = fmaxf(hi, x[i]);
-    fin = fin && isfinite(x[i]);
+  for (int i = 1; i < 8; ++i) {
+    lo = min_nan(lo, x[i]);
+    hi = max_nan(hi, x[i]);
   }
-  const unsigned lanes = ((1u << TPG) - 1) << (threadIdx.x & 31 & ~(TPG - 1));  // the group's threads
 #pragma unroll
   for (int o = 1; o < TPG; o <<= 1) {
-    lo = fminf(lo, __shfl_xor_sync(lanes, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(lanes, hi, o));
-    fin = __shfl_xor_sync(lanes, (int)fin, o) && fin;
+    lo = min_nan(lo, __shfl_xor_sync(lanes, lo, o));
+    hi = max_nan(hi, __shfl_xor_sync(lanes, hi, o));
   }
   float scale, low;
-  quant_params(lo, hi, fin, scale, low);
-  const float inv = __frcp_rn(scale);
+  quant_params(lo, hi, isfinite(lo) && isfinite(hi), scale, low);
   uint32_t w = 0;
+  if (EXACT && scale > 1e-30f) {
+    constexpr uint32_t ONE_HALF = 0x4B400000u;   // 1.5 2^23
+    const float inv = rcp_about(scale), big = __uint_as_float(ONE_HALF);
+    const uint32_t twice_half = 2u * __float_as_uint(0.5f * scale);
+    const uint64_t nlow2 = f2_pack(-low, -low), inv2 = f2_pack(inv, inv), ns2 = f2_pack(-scale, -scale), big2 = f2_pack(big, big), nbig2 = f2_pack(-big, -big);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float code = quant_code(x[i], scale, low, inv);
-    w |= code_bits(code) << (4 * i);
-    x[i] = fmaf(code, scale, low);
+    for (int i = 6; i >= 0; i -= 2) {
+      const uint64_t d = f2_add(f2_pack(x[i], x[i + 1]), nlow2), t = f2_fma(d, inv2, big2), r = f2_fma(f2_add(t, nbig2), ns2, d);
+      float t0, t1, r0, r1;
+      f2_unpack(t, t0, t1);
+      f2_unpack(r, r0, r1);
+      auto code = [&](float tf, float rf) {
+        uint32_t k = __float_as_uint(tf);
+        const uint32_t e = __float_as_uint(rf);
+        if (2u * e + (k & 1u) > twice_half) k += (uint32_t)((int)e >> 31 | 1);
+        return k;
+      };
+      w = 16u * w + code(t1, r1);
+      w = 16u * w + code(t0, r0);
+    }
+    w -= ONE_HALF + 16u * ONE_HALF + 256u * ONE_HALF;   // (the others have left the word)
+  } else {
+    const float inv = __frcp_rn(scale);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w |= code_bits(quant_code(x[i], scale, low, inv)) << (4 * i);
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = fmaf((float)(w >> (4 * i) & 15u), scale, low);
   if (write) {
     *reinterpret_cast<uint32_t*>(q_row + c0 / 2) = w;
     if (c0 % GS == 0)
@@ -56,20 +93,34 @@ __device__ __forceinline__ void quantize8(float (&x)[8], int c0, uint8_t* q_row,
 }
 
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
-  if constexpr (sizeof(T) == 4) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  } else {
-    const uint4 w = *reinterpret_cast<const uint4*>(p);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+struct Raw8 {   // eight channels as they are stored
+  uint4 u[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ Raw8<T> raw8(const T* p) {
+  Raw8<T> r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(u[i] << 16);
-      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.u[i] = reinterpret_cast<const uint4*>(p)[i];
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void widen8(const Raw8<T>& r, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+    const uint32_t u[4] = {r.u[i].x, r.u[i].y, r.u[i].z, r.u[i].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (sizeof(T) == 4) {
+        x[4 * i + j] = __uint_as_float(u[j]);
+      } else {
+        x[2 * j] = bf16_lo(u[j]);
+        x[2 * j + 1] = bf16_hi(u[j]);
+      }
     }
   }
 }
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&x)[8]) { widen8(raw8(p), x); }
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
   if constexpr (sizeof(T) == 4) {
@@ -85,13 +136,22 @@ __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
+// eight codes and the group's (scale, minimum)
+struct Codes8 {
+  uint32_t w;
+  __nv_bfloat162 p;
+};
 template <int D>
-__device__ __forceinline__ void load8q(const uint8_t* q_row, const bf16* p_row, int c0, float (&x)[8]) {
-  const uint32_t w = *reinterpret_cast<const uint32_t*>(q_row + c0 / 2);
-  const __nv_bfloat162 p = reinterpret_cast<const __nv_bfloat162*>(p_row)[c0 / quant_group(D)];
-  const float scale = __bfloat162float(p.x), low = __bfloat162float(p.y);
+__device__ __forceinline__ Codes8 codes8(const uint8_t* q_row, const bf16* p_row, int c0) {
+  return Codes8{*reinterpret_cast<const uint32_t*>(q_row + c0 / 2), reinterpret_cast<const __nv_bfloat162*>(p_row)[c0 / quant_group(D)]};
+}
+__device__ __forceinline__ void widen8(const Codes8& r, float (&x)[8]) {
+  const float scale = __bfloat162float(r.p.x), low = __bfloat162float(r.p.y);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = fmaf((float)(w >> (4 * i) & 15u), scale, low);
+  for (int i = 0; i < 8; i += 2) {   // (2^23 + code: the code in the last bits; both steps to the code are exact)
+    const uint64_t c = f2_pack(__uint_as_float((r.w >> (4 * i) & 15u) | 0x4B000000u), __uint_as_float((r.w >> (4 * i + 4) & 15u) | 0x4B000000u));
+    f2_unpack(f2_fma(f2_add(c, f2_pack(-8388608.f, -8388608.f)), f2_pack(scale, scale), f2_pack(low, low)), x[i], x[i + 1]);
+  }
 }
 
 // T: storage type of the step's own tensors; QUANT: the cache holds 4-bit codes
@@ -131,13 +191,15 @@ __global__ void __launch_bounds__(DEC_THREADS) attn_decode_kernel(const DecArgs 
           const size_t row = ((size_t)b * a.H_kv + g) * a.C + slot;
           constexpr int NG = D / quant_group(D);
           if (fresh) {
+            constexpr int TPG = quant_group(D) / 8;
+            const unsigned lanes = ((1u << TPG) - 1) << (lane & ~(TPG - 1));   // (the row's other groups may lie in another warp)
             load8(k_t + c0, x);
             load8(v_t + c0, y);
-            quantize8<D>(x, c0, a.kq + row * (D / 2), a.kp + row * (2 * NG), hg == 0);
-            quantize8<D>(y, c0, a.vq + row * (D / 2), a.vp + row * (2 * NG), hg == 0);
+            quantize8<D, sizeof(T) == 2>(x, c0, a.kq + row * (D / 2), a.kp + row * (2 * NG), hg == 0, lanes);
+            quantize8<D, sizeof(T) == 2>(y, c0, a.vq + row * (D / 2), a.vp + row * (2 * NG), hg == 0, lanes);
           } else {
-            load8q<D>(a.kq + row * (D / 2), a.kp + row * (2 * NG), c0, x);
-            load8q<D>(a.vq + row * (D / 2), a.vp + row * (2 * NG), c0, y);
+            widen8(codes8<D>(a.kq + row * (D / 2), a.kp + row * (2 * NG), c0), x);
+            widen8(codes8<D>(a.vq + row * (D / 2), a.vp + row * (2 * NG), c0), y);
           }
         } else {
           const size_t row = (((size_t)b * a.C + slot) * a.H_kv + g) * D + c0;
@@ -256,45 +318,45 @@ struct QuantArgs {
   const int* pos;
   uint8_t *kq, *vq;
   bf16 *kp, *vp;
-  int T, H_kv, C, chunks;
+  int T, H_kv, C;
+  FastDiv slots, chunks, heads;   // C, a head's blocks, H_kv
 };
 constexpr int QUANT_ROWS = 4;   // rows of a thread
 __host__ __device__ constexpr int quant_tokens(int d) { return QUANT_ROWS * 256 / (d / 8); }
 template <typename T, int D, bool WRITE>
 __global__ void __launch_bounds__(256) attn_quant_kernel(const QuantArgs a) {
-  constexpr int V8 = D / 8, NG = D / quant_group(D), ROWS = 256 / V8;
-  const int bg = blockIdx.x / a.chunks, t0 = (int)(blockIdx.x - bg * a.chunks) * quant_tokens(D), b = bg / a.H_kv, g = bg - b * a.H_kv;
-  const int c0 = threadIdx.x % V8 * 8;
+  constexpr int V8 = D / 8, NG = D / quant_group(D), ROWS = 256 / V8, N = QUANT_ROWS;
+  const int bg = quot(blockIdx.x, a.chunks), b = quot(bg, a.heads), g = rest(bg, b, a.heads);
+  const int t0 = rest(blockIdx.x, bg, a.chunks) * quant_tokens(D) + (int)threadIdx.x / V8, c0 = threadIdx.x % V8 * 8;
   const bool is_v = blockIdx.y;
-  const int p0 = a.pos[b], first = p0 < 0 ? 0 : p0 % a.C;
+  const int p0 = a.pos[b], first = p0 < 0 ? 0 : rest(p0, quot(p0, a.slots), a.slots);
   T* const rows = (T*)(is_v ? a.v : a.k) + (((size_t)b * a.T) * a.H_kv + g) * D + c0;
   uint8_t* const q = is_v ? a.vq : a.kq;
   bf16* const p = is_v ? a.vp : a.kp;
-  constexpr int N = QUANT_ROWS;
-  auto token = [&](int i) { return t0 + i * ROWS + (int)threadIdx.x / V8; };
-  auto slot_of = [&](int t) {
-    int slot = first + t % a.C;
-    if (slot >= a.C) slot -= a.C;
-    return (size_t)bg * a.C + slot;
-  };
-  float x[N][8];
+  auto slot_of = [&](int t) { return (size_t)bg * a.C + rest(first + t, quot(first + t, a.slots), a.slots); };
+  std::conditional_t<WRITE, Raw8<T>, Codes8> raw[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {   // (all loads first)
-    const int t = token(i);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
-    if (t >= a.T || p0 < 0) continue;
-    if (WRITE) load8(rows + (size_t)t * a.H_kv * D, x[i]);
-    else load8q<D>(q + slot_of(t) * (D / 2), p + slot_of(t) * (2 * NG), c0, x[i]);
+    const int t = t0 + i * ROWS;
+    raw[i] = {};
+    if (t >= a.T) continue;
+    if constexpr (WRITE) {
+      raw[i] = raw8(rows + (size_t)t * a.H_kv * D);
+    } else if (p0 >= 0) {         // (zeros for a sequence that is not there)
+      const size_t at = slot_of(t);
+      raw[i] = codes8<D>(q + at * (D / 2), p + at * (2 * NG), c0);
+    }
   }
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int t = token(i);
-    if (WRITE) {   // (of more rows than slots the last stay)
+    const int t = t0 + i * ROWS;
+    float x[8];
+    widen8(raw[i], x);
+    if constexpr (WRITE) {   // (of more rows than slots the last stay)
       const size_t at = slot_of(min(t, a.T - 1));
-      quantize8<D>(x[i], c0, q + at * (D / 2), p + at * (2 * NG), t < a.T && t >= a.T - a.C && p0 >= 0);
+      quantize8<D, sizeof(T) == 2>(x, c0, q + at * (D / 2), p + at * (2 * NG), t < a.T && t >= a.T - a.C && p0 >= 0, 0xffffffffu);
     } else if (t < a.T) {
-      store8(rows + (size_t)t * a.H_kv * D, x[i]);   // (zeros for a sequence that is not there)
+      store8(rows + (size_t)t * a.H_kv * D, x);
     }
   }
 }
@@ -373,8 +435,8 @@ int launch_attn_decode(const AttnDecode& c) {
 
 int launch_attn_quant(const AttnDecode& c, int T, bool write) {
   attn::QuantArgs a{const_cast<void*>(c.k_t), const_cast<void*>(c.v_t), c.pos, (uint8_t*)c.kq, (uint8_t*)c.vq, (bf16*)c.kp, (bf16*)c.vp,
-                    T, c.H_kv, c.C, (T + attn::quant_tokens(c.d) - 1) / attn::quant_tokens(c.d)};
-  const unsigned long long n = (unsigned long long)c.B * c.H_kv * a.chunks;
+                    T, c.H_kv, c.C, attn::fast_div(c.C), attn::fast_div((T + attn::quant_tokens(c.d) - 1) / attn::quant_tokens(c.d)), attn::fast_div(c.H_kv)};
+  const unsigned long long n = (unsigned long long)c.B * c.H_kv * a.chunks.d;
   if (n > 0x7fffffffULL) return LAWCAT_ERR_UNSUPPORTED;
   return by_width(c.d, [&](auto dd) {
     constexpr int D = decltype(dd)::value;
