@@ -12,6 +12,10 @@
 // tiles took 3300 cycles; tensor memory holds no second place of 128 columns beside two O of 128).
 // The accumulator O_i is rescaled only when a row's maximum has grown by more than 2^8 since it was last scaled (the weights then
 // stay within 2^8 in fp32 and bf16 alike), by the softmax warps themselves, behind the product of the tile in front.
+// With distance biases the keys are walked from the last tile to the first: the largest weights come first, and the maximum hardly grows
+// again (walked upwards, a head with a slope above 1/8 rescaled O in every tile: 8192 causal tokens, 32/8 heads of 64 and of 128, 563 and
+// 645 us; now 425 and 460, without biases 389 and 445). On one side of the query a bias is linear in the key, so that it is one addition
+// per pair of scores, with a bound in place of the maximum.
 // The products of the two tiles are issued in turn (S_0, O_0, S_1, O_1), which keeps the warpgroups half a step apart: weighing in
 // step, they meet at the pipe of the special functions and leave it idle together. (Taking a quarter, three eighths or half of the
 // exponentials as polynomials on the FMA pipe made it slower, 440 us at 8192 tokens and 32/8 heads of 128 against 457, 479 and 487.)
@@ -185,7 +189,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             if (at >= L::ST) ok = wait_bar(bar(L::B_EMPTY + s), (at / L::ST - 1) & 1, s_abort, f.limit);
             if (!ok) break;
             mbar_arrive_expect_tx(bar(L::B_FULL + s), L::KT);
-            load_tile<D, 64>(sb + L::OFF_RING + s * L::KT, it & 1 ? &tm_v : &tm_k, bar(L::B_FULL + s), w.g, w.j_first + it / 2 * 64, w.b);
+            load_tile<D, 64>(sb + L::OFF_RING + s * L::KT, it & 1 ? &tm_v : &tm_k, bar(L::B_FULL + s), w.g, w.j_first + (BIAS ? w.n - 1 - it / 2 : it / 2) * 64, w.b);
           }
           ++seq;
         }
@@ -291,6 +295,9 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       const int n = w.n, h = head_of(w, i), t = row_of(w, i) + (tid & 127);
       const int2 iv = interval(a.mask, w.b, min(t, T - 1));   // (rows behind the last are never stored)
       const float slope2 = BIAS && a.slopes ? a.slopes[h] * LOG2E : 0.f;
+      // (the maximum is then up to 15 slopes too large, 2^30, and 2^40 more ahead of the query: far from the 2^126 that fp32 has below
+      // one; and the largest score has to be the largest exponent)
+      const bool linear = (CAP || scale2 > 0.f) && fabsf(slope2) < 2.f;
       // what the warp's rows see in all: [lo0, hi1), of which every row sees [lo1, hi0)
       int lo0 = 0, lo1 = 0, hi0 = 0, hi1 = 0;
       float m = -INFINITY, l = 0.f;
@@ -304,7 +311,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           hi0 = __shfl_sync(0xffffffffu, iv.y, 0);
           hi1 = __shfl_sync(0xffffffffu, iv.y, 31);
         }
-        const int j0 = w.j_first + it * 64;
+        const int j0 = w.j_first + (BIAS ? n - 1 - it : it) * 64;
         const uint32_t S = s_col(i, step) + lanes;
         float s[64];
         // halves of the tile that no row of the warp sees take no part: their weights are zero
@@ -314,25 +321,29 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         tmem_wait_ld();
         const bool low = lo1 > j0, high = hi0 < j0 + 64, whole = !low && !high;   // (the same for the warp)
         if constexpr (CAP) cap_scores(s, a.scale * inv_cap, a.cap * LOG2E);
+        // The exponent of column c is by s[c] + bias + slope c where all keys lie on one side (`slope` 0 without biases, and where they
+        // have been taken into s).
+        float by = CAP ? 1.f : scale2, bias = 0.f, slope = 0.f;
         if constexpr (BIAS) {
-          const float by = CAP ? 1.f : scale2, dist0 = (float)(t + a.mask.off - j0);
-          if (__all_sync(0xffffffffu, dist0 >= 63.f)) {   // (all keys lie behind: the distance is linear in the column)
-            const float base = -slope2 * dist0;
-#pragma unroll
-            for (int c = 0; c < 64; ++c) s[c] = fmaf(s[c], by, fmaf(slope2, (float)c, base));
+          const float dist0 = (float)(t + a.mask.off - j0);
+          const bool behind = __all_sync(0xffffffffu, dist0 >= 63.f);
+          if (linear && (behind || __all_sync(0xffffffffu, dist0 <= 0.f))) {
+            slope = behind ? slope2 : -slope2;
+            bias = -slope * dist0;
           } else {
 #pragma unroll
             for (int c = 0; c < 64; ++c) s[c] = fmaf(s[c], by, -slope2 * fabsf(dist0 - (float)c));
+            by = 1.f;
           }
         }
-        float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+        float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;   // of 16 columns each
         if (whole) {
 #pragma unroll
-          for (int c = 0; c < 64; c += 8) {
+          for (int c = 0; c < 16; c += 2) {
             mx0 = fmaxf(fmaxf(mx0, s[c]), s[c + 1]);
-            mx1 = fmaxf(fmaxf(mx1, s[c + 2]), s[c + 3]);
-            mx2 = fmaxf(fmaxf(mx2, s[c + 4]), s[c + 5]);
-            mx3 = fmaxf(fmaxf(mx3, s[c + 6]), s[c + 7]);
+            mx1 = fmaxf(fmaxf(mx1, s[c + 16]), s[c + 17]);
+            mx2 = fmaxf(fmaxf(mx2, s[c + 32]), s[c + 33]);
+            mx3 = fmaxf(fmaxf(mx3, s[c + 48]), s[c + 49]);
           }
         } else {
           const int rl = iv.x - j0, rh = iv.y - j0;
@@ -346,16 +357,24 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll
               for (int c = c0; c < c0 + 32; ++c) s[c] = c >= rh ? -INFINITY : s[c];
 #pragma unroll
-            for (int c = c0; c < c0 + 32; c += 4) {
-              mx0 = fmaxf(fmaxf(mx0, s[c]), s[c + 1]);
-              mx1 = fmaxf(fmaxf(mx1, s[c + 2]), s[c + 3]);
+            for (int c = c0; c < c0 + 16; c += 2) {
+              float &x = c0 ? mx2 : mx0, &y = c0 ? mx3 : mx1;
+              x = fmaxf(fmaxf(x, s[c]), s[c + 1]);
+              y = fmaxf(fmaxf(y, s[c + 16]), s[c + 17]);
             }
           }
         }
-        float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
-        if constexpr (!CAP && !BIAS) mx *= scale2;
+        float mx;
+        if constexpr (BIAS) {   // (not the largest exponent itself but at most 15 slopes above it: the weights' common factor is free)
+          mx = fmaxf(fmaxf(fmaf(mx0, by, 0.f), fmaf(mx1, by, 16.f * slope)), fmaxf(fmaf(mx2, by, 32.f * slope), fmaf(mx3, by, 48.f * slope)));
+          mx += bias + fmaxf(15.f * slope, 0.f);
+        } else {
+          mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * by;
+        }
         const bool grow = mx > m + RESCALE || (m == -INFINITY && mx > m);
         if (__any_sync(0xffffffffu, grow)) {
+          // (ahead of the query, the biases grow from here to its own key: that is taken into account once)
+          if constexpr (BIAS) mx += fminf(fmaxf(slope2 * (float)(j0 - max(t + a.mask.off, iv.x)), 0.f), 40.f);
           const float base = grow ? mx : m, factor = m == -INFINITY ? 0.f : ex2f(m - base);
           if (it > 0) {
             ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_O + 2 * i + (step - 1 & 1)), (step - 1) >> 1 & 1, s_abort, f.limit));   // (the product in front)
@@ -376,15 +395,21 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           m = base;
         }
         const float base = m == -INFINITY ? 0.f : m;
-        const uint64_t sc = f2_pack(CAP || BIAS ? 1.f : scale2, CAP || BIAS ? 1.f : scale2), nb = f2_pack(-base, -base);
+        const uint64_t sc = f2_pack(by, by), nb = f2_pack(bias - base, bias - base);
         uint64_t sum0 = 0, sum1 = 0;
         auto weigh = [&](auto first) {   // 32 scores from column `first` on: the weights, two to a register, in their place
           constexpr int c = decltype(first)::value;
+          uint64_t add = nb;
+          if constexpr (BIAS) add = f2_pack(fmaf(slope, (float)c, bias - base), fmaf(slope, (float)(c + 1), bias - base));
+          const uint64_t slope_2 = f2_pack(2.f * slope, 2.f * slope);
 #pragma unroll
           for (int q = 0; q < 16; q += 8) {   // (step by step over eight pairs: what one warp has in flight is all that hides latencies)
             uint64_t z[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = f2_fma(f2_pack(s[c + 2 * (q + e)], s[c + 2 * (q + e) + 1]), sc, nb);
+            for (int e = 0; e < 8; ++e) {
+              z[e] = f2_fma(f2_pack(s[c + 2 * (q + e)], s[c + 2 * (q + e) + 1]), sc, add);
+              if constexpr (BIAS) add = f2_add(add, slope_2);
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               float u, v;

@@ -91,15 +91,16 @@ def attention(q, k, v, see, scale, cap=0.0, slopes=None, dO=None, stored_o=None)
     return r
 
 
-def check(got, want, err, out_eps, what):
-    """|got - want| <= err + out_eps |want|, element by element (out_eps: the result's own rounding)."""
+def check(got, want, err, out_eps, what, tiny=1e-37):
+    """|got - want| <= err + out_eps |want| + tiny, element by element (out_eps: the result's own rounding; tiny: what is lost below
+    fp32's least normal number)."""
     got, want = got.double(), want.to(got.device)
     assert got.shape == want.shape, (what, got.shape, want.shape)
     fin = torch.isfinite(want)
     assert torch.equal(got[~fin], want[~fin]), f"{what}: {int((got[~fin] != want[~fin]).sum())} values that are not finite differ"
     if not fin.any():
         return
-    tol = (err.to(got.device).expand_as(want) + out_eps * want.abs() * 1.0001 + 1e-37)[fin]
+    tol = (err.to(got.device).expand_as(want) + out_eps * want.abs() * 1.0001 + tiny)[fin]
     over = (got - want)[fin].abs() / tol
     assert torch.isfinite(got[fin]).all(), f"{what}: values that are not finite"
     assert float(over.max()) <= 1.0, f"{what}: {float(over.max()):.3g} times the tolerance"

@@ -90,6 +90,34 @@ def test_other_number_of_keys(T, T_k, kw, dtype, exact):
         assert not r["dk"].any() and not r["dv"].any()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,exact", KINDS)
+@pytest.mark.parametrize("kw", [dict(), dict(causal=0), dict(causal=0, T_k=1100), dict(causal=0, T_k=150), dict(prefix=[0, 390, 200]), dict(causal=0, cap=7.0), dict(window=90)])
+def test_steep_biases(kw, dtype, exact):
+    """Slopes from far above one to below zero, keys on both sides, queries in front of the first key."""
+    steep_case(dtype, exact, **kw)
+
+
+def steep_case(dtype, exact, causal=1, T_k=None, prefix=None, cap=0.0, window=0):
+    B, T, H, H_kv, d = 3, 400, 6, 2, 64
+    T_k = T if T_k is None else T_k
+    q, k, v, dO = [draw((B, n, h, d), 60 + i, dtype, 1.5 if i == 0 else 1.0) for i, (n, h) in enumerate(((T, H), (T_k, H_kv), (T_k, H_kv), (T, H)))]
+    sl = torch.tensor([1.3, -0.4, 9.0, 0.84, 2.9, -1.2], device="cuda")
+    p = api.attn_params(B, T, H, H_kv, d, T_k=T_k, dtype=dtype, causal=causal, window=window, cap=cap, exact=exact)
+    r = api.lawcat_attn_fwd(p, q, k, v, slopes=sl, prefix=prefix)
+    r.update(api.lawcat_attn_bwd(p, q, k, v, r["o"], r["lse"], dO, slopes=sl, prefix=prefix))
+    ref = attention(q, k, v, visible(T, T_k, causal, window, None, prefix, B), float(torch.tensor(d ** -0.5)), cap, sl, dO, r["o"])
+    coarse, out = U16 if dtype == "bf16" and not exact else 0.0, U16 if dtype == "bf16" else U32
+    err = dict(ref["grad_err"](coarse, out), o=ref["o_sum"] + coarse * ref["o_mag"], lse=ref["lse_err"])
+    # A key far from every query has weights around fp32's least normal number 2^-126; one below it counts as zero, so that each of a key's
+    # T H / H_kv weights is off by 2^-126 at most. dv sums p dO; dk sums scale p (dP - D) q with |dP|, |D| <= d max|dO| max|v|.
+    top = [float(x.double().abs().max()) for x in (q, v, dO)]
+    lost = T * H // H_kv * 2.0 ** -126
+    tiny = dict(dv=lost * top[2], dk=lost * d ** -0.5 * 2 * d * top[2] * top[1] * top[0])
+    for n in ("o", "lse", "dq", "dk", "dv"):
+        check(r[n], ref[n], err[n], U32 if n == "lse" else out, n, 1e-37 + tiny.get(n, 0.0))
+
+
 DOCS = [
     ([0, 300], None), ([0, 1, 300], None), ([0, 0, 128, 128, 256, 300, 300], None), ([0, 63, 64, 65, 130, 299, 300], None),
     ([0, 100, 300], [100, 0]), ([0, 40, 41, 300], [13, 1, 200]), (list(range(0, 301)), None), (list(range(0, 301, 4)), [3] * 75),
@@ -113,6 +141,23 @@ def test_more_documents_than_one_table(dtype):
         cu.append(cu[-1] + (i * 7) % 4)
     case(T=cu[-1], H=2, H_kv=1, dtype=dtype, cu=cu, seed=9)
     case(T=cu[-1], H=2, H_kv=1, dtype=dtype, cu=[0, 500, cu[-1]], window=33, seed=10)
+
+
+@pytest.mark.gpu
+def test_more_tiles_of_documents_than_are_put_in_order():
+    """140400 packed tokens, 1097 tiles of keys: the first, the last and some other documents."""
+    n, T, d = 260, 540, 64
+    q, k, v, dO = [draw((1, n * T, h, d), i, "bf16") for i, h in enumerate((2, 1, 1, 2))]
+    p = api.attn_params(1, n * T, 2, 1, d)
+    cu = list(range(0, n * T + 1, T))
+    r = api.lawcat_attn_fwd(p, q, k, v, cu_seqlens=cu)
+    r.update(api.lawcat_attn_bwd(p, q, k, v, r["o"], r["lse"], dO, cu_seqlens=cu))
+    one = [0, 1, 130, 255, 256, 259]
+    part = lambda x: x.reshape(n, T, *x.shape[2:])[one]  # noqa: E731
+    ref = attention(part(q), part(k), part(v), visible(T, T, 1, 0, B=len(one)), float(torch.tensor(d ** -0.5)), 0.0, None, part(dO), part(r["o"]))
+    err = dict(ref["grad_err"](U16, U16), o=ref["o_sum"] + U16 * ref["o_mag"], lse=ref["lse_err"])
+    for x in ("o", "lse", "dq", "dk", "dv"):
+        check(part(r[x]), ref[x], err[x], U32 if x == "lse" else U16, x)
 
 
 @pytest.mark.gpu
