@@ -367,8 +367,12 @@ size_t lawcat_attn_workspace_bytes(const lawcat_attn_params* p, int op);
  *   prefix: NULL, or a HOST array of nseq ints (nseq = B without cu_seqlens): the first prefix[i] keys of sequence i are seen by
  *     every query of that sequence (causal = 1, no window).
  *   nseq is 0 when both are NULL. The arrays are read during the call; a captured call keeps their values.
- * fp32 accumulation, softmax statistics in fp32, one rounding of o.
- * A key or value row that a query does not see does not reach its results, not even as a NaN.
+ * fp32 accumulation, softmax statistics in fp32, one rounding of o. bf16 with d = 64 or 128 (and exact = 0) runs on the tensor cores:
+ * the weights are rounded to bf16 as an operand as well (in the backward the weights and their gradients). Everything else runs on
+ * the CUDA cores in fp32.
+ * A key or value row that a query does not see does not reach its results, not even as a NaN. (The tensor-core kernels compute
+ * a row that comes out not finite again on the CUDA cores, which takes its time where many do.)
+ * dev_status (nullable, device int) is set to LAWCAT_ERR_TIMEOUT when a kernel's internal wait runs out.
  */
 int lawcat_attn_fwd(const lawcat_attn_params* p, const int32_t* cu_seqlens, const int32_t* prefix, int32_t nseq, const void* q,
                     const void* k, const void* v, const float* slopes, void* o, float* lse, void* ws, size_t ws_bytes, void* stream,

@@ -298,155 +298,155 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
     const float scale2 = a.scale * LOG2E, c2 = a.cap * LOG2E, nic2 = CAP ? -1.f / (c2 * c2) : 0.f;
     int base = 0, seq = 0;   // walked tiles and items with tiles so far
     for (int k = 0;; ++k) {
-    Item w;
-    w.n = -1;
-    bool ok = __all_sync(0xffffffffu, item_at(k, w));
-    if (!ok || w.n < 0) break;
-    if (lane == 0) item_read(k);
-    if (w.n == 0) continue;
-    const int n = w.n, r = w.r0 + r128;
-    // the columns that this row meets: the keys that the query sees, or the queries that see the key
-    const int2 iv = KV ? key_interval(a.mask, w.b, min(r, rows - 1)) : interval(a.mask, w.b, min(r, rows - 1));   // (rows behind the last are never stored)
-    int lo0 = 0, lo1 = 0, hi0 = 0, hi1 = 0;   // what the warp's rows meet in all: [lo0, hi1), every row: [lo1, hi0)
-    float nl = 0.f, nd = 0.f;   // -lse log2e and -dO.o of an own query
-    uint64_t dex = 0;           // sums of p dP
-    if (!KV) {
-      const float lse = r < rows ? a.lse[((size_t)w.b * a.mask.T + r) * a.H + w.own] : 0.f;
-      ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_A), seq & 1, s_abort, f.limit));
-      if (!ok) break;
-      const uint32_t row = sb + L::OFF_A + L::OWN + sw128(r128, 0);   // (chunk j of a row: its address with bits 4 ... 6 turned over by j)
-      float d0 = 0.f, d1 = 0.f;
+      Item w;
+      w.n = -1;
+      bool ok = __all_sync(0xffffffffu, item_at(k, w));
+      if (!ok || w.n < 0) break;
+      if (lane == 0) item_read(k);
+      if (w.n == 0) continue;
+      const int n = w.n, r = w.r0 + r128;
+      // the columns that this row meets: the keys that the query sees, or the queries that see the key
+      const int2 iv = KV ? key_interval(a.mask, w.b, min(r, rows - 1)) : interval(a.mask, w.b, min(r, rows - 1));   // (rows behind the last are never stored)
+      int lo0 = 0, lo1 = 0, hi0 = 0, hi1 = 0;   // what the warp's rows meet in all: [lo0, hi1), every row: [lo1, hi0)
+      float nl = 0.f, nd = 0.f;   // -lse log2e and -dO.o of an own query
+      uint64_t dex = 0;           // sums of p dP
+      if (!KV) {
+        const float lse = r < rows ? a.lse[((size_t)w.b * a.mask.T + r) * a.H + w.own] : 0.f;
+        ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_A), seq & 1, s_abort, f.limit));
+        if (!ok) break;
+        const uint32_t row = sb + L::OFF_A + L::OWN + sw128(r128, 0);   // (chunk j of a row: its address with bits 4 ... 6 turned over by j)
+        float d0 = 0.f, d1 = 0.f;
 #pragma unroll 4
-      for (int j = 0; j < D / 8; ++j) {
-        const uint32_t at = (row ^ (uint32_t)((j & 7) << 4)) + (j >> 3) * 16384;
-        const uint4 x = lds128(at), y = lds128(at + L::OWN);
-        d0 = fmaf(bf16_lo(x.x), bf16_lo(y.x), fmaf(bf16_lo(x.y), bf16_lo(y.y), d0));
-        d1 = fmaf(bf16_hi(x.x), bf16_hi(y.x), fmaf(bf16_hi(x.y), bf16_hi(y.y), d1));
-        d0 = fmaf(bf16_lo(x.z), bf16_lo(y.z), fmaf(bf16_lo(x.w), bf16_lo(y.w), d0));
-        d1 = fmaf(bf16_hi(x.z), bf16_hi(y.z), fmaf(bf16_hi(x.w), bf16_hi(y.w), d1));
+        for (int j = 0; j < D / 8; ++j) {
+          const uint32_t at = (row ^ (uint32_t)((j & 7) << 4)) + (j >> 3) * 16384;
+          const uint4 x = lds128(at), y = lds128(at + L::OWN);
+          d0 = fmaf(bf16_lo(x.x), bf16_lo(y.x), fmaf(bf16_lo(x.y), bf16_lo(y.y), d0));
+          d1 = fmaf(bf16_hi(x.x), bf16_hi(y.x), fmaf(bf16_hi(x.y), bf16_hi(y.y), d1));
+          d0 = fmaf(bf16_lo(x.z), bf16_lo(y.z), fmaf(bf16_lo(x.w), bf16_lo(y.w), d0));
+          d1 = fmaf(bf16_hi(x.z), bf16_hi(y.z), fmaf(bf16_hi(x.w), bf16_hi(y.w), d1));
+        }
+        mbar_arrive(bar(L::B_AE));
+        nd = -(d0 + d1);
+        nl = -lse * LOG2E;
+        if (wg == 0) {
+          float* const own = reinterpret_cast<float*>(smem + L::OFF_OWN) + (seq & 1) * 256;
+          own[r128] = nl;
+          own[128 + r128] = nd;
+        }
       }
-      mbar_arrive(bar(L::B_AE));
-      nd = -(d0 + d1);
-      nl = -lse * LOG2E;
-      if (wg == 0) {
-        float* const own = reinterpret_cast<float*>(smem + L::OFF_OWN) + (seq & 1) * 256;
-        own[r128] = nl;
-        own[128 + r128] = nd;
-      }
-    }
-    lo0 = __shfl_sync(0xffffffffu, iv.x, 0);
-    lo1 = __shfl_sync(0xffffffffu, iv.x, 31);
-    hi0 = __shfl_sync(0xffffffffu, iv.y, 0);
-    hi1 = __shfl_sync(0xffffffffu, iv.y, 31);
-    int h = KV ? w.own * G : w.own, col = (wg ^ base) & 1;   // of this group's next tile: the head, and its number within it
-    for (int it = col; it < n && ok; it += 2, col += 2) {
-      while (KV && col >= w.per) {
-        col -= w.per;
-        ++h;
-      }
-      const int step = base + it;
-      ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_S + wg), (step >> 1) & 1, s_abort, f.limit));
-      if (!ok) break;
-      tc_fence_after_sync();
-      const int c0 = w.w0 + col * 64, st = step % L::ST;
-      const float4* stat = reinterpret_cast<const float4*>(smem + L::OFF_STAT + st * L::STAT);
-      const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f;
-      if (KV) mbar_wait(bar(L::B_FULL + st), (step / L::ST) & 1);   // (complete by now; makes the copied statistics visible here)
-      const uint64_t sc = f2_pack(CAP ? 1.f : scale2, CAP ? 1.f : scale2), one = f2_pack(1.f, 1.f), nic = f2_pack(nic2, nic2);
-      // weights and their gradients over the scores, as bf16 pairs; `some`: not every column is met, or not all lie on one side
+      lo0 = __shfl_sync(0xffffffffu, iv.x, 0);
+      lo1 = __shfl_sync(0xffffffffu, iv.x, 31);
+      hi0 = __shfl_sync(0xffffffffu, iv.y, 0);
+      hi1 = __shfl_sync(0xffffffffu, iv.y, 31);
+      int h = KV ? w.own * G : w.own, col = (wg ^ base) & 1;   // of this group's next tile: the head, and its number within it
+      for (int it = col; it < n && ok; it += 2, col += 2) {
+        while (KV && col >= w.per) {
+          col -= w.per;
+          ++h;
+        }
+        const int step = base + it;
+        ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_S + wg), (step >> 1) & 1, s_abort, f.limit));
+        if (!ok) break;
+        tc_fence_after_sync();
+        const int c0 = w.w0 + col * 64, st = step % L::ST;
+        const float4* stat = reinterpret_cast<const float4*>(smem + L::OFF_STAT + st * L::STAT);
+        const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.f;
+        if (KV) mbar_wait(bar(L::B_FULL + st), (step / L::ST) & 1);   // (complete by now; makes the copied statistics visible here)
+        const uint64_t sc = f2_pack(CAP ? 1.f : scale2, CAP ? 1.f : scale2), one = f2_pack(1.f, 1.f), nic = f2_pack(nic2, nic2);
+        // weights and their gradients over the scores, as bf16 pairs; `some`: not every column is met, or not all lie on one side
 #pragma unroll 1
-      for (int hf = 0; hf < 2; ++hf) {   // 32 columns at a time: what a thread holds of them has to fit beside the other warps' registers
-      const int c1 = c0 + hf * 32;
-      if (c1 >= hi1 || c1 + 32 <= lo0) {   // (no row of the warp meets them)
-        float z[16];
+        for (int hf = 0; hf < 2; ++hf) {   // 32 columns at a time: what a thread holds of them has to fit beside the other warps' registers
+          const int c1 = c0 + hf * 32;
+          if (c1 >= hi1 || c1 + 32 <= lo0) {   // (no row of the warp meets them)
+            float z[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) z[e] = 0.f;
-        tmem_st16(S + hf * 16, z);
-        tmem_st16(P + hf * 16, z);
-        continue;
-      }
-      float s[32], p[32];
-      tmem_ld32(S + hf * 32, s);
-      tmem_ld32(P + hf * 32, p);
-      tmem_wait_ld();
-      if (CAP) cap_scores(s, a.scale / a.cap, c2);
-      // |i - j| = |dist0 - c|
-      const float dist0 = (float)(KV ? r - c1 - a.mask.off : r + a.mask.off - c1);
-      const float slope_c = KV ? -slope2 : slope2, bias0 = -slope_c * dist0;   // (on one side: the bias is bias0 + slope_c c)
-      auto weigh = [&](auto some) {
-        const int rel = iv.x - c1;
-        const uint32_t len = (uint32_t)(iv.y - iv.x);
-#pragma unroll
-        for (int q = 0; q < 32; q += 4) {
-          float4 l4 = make_float4(nl, nl, nl, nl), d4 = make_float4(nd, nd, nd, nd);
-          if (KV) {
-            l4 = stat[hf * 8 + q / 4];
-            d4 = stat[16 + hf * 8 + q / 4];
+            for (int e = 0; e < 16; ++e) z[e] = 0.f;
+            tmem_st16(S + hf * 16, z);
+            tmem_st16(P + hf * 16, z);
+            continue;
           }
+          float s[32], p[32];
+          tmem_ld32(S + hf * 32, s);
+          tmem_ld32(P + hf * 32, p);
+          tmem_wait_ld();
+          if (CAP) cap_scores(s, a.scale / a.cap, c2);
+          // |i - j| = |dist0 - c|
+          const float dist0 = (float)(KV ? r - c1 - a.mask.off : r + a.mask.off - c1);
+          const float slope_c = KV ? -slope2 : slope2, bias0 = -slope_c * dist0;   // (on one side: the bias is bias0 + slope_c c)
+          auto weigh = [&](auto some) {
+            const int rel = iv.x - c1;
+            const uint32_t len = (uint32_t)(iv.y - iv.x);
 #pragma unroll
-          for (int e = 0; e < 4; e += 2) {
-            const int c = q + e;
-            const uint64_t x = f2_pack(s[c], s[c + 1]), l = e ? f2_pack(l4.z, l4.w) : f2_pack(l4.x, l4.y), d = e ? f2_pack(d4.z, d4.w) : f2_pack(d4.x, d4.y);
-            uint64_t add = l, fac = one;
-            if (BIAS) {
-              float b0, b1;
-              if (decltype(some)::value) {
-                f2_unpack(l, b0, b1);
-                b0 = fmaf(-slope2, fabsf(dist0 - (float)c), b0);
-                b1 = fmaf(-slope2, fabsf(dist0 - (float)(c + 1)), b1);
-                add = f2_pack(b0, b1);
-              } else {
-                add = f2_add(l, f2_pack(fmaf(slope_c, (float)c, bias0), fmaf(slope_c, (float)(c + 1), bias0)));
+            for (int q = 0; q < 32; q += 4) {
+              float4 l4 = make_float4(nl, nl, nl, nl), d4 = make_float4(nd, nd, nd, nd);
+              if (KV) {
+                l4 = stat[hf * 8 + q / 4];
+                d4 = stat[16 + hf * 8 + q / 4];
+              }
+#pragma unroll
+              for (int e = 0; e < 4; e += 2) {
+                const int c = q + e;
+                const uint64_t x = f2_pack(s[c], s[c + 1]), l = e ? f2_pack(l4.z, l4.w) : f2_pack(l4.x, l4.y), d = e ? f2_pack(d4.z, d4.w) : f2_pack(d4.x, d4.y);
+                uint64_t add = l, fac = one;
+                if (BIAS) {
+                  float b0, b1;
+                  if (decltype(some)::value) {
+                    f2_unpack(l, b0, b1);
+                    b0 = fmaf(-slope2, fabsf(dist0 - (float)c), b0);
+                    b1 = fmaf(-slope2, fabsf(dist0 - (float)(c + 1)), b1);
+                    add = f2_pack(b0, b1);
+                  } else {
+                    add = f2_add(l, f2_pack(fmaf(slope_c, (float)c, bias0), fmaf(slope_c, (float)(c + 1), bias0)));
+                  }
+                }
+                const uint64_t y = f2_fma(x, sc, add);
+                if (CAP) fac = f2_fma(f2_mul(x, x), nic, one);   // 1 - tanh^2
+                float p0, p1;
+                f2_unpack(y, p0, p1);
+                p0 = ex2f(p0);
+                p1 = ex2f(p1);
+                float g0 = p[c], g1 = p[c + 1], f0 = 1.f, f1 = 1.f;
+                if (CAP) f2_unpack(fac, f0, f1);
+                if (decltype(some)::value) {
+                  const bool v0 = (uint32_t)(c - rel) < len, v1 = (uint32_t)(c + 1 - rel) < len;
+                  p0 = v0 ? p0 : 0.f;
+                  g0 = v0 ? g0 : 0.f;
+                  f0 = v0 ? f0 : 0.f;
+                  p1 = v1 ? p1 : 0.f;
+                  g1 = v1 ? g1 : 0.f;
+                  f1 = v1 ? f1 : 0.f;
+                }
+                const uint64_t pp = f2_pack(p0, p1), gg = f2_pack(g0, g1);
+                if (!KV) dex = f2_fma(pp, gg, dex);
+                const uint64_t pf = CAP ? f2_mul(pp, f2_pack(f0, f1)) : pp;
+                const uint64_t dx = f2_mul(pf, f2_add(gg, d));
+                float y0, y1;
+                f2_unpack(KV ? pp : pf, y0, y1);
+                s[c / 2] = __uint_as_float(pack_bf16(y0, y1));
+                f2_unpack(dx, y0, y1);
+                p[c / 2] = __uint_as_float(pack_bf16(y0, y1));
               }
             }
-            const uint64_t y = f2_fma(x, sc, add);
-            if (CAP) fac = f2_fma(f2_mul(x, x), nic, one);   // 1 - tanh^2
-            float p0, p1;
-            f2_unpack(y, p0, p1);
-            p0 = ex2f(p0);
-            p1 = ex2f(p1);
-            float g0 = p[c], g1 = p[c + 1], f0 = 1.f, f1 = 1.f;
-            if (CAP) f2_unpack(fac, f0, f1);
-            if (decltype(some)::value) {
-              const bool v0 = (uint32_t)(c - rel) < len, v1 = (uint32_t)(c + 1 - rel) < len;
-              p0 = v0 ? p0 : 0.f;
-              g0 = v0 ? g0 : 0.f;
-              f0 = v0 ? f0 : 0.f;
-              p1 = v1 ? p1 : 0.f;
-              g1 = v1 ? g1 : 0.f;
-              f1 = v1 ? f1 : 0.f;
-            }
-            const uint64_t pp = f2_pack(p0, p1), gg = f2_pack(g0, g1);
-            if (!KV) dex = f2_fma(pp, gg, dex);
-            const uint64_t pf = CAP ? f2_mul(pp, f2_pack(f0, f1)) : pp;
-            const uint64_t dx = f2_mul(pf, f2_add(gg, d));
-            float y0, y1;
-            f2_unpack(KV ? pp : pf, y0, y1);
-            s[c / 2] = __uint_as_float(pack_bf16(y0, y1));
-            f2_unpack(dx, y0, y1);
-            p[c / 2] = __uint_as_float(pack_bf16(y0, y1));
-          }
+          };
+          if (lo1 <= c1 && hi0 >= c1 + 32 && (!BIAS || __all_sync(0xffffffffu, KV ? dist0 <= 0.f : dist0 >= 31.f))) weigh(std::false_type{});
+          else weigh(std::true_type{});
+          tmem_st16(S + hf * 16, s);
+          tmem_st16(P + hf * 16, p);
         }
-      };
-      if (lo1 <= c1 && hi0 >= c1 + 32 && (!BIAS || __all_sync(0xffffffffu, KV ? dist0 <= 0.f : dist0 >= 31.f))) weigh(std::false_type{});
-      else weigh(std::true_type{});
-      tmem_st16(S + hf * 16, s);
-      tmem_st16(P + hf * 16, p);
+        tmem_wait_st();
+        tc_fence_before_sync();
+        mbar_arrive(bar(L::B_P + wg));
+        if (KV) mbar_arrive(bar(L::B_EMPTY + st));
       }
-      tmem_wait_st();
-      tc_fence_before_sync();
-      mbar_arrive(bar(L::B_P + wg));
-      if (KV) mbar_arrive(bar(L::B_EMPTY + st));
-    }
-    base += n;
-    if (!ok) break;
-    if (!KV) {
-      float d0, d1;
-      f2_unpack(dex, d0, d1);
-      reinterpret_cast<float*>(smem + L::OFF_DEX)[(seq & 1) * 256 + tid] = d0 + d1;
-      mbar_arrive(bar(L::B_DEX + (seq & 1)));
-    }
-    ++seq;
+      base += n;
+      if (!ok) break;
+      if (!KV) {
+        float d0, d1;
+        f2_unpack(dex, d0, d1);
+        reinterpret_cast<float*>(smem + L::OFF_DEX)[(seq & 1) * 256 + tid] = d0 + d1;
+        mbar_arrive(bar(L::B_DEX + (seq & 1)));
+      }
+      ++seq;
     }
   } else {
     // ------------------------------------------------------------------------------------------------ outputs
@@ -455,85 +455,85 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
     int seq = 0;
     bool fail = false;
     for (int k = 0;; ++k) {
-    Item w;
-    w.n = -1;
-    fail = !item_at(k, w);
-    if (named_bar_or(2, 128, fail) || w.n < 0) break;
-    if (lane == 0) item_read(k);
-    const int n = w.n, r = w.r0 + r128;
-    const bool valid = r < rows;
-    float fix = 0.f;   // dO.o - D
-    if (n > 0) {
-      fail = !wait_bar(bar(L::B_ACC), seq & 1, s_abort, f.limit);
-      if (!KV) {
-        if (!fail) fail = !wait_bar(bar(L::B_DEX + (seq & 1)), (seq >> 1) & 1, s_abort, f.limit);
-        const float* const dex = reinterpret_cast<const float*>(smem + L::OFF_DEX) + (seq & 1) * 256;
-        const float* const own = reinterpret_cast<const float*>(smem + L::OFF_OWN) + (seq & 1) * 256;
-        const float d = dex[r128] + dex[128 + r128], nl = own[r128];
-        fix = -own[128 + r128] - d;
-        if (valid) {
-          float* const st = a.stat + ((size_t)w.b * a.H + w.own) * a.stat_stride + r;
-          st[0] = nl;
-          st[(size_t)a.B * a.H * a.stat_stride] = -d;
-        }
-      }
-      __syncwarp();
-      tc_fence_after_sync();
-    }
-    // dq; or dk, then dv: by 64 channels through shared memory and the copy engine, which leaves out rows behind the last
-    float test = 0.f;
-#pragma unroll 1
-    for (int x = 0; x < (KV ? 2 * D : D); x += 32) {
-      const bool second = KV && x >= D;              // (dv)
-      const int c = second ? x - D : x;
-      const uint32_t out = sb + L::OFF_OUT + (L::OUTS == 2 ? (x / 64 & 1) : 0) * L::OUT;
-      const float mul = second ? 1.f : a.scale;
-      float o[32];
+      Item w;
+      w.n = -1;
+      fail = !item_at(k, w);
+      if (named_bar_or(2, 128, fail) || w.n < 0) break;
+      if (lane == 0) item_read(k);
+      const int n = w.n, r = w.r0 + r128;
+      const bool valid = r < rows;
+      float fix = 0.f;   // dO.o - D
       if (n > 0) {
-        tmem_ld32(acc1 + lanes + x, o);              // (acc2 lies behind acc1)
+        fail = !wait_bar(bar(L::B_ACC), seq & 1, s_abort, f.limit);
         if (!KV) {
-          float u[32];
-          tmem_ld32(acc2 + lanes + x, u);
+          if (!fail) fail = !wait_bar(bar(L::B_DEX + (seq & 1)), (seq >> 1) & 1, s_abort, f.limit);
+          const float* const dex = reinterpret_cast<const float*>(smem + L::OFF_DEX) + (seq & 1) * 256;
+          const float* const own = reinterpret_cast<const float*>(smem + L::OFF_OWN) + (seq & 1) * 256;
+          const float d = dex[r128] + dex[128 + r128], nl = own[r128];
+          fix = -own[128 + r128] - d;
+          if (valid) {
+            float* const st = a.stat + ((size_t)w.b * a.H + w.own) * a.stat_stride + r;
+            st[0] = nl;
+            st[(size_t)a.B * a.H * a.stat_stride] = -d;
+          }
+        }
+        __syncwarp();
+        tc_fence_after_sync();
+      }
+      // dq; or dk, then dv: by 64 channels through shared memory and the copy engine, which leaves out rows behind the last
+      float test = 0.f;
+#pragma unroll 1
+      for (int x = 0; x < (KV ? 2 * D : D); x += 32) {
+        const bool second = KV && x >= D;              // (dv)
+        const int c = second ? x - D : x;
+        const uint32_t out = sb + L::OFF_OUT + (L::OUTS == 2 ? (x / 64 & 1) : 0) * L::OUT;
+        const float mul = second ? 1.f : a.scale;
+        float o[32];
+        if (n > 0) {
+          tmem_ld32(acc1 + lanes + x, o);              // (acc2 lies behind acc1)
+          if (!KV) {
+            float u[32];
+            tmem_ld32(acc2 + lanes + x, u);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = fmaf(fix, u[e], o[e]);
+          }
           tmem_wait_ld();
+          if (x + 32 == (KV ? 2 * D : D)) {
+            tc_fence_before_sync();
+            mbar_arrive(bar(L::B_ACCE));
+          }
+        } else {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = fmaf(fix, u[e], o[e]);
+          for (int e = 0; e < 32; ++e) o[e] = 0.f;
         }
-        tmem_wait_ld();
-        if (x + 32 == (KV ? 2 * D : D)) {
-          tc_fence_before_sync();
-          mbar_arrive(bar(L::B_ACCE));
+        if (c % 64 == 0) {
+          if (r128 == 0) {                             // (this place's last store has read it)
+            if (L::OUTS == 2) tma_store_wait_read_1();
+            else tma_store_wait_read();
+          }
+          named_bar_sync(2, 128);
         }
-      } else {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) o[e] = 0.f;
-      }
-      if (c % 64 == 0) {
-        if (r128 == 0) {                             // (this place's last store has read it)
-          if (L::OUTS == 2) tma_store_wait_read_1();
-          else tma_store_wait_read();
+        for (int e = 0; e < 32; ++e) {
+          o[e] *= mul;
+          test = fmaf(o[e], 0.f, test);
         }
-        named_bar_sync(2, 128);
-      }
 #pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        o[e] *= mul;
-        test = fmaf(o[e], 0.f, test);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        sts128(out + sw128(r128, c / 8 % 8 + e), make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]),
-                                                          pack_bf16(o[8 * e + 4], o[8 * e + 5]), pack_bf16(o[8 * e + 6], o[8 * e + 7])));
-      if (c % 64 == 32) {
-        fence_proxy_async();
-        named_bar_sync(2, 128);
-        if (r128 == 0) {
-          tma_store_4d(second ? &tm_o2 : &tm_o1, out, c - 32, w.own, w.r0, w.b);
-          tma_store_commit();
+        for (int e = 0; e < 4; ++e)
+          sts128(out + sw128(r128, c / 8 % 8 + e), make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]),
+                                                            pack_bf16(o[8 * e + 4], o[8 * e + 5]), pack_bf16(o[8 * e + 6], o[8 * e + 7])));
+        if (c % 64 == 32) {
+          fence_proxy_async();
+          named_bar_sync(2, 128);
+          if (r128 == 0) {
+            tma_store_4d(second ? &tm_o2 : &tm_o1, out, c - 32, w.own, w.r0, w.b);
+            tma_store_commit();
+          }
         }
       }
-    }
-    if (__any_sync(0xffffffffu, valid && !(test == 0.f)) && lane == 0) note_bad(s_list, (int*)(s_flags + 2), w.idx);
-    if (n > 0) ++seq;
+      if (__any_sync(0xffffffffu, valid && !(test == 0.f)) && lane == 0) note_bad(s_list, (int*)(s_flags + 2), w.idx);
+      if (n > 0) ++seq;
     }
     if (r128 == 0) tma_store_wait_all();
   }

@@ -472,79 +472,79 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       step += n;
 #pragma unroll 1
       for (int i = 0; i < NT; ++i) {
-      const uint32_t O = o_col(i) + lanes;
-      const int h = head_of(w, i), t = row_of(w, i) + r128;
-      const bool valid = t < T;
-      float m = -INFINITY, l = 0.f;
-      if (n > 0) {
-        fail = !wait_bar(bar(L::B_ML + i), seq & 1, s_abort, f.limit) ||
-               !wait_bar(bar(L::B_O + 2 * i + (step - 1 & 1)), (step - 1) >> 1 & 1, s_abort, f.limit);
-        __syncwarp();
-        const float2 ml = reinterpret_cast<const float2*>(smem + L::OFF_ML)[(seq & 1) * 256 + i * 128 + r128];
-        m = ml.x;
-        l = ml.y;
-        tc_fence_after_sync();
-      }
-      const size_t row = ((size_t)w.b * T + t) * a.H + h;                                                // of [B, T, H]
-      const size_t prow0 = (((size_t)w.part * a.B + w.b) * a.H + h) * (size_t)T + row_of(w, i), prow = prow0 + r128;  // of [parts, B, H, T]
-      const float inv = f.parts > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
-      float test = l * 0.f;
-      // outputs through shared memory: 64 channels at a time by the copy engine (which leaves out rows behind the last), or 32 in fp32
-      const int rows = min(128, T - row_of(w, i));
-#pragma unroll 1
-      for (int c = 0; c < D; c += 32) {
-        float o[32];
+        const uint32_t O = o_col(i) + lanes;
+        const int h = head_of(w, i), t = row_of(w, i) + r128;
+        const bool valid = t < T;
+        float m = -INFINITY, l = 0.f;
         if (n > 0) {
-          tmem_ld32(O + c, o);
-          tmem_wait_ld();
-        } else {
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+          fail = !wait_bar(bar(L::B_ML + i), seq & 1, s_abort, f.limit) ||
+                 !wait_bar(bar(L::B_O + 2 * i + (step - 1 & 1)), (step - 1) >> 1 & 1, s_abort, f.limit);
+          __syncwarp();
+          const float2 ml = reinterpret_cast<const float2*>(smem + L::OFF_ML)[(seq & 1) * 256 + i * 128 + r128];
+          m = ml.x;
+          l = ml.y;
+          tc_fence_after_sync();
         }
-        if (c + 32 == D && n > 0) {
-          tc_fence_before_sync();
-          mbar_arrive(bar(L::B_OE + i));
-        }
+        const size_t row = ((size_t)w.b * T + t) * a.H + h;                                                // of [B, T, H]
+        const size_t prow0 = (((size_t)w.part * a.B + w.b) * a.H + h) * (size_t)T + row_of(w, i), prow = prow0 + r128;  // of [parts, B, H, T]
+        const float inv = f.parts > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+        float test = l * 0.f;
+        // outputs through shared memory: 64 channels at a time by the copy engine (which leaves out rows behind the last), or 32 in fp32
+        const int rows = min(128, T - row_of(w, i));
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          float o[32];
+          if (n > 0) {
+            tmem_ld32(O + c, o);
+            tmem_wait_ld();
+          } else {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          o[e] *= inv;
-          test = fmaf(o[e], 0.f, test);
-        }
-        if (f.parts > 1) {
-          named_bar_sync(2, 128);   // (the last quarter is out of shared memory)
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            sts128(out + sw128(r128, e), make_uint4(__float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]), __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3])));
-          named_bar_sync(2, 128);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int k = e * 16 + (r128 >> 3);
-            if (k < rows) *reinterpret_cast<uint4*>(f.part_o + (prow0 + k) * D + c + (r128 & 7) * 4) = lds128(out + sw128(k, r128 & 7));
+            for (int e = 0; e < 32; ++e) o[e] = 0.f;
           }
-        } else {
-          if (c % 64 == 0) {
-            if (r128 == 0) tma_store_wait_read();
-            named_bar_sync(2, 128);
+          if (c + 32 == D && n > 0) {
+            tc_fence_before_sync();
+            mbar_arrive(bar(L::B_OE + i));
           }
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            sts128(out + sw128(r128, c / 8 % 8 + e), make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]),
-                                                              pack_bf16(o[8 * e + 4], o[8 * e + 5]), pack_bf16(o[8 * e + 6], o[8 * e + 7])));
-          if (c % 64 == 32) {
-            fence_proxy_async();
+          for (int e = 0; e < 32; ++e) {
+            o[e] *= inv;
+            test = fmaf(o[e], 0.f, test);
+          }
+          if (f.parts > 1) {
+            named_bar_sync(2, 128);   // (the last quarter is out of shared memory)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              sts128(out + sw128(r128, e), make_uint4(__float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]), __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3])));
             named_bar_sync(2, 128);
-            if (r128 == 0 && rows > 0) {
-              tma_store_4d(&tm_o, out, c - 32, h, row_of(w, i), w.b);
-              tma_store_commit();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int k = e * 16 + (r128 >> 3);
+              if (k < rows) *reinterpret_cast<uint4*>(f.part_o + (prow0 + k) * D + c + (r128 & 7) * 4) = lds128(out + sw128(k, r128 & 7));
+            }
+          } else {
+            if (c % 64 == 0) {
+              if (r128 == 0) tma_store_wait_read();
+              named_bar_sync(2, 128);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              sts128(out + sw128(r128, c / 8 % 8 + e), make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]),
+                                                                pack_bf16(o[8 * e + 4], o[8 * e + 5]), pack_bf16(o[8 * e + 6], o[8 * e + 7])));
+            if (c % 64 == 32) {
+              fence_proxy_async();
+              named_bar_sync(2, 128);
+              if (r128 == 0 && rows > 0) {
+                tma_store_4d(&tm_o, out, c - 32, h, row_of(w, i), w.b);
+                tma_store_commit();
+              }
             }
           }
         }
-      }
-      if (valid) {
-        if (f.parts > 1) f.part_ml[prow] = make_float2(m, l);
-        else if (a.lse) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
-      }
-      if (__any_sync(0xffffffffu, valid && !(test == 0.f)) && lane == 0) note_bad(s_list, (int*)(s_flags + 2), w.idx);
+        if (valid) {
+          if (f.parts > 1) f.part_ml[prow] = make_float2(m, l);
+          else if (a.lse) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+        }
+        if (__any_sync(0xffffffffu, valid && !(test == 0.f)) && lane == 0) note_bad(s_list, (int*)(s_flags + 2), w.idx);
       }
       if (n > 0) ++seq;
     }
