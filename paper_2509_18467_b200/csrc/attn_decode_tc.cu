@@ -145,7 +145,7 @@ attn_step_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     // ------------------------------------------------------------------------------------------------ copies
     if (elect_one()) {
       for (int it = 0; it < n; ++it) {
-        const int s = it % L::ST, s0 = arc_tile(arc, k0 + it) * 128;
+        const int s = it % L::ST, s0 = arc_tile(arc, k0 + n - 1 - it) * 128;
         if (it >= L::ST && !wait_bar(bar(L::B_EMPTY + s), (it / L::ST - 1) & 1, s_abort, limit)) break;
         mbar_arrive_expect_tx(bar(L::B_FULL + s), L::STAGE);
         load_tile<D, 128>(sb + s * L::STAGE + L::TILE, &tm_k, bar(L::B_FULL + s), g, s0, b);
@@ -161,7 +161,7 @@ attn_step_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       auto scores = [&](int it) {
         const int s = it % L::ST;
         if (!wait_bar(bar(L::B_FULL + s), (it / L::ST) & 1, s_abort, limit)) return false;
-        if (!arc_whole(arc, arc_tile(arc, k0 + it) * 128, a.C) && !wait_bar(bar(L::B_FIX), fixed++ & 1, s_abort, limit)) return false;
+        if (!arc_whole(arc, arc_tile(arc, k0 + n - 1 - it) * 128, a.C) && !wait_bar(bar(L::B_FIX), fixed++ & 1, s_abort, limit)) return false;
         tc_fence_after_sync();
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) mma_f16(s_col(it), kdesc<128>(sb + s * L::STAGE + L::TILE, kk), kdesc<16>(sb + L::OFF_Q, kk), id_s, kk != 0);
@@ -194,7 +194,7 @@ attn_step_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     bool fail = false;
     for (int it = 0; it < n; ++it) {
-      const int s0 = arc_tile(arc, k0 + it) * 128, slot = s0 + tid, st = it % L::ST;
+      const int s0 = arc_tile(arc, k0 + n - 1 - it) * 128, slot = s0 + tid, st = it % L::ST;
       const int back = slot < a.C ? arc_back(arc, slot, a.C) : 0;
       const bool seen = slot < a.C && back < arc.n;
       if (!arc_whole(arc, s0, a.C)) {
@@ -364,7 +364,7 @@ attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, in
     }
   };
   auto fetch = [&](int it) {
-    const int s0 = arc_tile(arc, k0 + it) * 128, slot = s0 + tid;
+    const int s0 = arc_tile(arc, k0 + n - 1 - it) * 128, slot = s0 + tid;
     if (arc_whole(arc, s0, a.C)) {
       load_slot(row0 + slot);
       return;
@@ -451,7 +451,7 @@ attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, in
   const uint32_t v_row = sb + L::OFF_V + sw128(tid, 0);   // (chunk j of the row: its address with bits 4 ... 6 turned over by j)
   bool fail = false;
   for (int it = 0; it < n; ++it) {
-    const int slot = arc_tile(arc, k0 + it) * 128 + tid;
+    const int slot = arc_tile(arc, k0 + n - 1 - it) * 128 + tid;
     const int back = slot < a.C ? arc_back(arc, slot, a.C) : 0;
     const bool seen = slot < a.C && back < arc.n;
     if (seen && back == 0) {
@@ -638,7 +638,7 @@ attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, in
 // Heads per block, and parts of the keys: as many as give every SM four rounds of blocks, of at least four tiles of slots each.
 static int step_heads(const AttnDecode& c) {
   const int G = c.H / c.H_kv;
-  if (c.kq) return c.d == 128 && G <= 4 ? 4 : 8;
+  if (c.kq) return G <= 4 ? 4 : 8;
   return G <= 4 ? 4 : G <= 8 ? 8 : 16;
 }
 
@@ -683,7 +683,7 @@ int launch_attn_decode_tc(const AttnDecode& c) {
   if (blocks > 0x7fffffffLL) return LAWCAT_ERR_UNSUPPORTED;
   const unsigned n = (unsigned)blocks;
   if (c.kq) {
-    if (c.d == 64) return attn::step_quant_tc<64, 8>(c, a, n);
+    if (c.d == 64) return hpb == 4 ? attn::step_quant_tc<64, 4>(c, a, n) : attn::step_quant_tc<64, 8>(c, a, n);
     return hpb == 4 ? attn::step_quant_tc<128, 4>(c, a, n) : attn::step_quant_tc<128, 8>(c, a, n);
   }
   if (c.d == 64) return hpb == 4 ? attn::step_tc<64, 4>(c, a, n) : hpb == 8 ? attn::step_tc<64, 8>(c, a, n) : attn::step_tc<64, 16>(c, a, n);
