@@ -18,6 +18,13 @@
 //         rounded weight times the value would be.)
 // Codes are unpacked two at a time as channels (i, i + 4) of eight; q is stored in that order and the outputs' lanes are read in it.
 //
+// What bounds the 4-bit form is unpacking and weighing in the threads (at width 128 the integer pipe, at half the issue rate, for 1040 of
+// 1900 cycles a tile), so that as many blocks as tensor memory and registers hold share an SM: 64 sequences of 16384 slots, 32/8 heads
+// of 128: 328 us, 3.1 TB/s of codes; of 64: 239 us with six blocks of four heads (four blocks 268, of eight heads 308). The form in the
+// storage type: 64 sequences of 8192 slots, 32/8 heads of 128, 2.15 GB: 319 us, 6.7 TB/s. Both walk their slots from the newest to
+// the oldest: under distance biases the references then stay where the first tile puts them (the 4-bit form at width 64 with biases, of
+// eight heads: 387 us the other way round, 310 so).
+//
 // Rounding: weights to bf16 as an operand, o once; all else fp32.
 #include <cuda_bf16.h>
 
@@ -309,12 +316,12 @@ struct QuantLay {
   static constexpr uint32_t OFF_V = 0, OFF_Q = V, OFF_P = OFF_Q + (D / 64) * QROWS * 128, OFF_QS = OFF_P + (NCOL / 8) * 2048;
   static constexpr uint32_t OFF_RED = OFF_QS + NCOL * 4, OFF_NEW = OFF_RED + 4 * 16 * 4 + 4 * NCOL * 4, OFF_BAR = OFF_NEW + D + 4 * NG * 2;
   static constexpr uint32_t BYTES0 = OFF_BAR + 64, BYTES = BYTES0 > 32768u ? BYTES0 : 32768u;  // (D = 64: the product reads 32 KB from V on)
-  static constexpr uint32_t K_COLS = D / 2, COLS = 128;
+  static constexpr uint32_t K_COLS = D / 2, COLS = K_COLS + 2 * NCOL <= 64 ? 64 : 128;
   static_assert(K_COLS + 2 * NCOL <= COLS && QROWS * 128 % 1024 == 0 && OFF_BAR % 16 == 0, "layout");
 };
 
 template <int D, int HPB>
-__global__ void __launch_bounds__(128, HPB * (D / 32) <= 16 ? 4 : 3)
+__global__ void __launch_bounds__(128, HPB * (D / 32) <= 8 ? 6 : HPB * (D / 32) <= 16 ? 4 : 3)
 attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, int* dev_status) {
   using L = QuantLay<D, HPB>;
   constexpr int NG = L::NG, NCOL = L::NCOL, WPR = D / 8;  // words of codes per row
