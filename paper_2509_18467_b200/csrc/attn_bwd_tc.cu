@@ -59,7 +59,7 @@ static void order_tiles(const AttnCall& c, BwdArgs<true>& f) {
     steps[i] = queries(std::min(i * 128 + 128, c.a.mask.T_k) - 1).y - first;
     f.order[i] = (uint16_t)i;
   }
-  std::stable_sort(f.order, f.order + f.tiles, [&](uint16_t x, uint16_t y) { return steps[x] > steps[y]; });
+  std::sort(f.order, f.order + f.tiles, [&](uint16_t x, uint16_t y) { return steps[x] != steps[y] ? steps[x] > steps[y] : x < y; });
 }
 
 template <int D>

@@ -48,14 +48,12 @@ struct StepLay {
   static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 256, "shared memory");
 };
 
-// scores in log2 units of one slot from its dot products
+// scores in log2 units of one slot from its dot products (all lanes of a warp together)
 template <int HPB>
 __device__ __forceinline__ void step_scores(const DecArgs& a, float (&x)[HPB], float back, const float* slope2, bool seen) {
   const float scale2 = a.scale * LOG2E;
   if (a.cap > 0.f) {
-    const float k1 = 2.f * LOG2E * a.scale / a.cap, c2 = a.cap * LOG2E;
-#pragma unroll
-    for (int h = 0; h < HPB; ++h) x[h] = c2 - 2.f * c2 * rcpf(1.f + ex2f(x[h] * k1));
+    cap_scores(x, a.scale / a.cap, a.cap * LOG2E);
   } else {
 #pragma unroll
     for (int h = 0; h < HPB; ++h) x[h] *= scale2;

@@ -19,7 +19,7 @@ def draw(shape, seed, dtype, std=1.0, device="cuda"):
 
 
 def case(B=1, T=64, T_k=None, H=4, H_kv=2, d=64, dtype="bf16", causal=1, window=0, cap=0.0, slopes=False, cu=None, prefix=None,
-         exact=0, grad=True, seed=0):
+         exact=0, grad=True, seed=0, ref_cap=None):
     T_k = T if T_k is None else T_k
     q, k, v = draw((B, T, H, d), seed, dtype, 1.5), draw((B, T_k, H_kv, d), seed + 1, dtype), draw((B, T_k, H_kv, d), seed + 2, dtype)
     dO = draw((B, T, H, d), seed + 3, dtype)
@@ -29,7 +29,7 @@ def case(B=1, T=64, T_k=None, H=4, H_kv=2, d=64, dtype="bf16", causal=1, window=
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     r = api.lawcat_attn_fwd(p, q, k, v, dev_status=status, **more)
     see = visible(T, T_k, causal, window, cu, prefix, B)
-    ref = attention(q, k, v, see, float(torch.tensor(d ** -0.5)), cap, sl, dO, r["o"])
+    ref = attention(q, k, v, see, float(torch.tensor(d ** -0.5)), cap if ref_cap is None else ref_cap, sl, dO, r["o"])
     coarse = U16 if dtype == "bf16" and not exact else 0.0     # the tensor-core kernels round weights to bf16
     out = U16 if dtype == "bf16" else U32
     check(r["o"], ref["o"], ref["o_sum"] + coarse * ref["o_mag"], out, "o")
@@ -75,6 +75,13 @@ MASKS = [
 @pytest.mark.parametrize("i", range(len(MASKS)))
 def test_masks(i, d, dtype, exact):
     case(B=2, T=300, d=d, dtype=dtype, exact=exact, seed=50 + i, **MASKS[i])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,exact", KINDS)
+def test_a_cap_far_above_the_scores(dtype, exact):
+    """No cap, up to some steps of 2^-24 of the scores, which their bound has room for: none of the cap's."""
+    case(T=200, dtype=dtype, exact=exact, seed=9, cap=1e6, ref_cap=0.0)
 
 
 @pytest.mark.gpu

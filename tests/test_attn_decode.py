@@ -24,7 +24,7 @@ def rows_of(cache, b, slots):
     return out
 
 
-def step(quant, pos, C=100, H=4, H_kv=2, d=64, dtype="bf16", window=0, cap=0.0, slopes=False, exact=0, seed=0, garbage=math.nan):
+def step(quant, pos, C=100, H=4, H_kv=2, d=64, dtype="bf16", window=0, cap=0.0, slopes=False, exact=0, seed=0, garbage=math.nan, ref_cap=None):
     """One step for sequences at positions `pos`; slots without a token hold `garbage`."""
     B = len(pos)
     q, k, v = draw((B, H, d), seed, dtype, 1.5), draw((B, H_kv, d), seed + 1, dtype), draw((B, H_kv, d), seed + 2, dtype)
@@ -71,7 +71,7 @@ def step(quant, pos, C=100, H=4, H_kv=2, d=64, dtype="bf16", window=0, cap=0.0, 
             a, c = (t[b][:, other], was[b][:, other]) if quant else (t[b][other], was[b][other])
             assert torch.equal(a.contiguous().view(torch.uint8), c.contiguous().view(torch.uint8))
         see = torch.ones(1, 1, n, dtype=torch.bool)
-        ref = attention(q[b][None, None], K[None], V[None], see, float(torch.tensor(d ** -0.5)), cap, sl)
+        ref = attention(q[b][None, None], K[None], V[None], see, float(torch.tensor(d ** -0.5)), cap if ref_cap is None else ref_cap, sl)
         more = 0.0
         if quant:  # products with codes and with the minimum apart: each is as large as 32 times the largest value at most in fp32,
             # and a rounded weight meets scale times code, at most twice the largest value
@@ -102,6 +102,13 @@ def test_heads_and_widths(H, H_kv, d, quant, dtype, exact):
 @pytest.mark.parametrize("kw", [dict(window=1), dict(window=64), dict(window=333, slopes=True), dict(cap=4.0), dict(cap=20.0, slopes=True), dict(slopes=True)])
 def test_windows_caps_and_biases(kw, quant, dtype):
     step(quant, [0, 63, 64, 500, 1111], 600, dtype=dtype, d=128, H=8, H_kv=2, seed=7, **kw)
+
+
+@pytest.mark.parametrize("dtype,exact", [("f32", 0), ("bf16", 1), ("bf16", 0)])
+@pytest.mark.parametrize("quant", [False, True])
+def test_a_cap_far_above_the_scores(quant, dtype, exact):
+    """No cap, up to some steps of 2^-24 of the scores, which their bound has room for: none of the cap's."""
+    step(quant, [0, 77, 300, 1111], 400, dtype=dtype, exact=exact, H=8, H_kv=2, seed=11, cap=1e6, ref_cap=0.0)
 
 
 @pytest.mark.parametrize("quant", [False, True])
