@@ -66,14 +66,18 @@ template <int D>
 struct BwdLay {
   static constexpr uint32_t OWN = 128 * D * 2, WALK = 64 * D * 2, STAT = 512;   // (a tile's -lse log2e, then its -D)
   static constexpr int ST = D == 128 ? 3 : 4, SLOTS = 4;
+  static constexpr int NA = D == 64 ? 2 : 1;   // items whose own tiles fit (8 x 1024 tokens, window 64, dQ: 60 us with one, 54 with two)
+  // Items whose row sums are on their way from the weights' threads to the outputs': the weights begin item i + 2 when item i + 1's scores
+  // are weighed, which waits for nothing that the outputs do with item i; item i + 3 waits for item i's place in tensor memory.
+  static constexpr int DEEP = 4;
   static constexpr int OUTS = D == 128 ? 1 : 2;                                 // places for gradients on their way, of 64 channels
   static constexpr uint32_t STAGE = 2 * WALK, OUT = 128 * 128;
-  static constexpr uint32_t OFF_A = 0, OFF_RING = 3 * OWN, OFF_OUT = OFF_RING + ST * STAGE, OFF_STAT = OFF_OUT + OUTS * OUT, OFF_DEX = OFF_STAT + ST * STAT,
-                            OFF_OWN = OFF_DEX + 2048, OFF_LIST = OFF_OWN + 2048, OFF_ITEM = OFF_LIST + BAD_MAX * 4, OFF_ASK = OFF_ITEM + SLOTS * 64, OFF_BAR = OFF_ASK + 16;
+  static constexpr uint32_t OFF_A = 0, OFF_RING = NA * 3 * OWN, OFF_OUT = OFF_RING + ST * STAGE, OFF_STAT = OFF_OUT + OUTS * OUT, OFF_DEX = OFF_STAT + ST * STAT,
+                            OFF_OWN = OFF_DEX + DEEP * 1024, OFF_LIST = OFF_OWN + DEEP * 1024, OFF_ITEM = OFF_LIST + BAD_MAX * 4, OFF_ASK = OFF_ITEM + SLOTS * 64, OFF_BAR = OFF_ASK + 16;
   static constexpr uint32_t BYTES = OFF_BAR + 512, E1 = (uint32_t)dq_smem<D, 4, 128>(), E2 = (uint32_t)dkdv_smem<D, 4, 128>();
   static constexpr int THREADS = 448;   // weights, outputs, copies, products
-  static constexpr int B_A = 0, B_AE = 1, B_FULL = 2, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + 2, B_ACC = B_P + 2, B_ACCE = B_ACC + 1,
-                       B_DEX = B_ACCE + 1, B_ITEM = B_DEX + 2, B_ITEME = B_ITEM + SLOTS, B_ASK = B_ITEME + SLOTS, NBAR = B_ASK + 1;
+  static constexpr int B_A = 0, B_AE = NA, B_FULL = 2 * NA, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + 2, B_ACC = B_P + 2, B_ACCE = B_ACC + 1,
+                       B_DEX = B_ACCE + 1, B_ITEM = B_DEX + DEEP, B_ITEME = B_ITEM + SLOTS, B_ASK = B_ITEME + SLOTS, NBAR = B_ASK + 1;
   static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 512 && E1 <= OFF_LIST && E2 <= OFF_LIST, "shared memory");
 };
 
@@ -136,8 +140,10 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
   };
 
   if (tid == 0) {
-    mbar_init(bar(L::B_A), 1);
-    mbar_init(bar(L::B_AE), KV ? 1 : 257);                // (the threads of weights read dO and o)
+    for (int i = 0; i < L::NA; ++i) {
+      mbar_init(bar(L::B_A + i), 1);
+      mbar_init(bar(L::B_AE + i), KV ? 1 : 257);          // (the threads of weights read dO and o)
+    }
     for (int i = 0; i < L::ST; ++i) {
       mbar_init(bar(L::B_FULL + i), 1);
       mbar_init(bar(L::B_EMPTY + i), KV ? 129 : 1);   // (the softmax threads read the statistics)
@@ -145,8 +151,8 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(L::B_S + i), 1);
       mbar_init(bar(L::B_P + i), 128);
-      mbar_init(bar(L::B_DEX + i), 256);
     }
+    for (int i = 0; i < L::DEEP; ++i) mbar_init(bar(L::B_DEX + i), 256);
     mbar_init(bar(L::B_ACC), 1);
     mbar_init(bar(L::B_ACCE), 128);
     for (int i = 0; i < L::SLOTS; ++i) {
@@ -182,6 +188,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
     return true;
   };
   auto item_read = [&](int k) { mbar_arrive(bar(L::B_ITEME + k % L::SLOTS)); };
+  auto own_tiles = [&](int seq) { return sb + L::OFF_A + (uint32_t)(seq % L::NA) * 3 * L::OWN; };   // of the seq-th item with tiles
 
   if (warp == 12) {
     // ------------------------------------------------------------------------------------------------ copies
@@ -199,12 +206,13 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
         ++k;
         if (idx < 0) break;
         if (w.n > 0) {
-          if (seq > 0) ok = wait_bar(bar(L::B_AE), (seq - 1) & 1, s_abort, f.limit);
+          const uint32_t own = own_tiles(seq), full = bar(L::B_A + seq % L::NA);
+          if (seq >= L::NA) ok = wait_bar(bar(L::B_AE + seq % L::NA), (seq / L::NA - 1) & 1, s_abort, f.limit);
           if (!ok) break;
-          mbar_arrive_expect_tx(bar(L::B_A), (KV ? 2 : 3) * L::OWN);
-          load_tile<D, 128>(sb + L::OFF_A, &tm_a1, bar(L::B_A), w.own, w.r0, w.b);
-          load_tile<D, 128>(sb + L::OFF_A + L::OWN, &tm_a2, bar(L::B_A), w.own, w.r0, w.b);
-          if (!KV) load_tile<D, 128>(sb + L::OFF_A + 2 * L::OWN, &tm_o2, bar(L::B_A), w.own, w.r0, w.b);   // (o)
+          mbar_arrive_expect_tx(full, (KV ? 2 : 3) * L::OWN);
+          load_tile<D, 128>(own, &tm_a1, full, w.own, w.r0, w.b);
+          load_tile<D, 128>(own + L::OWN, &tm_a2, full, w.own, w.r0, w.b);
+          if (!KV) load_tile<D, 128>(own + 2 * L::OWN, &tm_o2, full, w.own, w.r0, w.b);   // (o)
           int h = KV ? w.own * G : quot(w.own, f.group), at = w.w0, left = w.per;
           for (int it = 0; it < w.n; ++it, ++step) {
             const int s = step % L::ST;
@@ -244,17 +252,20 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
       constexpr uint32_t id_s = instr_desc(128, 64, FMT_BF16, MAJOR_K, MAJOR_K);
       constexpr uint32_t id_a = instr_desc(128, D, FMT_BF16, MAJOR_K, MAJOR_MN);
       auto b1 = [&](int step) { return sb + L::OFF_RING + (uint32_t)(step % L::ST) * L::STAGE; };
-      auto scores = [&](int step, bool last) {
+      auto scores = [&](int seq, int step, bool last) {   // of a step of the seq-th item; `last`: of the item
         if (!wait_bar(bar(L::B_FULL + step % L::ST), (step / L::ST) & 1, s_abort, f.limit)) return false;
         tc_fence_after_sync();
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) mma_f16(s_col(step & 1), kdesc<128>(sb + L::OFF_A, kk), kdesc<64>(b1(step), kk), id_s, kk != 0);
+        for (int kk = 0; kk < D / 16; ++kk) mma_f16(s_col(step & 1), kdesc<128>(own_tiles(seq), kk), kdesc<64>(b1(step), kk), id_s, kk != 0);
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
-          mma_f16(p_col(step & 1), kdesc<128>(sb + L::OFF_A + L::OWN, kk), kdesc<64>(b1(step) + L::WALK, kk), id_s, kk != 0);
+          mma_f16(p_col(step & 1), kdesc<128>(own_tiles(seq) + L::OWN, kk), kdesc<64>(b1(step) + L::WALK, kk), id_s, kk != 0);
         mma_commit(bar(L::B_S + (step & 1)));
-        if (last) mma_commit(bar(L::B_AE));
+        if (last) mma_commit(bar(L::B_AE + seq % L::NA));
         return true;
+      };
+      auto first_scores = [&](int seq, int step, int n) {
+        return wait_bar(bar(L::B_A + seq % L::NA), (seq / L::NA) & 1, s_abort, f.limit) && scores(seq, step, n == 1);
       };
       int k = 0, seq = 0, step = 0;
       auto next_item = [&]() {   // tiles of the next item that has any; 0 or less behind the last
@@ -267,10 +278,10 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
         return w.n;
       };
       int n = next_item();
-      bool ok = n > 0 && wait_bar(bar(L::B_A), 0, s_abort, f.limit) && scores(0, n == 1);
+      bool ok = n > 0 && first_scores(0, 0, n);
       while (n > 0 && ok) {
         for (int it = 0; it < n && ok; ++it, ++step) {
-          if (it + 1 < n) ok = scores(step + 1, it + 2 == n);
+          if (it + 1 < n) ok = scores(seq, step + 1, it + 2 == n);
           if (ok) ok = wait_bar(bar(L::B_P + (step & 1)), (step >> 1) & 1, s_abort, f.limit);
           if (ok && it == 0 && seq > 0) ok = wait_bar(bar(L::B_ACCE), (seq - 1) & 1, s_abort, f.limit);
           if (!ok) break;
@@ -284,10 +295,12 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
         }
         if (!ok) break;
         mma_commit(bar(L::B_ACC));
-        // (asked for behind the item's last product: the other roles finish with it before the copy warp comes to write more down)
+        // (asked for behind the item's last product: the other roles finish with it before the copy warp comes to write more down. Its
+        // first scores in front of that product, where its tiles are there: 8 x 1024 tokens under a window of 64 dQ 54 -> 51 us, but
+        // 4096 causal tokens 163 -> 170, the warpgroups then weigh in step.)
         n = next_item();
         ++seq;
-        if (n > 0) ok = wait_bar(bar(L::B_A), seq & 1, s_abort, f.limit) && scores(step, n == 1);
+        if (n > 0) ok = first_scores(seq, step, n);
       }
     }
   } else if (warp < 8) {
@@ -312,9 +325,9 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
       uint64_t dex = 0;           // sums of p dP
       if (!KV) {
         const float lse = r < rows ? a.lse[((size_t)w.b * a.mask.T + r) * a.H + w.own] : 0.f;
-        ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_A), seq & 1, s_abort, f.limit));
+        ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_A + seq % L::NA), (seq / L::NA) & 1, s_abort, f.limit));
         if (!ok) break;
-        const uint32_t row = sb + L::OFF_A + L::OWN + sw128(r128, 0);   // (chunk j of a row: its address with bits 4 ... 6 turned over by j)
+        const uint32_t row = own_tiles(seq) + L::OWN + sw128(r128, 0);   // (chunk j of a row: its address with bits 4 ... 6 turned over by j)
         float d0 = 0.f, d1 = 0.f;
 #pragma unroll 4
         for (int j = 0; j < D / 8; ++j) {
@@ -325,11 +338,11 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
           d0 = fmaf(bf16_lo(x.z), bf16_lo(y.z), fmaf(bf16_lo(x.w), bf16_lo(y.w), d0));
           d1 = fmaf(bf16_hi(x.z), bf16_hi(y.z), fmaf(bf16_hi(x.w), bf16_hi(y.w), d1));
         }
-        mbar_arrive(bar(L::B_AE));
+        mbar_arrive(bar(L::B_AE + seq % L::NA));
         nd = -(d0 + d1);
         nl = -lse * LOG2E;
         if (wg == 0) {
-          float* const own = reinterpret_cast<float*>(smem + L::OFF_OWN) + (seq & 1) * 256;
+          float* const own = reinterpret_cast<float*>(smem + L::OFF_OWN) + seq % L::DEEP * 256;
           own[r128] = nl;
           own[128 + r128] = nd;
         }
@@ -443,8 +456,8 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
       if (!KV) {
         float d0, d1;
         f2_unpack(dex, d0, d1);
-        reinterpret_cast<float*>(smem + L::OFF_DEX)[(seq & 1) * 256 + tid] = d0 + d1;
-        mbar_arrive(bar(L::B_DEX + (seq & 1)));
+        reinterpret_cast<float*>(smem + L::OFF_DEX)[seq % L::DEEP * 256 + tid] = d0 + d1;
+        mbar_arrive(bar(L::B_DEX + seq % L::DEEP));
       }
       ++seq;
     }
@@ -466,9 +479,9 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
       if (n > 0) {
         fail = !wait_bar(bar(L::B_ACC), seq & 1, s_abort, f.limit);
         if (!KV) {
-          if (!fail) fail = !wait_bar(bar(L::B_DEX + (seq & 1)), (seq >> 1) & 1, s_abort, f.limit);
-          const float* const dex = reinterpret_cast<const float*>(smem + L::OFF_DEX) + (seq & 1) * 256;
-          const float* const own = reinterpret_cast<const float*>(smem + L::OFF_OWN) + (seq & 1) * 256;
+          if (!fail) fail = !wait_bar(bar(L::B_DEX + seq % L::DEEP), (seq / L::DEEP) & 1, s_abort, f.limit);
+          const float* const dex = reinterpret_cast<const float*>(smem + L::OFF_DEX) + seq % L::DEEP * 256;
+          const float* const own = reinterpret_cast<const float*>(smem + L::OFF_OWN) + seq % L::DEEP * 256;
           const float d = dex[r128] + dex[128 + r128], nl = own[r128];
           fix = -own[128 + r128] - d;
           if (valid) {
