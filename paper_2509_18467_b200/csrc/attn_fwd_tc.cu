@@ -56,13 +56,16 @@ struct FwdLay {
   static constexpr int NQ = D == 64 ? 2 : 1;                     // items whose Q tiles fit
   static constexpr uint32_t OUT = 128 * 128;                     // a warpgroup's outputs on their way: 64 channels (or 32 in fp32)
   static constexpr int SLOTS = 4;                                // items on their way
-  static constexpr uint32_t OFF_Q = 0, OFF_RING = NQ * NT * TILE, OFF_OUT = OFF_RING + ST * KT, OFF_ML = OFF_OUT + OUT, OFF_LIST = OFF_ML + 2 * NT * 128 * 8,
+  // Items whose (maximum, sum) are on their way from the softmax to the outputs: scores go up to an item ahead of the products, so that
+  // with one key tile each the softmax may be done with items i, i + 1 and i + 2 before item i's outputs are taken up.
+  static constexpr int DEEP = 4;
+  static constexpr uint32_t OFF_Q = 0, OFF_RING = NQ * NT * TILE, OFF_OUT = OFF_RING + ST * KT, OFF_ML = OFF_OUT + OUT, OFF_LIST = OFF_ML + DEEP * NT * 128 * 8,
                             OFF_ITEM = OFF_LIST + BAD_MAX * 4, OFF_ASK = OFF_ITEM + SLOTS * 64, OFF_BAR = OFF_ASK + 16;
   static constexpr uint32_t BYTES = OFF_BAR + 512;
   static constexpr int THREADS = NT * 128 + 192;                 // softmax, outputs, copies, products
   // mbarriers
   static constexpr int B_Q = 0, B_QE = NQ, B_FULL = 2 * NQ, B_EMPTY = B_FULL + ST, B_S = B_EMPTY + ST, B_P = B_S + 2 * NT, B_O = B_P + 2 * NT, B_OE = B_O + 2 * NT,
-                       B_ML = B_OE + NT, B_ITEM = B_ML + NT, B_ITEME = B_ITEM + SLOTS, B_ASK = B_ITEME + SLOTS, NBAR = B_ASK + 1;
+                       B_ML = B_OE + NT, B_ITEM = B_ML + NT * DEEP, B_ITEME = B_ITEM + SLOTS, B_ASK = B_ITEME + SLOTS, NBAR = B_ASK + 1;
   static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 512 && fwd_smem<D, 4, 128>() <= OFF_LIST && NT * (128 + D) <= 512, "shared memory, tensor memory");
 };
 
@@ -128,8 +131,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         mbar_init(bar(L::B_O + 2 * i + u), 1);   // (a softmax warp may be two products ahead: a barrier of one phase bit would mislead it)
       }
       mbar_init(bar(L::B_OE + i), 128);
-      mbar_init(bar(L::B_ML + i), 128);
     }
+    for (int i = 0; i < NT * L::DEEP; ++i) mbar_init(bar(L::B_ML + i), 128);
     for (int i = 0; i < L::SLOTS; ++i) {
       mbar_init(bar(L::B_ITEM + i), 1);
       mbar_init(bar(L::B_ITEME + i), 13);   // (warps of softmax and outputs, and the product thread)
@@ -452,8 +455,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         mbar_arrive(bar(L::B_P + 2 * i + (step & 1)));
       }
       if (!ok) break;
-      reinterpret_cast<float2*>(smem + L::OFF_ML)[(seq & 1) * 256 + i * 128 + (tid & 127)] = make_float2(m, l);
-      mbar_arrive(bar(L::B_ML + i));
+      reinterpret_cast<float2*>(smem + L::OFF_ML)[seq % L::DEEP * 256 + i * 128 + (tid & 127)] = make_float2(m, l);
+      mbar_arrive(bar(L::B_ML + seq % L::DEEP * NT + i));
       ++seq;
     }
   } else {
@@ -477,10 +480,10 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const bool valid = t < T;
         float m = -INFINITY, l = 0.f;
         if (n > 0) {
-          fail = !wait_bar(bar(L::B_ML + i), seq & 1, s_abort, f.limit) ||
+          fail = !wait_bar(bar(L::B_ML + seq % L::DEEP * NT + i), (seq / L::DEEP) & 1, s_abort, f.limit) ||
                  !wait_bar(bar(L::B_O + 2 * i + (step - 1 & 1)), (step - 1) >> 1 & 1, s_abort, f.limit);
           __syncwarp();
-          const float2 ml = reinterpret_cast<const float2*>(smem + L::OFF_ML)[(seq & 1) * 256 + i * 128 + r128];
+          const float2 ml = reinterpret_cast<const float2*>(smem + L::OFF_ML)[seq % L::DEEP * 256 + i * 128 + r128];
           m = ml.x;
           l = ml.y;
           tc_fence_after_sync();

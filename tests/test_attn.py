@@ -358,6 +358,27 @@ def test_long_sequence_on_its_last_rows(d, kw):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T,window", [(50, 0), (1000, 1)])
+def test_many_items_of_one_tile(T, window, d):
+    """Thousands of items that meet one or two tiles of keys each: the roles of a block are then several items apart."""
+    B, H, H_kv = (1500, 4, 2) if T == 50 else (40, 8, 4)
+    q, k, v, dO = [draw((B, T, h, d), i, "bf16") for i, h in enumerate((H, H_kv, H_kv, H))]
+    p = api.attn_params(B, T, H, H_kv, d, window=window)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for again in range(3):
+        r = api.lawcat_attn_fwd(p, q, k, v, dev_status=status)
+        r.update(api.lawcat_attn_bwd(p, q, k, v, r["o"], r["lse"], dO, dev_status=status))
+        assert int(status.item()) == 0
+        for b in range(0, B, 100 if T == 50 else 10):
+            s = slice(b, b + 20 if T == 50 else b + 2)
+            ref = attention(q[s], k[s], v[s], visible(T, T, 1, window, B=len(q[s])), float(torch.tensor(d ** -0.5)), 0.0, None, dO[s], r["o"][s])
+            err = dict(ref["grad_err"](U16, U16), o=ref["o_sum"] + U16 * ref["o_mag"], lse=ref["lse_err"])
+            for n in ("o", "lse", "dq", "dk", "dv"):
+                check(r[n][s], ref[n], err[n], U32 if n == "lse" else U16, n)
+
+
+@pytest.mark.gpu
 def test_two_calls_at_once():
     """Different calls on two streams, many blocks each, over and over: the results of the calls one after the other."""
     T, H, H_kv, d = 700, 8, 2, 64
