@@ -51,6 +51,7 @@ struct Sequences {
 
 // rows[b][t] = the keys that query t sees, and keys[b][j] = the queries that see key j
 __global__ void attn_rows_kernel(const __grid_constant__ Sequences s, const attn::Mask m, int2* rows, int2* keys) {
+  attn::behind_last_kernel();
   const int i = blockIdx.x * blockDim.x + threadIdx.x;
   if (s.docs) {  // one packed batch: the launch's sequences cover tokens [start[0], start[n])
     const int t = s.start[0] + i;
@@ -96,7 +97,7 @@ int fill_rows(const lawcat_attn_params* p, const int32_t* cu, const int32_t* pre
     const int tokens = cu ? s.start[s.n] - s.start[0] : keys && m.T_k > m.T ? m.T_k : m.T;
     if (!tokens) continue;
     const dim3 grid((unsigned)((tokens + 255) / 256), cu ? 1u : (unsigned)s.n);
-    LAWCAT_LAUNCH("attn_rows", stream, attn_rows_kernel<<<grid, 256, 0, stream>>>(s, m, rows, keys));
+    LAWCAT_LAUNCH("attn_rows", stream, launch_behind(attn_rows_kernel, grid, dim3(256), 0, stream, s, m, rows, keys));
     LAWCAT_CHECK_LAUNCH();
   }
   m.rows = rows;

@@ -168,6 +168,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
     tma_prefetch_desc(&tm_b1);
     tma_prefetch_desc(&tm_b2);
   }
+  behind_last_kernel();
   if (warp == 12) {
     tmem_alloc(sb + L::OFF_BAR + 8 * L::NBAR, 512);
     tmem_relinquish();
@@ -595,7 +596,7 @@ static int bwd_tc(const AttnCall& c) {
   f.limit = wait_limit();
   order_tiles(c, f);
   LAWCAT_LAUNCH(KV ? "attn_dkdv_tc" : "attn_dq_tc", c.stream,
-                kernel<<<(unsigned)blocks, L::THREADS, L::BYTES, c.stream>>>(KV ? k : q, KV ? v : g, KV ? q : k, KV ? g : v, o1, o2, f));
+                launch_behind(kernel, dim3((unsigned)blocks), dim3(L::THREADS), L::BYTES, c.stream, KV ? k : q, KV ? v : g, KV ? q : k, KV ? g : v, o1, o2, f));
   LAWCAT_CHECK_LAUNCH();
   return LAWCAT_OK;
 }

@@ -164,6 +164,7 @@ __global__ void __launch_bounds__(DEC_THREADS) attn_decode_kernel(const DecArgs 
   const int G = a.H / a.H_kv, HG = (G + HB - 1) / HB;
   const int part = blockIdx.x % a.parts, hg = blockIdx.x / a.parts % HG, bg = blockIdx.x / a.parts / HG;
   const int b = bg / a.H_kv, g = bg % a.H_kv, h0 = g * G + hg * HB, nh = min(HB, G - hg * HB);
+  behind_last_kernel();
   const int pos = a.pos[b];
   int n = pos < 0 ? 0 : min(pos, a.C - 1) + 1;                         // keys that are seen: positions pos - n + 1 ... pos
   if (a.window && n > a.window) n = a.window;
@@ -283,6 +284,7 @@ __global__ void __launch_bounds__(128) attn_decode_join_kernel(const DecArgs a) 
   constexpr int NC = D / 32 > 0 ? D / 32 : 1;
   __shared__ float s_acc[4][D], s_l[4];
   const int bh = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  behind_last_kernel();
   const float* w = a.part + (size_t)bh * a.parts * (D + 2);
   float m = -INFINITY;
   for (int i = lane; i < a.parts; i += 32) m = fmaxf(m, w[(size_t)i * (D + 2)]);
@@ -331,6 +333,7 @@ __global__ void __launch_bounds__(256) attn_quant_kernel(const QuantArgs a) {
   const int bg = quot(blockIdx.x, a.chunks), b = quot(bg, a.heads), g = rest(bg, b, a.heads);
   const int t0 = rest(blockIdx.x, bg, a.chunks) * quant_tokens(D) + (int)threadIdx.x / V8, c0 = threadIdx.x % V8 * 8;
   const bool is_v = blockIdx.y;
+  behind_last_kernel();
   const int p0 = a.pos[b], first = p0 < 0 ? 0 : rest(p0, quot(p0, a.slots), a.slots);
   T* const rows = (T*)(is_v ? a.v : a.k) + (((size_t)b * a.T) * a.H_kv + g) * D + c0;
   uint8_t* const q = is_v ? a.vq : a.kq;
@@ -404,7 +407,7 @@ int launch_attn_decode_join(const attn::DecArgs& a, int d, int dtype, cudaStream
     auto go = [&](auto t) -> int {
       using T = decltype(t);
       LAWCAT_LAUNCH("attn_decode_join", stream,
-                    attn::attn_decode_join_kernel<T, D><<<(unsigned)(a.B * a.H), 128, 0, stream>>>(a));
+                    launch_behind(attn::attn_decode_join_kernel<T, D>, dim3((unsigned)(a.B * a.H)), dim3(128), 0, stream, a));
       LAWCAT_CHECK_LAUNCH();
       return LAWCAT_OK;
     };
@@ -426,7 +429,7 @@ int launch_attn_decode(const AttnDecode& c) {
       const size_t sm = sizeof(float) * ((2 * attn::TK + attn::HB) * (D + 4) + attn::HB * attn::TK + attn::HB);
       if (int r = grant_smem<attn::attn_decode_kernel<T, D, Q4>>(sm)) return r;
       LAWCAT_LAUNCH("attn_decode", c.stream,
-                    attn::attn_decode_kernel<T, D, Q4><<<(unsigned)blocks, attn::DEC_THREADS, sm, c.stream>>>(a));
+                    launch_behind(attn::attn_decode_kernel<T, D, Q4>, dim3((unsigned)blocks), dim3(attn::DEC_THREADS), sm, c.stream, a));
       LAWCAT_CHECK_LAUNCH();
       return a.parts > 1 ? launch_attn_decode_join(a, c.d, c.dtype, c.stream) : (int)LAWCAT_OK;
     };
@@ -446,9 +449,9 @@ int launch_attn_quant(const AttnDecode& c, int T, bool write) {
       using U = decltype(t);
       const dim3 grid((unsigned)n, 2);
       if (write) {
-        LAWCAT_LAUNCH("attn_quantize", c.stream, attn::attn_quant_kernel<U, D, true><<<grid, 256, 0, c.stream>>>(a));
+        LAWCAT_LAUNCH("attn_quantize", c.stream, launch_behind(attn::attn_quant_kernel<U, D, true>, grid, dim3(256), 0, c.stream, a));
       } else {
-        LAWCAT_LAUNCH("attn_dequantize", c.stream, attn::attn_quant_kernel<U, D, false><<<grid, 256, 0, c.stream>>>(a));
+        LAWCAT_LAUNCH("attn_dequantize", c.stream, launch_behind(attn::attn_quant_kernel<U, D, false>, grid, dim3(256), 0, c.stream, a));
       }
       LAWCAT_CHECK_LAUNCH();
       return LAWCAT_OK;

@@ -103,6 +103,7 @@ attn_step_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   const int G = a.H / a.H_kv, HG = (G + HPB - 1) / HPB;
   const int part = blockIdx.x % a.parts, hg = blockIdx.x / a.parts % HG, bg = blockIdx.x / a.parts / HG;
   const int b = bg / a.H_kv, g = bg % a.H_kv, h0 = g * G + hg * HPB, nh = min(HPB, G - hg * HPB);
+  behind_last_kernel();
   const int pos = a.pos[b];
   const Arc arc = arc_of(pos, a.C, a.window);
   const int per = (arc.count + a.parts - 1) / a.parts, k0 = min(arc.count, part * per), n = min(arc.count - k0, per);
@@ -338,6 +339,7 @@ attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, in
   const int G = a.H / a.H_kv, HG = (G + HPB - 1) / HPB;
   const int part = blockIdx.x % a.parts, hg = blockIdx.x / a.parts % HG, bg = blockIdx.x / a.parts / HG;
   const int b = bg / a.H_kv, g = bg % a.H_kv, h0 = g * G + hg * HPB, nh = min(HPB, G - hg * HPB);
+  behind_last_kernel();
   const int pos = a.pos[b];
   const Arc arc = arc_of(pos, a.C, a.window);
   const int per = (arc.count + a.parts - 1) / a.parts, k0 = min(arc.count, part * per), n = min(arc.count - k0, per);
@@ -655,7 +657,7 @@ static int step_tc(const AttnDecode& c, const DecArgs& a, unsigned blocks) {
     return LAWCAT_ERR_CUDA;
   constexpr auto kernel = attn_step_tc_kernel<D, HPB>;
   if (int r = grant_smem<kernel>(L::BYTES)) return r;
-  LAWCAT_LAUNCH("attn_decode_tc", c.stream, kernel<<<blocks, L::THREADS, L::BYTES, c.stream>>>(tk, tv, a, wait_limit(), c.dev_status));
+  LAWCAT_LAUNCH("attn_decode_tc", c.stream, launch_behind(kernel, dim3(blocks), dim3(L::THREADS), L::BYTES, c.stream, tk, tv, a, wait_limit(), c.dev_status));
   LAWCAT_CHECK_LAUNCH();
   return a.parts > 1 ? launch_attn_decode_join(a, D, LAWCAT_BF16, c.stream) : (int)LAWCAT_OK;
 }
@@ -665,7 +667,7 @@ static int step_quant_tc(const AttnDecode& c, const DecArgs& a, unsigned blocks)
   using L = QuantLay<D, HPB>;
   constexpr auto kernel = attn_step_quant_tc_kernel<D, HPB>;
   if (int r = grant_smem<kernel>(L::BYTES)) return r;
-  LAWCAT_LAUNCH("attn_decode_quant_tc", c.stream, kernel<<<blocks, 128, L::BYTES, c.stream>>>(a, wait_limit(), c.dev_status));
+  LAWCAT_LAUNCH("attn_decode_quant_tc", c.stream, launch_behind(kernel, dim3(blocks), dim3(128), L::BYTES, c.stream, a, wait_limit(), c.dev_status));
   LAWCAT_CHECK_LAUNCH();
   return a.parts > 1 ? launch_attn_decode_join(a, D, LAWCAT_BF16, c.stream) : (int)LAWCAT_OK;
 }

@@ -20,6 +20,7 @@ struct Parts {
 
 template <typename T, int D, int RM>
 __global__ void __launch_bounds__(THREADS) attn_fwd_exact_kernel(const Args a, int tiles, const Parts p) {
+  behind_last_kernel();
   extern __shared__ __align__(16) float sm[];
   const int part = blockIdx.x % p.n, x = blockIdx.x / p.n, bh = x % (a.B * a.H), b = bh / a.H;
   const int t0 = (tiles - 1 - x / (a.B * a.H)) * 16 * RM;  // (under a causal mask the longest rows first)
@@ -36,6 +37,7 @@ __global__ void __launch_bounds__(THREADS) attn_fwd_exact_kernel(const Args a, i
 // dq, and (lse log2e, dO.o) of every query for the other kernel
 template <typename T, int D, int RM>
 __global__ void __launch_bounds__(THREADS) attn_dq_exact_kernel(const Args a, int tiles, const Parts p) {
+  behind_last_kernel();
   extern __shared__ __align__(16) float sm[];
   const int part = blockIdx.x % p.n, x = blockIdx.x / p.n, bh = x % (a.B * a.H);
   const int t0 = (tiles - 1 - x / (a.B * a.H)) * 16 * RM;
@@ -44,6 +46,7 @@ __global__ void __launch_bounds__(THREADS) attn_dq_exact_kernel(const Args a, in
 
 template <typename T, int D, int RM>
 __global__ void __launch_bounds__(THREADS) attn_dkdv_exact_kernel(const Args a, int tiles, const Parts p) {
+  behind_last_kernel();
   extern __shared__ __align__(16) float sm[];
   const int part = blockIdx.x % p.n, x = blockIdx.x / p.n, bg = x % (a.B * a.H_kv);
   const size_t at = ((size_t)part * a.B * a.H_kv + bg) * a.mask.T_k * D;
@@ -53,6 +56,7 @@ __global__ void __launch_bounds__(THREADS) attn_dkdv_exact_kernel(const Args a, 
 // o and lse of every query from its parts; one warp per (batch, token, head)
 template <typename T, int D>
 __global__ void __launch_bounds__(256) attn_fwd_join_kernel(const Args a, const Parts p) {
+  behind_last_kernel();
   const size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) >> 5, rows = (size_t)a.B * a.mask.T * a.H;
   const int lane = threadIdx.x & 31;
   if (row >= rows) return;
@@ -85,6 +89,7 @@ __global__ void __launch_bounds__(256) attn_fwd_join_kernel(const Args a, const 
 // out [B, rows, heads, D] = the sum of the parts [n, B, heads, rows, D], of x and (gridDim.y = 2) of y; four channels per thread
 template <typename T, int D>
 __global__ void __launch_bounds__(256) attn_sum_kernel(const Parts p, T* out_x, T* out_y, int B, int heads, int rows) {
+  behind_last_kernel();
   const float* const x = blockIdx.y ? p.y : p.x;
   T* const out = blockIdx.y ? out_y : out_x;
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, all = (size_t)B * heads * rows * (D / 4);
@@ -133,7 +138,7 @@ static int fwd(const AttnCall& c, const Parts& p) {
   if (!n) return LAWCAT_ERR_UNSUPPORTED;
   constexpr size_t sm = fwd_smem<D, RM, THREADS>();
   if (int r = grant_smem<attn_fwd_exact_kernel<T, D, RM>>(sm)) return r;
-  LAWCAT_LAUNCH("attn_fwd_exact", c.stream, attn_fwd_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles, p));
+  LAWCAT_LAUNCH("attn_fwd_exact", c.stream, launch_behind(attn_fwd_exact_kernel<T, D, RM>, dim3(n), dim3(THREADS), sm, c.stream, c.a, tiles, p));
   LAWCAT_CHECK_LAUNCH();
   return p.n > 1 ? launch_attn_fwd_join(c, p.n, p.x, p.ml) : (int)LAWCAT_OK;
 }
@@ -142,7 +147,7 @@ template <typename T, int D>
 static int sum(const AttnCall& c, const Parts& p, void* out_x, void* out_y, int heads, int rows) {
   const long long n = ((long long)c.a.B * heads * rows * (D / 4) + 255) / 256;
   LAWCAT_LAUNCH("attn_sum", c.stream,
-                attn_sum_kernel<T, D><<<dim3((unsigned)n, out_y ? 2 : 1), 256, 0, c.stream>>>(p, (T*)out_x, (T*)out_y, c.a.B, heads, rows));
+                launch_behind(attn_sum_kernel<T, D>, dim3((unsigned)n, out_y ? 2 : 1), dim3(256), 0, c.stream, p, (T*)out_x, (T*)out_y, c.a.B, heads, rows));
   LAWCAT_CHECK_LAUNCH();
   return LAWCAT_OK;
 }
@@ -154,7 +159,7 @@ static int dq(const AttnCall& c, const Parts& p) {
   if (!n) return LAWCAT_ERR_UNSUPPORTED;
   constexpr size_t sm = dq_smem<D, RM, THREADS>();
   if (int r = grant_smem<attn_dq_exact_kernel<T, D, RM>>(sm)) return r;
-  LAWCAT_LAUNCH("attn_dq_exact", c.stream, attn_dq_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles, p));
+  LAWCAT_LAUNCH("attn_dq_exact", c.stream, launch_behind(attn_dq_exact_kernel<T, D, RM>, dim3(n), dim3(THREADS), sm, c.stream, c.a, tiles, p));
   LAWCAT_CHECK_LAUNCH();
   return p.n > 1 ? sum<T, D>(c, p, c.a.dq, nullptr, c.a.H, c.a.mask.T) : (int)LAWCAT_OK;
 }
@@ -166,7 +171,7 @@ static int dkdv(const AttnCall& c, const Parts& p) {
   if (!n) return LAWCAT_ERR_UNSUPPORTED;
   constexpr size_t sm = dkdv_smem<D, RM, THREADS>();
   if (int r = grant_smem<attn_dkdv_exact_kernel<T, D, RM>>(sm)) return r;
-  LAWCAT_LAUNCH("attn_dkdv_exact", c.stream, attn_dkdv_exact_kernel<T, D, RM><<<n, THREADS, sm, c.stream>>>(c.a, tiles, p));
+  LAWCAT_LAUNCH("attn_dkdv_exact", c.stream, launch_behind(attn_dkdv_exact_kernel<T, D, RM>, dim3(n), dim3(THREADS), sm, c.stream, c.a, tiles, p));
   LAWCAT_CHECK_LAUNCH();
   return p.n > 1 ? sum<T, D>(c, p, c.a.dk, c.a.dv, c.a.H_kv, c.a.mask.T_k) : (int)LAWCAT_OK;
 }
@@ -192,7 +197,7 @@ int launch_attn_fwd_join(const AttnCall& c, int parts, const float* part_o, cons
     constexpr int D = decltype(d)::value;
     const attn::Parts p{parts, const_cast<float*>(part_o), nullptr, const_cast<float2*>(part_ml)};
     const size_t n = (size_t)c.a.B * c.a.H * c.a.mask.T;
-    LAWCAT_LAUNCH("attn_fwd_join", c.stream, attn::attn_fwd_join_kernel<T, D><<<(unsigned)((n + 7) / 8), 256, 0, c.stream>>>(c.a, p));
+    LAWCAT_LAUNCH("attn_fwd_join", c.stream, launch_behind(attn::attn_fwd_join_kernel<T, D>, dim3((unsigned)((n + 7) / 8)), dim3(256), 0, c.stream, c.a, p));
     LAWCAT_CHECK_LAUNCH();
     return LAWCAT_OK;
   });

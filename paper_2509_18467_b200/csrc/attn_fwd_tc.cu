@@ -145,6 +145,7 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
   }
+  behind_last_kernel();
   if (warp == NT * 4 + 4) {
     tmem_alloc(sb + L::OFF_BAR + 8 * L::NBAR, 512);
     tmem_relinquish();
@@ -610,7 +611,7 @@ static int fwd_tc(const AttnCall& c, const FwdPlan& pl, void* ws) {
   }
   constexpr auto kernel = attn_fwd_tc_kernel<D, CAP, BIAS>;
   if (int r = grant_smem<kernel>(L::BYTES)) return r;
-  LAWCAT_LAUNCH("attn_fwd_tc", c.stream, kernel<<<(unsigned)pl.blocks, L::THREADS, L::BYTES, c.stream>>>(tq, tk, tv, to, f));
+  LAWCAT_LAUNCH("attn_fwd_tc", c.stream, launch_behind(kernel, dim3((unsigned)pl.blocks), dim3(L::THREADS), L::BYTES, c.stream, tq, tk, tv, to, f));
   LAWCAT_CHECK_LAUNCH();
   return pl.parts > 1 ? launch_attn_fwd_join(c, pl.parts, f.part_o, f.part_ml) : (int)LAWCAT_OK;
 }
