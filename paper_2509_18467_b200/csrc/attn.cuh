@@ -12,7 +12,8 @@ namespace attn {
 
 // Every kernel here is launched behind the kernel in front of it on the stream (launch_behind): its launch overlaps that one's end.
 // Before the first access to memory, and before tensor memory is taken, which the kernel in front may still be waiting for.
-// (512 tokens, 4 heads of 64 in fp32, forward and gradients, six kernels: 79 us without, 69 us so; a step over 32768 slots in 4 bits and its join 39 and 32 us.)
+// (512 tokens, 4 heads of 64 in fp32, forward and gradients, six kernels: 79 us without, 69 us so; a step over 32768 slots in 4 bits and its join 39 and 32;
+// 77 queries over 8192 keys and their join 37 and 33. With a trigger at the start of kernels that share out their work, 72, 32 and 37.)
 __device__ __forceinline__ void behind_last_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 constexpr float LOG2E = 1.4426950408889634f;
