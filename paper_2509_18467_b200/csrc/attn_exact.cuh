@@ -4,7 +4,10 @@
 //
 // All three are the same tiling: NTHR threads own BM rows (queries; keys for dk/dv) of one head in shared memory and walk the
 // other side in tiles of 64 rows. A thread, one of NTHR / 16 x 16, holds RM rows x 4 columns of the scores and RM rows x D / 16
-// channels of what it accumulates, so that a row's statistics are shuffles among 16 lanes. The running maximum and sum of the
+// channels of what it accumulates, so that a row's statistics are shuffles among 16 lanes. (1500 tokens, 32/8 heads of 64 in fp32:
+// forward 310 us, 18 TFLOP/s, dQ 430, dK and dV 636. Loads from shared memory take 77 % of their pipe in the forward, multiply-adds 54 %.
+// With 8 lanes to a row, 4 x 8 scores a thread and half the loads, half as many warps hide them worse: 351, 452 and 548 us, and at
+// width 128 808, 1089 and 1999 in place of 640, 820 and 1160.) The running maximum and sum of the
 // softmax stay in registers: one pass over the keys.
 // The gradients take two kernels, one per side, each recomputing the scores: the sums over queries and over keys then both
 // stay in registers of one block, in one order (no atomics, the same bits every time), at 14 instead of 10 D flop per pair.
