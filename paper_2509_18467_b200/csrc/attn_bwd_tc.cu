@@ -419,10 +419,15 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
                 f2_unpack(y, p0, p1);
                 p0 = ex2f(p0);
                 p1 = ex2f(p1);
-                float g0 = p[c], g1 = p[c + 1], f0 = 1.f, f1 = 1.f;
+                float g0 = p[c], g1 = p[c + 1], f0 = 1.f, f1 = 1.f, e0, e1;
                 if (CAP) f2_unpack(fac, f0, f1);
                 if (decltype(some)::value) {
                   const bool v0 = (uint32_t)(c - rel) < len, v1 = (uint32_t)(c + 1 - rel) < len;
+                  if (KV) {   // (-D of a query behind the last is whatever the scratch held)
+                    f2_unpack(d, e0, e1);
+                    g0 += e0;
+                    g1 += e1;
+                  }
                   p0 = v0 ? p0 : 0.f;
                   g0 = v0 ? g0 : 0.f;
                   f0 = v0 ? f0 : 0.f;
@@ -433,7 +438,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
                 const uint64_t pp = f2_pack(p0, p1), gg = f2_pack(g0, g1);
                 if (!KV) dex = f2_fma(pp, gg, dex);
                 const uint64_t pf = CAP ? f2_mul(pp, f2_pack(f0, f1)) : pp;
-                const uint64_t dx = f2_mul(pf, f2_add(gg, d));
+                const uint64_t dx = f2_mul(pf, KV && decltype(some)::value ? gg : f2_add(gg, d));
                 float y0, y1;
                 f2_unpack(KV ? pp : pf, y0, y1);
                 s[c / 2] = __uint_as_float(pack_bf16(y0, y1));

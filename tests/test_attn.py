@@ -379,6 +379,26 @@ def test_many_items_of_one_tile(T, window, d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,exact", KINDS)
+@pytest.mark.parametrize("kw", [dict(T=200), dict(T=77, T_k=900), dict(T=150, causal=0, cap=9.0), dict(T=300, cu=[0, 90, 300])])
+def test_what_the_scratch_held_makes_no_difference(kw, dtype, exact):
+    """The same bits over scratch full of zeros and full of NaN (a row that came out not finite would be computed in another way)."""
+    T, T_k, cu = kw["T"], kw.get("T_k", kw["T"]), kw.get("cu")
+    B, H, H_kv, d = 1 if cu else 2, 4, 2, 64
+    q, k, v, dO = [draw((B, n, h, d), i, dtype) for i, (n, h) in enumerate(((T, H), (T_k, H_kv), (T_k, H_kv), (T, H)))]
+    p = api.attn_params(B, T, H, H_kv, d, T_k=T_k, dtype=dtype, exact=exact, causal=kw.get("causal", 1), cap=kw.get("cap", 0.0))
+    n = [api.lib().lawcat_attn_workspace_bytes(ctypes.byref(p), op) for op in (api.OP_ATTN_FWD, api.OP_ATTN_BWD)]
+    got = []
+    for fill in (0, 255):
+        ws = [torch.full((max(x, 1),), fill, dtype=torch.uint8, device="cuda") for x in n]
+        r = api.lawcat_attn_fwd(p, q, k, v, cu_seqlens=cu, ws=ws[0])
+        r.update(api.lawcat_attn_bwd(p, q, k, v, r["o"], r["lse"], dO, cu_seqlens=cu, ws=ws[1]))
+        got.append(r)
+    for x in got[0]:
+        assert torch.equal(got[0][x], got[1][x]), x
+
+
+@pytest.mark.gpu
 def test_two_calls_at_once():
     """Different calls on two streams, many blocks each, over and over: the results of the calls one after the other."""
     T, H, H_kv, d = 700, 8, 2, 64
