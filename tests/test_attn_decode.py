@@ -1,5 +1,6 @@
 """One step of softmax attention over a cache, in the storage type and in 4 bits, and the 4-bit cache itself, against 64 bits
 (attn_reference.py): rings that wrap, windows, slots that hold no token, sequences that are not there, every head grouping."""
+import ctypes
 import math
 
 import pytest
@@ -200,6 +201,25 @@ def test_quantize_values_that_are_not_finite():
         bad = bad.repeat_interleave(32, -1)
         assert torch.isnan(back[n][bad]).all()
         assert torch.equal(back[n][~bad], quantized(x)[3].float().bfloat16()[~bad])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("quant", [False, True])
+def test_what_the_scratch_held_makes_no_difference(quant, dtype):
+    """The same bits over scratch full of zeros and full of NaN, most parts of the slots without a key."""
+    B, C, H, H_kv, d = 4, 9000, 8, 2, 64
+    p = api.attn_params(B, 1, H, H_kv, d, T_k=C, dtype=dtype)
+    q, k, v = draw((B, H, d), 1, dtype, 1.5), draw((B, H_kv, d), 2, dtype), draw((B, H_kv, d), 3, dtype)
+    pos = torch.tensor([-1, 0, 700, 8999], dtype=torch.int32, device="cuda")
+    pasts = [draw((B, C, H_kv, d), 4 + i, dtype) for i in range(2)]
+    cache = api.quant_cache(p) if quant else tuple(pasts)
+    if quant:
+        api.lawcat_cache_quantize(api.attn_params(B, C, H, H_kv, d, T_k=C, dtype=dtype), *pasts, torch.zeros_like(pos), *cache)
+    n = api.lib().lawcat_attn_workspace_bytes(ctypes.byref(p), api.OP_ATTN_DECODE)
+    assert n > 0
+    f = api.lawcat_attn_decode_quant if quant else api.lawcat_attn_decode
+    got = [f(p, q, k, v, *[t.clone() for t in cache], pos, ws=torch.full((n,), fill, dtype=torch.uint8, device="cuda")) for fill in (0, 255)]
+    assert torch.equal(*got) and not got[0][0].any() and torch.isfinite(got[0]).all()
 
 
 @pytest.mark.parametrize("quant", [False, True])
