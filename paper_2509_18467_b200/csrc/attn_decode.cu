@@ -278,38 +278,61 @@ __global__ void __launch_bounds__(DEC_THREADS) attn_decode_kernel(const DecArgs 
   }
 }
 
-// The parts of a (sequence, head): four warps share them out, each at the common maximum, four parts' loads in flight.
-template <typename T, int D>
-__global__ void __launch_bounds__(128) attn_decode_join_kernel(const DecArgs a) {
-  constexpr int NC = D / 32 > 0 ? D / 32 : 1;
-  __shared__ float s_acc[4][D], s_l[4];
+// The parts of a (sequence, head): W warps share them out, each at the maximum of its own, four parts' loads in flight; then the warps'
+// sums at the common maximum.
+template <typename T, int D, int W>
+__global__ void __launch_bounds__(32 * W) attn_decode_join_kernel(const DecArgs a) {
+  constexpr int NC = D / 32 > 0 ? D / 32 : 1, U = 4;
+  __shared__ float s_acc[W][D], s_ml[W][2];
   const int bh = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   behind_last_kernel();
   const float* w = a.part + (size_t)bh * a.parts * (D + 2);
-  float m = -INFINITY;
-  for (int i = lane; i < a.parts; i += 32) m = fmaxf(m, w[(size_t)i * (D + 2)]);
-  m = warp_max(m);
-  const float base = m == -INFINITY ? 0.f : m;
-  float l = 0.f, acc[NC] = {};
-#pragma unroll 4
-  for (int i = warp; i < a.parts; i += 4) {
-    const float* x = w + (size_t)i * (D + 2);
-    const bool some = x[1] != 0.f;               // (a part without keys has written nothing else)
-    const float f = exp2f(x[0] - base);
-    l += some ? f * x[1] : 0.f;
+  float m = -INFINITY, l = 0.f, acc[NC] = {};
+  for (int i0 = warp; i0 < a.parts; i0 += U * W) {
+    float pm[U], pl[U], x[U][NC];
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-      if (lane + 32 * c < D) acc[c] += some ? f * x[2 + lane + 32 * c] : 0.f;
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * W;
+      const float* p = w + (size_t)i * (D + 2);
+      pm[u] = i < a.parts ? p[0] : -INFINITY;
+      pl[u] = i < a.parts ? p[1] : 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) x[u][c] = i < a.parts && lane + 32 * c < D ? p[2 + lane + 32 * c] : 0.f;
+    }
+    float n = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) n = fmaxf(n, pm[u]);
+    const float base = n == -INFINITY ? 0.f : n, f = exp2f(m - base);
+    m = n;
+    l *= f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[c] *= f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool some = pl[u] != 0.f;               // (a part without keys has written nothing else)
+      const float g = exp2f(pm[u] - base);
+      l += some ? g * pl[u] : 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) acc[c] += some ? g * x[u][c] : 0.f;
+    }
   }
 #pragma unroll
   for (int c = 0; c < NC; ++c)
     if (lane + 32 * c < D) s_acc[warp][lane + 32 * c] = acc[c];
-  if (lane == 0) s_l[warp] = l;
+  if (lane == 0) {
+    s_ml[warp][0] = m;
+    s_ml[warp][1] = l;
+  }
   __syncthreads();
-  l = s_l[0] + s_l[1] + s_l[2] + s_l[3];
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  for (int c = threadIdx.x; c < D; c += 128)
-    stf<T>((T*)a.o + (size_t)bh * D + c, (s_acc[0][c] + s_acc[1][c] + s_acc[2][c] + s_acc[3][c]) * inv);
+  const float top = warp_max(lane < W ? s_ml[lane][0] : -INFINITY), base = top == -INFINITY ? 0.f : top;
+  const float f = lane < W ? exp2f(s_ml[lane][0] - base) : 0.f, sum = warp_sum(lane < W ? f * s_ml[lane][1] : 0.f);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  for (int c = threadIdx.x; c < (D < 32 ? 32 : D); c += 32 * W) {
+    float o = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) o = fmaf(__shfl_sync(0xffffffffu, f, i), s_acc[i][c < D ? c : 0], o);
+    if (c < D) stf<T>((T*)a.o + (size_t)bh * D + c, o * inv);
+  }
 }
 
 // Rows of k and v [B, T, H_kv, D] to and from the slots (pos + t) mod C: memory-bound. A block has 8192 / D tokens of one (sequence,
@@ -406,8 +429,9 @@ int launch_attn_decode_join(const attn::DecArgs& a, int d, int dtype, cudaStream
     constexpr int D = decltype(dd)::value;
     auto go = [&](auto t) -> int {
       using T = decltype(t);
-      LAWCAT_LAUNCH("attn_decode_join", stream,
-                    launch_behind(attn::attn_decode_join_kernel<T, D>, dim3((unsigned)(a.B * a.H)), dim3(128), 0, stream, a));
+      const dim3 grid((unsigned)(a.B * a.H));
+      if (a.parts > 16) LAWCAT_LAUNCH("attn_decode_join", stream, launch_behind(attn::attn_decode_join_kernel<T, D, 16>, grid, dim3(512), 0, stream, a));
+      else LAWCAT_LAUNCH("attn_decode_join", stream, launch_behind(attn::attn_decode_join_kernel<T, D, 4>, grid, dim3(128), 0, stream, a));
       LAWCAT_CHECK_LAUNCH();
       return LAWCAT_OK;
     };
