@@ -66,17 +66,34 @@ __global__ void __launch_bounds__(256) attn_fwd_join_kernel(const Args a, const 
   constexpr int NC = D / 32 > 0 ? D / 32 : 1;
   const bool mine = lane * NC < D;
   float m = -INFINITY, l = 0.f, acc[NC] = {};
-  for (int i = lane; i < p.n; i += 32) m = fmaxf(m, p.ml[i * step + at].x);
-  m = warp_max(m);
-  const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll 4
-  for (int i = 0; i < p.n; ++i) {   // (a part without keys: maximum -infinity, sum and values zero)
-    const float2 ml = p.ml[i * step + at];
-    const float* x = p.x + (i * step + at) * D + (mine ? lane * NC : 0);
-    const float w = exp2f(ml.x - base);
-    l = fmaf(w, ml.y, l);
+  constexpr int U = 8;
+  using V = std::conditional_t<NC == 4, float4, std::conditional_t<NC == 2, float2, float>>;
+  for (int i0 = 0; i0 < p.n; i0 += U) {   // (eight parts' loads in flight)
+    float2 ml[U];
+    alignas(16) float x[U][NC];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) acc[c] = fmaf(w, x[c], acc[c]);
+    for (int u = 0; u < U; ++u) {
+      const bool there = i0 + u < p.n;
+      ml[u] = there ? p.ml[(i0 + u) * step + at] : make_float2(-INFINITY, 0.f);
+      V v{};
+      if (there && mine) v = *reinterpret_cast<const V*>(p.x + ((i0 + u) * step + at) * D + lane * NC);
+      *reinterpret_cast<V*>(x[u]) = v;
+    }
+    float n = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) n = fmaxf(n, ml[u].x);
+    const float base = n == -INFINITY ? 0.f : n, f = exp2f(m - base);
+    m = n;
+    l *= f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[c] *= f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {   // (a part without keys: maximum -infinity, sum and values zero)
+      const float w = exp2f(ml[u].x - base);
+      l = fmaf(w, ml[u].y, l);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) acc[c] = fmaf(w, x[u][c], acc[c]);
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T* o = (T*)a.o + row * D + lane * NC;
