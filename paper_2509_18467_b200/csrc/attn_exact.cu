@@ -132,18 +132,29 @@ static int rows_per_thread(int rows) { return rows <= 16 ? 1 : 4; }
 // Parts that a row block's `tiles` tiles are shared out into: as many as give every SM two blocks, four where the blocks differ in length
 // and there are fewer than that (1500 tokens, 32/8 heads of 64 in fp32, 192 blocks of keys: the gradients of K and V take 636 + 9 us,
 // 888 us with a block each; 4 x 300 tokens, 8 heads: the three kernels within 3 % either way).
-static int parts_of(int rows, long long n, long long tiles) {
-  const long long x = (rows + 63) / 64 * n, sms = sm_count();
-  if (x == 0 || x >= 4 * sms) return 1;
-  return (int)std::max(1LL, std::min(std::min(((x < sms ? 2 : 4) * sms + x - 1) / x, tiles), 16LL));
+// Where all blocks have the same tiles to walk or nearly so (`even`), of up to twice as many the number whose blocks fill the SMs' places
+// best in whole rounds (forward and gradients in fp32, 187 queries behind 1313 keys, 32/4 heads of 64: 446 -> 369 us; 1500 tokens without
+// a mask, 4 heads of 128: 732 -> 675; 1196 causal ones, whose blocks differ, would go from 266 to 275).
+static int parts_of(int rows, long long n, long long tiles, int resident, bool even) {
+  const long long x = (rows + 63) / 64 * n, sms = sm_count(), places = sms * resident, most = std::min(tiles, 16LL);
+  if (x == 0 || x >= 4 * sms || most < 2) return 1;
+  const long long least = std::min(((x < sms ? 2 : 4) * sms + x - 1) / x, most);
+  long long best = least;
+  auto rounds = [&](long long p) { return (x * p + places - 1) / places; };   // each a p-th of a block's work
+  for (long long p = least + 1; even && p <= std::min(2 * least, most); ++p)
+    if (rounds(p) * best * 100 < rounds(best) * p * 95) best = p;
+  return (int)best;
 }
-static int parts_q(const Mask& m, int B, int H) {
+static bool even(const Mask& m) { return !m.causal || m.off >= m.T; }
+// blocks that fit on an SM: of the gradients' kernels at width 128 one, of the others two
+static int resident(int d, bool gradients) { return gradients && d == 128 ? 1 : 2; }
+static int parts_q(const Mask& m, int B, int H, int d, bool gradients) {
   const long long keys = m.window && m.window < m.T_k ? std::min<long long>(m.T_k, (long long)m.window + 63) : m.T_k;
-  return parts_of(m.T, (long long)B * H, (keys + 63) / 64);
+  return parts_of(m.T, (long long)B * H, (keys + 63) / 64, resident(d, gradients), even(m));
 }
-static int parts_k(const Mask& m, int B, int H, int H_kv) {
+static int parts_k(const Mask& m, int B, int H, int H_kv, int d) {
   const long long queries = m.window && m.window < m.T ? std::min<long long>(m.T, (long long)m.window + 63) : m.T;
-  return parts_of(m.T_k, (long long)B * H_kv, (queries + 63) / 64 * (H / H_kv));
+  return parts_of(m.T_k, (long long)B * H_kv, (queries + 63) / 64 * (H / H_kv), resident(d, true), even(m));
 }
 // one part's sums behind another's: forward, queries, keys
 static size_t part_bytes(int parts, size_t rows, int d) { return parts == 1 ? 0 : align_up(sizeof(float) * parts * rows * d, 256); }
@@ -221,13 +232,13 @@ int launch_attn_fwd_join(const AttnCall& c, int parts, const float* part_o, cons
 }
 
 size_t attn_fwd_exact_workspace_bytes(const AttnCall& c) {
-  const int parts = attn::parts_q(c.a.mask, c.a.B, c.a.H);
+  const int parts = attn::parts_q(c.a.mask, c.a.B, c.a.H, c.d, false);
   const size_t rows = (size_t)c.a.B * c.a.H * c.a.mask.T;
   return parts == 1 ? 0 : attn::part_bytes(parts, rows, c.d) + align_up(sizeof(float2) * parts * rows, 256);
 }
 
 int launch_attn_fwd_exact(const AttnCall& c, void* ws) {
-  attn::Parts p{ws ? attn::parts_q(c.a.mask, c.a.B, c.a.H) : 1, (float*)ws, nullptr, nullptr};
+  attn::Parts p{ws ? attn::parts_q(c.a.mask, c.a.B, c.a.H, c.d, false) : 1, (float*)ws, nullptr, nullptr};
   if (p.n > 1) p.ml = (float2*)((char*)ws + attn::part_bytes(p.n, (size_t)c.a.B * c.a.H * c.a.mask.T, c.d));
   return attn::dispatch(c, [&](auto t, auto d) {
     using T = decltype(t);
@@ -237,14 +248,14 @@ int launch_attn_fwd_exact(const AttnCall& c, void* ws) {
 }
 
 size_t attn_bwd_exact_workspace_bytes(const AttnCall& c) {
-  const size_t q = attn::part_bytes(attn::parts_q(c.a.mask, c.a.B, c.a.H), (size_t)c.a.B * c.a.H * c.a.mask.T, c.d);
-  const size_t k = attn::part_bytes(attn::parts_k(c.a.mask, c.a.B, c.a.H, c.a.H_kv), (size_t)c.a.B * c.a.H_kv * c.a.mask.T_k, c.d);
+  const size_t q = attn::part_bytes(attn::parts_q(c.a.mask, c.a.B, c.a.H, c.d, true), (size_t)c.a.B * c.a.H * c.a.mask.T, c.d);
+  const size_t k = attn::part_bytes(attn::parts_k(c.a.mask, c.a.B, c.a.H, c.a.H_kv, c.d), (size_t)c.a.B * c.a.H_kv * c.a.mask.T_k, c.d);
   return std::max(q, 2 * k);
 }
 
 int launch_attn_bwd_exact(const AttnCall& c, void* ws) {
-  const attn::Parts pq{ws ? attn::parts_q(c.a.mask, c.a.B, c.a.H) : 1, (float*)ws, nullptr, nullptr};
-  attn::Parts pk{ws ? attn::parts_k(c.a.mask, c.a.B, c.a.H, c.a.H_kv) : 1, (float*)ws, nullptr, nullptr};
+  const attn::Parts pq{ws ? attn::parts_q(c.a.mask, c.a.B, c.a.H, c.d, true) : 1, (float*)ws, nullptr, nullptr};
+  attn::Parts pk{ws ? attn::parts_k(c.a.mask, c.a.B, c.a.H, c.a.H_kv, c.d) : 1, (float*)ws, nullptr, nullptr};
   if (pk.n > 1) pk.y = (float*)((char*)ws + attn::part_bytes(pk.n, (size_t)c.a.B * c.a.H_kv * c.a.mask.T_k, c.d));
   return attn::dispatch(c, [&](auto t, auto d) {
     using T = decltype(t);
