@@ -505,7 +505,8 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
       for (int x = 0; x < (KV ? 2 * D : D); x += 32) {
         const bool second = KV && x >= D;              // (dv)
         const int c = second ? x - D : x;
-        const uint32_t out = sb + L::OFF_OUT + (L::OUTS == 2 ? (x / 64 & 1) : 0) * L::OUT;
+        // (with two places stores take them in turn: dk and dv; dq, one store per item, by the item's number)
+        const uint32_t out = sb + L::OFF_OUT + (L::OUTS == 2 ? ((KV ? x / 64 : k) & 1) : 0) * L::OUT;
         const float mul = second ? 1.f : a.scale;
         float o[32];
         if (n > 0) {
@@ -527,7 +528,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
           for (int e = 0; e < 32; ++e) o[e] = 0.f;
         }
         if (c % 64 == 0) {
-          if (r128 == 0) {                             // (this place's last store has read it)
+          if (r128 == 0) {                             // (this place's last store has read it; the newest may be at the other place)
             if (L::OUTS == 2) tma_store_wait_read_1();
             else tma_store_wait_read();
           }
