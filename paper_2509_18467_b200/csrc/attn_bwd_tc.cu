@@ -483,7 +483,7 @@ attn_bwd_tc_kernel(const __grid_constant__ CUtensorMap tm_a1, const __grid_const
       const bool valid = r < rows;
       float fix = 0.f;   // dO.o - D
       if (n > 0) {
-        fail = !wait_bar(bar(L::B_ACC), seq & 1, s_abort, f.limit);
+        fail = !wait_bar(bar(L::B_ACC), seq & 1, s_abort, item_limit(f.limit, n));
         if (!KV) {
           if (!fail) fail = !wait_bar(bar(L::B_DEX + seq % L::DEEP), (seq / L::DEEP) & 1, s_abort, f.limit);
           const float* const dex = reinterpret_cast<const float*>(smem + L::OFF_DEX) + seq % L::DEEP * 256;

@@ -481,8 +481,8 @@ attn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const bool valid = t < T;
         float m = -INFINITY, l = 0.f;
         if (n > 0) {
-          fail = !wait_bar(bar(L::B_ML + seq % L::DEEP * NT + i), (seq / L::DEEP) & 1, s_abort, f.limit) ||
-                 !wait_bar(bar(L::B_O + 2 * i + (step - 1 & 1)), (step - 1) >> 1 & 1, s_abort, f.limit);
+          fail = !wait_bar(bar(L::B_ML + seq % L::DEEP * NT + i), (seq / L::DEEP) & 1, s_abort, item_limit(f.limit, n)) ||
+                 !wait_bar(bar(L::B_O + 2 * i + (step - 1 & 1)), (step - 1) >> 1 & 1, s_abort, item_limit(f.limit, n));
           __syncwarp();
           const float2 ml = reinterpret_cast<const float2*>(smem + L::OFF_ML)[seq % L::DEEP * 256 + i * 128 + r128];
           m = ml.x;

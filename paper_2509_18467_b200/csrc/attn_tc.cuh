@@ -40,6 +40,10 @@ __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile
   }
 }
 
+// The bound for a role that waits for the end of an item of n tiles: the others' bounds are on one step each, and tell this one when
+// something is lost; by itself an item may take as long as its tiles do (2 s for each 64 of them, which take 0.1 ms).
+__device__ __forceinline__ long long item_limit(long long limit, int n) { return limit * (1 + n / 64); }
+
 // n / d for 0 <= n < 2^31: items are numbered, and their digits are run-time sizes (a division proper costs as much as an exponential
 // of a whole row).
 struct FastDiv {

@@ -39,3 +39,29 @@ def test_gradients_of_short_and_empty_items(B, T, T_k, H, H_kv, window, d):
         err = dict(ref["grad_err"](U16, U16), o=ref["o_sum"] + U16 * ref["o_mag"], lse=ref["lse_err"])
         for n in ("o", "lse", "dq", "dk", "dv"):
             check(first[n][s], ref[n], err[n], U32 if n == "lse" else U16, f"{n} of sequence {b}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_bound_on_waits_is_not_one_on_an_item(d):
+    """Under a bound of 400000 clock cycles, a hundred times what a step takes and a small part of an item of 2200 tiles: a block whose
+    roles all go on is not one that has lost something, however long its item. (Which roles wait for an item's end depends on its
+    length alone: with the bound's usual value the same goes for items of some million tiles.)"""
+    T, H = 140001, 2
+    q, k, v, dO = [draw((1, T, h, d), i, "bf16") for i, h in enumerate((H, 1, 1, H))]
+    p = api.attn_params(1, T, H, 1, d)
+    want = gradients(p, q, k, v, dO)
+    torch.cuda.synchronize()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    api.test_set_wait_limit(400000)
+    try:
+        r = api.lawcat_attn_fwd(p, q, k, v, dev_status=status)
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0, "forward"
+        r.update(api.lawcat_attn_bwd(p, q, k, v, r["o"], r["lse"], dO, dev_status=status))
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0, "gradients"
+    finally:
+        api.test_set_wait_limit(0)
+    for n in want:
+        assert torch.equal(r[n], want[n]), n
