@@ -328,6 +328,10 @@ def lawcat_decode_step(p: Params, q_t, k_t, v_t, gate_t, w_q, w_k, W, S, z, cach
 def _attn_call(name, p, op, args, ws, stream, dev_status, nint=0):
     """op: the call's LAWCAT_OP_ATTN (its scratch is taken from torch's allocator when ws is None), or None for no scratch."""
     b = _binding or _bind()
+    if ws is not None:
+        b.expect("ws", ws)
+    if dev_status is not None:
+        b.expect("dev_status", dev_status)
     st = b.call(_addr[name], ctypes.addressof(p), 0 if op is None else _addr["lawcat_attn_workspace_bytes"], -1 if op is None else op,
                 args, ws, stream and stream.cuda_stream, dev_status, nint)
     if st != 0:
@@ -338,7 +342,8 @@ U8, I32 = 2, 3  # (beside F32 and BF16: the types that the native module's expec
 
 
 def _checked():
-    """The native module's expect(name, tensor, type, sizes...): the kernels trust sizes and types, None is skipped."""
+    """The native module's expect(name, tensor, type, sizes...): the kernels trust sizes, types and that everything is on the current
+    device; None is skipped."""
     return (_binding or _bind()).expect
 
 

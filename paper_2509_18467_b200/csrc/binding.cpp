@@ -1,6 +1,7 @@
 // CPython module behind api.py: turns torch tensors into the device pointers of a C entry point and calls it. A decode step
 // takes thirteen tensors; marshalling them through ctypes objects cost 25 us of host time per call, more than the kernels of
 // a small step, and about a microsecond here.
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/torch.h>
@@ -131,17 +132,18 @@ PyObject* empty(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   }
 }
 
-// expect(name, tensor, dtype, sizes...): ValueError unless the tensor (None passes) has these sizes and this type;
-// dtype: 0 fp32, 1 bf16, 2 uint8, 3 int32
+// expect(name, tensor, dtype, sizes...): ValueError unless the tensor (None passes) has these sizes and this type, and, where it is a
+// CUDA tensor, lies on the current device (a launch goes there, whichever device a pointer belongs to); dtype: 0 fp32, 1 bf16, 2 uint8,
+// 3 int32. expect(name, tensor): the device alone.
 PyObject* expect(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   static constexpr at::ScalarType types[] = {at::kFloat, at::kBFloat16, at::kByte, at::kInt};
   static const char* const names[] = {"float32", "bfloat16", "uint8", "int32"};
-  if (nargs < 3 || nargs > 8) {
-    PyErr_SetString(PyExc_TypeError, "expect(name, tensor, dtype, sizes...)");
+  if (nargs < 2 || nargs > 8) {
+    PyErr_SetString(PyExc_TypeError, "expect(name, tensor[, dtype, sizes...])");
     return nullptr;
   }
   if (args[1] == Py_None) Py_RETURN_NONE;
-  const long dt = PyLong_AsLong(args[2]);
+  const long dt = nargs > 2 ? PyLong_AsLong(args[2]) : 0;
   int64_t sz[5];
   for (Py_ssize_t i = 3; i < nargs; ++i) sz[i - 3] = PyLong_AsLongLong(args[i]);
   if (PyErr_Occurred()) return nullptr;
@@ -150,19 +152,31 @@ PyObject* expect(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return nullptr;
   }
   const at::Tensor& t = THPVariable_Unpack(args[1]);
-  if (t.scalar_type() == types[dt] && t.sizes() == at::IntArrayRef(sz, (size_t)nargs - 3)) Py_RETURN_NONE;
+  const char* name = PyUnicode_AsUTF8(args[0]);
+  if (!name) return nullptr;
+  if (t.is_cuda()) {
+    try {
+      const int here = c10::cuda::device_count() > 0 ? (int)c10::cuda::current_device() : 0;
+      if (t.device().index() != here) {
+        PyErr_Format(PyExc_ValueError, "%s: on device cuda:%d, the current device is cuda:%d", name, (int)t.device().index(), here);
+        return nullptr;
+      }
+    } catch (const std::exception& e) {
+      PyErr_SetString(PyExc_RuntimeError, e.what());
+      return nullptr;
+    }
+  }
+  if (nargs == 2 || (t.scalar_type() == types[dt] && t.sizes() == at::IntArrayRef(sz, (size_t)nargs - 3))) Py_RETURN_NONE;
   std::string want, got;
   for (Py_ssize_t i = 3; i < nargs; ++i) want += (i > 3 ? ", " : "") + std::to_string(sz[i - 3]);
   for (int64_t i = 0; i < t.dim(); ++i) got += (i ? ", " : "") + std::to_string(t.size(i));
-  const char* name = PyUnicode_AsUTF8(args[0]);
-  PyErr_Format(PyExc_ValueError, "%s: expected [%s] of %s, got [%s] of %s", name ? name : "tensor", want.c_str(), names[dt], got.c_str(),
-               c10::toString(t.scalar_type()));
+  PyErr_Format(PyExc_ValueError, "%s: expected [%s] of %s, got [%s] of %s", name, want.c_str(), names[dt], got.c_str(), c10::toString(t.scalar_type()));
   return nullptr;
 }
 
 PyMethodDef methods[] = {
     {"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, "call an entry point of the CUDA library"},
-    {"expect", (PyCFunction)(void (*)(void))expect, METH_FASTCALL, "check a tensor's sizes and type"},
+    {"expect", (PyCFunction)(void (*)(void))expect, METH_FASTCALL, "check a tensor's sizes, type and device"},
     {"empty", (PyCFunction)(void (*)(void))empty, METH_FASTCALL, "uninitialised tensor"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods};
