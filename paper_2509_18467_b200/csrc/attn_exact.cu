@@ -135,26 +135,53 @@ static int rows_per_thread(int rows) { return rows <= 16 ? 1 : 4; }
 // Where all blocks have the same tiles to walk or nearly so (`even`), of up to twice as many the number whose blocks fill the SMs' places
 // best in whole rounds (forward and gradients in fp32, 187 queries behind 1313 keys, 32/4 heads of 64: 446 -> 369 us; 1500 tokens without
 // a mask, 4 heads of 128: 732 -> 675; 1196 causal ones, whose blocks differ, would go from 266 to 275).
-static int parts_of(int rows, long long n, long long tiles, int resident, bool even) {
-  const long long x = (rows + 63) / 64 * n, sms = sm_count(), places = sms * resident, most = std::min(tiles, 16LL);
+// `resident`: the blocks that an SM holds of the kernel that is launched, asked of the runtime where it matters (in fp32 one of the
+// forward and of dQ at width 128 and of dK and dV from width 64 on, else two or more; 2 x 1057 tokens without a mask, 4/2 heads of 128 in
+// fp32, forward: four parts for two blocks an SM 190 us, three for one 177).
+template <typename F>
+static int parts_of(int rows, long long n, long long tiles, F resident, bool even) {
+  const long long x = (rows + 63) / 64 * n, sms = sm_count(), most = std::min(tiles, 16LL);
   if (x == 0 || x >= 4 * sms || most < 2) return 1;
   const long long least = std::min(((x < sms ? 2 : 4) * sms + x - 1) / x, most);
+  if (!even || least == most) return (int)least;
+  const long long places = sms * resident();
   long long best = least;
   auto rounds = [&](long long p) { return (x * p + places - 1) / places; };   // each a p-th of a block's work
-  for (long long p = least + 1; even && p <= std::min(2 * least, most); ++p)
+  for (long long p = least + 1; p <= std::min(2 * least, most); ++p)
     if (rounds(p) * best * 100 < rounds(best) * p * 95) best = p;
   return (int)best;
 }
 static bool even(const Mask& m) { return !m.causal || m.off >= m.T; }
-// blocks that fit on an SM: of the gradients' kernels at width 128 one, of the others two
-static int resident(int d, bool gradients) { return gradients && d == 128 ? 1 : 2; }
-static int parts_q(const Mask& m, int B, int H, int d, bool gradients) {
-  const long long keys = m.window && m.window < m.T_k ? std::min<long long>(m.T_k, (long long)m.window + 63) : m.T_k;
-  return parts_of(m.T, (long long)B * H, (keys + 63) / 64, resident(d, gradients), even(m));
+// Blocks of a kernel that an SM holds, from its registers and shared memory. Asked once per device, and the first answer stays (1 where
+// there is none): the scratch that a call asked for and its launch agree.
+template <auto KERNEL>
+static int resident(size_t smem) {
+  static std::atomic<int> known[64] = {};
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+    cudaGetLastError();
+    return 1;
+  }
+  if ((n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
+  if (grant_smem<KERNEL>(smem) != LAWCAT_OK || cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, KERNEL, THREADS, smem) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    n = 1;
+  }
+  int none = 0;
+  return known[dev].compare_exchange_strong(none, n) ? n : none;
 }
-static int parts_k(const Mask& m, int B, int H, int H_kv, int d) {
+// parts of a block of queries (its head's keys), and of a block of keys (the queries of its group's heads)
+template <typename F>
+static int parts_q(const AttnCall& c, F resident) {
+  const Mask& m = c.a.mask;
+  const long long keys = m.window && m.window < m.T_k ? std::min<long long>(m.T_k, (long long)m.window + 63) : m.T_k;
+  return parts_of(m.T, (long long)c.a.B * c.a.H, (keys + 63) / 64, resident, even(m));
+}
+template <typename F>
+static int parts_k(const AttnCall& c, F resident) {
+  const Mask& m = c.a.mask;
   const long long queries = m.window && m.window < m.T ? std::min<long long>(m.T, (long long)m.window + 63) : m.T;
-  return parts_of(m.T_k, (long long)B * H_kv, (queries + 63) / 64 * (H / H_kv), resident(d, true), even(m));
+  return parts_of(m.T_k, (long long)c.a.B * c.a.H_kv, (queries + 63) / 64 * (c.a.H / c.a.H_kv), resident, even(m));
 }
 // one part's sums behind another's: forward, queries, keys
 static size_t part_bytes(int parts, size_t rows, int d) { return parts == 1 ? 0 : align_up(sizeof(float) * parts * rows * d, 256); }
@@ -231,14 +258,41 @@ int launch_attn_fwd_join(const AttnCall& c, int parts, const float* part_o, cons
   });
 }
 
+namespace attn {
+static int parts_fwd(const AttnCall& c) {
+  return dispatch(c, [&](auto t, auto d) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value;
+    return rows_per_thread(c.a.mask.T) == 1 ? parts_q(c, [] { return resident<attn_fwd_exact_kernel<T, D, 1>>(fwd_smem<D, 1, THREADS>()); })
+                                            : parts_q(c, [] { return resident<attn_fwd_exact_kernel<T, D, 4>>(fwd_smem<D, 4, THREADS>()); });
+  });
+}
+static int parts_dq(const AttnCall& c) {
+  return dispatch(c, [&](auto t, auto d) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value;
+    return rows_per_thread(c.a.mask.T) == 1 ? parts_q(c, [] { return resident<attn_dq_exact_kernel<T, D, 1>>(dq_smem<D, 1, THREADS>()); })
+                                            : parts_q(c, [] { return resident<attn_dq_exact_kernel<T, D, 4>>(dq_smem<D, 4, THREADS>()); });
+  });
+}
+static int parts_dkdv(const AttnCall& c) {
+  return dispatch(c, [&](auto t, auto d) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value;
+    return rows_per_thread(c.a.mask.T_k) == 1 ? parts_k(c, [] { return resident<attn_dkdv_exact_kernel<T, D, 1>>(dkdv_smem<D, 1, THREADS>()); })
+                                              : parts_k(c, [] { return resident<attn_dkdv_exact_kernel<T, D, 4>>(dkdv_smem<D, 4, THREADS>()); });
+  });
+}
+}  // namespace attn
+
 size_t attn_fwd_exact_workspace_bytes(const AttnCall& c) {
-  const int parts = attn::parts_q(c.a.mask, c.a.B, c.a.H, c.d, false);
+  const int parts = attn::parts_fwd(c);
   const size_t rows = (size_t)c.a.B * c.a.H * c.a.mask.T;
   return parts == 1 ? 0 : attn::part_bytes(parts, rows, c.d) + align_up(sizeof(float2) * parts * rows, 256);
 }
 
 int launch_attn_fwd_exact(const AttnCall& c, void* ws) {
-  attn::Parts p{ws ? attn::parts_q(c.a.mask, c.a.B, c.a.H, c.d, false) : 1, (float*)ws, nullptr, nullptr};
+  attn::Parts p{ws ? attn::parts_fwd(c) : 1, (float*)ws, nullptr, nullptr};
   if (p.n > 1) p.ml = (float2*)((char*)ws + attn::part_bytes(p.n, (size_t)c.a.B * c.a.H * c.a.mask.T, c.d));
   return attn::dispatch(c, [&](auto t, auto d) {
     using T = decltype(t);
@@ -248,14 +302,14 @@ int launch_attn_fwd_exact(const AttnCall& c, void* ws) {
 }
 
 size_t attn_bwd_exact_workspace_bytes(const AttnCall& c) {
-  const size_t q = attn::part_bytes(attn::parts_q(c.a.mask, c.a.B, c.a.H, c.d, true), (size_t)c.a.B * c.a.H * c.a.mask.T, c.d);
-  const size_t k = attn::part_bytes(attn::parts_k(c.a.mask, c.a.B, c.a.H, c.a.H_kv, c.d), (size_t)c.a.B * c.a.H_kv * c.a.mask.T_k, c.d);
+  const size_t q = attn::part_bytes(attn::parts_dq(c), (size_t)c.a.B * c.a.H * c.a.mask.T, c.d);
+  const size_t k = attn::part_bytes(attn::parts_dkdv(c), (size_t)c.a.B * c.a.H_kv * c.a.mask.T_k, c.d);
   return std::max(q, 2 * k);
 }
 
 int launch_attn_bwd_exact(const AttnCall& c, void* ws) {
-  const attn::Parts pq{ws ? attn::parts_q(c.a.mask, c.a.B, c.a.H, c.d, true) : 1, (float*)ws, nullptr, nullptr};
-  attn::Parts pk{ws ? attn::parts_k(c.a.mask, c.a.B, c.a.H, c.a.H_kv, c.d) : 1, (float*)ws, nullptr, nullptr};
+  const attn::Parts pq{ws ? attn::parts_dq(c) : 1, (float*)ws, nullptr, nullptr};
+  attn::Parts pk{ws ? attn::parts_dkdv(c) : 1, (float*)ws, nullptr, nullptr};
   if (pk.n > 1) pk.y = (float*)((char*)ws + attn::part_bytes(pk.n, (size_t)c.a.B * c.a.H_kv * c.a.mask.T_k, c.d));
   return attn::dispatch(c, [&](auto t, auto d) {
     using T = decltype(t);
