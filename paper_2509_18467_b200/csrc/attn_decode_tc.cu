@@ -28,6 +28,8 @@
 // Rounding: weights to bf16 as an operand, o once; all else fp32.
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "attn_decode.cuh"
 #include "attn_tc.cuh"
 
@@ -308,6 +310,8 @@ attn_step_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 }
 
 // ---------------------------------------------------------------------------------------------------- 4 bits
+// blocks that share an SM (registers; tensor memory and shared memory leave room for as many)
+constexpr int quant_resident(int d, int heads) { return heads * (d / 32) <= 8 ? 6 : heads * (d / 32) <= 16 ? 4 : 3; }
 template <int D, int HPB>
 struct QuantLay {
   static constexpr int NG = D / 32, USED = HPB * NG, NCOL = USED < 16 ? 16 : USED;   // columns: head * NG + group
@@ -320,7 +324,7 @@ struct QuantLay {
 };
 
 template <int D, int HPB>
-__global__ void __launch_bounds__(128, HPB * (D / 32) <= 8 ? 6 : HPB * (D / 32) <= 16 ? 4 : 3)
+__global__ void __launch_bounds__(128, quant_resident(D, HPB))
 attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, int* dev_status) {
   using L = QuantLay<D, HPB>;
   constexpr int NG = L::NG, NCOL = L::NCOL, WPR = D / 8;  // words of codes per row
@@ -642,7 +646,7 @@ attn_step_quant_tc_kernel(const __grid_constant__ DecArgs a, long long limit, in
   if (warp == 0) tmem_dealloc(tmem, L::COLS);
 }
 
-// Heads per block, and parts of the keys: as many as give every SM four rounds of blocks, of at least four tiles of slots each.
+// Heads per block.
 static int step_heads(const AttnDecode& c) {
   const int G = c.H / c.H_kv;
   if (c.kq) return G <= 4 ? 4 : 8;
@@ -674,11 +678,15 @@ static int step_quant_tc(const AttnDecode& c, const DecArgs& a, unsigned blocks)
 
 }  // namespace attn
 
+// Parts of the slots: as many as give every SM four rounds of the blocks that share it, sixteen blocks at most, and no more than there are
+// pieces of 512 slots (a part may get fewer: 520 slots are parts of three tiles and of two). In 4 bits, against four blocks an SM whatever the
+// form: eight heads of 128, three blocks (16 sequences of 16384 slots, 64/8 heads): 178 -> 162 us; four heads of 64, six blocks: with four
+// rounds of all six 16 sequences of 16384 slots, 32/8 heads, would go from 77 to 83, 24 of 9000 from 67 to 75.
 int attn_decode_tc_parts(const AttnDecode& c) {
   const int hpb = attn::step_heads(c), G = c.H / c.H_kv;
   const long long n = (long long)c.B * c.H_kv * ((G + hpb - 1) / hpb);
   const int keys = c.window && c.window < c.C ? c.window : c.C, most = (keys + 511) / 512;
-  const int resident = c.kq ? 4 : c.d == 64 ? 2 : 1;
+  const int resident = c.kq ? std::min(attn::quant_resident(c.d, hpb), 4) : c.d == 64 ? 2 : 1;
   const long long want = (4LL * resident * sm_count() + n - 1) / (n > 0 ? n : 1);
   return (int)(want < 1 ? 1 : want < most ? want : most);
 }

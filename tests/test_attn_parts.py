@@ -26,3 +26,16 @@ def test_whole_rounds_of_the_blocks_that_an_SM_holds(B, T, T_k, H):
             best = n
     want = up(8 * B * T, 256) * 256 + up(4 * best * rows * 128, 256) * 256 + up(8 * best * rows, 256) * 256
     assert api.lib().lawcat_attn_workspace_bytes(ctypes.byref(p), api.OP_ATTN_FWD) == want, (least, best)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H,H_kv,d,heads,resident", [(32, 8, 64, 4, 4), (64, 8, 64, 8, 4), (32, 8, 128, 4, 4), (64, 8, 128, 8, 3), (8, 1, 128, 8, 3)])
+@pytest.mark.parametrize("B,C", [(1, 32768), (16, 16384), (64, 16384), (64, 3000)])
+def test_parts_of_a_step_over_a_cache_in_4_bits(B, C, H, H_kv, d, heads, resident):
+    """Four rounds of the blocks that share an SM (four at most: three where a block takes eight heads of 128), no more than pieces of 512
+    slots. (The scratch is that of the step in the storage type, with two blocks an SM or one and sixteen heads a block, where that is larger.)"""
+    p = api.attn_params(B, 1, H, H_kv, d, T_k=C)
+    sms, G = torch.cuda.get_device_properties(0).multi_processor_count, H // H_kv
+    parts = lambda heads, resident: max(1, min(up(4 * resident * sms, B * H_kv * up(G, heads)), up(C, 512)))  # noqa: E731
+    n = max(parts(heads, resident), parts(4 if G <= 4 else 8, 2 if d == 64 else 1))
+    assert api.lib().lawcat_attn_workspace_bytes(ctypes.byref(p), api.OP_ATTN_DECODE) == (0 if n == 1 else up(4 * B * H * n * (d + 2), 256) * 256)
