@@ -350,8 +350,8 @@ typedef struct {
   int32_t causal;    /* 0 | 1 */
   int32_t window;    /* 0 = none */
   int32_t exact;     /* 1 = the fp32 CUDA-core kernels whatever the shape */
-  float scale;       /* usually 1 / sqrt(d) */
-  float cap;         /* 0 = none */
+  float scale;       /* usually 1 / sqrt(d); any sign; 1.45 scale has to be finite in fp32 */
+  float cap;         /* 0 = none; 1.45 cap, 1 / cap and 2.9 scale / cap have to be finite in fp32 */
 } lawcat_attn_params;
 
 enum { LAWCAT_OP_ATTN_FWD = 7, LAWCAT_OP_ATTN_BWD = 8, LAWCAT_OP_ATTN_DECODE = 9 };

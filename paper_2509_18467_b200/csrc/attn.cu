@@ -18,6 +18,10 @@ int check(const lawcat_attn_params* p) {
   if (p->dtype != LAWCAT_F32 && p->dtype != LAWCAT_BF16) return LAWCAT_ERR_INVALID_ARG;
   if ((p->causal | 1) != 1 || (p->exact | 1) != 1 || p->window < 0) return LAWCAT_ERR_INVALID_ARG;
   if (!std::isfinite(p->scale) || !std::isfinite(p->cap) || p->cap < 0.f) return LAWCAT_ERR_INVALID_ARG;
+  // (what the kernels make of them in fp32: scores in units of log2, and the argument of the tanh)
+  if (!std::isfinite(p->scale * attn::LOG2E)) return LAWCAT_ERR_INVALID_ARG;
+  if (p->cap > 0.f && (!std::isfinite(p->cap * attn::LOG2E) || !std::isfinite(1.f / p->cap) || !std::isfinite(2.f * attn::LOG2E * (p->scale / p->cap))))
+    return LAWCAT_ERR_INVALID_ARG;
   if (p->d != 16 && p->d != 32 && p->d != 64 && p->d != 128) return LAWCAT_ERR_UNSUPPORTED;
   if (p->T > MAX_TOKENS || p->T_k > MAX_TOKENS || (long long)p->B * p->H > 0x7fffffffLL / 64) return LAWCAT_ERR_UNSUPPORTED;
   return LAWCAT_OK;
