@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(256) attn_quant_kernel(const QuantArgs a) {
   }
 }
 
-// Parts of the keys: as many as give each SM two blocks, while a part keeps at least 256 keys.
+// Parts of the keys: as many as give each SM two blocks, and no more than there are pieces of 256 keys (257 keys may be two parts).
 int decode_parts(int B, int H, int H_kv, int C, int window) {
   const int G = H / H_kv;
   const long long n = (long long)B * H_kv * ((G + HB - 1) / HB);

@@ -18,9 +18,11 @@
 //         rounded weight times the value would be.)
 // Codes are unpacked two at a time as channels (i, i + 4) of eight; q is stored in that order and the outputs' lanes are read in it.
 //
-// What bounds the 4-bit form is unpacking and weighing in the threads (at width 128 the integer pipe, at half the issue rate, for 1040 of
-// 1900 cycles a tile), so that as many blocks as tensor memory and registers hold share an SM: 64 sequences of 16384 slots, 32/8 heads
-// of 128: 328 us, 3.1 TB/s of codes; of 64: 239 us with six blocks of four heads (four blocks 268, of eight heads 308). The form in the
+// What bounds the 4-bit form is unpacking and weighing in the threads: at width 128, four heads, a tile takes 1656 cycles of an SM, of which
+// the integer pipe (half the issue rate) is busy for 827 and instruction issue for 824; shared memory 28 %, HBM 28 %, tensor pipe 6 %. The
+// rest are waits from one phase of a block to the next, so that as many blocks as tensor memory and registers hold share an SM: 64
+// sequences of 16384 slots, 32/8 heads of 128: 328 us, 3.2 TB/s of codes; of 64: 239 us with six blocks of four heads (four blocks 268, of
+// eight heads 308). The form in the
 // storage type: 64 sequences of 8192 slots, 32/8 heads of 128, 2.15 GB: 319 us, 6.7 TB/s. Both walk their slots from the newest to
 // the oldest: under distance biases the references then stay where the first tile puts them (the 4-bit form at width 64 with biases, of
 // eight heads: 387 us the other way round, 310 so).

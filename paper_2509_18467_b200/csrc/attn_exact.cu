@@ -34,7 +34,7 @@ __global__ void __launch_bounds__(THREADS) attn_fwd_exact_kernel(const Args a, i
   fwd_rows<T, D, RM, THREADS>(a, sm, b, bh % a.H, t0, lo + part * per, lo + (part + 1) * per, p.x + at * D, p.ml + at);
 }
 
-// dq, and (lse log2e, dO.o) of every query for the other kernel
+// dq, and (-lse log2e, -dO.o) of every query for the other kernel
 template <typename T, int D, int RM>
 __global__ void __launch_bounds__(THREADS) attn_dq_exact_kernel(const Args a, int tiles, const Parts p) {
   behind_last_kernel();

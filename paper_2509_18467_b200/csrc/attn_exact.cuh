@@ -5,7 +5,8 @@
 // All three are the same tiling: NTHR threads own BM rows (queries; keys for dk/dv) of one head in shared memory and walk the
 // other side in tiles of 64 rows. A thread, one of NTHR / 16 x 16, holds RM rows x 4 columns of the scores and RM rows x D / 16
 // channels of what it accumulates, so that a row's statistics are shuffles among 16 lanes. (1500 tokens, 32/8 heads of 64 in fp32:
-// forward 310 us, 18 TFLOP/s, dQ 430, dK and dV 636. Loads from shared memory take 77 % of their pipe in the forward, multiply-adds 54 %.
+// forward 310 us, 18 TFLOP/s, dQ 430, dK and dV 636. In the forward loads from shared memory take 78 % of
+// their pipe and packed multiply-adds 54 % of theirs.
 // With 8 lanes to a row, 4 x 8 scores a thread and half the loads, half as many warps hide them worse: 351, 452 and 548 us, and at
 // width 128 808, 1089 and 1999 in place of 640, 820 and 1160.) The running maximum and sum of the
 // softmax stay in registers: one pass over the keys.
@@ -267,7 +268,7 @@ __device__ __forceinline__ void fwd_rows(const Args& a, float* sm, int b, int h,
   store_rows<T, D, RM>((T*)a.o + (size_t)b * a.mask.T * qs + (size_t)h * D, qs, t0, t_end, ty, tx, acc);
 }
 
-// dq, and (lse log2e, dO.o) of every query for the other kernel. part of parts: this share of the row block's key tiles, the sums in
+// dq, and (-lse log2e, -dO.o) of every query for the other kernel. part of parts: this share of the row block's key tiles, the sums in
 // fp32 to part_o [T, D] of the head where parts > 1.
 template <typename T, int D, int RM, int NTHR>
 __device__ __forceinline__ void dq_rows(const Args& a, float* sm, int b, int h, int t0, int part, int parts, float* part_o) {

@@ -587,7 +587,7 @@ static FwdPlan fwd_plan(int B, int H, int H_kv, int T, int T_k, int window) {
   p.tiles = (T + rows - 1) / rows;
   p.pairs = p.two_heads ? H / 2 : H;
   const long long blocks = (long long)B * p.pairs * p.tiles;
-  // the keys are shared out where the blocks leave half of the SMs idle, in parts of four tiles at least
+  // the keys are shared out where the blocks leave half of the SMs idle, into no more parts than there are whole pieces of 512 keys
   long long keys = window && window < T_k ? std::min<long long>(T_k, (long long)window + rows) : T_k;
   const long long room = sm_count() / std::max<long long>(blocks, 1), most = keys / 512;
   p.parts = (int)std::max<long long>(1, std::min(room, most));
