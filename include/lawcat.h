@@ -424,6 +424,91 @@ int lawcat_attn_decode_quant(const lawcat_attn_params* p, const void* q_t, const
                              void* vp, const int32_t* pos, const float* slopes, void* o_t, void* ws, size_t ws_bytes, void* stream,
                              int* dev_status);
 
+/*
+ * Rotary positions of the queries and keys that softmax attention takes (the linearized layer itself uses none, Section 5; the models that
+ * it is distilled from and the softmax layers of a hybrid do). The leading `rot` channels of a head form rot / 2 pairs; pair i of a token at
+ * position n is turned by the angle n freq[i] and multiplied by `scale`:
+ *   (x, y) -> scale (x cos a - y sin a, x sin a + y cos a),  a = n freq[i]
+ * The other channels are copied. All in fp32 but the angle, which is exact to 2^-32 of a turn at every 32-bit position; one rounding.
+ */
+typedef struct {
+  int32_t B, T;
+  int32_t H, H_kv, d; /* d in {16, 32, 64, 128} */
+  int32_t dtype;      /* LAWCAT_F32 | LAWCAT_BF16 */
+  int32_t rot;        /* channels that are turned: even, 2 ... d */
+  int32_t layout;     /* LAWCAT_ROPE_*: the pairs are (i, i + rot / 2) or (2 i, 2 i + 1) */
+  float scale;        /* usually 1; some ways to stretch a context multiply queries and keys */
+} lawcat_rope_params;
+
+enum { LAWCAT_ROPE_HALF = 0, LAWCAT_ROPE_INTERLEAVED = 1 };
+enum {
+  LAWCAT_ROPE_PLAIN = 0,         /* f_i = base^(-2 i / rot) */
+  LAWCAT_ROPE_LINEAR = 1,        /* f_i / factor */
+  LAWCAT_ROPE_BASE = 2,          /* base factor^(rot / (rot - 2)) in place of base: the last pair slows down by factor, the first by nothing */
+  LAWCAT_ROPE_BY_WAVELENGTH = 3, /* f_i (w + (1 - w) / factor), w = clamp((original f_i / (2 pi) - low) / (high - low), 0, 1) */
+  LAWCAT_ROPE_BY_CHANNEL = 4     /* the same with w = 1 - clamp((i - a) / max(z - a, 0.001), 0, 1), a = max(0, floor c(high)),
+                                    z = min(rot - 1, ceil c(low)), c(r) = rot ln(original / (2 pi r)) / (2 ln base): the pair that turns r
+                                    times over the original length */
+};
+
+/* Angles per token of the rot / 2 pairs into the HOST array freq; base > 1, factor >= 1, 0 < low < high (those that the scaling reads). */
+int lawcat_rope_frequencies(int32_t rot, double base, int32_t scaling, double factor, double original, double low, double high, double* freq);
+
+/*
+ * Forward: q [B,T,H,d], k [B,T,H_kv,d] (either may be NULL) -> q_out, k_out, which may be q and k themselves.
+ *   freq: HOST array of rot / 2 angles per token, each in [0, 2 pi]; read during the call, a captured call keeps its values.
+ * The position of token t of sequence b, all DEVICE ints of any sign:
+ *   positions [B,T] given: positions[b][t] (documents packed along T start over, for one)
+ *   else start [B] (nullable: 0) plus t; with parent [B,T] (the drafted nodes of lawcat_attn_tree) plus the node's depth instead, which is 0
+ *   for a node that is not there.
+ */
+int lawcat_rope_fwd(const lawcat_rope_params* p, const double* freq, const void* q, const void* k, const int32_t* positions, const int32_t* start,
+                    const int32_t* parent, void* q_out, void* k_out, void* ws, size_t ws_bytes, void* stream, int* dev_status);
+
+/* Backward: the gradients of q_out and k_out -> those of q and k (turned the other way, the same scale); arguments as in the forward. */
+int lawcat_rope_bwd(const lawcat_rope_params* p, const double* freq, const void* dq_out, const void* dk_out, const int32_t* positions,
+                    const int32_t* start, const int32_t* parent, void* dq, void* dk, void* ws, size_t ws_bytes, void* stream, int* dev_status);
+
+/*
+ * Softmax attention of drafted tokens over a cache: several candidate continuations of each sequence are verified by one pass over its keys.
+ *   q_t [B,N,H,d]  k_t, v_t [B,N,H_kv,d]  K, V [B,C,H_kv,d]  pos [B]  parent [B,N]  slopes [H] fp32 or NULL  ->  o_t [B,N,H,d]
+ * with N = p->T nodes (at most 256) and C = p->T_k slots; p->causal is ignored. K, V are read only: what is accepted goes there by
+ * lawcat_cache_accept.
+ *   pos, DEVICE ints: the sequence's tokens so far, which the cache holds in slots j mod C. A sequence with pos < 0 is not there: its o_t is 0.
+ *   parent, DEVICE ints: the node behind which a node was drafted, an earlier one; -1 = behind the sequence's last token. A node with any
+ *     other value, and every node that hangs from it, is not there: its o_t is 0, and its q_t, k_t, v_t may hold anything. parent = NULL:
+ *     each node behind the one in front of it.
+ * A node of depth e (0 for parent -1) stands at position pos + e and sees, as the same tokens fed to lawcat_attn_decode one by one would,
+ * the cached tokens and the nodes of its path, itself included, that lie less than W behind it: W = p->window, or C without one.
+ * Distances (slopes) are those of the positions. Slots that hold no token yet may hold anything.
+ * Rounding as in lawcat_attn_fwd; bf16 with d = 64 or 128 (and exact = 0) runs on the tensor cores. A key or value row that a node does not
+ * see does not reach its result, not even as a NaN (a row that comes out not finite is computed again, which takes its time).
+ */
+enum { LAWCAT_OP_ATTN_TREE = 10 }; /* for lawcat_attn_workspace_bytes; both caches share it */
+int lawcat_attn_tree(const lawcat_attn_params* p, const void* q_t, const void* k_t, const void* v_t, const void* K, const void* V,
+                     const int32_t* pos, const int32_t* parent, const float* slopes, void* o_t, void* ws, size_t ws_bytes, void* stream,
+                     int* dev_status);
+
+/*
+ * lawcat_attn_tree over a cache in 4 bits (read only); a node's key and value are what the cache would hold of k_t, v_t.
+ */
+int lawcat_attn_tree_quant(const lawcat_attn_params* p, const void* q_t, const void* k_t, const void* v_t, const void* kq, const void* kp,
+                           const void* vq, const void* vp, const int32_t* pos, const int32_t* parent, const float* slopes, void* o_t, void* ws,
+                           size_t ws_bytes, void* stream, int* dev_status);
+
+/*
+ * Accepted tokens into the cache: rows of k_t, v_t [B,T,H_kv,d] go to slots (pos + i) mod C of K, V [B,C,H_kv,d].
+ *   path [B,M] DEVICE ints: the i-th row of sequence b is path[b][i], up to the first entry that is not in 0 ... T-1 (a path of nodes,
+ *     padded with -1); path = NULL: all T rows in order (a piece of a prompt; M is ignored).
+ *   pos [B] DEVICE ints, as above; pos_out [B] (nullable, not pos itself): pos plus the rows accepted. (pos is not advanced in place: several layers
+ *     share it.) Of more than C rows the last C are kept. A sequence with pos < 0 is left as it is, and so is its pos.
+ * No scratch: ws may be NULL. The other form quantizes the rows as lawcat_cache_quantize does.
+ */
+int lawcat_cache_accept(const lawcat_attn_params* p, int32_t M, const void* k_t, const void* v_t, const int32_t* pos, const int32_t* path, void* K,
+                        void* V, int32_t* pos_out, void* ws, size_t ws_bytes, void* stream, int* dev_status);
+int lawcat_cache_accept_quant(const lawcat_attn_params* p, int32_t M, const void* k_t, const void* v_t, const int32_t* pos, const int32_t* path,
+                              void* kq, void* kp, void* vq, void* vp, int32_t* pos_out, void* ws, size_t ws_bytes, void* stream, int* dev_status);
+
 #ifdef __cplusplus
 }
 #endif

@@ -20,7 +20,8 @@ F32, BF16 = 0, 1
 PHI_SOFTMAX, PHI_ELU1, PHI_IDENTITY = 0, 1, 2
 GATE_LOGITS, GATE_LOGDECAY = 0, 1
 OP_CONV_FWD, OP_CONV_BWD, OP_GLA_FWD, OP_GLA_BWD, OP_LAYER_FWD, OP_DECODE_STEP, OP_LAYER_BWD = range(7)
-OP_ATTN_FWD, OP_ATTN_BWD, OP_ATTN_DECODE = range(7, 10)
+OP_ATTN_FWD, OP_ATTN_BWD, OP_ATTN_DECODE, OP_ATTN_TREE = range(7, 11)
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 
 EXPORTS = ["lawcat_workspace_bytes", "lawcat_status_string", "lawcat_version", "lawcat_launch_count",
            "lawcat_trace_begin", "lawcat_trace_end", "lawcat_test_set_wait_limit", "lawcat_conv_fwd", "lawcat_conv_bwd", "lawcat_gla_fwd",
@@ -28,7 +29,8 @@ EXPORTS = ["lawcat_workspace_bytes", "lawcat_status_string", "lawcat_version", "
            "lawcat_layer_fwd_varlen", "lawcat_layer_bwd", "lawcat_decode_step", "lawcat_layer_fwd_host_arena_bytes",
            "lawcat_layer_fwd_host", "lawcat_noalloc_scratch_bytes", "lawcat_layer_fwd_noalloc", "lawcat_last_cuda_error", "lawcat_gate_fn_workspace_bytes",
            "lawcat_gate_fn_fwd", "lawcat_attn_workspace_bytes", "lawcat_attn_fwd", "lawcat_attn_bwd", "lawcat_attn_decode",
-           "lawcat_cache_quantize", "lawcat_cache_dequantize", "lawcat_attn_decode_quant"]
+           "lawcat_cache_quantize", "lawcat_cache_dequantize", "lawcat_attn_decode_quant", "lawcat_rope_frequencies", "lawcat_rope_fwd",
+           "lawcat_rope_bwd", "lawcat_attn_tree", "lawcat_attn_tree_quant", "lawcat_cache_accept", "lawcat_cache_accept_quant"]
 
 
 class LawcatError(RuntimeError):
@@ -74,6 +76,21 @@ def attn_params(B, T, H, H_kv, d, T_k=None, dtype=BF16, causal=1, window=0, exac
                       d ** -0.5 if scale is None else scale, cap)
 
 
+class RopeParams(ctypes.Structure):
+    """Mirror of ``lawcat_rope_params``."""
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("H", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("rot", ctypes.c_int32), ("layout", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+def rope_params(B, T, H, H_kv, d, rot=None, layout="half", dtype=BF16, scale=1.0) -> RopeParams:
+    """rot defaults to d; layout: "half" or "interleaved"."""
+    if isinstance(dtype, str):
+        dtype = {"f32": F32, "bf16": BF16}[dtype]
+    if isinstance(layout, str):
+        layout = {"half": ROPE_HALF, "interleaved": ROPE_INTERLEAVED}[layout]
+    return RopeParams(B, T, H, H_kv, d, dtype, d if rot is None else rot, layout, scale)
+
+
 _lib = None
 
 
@@ -115,6 +132,23 @@ def lib() -> ctypes.CDLL:
             f.restype = ctypes.c_int
             f.argtypes = [ctypes.POINTER(AttnParams), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32] + \
                          [ctypes.c_void_p] * nptr + [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p]
+        L.lawcat_rope_frequencies.restype = ctypes.c_int
+        L.lawcat_rope_frequencies.argtypes = [ctypes.c_int32, ctypes.c_double, ctypes.c_int32] + [ctypes.c_double] * 4 + [ctypes.c_void_p]
+        for name, nptr in (("lawcat_attn_tree", 9), ("lawcat_attn_tree_quant", 11)):
+            f = getattr(L, name)
+            f.restype = ctypes.c_int
+            f.argtypes = [ctypes.POINTER(AttnParams)] + [ctypes.c_void_p] * nptr + \
+                         [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p]
+        for name, nptr in (("lawcat_cache_accept", 7), ("lawcat_cache_accept_quant", 9)):
+            f = getattr(L, name)
+            f.restype = ctypes.c_int
+            f.argtypes = [ctypes.POINTER(AttnParams), ctypes.c_int32] + [ctypes.c_void_p] * nptr + \
+                         [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p]
+        for name in ("lawcat_rope_fwd", "lawcat_rope_bwd"):
+            f = getattr(L, name)
+            f.restype = ctypes.c_int
+            f.argtypes = [ctypes.POINTER(RopeParams)] + [ctypes.c_void_p] * 8 + \
+                         [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p]
         L.lawcat_layer_fwd_varlen_workspace_bytes.restype = ctypes.c_size_t
         L.lawcat_layer_fwd_varlen_workspace_bytes.argtypes = [ctypes.POINTER(Params), ctypes.c_void_p, ctypes.c_int]
         for name, nptr in (("lawcat_conv_fwd", 9), ("lawcat_conv_bwd", 14), ("lawcat_gla_fwd", 10),
@@ -459,6 +493,113 @@ def lawcat_attn_decode_quant(p: AttnParams, q_t, k_t, v_t, kq, kp, vq, vp, pos, 
     _check_cache(p, kq, kp, vq, vp)
     _attn_call("lawcat_attn_decode_quant", p, OP_ATTN_DECODE, (q_t, k_t, v_t, kq, kp, vq, vp, pos, slopes, o_t), ws, stream, dev_status)
     return o_t
+
+
+def rope_frequencies(rot, base=10000.0, scaling="plain", factor=1.0, original=0.0, low=1.0, high=4.0):
+    """Angles per token of the rot / 2 pairs, as the HOST array that the rotary calls take (any other sequence of angles within 0 ... 2 pi
+    does as well). scaling: "plain", "linear", "base", "wavelength" (high: 4 is usual) or "channel" (32)."""
+    freq = (ctypes.c_double * max(1, rot // 2))()
+    kind = {"plain": 0, "linear": 1, "base": 2, "wavelength": 3, "channel": 4}[scaling]
+    st = lib().lawcat_rope_frequencies(rot, base, kind, factor, original, low, high, freq)
+    if st != 0:
+        raise LawcatError(st, "lawcat_rope_frequencies")
+    return freq
+
+
+def _rope(name, p, freq, q, k, positions, start, parent, q_out, k_out, stream):
+    B, T, dt, check = p.B, p.T, p.dtype, _checked()
+    if len(freq) != p.rot // 2:
+        raise ValueError(f"freq holds {len(freq)} angles, rot = {p.rot} takes {p.rot // 2}")
+    if not isinstance(freq, ctypes.Array):
+        freq = (ctypes.c_double * len(freq))(*[float(x) for x in freq])
+    for x, out, heads, what in ((q, q_out, p.H, "q"), (k, k_out, p.H_kv, "k")):
+        check(what, x, dt, B, T, heads, p.d)
+        check(what + "_out", out, dt, B, T, heads, p.d)
+    check("positions", positions, I32, B, T)
+    check("start", start, I32, B)
+    check("parent", parent, I32, B, T)
+    if q_out is None and q is not None:
+        q_out = _empty(q, dt, B, T, p.H, p.d)
+    if k_out is None and k is not None:
+        k_out = _empty(k, dt, B, T, p.H_kv, p.d)
+    _attn_call(name, p, None, (ctypes.addressof(freq), q, k, positions, start, parent, q_out, k_out), None, stream, None, 1)
+    return q_out, k_out
+
+
+def lawcat_rope_fwd(p: RopeParams, freq, q, k=None, positions=None, start=None, parent=None, q_out=None, k_out=None, stream=None):
+    """Rotary positions: positions [B,T], or start [B] (plus t, or plus the depth of drafted node t given by parent [B,T]). The outputs may
+    be q and k themselves. Returns (q, k) turned; either may be left out."""
+    return _rope("lawcat_rope_fwd", p, freq, q, k, positions, start, parent, q_out, k_out, stream)
+
+
+def lawcat_rope_bwd(p: RopeParams, freq, dq_out, dk_out=None, positions=None, start=None, parent=None, dq=None, dk=None, stream=None):
+    """The gradients of the turned q and k -> those of q and k."""
+    return _rope("lawcat_rope_bwd", p, freq, dq_out, dk_out, positions, start, parent, dq, dk, stream)
+
+
+def _check_tree(p, q_t, k_t, v_t, pos, parent, slopes, o_t):
+    B, N, H, H_kv, d, dt, check = p.B, p.T, p.H, p.H_kv, p.d, p.dtype, _checked()
+    check("q_t", q_t, dt, B, N, H, d)
+    check("k_t", k_t, dt, B, N, H_kv, d)
+    check("v_t", v_t, dt, B, N, H_kv, d)
+    check("pos", pos, I32, B)
+    check("parent", parent, I32, B, N)
+    check("slopes", slopes, F32, H)
+    if o_t is None:
+        return _empty(q_t, dt, B, N, H, d)
+    check("o_t", o_t, dt, B, N, H, d)
+    return o_t
+
+
+def lawcat_attn_tree(p: AttnParams, q_t, k_t, v_t, K, V, pos, parent=None, slopes=None, o_t=None, ws=None, stream=None, dev_status=None):
+    """p.T drafted tokens per sequence over caches of p.T_k slots, which stay as they are; parent [B,T] (None: a chain). Returns o_t [B,T,H,d]."""
+    o_t = _check_tree(p, q_t, k_t, v_t, pos, parent, slopes, o_t)
+    check, sizes = _checked(), (p.dtype, p.B, p.T_k, p.H_kv, p.d)
+    check("K", K, *sizes)
+    check("V", V, *sizes)
+    _attn_call("lawcat_attn_tree", p, OP_ATTN_TREE, (q_t, k_t, v_t, K, V, pos, parent, slopes, o_t), ws, stream, dev_status)
+    return o_t
+
+
+def lawcat_attn_tree_quant(p: AttnParams, q_t, k_t, v_t, kq, kp, vq, vp, pos, parent=None, slopes=None, o_t=None, ws=None, stream=None,
+                           dev_status=None):
+    """The same over a cache in 4 bits."""
+    o_t = _check_tree(p, q_t, k_t, v_t, pos, parent, slopes, o_t)
+    _check_cache(p, kq, kp, vq, vp)
+    _attn_call("lawcat_attn_tree_quant", p, OP_ATTN_TREE, (q_t, k_t, v_t, kq, kp, vq, vp, pos, parent, slopes, o_t), ws, stream, dev_status)
+    return o_t
+
+
+def _check_accept(p, k_t, v_t, pos, path, pos_out):
+    check, sizes = _checked(), (p.dtype, p.B, p.T, p.H_kv, p.d)
+    check("k_t", k_t, *sizes)
+    check("v_t", v_t, *sizes)
+    check("pos", pos, I32, p.B)
+    M = 0 if path is None else path.shape[-1]
+    check("path", path, I32, p.B, M)
+    if path is not None and path.numel() == 0 and p.B:
+        raise ValueError("path: no entries (a sequence that takes nothing has a negative first one)")
+    check("pos_out", pos_out, I32, p.B)
+    return M, torch.empty_like(pos) if pos_out is None else pos_out
+
+
+def lawcat_cache_accept(p: AttnParams, k_t, v_t, pos, K, V, path=None, pos_out=None, stream=None, dev_status=None):
+    """Rows path[b][0 ...] (up to the first entry that is no row; None: all p.T rows) of k_t, v_t [B,T,H_kv,d] into the caches of p.T_k slots
+    from position pos on, in place. Returns the positions behind them [B]."""
+    M, pos_out = _check_accept(p, k_t, v_t, pos, path, pos_out)
+    check, sizes = _checked(), (p.dtype, p.B, p.T_k, p.H_kv, p.d)
+    check("K", K, *sizes)
+    check("V", V, *sizes)
+    _attn_call("lawcat_cache_accept", p, None, (M, k_t, v_t, pos, path, K, V, pos_out), None, stream, dev_status, 1)
+    return pos_out
+
+
+def lawcat_cache_accept_quant(p: AttnParams, k_t, v_t, pos, kq, kp, vq, vp, path=None, pos_out=None, stream=None, dev_status=None):
+    """The same into a cache in 4 bits."""
+    M, pos_out = _check_accept(p, k_t, v_t, pos, path, pos_out)
+    _check_cache(p, kq, kp, vq, vp)
+    _attn_call("lawcat_cache_accept_quant", p, None, (M, k_t, v_t, pos, path, kq, kp, vq, vp, pos_out), None, stream, dev_status, 1)
+    return pos_out
 
 
 def lawcat_layer_fwd_host(p: Params, h_q, h_k, h_v, h_gate, h_w_q, h_w_k, h_W, h_o, arena, stream=None):

@@ -157,6 +157,11 @@ int check_cache(const lawcat_attn_params* p) {
 
 }  // namespace
 
+namespace lawcat {
+int attn_check(const lawcat_attn_params* p) { return check(p); }
+int attn_check_cache(const lawcat_attn_params* p) { return check_cache(p); }
+}  // namespace lawcat
+
 extern "C" {
 
 size_t lawcat_attn_workspace_bytes(const lawcat_attn_params* p, int op) {
@@ -170,6 +175,7 @@ size_t lawcat_attn_workspace_bytes(const lawcat_attn_params* p, int op) {
       return rows_bytes(p) + keys_bytes(p) + stat_bytes(p) +
              (attn_tc_supported(p->dtype, p->d, p->exact) ? 0 : attn_bwd_exact_workspace_bytes(make_call(p, nullptr, nullptr, nullptr)));
     case LAWCAT_OP_ATTN_DECODE: return align_up(attn_decode_workspace_bytes(make_decode(p, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr)), 256);
+    case LAWCAT_OP_ATTN_TREE: return attn_tree_workspace_bytes(p);
     default: return 0;
   }
 }

@@ -143,6 +143,11 @@ struct AttnDecode {
 };
 size_t attn_decode_workspace_bytes(const AttnDecode& c);
 int launch_attn_decode(const AttnDecode& c);
+// checks of a call's parameters, and of those that name a cache (attn.cu)
+int attn_check(const lawcat_attn_params* p);
+int attn_check_cache(const lawcat_attn_params* p);
+// attention of drafted tokens (attn_tree.cu)
+size_t attn_tree_workspace_bytes(const lawcat_attn_params* p);
 // T rows per sequence of k_t, v_t into the 4-bit cache, or (write = false) out of it
 int launch_attn_quant(const AttnDecode& c, int T, bool write);
 
