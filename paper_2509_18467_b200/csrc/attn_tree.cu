@@ -17,126 +17,6 @@ namespace attn {
 
 constexpr int TREE_ROWS = 32, TREE_KEYS = 64, TREE_THREADS = 256, TREE_RW = 4;   // rows and keys of a tile; rows of a warp
 
-__device__ __forceinline__ float tree_score(const TreeArgs& a, float dot, float slope, int dist) {
-  float x = dot * a.scale;
-  if (a.cap > 0.f) x = a.cap * tanhf(x / a.cap);
-  return (x - slope * (float)dist) * LOG2E;
-}
-
-// one group of channels of a row, as the step reads it: `node` >= 0 a node's own row, else the slot's
-template <typename T, int D, bool QUANT>
-__device__ __forceinline__ void row_group(const TreeArgs& a, bool v, int b, int g, int node, size_t slot, int c0, float (&x)[quant_group(D)]) {
-  constexpr int GS = quant_group(D);
-  if (node >= 0 || !QUANT) {
-    const T* src = node >= 0 ? (const T*)(v ? a.v_t : a.k_t) + (((size_t)b * a.N + node) * a.H_kv + g) * D + c0
-                             : (const T*)(v ? a.V : a.K) + (((size_t)b * a.C + slot) * a.H_kv + g) * D + c0;
-#pragma unroll 1
-    for (int i = 0; i < GS; ++i) x[i] = ldf<T>(src + i);
-    if (!QUANT) return;
-    float lo = x[0], hi = x[0], scale, low;
-#pragma unroll 1
-    for (int i = 1; i < GS; ++i) {
-      lo = min_nan(lo, x[i]);
-      hi = max_nan(hi, x[i]);
-    }
-    quant_params(lo, hi, isfinite(lo) && isfinite(hi), scale, low);
-    const float inv = __frcp_rn(scale);
-#pragma unroll 1
-    for (int i = 0; i < GS; ++i) x[i] = fmaf((float)code_bits(quant_code(x[i], scale, low, inv)), scale, low);
-  } else {
-    const size_t row = ((size_t)b * a.H_kv + g) * a.C + slot;
-    const uint8_t* q = (v ? a.vq : a.kq) + row * (D / 2) + c0 / 2;
-    const bf16* p = (v ? a.vp : a.kp) + (row * (D / GS) + c0 / GS) * 2;
-    const float scale = __bfloat162float(p[0]), low = __bfloat162float(p[1]);
-#pragma unroll 1
-    for (int i = 0; i < GS; ++i) x[i] = fmaf((float)(q[i / 2] >> (4 * (i & 1)) & 15), scale, low);
-  }
-}
-
-// One row by one warp, from the keys that it sees alone, 32 at a time: a lane's key for the scores, all lanes' channels for the values.
-template <typename T, int D, bool QUANT>
-__device__ __noinline__ void tree_row_again(const TreeArgs& a, int b, int node, int h) {
-  constexpr int NC = D / 32 > 0 ? D / 32 : 1, GS = quant_group(D);
-  const int lane = threadIdx.x & 31, g = h / (a.H / a.H_kv), pos = a.pos[b];
-  const size_t row = ((size_t)b * a.N + node) * a.H + h;
-  const T* const q = (const T*)a.q + row * D;
-  const float slope = a.slopes ? a.slopes[h] : 0.f;
-  int depth = 0;
-  bool there = pos >= 0;
-  for (int i = node; there && i >= 0;) {
-    const int p = a.parent ? a.parent[(size_t)b * a.N + i] : i - 1;
-    there = p >= -1 && p < i;
-    depth += p >= 0;
-    i = p;
-  }
-  const int cached = there ? max(0, min(cached_keys(pos, a.W), a.W - 1 - depth)) : 0;
-  const int path = there ? min(depth + 1, a.W) : 0;       // nodes of the path that are near enough, from the row's own on
-  float m = -INFINITY, l = 0.f, acc[NC] = {};
-  int next = node;                                        // the path's next node
-  for (int k0 = 0; k0 < path + cached; k0 += 32) {
-    const int k = k0 + lane;
-    int mine = -1, dist = k;
-    for (int i = 0; i < 32 && k0 + i < path; ++i) {       // (all lanes walk, one keeps)
-      if (i == lane) mine = next;
-      next = a.parent ? a.parent[(size_t)b * a.N + next] : next - 1;
-    }
-    size_t slot = 0;
-    if (k >= path) {
-      const int back = k - path + 1;
-      dist = depth + back;
-      int s = pos % a.C - back % a.C;
-      slot = s < 0 ? s + a.C : s;
-    }
-    float x = -INFINITY;
-    if (k < path + cached) {
-      float d = 0.f, u[GS];
-      for (int c = 0; c < D; c += GS) {
-        row_group<T, D, QUANT>(a, false, b, g, mine, slot, c, u);
-        for (int i = 0; i < GS; ++i) d = fmaf(ldf<T>(q + c + i), u[i], d);
-      }
-      x = tree_score(a, d, slope, dist);
-    }
-    const float mx = fmaxf(m, warp_max(x)), base = mx == -INFINITY ? 0.f : mx, f = exp2f(m - base);
-    const float p = k < path + cached ? exp2f(x - base) : 0.f;
-    l = l * f + warp_sum(p);
-    m = mx;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) acc[c] *= f;
-    for (int i = 0; i < 32 && k0 + i < path + cached; ++i) {
-      const float w = __shfl_sync(0xffffffffu, p, i);
-      const int n = __shfl_sync(0xffffffffu, mine, i);
-      const size_t s = __shfl_sync(0xffffffffu, (unsigned long long)slot, i);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        float y;
-        const int ch = D >= 32 ? lane + 32 * c : lane % D;
-        if (n >= 0 || !QUANT) {
-          y = ldf<T>(n >= 0 ? (const T*)a.v_t + (((size_t)b * a.N + n) * a.H_kv + g) * D + ch : (const T*)a.V + (((size_t)b * a.C + s) * a.H_kv + g) * D + ch);
-          if (QUANT) {
-            float lo = y, hi = y, scale, low;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {            // (a group is a warp's channels, at width 16 twice the same)
-              lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-              hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-            }
-            quant_params(lo, hi, isfinite(lo) && isfinite(hi), scale, low);
-            y = fmaf((float)code_bits(quant_code(y, scale, low, __frcp_rn(scale))), scale, low);
-          }
-        } else {
-          const size_t r = ((size_t)b * a.H_kv + g) * a.C + s;
-          const bf16* pr = a.vp + (r * (D / GS) + ch / GS) * 2;
-          y = fmaf((float)(a.vq[r * (D / 2) + ch / 2] >> (4 * (ch & 1)) & 15), __bfloat162float(pr[0]), __bfloat162float(pr[1]));
-        }
-        acc[c] = fmaf(w, y, acc[c]);
-      }
-    }
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-  for (int c = 0; c < NC; ++c)
-    if (lane + 32 * c < D) stf<T>((T*)a.o + row * D + lane + 32 * c, l == 0.f ? 0.f : acc[c] * inv);
-}
-
 template <int D>
 struct TreeLay {
   static constexpr int LD = D + 4;
@@ -499,7 +379,7 @@ int tree(const lawcat_attn_params* p, AttnTree& c, const void* const (&req)[8], 
     if (!aligned(x)) return LAWCAT_ERR_INVALID_ARG;
   const size_t need = lawcat_attn_workspace_bytes(p, LAWCAT_OP_ATTN_TREE);
   if (need && (!c.ws || ws_bytes < need)) return LAWCAT_ERR_WORKSPACE_TOO_SMALL;
-  return launch_tree_exact(c);
+  return attn_tc_supported(c.dtype, c.d, c.exact) ? launch_attn_tree_tc(c) : launch_tree_exact(c);
 }
 
 template <bool QUANT>
@@ -552,6 +432,7 @@ int launch_attn_tree_join(const AttnTree& c) {
 size_t attn_tree_workspace_bytes(const lawcat_attn_params* p) {
   if (tree_check(p) != LAWCAT_OK) return 0;
   const AttnTree c = make_tree(p);
+  if (attn_tc_supported(c.dtype, c.d, c.exact)) return attn_tree_tc_workspace_bytes(c.a.B, c.a.N, c.a.H, c.a.H_kv, c.a.C, c.a.W, c.d);
   return part_bytes(c, attn::tree_parts(c));
 }
 

@@ -69,7 +69,7 @@ def tree(quant, pos, N, C=100, H=4, H_kv=2, d=64, dtype="bf16", window=0, cap=0.
         assert torch.equal(t.view(torch.uint8), was.view(torch.uint8))
     coarse = dtype == "bf16" and not exact and d >= 64
     # operands on the tensor cores: weights in the storage type; over 4 bits weights, keys and values in fp16
-    eps = dict(eps_p=U11, eps_k=U11, eps_v=U11) if coarse and quant else dict(eps_p=U16) if coarse else {}
+    eps = dict(eps_p=U11, eps_k=U11, eps_v=U11, min_p=2.0 ** -25) if coarse and quant else dict(eps_p=U16) if coarse else {}
     for b, x in enumerate(pos):
         cached, see, dist = sees(parents[b], x, C, window)
         slots = torch.tensor(cached, dtype=torch.long, device="cuda") % C

@@ -2,6 +2,9 @@
 
 Tolerances as in attn_reference.py: a score is off by (d + 16) 2^-24 (scale sum|q||k| + slope distance + cap), a weight by twice that relatively
 plus n + 16 steps of 2^-24; operands that a kernel rounds add half a step each: weights eps_p, keys eps_k (to the score), values eps_v.
+Weights in fp16 are whole multiples of 2^-24 below 2^-14 (min_p = 2^-25, half of that): the weights are relative to a score of the row, so that
+their sum is at least 1, and sum_j p_j v_j / sum_j p_j is off by min_p sum_j |v_j| over the keys that are seen. (A weight of 2e-11 beside one
+of 1, whose value is 0: the result is 1.1e-11 by the definition and 0 with weights in fp16, which is 6.67 times the bound without this term.)
 """
 import math
 
@@ -41,7 +44,7 @@ def sees(parent, pos, C, window):
     return cached, see, dist
 
 
-def tree_attention(q, k, v, see, dist, scale, cap=0.0, slopes=None, eps_p=0.0, eps_k=0.0, eps_v=0.0):
+def tree_attention(q, k, v, see, dist, scale, cap=0.0, slopes=None, eps_p=0.0, eps_k=0.0, eps_v=0.0, min_p=0.0):
     """q [N, H, d], k, v [n, H_kv, d] in any type; o [N, H, d] and its error bound but for the result's own rounding, in 64 bits."""
     N, H, d = q.shape
     G = H // k.shape[1]
@@ -62,7 +65,7 @@ def tree_attention(q, k, v, see, dist, scale, cap=0.0, slopes=None, eps_p=0.0, e
     p_err = 2 * row + (see.sum(-1, keepdim=True) + 16) * U32
     o = torch.einsum("hts,shd->thd", p, v)
     bound = torch.einsum("hts,shd->thd", p * (p_err + eps_p + eps_v), v.abs())
-    return o, bound
+    return o, bound + min_p * torch.einsum("hts,shd->thd", see.double().expand_as(p), v.abs())
 
 
 __all__ = ["U11", "U16", "U32", "paths_of", "sees", "tree_attention"]
