@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(TREE_THREADS) attn_tree_kernel(const __grid_co
   const int b = bg / a.H_kv, g = bg % a.H_kv, r0 = rb * TREE_ROWS;
   behind_last_kernel();
   const int pos = a.pos[b];
-  find_paths(a, b, paths);
+  find_paths<TREE_THREADS>(a, b, paths, tid, 1);
   auto row_at = [&](int r) { return ((size_t)b * a.N + r / G) * a.H + g * G + r % G; };   // of [B, N, H]
   // keys: the nodes' own up to the last one of these rows, then the cached ones from the newest on; tiles of 64, each of one kind
   const int nodes = pos < 0 ? 0 : min(a.N, (r0 + TREE_ROWS - 1) / G + 1), cached = cached_keys(pos, a.W);
@@ -379,7 +379,8 @@ int tree(const lawcat_attn_params* p, AttnTree& c, const void* const (&req)[8], 
     if (!aligned(x)) return LAWCAT_ERR_INVALID_ARG;
   const size_t need = lawcat_attn_workspace_bytes(p, LAWCAT_OP_ATTN_TREE);
   if (need && (!c.ws || ws_bytes < need)) return LAWCAT_ERR_WORKSPACE_TOO_SMALL;
-  return attn_tc_supported(c.dtype, c.d, c.exact) ? launch_attn_tree_tc(c) : launch_tree_exact(c);
+  if (!attn_tc_supported(c.dtype, c.d, c.exact)) return launch_tree_exact(c);
+  return c.a.kq ? launch_attn_tree_quant_tc(c) : launch_attn_tree_tc(c);
 }
 
 template <bool QUANT>
@@ -432,7 +433,8 @@ int launch_attn_tree_join(const AttnTree& c) {
 size_t attn_tree_workspace_bytes(const lawcat_attn_params* p) {
   if (tree_check(p) != LAWCAT_OK) return 0;
   const AttnTree c = make_tree(p);
-  if (attn_tc_supported(c.dtype, c.d, c.exact)) return attn_tree_tc_workspace_bytes(c.a.B, c.a.N, c.a.H, c.a.H_kv, c.a.C, c.a.W, c.d);
+  if (c.a.B == 0 || c.a.N == 0) return 0;
+  if (attn_tc_supported(c.dtype, c.d, c.exact)) return std::max(attn_tree_tc_workspace_bytes(c), attn_tree_quant_tc_workspace_bytes(c));
   return part_bytes(c, attn::tree_parts(c));
 }
 

@@ -32,46 +32,65 @@ struct Paths {
   uint32_t on[TREE_MAX][TREE_MAX / 32];
   int up[TREE_MAX];
 };
-// Paths by doubling: after step k a node's bits are its nearest 2^k ancestors, `up` the next one. All threads of a block of at least
-// TREE_MAX threads; ends with a barrier.
-__device__ __forceinline__ void find_paths(const TreeArgs& a, int b, Paths& s) {
-  const int i = threadIdx.x, words = (a.N + 31) / 32;
-  int up = -1;
-  if (i < a.N) {
-    up = i - 1;
+// Paths by doubling: after step k a node's bits are its nearest 2^k ancestors, `up` the next one. By THREADS threads (their numbers `tid`,
+// a named barrier of theirs), which find everything behind the barrier that it ends with.
+template <int THREADS>
+__device__ __forceinline__ void find_paths(const TreeArgs& a, int b, Paths& s, int tid, int barrier) {
+  constexpr int PER = TREE_MAX / THREADS, WORDS = TREE_MAX / 32;
+  int up[PER];
+  bool climb = false;
+#pragma unroll
+  for (int p = 0; p < PER; ++p) {
+    const int i = tid + p * THREADS;
+    up[p] = -1;
+    if (i >= a.N) continue;
+    up[p] = i - 1;
     if (a.parent) {
-      up = a.parent[(size_t)b * a.N + i];
-      if (up < -1 || up >= i) up = -2;
+      up[p] = a.parent[(size_t)b * a.N + i];
+      if (up[p] < -1 || up[p] >= i) up[p] = -2;
     }
 #pragma unroll
-    for (int w = 0; w < TREE_MAX / 32; ++w) {
+    for (int w = 0; w < WORDS; ++w) {
       uint32_t bits = w == i / 32 ? 1u << (i & 31) : 0u;
       if (!a.parent) bits = w < i / 32 ? 0xffffffffu : w == i / 32 ? 0xffffffffu >> (31 - (i & 31)) : 0u;   // (a chain: all in front)
       s.on[i][w] = bits;
     }
-    s.up[i] = up;
+    s.up[i] = up[p];
+    climb = climb || up[p] >= 0;
   }
   if (a.parent) {
-    while (__syncthreads_or(i < a.N && up >= 0)) {   // (at most eight times: distances double)
-      uint32_t more[TREE_MAX / 32];
-      int next = up;
-      if (up >= 0 && i < a.N) {
-        next = s.up[up];
+    const int words = (a.N + 31) / 32;
+    while (tc::named_bar_or(barrier, THREADS, climb)) {   // (at most eight times: distances double)
+      uint32_t more[PER][WORDS];
+      int next[PER];
 #pragma unroll
-        for (int w = 0; w < TREE_MAX / 32; ++w) more[w] = w < words ? s.on[up][w] : 0u;
+      for (int p = 0; p < PER; ++p) {
+        next[p] = up[p];
+        if (up[p] < 0) continue;
+        next[p] = s.up[up[p]];
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) more[p][w] = w < words ? s.on[up[p]][w] : 0u;
       }
-      __syncthreads();
-      if (up >= 0 && i < a.N) {
+      tc::named_bar_sync(barrier, THREADS);
+      climb = false;
 #pragma unroll
-        for (int w = 0; w < TREE_MAX / 32; ++w)
-          if (w < words) s.on[i][w] |= more[w];
-        s.up[i] = up = next;
+      for (int p = 0; p < PER; ++p) {
+        if (up[p] < 0) continue;
+        const int i = tid + p * THREADS;
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w)
+          if (w < words) s.on[i][w] |= more[p][w];
+        s.up[i] = up[p] = next[p];
+        climb = climb || up[p] >= 0;
       }
     }
-    if (i < a.N && up == -2)
-      for (int w = 0; w < words; ++w) s.on[i][w] = 0u;
+#pragma unroll
+    for (int p = 0; p < PER; ++p)
+      if (up[p] == -2)
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) s.on[tid + p * THREADS][w] = 0u;
   }
-  __syncthreads();
+  tc::named_bar_sync(barrier, THREADS);
 }
 __device__ __forceinline__ int node_depth(const Paths& s, int i, int N) {
   int n = -1;
@@ -211,7 +230,10 @@ struct AttnTree {
 };
 int launch_attn_tree_join(const AttnTree& c);
 // the tensor-core kernels (attn_tree_tc.cu): bf16 storage, d = 64 or 128
-size_t attn_tree_tc_workspace_bytes(int B, int N, int H, int H_kv, int C, int W, int d);
+size_t attn_tree_tc_workspace_bytes(const AttnTree& c);
 int launch_attn_tree_tc(const AttnTree& c);
+// the same over 4 bits (attn_tree_quant_tc.cu)
+size_t attn_tree_quant_tc_workspace_bytes(const AttnTree& c);
+int launch_attn_tree_quant_tc(const AttnTree& c);
 
 }  // namespace lawcat
