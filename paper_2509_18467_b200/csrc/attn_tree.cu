@@ -353,6 +353,9 @@ int launch_tree_exact(const AttnTree& c) {
   });
 }
 
+// (a node's rows are one box of a tile: 128 query heads to a key-value head at most)
+bool tree_tc_supported(const AttnTree& c) { return attn_tc_supported(c.dtype, c.d, c.exact) && c.a.H / c.a.H_kv <= 128; }
+
 int tree_check(const lawcat_attn_params* p) {
   int r = attn_check(p);
   if (r || (r = attn_check_cache(p))) return r;
@@ -379,7 +382,7 @@ int tree(const lawcat_attn_params* p, AttnTree& c, const void* const (&req)[8], 
     if (!aligned(x)) return LAWCAT_ERR_INVALID_ARG;
   const size_t need = lawcat_attn_workspace_bytes(p, LAWCAT_OP_ATTN_TREE);
   if (need && (!c.ws || ws_bytes < need)) return LAWCAT_ERR_WORKSPACE_TOO_SMALL;
-  if (!attn_tc_supported(c.dtype, c.d, c.exact)) return launch_tree_exact(c);
+  if (!tree_tc_supported(c)) return launch_tree_exact(c);
   return c.a.kq ? launch_attn_tree_quant_tc(c) : launch_attn_tree_tc(c);
 }
 
@@ -434,7 +437,7 @@ size_t attn_tree_workspace_bytes(const lawcat_attn_params* p) {
   if (tree_check(p) != LAWCAT_OK) return 0;
   const AttnTree c = make_tree(p);
   if (c.a.B == 0 || c.a.N == 0) return 0;
-  if (attn_tc_supported(c.dtype, c.d, c.exact)) return std::max(attn_tree_tc_workspace_bytes(c), attn_tree_quant_tc_workspace_bytes(c));
+  if (tree_tc_supported(c)) return std::max(attn_tree_tc_workspace_bytes(c), attn_tree_quant_tc_workspace_bytes(c));
   return part_bytes(c, attn::tree_parts(c));
 }
 

@@ -135,8 +135,9 @@ __device__ __forceinline__ void row_group(const TreeArgs& a, bool v, int b, int 
 }
 
 // One row by one warp, from the keys that it sees alone, 32 at a time: a lane's key for the scores, all lanes' channels for the values.
+// (c_first, channels: those that are stored.)
 template <typename T, int D, bool QUANT>
-__device__ __noinline__ void tree_row_again(const TreeArgs& a, int b, int node, int h) {
+__device__ __noinline__ void tree_row_again(const TreeArgs& a, int b, int node, int h, int c_first = 0, int channels = D) {
   constexpr int NC = D / 32 > 0 ? D / 32 : 1, GS = quant_group(D);
   const int lane = threadIdx.x & 31, g = h / (a.H / a.H_kv), pos = a.pos[b];
   const size_t row = ((size_t)b * a.N + node) * a.H + h;
@@ -215,7 +216,7 @@ __device__ __noinline__ void tree_row_again(const TreeArgs& a, int b, int node, 
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int c = 0; c < NC; ++c)
-    if (lane + 32 * c < D) stf<T>((T*)a.o + row * D + lane + 32 * c, l == 0.f ? 0.f : acc[c] * inv);
+    if (lane + 32 * c < D && lane + 32 * c >= c_first && lane + 32 * c < c_first + channels) stf<T>((T*)a.o + row * D + lane + 32 * c, l == 0.f ? 0.f : acc[c] * inv);
 }
 
 }  // namespace attn

@@ -45,25 +45,50 @@ __device__ __forceinline__ uint4 unpack8(uint32_t w, const GroupScale& g) {
 template <int D, int NCOL>
 struct ColLay {
   static constexpr int NG = D / 32, WPR = D / 8;
-  static constexpr uint32_t V = 128 * D * 2, OFF_Q = V, OFF_P = OFF_Q + (D / 64) * NCOL * 128, OFF_COL = OFF_P + (NCOL / 8) * 2048;
-  static constexpr uint32_t OFF_ON = OFF_COL + 6 * NCOL * 4, OFF_RED = OFF_ON + NCOL * (TREE_MAX / 32) * 4, OFF_BAR = OFF_RED + 6 * NCOL * 4;
-  static constexpr uint32_t BYTES0 = OFF_BAR + 64, BYTES = BYTES0 > 32768u ? BYTES0 : 32768u;   // (D = 64: the product reads 32 KB from V on)
+  static constexpr uint32_t OFF_Q = 32768, OFF_P = OFF_Q + (D / 64) * NCOL * 128, OFF_COL = OFF_P + (NCOL / 8) * 2048;   // (D = 64: the product reads 32 KB from V on)
+  static constexpr uint32_t OFF_ON = OFF_COL + 8 * NCOL * 4, OFF_RED = OFF_ON + NCOL * (TREE_MAX / 32) * 4, OFF_BAR = OFF_RED + 6 * NCOL * 4, BYTES = OFF_BAR + 64;
+  static constexpr uint32_t OFF_CODES = 0, OFF_PAIRS = 128 * WPR * 4, STAGED = OFF_PAIRS + 128 * NG * 4;   // a node tile's keys as the cache would hold them, then its values
   static constexpr uint32_t K_COLS = D / 2, COLS = K_COLS + 2 * NCOL <= 128 ? 128 : 256;
   static constexpr int RESIDENT = COLS == 128 ? 4 : 2;
-  static_assert(K_COLS + 2 * NCOL <= COLS && OFF_P % 1024 == 0 && OFF_BAR % 16 == 0 && sizeof(Paths) <= V && RESIDENT * BYTES <= 232448, "layout");
+  static_assert(K_COLS + 2 * NCOL <= COLS && OFF_P % 1024 == 0 && OFF_BAR % 16 == 0 && sizeof(Paths) <= OFF_Q && 2 * STAGED <= OFF_Q && RESIDENT * (BYTES + 1024) <= 233472, "layout");
 };
+
+// Sums (or maxima) of N columns over a warp, lane l ending with column l (and l + 32 in the second of two, l % 16 of 16): halves of the columns
+// change places at each step, so that 31 exchanges do for 32 columns.
+template <int N, typename F>
+__device__ __forceinline__ float across(float (&x)[N], int lane, F op) {
+  static_assert(N == 16 || N == 32, "");
+  float y[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) y[i] = x[i];
+  if constexpr (N == 16) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = op(y[i], __shfl_xor_sync(0xffffffffu, y[i], 16));
+  }
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const float give = up ? y[i] : y[i + o], keep = up ? y[i + o] : y[i];
+      y[i] = op(keep, __shfl_xor_sync(0xffffffffu, give, o));
+    }
+  }
+  return y[0];
+}
 
 // BIAS: distance biases
 template <int D, int NCOL, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quant_tc_kernel(const __grid_constant__ TreeTcArgs f) {
   using L = ColLay<D, NCOL>;
-  constexpr int NG = L::NG, WPR = L::WPR;
+  constexpr int NG = L::NG, WPR = L::WPR, QV = NCOL * (D / 8) / 128;   // QV: vectors of queries per thread
   extern __shared__ __align__(1024) uint8_t smem[];
   const TreeArgs& a = f.a;
   const uint32_t sb = smem_u32(smem);
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  float* const s_sc = reinterpret_cast<float*>(smem + L::OFF_COL);   // [NCOL / 2] (scale, scale, -reference, -reference) of two columns; CAP: scale without the softmax's
-  float* const s_bias = s_sc + 2 * NCOL;                             // [NCOL / 2] (-slope, -slope, -slope depth, -slope depth)
+  float* const s_ref = reinterpret_cast<float*>(smem + L::OFF_COL);  // [NCOL / 2] (scale, scale, -reference, -reference) of two columns (CAP: scale without the softmax's)
+  float* const s_raw = s_ref + 2 * NCOL;                             // the same with references of zero
+  float* const s_bias = s_raw + 2 * NCOL;                            // [NCOL / 2] (-slope, -slope, -slope depth, -slope depth)
   int* const s_far = reinterpret_cast<int*>(s_bias + 2 * NCOL);      // [NCOL] the farthest key that is seen
   int* const s_depth = s_far + NCOL;
   uint32_t(*const s_on)[TREE_MAX / 32] = reinterpret_cast<uint32_t(*)[TREE_MAX / 32]>(smem + L::OFF_ON);
@@ -71,10 +96,9 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
   float* const s_factor = s_red + 4 * NCOL;
   float* const s_sum = s_factor + NCOL;
   Paths& paths = *reinterpret_cast<Paths*>(smem);                    // (over V, ahead of a segment's tiles)
-  volatile int* const s_flags = reinterpret_cast<volatile int*>(smem + L::OFF_BAR + 16);   // tensor memory, abort, rows to be computed again
+  volatile int* const s_flags = reinterpret_cast<volatile int*>(smem + L::OFF_BAR + 16);   // tensor memory, abort
   volatile int* const s_abort = s_flags + 1;
-  uint32_t* const s_bad = const_cast<uint32_t*>(reinterpret_cast<volatile uint32_t*>(s_flags + 2));     // [2]
-  uint32_t* const s_large = s_bad + 2;
+  uint32_t* const s_bad = reinterpret_cast<uint32_t*>(smem + L::OFF_BAR + 24);             // [2] rows to be computed again
   const uint32_t bar_s = sb + L::OFF_BAR, bar_o = bar_s + 8;
   const int G = a.H / a.H_kv, R = a.N * G;
 
@@ -82,6 +106,7 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
     mbar_init(bar_s, 1);
     mbar_init(bar_o, 1);
     s_flags[1] = 0;
+    s_bad[0] = s_bad[1] = 0u;
     mbar_fence_init();
   }
   behind_last_kernel();
@@ -103,16 +128,12 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
     const int b = w.b, pos = w.pos, r0 = w.rb * NCOL, n = w.n;
     const Ring<128> ring = ring_of<128>(pos, a.C, a.W);
     const size_t head = ((size_t)b * a.H_kv + w.g) * a.C;
-    // this thread's slot of a tile
+    // this thread's slot of a tile: codes and (scale, minimum) pairs; zeros where no row may see it
     uint32_t kc[WPR], vc[WPR], kp[NG], vp[NG];
-    auto slot_of = [&](int it, size_t& row) {   // whether any row may see it
-      const CachedTile t = cached_tile(ring, it - f.node_tiles, a.C);
-      row = head + (t.s0 + tid);
-      return tid >= t.lo && t.s0 + tid >= 0 && t.back0 - tid <= ring.cached;
-    };
     auto fetch = [&](int it, const uint8_t* q, const bf16* p, uint32_t (&codes)[WPR], uint32_t (&pairs)[NG]) {
-      size_t row;
-      if (slot_of(it, row)) {
+      const CachedTile t = cached_tile(ring, it - f.node_tiles, a.C);
+      if (tid >= t.lo && t.s0 + tid >= 0 && t.back0 - tid <= ring.cached) {
+        const size_t row = head + (t.s0 + tid);
 #pragma unroll
         for (int i = 0; i < WPR / 4; ++i) {
           const uint4 x = __ldcs(reinterpret_cast<const uint4*>(q + row * (D / 2)) + i);
@@ -132,40 +153,16 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
         for (int i = 0; i < NG; ++i) pairs[i] = 0u;
       }
     };
-    // a node's row as the cache would hold it
-    auto hold = [&](const void* src, bool some, int node, uint32_t (&codes)[WPR], uint32_t (&pairs)[NG]) {
-#pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        pairs[i] = codes[4 * i] = codes[4 * i + 1] = codes[4 * i + 2] = codes[4 * i + 3] = 0u;
-        if (!some) continue;
-        const bf16* const p = (const bf16*)src + (((size_t)b * a.N + node) * a.H_kv + w.g) * D + i * 32;
-        float x[32];
-#pragma unroll
-        for (int j = 0; j < 32; j += 8) {
-          float y[8];
-          load8(p + j, y);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[j + e] = y[e];
-        }
-        float lo = x[0], hi = x[0], scale, low;
-#pragma unroll
-        for (int j = 1; j < 32; ++j) {
-          lo = min_nan(lo, x[j]);
-          hi = max_nan(hi, x[j]);
-        }
-        quant_params(lo, hi, isfinite(lo) && isfinite(hi), scale, low);
-        const float inv = __frcp_rn(scale);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) codes[4 * i + j / 8] |= code_bits(quant_code(x[j], scale, low, inv)) << (4 * (j & 7));
-        pairs[i] = pack_bf16(scale, low);
-      }
-    };
-    if (w.t0 >= f.node_tiles) {
-      fetch(w.t0, a.kq, a.kp, kc, kp);
-      fetch(w.t0, a.vq, a.vp, vc, vp);
-    }
 
     // ------------------------------------------------------------------------------------------------ rows
+    // (queries of rows that are not there may be anything: a column of the products each, which nothing else meets)
+    uint4 q[QV];
+#pragma unroll
+    for (int i = 0; i < QV; ++i) {
+      const int at = tid + 128 * i, r = min(r0 + at / (D / 8), R - 1), node = quot(r, f.group);
+      q[i] = *reinterpret_cast<const uint4*>((const bf16*)a.q + (((size_t)b * a.N + node) * a.H + w.g * G + rest(r, node, f.group)) * D + at % (D / 8) * 8);
+    }
+    if (w.t0 >= f.node_tiles) fetch(w.t0, a.kq, a.kp, kc, kp);
     find_paths<128>(a, b, paths, tid, 1);
     int my_depth[TREE_MAX / 128];   // of this thread's nodes
 #pragma unroll
@@ -175,35 +172,30 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
       const int depth = pos >= 0 && r0 + tid < R ? node_depth(paths, node, a.N) : -1;
       const float slope = BIAS ? a.slopes[h] * LOG2E : 0.f;
       s_depth[tid] = depth;
-      s_far[tid] = depth >= 0 ? min(a.W - 1 - depth, pos) : 0x3fffffff;   // (rows that are not there weigh zeros, and are stored as zeros)
+      s_far[tid] = depth >= 0 ? min(a.W - 1 - depth, pos) : 0x3fffffff;
       const int at = tid / 2 * 4 + (tid & 1);
-      s_sc[at + 2] = depth >= 0 ? -NO_REFERENCE : 0.f;
-      s_bias[at] = depth >= 0 ? -slope : 0.f;
-      s_bias[at + 2] = depth >= 0 ? -slope * (float)depth : 0.f;
+      s_ref[at + 2] = depth >= 0 ? -NO_REFERENCE : 0.f;
+      s_raw[at + 2] = 0.f;
+      s_bias[at] = -slope;
+      s_bias[at + 2] = -slope * (float)depth;
 #pragma unroll
       for (int i = 0; i < TREE_MAX / 32; ++i) s_on[tid][i] = depth >= 0 ? paths.on[node][i] : 0u;
     }
-    if (tid == 0) {
-      s_bad[0] = s_bad[1] = s_large[0] = s_large[1] = 0u;
-    }
-    named_bar_sync(1, 128);
-#pragma unroll 2
-    for (int i = tid; i < NCOL * (D / 8); i += 128) {
-      const int c = i / (D / 8), j = i % (D / 8), r = min(r0 + c, R - 1), node = quot(r, f.group);
-      uint4 q = make_uint4(0u, 0u, 0u, 0u);
-      if (s_depth[c] >= 0) q = *reinterpret_cast<const uint4*>((const bf16*)a.q + (((size_t)b * a.N + node) * a.H + w.g * G + rest(r, node, f.group)) * D + j * 8);
-      float x[8] = {bf16_lo(q.x), bf16_hi(q.x), bf16_lo(q.y), bf16_hi(q.y), bf16_lo(q.z), bf16_hi(q.z), bf16_lo(q.w), bf16_hi(q.w)};
+#pragma unroll
+    for (int i = 0; i < QV; ++i) {
+      const int at = tid + 128 * i, c = at / (D / 8), j = at % (D / 8);
+      float x[8] = {bf16_lo(q[i].x), bf16_hi(q[i].x), bf16_lo(q[i].y), bf16_hi(q[i].y), bf16_lo(q[i].z), bf16_hi(q[i].z), bf16_lo(q[i].w), bf16_hi(q[i].w)};
       uint32_t top = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
 #pragma unroll
       for (int o = 1; o < D / 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));   // (a row's threads lie side by side)
       const uint32_t e2 = min(max(top >> 23, 1u), 253u);   // largest value in [1, 2)
-      const float down = __uint_as_float((254u - e2) << 23);
+      const float down = __uint_as_float((254u - e2) << 23), up = (CAP ? 1.f : a.scale * LOG2E) * (__uint_as_float(e2 << 23) / KV_FACTOR);
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] *= down;
       sts128(sb + L::OFF_Q + (uint32_t)(j >> 3) * (NCOL * 128) + sw128(c, j & 7), make_uint4(pack_f16(x[0], x[4]), pack_f16(x[1], x[5]), pack_f16(x[2], x[6]), pack_f16(x[3], x[7])));
-      if (j == 0) s_sc[c / 2 * 4 + (c & 1)] = (CAP ? 1.f : a.scale * LOG2E) * (s_depth[c] >= 0 ? __uint_as_float(e2 << 23) / KV_FACTOR : 0.f);
+      if (j == 0) s_ref[c / 2 * 4 + (c & 1)] = s_raw[c / 2 * 4 + (c & 1)] = up;
     }
     fence_proxy_async();
     named_bar_sync(1, 128);
@@ -215,16 +207,43 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
     for (int c = 0; c < NCOL; ++c) l[c] = 0.f;
 
     // ------------------------------------------------------------------------------------------------ tiles
+#pragma unroll 1
     for (int i = 0; i < n; ++i, ++count) {
       const int it = w.t0 + i;
       const bool fresh = it < f.node_tiles;
+      bool v_free = i == 0;   // values and weights of the tile in front have been read
       if (fresh) {
-        const int node = it * 128 + tid;
-        int depth = my_depth[0];
+        // the nodes' rows, quantized eight channels to a thread, through shared memory to their threads
+        if (!v_free && !fail) fail = !wait_bar(bar_o, (count - 1) & 1, s_abort, f.limit);
+        v_free = true;
+        const int rows = min(128, a.N - it * 128), items = (rows * WPR + 31) & ~31;
+#pragma unroll 1
+        for (int v = 0; v < 2; ++v) {
+          uint8_t* const at = smem + (v ? L::STAGED : 0u);
+#pragma unroll 1
+          for (int x = tid; x < items; x += 128) {
+            const int r = min(x / WPR, rows - 1), c0 = x % WPR * 8;
+            float y[8];
+            load8((const bf16*)(v ? a.v_t : a.k_t) + (((size_t)b * a.N + it * 128 + r) * a.H_kv + w.g) * D + c0, y);
+            quantize8<D, true>(y, c0, at + L::OFF_CODES + r * (D / 2), reinterpret_cast<bf16*>(at + L::OFF_PAIRS) + r * (2 * NG), x < rows * WPR, 0xffffffffu);
+          }
+        }
+        named_bar_sync(1, 128);
+        const bool there = (it == 0 ? my_depth[0] : my_depth[1]) >= 0;
+        const uint32_t at = sb + tid * (D / 2), pt = sb + L::OFF_PAIRS + tid * (4 * NG);
 #pragma unroll
-        for (int e = 1; e < TREE_MAX / 128; ++e) depth = it == e ? my_depth[e] : depth;
-        hold(a.k_t, depth >= 0, node, kc, kp);
-        hold(a.v_t, depth >= 0, node, vc, vp);
+        for (int e = 0; e < WPR; e += 4) {
+          const uint4 zero = make_uint4(0u, 0u, 0u, 0u), x = there ? lds128(at + 4 * e) : zero, y = there ? lds128(at + L::STAGED + 4 * e) : zero;
+          kc[e] = x.x; kc[e + 1] = x.y; kc[e + 2] = x.z; kc[e + 3] = x.w;
+          vc[e] = y.x; vc[e + 1] = y.y; vc[e + 2] = y.z; vc[e + 3] = y.w;
+        }
+#pragma unroll
+        for (int e = 0; e < NG; ++e) {
+          kp[e] = there ? *reinterpret_cast<const uint32_t*>(smem + (pt - sb) + 4 * e) : 0u;
+          vp[e] = there ? *reinterpret_cast<const uint32_t*>(smem + (pt - sb) + L::STAGED + 4 * e) : 0u;
+        }
+      } else {
+        fetch(it, a.vq, a.vp, vc, vp);
       }
 #pragma unroll
       for (int s = 0; s < D / 64; ++s) {
@@ -247,42 +266,43 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
         mma_commit(bar_s);
       }
       __syncwarp();
-      const bool more = i + 1 < n && it + 1 >= f.node_tiles;
-      if (more) fetch(it + 1, a.kq, a.kp, kc, kp);
-      // (values and weights of the tile in front have been read)
-      if (i > 0 && !fail) fail = !wait_bar(bar_o, (count - 1) & 1, s_abort, f.limit);
+      if (i + 1 < n && it + 1 >= f.node_tiles) fetch(it + 1, a.kq, a.kp, kc, kp);
+      if (!v_free && !fail) fail = !wait_bar(bar_o, (count - 1) & 1, s_abort, f.limit);
       __syncwarp();
 #pragma unroll
       for (int e = 0; e < WPR; ++e) sts128(sb + (uint32_t)(e >> 3) * 16384 + sw128(tid, e & 7), unpack8(vc[e], group_scale(vp[e / 4])));
-      if (more) fetch(it + 1, a.vq, a.vp, vc, vp);
       if (!fail) fail = !wait_bar(bar_s, count & 1, s_abort, f.limit);
       __syncwarp();
       tc_fence_after_sync();
 
       CachedTile t{0, 0, 0};
       if (!fresh) t = cached_tile(ring, it - f.node_tiles, a.C);
-      const int back = t.back0 - tid;
+      const int back = t.back0 - tid, mine = it == 0 ? my_depth[0] : my_depth[1];
       const bool whole = !fresh && t.back0 <= far_all && t.lo == 0;   // every row sees every slot
+      const float dist = fresh ? -(float)mine : (float)back;          // (to a row of depth zero)
       float z[NCOL];
-      // scores in log2 units, less the references (or not)
-      auto scores = [&](bool relative) {
+      // Scores in log2 units, less the references: as they stand, or (a segment's first tile, or one of them is more than 2^8 too low) without
+      // any, whose maxima become the new ones, and then less those.
+      bool again = false;
+      const float* table = i == 0 ? s_raw : s_ref;
+#pragma unroll 1
+      for (;;) {
 #pragma unroll
         for (int c = 0; c < NCOL; c += 16) tmem_ld16(s_col + lanes + c, z + c);
         tmem_wait_ld();
         if constexpr (CAP) {
 #pragma unroll
-          for (int c = 0; c < NCOL; ++c) z[c] *= s_sc[c / 2 * 4 + (c & 1)];
+          for (int c = 0; c < NCOL; ++c) z[c] *= s_ref[c / 2 * 4 + (c & 1)];
           cap_scores(z, a.scale / a.cap, a.cap * LOG2E);
         }
-        const float d = fresh ? 0.f : (float)back;
-        const uint64_t back2 = f2_pack(d, d);
+        const uint64_t dist2 = f2_pack(dist, dist);
 #pragma unroll
         for (int c = 0; c < NCOL; c += 2) {
-          const float4 k = *reinterpret_cast<const float4*>(s_sc + 2 * c);
-          uint64_t add = relative ? f2_pack(k.z, k.w) : 0ull;
+          const float4 k = *reinterpret_cast<const float4*>(table + 2 * c);
+          uint64_t add = f2_pack(k.z, k.w);
           if constexpr (BIAS) {
             const float4 e = *reinterpret_cast<const float4*>(s_bias + 2 * c);
-            add = f2_add(add, f2_fma(f2_pack(e.x, e.y), back2, f2_pack(e.z, e.w)));
+            add = f2_add(add, f2_fma(f2_pack(e.x, e.y), dist2, f2_pack(e.z, e.w)));
           }
           const uint64_t x = f2_pack(z[c], z[c + 1]);
           f2_unpack(CAP ? f2_add(x, add) : f2_fma(x, f2_pack(k.x, k.y), add), z[c], z[c + 1]);
@@ -290,49 +310,47 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
         if (!whole) {
           if (fresh) {   // nodes of the row's path, by their distance
             const int j = it * 128 + tid;
-            int mine = my_depth[0];
 #pragma unroll
-            for (int e = 1; e < TREE_MAX / 128; ++e) mine = it == e ? my_depth[e] : mine;
-#pragma unroll
-            for (int c = 0; c < NCOL; ++c) {
-              const bool see = (s_on[c][j >> 5] >> (j & 31) & 1u) && s_depth[c] - mine < a.W;
-              if constexpr (BIAS) z[c] -= s_bias[c / 2 * 4 + (c & 1)] * (float)mine;   // (back = -depth)
-              z[c] = see ? z[c] : -INFINITY;
-            }
+            for (int c = 0; c < NCOL; ++c) z[c] = (s_on[c][j >> 5] >> (j & 31) & 1u) && s_depth[c] - mine < a.W ? z[c] : -INFINITY;
           } else {
 #pragma unroll
             for (int c = 0; c < NCOL; ++c) z[c] = back <= s_far[c] && tid >= t.lo ? z[c] : -INFINITY;
           }
         }
-      };
-      scores(true);
-      float mx0 = z[0], mx1 = z[1];
+        if (again) break;
+        if (table == s_ref) {
+          float mx0 = z[0], mx1 = z[1];
 #pragma unroll
-      for (int c = 2; c < NCOL; c += 2) {
-        mx0 = fmaxf(mx0, z[c]);
-        mx1 = fmaxf(mx1, z[c + 1]);
-      }
-      if (named_bar_or(3, 128, fmaxf(mx0, mx1) > COL_RESCALE || fail)) {
-        // new references: the block's maximum of each row
-        if (named_bar_or(3, 128, fail)) break;
-        scores(false);
-#pragma unroll
-        for (int c = 0; c < NCOL; ++c) {
-          const float x = warp_max(z[c]);
-          if (lane == 0) s_red[warp * NCOL + c] = x;
+          for (int c = 2; c < NCOL; c += 2) {
+            mx0 = fmaxf(mx0, z[c]);
+            mx1 = fmaxf(mx1, z[c + 1]);
+          }
+          if (!named_bar_or(3, 128, fmaxf(mx0, mx1) > COL_RESCALE || fail)) break;
+          if (named_bar_or(3, 128, fail)) break;
+          table = s_raw;
+          continue;
+        }
+        auto larger = [](float x, float y) { return fmaxf(x, y); };
+        if constexpr (NCOL <= 32) {
+          const float x = across<NCOL>(z, lane, larger);
+          if (lane < NCOL) s_red[warp * NCOL + lane] = x;
+        } else {
+          float(&lo)[32] = *reinterpret_cast<float(*)[32]>(z), (&hi)[32] = *reinterpret_cast<float(*)[32]>(z + 32);
+          s_red[warp * NCOL + lane] = across<32>(lo, lane, larger);
+          s_red[warp * NCOL + 32 + lane] = across<32>(hi, lane, larger);
         }
         named_bar_sync(3, 128);
         if (tid < NCOL) {
           const float x = fmaxf(fmaxf(s_red[tid], s_red[NCOL + tid]), fmaxf(s_red[2 * NCOL + tid], s_red[3 * NCOL + tid]));
-          float& neg = s_sc[tid / 2 * 4 + 2 + (tid & 1)];
+          float& neg = s_ref[tid / 2 * 4 + 2 + (tid & 1)];
           const bool grow = x > -neg + COL_RESCALE;
           s_factor[tid] = grow ? ex2f(-neg - x) : 1.f;
           if (grow) neg = -x;
         }
         named_bar_sync(3, 128);
-#pragma unroll
-        for (int c = 0; c < NCOL; ++c) l[c] *= s_factor[c];
         if (i > 0) {
+#pragma unroll
+          for (int c = 0; c < NCOL; ++c) l[c] *= s_factor[c];
 #pragma unroll
           for (int c = 0; c < NCOL; c += 16) {
             float o[16];
@@ -344,23 +362,23 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
           }
           tmem_wait_st();
         }
-        scores(true);
+        table = s_ref;
+        again = true;
       }
 #pragma unroll
       for (int c = 0; c < NCOL; c += 8) {
         uint32_t p[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = ex2f(z[c + 2 * e]), y = ex2f(z[c + 2 * e + 1]);
-          l[c + 2 * e] += x;
-          l[c + 2 * e + 1] += y;
-          p[e] = pack_f16(x, y);
+        for (int e = 0; e < 8; e += 2) {
+          const float x = ex2f(z[c + e]), y = ex2f(z[c + e + 1]);
+          f2_unpack(f2_add(f2_pack(l[c + e], l[c + e + 1]), f2_pack(x, y)), l[c + e], l[c + e + 1]);
+          p[e / 2] = pack_f16(x, y);
         }
         sts128(sb + L::OFF_P + (uint32_t)(c / 8) * 2048 + tid * 16, make_uint4(p[0], p[1], p[2], p[3]));
       }
       fence_proxy_async();
       tc_fence_before_sync();
-      named_bar_sync(4, 128);
+      if (named_bar_or(4, 128, fail)) break;
       if (warp == 0 && elect_one()) {
         constexpr uint32_t id_o = instr_desc(128, NCOL, FMT_F16, MAJOR_MN, MAJOR_MN);
         tc_fence_after_sync();
@@ -372,58 +390,75 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
     }
 
     // ------------------------------------------------------------------------------------------------ outputs
+    {
+      auto sum = [](float x, float y) { return x + y; };
+      if constexpr (NCOL <= 32) {
+        const float x = across<NCOL>(l, lane, sum);
+        if (lane < NCOL) s_red[warp * NCOL + lane] = x;
+      } else {
+        float(&lo)[32] = *reinterpret_cast<float(*)[32]>(l), (&hi)[32] = *reinterpret_cast<float(*)[32]>(l + 32);
+        s_red[warp * NCOL + lane] = across<32>(lo, lane, sum);
+        s_red[warp * NCOL + 32 + lane] = across<32>(hi, lane, sum);
+      }
+    }
     if (!fail) fail = !wait_bar(bar_o, (count - 1) & 1, s_abort, f.limit);
     if (named_bar_or(3, 128, fail)) break;
     tc_fence_after_sync();
-#pragma unroll
-    for (int c = 0; c < NCOL; ++c) {
-      const float x = warp_sum(l[c]);
-      if (lane == 0) s_red[warp * NCOL + c] = x;
-    }
-    named_bar_sync(3, 128);
     const bool direct = is_whole(w);
     const size_t slot = piece_slot(w, (int)blockIdx.x);
     if (tid < NCOL) {
-      float sum = s_red[tid] + s_red[NCOL + tid] + s_red[2 * NCOL + tid] + s_red[3 * NCOL + tid];
+      float sum = (s_red[tid] + s_red[NCOL + tid]) + (s_red[2 * NCOL + tid] + s_red[3 * NCOL + tid]);
       if (s_depth[tid] < 0) sum = 0.f;
-      s_sum[tid] = sum;
-      const float m = -s_sc[tid / 2 * 4 + 2 + (tid & 1)];
+      s_sum[tid] = direct ? sum == 0.f ? 0.f : 1.f / (sum * KV_FACTOR) : 1.f / KV_FACTOR;
+      const float m = -s_ref[tid / 2 * 4 + 2 + (tid & 1)];
       if (!direct && r0 + tid < R) f.part_ml[slot * f.rows_pad + tid] = make_float2(sum == 0.f ? -INFINITY : m, sum);
     }
-    named_bar_sync(3, 128);
     float o[NCOL];
 #pragma unroll
     for (int c = 0; c < NCOL; c += 16) tmem_ld16(o_col + lanes + c, o + c);
     tmem_wait_ld();
-    const int ch = (tid & ~7) + ((tid & 7) >> 1) + 4 * (tid & 1);   // the lane's channel
-#pragma unroll
-    for (int c = 0; c < NCOL; ++c) {
-      const int r = r0 + c;
-      if (r >= R) break;
-      const float sum = s_sum[c];
-      if (!direct) {
-        if (tid < D) f.part_o[(slot * f.rows_pad + c) * D + ch] = o[c] * (1.f / KV_FACTOR);
-      } else {
-        const float y = sum == 0.f ? 0.f : o[c] / (sum * KV_FACTOR);
-        const int node = quot(r, f.group);
-        if (tid < D) ((bf16*)a.o)[(((size_t)b * a.N + node) * a.H + w.g * G + rest(r, node, f.group)) * D + ch] = __float2bfloat16_rn(y);
-        const uint32_t bad = __ballot_sync(0xffffffffu, tid < D && !isfinite(y)), large = __ballot_sync(0xffffffffu, tid < D && !(fabsf(y) < SMALL));
-        if (lane == 0) {
-          if (bad) atomicOr(s_bad + c / 32, 1u << (c & 31));
-          if (large || sum == 0.f) atomicOr(s_large + c / 32, 1u << (c & 31));
-        }
-      }
-    }
-    tc_fence_before_sync();
     named_bar_sync(3, 128);
-    if (direct) {
+    const int ch = (tid & ~7) + ((tid & 7) >> 1) + 4 * (tid & 1);   // the lane's channel
+    if (!direct) {
+      float* const dst = f.part_o + slot * f.rows_pad * D + ch;
+#pragma unroll
+      for (int c = 0; c < NCOL; ++c)
+        if (r0 + c < R && tid < D) dst[c * D] = o[c] * s_sum[c];
+      tc_fence_before_sync();
+      named_bar_sync(3, 128);
+    } else {
+      bf16* const s_out = reinterpret_cast<bf16*>(smem);   // [NCOL][D] over V
+#pragma unroll
+      for (int c = 0; c < NCOL; ++c)
+        if (tid < D) s_out[c * D + ch] = __float2bfloat16_rn(s_sum[c] == 0.f ? 0.f : o[c] * s_sum[c]);
+      tc_fence_before_sync();
+      named_bar_sync(3, 128);
 #pragma unroll 1
-      for (int c = warp; c < NCOL && r0 + c < R; c += 4)
-        if ((s_bad[c / 32] | ~s_large[c / 32]) >> (c & 31) & 1u) {
-          const int node = quot(r0 + c, f.group);
-          tree_row_again<bf16, D, true>(a, b, node, w.g * G + rest(r0 + c, node, f.group));
-        }
-      named_bar_sync(3, 128);   // (the flags have been read)
+      for (int x = tid; x < NCOL * (D / 8); x += 128) {
+        const int c = x / (D / 8), r = r0 + c, node = quot(min(r, R - 1), f.group);
+        const uint4 y = lds128(sb + x * 16);
+        if (r < R) *reinterpret_cast<uint4*>((bf16*)a.o + (((size_t)b * a.N + node) * a.H + w.g * G + rest(r, node, f.group)) * D + x % (D / 8) * 8) = y;
+        // rows to be computed again: not finite somewhere, or small everywhere
+        const uint32_t u[4] = {y.x & 0x7fff7fffu, y.y & 0x7fff7fffu, y.z & 0x7fff7fffu, y.w & 0x7fff7fffu};
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = max(top, max(u[e] >> 16, u[e] & 0xffffu));
+#pragma unroll
+        for (int m = 1; m < D / 8; m <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, m));
+        if (x % (D / 8) == 0 && r < R && s_depth[c] >= 0 && (top >= 0x7f80u || __uint_as_float(top << 16) < SMALL)) atomicOr(s_bad + c / 32, 1u << (c & 31));
+      }
+      named_bar_sync(3, 128);
+      if (s_bad[0] | s_bad[1]) {
+#pragma unroll 1
+        for (int c = warp; c < NCOL && r0 + c < R; c += 4)
+          if (s_bad[c / 32] >> (c & 31) & 1u) {
+            const int node = quot(r0 + c, f.group);
+            tree_row_again<bf16, D, true>(a, b, node, w.g * G + rest(r0 + c, node, f.group));
+          }
+        named_bar_sync(3, 128);
+        if (tid < 2) s_bad[tid] = 0u;
+        named_bar_sync(3, 128);
+      }
     }
   }
   __syncthreads();
@@ -443,13 +478,15 @@ static int columns(int N, int H, int H_kv) {
 template <int NCOL>
 static TreePlan cols_plan(const AttnTree& c) {
   const TreeArgs& a = c.a;
-  return tree_plan(a.B, a.N, a.H, a.H_kv, a.C, a.W, NCOL, 128, ColLay<128, NCOL>::RESIDENT);
+  return tree_plan(a.B, a.N, a.H, a.H_kv, a.C, a.W, NCOL, NCOL, NCOL, 128, ColLay<128, NCOL>::RESIDENT);
 }
 
 template <int D, int NCOL, bool CAP, bool BIAS>
 static int tree_quant_tc(const AttnTree& c) {
   using L = ColLay<D, NCOL>;
-  const TreeTcArgs f = tree_tc_args(c, cols_plan<NCOL>(c));
+  const TreePlan p = cols_plan<NCOL>(c);
+  if (!p.fits) return LAWCAT_ERR_UNSUPPORTED;
+  const TreeTcArgs f = tree_tc_args(c, p);
   constexpr auto kernel = attn_tree_quant_tc_kernel<D, NCOL, CAP, BIAS>;
   if (int r = grant_smem<kernel>(L::BYTES)) return r;
   LAWCAT_LAUNCH("attn_tree_quant_tc", c.stream, launch_behind(kernel, dim3((unsigned)f.shares), dim3(128), L::BYTES, c.stream, f));

@@ -2,11 +2,11 @@
 //
 // A block walks segments of up to 256 rows (node, query head) of one (sequence, key-value head) and their keys, in tiles of 64:
 //   two warpgroups    softmax, one thread per row: S from tensor memory, masks, running maximum and sum in registers, P = exp2(x - m) over S;
-//                     a segment's queries into shared memory, its outputs out of tensor memory
-//   copy warp         K and V tiles through a ring of stages by TMA, on into the next segment while this one ends
+//                     then the segment's outputs
+//   copy warp         queries, K and V tiles (through a ring of stages) by TMA, on into the next segment while this one ends
 //   product warp      S = Q K^T (shared memory), O += P V (P from tensor memory); fp32 accumulation
-// Of more than 128 rows each warpgroup has a tile of 128, and both meet every key; of fewer, both have the same rows and take the key tiles in
-// turn, each with sums of its own that meet at the segment's end. S has two places per warpgroup; O is rescaled only when a maximum grew by
+// A tile of rows is as many whole nodes as 128 rows hold. Of two tiles each warpgroup has one, and both meet every key; of one, both have its
+// rows and take the key tiles in turn, each with sums of its own (in the same lanes of tensor memory) that meet at the segment's end. S has two places per warpgroup; O is rescaled only when a maximum grew by
 // more than 2^8.
 //
 // The keys are walked from the newest to the oldest: the nodes' own rows first (the values of nodes that are not there are set to zero), then
@@ -28,17 +28,17 @@ struct TreeTc {
   static constexpr uint32_t TILE = 128 * D * 2, KT = 64 * D * 2;   // rows' queries; keys or values of a tile
   static constexpr int ST = D == 64 ? 16 : 8;                      // stages, K and V tiles in turn
   static constexpr uint32_t OFF_RING = 2 * TILE, OFF_PATHS = OFF_RING + ST * KT, OFF_DEPTH = OFF_PATHS + sizeof(Paths), OFF_ML = OFF_DEPTH + TREE_MAX * 4;
-  static constexpr uint32_t OFF_BAR = OFF_ML + 128 * 8, BYTES = OFF_BAR + 512;
+  static constexpr uint32_t OFF_BAD = OFF_ML + 256 * 8, OFF_BAR = OFF_BAD + 64, BYTES = OFF_BAR + 512;
   static constexpr int THREADS = 320;
-  static constexpr int B_FULL = 0, B_EMPTY = ST, B_S = 2 * ST, B_P = B_S + 4, B_O = B_P + 4, B_DONE = B_O + 4, B_Q = B_DONE + 1, B_FIX = B_Q + 1, NBAR = B_FIX + 1;
-  static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 512 && 256 + 2 * D <= 512 && 128 * D * 4 <= 2 * TILE && TREE_MAX / 64 * 2 <= ST, "shared memory, tensor memory");
+  static constexpr int B_FULL = 0, B_EMPTY = ST, B_S = 2 * ST, B_P = B_S + 4, B_O = B_P + 4, B_DONE = B_O + 4, B_Q = B_DONE + 1, B_QE = B_Q + 2, B_OE = B_QE + 2, B_FIX = B_OE + 1, NBAR = B_FIX + 1;
+  static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 512 && 256 + 2 * D <= 512 && TREE_MAX / 64 * 2 <= ST, "shared memory, tensor memory");
 };
 
 // BIAS also serves a scale that is not positive: the scores are scaled before anything else looks at them
 template <int D, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(TreeTc<D>::THREADS, 1)
 attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_kt,
-                    const __grid_constant__ CUtensorMap tm_vt, const __grid_constant__ TreeTcArgs f) {
+                    const __grid_constant__ CUtensorMap tm_vt, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ TreeTcArgs f) {
   using L = TreeTc<D>;
   constexpr int ST = L::ST;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -48,8 +48,10 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   volatile int* const s_flags = reinterpret_cast<volatile int*>(smem + L::OFF_BAR + 8 * L::NBAR);   // tmem base, abort
   volatile int* const s_abort = s_flags + 1;
   auto bar = [&](int i) { return sb + L::OFF_BAR + 8 * (uint32_t)i; };
+  uint32_t* const s_bad = reinterpret_cast<uint32_t*>(smem + L::OFF_BAD);   // [8] rows to be computed again
   const int G = a.H / a.H_kv, R = a.N * G;
-  const bool two = f.rows == 256;
+  const bool two = f.rows > f.tile_rows;
+  const int q_tiles = two ? 2 : 1, q_places = two ? 1 : 2;   // of a segment, and segments whose queries fit
 
   if (tid == 0) {
     for (int i = 0; i < ST; ++i) {
@@ -62,10 +64,16 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       mbar_init(bar(L::B_O + i), 1);
     }
     mbar_init(bar(L::B_DONE), 1);
-    mbar_init(bar(L::B_Q), 256);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar(L::B_Q + i), 1);
+      mbar_init(bar(L::B_QE + i), 1);
+    }
+    mbar_init(bar(L::B_OE), 256);
     mbar_init(bar(L::B_FIX), 256);
     s_flags[1] = 0;
+    for (int i = 0; i < 8; ++i) s_bad[i] = 0u;
     mbar_fence_init();
+    tma_prefetch_desc(&tm_q);
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
     tma_prefetch_desc(&tm_kt);
@@ -92,34 +100,19 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     // ------------------------------------------------------------------------------------------------ softmax
     Paths& paths = *reinterpret_cast<Paths*>(smem + L::OFF_PATHS);
     int* const s_depth = reinterpret_cast<int*>(smem + L::OFF_DEPTH);
-    float* const s_o = reinterpret_cast<float*>(smem);   // [D / 4][128] four channels of a row, over the queries of a segment that is done
-    float2* const s_ml = reinterpret_cast<float2*>(smem + L::OFF_ML);
+    float2* const s_ml = reinterpret_cast<float2*>(smem + L::OFF_ML);   // [2][128]
     const int u = warp >> 2, r128 = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, O = o_col(u) + lanes;
     int step = 0, seq = 0, at = 0, b_last = -1;   // steps, pieces and tiles so far
     bool ok = true;
     while (walk.next(f, w)) {
-      const int b = w.b, pos = w.pos, r0 = w.rb * f.rows, n = w.n, steps = steps_of(u, n), node_tiles = max(0, min(f.node_tiles - w.t0, n));
+      const int b = w.b, pos = w.pos, n = w.n, steps = steps_of(u, n), node_tiles = max(0, min(f.node_tiles - w.t0, n));
       if (b != b_last) {
         find_paths<256>(a, b, paths, tid, 1);
         if (tid < a.N) s_depth[tid] = pos < 0 ? -1 : node_depth(paths, tid, a.N);
         named_bar_sync(1, 256);
         b_last = b;
       }
-      // queries; rows that are not there are zeros
-      const int q_rows = two ? 256 : 128;
-#pragma unroll 4
-      for (int i = tid; i < q_rows * (D / 8); i += 256) {
-        const int r = i / (D / 8), j = i % (D / 8), row = r0 + r;
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (row < R) {
-          const int node = quot(row, f.group);
-          if (s_depth[node] >= 0) x = *reinterpret_cast<const uint4*>((const bf16*)a.q + (((size_t)b * a.N + node) * a.H + w.g * G + rest(row, node, f.group)) * D + j * 8);
-        }
-        sts128(sb + (uint32_t)(r >> 7) * L::TILE + (uint32_t)(j >> 3) * 16384 + sw128(r & 127, j & 7), x);
-      }
-      fence_proxy_async();
-      mbar_arrive(bar(L::B_Q));
       // the values of nodes that are not there: zeros (their weights are, and whatever they hold must not meet those)
       for (int it = 0; it < node_tiles; ++it) {
         const int st = 2 * (at + it) + 1, k = (w.t0 + it) * 64 + (tid >> 2);
@@ -136,12 +129,13 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       __syncwarp();
       ok = __all_sync(0xffffffffu, ok);
 
-      const int r = r0 + (two ? 128 * u : 0) + r128, node = quot(min(r, R - 1), f.group), h = w.g * G + rest(min(r, R - 1), node, f.group);
+      const int rp = (two ? 128 * u : 0) + r128, r = row_of_piece(f, w.rb, rp);
+      const int node = quot(min(r, R - 1), f.group), h = w.g * G + rest(min(r, R - 1), node, f.group);
       const int depth = s_depth[node];
       const bool there = r < R && depth >= 0;
       const float scale2 = a.scale * LOG2E, slope2 = BIAS && a.slopes ? a.slopes[h] * LOG2E : 0.f;
       const Ring<64> ring = ring_of<64>(pos, a.C, a.W);
-      // the farthest key that the row sees, and the least of the warp's (rows that are not there weigh zeros, and are stored as zeros)
+      // the farthest key that the row sees, and the least of the warp's (of rows that are not there nothing is stored but zeros)
       const int far = there ? min(a.W - 1 - depth, pos) : 0x3fffffff;
       const int far_all = __reduce_min_sync(0xffffffffu, far);
       const bool idle = !__any_sync(0xffffffffu, there);
@@ -266,99 +260,94 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       // ---------------------------------------------------------------------------------------------- outputs
       ok = ok && __all_sync(0xffffffffu, wait_bar(bar(L::B_DONE), seq & 1, s_abort, item_limit(f.limit, n)));
       tc_fence_after_sync();
+      // with one tile of rows a warpgroup has half of the channels of both sums
+      const bool direct = is_whole(w);
+      float f0 = 1.f, f1 = 0.f;
       if (!two) {
-        if (u == 1) {
-          s_ml[r128] = make_float2(m, l);
-          if (steps > 0) {
-#pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-              float o[32];
-              tmem_ld32(O + c, o);
-              tmem_wait_ld();
-#pragma unroll
-              for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(s_o + ((c + e) / 4 * 128 + r128) * 4) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-            }
-          }
-        }
+        s_ml[u * 128 + r128] = make_float2(m, l);
         named_bar_sync(2, 256);
+        const float2 x = s_ml[r128], y = s_ml[128 + r128];
+        const float top = fmaxf(x.x, y.x), base = top == -INFINITY ? 0.f : top;
+        f0 = x.x == -INFINITY ? 0.f : ex2f(x.x - base);
+        f1 = y.x == -INFINITY ? 0.f : ex2f(y.x - base);
+        l = x.y * f0 + y.y * f1;
+        m = top;
       }
-      if (u == 0 || two) {
-        const bool direct = is_whole(w);
-        float fa = 1.f, fb = 0.f;
-        if (!two) {
-          const float2 ml = s_ml[r128];
-          const float top = fmaxf(m, ml.x), base = top == -INFINITY ? 0.f : top;
-          fa = m == -INFINITY ? 0.f : ex2f(m - base);
-          fb = ml.x == -INFINITY ? 0.f : ex2f(ml.x - base);
-          l = l * fa + ml.y * fb;
-          m = top;
-        }
-        const bool both = !two && steps_of(1, n) > 0, some = steps > 0;
-        if (!there) l = 0.f;
-        const float inv = !direct ? 1.f : l == 0.f ? 0.f : 1.f / l;
-        float test = l * 0.f;
-        const size_t slot = piece_slot(w, (int)blockIdx.x);
-        bf16* const dst = (bf16*)a.o + (((size_t)b * a.N + node) * a.H + h) * D;
-        const int rp = r - r0;
-        float* const pdst = f.part_o + slot * D * f.rows_pad + rp;
+      if (!there) l = 0.f;
+      const float inv = !direct ? 1.f : l == 0.f ? 0.f : 1.f / l;
+      f0 *= inv;
+      f1 *= inv;
+      float test = l * 0.f;
+      const size_t slot = piece_slot(w, (int)blockIdx.x);
+      bf16* const dst = (bf16*)a.o + (((size_t)b * a.N + node) * a.H + h) * D;
+      float* const pdst = f.part_o + slot * D * f.rows_pad + rp;
+      const int c0 = two ? 0 : u * (D / 2), c1 = two ? D : c0 + D / 2;
+      const uint32_t O0 = o_col(two ? u : 0) + lanes, O1 = o_col(1) + lanes;
+      const bool both = !two && n > 1;
 #pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          float o[32];
-          if (some) {
-            tmem_ld32(O + c, o);
-            tmem_wait_ld();
+      for (int c = c0; c < c1; c += 32) {
+        float o[32];
+        tmem_ld32(O0 + c, o);
+        if (both) {
+          float y[32];
+          tmem_ld32(O1 + c, y);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = (f0 == 0.f ? 0.f : o[e] * f0) + (f1 == 0.f ? 0.f : y[e] * f1);
+        } else {
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] *= f0;
+        }
+#pragma unroll
+        for (int e = 0; e < 32; ++e) test = fmaf(o[e], 0.f, test);
+        if (r < R) {
+          if (!direct) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) pdst[(size_t)(c + e) * f.rows_pad] = o[e];
           } else {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = 0.f;
+            for (int e = 0; e < 32; e += 8)
+              *reinterpret_cast<uint4*>(dst + c + e) = l == 0.f ? make_uint4(0u, 0u, 0u, 0u)
+                                                                : make_uint4(pack_bf16(o[e], o[e + 1]), pack_bf16(o[e + 2], o[e + 3]), pack_bf16(o[e + 4], o[e + 5]), pack_bf16(o[e + 6], o[e + 7]));
           }
-          if (!two) {
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (both) x = *reinterpret_cast<const float4*>(s_o + ((c + e) / 4 * 128 + r128) * 4);
-              const float y[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-              for (int k = 0; k < 4; ++k) o[e + k] = (fa == 0.f ? 0.f : o[e + k] * fa) + (fb == 0.f ? 0.f : y[k] * fb);
-            }
-          }
-#pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            o[e] *= inv;
-            test = fmaf(o[e], 0.f, test);
-          }
-          if (r < R) {
-            if (!direct) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) pdst[(size_t)(c + e) * f.rows_pad] = o[e];
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; e += 8)
-                *reinterpret_cast<uint4*>(dst + c + e) = l == 0.f ? make_uint4(0u, 0u, 0u, 0u)
-                                                                  : make_uint4(pack_bf16(o[e], o[e + 1]), pack_bf16(o[e + 2], o[e + 3]), pack_bf16(o[e + 4], o[e + 5]), pack_bf16(o[e + 6], o[e + 7]));
-            }
-          }
-        }
-        if (r < R && !direct) f.part_ml[slot * f.rows_pad + rp] = make_float2(m, l);
-        // rows to be computed again (of a segment in pieces the join looks)
-        uint32_t left = __ballot_sync(0xffffffffu, ok && there && direct && !(test == 0.f));
-        __syncwarp();   // (behind the stores of the row's own thread)
-        for (; left; left &= left - 1) {
-          const int from = __ffs(left) - 1;
-          tree_row_again<bf16, D, false>(a, b, __shfl_sync(0xffffffffu, node, from), __shfl_sync(0xffffffffu, h, from));
         }
       }
-      tc_fence_before_sync();   // (tensor memory has been read; the arrival on the next queries tells the product warp)
+      tc_fence_before_sync();
+      mbar_arrive(bar(L::B_OE));
+      if (r < R && !direct && (two || u == 0)) f.part_ml[slot * f.rows_pad + rp] = make_float2(m, l);
+      // rows to be computed again (of a segment in pieces the join looks)
+      const uint32_t bad = __ballot_sync(0xffffffffu, ok && there && direct && !(test == 0.f));
+      if (bad && lane == 0) atomicOr(s_bad + (rp >> 5), bad);
+      if (named_bar_or(2, 256, bad != 0u)) {
+        for (int i = warp; i < 256; i += 8)
+          if (s_bad[i >> 5] >> (i & 31) & 1u) {
+            const int row = row_of_piece(f, w.rb, i), again = quot(row, f.group);
+            tree_row_again<bf16, D, false>(a, b, again, w.g * G + rest(row, again, f.group));
+          }
+        named_bar_sync(2, 256);
+        if (tid < 8) s_bad[tid] = 0u;
+      }
       ++seq;
       at += n;
-      if (named_bar_or(2, 256, !ok)) break;   // (s_o, s_ml and the paths have been read)
+      if (named_bar_or(2, 256, !ok)) break;   // (s_ml and the paths have been read)
     }
   } else if (warp == 8) {
     // ------------------------------------------------------------------------------------------------ copies
     if (elect_one()) {
-      int at = 0;
+      int at = 0, seq = 0;
       bool ok = true;
       while (ok && walk.next(f, w)) {
         const Ring<64> ring = ring_of<64>(w.pos, a.C, a.W);
+        const int qb = seq % q_places;
+        if (seq >= q_places) ok = wait_bar(bar(L::B_QE + qb), (seq / q_places - 1) & 1, s_abort, item_limit(f.limit, w.tiles));
+        if (!ok) break;
+        mbar_arrive_expect_tx(bar(L::B_Q + qb), (uint32_t)(q_tiles * (D / 64) * f.tile_rows * 128));
+        for (int i = 0; i < q_tiles; ++i)
+#pragma unroll
+          for (int s = 0; s < D / 64; ++s)
+            tma_load_4d(sb + (uint32_t)(qb + i) * L::TILE + s * 16384, &tm_q, bar(L::B_Q + qb), s * 64, w.g * G, quot(w.rb * f.rows + i * f.tile_rows, f.group), w.b);
+        ++seq;
         for (int it = w.t0; it < w.t0 + w.n && ok; ++it) {
           const bool fresh = it < f.node_tiles;
           const int s0 = fresh ? it * 64 : cached_tile(ring, it - f.node_tiles, a.C).s0;
@@ -381,11 +370,12 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       auto stage = [&](int at) { return sb + L::OFF_RING + (uint32_t)(at % ST) * L::KT; };
       auto full = [&](int at) { return wait_bar(bar(L::B_FULL + at % ST), (at / ST) & 1, s_abort, f.limit); };
       int tile = 0, seq = 0, fixed = 0, steps[2] = {0, 0};   // tiles, pieces, those with node tiles, and the warpgroups' products so far
+      int qb = 0;
       auto scores = [&](int u, int it, int step, bool first, bool last) {   // first, last: of the warpgroups that meet the tile
         if (first && !full(2 * it)) return false;
         tc_fence_after_sync();
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) mma_f16(s_col(u, step), kdesc<128>(sb + (two ? u : 0) * L::TILE, kk), kdesc<64>(stage(2 * it), kk), id_s, kk != 0);
+        for (int kk = 0; kk < D / 16; ++kk) mma_f16(s_col(u, step), kdesc<128>(sb + (qb + (two ? u : 0)) * L::TILE, kk), kdesc<64>(stage(2 * it), kk), id_s, kk != 0);
         mma_commit(bar(L::B_S + 2 * u + (step & 1)));
         if (last) mma_commit(bar(L::B_EMPTY + 2 * it % ST));
         return true;
@@ -404,17 +394,20 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       while (ok && walk.next(f, w)) {
         const int n = w.n;
         bool fix = w.t0 < f.node_tiles;
-        // (the last piece's outputs may take as long as rows that are computed again do)
-        ok = wait_bar(bar(L::B_Q), seq & 1, s_abort, item_limit(f.limit, w.tiles));
+        qb = seq % q_places;
+        ok = wait_bar(bar(L::B_Q + qb), (seq / q_places) & 1, s_abort, f.limit);
         if (!ok) break;
-        tc_fence_after_sync();
+        // (the last piece's outputs may take as long as rows that are computed again do)
+        auto outputs_read = [&] { return seq == 0 || wait_bar(bar(L::B_OE), (seq - 1) & 1, s_abort, item_limit(f.limit, w.tiles)); };
         if (two) {
           ok = scores(0, tile, steps[0], true, false) && scores(1, tile, steps[0], false, true);
           for (int it = 0; it < n && ok; ++it, ++tile, ++steps[0]) {
 #pragma unroll
             for (int u = 0; u < 2 && ok; ++u) {
               if (it + 1 < n) ok = scores(u, tile + 1, steps[0] + 1, u == 0, u == 1);
-              if (ok && fix) ok = wait_bar(bar(L::B_FIX), fixed++ & 1, s_abort, f.limit);
+              if (ok && it == 0 && u == 0) ok = outputs_read();
+              if (it + 1 == n && u == 1) mma_commit(bar(L::B_QE));   // (the queries' last product)
+              if (ok && fix) ok = wait_bar(bar(L::B_FIX), fixed++ & 1, s_abort, item_limit(f.limit, w.tiles));
               fix = false;
               if (ok) ok = values(u, tile, steps[0], u == 0, u == 1, it == 0);
             }
@@ -424,7 +417,9 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           for (int it = 0; it < n && ok; ++it, ++tile) {
             const int u = it & 1;
             if (it + 2 < n) ok = scores(u, tile + 2, steps[u] + 1, true, true);
-            if (ok && fix) ok = wait_bar(bar(L::B_FIX), fixed++ & 1, s_abort, f.limit);
+            if (it + 1 == n) mma_commit(bar(L::B_QE + qb));   // (the queries' last product)
+            if (ok && it == 0) ok = outputs_read();
+            if (ok && fix) ok = wait_bar(bar(L::B_FIX), fixed++ & 1, s_abort, item_limit(f.limit, w.tiles));
             fix = false;
             if (ok) ok = values(u, tile, steps[u], true, true, it < 2);
             ++steps[u];
@@ -445,22 +440,27 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   if (warp == 9) tmem_dealloc(tmem, 512);
 }
 
-static TreePlan rows_plan(int B, int N, int H, int H_kv, int C, int W) {
-  return tree_plan(B, N, H, H_kv, C, W, N * (H / H_kv) > 128 ? 256 : 128, 64, 1);
+// a tile of rows: as many whole nodes as 128 rows hold; two of them where there are more
+static TreePlan rows_plan(const TreeArgs& a) {
+  const int G = a.H / a.H_kv, tile = 128 / G * G;
+  return tree_plan(a.B, a.N, a.H, a.H_kv, a.C, a.W, a.N * G > tile ? 2 * tile : tile, tile, 128, 64, 1);
 }
 
 template <int D, bool CAP, bool BIAS>
 static int tree_tc(const AttnTree& c) {
   using L = TreeTc<D>;
   const TreeArgs& a = c.a;
-  const TreeTcArgs f = tree_tc_args(c, rows_plan(a.B, a.N, a.H, a.H_kv, a.C, a.W));
-  CUtensorMap tk, tv, tkt, tvt;
-  if (!tensor_map(&tk, a.K, false, a.H_kv, a.C, a.B, D, 64, 64, true) || !tensor_map(&tv, a.V, false, a.H_kv, a.C, a.B, D, 64, 64, true) ||
-      !tensor_map(&tkt, a.k_t, false, a.H_kv, a.N, a.B, D, 64, 64, true) || !tensor_map(&tvt, a.v_t, false, a.H_kv, a.N, a.B, D, 64, 64, true))
+  const TreePlan p = rows_plan(a);
+  if (!p.fits) return LAWCAT_ERR_UNSUPPORTED;
+  const TreeTcArgs f = tree_tc_args(c, p);
+  const int G = a.H / a.H_kv;
+  CUtensorMap tk, tv, tkt, tvt, tq;
+  if (!tensor_map_of(&tk, a.K, a.H_kv, a.C, a.B, D, 1, 64) || !tensor_map_of(&tv, a.V, a.H_kv, a.C, a.B, D, 1, 64) || !tensor_map_of(&tkt, a.k_t, a.H_kv, a.N, a.B, D, 1, 64) ||
+      !tensor_map_of(&tvt, a.v_t, a.H_kv, a.N, a.B, D, 1, 64) || !tensor_map_of(&tq, a.q, a.H, a.N, a.B, D, G, 128 / G))
     return LAWCAT_ERR_CUDA;
   constexpr auto kernel = attn_tree_tc_kernel<D, CAP, BIAS>;
   if (int r = grant_smem<kernel>(L::BYTES)) return r;
-  LAWCAT_LAUNCH("attn_tree_tc", c.stream, launch_behind(kernel, dim3((unsigned)f.shares), dim3(L::THREADS), L::BYTES, c.stream, tk, tv, tkt, tvt, f));
+  LAWCAT_LAUNCH("attn_tree_tc", c.stream, launch_behind(kernel, dim3((unsigned)f.shares), dim3(L::THREADS), L::BYTES, c.stream, tk, tv, tkt, tvt, tq, f));
   LAWCAT_CHECK_LAUNCH();
   return f.whole ? (int)LAWCAT_OK : launch_tree_join<D, false, 64, true>(c, f);
 }
@@ -468,8 +468,7 @@ static int tree_tc(const AttnTree& c) {
 }  // namespace attn
 
 size_t attn_tree_tc_workspace_bytes(const AttnTree& c) {
-  const attn::TreeArgs& a = c.a;
-  return attn::tree_plan_bytes(attn::rows_plan(a.B, a.N, a.H, a.H_kv, a.C, a.W), c.d);
+  return attn::tree_plan_bytes(attn::rows_plan(c.a), c.d);
 }
 
 int launch_attn_tree_tc(const AttnTree& c) {

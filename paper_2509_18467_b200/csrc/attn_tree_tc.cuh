@@ -18,9 +18,9 @@ constexpr float SMALL = 1.f / (1 << 18);   // (the least difference of fp16 numb
 struct TreeTcArgs {
   TreeArgs a;
   FastDiv group;      // H / H_kv
-  int row_blocks;     // blocks of `rows` rows of a group
-  int rows;
-  int rows_pad;       // rows of a piece in scratch
+  int row_blocks;     // blocks of `rows` rows of a group, in tiles of tile_rows
+  int rows, tile_rows;
+  int stride, rows_pad;   // rows of a tile, and of a piece, as they lie in tensor memory and scratch
   int whole;          // shares are whole segments
   int node_tiles;     // key tiles of the nodes' own
   int shares;         // blocks
@@ -71,19 +71,24 @@ template <int TS>
 __device__ __forceinline__ int segment_tiles(const TreeTcArgs& f, int pos) { return f.node_tiles + ring_of<TS>(pos, f.a.C, f.a.W).tiles; }
 __device__ __forceinline__ int segments_of_one(const TreeTcArgs& f) { return f.a.H_kv * f.row_blocks; }
 
-// all tiles, and (at) the sequence that tile x lies in and the tiles in front of it; by a whole warp
+// all tiles of the first `end` sequences; by a whole warp
 template <int TS>
-__device__ __forceinline__ long long tiles_up_to(const TreeTcArgs& f, int end) {
-  long long n = 0;
+__device__ __forceinline__ int tiles_up_to(const TreeTcArgs& f, int end) {
+  int n = 0;
   for (int b = threadIdx.x & 31; b < end; b += 32) n += segment_tiles<TS>(f, f.a.pos[b]);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-  return n * segments_of_one(f);
+  return __reduce_add_sync(0xffffffffu, n) * segments_of_one(f);
 }
-__device__ __forceinline__ int share_count(const TreeTcArgs& f, long long total) {
-  return (int)min((long long)f.shares, max(1LL, total / f.least));
-}
-__device__ __forceinline__ long long share_begin(long long total, int count, int c) { return total * min(c, count) / count; }
+// Shares of n tiles: `more` of one + 1 tiles, then those of one.
+struct Shares {
+  int count, one, more;
+  __device__ __forceinline__ Shares(int n, int most, int least) {
+    count = min(most, max(1, n / least));
+    one = n / count;
+    more = n - one * count;
+  }
+  __device__ __forceinline__ int begin(int c) const { return min(c, count) * one + min(c, more); }
+  __device__ __forceinline__ int of(int x) const { return x < more * (one + 1) ? x / (one + 1) : more + (x - more * (one + 1)) / one; }   // (x: one of the n)
+};
 
 struct Piece {
   int b, segment, g, rb, pos;   // segment: of the sequence
@@ -93,48 +98,43 @@ struct Piece {
 // A block's walk over its share.
 template <int TS>
 struct Walk {
-  long long left;   // tiles (whole: segments) left
+  int left;   // tiles (whole: segments) left
   int b, segment, t, tiles, pos;
 
   __device__ __forceinline__ void start(const TreeTcArgs& f, int c) {   // by a whole warp
     const int per = segments_of_one(f), lane = threadIdx.x & 31;
+    b = segment = t = 0;
     if (f.whole) {
-      const long long all = (long long)f.a.B * per, x = share_begin(all, f.shares, c);
-      left = share_begin(all, f.shares, c + 1) - x;
-      b = (int)(x / per);
-      segment = (int)(x % per);
-      t = 0;
+      const Shares s(f.a.B * per, f.shares, 1);
+      const int x = s.begin(c);
+      left = s.begin(c + 1) - x;
+      b = x / per;
+      segment = x - b * per;
     } else {
-      const long long total = tiles_up_to<TS>(f, f.a.B);
-      const int count = share_count(f, total);
-      long long x = share_begin(total, count, c);
-      left = share_begin(total, count, c + 1) - x;
-      b = segment = t = 0;
-      if (left > 0) {
-        for (int b0 = 0;; b0 += 32) {   // (32 sequences at a time: the one that x lies in)
-          const long long mine = b0 + lane < f.a.B ? (long long)segment_tiles<TS>(f, f.a.pos[b0 + lane]) * per : 0;
-          long long upto = mine;
+      const int first = lane < f.a.B ? segment_tiles<TS>(f, f.a.pos[lane]) : 0;   // (of the first 32 sequences)
+      int n = __reduce_add_sync(0xffffffffu, first) * per;
+      if (f.a.B > 32) n = tiles_up_to<TS>(f, f.a.B);
+      const Shares s(n, f.shares, f.least);
+      int x = s.begin(c);
+      left = s.begin(c + 1) - x;
+      for (int b0 = 0; left > 0 && b0 < f.a.B; b0 += 32) {   // (32 sequences at a time: the one that x lies in)
+        const int mine = (b0 == 0 ? first : b0 + lane < f.a.B ? segment_tiles<TS>(f, f.a.pos[b0 + lane]) : 0) * per;
+        int upto = mine;
 #pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += y;
-          }
-          const uint32_t in = __ballot_sync(0xffffffffu, x < upto);
-          if (in) {
-            const int k = __ffs(in) - 1;
-            x -= __shfl_sync(0xffffffffu, upto - mine, k);
-            b = b0 + k;
-            const int one = (int)(__shfl_sync(0xffffffffu, mine, k) / per);
-            segment = (int)(x / one);
-            t = (int)(x % one);
-            break;
-          }
-          x -= __shfl_sync(0xffffffffu, upto, 31);
-          if (b0 + 32 >= f.a.B) {       // (never: x is one of the tiles)
-            left = 0;
-            break;
-          }
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += y;
         }
+        const uint32_t in = __ballot_sync(0xffffffffu, x < upto);
+        if (in) {
+          const int k = __ffs(in) - 1, all = __shfl_sync(0xffffffffu, mine, k), one = all / per;
+          x -= __shfl_sync(0xffffffffu, upto, k) - all;
+          b = b0 + k;
+          segment = x / one;
+          t = x - segment * one;
+          break;
+        }
+        x -= __shfl_sync(0xffffffffu, upto, 31);
       }
     }
     load(f);
@@ -153,7 +153,7 @@ struct Walk {
     p.pos = pos;
     p.t0 = t;
     p.tiles = tiles;
-    p.n = f.whole ? tiles : (int)min((long long)(tiles - t), left);
+    p.n = f.whole ? tiles : min(tiles - t, left);
     left -= f.whole ? 1 : p.n;
     t += p.n;
     if (t == tiles) {
@@ -167,45 +167,69 @@ struct Walk {
     return true;
   }
 };
+// the row of a group (0x7fffffff: none) at place rp of a piece
+__device__ __forceinline__ int row_of_piece(const TreeTcArgs& f, int rb, int rp) {
+  const int tile = rp / f.stride, in = rp - tile * f.stride;
+  return in < f.tile_rows ? rb * f.rows + tile * f.tile_rows + in : 0x7fffffff;
+}
 __device__ __forceinline__ bool is_whole(const Piece& p) { return p.n == p.tiles; }
 __device__ __forceinline__ int piece_slot(const Piece& p, int c) { return 2 * c + (p.t0 == 0); }
 
-// The pieces of a segment's rows, 32 at a time; a thread has eight channels of a row, two pieces' loads in flight. ROWS_INNER: a piece's
-// weighted values are D x rows_pad, else rows_pad x D.
+// The pieces of a segment's rows. A block has 1024 values of a piece, eight to a thread: 32 rows x 32 channels where a piece's weighted values are
+// D x rows_pad (ROWS_INNER), 1024 / D whole rows where they are rows_pad x D; four groups of threads share the pieces out, four pieces' loads
+// in flight, and meet in shared memory.
+template <int D, bool ROWS_INNER>
+struct JoinTile {
+  static constexpr int ROWS = ROWS_INNER ? 32 : 1024 / D, CHANNELS = ROWS_INNER ? 32 : D, SPLIT = D / CHANNELS;   // SPLIT: blocks of the same rows
+};
 template <int D, bool QUANT, int TS, bool ROWS_INNER>
-__global__ void __launch_bounds__(D * 4) attn_tree_join_tc_kernel(const __grid_constant__ TreeTcArgs f) {
+__global__ void __launch_bounds__(512) attn_tree_join_tc_kernel(const __grid_constant__ TreeTcArgs f) {
+  using J = JoinTile<D, ROWS_INNER>;
+  constexpr int GROUPS = 4, U = 4;
   const TreeArgs& a = f.a;
-  const int G = a.H / a.H_kv, chunks = f.rows_pad / 32, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-  const int per = segments_of_one(f), seg = blockIdx.x / chunks, b = seg / per, segment = seg % per, r_first = blockIdx.x % chunks * 32;
+  const int G = a.H / a.H_kv, chunks = f.rows_pad / J::ROWS, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  const int group = threadIdx.x / 128, in = threadIdx.x % 128;
+  const int per = segments_of_one(f), piece = blockIdx.x / J::SPLIT, seg = piece / chunks, b = seg / per, segment = seg % per, r_first = piece % chunks * J::ROWS;
+  const int c_first = blockIdx.x % J::SPLIT * J::CHANNELS;
+  __shared__ float s_acc[GROUPS][8][128];
+  __shared__ float2 s_ml[GROUPS][128];
   __shared__ uint32_t s_bad, s_large;
   if (threadIdx.x == 0) s_bad = s_large = 0u;
   behind_last_kernel();
-  const long long total = tiles_up_to<TS>(f, a.B), x0 = tiles_up_to<TS>(f, b);
-  const int tiles = segment_tiles<TS>(f, a.pos[b]), count = share_count(f, total);
-  const long long s0 = x0 + (long long)segment * tiles, s1 = s0 + tiles - 1;
-  // the shares that its first and its last tile lie in
-  auto share_of = [&](long long x) {
-    int c = (int)min((long long)count - 1, x * count / total);
-    while (c + 1 < count && share_begin(total, count, c + 1) <= x) ++c;
-    while (c > 0 && share_begin(total, count, c) > x) --c;
-    return c;
-  };
-  const int c0 = share_of(s0), c1 = share_of(s1);
+  const int tiles = segment_tiles<TS>(f, a.pos[b]);
+  int n, n0;   // all tiles, and those in front of this segment
+  if (a.B <= 32) {
+    const int mine = lane < a.B ? segment_tiles<TS>(f, a.pos[lane]) : 0;
+    n = __reduce_add_sync(0xffffffffu, mine) * per;
+    n0 = __reduce_add_sync(0xffffffffu, lane < b ? mine : 0) * per;
+  } else {
+    n = tiles_up_to<TS>(f, a.B);
+    n0 = tiles_up_to<TS>(f, b);
+  }
+  const Shares shares(n, f.shares, f.least);
+  const int x0 = n0 + segment * tiles, c0 = shares.of(x0), c1 = shares.of(x0 + tiles - 1);   // the shares that its first and its last tile lie in
   if (c0 == c1) return;                              // (one piece, which its block has stored)
-  const int ri = ROWS_INNER ? lane : threadIdx.x / (D / 8), ch = (ROWS_INNER ? warp : threadIdx.x % (D / 8)) * 8;
-  const int rp = r_first + ri, r = segment % f.row_blocks * f.rows + rp, R = a.N * G;
-  const bool some = rp < f.rows && r < R;
+  const int ri = ROWS_INNER ? lane : in / (D / 8), ch = c_first + (ROWS_INNER ? in / 32 : in % (D / 8)) * 8;
+  const int R = a.N * G, rp = r_first + ri, r = row_of_piece(f, segment % f.row_blocks, rp);
+  const bool some = r < R;
   float m = -INFINITY, l = 0.f, acc[8] = {};
-  if (some) {
-    constexpr int U = 2;
-    for (int i0 = c0; i0 <= c1; i0 += U) {
+  auto add = [&](float pm, float pl, const float (&x)[8]) {   // one more piece (one without keys has no weights)
+    if (pl == 0.f) return;
+    const float top = fmaxf(m, pm), base = top == -INFINITY ? 0.f : top, k = ex2f(m - base), w = ex2f(pm - base);
+    m = top;
+    l = l * k + w * pl;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = fmaf(w, x[e], acc[e] * k);
+  };
+  if (some)
+    for (int i0 = c0 + group; i0 <= c1; i0 += GROUPS * U) {
       float2 ml[U];
       float x[U][8];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int c = min(i0 + u, c1);
+        const int c = min(i0 + u * GROUPS, c1);
         const size_t slot = 2 * (size_t)c + (c == c0);
-        ml[u] = i0 + u <= c1 ? f.part_ml[slot * f.rows_pad + rp] : make_float2(-INFINITY, 0.f);
+        ml[u] = f.part_ml[slot * f.rows_pad + rp];
         if constexpr (ROWS_INNER) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[u][e] = f.part_o[(slot * D + ch + e) * f.rows_pad + rp];
@@ -216,65 +240,68 @@ __global__ void __launch_bounds__(D * 4) attn_tree_join_tc_kernel(const __grid_c
           x[u][4] = z.x; x[u][5] = z.y; x[u][6] = z.z; x[u][7] = z.w;
         }
       }
-      float top = m;
 #pragma unroll
-      for (int u = 0; u < U; ++u) top = fmaxf(top, ml[u].x);
-      const float base = top == -INFINITY ? 0.f : top, k = ex2f(m - base);
-      m = top;
-      l *= k;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] *= k;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const float w = ex2f(ml[u].x - base);
-        if (ml[u].y != 0.f) {                        // (a piece without keys has no weights)
-          l += w * ml[u].y;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) acc[e] = fmaf(w, x[u][e], acc[e]);
-        }
-      }
+      for (int u = 0; u < U; ++u)
+        if (i0 + u * GROUPS <= c1) add(ml[u].x, ml[u].y, x[u]);
     }
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  float test = l * 0.f, largest = 0.f;
+  if (group > 0) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    acc[e] *= inv;
-    test = fmaf(acc[e], 0.f, test);
-    largest = fmaxf(largest, fabsf(acc[e]));
+    for (int e = 0; e < 8; ++e) s_acc[group][e][in] = acc[e];
+    s_ml[group][in] = make_float2(m, l);
   }
-  const int g = segment / f.row_blocks;
-  if (some) {
-    const int node = quot(r, f.group), h = g * G + rest(r, node, f.group);
-    *reinterpret_cast<uint4*>((bf16*)a.o + (((size_t)b * a.N + node) * a.H + h) * D + ch) =
-        make_uint4(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]), pack_bf16(acc[4], acc[5]), pack_bf16(acc[6], acc[7]));
+  __syncthreads();
+  if (group == 0) {
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = s_acc[k][e][in];
+      add(s_ml[k][in].x, s_ml[k][in].y, x);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    float test = l * 0.f, largest = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      acc[e] *= inv;
+      test = fmaf(acc[e], 0.f, test);
+      largest = fmaxf(largest, fabsf(acc[e]));
+    }
+    if (some) {
+      const int node = quot(r, f.group), h = segment / f.row_blocks * G + rest(r, node, f.group);
+      *reinterpret_cast<uint4*>((bf16*)a.o + (((size_t)b * a.N + node) * a.H + h) * D + ch) =
+          make_uint4(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]), pack_bf16(acc[4], acc[5]), pack_bf16(acc[6], acc[7]));
+      if (!(test == 0.f)) atomicOr(&s_bad, 1u << ri);
+    }
+    if (QUANT && (!some || l == 0.f || !(largest < SMALL))) atomicOr(&s_large, 1u << ri);
   }
-  __syncthreads();   // (the flags are zero)
-  if (some && !(test == 0.f)) atomicOr(&s_bad, 1u << ri);
-  if (QUANT && (!some || l == 0.f || !(largest < SMALL))) atomicOr(&s_large, 1u << ri);
   __syncthreads();
   const uint32_t again = s_bad | (QUANT ? ~s_large : 0u);
-  for (int i = warp; i < 32; i += D / 8)             // (behind the barrier: nobody else writes these rows any more)
+  if (!again) return;
+  for (int i = warp; i < J::ROWS; i += 16)           // (behind the barrier: nobody else writes these channels any more)
     if (again >> i & 1u) {
-      const int row = segment % f.row_blocks * f.rows + r_first + i, node = quot(row, f.group);
-      tree_row_again<bf16, D, QUANT>(a, b, node, g * G + rest(row, node, f.group));
+      const int row = row_of_piece(f, segment % f.row_blocks, r_first + i), node = quot(row, f.group);
+      tree_row_again<bf16, D, QUANT>(a, b, node, segment / f.row_blocks * G + rest(row, node, f.group), c_first, J::CHANNELS);
     }
 }
 
-// how a call's work is shared out; `resident`: blocks that run at once on an SM
+// How a call's work is shared out. rows: of a block, in tiles of tile_rows, which lie `stride` apart; resident: blocks that run at once on an SM.
 struct TreePlan {
-  int rows, row_blocks, rows_pad, whole, node_tiles, shares, least;
+  int rows, tile_rows, stride, row_blocks, rows_pad, whole, node_tiles, shares, least;
+  bool fits;
 };
-inline TreePlan tree_plan(int B, int N, int H, int H_kv, int C, int W, int rows, int TS, int resident) {
+inline TreePlan tree_plan(int B, int N, int H, int H_kv, int C, int W, int rows, int tile_rows, int stride, int TS, int resident) {
   TreePlan p;
-  const int R = N * (H / H_kv);
+  const int R = N * (H / H_kv), places = rows / tile_rows * stride;
   p.rows = rows;
+  p.tile_rows = tile_rows;
+  p.stride = stride;
   p.row_blocks = (R + rows - 1) / rows;
-  p.rows_pad = ((R < rows ? R : rows) + 31) / 32 * 32;
+  p.rows_pad = rows == tile_rows && R < rows ? (R + 31) / 32 * 32 : (places + 31) / 32 * 32;
   p.node_tiles = (N + TS - 1) / TS;
   const int keys = W < C ? W : C;
   const int most = p.node_tiles + (keys - 1 + TS - 1) / TS + 1;       // tiles of a segment (one more where the ring wraps)
   const long long segments = (long long)B * H_kv * p.row_blocks, run = (long long)resident * sm_count();
+  p.fits = segments * most <= 0x7fffffffLL;
   p.least = TS == 64 ? 4 : 2;                                          // 256 keys
   p.whole = most <= 8 * 64 / TS;
   const long long all = p.whole ? segments : (segments * most + p.least - 1) / p.least;
@@ -289,7 +316,7 @@ inline TreeTcArgs tree_tc_args(const AttnTree& c, const TreePlan& p) {
   TreeTcArgs f{};
   f.a = c.a;
   f.group = fast_div(c.a.H / c.a.H_kv);
-  f.row_blocks = p.row_blocks; f.rows = p.rows; f.rows_pad = p.rows_pad; f.whole = p.whole; f.node_tiles = p.node_tiles;
+  f.row_blocks = p.row_blocks; f.rows = p.rows; f.tile_rows = p.tile_rows; f.stride = p.stride; f.rows_pad = p.rows_pad; f.whole = p.whole; f.node_tiles = p.node_tiles;
   f.shares = p.shares; f.least = p.least;
   f.part_ml = (float2*)c.ws;
   f.part_o = (float*)((char*)c.ws + align_up(sizeof(float2) * 2 * (size_t)p.shares * p.rows_pad, 256));
@@ -299,10 +326,11 @@ inline TreeTcArgs tree_tc_args(const AttnTree& c, const TreePlan& p) {
 }
 template <int D, bool QUANT, int TS, bool ROWS_INNER>
 int launch_tree_join(const AttnTree& c, const TreeTcArgs& f) {
-  const long long blocks = (long long)f.a.B * f.a.H_kv * f.row_blocks * (f.rows_pad / 32);
+  using J = JoinTile<D, ROWS_INNER>;
+  const long long blocks = (long long)f.a.B * f.a.H_kv * f.row_blocks * (f.rows_pad / J::ROWS) * J::SPLIT;
   if (blocks > 0x7fffffffLL) return LAWCAT_ERR_UNSUPPORTED;
   LAWCAT_LAUNCH("attn_tree_join_tc", c.stream,
-                launch_behind(attn_tree_join_tc_kernel<D, QUANT, TS, ROWS_INNER>, dim3((unsigned)blocks), dim3(D * 4), 0, c.stream, f));
+                launch_behind(attn_tree_join_tc_kernel<D, QUANT, TS, ROWS_INNER>, dim3((unsigned)blocks), dim3(512), 0, c.stream, f));
   LAWCAT_CHECK_LAUNCH();
   return LAWCAT_OK;
 }

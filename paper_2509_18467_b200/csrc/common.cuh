@@ -83,6 +83,8 @@ int validate_params(const lawcat_params* p, bool need_T);
 // [B, T, heads, dh] tensor (fp32 or bf16) as a 4-D map (channel, head, token, batch) with boxes of box_ch channels x rows tokens;
 // kept per host thread for the last few pointers and shapes (layer_tc.cu)
 bool tensor_map(CUtensorMap* m, const void* ptr, bool f32, int heads, int T, int B, int dh, int box_ch, int rows, bool swizzle);
+// [B, T, heads, dh] bf16 tensor in 128-byte-swizzled boxes of 64 channels x box_heads heads x rows tokens, encoded anew
+bool tensor_map_of(CUtensorMap* m, const void* ptr, int heads, int T, int B, int dh, int box_heads, int rows);
 
 // Chunkwise tensor-core layer forward (layer_tc.cu): whether it takes these parameters, and its launcher.
 bool layer_tc_supported(const lawcat_params& p);

@@ -67,6 +67,18 @@ bool tensor_map(CUtensorMap* m, const void* ptr, bool f32, int heads, int T, int
   return true;
 }
 
+bool tensor_map_of(CUtensorMap* m, const void* ptr, int heads, int T, int B, int dh, int box_heads, int rows) {
+  tc::EncodeTiledFn fn = tc::encode_fn();
+  if (!fn) return false;
+  const cuuint64_t row = (cuuint64_t)dh * 2;
+  const cuuint64_t dims[4] = {(cuuint64_t)dh, (cuuint64_t)heads, (cuuint64_t)T, (cuuint64_t)B};
+  const cuuint64_t strides[3] = {row, heads * row, T * (heads * row)};
+  const cuuint32_t box[4] = {64, (cuuint32_t)box_heads, (cuuint32_t)rows, 1};
+  const cuuint32_t es[4] = {1, 1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 namespace tc {
 
 // [B, T, heads, dh] bf16 tensor in boxes of 64 channels x rows tokens, 128-byte-swizzled
