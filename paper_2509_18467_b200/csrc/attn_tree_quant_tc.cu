@@ -7,11 +7,6 @@
 // relative to a reference per row that moves only when a score exceeds it by more than 2^8: one vote of the block per tile, and a maximum
 // is looked for only then. Sums stay with the slots' threads until the segment's end.
 //
-// All operands are fp16: a code becomes 1024 + code by an OR into the mantissa, less 1024, times scale, plus minimum (both times 16), one
-// rounding of 2^-11; queries are scaled by a power of two per row. Values beyond 4094 leave fp16's range, and outputs below 2^-18 feel the
-// smallest numbers that it holds: such rows, like all that come out not finite, are computed again on the CUDA cores. Channels of eight are
-// held in the order 0 4 1 5 2 6 3 7, in which a word of codes unpacks two at a time.
-//
 // The keys are walked from the newest to the oldest: the nodes' own first, quantized as the cache would hold them, then the cached ones.
 // Slots that no row sees, and nodes that are not there, are zeros, whatever they hold.
 //
@@ -24,23 +19,6 @@ namespace lawcat {
 namespace attn {
 
 constexpr float COL_RESCALE = 8.f, NO_REFERENCE = -1e30f;   // (below every score: the first one that is seen moves it)
-
-__device__ __forceinline__ __half2 as_half2(uint32_t w) { return *reinterpret_cast<const __half2*>(&w); }
-__device__ __forceinline__ uint32_t as_word(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
-struct GroupScale {
-  __half2 s1, s16, low;   // scale, scale / 16, minimum
-};
-__device__ __forceinline__ GroupScale group_scale(uint32_t pair) {   // (scale, minimum) in bf16
-  const float s = bf16_lo(pair) * KV_FACTOR, l = bf16_hi(pair) * KV_FACTOR;
-  return GroupScale{__floats2half2_rn(s, s), __floats2half2_rn(s * 0.0625f, s * 0.0625f), __floats2half2_rn(l, l)};
-}
-// a word of eight codes -> eight values in the order above
-__device__ __forceinline__ uint4 unpack8(uint32_t w, const GroupScale& g) {
-  const __half2 k = as_half2(0x64006400u);   // 1024
-  const uint32_t hi = w >> 8;
-  auto val = [&](uint32_t bits, __half2 s) { return as_word(__hfma2(__hsub2(as_half2(bits | 0x64006400u), k), s, g.low)); };
-  return make_uint4(val(w & 0x000F000Fu, g.s1), val(w & 0x00F000F0u, g.s16), val(hi & 0x000F000Fu, g.s1), val(hi & 0x00F000F0u, g.s16));
-}
 
 template <int D, int NCOL>
 struct ColLay {
@@ -184,17 +162,9 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
 #pragma unroll
     for (int i = 0; i < QV; ++i) {
       const int at = tid + 128 * i, c = at / (D / 8), j = at % (D / 8);
-      float x[8] = {bf16_lo(q[i].x), bf16_hi(q[i].x), bf16_lo(q[i].y), bf16_hi(q[i].y), bf16_lo(q[i].z), bf16_hi(q[i].z), bf16_lo(q[i].w), bf16_hi(q[i].w)};
-      uint32_t top = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-#pragma unroll
-      for (int o = 1; o < D / 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));   // (a row's threads lie side by side)
-      const uint32_t e2 = min(max(top >> 23, 1u), 253u);   // largest value in [1, 2)
-      const float down = __uint_as_float((254u - e2) << 23), up = (CAP ? 1.f : a.scale * LOG2E) * (__uint_as_float(e2 << 23) / KV_FACTOR);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] *= down;
-      sts128(sb + L::OFF_Q + (uint32_t)(j >> 3) * (NCOL * 128) + sw128(c, j & 7), make_uint4(pack_f16(x[0], x[4]), pack_f16(x[1], x[5]), pack_f16(x[2], x[6]), pack_f16(x[3], x[7])));
+      uint4 h;
+      const float up = (CAP ? 1.f : a.scale * LOG2E) * (scale_query<D>(q[i], h) / KV_FACTOR);
+      sts128(sb + L::OFF_Q + (uint32_t)(j >> 3) * (NCOL * 128) + sw128(c, j & 7), h);
       if (j == 0) s_ref[c / 2 * 4 + (c & 1)] = s_raw[c / 2 * 4 + (c & 1)] = up;
     }
     fence_proxy_async();
@@ -471,10 +441,6 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
   if (warp == 0) tmem_dealloc(tmem, L::COLS);
 }
 
-static int columns(int N, int H, int H_kv) {
-  const int R = N * (H / H_kv);
-  return R <= 16 ? 16 : R <= 32 ? 32 : 64;
-}
 template <int NCOL>
 static TreePlan cols_plan(const AttnTree& c) {
   const TreeArgs& a = c.a;
@@ -496,17 +462,24 @@ static int tree_quant_tc(const AttnTree& c) {
 
 }  // namespace attn
 
+// Columns for the rows of a group: 16 or 32; more go to the rows' kernel (0).
+static int columns(const AttnTree& c) {
+  const int R = c.a.N * (c.a.H / c.a.H_kv);
+  return R <= 16 ? 16 : R <= 32 ? 32 : 0;
+}
+
 size_t attn_tree_quant_tc_workspace_bytes(const AttnTree& c) {
-  const int n = attn::columns(c.a.N, c.a.H, c.a.H_kv);
-  return attn::tree_plan_bytes(n == 16 ? attn::cols_plan<16>(c) : n == 32 ? attn::cols_plan<32>(c) : attn::cols_plan<64>(c), c.d);
+  const int n = columns(c);
+  return n == 0 ? attn_tree_tc_workspace_bytes(c) : attn::tree_plan_bytes(n == 16 ? attn::cols_plan<16>(c) : attn::cols_plan<32>(c), c.d);
 }
 
 int launch_attn_tree_quant_tc(const AttnTree& c) {
-  const int n = attn::columns(c.a.N, c.a.H, c.a.H_kv);
+  const int n = columns(c);
+  if (n == 0) return launch_attn_tree_tc(c);
   auto by = [&](auto cap, auto bias) {
     constexpr bool CAP = decltype(cap)::value, BIAS = decltype(bias)::value;
-    if (c.d == 128) return n == 16 ? attn::tree_quant_tc<128, 16, CAP, BIAS>(c) : n == 32 ? attn::tree_quant_tc<128, 32, CAP, BIAS>(c) : attn::tree_quant_tc<128, 64, CAP, BIAS>(c);
-    return n == 16 ? attn::tree_quant_tc<64, 16, CAP, BIAS>(c) : n == 32 ? attn::tree_quant_tc<64, 32, CAP, BIAS>(c) : attn::tree_quant_tc<64, 64, CAP, BIAS>(c);
+    if (c.d == 128) return n == 16 ? attn::tree_quant_tc<128, 16, CAP, BIAS>(c) : attn::tree_quant_tc<128, 32, CAP, BIAS>(c);
+    return n == 16 ? attn::tree_quant_tc<64, 16, CAP, BIAS>(c) : attn::tree_quant_tc<64, 32, CAP, BIAS>(c);
   };
   const std::true_type yes{};
   const std::false_type no{};

@@ -1,9 +1,12 @@
-// Attention of drafted tokens over a cache in the storage type on the tensor cores: bf16, d = 64 or 128.
+// Attention of drafted tokens over a cache on the tensor cores: bf16, d = 64 or 128; the cache in the storage type, or in 4 bits where there are
+// more rows than attn_tree_quant_tc.cu has columns.
 //
 // A block walks segments of up to 256 rows (node, query head) of one (sequence, key-value head) and their keys, in tiles of 64:
 //   two warpgroups    softmax, one thread per row: S from tensor memory, masks, running maximum and sum in registers, P = exp2(x - m) over S;
 //                     then the segment's outputs
-//   copy warp         queries, K and V tiles (through a ring of stages) by TMA, on into the next segment while this one ends
+//   copy warp         queries, K and V tiles (through a ring of stages) by TMA, on into the next segment while this one ends;
+//                     over 4 bits seven warps in its place, which unpack codes into the stages (a warp at a time 32 groups of 32 channels, eight
+//                     of them on their way), and the queries come by the softmax warps
 //   product warp      S = Q K^T (shared memory), O += P V (P from tensor memory); fp32 accumulation
 // A tile of rows is as many whole nodes as 128 rows hold. Of two tiles each warpgroup has one, and both meet every key; of one, both have its
 // rows and take the key tiles in turn, each with sums of its own (in the same lanes of tensor memory) that meet at the segment's end. S has two places per warpgroup; O is rescaled only when a maximum grew by
@@ -23,23 +26,24 @@ namespace attn {
 
 constexpr float TREE_RESCALE = 8.f;
 
-template <int D>
+template <int D, bool QUANT>
 struct TreeTc {
   static constexpr uint32_t TILE = 128 * D * 2, KT = 64 * D * 2;   // rows' queries; keys or values of a tile
   static constexpr int ST = D == 64 ? 16 : 8;                      // stages, K and V tiles in turn
   static constexpr uint32_t OFF_RING = 2 * TILE, OFF_PATHS = OFF_RING + ST * KT, OFF_DEPTH = OFF_PATHS + sizeof(Paths), OFF_ML = OFF_DEPTH + TREE_MAX * 4;
-  static constexpr uint32_t OFF_BAD = OFF_ML + 256 * 8, OFF_BAR = OFF_BAD + 64, BYTES = OFF_BAR + 512;
-  static constexpr int THREADS = 320;
+  static constexpr uint32_t OFF_BAD = OFF_ML + 256 * 8, OFF_SCALE = OFF_BAD + 64, OFF_BAR = OFF_SCALE + 256 * 4, BYTES = OFF_BAR + 512;
+  static constexpr int LOADERS = QUANT ? 7 : 1, THREADS = 288 + 32 * LOADERS, FMT = QUANT ? FMT_F16 : FMT_BF16;
+  static constexpr int ITEMS = D / 16;   // a stage's parts over 4 bits: 32 groups of 32 channels
   static constexpr int B_FULL = 0, B_EMPTY = ST, B_S = 2 * ST, B_P = B_S + 4, B_O = B_P + 4, B_DONE = B_O + 4, B_Q = B_DONE + 1, B_QE = B_Q + 2, B_OE = B_QE + 2, B_FIX = B_OE + 1, NBAR = B_FIX + 1;
   static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 512 && 256 + 2 * D <= 512 && TREE_MAX / 64 * 2 <= ST, "shared memory, tensor memory");
 };
 
 // BIAS also serves a scale that is not positive: the scores are scaled before anything else looks at them
-template <int D, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(TreeTc<D>::THREADS, 1)
+template <int D, bool QUANT, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(TreeTc<D, QUANT>::THREADS, 1)
 attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_kt,
                     const __grid_constant__ CUtensorMap tm_vt, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ TreeTcArgs f) {
-  using L = TreeTc<D>;
+  using L = TreeTc<D, QUANT>;
   constexpr int ST = L::ST;
   extern __shared__ __align__(1024) uint8_t smem[];
   const TreeArgs& a = f.a;
@@ -49,13 +53,14 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   volatile int* const s_abort = s_flags + 1;
   auto bar = [&](int i) { return sb + L::OFF_BAR + 8 * (uint32_t)i; };
   uint32_t* const s_bad = reinterpret_cast<uint32_t*>(smem + L::OFF_BAD);   // [8] rows to be computed again
+  uint32_t* const s_large = s_bad + 8;                                       // [8] over 4 bits: rows that are not small everywhere
   const int G = a.H / a.H_kv, R = a.N * G;
   const bool two = f.rows > f.tile_rows;
-  const int q_tiles = two ? 2 : 1, q_places = two ? 1 : 2;   // of a segment, and segments whose queries fit
+  const int q_tiles = two ? 2 : 1, q_places = two || QUANT ? 1 : 2;   // of a segment, and segments whose queries fit
 
   if (tid == 0) {
     for (int i = 0; i < ST; ++i) {
-      mbar_init(bar(L::B_FULL + i), 1);
+      mbar_init(bar(L::B_FULL + i), QUANT ? L::ITEMS : 1);
       mbar_init(bar(L::B_EMPTY + i), 1);
     }
     for (int i = 0; i < 4; ++i) {
@@ -65,19 +70,21 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     }
     mbar_init(bar(L::B_DONE), 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar(L::B_Q + i), 1);
+      mbar_init(bar(L::B_Q + i), QUANT ? 256 : 1);
       mbar_init(bar(L::B_QE + i), 1);
     }
     mbar_init(bar(L::B_OE), 256);
     mbar_init(bar(L::B_FIX), 256);
     s_flags[1] = 0;
-    for (int i = 0; i < 8; ++i) s_bad[i] = 0u;
+    for (int i = 0; i < 16; ++i) s_bad[i] = 0u;
     mbar_fence_init();
-    tma_prefetch_desc(&tm_q);
-    tma_prefetch_desc(&tm_k);
-    tma_prefetch_desc(&tm_v);
-    tma_prefetch_desc(&tm_kt);
-    tma_prefetch_desc(&tm_vt);
+    if constexpr (!QUANT) {
+      tma_prefetch_desc(&tm_q);
+      tma_prefetch_desc(&tm_k);
+      tma_prefetch_desc(&tm_v);
+      tma_prefetch_desc(&tm_kt);
+      tma_prefetch_desc(&tm_vt);
+    }
   }
   behind_last_kernel();
   if (warp == 9) {
@@ -103,6 +110,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     float2* const s_ml = reinterpret_cast<float2*>(smem + L::OFF_ML);   // [2][128]
     const int u = warp >> 2, r128 = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, O = o_col(u) + lanes;
+    float* const s_scale = reinterpret_cast<float*>(smem + L::OFF_SCALE);   // over 4 bits: what a row's queries were divided by
     int step = 0, seq = 0, at = 0, b_last = -1;   // steps, pieces and tiles so far
     bool ok = true;
     while (walk.next(f, w)) {
@@ -112,6 +120,20 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         if (tid < a.N) s_depth[tid] = pos < 0 ? -1 : node_depth(paths, tid, a.N);
         named_bar_sync(1, 256);
         b_last = b;
+      }
+      if constexpr (QUANT) {   // (all products with the last piece's are done; queries of rows that are not there may be anything)
+#pragma unroll 4
+        for (int i = tid; i < q_tiles * 128 * (D / 8); i += 256) {
+          const int p = i / (D / 8), j = i % (D / 8), row = min(row_of_piece(f, w.rb, p), R - 1), nd = quot(row, f.group);
+          const uint4 x = *reinterpret_cast<const uint4*>((const bf16*)a.q + (((size_t)b * a.N + nd) * a.H + w.g * G + rest(row, nd, f.group)) * D + j * 8);
+          uint4 y;
+          const float up = scale_query<D>(x, y);
+          sts128(sb + (uint32_t)(p >> 7) * L::TILE + (uint32_t)(j >> 3) * 16384 + sw128(p & 127, j & 7), y);
+          if (j == 0) s_scale[p] = up / KV_FACTOR;
+        }
+        fence_proxy_async();
+        mbar_arrive(bar(L::B_Q));
+        named_bar_sync(2, 256);   // (s_scale)
       }
       // the values of nodes that are not there: zeros (their weights are, and whatever they hold must not meet those)
       for (int it = 0; it < node_tiles; ++it) {
@@ -133,7 +155,8 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       const int node = quot(min(r, R - 1), f.group), h = w.g * G + rest(min(r, R - 1), node, f.group);
       const int depth = s_depth[node];
       const bool there = r < R && depth >= 0;
-      const float scale2 = a.scale * LOG2E, slope2 = BIAS && a.slopes ? a.slopes[h] * LOG2E : 0.f;
+      const float unit = QUANT ? s_scale[rp] : 1.f;   // of a product in tensor memory
+      const float scale2 = a.scale * LOG2E * unit, slope2 = BIAS && a.slopes ? a.slopes[h] * LOG2E : 0.f;
       const Ring<64> ring = ring_of<64>(pos, a.C, a.W);
       // the farthest key that the row sees, and the least of the warp's (of rows that are not there nothing is stored but zeros)
       const int far = there ? min(a.W - 1 - depth, pos) : 0x3fffffff;
@@ -155,7 +178,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 #pragma unroll
         for (int c = 0; c < 64; c += 32) tmem_ld32(S + c, s + c);
         tmem_wait_ld();
-        if constexpr (CAP) cap_scores(s, a.scale / a.cap, a.cap * LOG2E);
+        if constexpr (CAP) cap_scores(s, a.scale * unit / a.cap, a.cap * LOG2E);
         float by = CAP ? 1.f : scale2;
         if (it < f.node_tiles) {
           // the nodes' own: those of the path, by their distance
@@ -246,7 +269,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           for (int e = 0; e < 8; ++e) {
             float x, y;
             f2_unpack(z[e], x, y);
-            s[q + e] = __uint_as_float(pack_bf16(x, y));
+            s[q + e] = __uint_as_float(QUANT ? pack_f16(x, y) : pack_bf16(x, y));
           }
         }
         tmem_st32(S, s);
@@ -274,10 +297,10 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         m = top;
       }
       if (!there) l = 0.f;
-      const float inv = !direct ? 1.f : l == 0.f ? 0.f : 1.f / l;
+      const float inv = (!direct ? 1.f : l == 0.f ? 0.f : 1.f / l) * (QUANT ? 1.f / KV_FACTOR : 1.f);
       f0 *= inv;
       f1 *= inv;
-      float test = l * 0.f;
+      float test = l * 0.f, largest = 0.f;
       const size_t slot = piece_slot(w, (int)blockIdx.x);
       bf16* const dst = (bf16*)a.o + (((size_t)b * a.N + node) * a.H + h) * D;
       float* const pdst = f.part_o + slot * D * f.rows_pad + rp;
@@ -300,7 +323,21 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           for (int e = 0; e < 32; ++e) o[e] *= f0;
         }
 #pragma unroll
-        for (int e = 0; e < 32; ++e) test = fmaf(o[e], 0.f, test);
+        for (int e = 0; e < 32; ++e) {
+          test = fmaf(o[e], 0.f, test);
+          if constexpr (QUANT) largest = fmaxf(largest, fabsf(o[e]));
+        }
+        if constexpr (QUANT) {   // channels of eight back into their order
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            const float x[8] = {o[e], o[e + 1], o[e + 2], o[e + 3], o[e + 4], o[e + 5], o[e + 6], o[e + 7]};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              o[e + k] = x[2 * k];
+              o[e + 4 + k] = x[2 * k + 1];
+            }
+          }
+        }
         if (r < R) {
           if (!direct) {
 #pragma unroll
@@ -318,23 +355,90 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       if (r < R && !direct && (two || u == 0)) f.part_ml[slot * f.rows_pad + rp] = make_float2(m, l);
       // rows to be computed again (of a segment in pieces the join looks)
       const uint32_t bad = __ballot_sync(0xffffffffu, ok && there && direct && !(test == 0.f));
-      if (bad && lane == 0) atomicOr(s_bad + (rp >> 5), bad);
-      if (named_bar_or(2, 256, bad != 0u)) {
-        for (int i = warp; i < 256; i += 8)
-          if (s_bad[i >> 5] >> (i & 31) & 1u) {
+      const uint32_t large = QUANT ? __ballot_sync(0xffffffffu, !(ok && there && direct) || l == 0.f || !(largest < SMALL)) : 0xffffffffu;
+      if (lane == 0) {
+        if (bad) atomicOr(s_bad + (rp >> 5), bad);
+        if (QUANT && large) atomicOr(s_large + (rp >> 5), large);
+      }
+      if (named_bar_or(2, 256, bad != 0u || large != 0xffffffffu)) {
+        for (int i = warp; i < q_tiles * 128; i += 8)
+          if ((s_bad[i >> 5] | (QUANT ? ~s_large[i >> 5] : 0u)) >> (i & 31) & 1u) {
             const int row = row_of_piece(f, w.rb, i), again = quot(row, f.group);
-            tree_row_again<bf16, D, false>(a, b, again, w.g * G + rest(row, again, f.group));
+            tree_row_again<bf16, D, QUANT>(a, b, again, w.g * G + rest(row, again, f.group));
           }
-        named_bar_sync(2, 256);
-        if (tid < 8) s_bad[tid] = 0u;
       }
       ++seq;
       at += n;
-      if (named_bar_or(2, 256, !ok)) break;   // (s_ml and the paths have been read)
+      if (named_bar_or(2, 256, !ok)) break;   // (s_ml, the paths and the flags have been read)
+      if (tid < 16) s_bad[tid] = 0u;          // (written again behind other barriers)
     }
-  } else if (warp == 8) {
+  } else if (warp != 9) {
     // ------------------------------------------------------------------------------------------------ copies
-    if (elect_one()) {
+    if constexpr (QUANT) {
+      // Parts of stages (a tile's keys, then its values), taken by the warps in turn: 32 / (D / 32) slots, all groups of each. Zeros where no row
+      // may see a slot.
+      constexpr int NG = D / 32, SLOTS = 32 / NG, DEEP = 8;
+      const int me = warp == 8 ? 0 : warp - 9, slot = lane / NG, grp = lane % NG;
+      int tile = 0;
+      bool ok = true;
+      while (ok && walk.next(f, w)) {
+        const Ring<64> ring = ring_of<64>(w.pos, a.C, a.W);
+        const size_t head = ((size_t)w.b * a.H_kv + w.g) * a.C;
+        const int fresh = max(0, min(f.node_tiles - w.t0, w.n)), all = w.n * 2 * L::ITEMS;
+        struct Codes {
+          uint4 q;
+          uint32_t p;
+        } buf[DEEP];
+        auto fetch = [&](int x, Codes& y) {   // part x of the piece
+          const int it = x / (2 * L::ITEMS), v = x / L::ITEMS % 2, c = x % L::ITEMS * SLOTS + slot;
+          y = Codes{make_uint4(0u, 0u, 0u, 0u), 0u};
+          if (x >= all || it < fresh) return;
+          const CachedTile t = cached_tile(ring, w.t0 + it - f.node_tiles, a.C);
+          if (c < t.lo || t.s0 + c < 0 || t.back0 - c > ring.cached) return;
+          const size_t row = head + (t.s0 + c);
+          y.q = __ldcs(reinterpret_cast<const uint4*>((v ? a.vq : a.kq) + row * (D / 2)) + grp);
+          y.p = __ldcs(reinterpret_cast<const uint32_t*>((v ? a.vp : a.kp) + row * (D / 16)) + grp);
+        };
+#pragma unroll
+        for (int e = 0; e < DEEP; ++e) fetch(me + e * L::LOADERS, buf[e]);
+#pragma unroll 1
+        for (int x0 = me; x0 < all && ok; x0 += DEEP * L::LOADERS) {
+#pragma unroll
+          for (int e = 0; e < DEEP; ++e) {
+            const int x = x0 + e * L::LOADERS;
+            if (x >= all || !ok) break;
+            const int it = x / (2 * L::ITEMS), v = x / L::ITEMS % 2, at = 2 * (tile + it) + v, s = at % ST;
+            if (at >= ST) ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_EMPTY + s), (at / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles)));
+            if (!ok) break;
+            const uint32_t st = sb + L::OFF_RING + (uint32_t)s * L::KT;
+            const int c0 = x % L::ITEMS * SLOTS;
+            if (it < fresh) {   // nodes, as the cache would hold them
+#pragma unroll 1
+              for (int y = lane; y < SLOTS * (D / 8); y += 32) {
+                const int r = c0 + y / (D / 8), j = y % (D / 8), k = (w.t0 + it) * 64 + r;
+                float h[8];
+                load8((const bf16*)(v ? a.v_t : a.k_t) + (((size_t)w.b * a.N + min(k, a.N - 1)) * a.H_kv + w.g) * D + j * 8, h);
+                quantize8<D, true>(h, j * 8, nullptr, nullptr, false, 0xffffffffu);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[i] = k < a.N ? h[i] * KV_FACTOR : 0.f;
+                sts128(st + (uint32_t)(j >> 3) * 8192 + sw128(r, j & 7), halves_in_order(h));
+              }
+            } else {
+              const GroupScale gs = group_scale(buf[e].p);
+              const bool turn = grp >= 2;   // (the second 64 channels: in another order, so that eight threads' stores take different banks)
+              const uint32_t word[4] = {turn ? buf[e].q.z : buf[e].q.x, turn ? buf[e].q.w : buf[e].q.y, turn ? buf[e].q.x : buf[e].q.z, turn ? buf[e].q.y : buf[e].q.w};
+#pragma unroll
+              for (int i = 0; i < 4; ++i) sts128(st + (uint32_t)(grp >> 1) * 8192 + sw128(c0 + slot, (grp & 1) * 4 + (turn ? i ^ 2 : i)), unpack8(word[i], gs));
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(L::B_FULL + s));
+            fetch(x + DEEP * L::LOADERS, buf[e]);
+          }
+        }
+        tile += w.n;
+      }
+    } else if (elect_one()) {
       int at = 0, seq = 0;
       bool ok = true;
       while (ok && walk.next(f, w)) {
@@ -365,8 +469,8 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   } else {
     // ------------------------------------------------------------------------------------------------ products
     if (elect_one()) {
-      constexpr uint32_t id_s = instr_desc(128, 64, FMT_BF16, MAJOR_K, MAJOR_K);
-      constexpr uint32_t id_o = instr_desc(128, D, FMT_BF16, MAJOR_K, MAJOR_MN);
+      constexpr uint32_t id_s = instr_desc(128, 64, L::FMT, MAJOR_K, MAJOR_K);
+      constexpr uint32_t id_o = instr_desc(128, D, L::FMT, MAJOR_K, MAJOR_MN);
       auto stage = [&](int at) { return sb + L::OFF_RING + (uint32_t)(at % ST) * L::KT; };
       auto full = [&](int at) { return wait_bar(bar(L::B_FULL + at % ST), (at / ST) & 1, s_abort, f.limit); };
       int tile = 0, seq = 0, fixed = 0, steps[2] = {0, 0};   // tiles, pieces, those with node tiles, and the warpgroups' products so far
@@ -446,23 +550,24 @@ static TreePlan rows_plan(const TreeArgs& a) {
   return tree_plan(a.B, a.N, a.H, a.H_kv, a.C, a.W, a.N * G > tile ? 2 * tile : tile, tile, 128, 64, 1);
 }
 
-template <int D, bool CAP, bool BIAS>
+template <int D, bool QUANT, bool CAP, bool BIAS>
 static int tree_tc(const AttnTree& c) {
-  using L = TreeTc<D>;
+  using L = TreeTc<D, QUANT>;
   const TreeArgs& a = c.a;
   const TreePlan p = rows_plan(a);
   if (!p.fits) return LAWCAT_ERR_UNSUPPORTED;
   const TreeTcArgs f = tree_tc_args(c, p);
   const int G = a.H / a.H_kv;
-  CUtensorMap tk, tv, tkt, tvt, tq;
-  if (!tensor_map_of(&tk, a.K, a.H_kv, a.C, a.B, D, 1, 64) || !tensor_map_of(&tv, a.V, a.H_kv, a.C, a.B, D, 1, 64) || !tensor_map_of(&tkt, a.k_t, a.H_kv, a.N, a.B, D, 1, 64) ||
-      !tensor_map_of(&tvt, a.v_t, a.H_kv, a.N, a.B, D, 1, 64) || !tensor_map_of(&tq, a.q, a.H, a.N, a.B, D, G, 128 / G))
+  CUtensorMap tk{}, tv{}, tkt{}, tvt{}, tq{};
+  if (!QUANT &&
+      (!tensor_map_of(&tk, a.K, a.H_kv, a.C, a.B, D, 1, 64) || !tensor_map_of(&tv, a.V, a.H_kv, a.C, a.B, D, 1, 64) || !tensor_map_of(&tkt, a.k_t, a.H_kv, a.N, a.B, D, 1, 64) ||
+      !tensor_map_of(&tvt, a.v_t, a.H_kv, a.N, a.B, D, 1, 64) || !tensor_map_of(&tq, a.q, a.H, a.N, a.B, D, G, 128 / G)))
     return LAWCAT_ERR_CUDA;
-  constexpr auto kernel = attn_tree_tc_kernel<D, CAP, BIAS>;
+  constexpr auto kernel = attn_tree_tc_kernel<D, QUANT, CAP, BIAS>;
   if (int r = grant_smem<kernel>(L::BYTES)) return r;
   LAWCAT_LAUNCH("attn_tree_tc", c.stream, launch_behind(kernel, dim3((unsigned)f.shares), dim3(L::THREADS), L::BYTES, c.stream, tk, tv, tkt, tvt, tq, f));
   LAWCAT_CHECK_LAUNCH();
-  return f.whole ? (int)LAWCAT_OK : launch_tree_join<D, false, 64, true>(c, f);
+  return f.whole ? (int)LAWCAT_OK : launch_tree_join<D, QUANT, 64, true>(c, f);
 }
 
 }  // namespace attn
@@ -474,7 +579,8 @@ size_t attn_tree_tc_workspace_bytes(const AttnTree& c) {
 int launch_attn_tree_tc(const AttnTree& c) {
   auto by = [&](auto cap, auto bias) {
     constexpr bool CAP = decltype(cap)::value, BIAS = decltype(bias)::value;
-    return c.d == 128 ? attn::tree_tc<128, CAP, BIAS>(c) : attn::tree_tc<64, CAP, BIAS>(c);
+    if (c.a.kq) return c.d == 128 ? attn::tree_tc<128, true, CAP, BIAS>(c) : attn::tree_tc<64, true, CAP, BIAS>(c);
+    return c.d == 128 ? attn::tree_tc<128, false, CAP, BIAS>(c) : attn::tree_tc<64, false, CAP, BIAS>(c);
   };
   const std::true_type yes{};
   const std::false_type no{};

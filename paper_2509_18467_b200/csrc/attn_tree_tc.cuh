@@ -11,9 +11,51 @@
 namespace lawcat {
 namespace attn {
 
-// Over 4 bits all operands are fp16, keys and values times 16 (see attn_tree_quant_tc.cu)
+// Over 4 bits all operands are fp16: a code becomes 1024 + code by an OR into the mantissa, less 1024, times scale, plus minimum (both times
+// 16), one rounding of 2^-11; queries are scaled by a power of two per row. Values beyond 4094 leave fp16's range, and outputs below 2^-18 feel
+// the smallest numbers that it holds: such rows, like all that come out not finite, are computed again on the CUDA cores. Channels of eight
+// are held in the order 0 4 1 5 2 6 3 7, in which a word of codes unpacks two at a time.
 constexpr float KV_FACTOR = 16.f;
 constexpr float SMALL = 1.f / (1 << 18);   // (the least difference of fp16 numbers, 2^-24 / 16, is 2^-10 of it)
+
+// eight channels as halves in that order
+__device__ __forceinline__ uint4 halves_in_order(const float (&x)[8]) {
+  return make_uint4(pack_f16(x[0], x[4]), pack_f16(x[1], x[5]), pack_f16(x[2], x[6]), pack_f16(x[3], x[7]));
+}
+// Eight channels of a query row, whose D / 8 threads lie side by side in a warp, scaled so that the row's largest value lies in [1, 2);
+// returns what that took.
+template <int D>
+__device__ __forceinline__ float scale_query(const uint4& q, uint4& halves) {
+  float x[8] = {bf16_lo(q.x), bf16_hi(q.x), bf16_lo(q.y), bf16_hi(q.y), bf16_lo(q.z), bf16_hi(q.z), bf16_lo(q.w), bf16_hi(q.w)};
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 1; o < D / 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const uint32_t e2 = min(max(top >> 23, 1u), 253u);
+  const float down = __uint_as_float((254u - e2) << 23);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] *= down;
+  halves = halves_in_order(x);
+  return __uint_as_float(e2 << 23);
+}
+
+__device__ __forceinline__ __half2 as_half2(uint32_t w) { return *reinterpret_cast<const __half2*>(&w); }
+__device__ __forceinline__ uint32_t as_word(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
+struct GroupScale {
+  __half2 s1, s16, low;   // scale, scale / 16, minimum
+};
+__device__ __forceinline__ GroupScale group_scale(uint32_t pair) {   // (scale, minimum) in bf16
+  const float s = bf16_lo(pair) * KV_FACTOR, l = bf16_hi(pair) * KV_FACTOR;
+  return GroupScale{__floats2half2_rn(s, s), __floats2half2_rn(s * 0.0625f, s * 0.0625f), __floats2half2_rn(l, l)};
+}
+// a word of eight codes -> eight values in the order above
+__device__ __forceinline__ uint4 unpack8(uint32_t w, const GroupScale& g) {
+  const __half2 k = as_half2(0x64006400u);   // 1024
+  const uint32_t hi = w >> 8;
+  auto val = [&](uint32_t bits, __half2 s) { return as_word(__hfma2(__hsub2(as_half2(bits | 0x64006400u), k), s, g.low)); };
+  return make_uint4(val(w & 0x000F000Fu, g.s1), val(w & 0x00F000F0u, g.s16), val(hi & 0x000F000Fu, g.s1), val(hi & 0x00F000F0u, g.s16));
+}
 
 struct TreeTcArgs {
   TreeArgs a;
@@ -175,24 +217,25 @@ __device__ __forceinline__ int row_of_piece(const TreeTcArgs& f, int rb, int rp)
 __device__ __forceinline__ bool is_whole(const Piece& p) { return p.n == p.tiles; }
 __device__ __forceinline__ int piece_slot(const Piece& p, int c) { return 2 * c + (p.t0 == 0); }
 
-// The pieces of a segment's rows. A block has 1024 values of a piece, eight to a thread: 32 rows x 32 channels where a piece's weighted values are
-// D x rows_pad (ROWS_INNER), 1024 / D whole rows where they are rows_pad x D; four groups of threads share the pieces out, four pieces' loads
-// in flight, and meet in shared memory.
-template <int D, bool ROWS_INNER>
+// The pieces of a segment's rows, eight channels to a thread. Of few pieces a block has 32 rows; of many it has 1024 values, 32 rows x 32 channels
+// where a piece's weighted values are D x rows_pad (ROWS_INNER), 1024 / D whole rows where they are rows_pad x D, and four groups of threads
+// share the pieces out, four pieces' loads in flight, and meet in shared memory.
+template <int D, bool ROWS_INNER, int GROUPS>
 struct JoinTile {
-  static constexpr int ROWS = ROWS_INNER ? 32 : 1024 / D, CHANNELS = ROWS_INNER ? 32 : D, SPLIT = D / CHANNELS;   // SPLIT: blocks of the same rows
+  static constexpr int ROWS = ROWS_INNER || GROUPS == 1 ? 32 : 1024 / D, CHANNELS = ROWS_INNER && GROUPS > 1 ? 32 : D, SPLIT = D / CHANNELS;   // SPLIT: blocks of the same rows
+  static constexpr int PER = ROWS * CHANNELS / 8, THREADS = GROUPS * PER;   // threads of a group
 };
-template <int D, bool QUANT, int TS, bool ROWS_INNER>
-__global__ void __launch_bounds__(512) attn_tree_join_tc_kernel(const __grid_constant__ TreeTcArgs f) {
-  using J = JoinTile<D, ROWS_INNER>;
-  constexpr int GROUPS = 4, U = 4;
+template <int D, bool QUANT, int TS, bool ROWS_INNER, int GROUPS>
+__global__ void __launch_bounds__(JoinTile<D, ROWS_INNER, GROUPS>::THREADS) attn_tree_join_tc_kernel(const __grid_constant__ TreeTcArgs f) {
+  using J = JoinTile<D, ROWS_INNER, GROUPS>;
+  constexpr int U = GROUPS == 1 ? 2 : 4;
   const TreeArgs& a = f.a;
   const int G = a.H / a.H_kv, chunks = f.rows_pad / J::ROWS, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-  const int group = threadIdx.x / 128, in = threadIdx.x % 128;
+  const int group = threadIdx.x / J::PER, in = threadIdx.x % J::PER;
   const int per = segments_of_one(f), piece = blockIdx.x / J::SPLIT, seg = piece / chunks, b = seg / per, segment = seg % per, r_first = piece % chunks * J::ROWS;
   const int c_first = blockIdx.x % J::SPLIT * J::CHANNELS;
-  __shared__ float s_acc[GROUPS][8][128];
-  __shared__ float2 s_ml[GROUPS][128];
+  __shared__ float s_acc[GROUPS - 1 ? GROUPS : 1][GROUPS - 1 ? 8 : 1][GROUPS - 1 ? J::PER : 1];
+  __shared__ float2 s_ml[GROUPS - 1 ? GROUPS : 1][GROUPS - 1 ? J::PER : 1];
   __shared__ uint32_t s_bad, s_large;
   if (threadIdx.x == 0) s_bad = s_large = 0u;
   behind_last_kernel();
@@ -244,10 +287,12 @@ __global__ void __launch_bounds__(512) attn_tree_join_tc_kernel(const __grid_con
       for (int u = 0; u < U; ++u)
         if (i0 + u * GROUPS <= c1) add(ml[u].x, ml[u].y, x[u]);
     }
-  if (group > 0) {
+  if constexpr (GROUPS > 1) {
+    if (group > 0) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s_acc[group][e][in] = acc[e];
-    s_ml[group][in] = make_float2(m, l);
+      for (int e = 0; e < 8; ++e) s_acc[group][e][in] = acc[e];
+      s_ml[group][in] = make_float2(m, l);
+    }
   }
   __syncthreads();
   if (group == 0) {
@@ -277,7 +322,7 @@ __global__ void __launch_bounds__(512) attn_tree_join_tc_kernel(const __grid_con
   __syncthreads();
   const uint32_t again = s_bad | (QUANT ? ~s_large : 0u);
   if (!again) return;
-  for (int i = warp; i < J::ROWS; i += 16)           // (behind the barrier: nobody else writes these channels any more)
+  for (int i = warp; i < J::ROWS; i += J::THREADS / 32)           // (behind the barrier: nobody else writes these channels any more)
     if (again >> i & 1u) {
       const int row = row_of_piece(f, segment % f.row_blocks, r_first + i), node = quot(row, f.group);
       tree_row_again<bf16, D, QUANT>(a, b, node, segment / f.row_blocks * G + rest(row, node, f.group), c_first, J::CHANNELS);
@@ -324,15 +369,20 @@ inline TreeTcArgs tree_tc_args(const AttnTree& c, const TreePlan& p) {
   f.dev_status = c.dev_status;
   return f;
 }
-template <int D, bool QUANT, int TS, bool ROWS_INNER>
+template <int D, bool QUANT, int TS, bool ROWS_INNER, int GROUPS>
 int launch_tree_join(const AttnTree& c, const TreeTcArgs& f) {
-  using J = JoinTile<D, ROWS_INNER>;
+  using J = JoinTile<D, ROWS_INNER, GROUPS>;
   const long long blocks = (long long)f.a.B * f.a.H_kv * f.row_blocks * (f.rows_pad / J::ROWS) * J::SPLIT;
   if (blocks > 0x7fffffffLL) return LAWCAT_ERR_UNSUPPORTED;
   LAWCAT_LAUNCH("attn_tree_join_tc", c.stream,
-                launch_behind(attn_tree_join_tc_kernel<D, QUANT, TS, ROWS_INNER>, dim3((unsigned)blocks), dim3(512), 0, c.stream, f));
+                launch_behind(attn_tree_join_tc_kernel<D, QUANT, TS, ROWS_INNER, GROUPS>, dim3((unsigned)blocks), dim3(J::THREADS), 0, c.stream, f));
   LAWCAT_CHECK_LAUNCH();
   return LAWCAT_OK;
+}
+template <int D, bool QUANT, int TS, bool ROWS_INNER>
+int launch_tree_join(const AttnTree& c, const TreeTcArgs& f) {   // (more than four shares to a segment are many pieces)
+  if (f.shares > 4LL * f.a.B * f.a.H_kv * f.row_blocks) return launch_tree_join<D, QUANT, TS, ROWS_INNER, 4>(c, f);
+  return launch_tree_join<D, QUANT, TS, ROWS_INNER, 1>(c, f);
 }
 
 }  // namespace attn
