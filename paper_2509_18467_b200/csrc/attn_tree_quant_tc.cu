@@ -27,7 +27,7 @@ struct ColLay {
   static constexpr uint32_t OFF_ON = OFF_COL + 8 * NCOL * 4, OFF_RED = OFF_ON + NCOL * (TREE_MAX / 32) * 4, OFF_BAR = OFF_RED + 6 * NCOL * 4, BYTES = OFF_BAR + 64;
   static constexpr uint32_t OFF_CODES = 0, OFF_PAIRS = 128 * WPR * 4, STAGED = OFF_PAIRS + 128 * NG * 4;   // a node tile's keys as the cache would hold them, then its values
   static constexpr uint32_t K_COLS = D / 2, COLS = K_COLS + 2 * NCOL <= 128 ? 128 : 256;
-  static constexpr int RESIDENT = COLS == 128 ? 4 : 2;
+  static constexpr int RESIDENT = COLS != 128 ? 2 : NCOL == 32 ? 3 : 4;
   static_assert(K_COLS + 2 * NCOL <= COLS && OFF_P % 1024 == 0 && OFF_BAR % 16 == 0 && sizeof(Paths) <= OFF_Q && 2 * STAGED <= OFF_Q && RESIDENT * (BYTES + 1024) <= 233472, "layout");
 };
 
@@ -107,21 +107,30 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
     const Ring<128> ring = ring_of<128>(pos, a.C, a.W);
     const size_t head = ((size_t)b * a.H_kv + w.g) * a.C;
     // this thread's slot of a tile: codes and (scale, minimum) pairs; zeros where no row may see it
+    const uint8_t *const kq = a.kq + head * (D / 2), *const vq = a.vq + head * (D / 2);
+    const bf16 *const kpr = a.kp + head * (2 * NG), *const vpr = a.vp + head * (2 * NG);
     uint32_t kc[WPR], vc[WPR], kp[NG], vp[NG];
-    auto fetch = [&](int it, const uint8_t* q, const bf16* p, uint32_t (&codes)[WPR], uint32_t (&pairs)[NG]) {
-      const CachedTile t = cached_tile(ring, it - f.node_tiles, a.C);
-      if (tid >= t.lo && t.s0 + tid >= 0 && t.back0 - tid <= ring.cached) {
-        const size_t row = head + (t.s0 + tid);
+    CachedTile ahead{0, 0, 0};      // the tile whose codes are on their way
+    auto look = [&](int it) { ahead = cached_tile(ring, it - f.node_tiles, a.C); };
+    auto to_l2 = [&](int it) {      // codes of keys and values, their pairs: a warp each
+      if (it >= w.t0 + n || it < f.node_tiles || lane != 0) return;
+      tile_to_l2<128>(cached_tile(ring, it - f.node_tiles, a.C), warp == 0 ? kq : warp == 1 ? vq : (const uint8_t*)(warp == 2 ? kpr : vpr), warp < 2 ? D / 2 : 4 * NG);
+    };
+    auto fetch = [&](const uint8_t* q, const bf16* p, uint32_t (&codes)[WPR], uint32_t (&pairs)[NG]) {
+      const int slot = ahead.s0 + tid;
+      if (tid >= ahead.lo && slot >= 0 && ahead.back0 - tid <= ring.cached) {
+        const uint4* const from = reinterpret_cast<const uint4*>(q + (size_t)(uint32_t)slot * (D / 2));
 #pragma unroll
         for (int i = 0; i < WPR / 4; ++i) {
-          const uint4 x = __ldcs(reinterpret_cast<const uint4*>(q + row * (D / 2)) + i);
+          const uint4 x = __ldcs(from + i);
           codes[4 * i] = x.x; codes[4 * i + 1] = x.y; codes[4 * i + 2] = x.z; codes[4 * i + 3] = x.w;
         }
+        const bf16* const pair = p + (size_t)(uint32_t)slot * (2 * NG);
         if constexpr (NG == 4) {
-          const uint4 x = __ldcs(reinterpret_cast<const uint4*>(p + row * (2 * NG)));
+          const uint4 x = __ldcs(reinterpret_cast<const uint4*>(pair));
           pairs[0] = x.x; pairs[1] = x.y; pairs[2] = x.z; pairs[3] = x.w;
         } else {
-          const uint2 x = __ldcs(reinterpret_cast<const uint2*>(p + row * (2 * NG)));
+          const uint2 x = __ldcs(reinterpret_cast<const uint2*>(pair));
           pairs[0] = x.x; pairs[1] = x.y;
         }
       } else {
@@ -140,7 +149,12 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
       const int at = tid + 128 * i, r = min(r0 + at / (D / 8), R - 1), node = quot(r, f.group);
       q[i] = *reinterpret_cast<const uint4*>((const bf16*)a.q + (((size_t)b * a.N + node) * a.H + w.g * G + rest(r, node, f.group)) * D + at % (D / 8) * 8);
     }
-    if (w.t0 >= f.node_tiles) fetch(w.t0, a.kq, a.kp, kc, kp);
+    if (w.t0 >= f.node_tiles) {
+      look(w.t0);
+      fetch(kq, kpr, kc, kp);
+    }
+    to_l2(w.t0);
+    to_l2(w.t0 + 1);
     find_paths<128>(a, b, paths, tid, 1);
     int my_depth[TREE_MAX / 128];   // of this thread's nodes
 #pragma unroll
@@ -213,8 +227,11 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
           vp[e] = there ? *reinterpret_cast<const uint32_t*>(smem + (pt - sb) + L::STAGED + 4 * e) : 0u;
         }
       } else {
-        fetch(it, a.vq, a.vp, vc, vp);
+        fetch(vq, vpr, vc, vp);
       }
+      to_l2(it + 2);
+      const CachedTile t = ahead;
+      const bool more = i + 1 < n && it + 1 >= f.node_tiles;
 #pragma unroll
       for (int s = 0; s < D / 64; ++s) {
         float x[32];
@@ -236,7 +253,10 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
         mma_commit(bar_s);
       }
       __syncwarp();
-      if (i + 1 < n && it + 1 >= f.node_tiles) fetch(it + 1, a.kq, a.kp, kc, kp);
+      if (more) {
+        look(it + 1);
+        fetch(kq, kpr, kc, kp);
+      }
       if (!v_free && !fail) fail = !wait_bar(bar_o, (count - 1) & 1, s_abort, f.limit);
       __syncwarp();
 #pragma unroll
@@ -245,8 +265,6 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
       __syncwarp();
       tc_fence_after_sync();
 
-      CachedTile t{0, 0, 0};
-      if (!fresh) t = cached_tile(ring, it - f.node_tiles, a.C);
       const int back = t.back0 - tid, mine = it == 0 ? my_depth[0] : my_depth[1];
       const bool whole = !fresh && t.back0 <= far_all && t.lo == 0;   // every row sees every slot
       const float dist = fresh ? -(float)mine : (float)back;          // (to a row of depth zero)
@@ -291,10 +309,11 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
         if (table == s_ref) {
           float mx0 = z[0], mx1 = z[1];
 #pragma unroll
-          for (int c = 2; c < NCOL; c += 2) {
-            mx0 = fmaxf(mx0, z[c]);
-            mx1 = fmaxf(mx1, z[c + 1]);
+          for (int c = 2; c + 3 < NCOL; c += 4) {
+            mx0 = fmaxf(fmaxf(mx0, z[c]), z[c + 1]);
+            mx1 = fmaxf(fmaxf(mx1, z[c + 2]), z[c + 3]);
           }
+          mx0 = fmaxf(fmaxf(mx0, z[NCOL - 2]), z[NCOL - 1]);
           if (!named_bar_or(3, 128, fmaxf(mx0, mx1) > COL_RESCALE || fail)) break;
           if (named_bar_or(3, 128, fail)) break;
           table = s_raw;
@@ -462,15 +481,15 @@ static int tree_quant_tc(const AttnTree& c) {
 
 }  // namespace attn
 
-// Columns for the rows of a group: 16 or 32; more go to the rows' kernel (0).
+// Columns for the rows of a group: 16, 32 or 64; more go to the rows' kernel (0).
 static int columns(const AttnTree& c) {
   const int R = c.a.N * (c.a.H / c.a.H_kv);
-  return R <= 16 ? 16 : R <= 32 ? 32 : 0;
+  return R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : 0;
 }
 
 size_t attn_tree_quant_tc_workspace_bytes(const AttnTree& c) {
   const int n = columns(c);
-  return n == 0 ? attn_tree_tc_workspace_bytes(c) : attn::tree_plan_bytes(n == 16 ? attn::cols_plan<16>(c) : attn::cols_plan<32>(c), c.d);
+  return n == 0 ? attn_tree_tc_workspace_bytes(c) : attn::tree_plan_bytes(n == 16 ? attn::cols_plan<16>(c) : n == 32 ? attn::cols_plan<32>(c) : attn::cols_plan<64>(c), c.d);
 }
 
 int launch_attn_tree_quant_tc(const AttnTree& c) {
@@ -478,8 +497,8 @@ int launch_attn_tree_quant_tc(const AttnTree& c) {
   if (n == 0) return launch_attn_tree_tc(c);
   auto by = [&](auto cap, auto bias) {
     constexpr bool CAP = decltype(cap)::value, BIAS = decltype(bias)::value;
-    if (c.d == 128) return n == 16 ? attn::tree_quant_tc<128, 16, CAP, BIAS>(c) : attn::tree_quant_tc<128, 32, CAP, BIAS>(c);
-    return n == 16 ? attn::tree_quant_tc<64, 16, CAP, BIAS>(c) : attn::tree_quant_tc<64, 32, CAP, BIAS>(c);
+    if (c.d == 128) return n == 16 ? attn::tree_quant_tc<128, 16, CAP, BIAS>(c) : n == 32 ? attn::tree_quant_tc<128, 32, CAP, BIAS>(c) : attn::tree_quant_tc<128, 64, CAP, BIAS>(c);
+    return n == 16 ? attn::tree_quant_tc<64, 16, CAP, BIAS>(c) : n == 32 ? attn::tree_quant_tc<64, 32, CAP, BIAS>(c) : attn::tree_quant_tc<64, 64, CAP, BIAS>(c);
   };
   const std::true_type yes{};
   const std::false_type no{};

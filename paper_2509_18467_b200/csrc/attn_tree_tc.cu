@@ -5,8 +5,7 @@
 //   two warpgroups    softmax, one thread per row: S from tensor memory, masks, running maximum and sum in registers, P = exp2(x - m) over S;
 //                     then the segment's outputs
 //   copy warp         queries, K and V tiles (through a ring of stages) by TMA, on into the next segment while this one ends;
-//                     over 4 bits seven warps in its place, which unpack codes into the stages (a warp at a time 32 groups of 32 channels, eight
-//                     of them on their way), and the queries come by the softmax warps
+//                     over 4 bits seven warps in its place, which unpack codes into the stages (a warp at a time 32 groups of 32 channels), and the queries come by the softmax warps
 //   product warp      S = Q K^T (shared memory), O += P V (P from tensor memory); fp32 accumulation
 // A tile of rows is as many whole nodes as 128 rows hold. Of two tiles each warpgroup has one, and both meet every key; of one, both have its
 // rows and take the key tiles in turn, each with sums of its own (in the same lanes of tensor memory) that meet at the segment's end. S has two places per warpgroup; O is rescaled only when a maximum grew by
@@ -33,7 +32,7 @@ struct TreeTc {
   static constexpr uint32_t OFF_RING = 2 * TILE, OFF_PATHS = OFF_RING + ST * KT, OFF_DEPTH = OFF_PATHS + sizeof(Paths), OFF_ML = OFF_DEPTH + TREE_MAX * 4;
   static constexpr uint32_t OFF_BAD = OFF_ML + 256 * 8, OFF_SCALE = OFF_BAD + 64, OFF_BAR = OFF_SCALE + 256 * 4, BYTES = OFF_BAR + 512;
   static constexpr int LOADERS = QUANT ? 7 : 1, THREADS = 288 + 32 * LOADERS, FMT = QUANT ? FMT_F16 : FMT_BF16;
-  static constexpr int ITEMS = D / 16;   // a stage's parts over 4 bits: 32 groups of 32 channels
+  static constexpr int ITEMS = D / 32;   // a tile's parts over 4 bits: 2 x 32 groups of 32 channels of keys and of values
   static constexpr int B_FULL = 0, B_EMPTY = ST, B_S = 2 * ST, B_P = B_S + 4, B_O = B_P + 4, B_DONE = B_O + 4, B_Q = B_DONE + 1, B_QE = B_Q + 2, B_OE = B_QE + 2, B_FIX = B_OE + 1, NBAR = B_FIX + 1;
   static_assert(BYTES <= 232448 && NBAR * 8 + 16 <= 512 && 256 + 2 * D <= 512 && TREE_MAX / 64 * 2 <= ST, "shared memory, tensor memory");
 };
@@ -375,65 +374,85 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   } else if (warp != 9) {
     // ------------------------------------------------------------------------------------------------ copies
     if constexpr (QUANT) {
-      // Parts of stages (a tile's keys, then its values), taken by the warps in turn: 32 / (D / 32) slots, all groups of each. Zeros where no row
-      // may see a slot.
-      constexpr int NG = D / 32, SLOTS = 32 / NG, DEEP = 8;
+      // Parts of tiles, taken by the warps in turn: the keys and the values of 2 x 32 / (D / 32) slots, so that one fence (some 700 cycles of a
+      // warp's time) does for four stores of 32 groups. Zeros where no row may see a slot.
+      constexpr int NG = D / 32, SLOTS = 32 / NG, AHEAD = 6;   // AHEAD: tiles towards L2
       const int me = warp == 8 ? 0 : warp - 9, slot = lane / NG, grp = lane % NG;
       int tile = 0;
       bool ok = true;
       while (ok && walk.next(f, w)) {
         const Ring<64> ring = ring_of<64>(w.pos, a.C, a.W);
         const size_t head = ((size_t)w.b * a.H_kv + w.g) * a.C;
-        const int fresh = max(0, min(f.node_tiles - w.t0, w.n)), all = w.n * 2 * L::ITEMS;
-        struct Codes {
-          uint4 q;
-          uint32_t p;
-        } buf[DEEP];
-        auto fetch = [&](int x, Codes& y) {   // part x of the piece
-          const int it = x / (2 * L::ITEMS), v = x / L::ITEMS % 2, c = x % L::ITEMS * SLOTS + slot;
-          y = Codes{make_uint4(0u, 0u, 0u, 0u), 0u};
+        const int fresh = max(0, min(f.node_tiles - w.t0, w.n)), all = w.n * L::ITEMS;
+        uint4 q[4];       // keys of the first and second slots, then values
+        uint32_t pr[4];
+        auto fetch = [&](int x) {   // part x of the piece
+          const int it = (uint32_t)x / L::ITEMS;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            q[e] = make_uint4(0u, 0u, 0u, 0u);
+            pr[e] = 0u;
+          }
           if (x >= all || it < fresh) return;
           const CachedTile t = cached_tile(ring, w.t0 + it - f.node_tiles, a.C);
-          if (c < t.lo || t.s0 + c < 0 || t.back0 - c > ring.cached) return;
-          const size_t row = head + (t.s0 + c);
-          y.q = __ldcs(reinterpret_cast<const uint4*>((v ? a.vq : a.kq) + row * (D / 2)) + grp);
-          y.p = __ldcs(reinterpret_cast<const uint32_t*>((v ? a.vp : a.kp) + row * (D / 16)) + grp);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int c = ((uint32_t)x % L::ITEMS * 2 + e) * SLOTS + slot;
+            if (c < t.lo || t.s0 + c < 0 || t.back0 - c > ring.cached) continue;
+            const size_t row = head + (uint32_t)(t.s0 + c);
+            q[e] = __ldcs(reinterpret_cast<const uint4*>(a.kq + row * (D / 2)) + grp);
+            q[2 + e] = __ldcs(reinterpret_cast<const uint4*>(a.vq + row * (D / 2)) + grp);
+            pr[e] = __ldcs(reinterpret_cast<const uint32_t*>(a.kp + row * (D / 16)) + grp);
+            pr[2 + e] = __ldcs(reinterpret_cast<const uint32_t*>(a.vp + row * (D / 16)) + grp);
+          }
         };
-#pragma unroll
-        for (int e = 0; e < DEEP; ++e) fetch(me + e * L::LOADERS, buf[e]);
+        auto to_l2 = [&](int it) {   // codes of keys and values, their pairs: a warp each
+          if (me >= 4 || lane != 0 || it < fresh || it >= w.n) return;
+          tile_to_l2<64>(cached_tile(ring, w.t0 + it - f.node_tiles, a.C),
+                         me < 2 ? (me ? a.vq : a.kq) + head * (D / 2) : (const uint8_t*)((me == 2 ? a.kp : a.vp) + head * (D / 16)), me < 2 ? D / 2 : D / 8);
+        };
+        for (int it = 0; it < AHEAD; ++it) to_l2(it);
+        int seen = -1;   // (the last tile that to_l2 has gone ahead of)
+        fetch(me);
 #pragma unroll 1
-        for (int x0 = me; x0 < all && ok; x0 += DEEP * L::LOADERS) {
-#pragma unroll
-          for (int e = 0; e < DEEP; ++e) {
-            const int x = x0 + e * L::LOADERS;
-            if (x >= all || !ok) break;
-            const int it = x / (2 * L::ITEMS), v = x / L::ITEMS % 2, at = 2 * (tile + it) + v, s = at % ST;
-            if (at >= ST) ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_EMPTY + s), (at / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles)));
-            if (!ok) break;
-            const uint32_t st = sb + L::OFF_RING + (uint32_t)s * L::KT;
-            const int c0 = x % L::ITEMS * SLOTS;
-            if (it < fresh) {   // nodes, as the cache would hold them
+        for (int x = me; x < all; x += L::LOADERS) {
+          const int it = (uint32_t)x / L::ITEMS, p = (uint32_t)x % L::ITEMS, at = 2 * (tile + it), s = (uint32_t)at % ST;
+          if (at >= ST)
+            ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_EMPTY + s), ((uint32_t)at / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles)) &&
+                                             wait_bar(bar(L::B_EMPTY + s + 1), ((uint32_t)at / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles)));
+          if (!ok) break;
+          while (seen < it) to_l2(++seen + AHEAD);
+          const uint32_t st = sb + L::OFF_RING + (uint32_t)s * L::KT;
+          if (it < fresh) {   // nodes, as the cache would hold them
 #pragma unroll 1
-              for (int y = lane; y < SLOTS * (D / 8); y += 32) {
-                const int r = c0 + y / (D / 8), j = y % (D / 8), k = (w.t0 + it) * 64 + r;
-                float h[8];
-                load8((const bf16*)(v ? a.v_t : a.k_t) + (((size_t)w.b * a.N + min(k, a.N - 1)) * a.H_kv + w.g) * D + j * 8, h);
-                quantize8<D, true>(h, j * 8, nullptr, nullptr, false, 0xffffffffu);
+            for (int y = lane; y < 2 * 2 * SLOTS * (D / 8); y += 32) {
+              const bool v = y >= 2 * SLOTS * (D / 8);
+              const int z = y % (2 * SLOTS * (D / 8)), r = p * 2 * SLOTS + z / (D / 8), j = z % (D / 8), k = (w.t0 + it) * 64 + r;
+              float h[8];
+              load8((const bf16*)(v ? a.v_t : a.k_t) + (((size_t)w.b * a.N + min(k, a.N - 1)) * a.H_kv + w.g) * D + j * 8, h);
+              quantize8<D, true>(h, j * 8, nullptr, nullptr, false, 0xffffffffu);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) h[i] = k < a.N ? h[i] * KV_FACTOR : 0.f;
-                sts128(st + (uint32_t)(j >> 3) * 8192 + sw128(r, j & 7), halves_in_order(h));
-              }
-            } else {
-              const GroupScale gs = group_scale(buf[e].p);
-              const bool turn = grp >= 2;   // (the second 64 channels: in another order, so that eight threads' stores take different banks)
-              const uint32_t word[4] = {turn ? buf[e].q.z : buf[e].q.x, turn ? buf[e].q.w : buf[e].q.y, turn ? buf[e].q.x : buf[e].q.z, turn ? buf[e].q.y : buf[e].q.w};
-#pragma unroll
-              for (int i = 0; i < 4; ++i) sts128(st + (uint32_t)(grp >> 1) * 8192 + sw128(c0 + slot, (grp & 1) * 4 + (turn ? i ^ 2 : i)), unpack8(word[i], gs));
+              for (int i = 0; i < 8; ++i) h[i] = k < a.N ? h[i] * KV_FACTOR : 0.f;
+              sts128(st + (v ? L::KT : 0u) + (uint32_t)(j >> 3) * 8192 + sw128(r, j & 7), halves_in_order(h));
             }
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(L::B_FULL + s));
-            fetch(x + DEEP * L::LOADERS, buf[e]);
+          } else {
+            const bool turn = grp >= 2;   // (the second 64 channels: in another order, so that eight threads' stores take different banks)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const GroupScale gs = group_scale(pr[e]);
+              const uint32_t word[4] = {turn ? q[e].z : q[e].x, turn ? q[e].w : q[e].y, turn ? q[e].x : q[e].z, turn ? q[e].y : q[e].w};
+              const int r = (p * 2 + (e & 1)) * SLOTS + slot;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                sts128(st + (e >> 1) * L::KT + (uint32_t)(grp >> 1) * 8192 + sw128(r, (grp & 1) * 4 + (turn ? i ^ 2 : i)), unpack8(word[i], gs));
+            }
+          }
+          fetch(x + L::LOADERS);
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(bar(L::B_FULL + s));
+            mbar_arrive(bar(L::B_FULL + s + 1));
           }
         }
         tile += w.n;

@@ -47,14 +47,21 @@ struct GroupScale {
 };
 __device__ __forceinline__ GroupScale group_scale(uint32_t pair) {   // (scale, minimum) in bf16
   const float s = bf16_lo(pair) * KV_FACTOR, l = bf16_hi(pair) * KV_FACTOR;
-  return GroupScale{__floats2half2_rn(s, s), __floats2half2_rn(s * 0.0625f, s * 0.0625f), __floats2half2_rn(l, l)};
+  const __half2 x = __floats2half2_rn(s, s * 0.0625f), y = __floats2half2_rn(l, l);
+  return GroupScale{__low2half2(x), __high2half2(x), y};
+}
+// (w & mask) | with, in one instruction (two constants would be two)
+__device__ __forceinline__ uint32_t mask_or(uint32_t w, uint32_t mask, uint32_t with) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(with));
+  return r;
 }
 // a word of eight codes -> eight values in the order above
 __device__ __forceinline__ uint4 unpack8(uint32_t w, const GroupScale& g) {
-  const __half2 k = as_half2(0x64006400u);   // 1024
-  const uint32_t hi = w >> 8;
-  auto val = [&](uint32_t bits, __half2 s) { return as_word(__hfma2(__hsub2(as_half2(bits | 0x64006400u), k), s, g.low)); };
-  return make_uint4(val(w & 0x000F000Fu, g.s1), val(w & 0x00F000F0u, g.s16), val(hi & 0x000F000Fu, g.s1), val(hi & 0x00F000F0u, g.s16));
+  const uint32_t k = 0x64006400u, hi = w >> 8;   // 1024
+  auto val = [&](uint32_t bits, __half2 s) { return as_word(__hfma2(__hsub2(as_half2(bits), as_half2(k)), s, g.low)); };
+  return make_uint4(val(mask_or(w, 0x000F000Fu, k), g.s1), val(mask_or(w, 0x00F000F0u, k), g.s16), val(mask_or(hi, 0x000F000Fu, k), g.s1),
+                    val(mask_or(hi, 0x00F000F0u, k), g.s16));
 }
 
 struct TreeTcArgs {
@@ -106,6 +113,13 @@ __device__ __forceinline__ CachedTile cached_tile(const Ring<TS>& r, int j, int 
     t.lo = 0;   // (slots below 0 lie C or more behind, which no row sees)
   }
   return t;
+}
+
+// `bytes` of each of a tile's slots towards L2, but for what lies in the same 16 bytes as something else
+template <int TS>
+__device__ __forceinline__ void tile_to_l2(const CachedTile& t, const void* base, uint32_t bytes) {
+  const uint64_t at = (uint64_t)base, lo = (at + (uint64_t)(uint32_t)max(t.s0 + t.lo, 0) * bytes + 15) & ~15ull, hi = (at + (uint64_t)(uint32_t)(t.s0 + TS) * bytes) & ~15ull;
+  if (hi > lo) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(lo), "r"((uint32_t)(hi - lo)) : "memory");
 }
 
 // tiles of one of sequence b's segments
