@@ -6,8 +6,9 @@
 // leading 32 bits go through sincospi, whose argument needs no reduction.
 //
 // Memory-bound: every value is read once and written once. A block takes a few tokens; their cosines and sines are computed once, into
-// shared memory, for all heads. A thread takes V pairs of one head (two loads of 16 bytes where the sizes allow it), four such items at a
-// time with all their loads in flight, the first four ahead of the cosines.
+// shared memory, for all heads. A thread has V pairs of a head (two loads of 16 bytes where the sizes allow it) and takes head after head,
+// four at a time with all their loads in flight, the first four ahead of the cosines. The table's pieces of 16 bytes are stored so that eight
+// threads side by side read them from different banks.
 #include "attn.cuh"
 #include "attn_tc.cuh"
 
@@ -24,8 +25,9 @@ struct RopeArgs {
   long long tokens;   // B T
   int T, H, H_kv, d, half;
   int per_block;      // tokens of a block
-  int chunks, turned; // items of a head, and how many of them are turned
-  attn::FastDiv by_chunks, by_heads, by_T;
+  int chunk_bits;     // a head has 2^chunk_bits pieces of V pairs,
+  int turned;         // `turned` of which are turned
+  attn::FastDiv by_heads, by_T;
   float scale, sign;
   uint64_t turn[MAX_PAIRS];   // 2^64 f / (2 pi)
 };
@@ -52,80 +54,88 @@ __device__ __forceinline__ long long position(const RopeArgs& a, long long token
   return start + depth;
 }
 
+// Where pair f of a token lies in the table (as float2): pieces of two pairs, those of the c-th four of them turned by c / 2 (a thread of eight
+// pairs reads four pieces one after the other, and its neighbours lie four pieces apart).
+__device__ __forceinline__ int table_place(int f) {
+  const int c = f >> 3;
+  return (f & ~7) | ((f + 2 * (c >> 1)) & 7);
+}
+
 // HALF: pairs (i, i + half); else (2 i, 2 i + 1)
 template <typename T, int V, bool HALF>
 __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constant__ RopeArgs a) {
-  extern __shared__ float2 s_cs[];   // [half][per_block] cosine and sine
+  extern __shared__ float2 s_cs[];   // [per_block][half] cosine and sine
   attn::behind_last_kernel();
   const long long t0 = (long long)blockIdx.x * a.per_block;
   const int nt = (int)min((long long)a.per_block, a.tokens - t0), tid = threadIdx.x;
-  const int heads = a.H + a.H_kv, items = nt * heads * a.chunks;
+  const int heads = a.H + a.H_kv, rows = nt * heads;
+  // this thread's piece of a head, and the rows (token, head) that it takes
+  const int chunk = tid & ((1 << a.chunk_bits) - 1), row0 = tid >> a.chunk_bits, step = ROPE_THREADS >> a.chunk_bits;
+  const bool turned = chunk < a.turned;
+  const int c0 = HALF && turned ? chunk * V : 2 * V * chunk, apart = HALF && turned ? a.half : V;   // (the half layout's other channels begin at 2 half)
+  const int tab = table_place(chunk * V);
 
   using W = Vec<T, V>;
   W x[ITEMS], y[ITEMS];
-  struct At {
-    size_t first, second;   // the two vectors' places
-    int token, chunk;
-    bool key;
-  };
-  auto place = [&](int i) {
-    At p;
-    const int th = attn::quot(i, a.by_chunks);
-    p.chunk = attn::rest(i, th, a.by_chunks);
-    p.token = attn::quot(th, a.by_heads);
-    const int h = attn::rest(th, p.token, a.by_heads);
-    p.key = h >= a.H;
-    const size_t row = p.key ? (size_t)(t0 + p.token) * a.H_kv + (h - a.H) : (size_t)(t0 + p.token) * a.H + h;
-    const int c = HALF && p.chunk < a.turned ? p.chunk * V : 2 * V * p.chunk;   // (the half layout's other channels begin at 2 half)
-    p.first = row * a.d + c;
-    p.second = p.first + (HALF && p.chunk < a.turned ? a.half : V);
-    return p;
-  };
-  auto load = [&](int i0) {
+  size_t at[ITEMS];
+  int tok[ITEMS];
+  bool key[ITEMS];
+  auto load = [&](int r0) {
 #pragma unroll
     for (int u = 0; u < ITEMS; ++u) {
-      const int i = i0 + u * ROPE_THREADS;
-      if (i < items) {
-        const At p = place(i);
-        const T* const src = (const T*)(p.key ? a.k : a.q);
-        x[u] = *reinterpret_cast<const W*>(src + p.first);
-        y[u] = *reinterpret_cast<const W*>(src + p.second);
-      }
+      const int r = r0 + u * step;
+      if (r >= rows) continue;
+      tok[u] = attn::quot(r, a.by_heads);
+      const int h = attn::rest(r, tok[u], a.by_heads);
+      key[u] = h >= a.H;
+      at[u] = (key[u] ? (size_t)(t0 + tok[u]) * a.H_kv + (h - a.H) : (size_t)(t0 + tok[u]) * a.H + h) * a.d + c0;
+      const T* const src = (const T*)(key[u] ? a.k : a.q) + at[u];
+      x[u] = *reinterpret_cast<const W*>(src);
+      y[u] = *reinterpret_cast<const W*>(src + apart);
     }
   };
-  load(tid);
+  load(row0);
 
   for (int i = tid; i < nt * a.half; i += ROPE_THREADS) {   // (a token per lane: few different frequencies in a warp)
     const int f = i / nt, j = i - f * nt;
     const uint64_t phase = (uint64_t)position(a, t0 + j) * a.turn[f];
     float sn, cs;
     sincospif((float)(int32_t)(phase >> 32) * 4.656612873077393e-10f, &sn, &cs);   // 2^-31: half turns, within [-1, 1)
-    s_cs[f * a.per_block + j] = make_float2(cs * a.scale, sn * a.scale * a.sign);
+    s_cs[j * a.half + (V == 8 ? table_place(f) : f)] = make_float2(cs * a.scale, sn * a.scale * a.sign);
   }
   __syncthreads();
 
-  for (int i0 = tid; i0 < items; i0 += ITEMS * ROPE_THREADS) {
-    if (i0 != tid) load(i0);
+  for (int r0 = row0; r0 < rows; r0 += ITEMS * step) {
+    if (r0 != row0) load(r0);
 #pragma unroll
     for (int u = 0; u < ITEMS; ++u) {
-      const int i = i0 + u * ROPE_THREADS;
-      if (i >= items) continue;
-      const At p = place(i);
-      if (p.chunk < a.turned) {
-        const float2* const cs = s_cs + (size_t)p.chunk * V * a.per_block + p.token;
+      if (r0 + u * step >= rows) continue;
+      if (turned) {
+        float2 w[V];
+        const float2* const cs = s_cs + tok[u] * a.half;
+        if constexpr (V == 8) {
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const float4 p = *reinterpret_cast<const float4*>(cs + ((tab & ~7) | ((tab + e) & 7)));
+            w[e] = make_float2(p.x, p.y);
+            w[e + 1] = make_float2(p.z, p.w);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e) w[e] = cs[chunk * V + e];
+        }
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          const float2 w = cs[e * a.per_block];
           T &u0 = HALF ? x[u].x[e] : 2 * e < V ? x[u].x[2 * e < V ? 2 * e : 0] : y[u].x[2 * e < V ? 0 : 2 * e - V];
           T &u1 = HALF ? y[u].x[e] : 2 * e + 1 < V ? x[u].x[2 * e + 1 < V ? 2 * e + 1 : 0] : y[u].x[2 * e + 1 < V ? 0 : 2 * e + 1 - V];
           const float f0 = ldf<T>(&u0), f1 = ldf<T>(&u1);
-          stf<T>(&u0, f0 * w.x - f1 * w.y);
-          stf<T>(&u1, f0 * w.y + f1 * w.x);
+          stf<T>(&u0, f0 * w[e].x - f1 * w[e].y);
+          stf<T>(&u1, f0 * w[e].y + f1 * w[e].x);
         }
       }
-      T* const dst = (T*)(p.key ? a.k_out : a.q_out);
-      *reinterpret_cast<W*>(dst + p.first) = x[u];
-      *reinterpret_cast<W*>(dst + p.second) = y[u];
+      T* const dst = (T*)(key[u] ? a.k_out : a.q_out) + at[u];
+      *reinterpret_cast<W*>(dst) = x[u];
+      *reinterpret_cast<W*>(dst + apart) = y[u];
     }
   }
 }
@@ -177,15 +187,15 @@ int rope(const lawcat_rope_params* p, const double* freq, const void* q, const v
   // as wide as 16 bytes, the pairs' number and the distance of a pair's halves allow
   int V = p->dtype == LAWCAT_F32 ? 4 : 8;
   while (a.half % V) V /= 2;
-  a.chunks = p->d / 2 / V;
+  const int chunks = p->d / 2 / V;   // (a power of two, 1 ... 64)
+  for (a.chunk_bits = 0; 1 << a.chunk_bits < chunks;) ++a.chunk_bits;
   a.turned = a.half / V;
   // Tokens of a block: about eight items a thread, but one where blocks would not fill the SMs twice.
-  const int items = (a.H + a.H_kv) * a.chunks;
+  const int items = (a.H + a.H_kv) * chunks;
   long long per = (2 * ITEMS * ROPE_THREADS + items / 2) / items;
   const long long most = a.tokens / (2 * sm_count());
   per = per < most ? per : most;
   a.per_block = (int)(per < 1 ? 1 : per > 16 ? 16 : per);
-  a.by_chunks = attn::fast_div(a.chunks);
   a.by_heads = attn::fast_div(a.H + a.H_kv);
   a.by_T = attn::fast_div(a.T);
   const unsigned blocks = (unsigned)((a.tokens + a.per_block - 1) / a.per_block);
