@@ -88,6 +88,7 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
     mbar_fence_init();
   }
   behind_last_kernel();
+  const int pos_lane = lane_position(f);
   if (warp == 0) {
     tmem_alloc(sb + L::OFF_BAR + 16, L::COLS);
     tmem_relinquish();
@@ -98,7 +99,7 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
   const uint32_t tmem = (uint32_t)s_flags[0], k_col = tmem, s_col = tmem + L::K_COLS, o_col = s_col + NCOL, lanes = (uint32_t)(warp * 32) << 16;
 
   Walk<128> walk;
-  walk.start(f, (int)blockIdx.x);
+  walk.start(f, (int)blockIdx.x, pos_lane);
   Piece w;
   int count = 0;   // tiles so far
   bool fail = false;

@@ -86,6 +86,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     }
   }
   behind_last_kernel();
+  const int pos_lane = lane_position(f);
   if (warp == 9) {
     tmem_alloc(sb + L::OFF_BAR + 8 * L::NBAR, 512);
     tmem_relinquish();
@@ -99,7 +100,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   // a warpgroup's steps of a piece: every tile, or every other one
   auto steps_of = [&](int u, int n) { return two ? n : (n + 1 - u) / 2; };
   Walk<64> walk;
-  walk.start(f, (int)blockIdx.x);
+  walk.start(f, (int)blockIdx.x, pos_lane);
   Piece w;
 
   if (warp < 8) {
@@ -307,28 +308,28 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       const uint32_t O0 = o_col(two ? u : 0) + lanes, O1 = o_col(1) + lanes;
       const bool both = !two && n > 1;
 #pragma unroll 1
-      for (int c = c0; c < c1; c += 32) {
-        float o[32];
-        tmem_ld32(O0 + c, o);
+      for (int c = c0; c < c1; c += 16) {   // (code that runs once per piece is short: it comes from the instruction caches' far end)
+        float o[16];
+        tmem_ld16(O0 + c, o);
         if (both) {
-          float y[32];
-          tmem_ld32(O1 + c, y);
+          float y[16];
+          tmem_ld16(O1 + c, y);
           tmem_wait_ld();
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = (f0 == 0.f ? 0.f : o[e] * f0) + (f1 == 0.f ? 0.f : y[e] * f1);
+          for (int e = 0; e < 16; ++e) o[e] = (f0 == 0.f ? 0.f : o[e] * f0) + (f1 == 0.f ? 0.f : y[e] * f1);
         } else {
           tmem_wait_ld();
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] *= f0;
+          for (int e = 0; e < 16; ++e) o[e] *= f0;
         }
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
+        for (int e = 0; e < 16; ++e) {
           test = fmaf(o[e], 0.f, test);
           if constexpr (QUANT) largest = fmaxf(largest, fabsf(o[e]));
         }
         if constexpr (QUANT) {   // channels of eight back into their order
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
+          for (int e = 0; e < 16; e += 8) {
             const float x[8] = {o[e], o[e + 1], o[e + 2], o[e + 3], o[e + 4], o[e + 5], o[e + 6], o[e + 7]};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -339,11 +340,12 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         }
         if (r < R) {
           if (!direct) {
+            float* const to = pdst + (size_t)c * f.rows_pad;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) pdst[(size_t)(c + e) * f.rows_pad] = o[e];
+            for (int e = 0; e < 16; ++e) to[e * f.rows_pad] = o[e];
           } else {
 #pragma unroll
-            for (int e = 0; e < 32; e += 8)
+            for (int e = 0; e < 16; e += 8)
               *reinterpret_cast<uint4*>(dst + c + e) = l == 0.f ? make_uint4(0u, 0u, 0u, 0u)
                                                                 : make_uint4(pack_bf16(o[e], o[e + 1]), pack_bf16(o[e + 2], o[e + 3]), pack_bf16(o[e + 4], o[e + 5]), pack_bf16(o[e + 6], o[e + 7]));
           }

@@ -4,7 +4,8 @@
 // the device (a captured call is replayed at every length), so that blocks find their work there: all tiles of all segments in a row, cut
 // into as many equal shares as blocks run at once. A block walks its share, segment by segment; a segment that lies in one share is stored
 // by its block, the pieces of one that does not (at most two a block: the first of its share and the last) meet in a second kernel. Where
-// the capacity allows a segment a few tiles only, shares are whole segments, and there is no second kernel.
+// there are four blocks or more to a segment, no share reaches over a segment's end (a block's second segment costs it 4 us). Where the
+// capacity allows a segment a few tiles only, shares are whole segments, and there is no second kernel.
 #pragma once
 #include "attn_tree.cuh"
 
@@ -71,6 +72,7 @@ struct TreeTcArgs {
   int rows, tile_rows;
   int stride, rows_pad;   // rows of a tile, and of a piece, as they lie in tensor memory and scratch
   int whole;          // shares are whole segments
+  int apart;          // shares end where segments do (at most 32 sequences)
   int node_tiles;     // key tiles of the nodes' own
   int shares;         // blocks
   int least;          // tiles that make a share
@@ -146,6 +148,31 @@ struct Shares {
   __device__ __forceinline__ int of(int x) const { return x < more * (one + 1) ? x / (one + 1) : more + (x - more * (one + 1)) / one; }   // (x: one of the n)
 };
 
+// Shares that end where segments do: a segment of n tiles is ceil(n / quota) equal pieces, with the least quota (but for a sixteenth) under
+// which there are no more pieces than blocks. A lane has a sequence.
+struct Apart {
+  int pieces;   // of one of the lane's sequence's segments
+  __device__ __forceinline__ Apart(const TreeTcArgs& f, int tiles) {
+    const int per = segments_of_one(f), n = __reduce_add_sync(0xffffffffu, tiles) * per;
+    int quota = max(f.least, (n + f.shares - 1) / f.shares);
+    const int step = quota / 16 + 1;
+    for (;; quota += step) {   // (ends: with one piece each there are four times as many blocks)
+      pieces = (tiles + quota - 1) / quota;
+      if (__reduce_add_sync(0xffffffffu, pieces) * per <= f.shares) break;
+    }
+  }
+  __device__ __forceinline__ static int before(int mine, int lane) {
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+    return upto - mine;
+  }
+  __device__ __forceinline__ static int begin(int tiles, int n, int i) { return tiles / n * i + min(i, tiles % n); }
+};
+
 struct Piece {
   int b, segment, g, rb, pos;   // segment: of the sequence
   int t0, n, tiles;             // its tiles, of the segment's
@@ -157,7 +184,8 @@ struct Walk {
   int left;   // tiles (whole: segments) left
   int b, segment, t, tiles, pos;
 
-  __device__ __forceinline__ void start(const TreeTcArgs& f, int c) {   // by a whole warp
+  // By a whole warp; pos_lane: the position of sequence `lane`, which is asked for ahead of what comes before.
+  __device__ __forceinline__ void start(const TreeTcArgs& f, int c, int pos_lane) {
     const int per = segments_of_one(f), lane = threadIdx.x & 31;
     b = segment = t = 0;
     if (f.whole) {
@@ -166,32 +194,49 @@ struct Walk {
       left = s.begin(c + 1) - x;
       b = x / per;
       segment = x - b * per;
-    } else {
-      const int first = lane < f.a.B ? segment_tiles<TS>(f, f.a.pos[lane]) : 0;   // (of the first 32 sequences)
-      int n = __reduce_add_sync(0xffffffffu, first) * per;
-      if (f.a.B > 32) n = tiles_up_to<TS>(f, f.a.B);
-      const Shares s(n, f.shares, f.least);
-      int x = s.begin(c);
-      left = s.begin(c + 1) - x;
-      for (int b0 = 0; left > 0 && b0 < f.a.B; b0 += 32) {   // (32 sequences at a time: the one that x lies in)
-        const int mine = (b0 == 0 ? first : b0 + lane < f.a.B ? segment_tiles<TS>(f, f.a.pos[b0 + lane]) : 0) * per;
-        int upto = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int y = __shfl_up_sync(0xffffffffu, upto, o);
-          if (lane >= o) upto += y;
-        }
-        const uint32_t in = __ballot_sync(0xffffffffu, x < upto);
-        if (in) {
-          const int k = __ffs(in) - 1, all = __shfl_sync(0xffffffffu, mine, k), one = all / per;
-          x -= __shfl_sync(0xffffffffu, upto, k) - all;
-          b = b0 + k;
-          segment = x / one;
-          t = x - segment * one;
-          break;
-        }
-        x -= __shfl_sync(0xffffffffu, upto, 31);
+      load(f);
+      return;
+    }
+    const int first = lane < f.a.B ? segment_tiles<TS>(f, pos_lane) : 0;   // (of the first 32 sequences)
+    if (f.apart) {
+      const Apart s(f, first);
+      const int x = c - s.before(s.pieces * per, lane);                   // (of the lane's sequence)
+      const uint32_t in = __ballot_sync(0xffffffffu, x >= 0 && x < s.pieces * per);
+      left = 0;
+      if (in) {
+        b = __ffs(in) - 1;
+        const int r = __shfl_sync(0xffffffffu, x, b), n = __shfl_sync(0xffffffffu, s.pieces, b);
+        tiles = __shfl_sync(0xffffffffu, first, b);
+        pos = __shfl_sync(0xffffffffu, pos_lane, b);
+        segment = r / n;
+        t = Apart::begin(tiles, n, r - segment * n);
+        left = Apart::begin(tiles, n, r - segment * n + 1) - t;
       }
+      return;
+    }
+    int n = __reduce_add_sync(0xffffffffu, first) * per;
+    if (f.a.B > 32) n = tiles_up_to<TS>(f, f.a.B);
+    const Shares s(n, f.shares, f.least);
+    int x = s.begin(c);
+    left = s.begin(c + 1) - x;
+    for (int b0 = 0; left > 0 && b0 < f.a.B; b0 += 32) {   // (32 sequences at a time: the one that x lies in)
+      const int mine = (b0 == 0 ? first : b0 + lane < f.a.B ? segment_tiles<TS>(f, f.a.pos[b0 + lane]) : 0) * per;
+      int upto = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
+      }
+      const uint32_t in = __ballot_sync(0xffffffffu, x < upto);
+      if (in) {
+        const int k = __ffs(in) - 1, all = __shfl_sync(0xffffffffu, mine, k), one = all / per;
+        x -= __shfl_sync(0xffffffffu, upto, k) - all;
+        b = b0 + k;
+        segment = x / one;
+        t = x - segment * one;
+        break;
+      }
+      x -= __shfl_sync(0xffffffffu, upto, 31);
     }
     load(f);
   }
@@ -253,18 +298,29 @@ __global__ void __launch_bounds__(JoinTile<D, ROWS_INNER, GROUPS>::THREADS) attn
   __shared__ uint32_t s_bad, s_large;
   if (threadIdx.x == 0) s_bad = s_large = 0u;
   behind_last_kernel();
-  const int tiles = segment_tiles<TS>(f, a.pos[b]);
-  int n, n0;   // all tiles, and those in front of this segment
-  if (a.B <= 32) {
-    const int mine = lane < a.B ? segment_tiles<TS>(f, a.pos[lane]) : 0;
-    n = __reduce_add_sync(0xffffffffu, mine) * per;
-    n0 = __reduce_add_sync(0xffffffffu, lane < b ? mine : 0) * per;
+  int c0, c1;   // the shares that its first and its last tile lie in
+  const int mine = lane < a.B ? segment_tiles<TS>(f, a.pos[lane]) : 0;   // (of the first 32 sequences)
+  if (f.apart) {
+    const Apart s(f, mine);
+    const int n = __shfl_sync(0xffffffffu, s.pieces, b);
+    c0 = __shfl_sync(0xffffffffu, s.before(s.pieces * per, lane), b) + segment * n;
+    c1 = c0 + n - 1;
   } else {
-    n = tiles_up_to<TS>(f, a.B);
-    n0 = tiles_up_to<TS>(f, b);
+    int n, n0, tiles;   // all tiles, those in front of this sequence, and a segment's
+    if (a.B <= 32) {
+      n = __reduce_add_sync(0xffffffffu, mine) * per;
+      n0 = __reduce_add_sync(0xffffffffu, lane < b ? mine : 0) * per;
+      tiles = __shfl_sync(0xffffffffu, mine, b);
+    } else {
+      n = tiles_up_to<TS>(f, a.B);
+      n0 = tiles_up_to<TS>(f, b);
+      tiles = segment_tiles<TS>(f, a.pos[b]);
+    }
+    const Shares shares(n, f.shares, f.least);
+    const int x0 = n0 + segment * tiles;
+    c0 = shares.of(x0);
+    c1 = shares.of(x0 + tiles - 1);
   }
-  const Shares shares(n, f.shares, f.least);
-  const int x0 = n0 + segment * tiles, c0 = shares.of(x0), c1 = shares.of(x0 + tiles - 1);   // the shares that its first and its last tile lie in
   if (c0 == c1) return;                              // (one piece, which its block has stored)
   const int ri = ROWS_INNER ? lane : in / (D / 8), ch = c_first + (ROWS_INNER ? in / 32 : in % (D / 8)) * 8;
   const int R = a.N * G, rp = r_first + ri, r = row_of_piece(f, segment % f.row_blocks, rp);
@@ -343,9 +399,15 @@ __global__ void __launch_bounds__(JoinTile<D, ROWS_INNER, GROUPS>::THREADS) attn
     }
 }
 
+// the positions of the first 32 sequences, a lane each
+__device__ __forceinline__ int lane_position(const TreeTcArgs& f) {
+  const int lane = threadIdx.x & 31;
+  return !f.whole && lane < f.a.B ? f.a.pos[lane] : -1;
+}
+
 // How a call's work is shared out. rows: of a block, in tiles of tile_rows, which lie `stride` apart; resident: blocks that run at once on an SM.
 struct TreePlan {
-  int rows, tile_rows, stride, row_blocks, rows_pad, whole, node_tiles, shares, least;
+  int rows, tile_rows, stride, row_blocks, rows_pad, whole, apart, node_tiles, shares, least;
   bool fits;
 };
 inline TreePlan tree_plan(int B, int N, int H, int H_kv, int C, int W, int rows, int tile_rows, int stride, int TS, int resident) {
@@ -365,6 +427,7 @@ inline TreePlan tree_plan(int B, int N, int H, int H_kv, int C, int W, int rows,
   p.whole = most <= 8 * 64 / TS;
   const long long all = p.whole ? segments : (segments * most + p.least - 1) / p.least;
   p.shares = (int)(all < run ? all : run);
+  p.apart = !p.whole && B <= 32 && p.shares >= 4 * segments;
   return p;
 }
 inline size_t tree_plan_bytes(const TreePlan& p, int d) {
@@ -375,7 +438,7 @@ inline TreeTcArgs tree_tc_args(const AttnTree& c, const TreePlan& p) {
   TreeTcArgs f{};
   f.a = c.a;
   f.group = fast_div(c.a.H / c.a.H_kv);
-  f.row_blocks = p.row_blocks; f.rows = p.rows; f.tile_rows = p.tile_rows; f.stride = p.stride; f.rows_pad = p.rows_pad; f.whole = p.whole; f.node_tiles = p.node_tiles;
+  f.row_blocks = p.row_blocks; f.rows = p.rows; f.tile_rows = p.tile_rows; f.stride = p.stride; f.rows_pad = p.rows_pad; f.whole = p.whole; f.apart = p.apart; f.node_tiles = p.node_tiles;
   f.shares = p.shares; f.least = p.least;
   f.part_ml = (float2*)c.ws;
   f.part_o = (float*)((char*)c.ws + align_up(sizeof(float2) * 2 * (size_t)p.shares * p.rows_pad, 256));
