@@ -6,9 +6,10 @@
 // leading 32 bits go through sincospi, whose argument needs no reduction.
 //
 // Memory-bound: every value is read once and written once. A block takes a few tokens; their cosines and sines are computed once, into
-// shared memory, for all heads. A thread has V pairs of a head (two loads of 16 bytes where the sizes allow it) and takes head after head,
-// four at a time with all their loads in flight, the first four ahead of the cosines. The table's pieces of 16 bytes are stored so that eight
-// threads side by side read them from different banks.
+// shared memory, for all heads. A thread has V pairs of a head (two loads of 16 bytes where the sizes allow it) and takes head after head, the
+// first ahead of the cosines; loads in flight come from 48 warps an SM. (32768 tokens, 32/8 heads of 128 in bf16, 671 MB: 104.5 us, the
+// measured copy rate would take 102.5; with two heads at a time in a thread and four blocks an SM 123, with four 175.) The table's pieces of
+// 16 bytes are stored so that eight threads side by side read them from different banks.
 #include "attn.cuh"
 #include "attn_tc.cuh"
 
@@ -16,7 +17,7 @@ namespace lawcat {
 namespace {
 
 constexpr int MAX_PAIRS = 64;
-constexpr int ROPE_THREADS = 256, ITEMS = 4;
+constexpr int ROPE_THREADS = 256, ROPE_BLOCKS = 6;   // an SM's blocks
 
 struct RopeArgs {
   const void *q, *k;
@@ -63,7 +64,7 @@ __device__ __forceinline__ int table_place(int f) {
 
 // HALF: pairs (i, i + half); else (2 i, 2 i + 1)
 template <typename T, int V, bool HALF>
-__global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(ROPE_THREADS, ROPE_BLOCKS) rope_kernel(const __grid_constant__ RopeArgs a) {
   extern __shared__ float2 s_cs[];   // [per_block][half] cosine and sine
   attn::behind_last_kernel();
   const long long t0 = (long long)blockIdx.x * a.per_block;
@@ -76,25 +77,20 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
   const int tab = table_place(chunk * V);
 
   using W = Vec<T, V>;
-  W x[ITEMS], y[ITEMS];
-  size_t at[ITEMS];
-  int tok[ITEMS];
-  bool key[ITEMS];
-  auto load = [&](int r0) {
-#pragma unroll
-    for (int u = 0; u < ITEMS; ++u) {
-      const int r = r0 + u * step;
-      if (r >= rows) continue;
-      tok[u] = attn::quot(r, a.by_heads);
-      const int h = attn::rest(r, tok[u], a.by_heads);
-      key[u] = h >= a.H;
-      at[u] = (key[u] ? (size_t)(t0 + tok[u]) * a.H_kv + (h - a.H) : (size_t)(t0 + tok[u]) * a.H + h) * a.d + c0;
-      const T* const src = (const T*)(key[u] ? a.k : a.q) + at[u];
-      x[u] = *reinterpret_cast<const W*>(src);
-      y[u] = *reinterpret_cast<const W*>(src + apart);
-    }
+  W x, y;
+  size_t at;
+  int tok;
+  bool key;
+  auto load = [&](int r) {
+    tok = attn::quot(r, a.by_heads);
+    const int h = attn::rest(r, tok, a.by_heads);
+    key = h >= a.H;
+    at = (key ? (size_t)(t0 + tok) * a.H_kv + (h - a.H) : (size_t)(t0 + tok) * a.H + h) * a.d + c0;
+    const T* const src = (const T*)(key ? a.k : a.q) + at;
+    x = *reinterpret_cast<const W*>(src);
+    y = *reinterpret_cast<const W*>(src + apart);
   };
-  load(row0);
+  if (row0 < rows) load(row0);
 
   for (int i = tid; i < nt * a.half; i += ROPE_THREADS) {   // (a token per lane: few different frequencies in a warp)
     const int f = i / nt, j = i - f * nt;
@@ -105,38 +101,34 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
   }
   __syncthreads();
 
-  for (int r0 = row0; r0 < rows; r0 += ITEMS * step) {
-    if (r0 != row0) load(r0);
+  for (int r = row0; r < rows; r += step) {
+    if (r != row0) load(r);
+    if (turned) {
+      float2 w[V];
+      const float2* const cs = s_cs + tok * a.half;
+      if constexpr (V == 8) {
 #pragma unroll
-    for (int u = 0; u < ITEMS; ++u) {
-      if (r0 + u * step >= rows) continue;
-      if (turned) {
-        float2 w[V];
-        const float2* const cs = s_cs + tok[u] * a.half;
-        if constexpr (V == 8) {
-#pragma unroll
-          for (int e = 0; e < 8; e += 2) {
-            const float4 p = *reinterpret_cast<const float4*>(cs + ((tab & ~7) | ((tab + e) & 7)));
-            w[e] = make_float2(p.x, p.y);
-            w[e + 1] = make_float2(p.z, p.w);
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < V; ++e) w[e] = cs[chunk * V + e];
+        for (int e = 0; e < 8; e += 2) {
+          const float4 p = *reinterpret_cast<const float4*>(cs + ((tab & ~7) | ((tab + e) & 7)));
+          w[e] = make_float2(p.x, p.y);
+          w[e + 1] = make_float2(p.z, p.w);
         }
+      } else {
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          T &u0 = HALF ? x[u].x[e] : 2 * e < V ? x[u].x[2 * e < V ? 2 * e : 0] : y[u].x[2 * e < V ? 0 : 2 * e - V];
-          T &u1 = HALF ? y[u].x[e] : 2 * e + 1 < V ? x[u].x[2 * e + 1 < V ? 2 * e + 1 : 0] : y[u].x[2 * e + 1 < V ? 0 : 2 * e + 1 - V];
-          const float f0 = ldf<T>(&u0), f1 = ldf<T>(&u1);
-          stf<T>(&u0, f0 * w[e].x - f1 * w[e].y);
-          stf<T>(&u1, f0 * w[e].y + f1 * w[e].x);
-        }
+        for (int e = 0; e < V; ++e) w[e] = cs[chunk * V + e];
       }
-      T* const dst = (T*)(key[u] ? a.k_out : a.q_out) + at[u];
-      *reinterpret_cast<W*>(dst) = x[u];
-      *reinterpret_cast<W*>(dst + apart) = y[u];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        T &u0 = HALF ? x.x[e] : 2 * e < V ? x.x[2 * e < V ? 2 * e : 0] : y.x[2 * e < V ? 0 : 2 * e - V];
+        T &u1 = HALF ? y.x[e] : 2 * e + 1 < V ? x.x[2 * e + 1 < V ? 2 * e + 1 : 0] : y.x[2 * e + 1 < V ? 0 : 2 * e + 1 - V];
+        const float f0 = ldf<T>(&u0), f1 = ldf<T>(&u1);
+        stf<T>(&u0, f0 * w[e].x - f1 * w[e].y);
+        stf<T>(&u1, f0 * w[e].y + f1 * w[e].x);
+      }
     }
+    T* const dst = (T*)(key ? a.k_out : a.q_out) + at;
+    *reinterpret_cast<W*>(dst) = x;
+    *reinterpret_cast<W*>(dst + apart) = y;
   }
 }
 
@@ -190,9 +182,10 @@ int rope(const lawcat_rope_params* p, const double* freq, const void* q, const v
   const int chunks = p->d / 2 / V;   // (a power of two, 1 ... 64)
   for (a.chunk_bits = 0; 1 << a.chunk_bits < chunks;) ++a.chunk_bits;
   a.turned = a.half / V;
-  // Tokens of a block: about eight items a thread, but one where blocks would not fill the SMs twice.
+  // Tokens of a block: about four heads a thread (of 32768 tokens, 32/8 heads of 128: two and three took 108 us, six 104, four 104.5; of 4856
+  // tokens, heads of 64: six 12.3, four 10.6), but one where blocks would not fill the SMs twice.
   const int items = (a.H + a.H_kv) * chunks;
-  long long per = (2 * ITEMS * ROPE_THREADS + items / 2) / items;
+  long long per = (4 * ROPE_THREADS + items / 2) / items;
   const long long most = a.tokens / (2 * sm_count());
   per = per < most ? per : most;
   a.per_block = (int)(per < 1 ? 1 : per > 16 ? 16 : per);
