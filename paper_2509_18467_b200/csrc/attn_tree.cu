@@ -244,11 +244,11 @@ __global__ void __launch_bounds__(32 * W) attn_tree_join_kernel(const __grid_con
   if (__syncthreads_or(!fine) && warp == 0) tree_row_again<T, D, QUANT>(a, (int)(row / ((size_t)a.N * a.H)), (int)(row / a.H % a.N), (int)(row % a.H));
 }
 
-// Parts of the keys: as many as give each SM two blocks, and no more than there are pieces of 256 keys.
+// Parts of the keys: as many as give each SM two blocks, and no more than there are tiles.
 static int tree_parts(const AttnTree& c) {
   const attn::TreeArgs& a = c.a;
   const long long rows = (long long)a.N * (a.H / a.H_kv), n = (long long)a.B * a.H_kv * ((rows + TREE_ROWS - 1) / TREE_ROWS);
-  const int most = std::min(a.W, a.C) / 256 + 1;
+  const int most = std::min(a.W, a.C) / TREE_KEYS + 1;
   const long long want = (2LL * sm_count() + n - 1) / (n > 0 ? n : 1);
   return (int)(want < 1 ? 1 : want < most ? want : most);
 }
