@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
         const uint4* const from = reinterpret_cast<const uint4*>(q + (size_t)(uint32_t)slot * (D / 2));
 #pragma unroll
         for (int i = 0; i < WPR / 4; ++i) {
-          const uint4 x = __ldcs(from + i);
+          const uint4 x = __ldg(from + i);   // (half a sector: the other half comes from L1)
           codes[4 * i] = x.x; codes[4 * i + 1] = x.y; codes[4 * i + 2] = x.z; codes[4 * i + 3] = x.w;
         }
         const bf16* const pair = p + (size_t)(uint32_t)slot * (2 * NG);
@@ -234,14 +234,14 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
       const CachedTile t = ahead;
       const bool more = i + 1 < n && it + 1 >= f.node_tiles;
 #pragma unroll
-      for (int s = 0; s < D / 64; ++s) {
-        float x[32];
+      for (int s = 0; s < NG; ++s) {   // a group's 32 channels at a time
+        float x[16];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint4 y = unpack8(kc[8 * s + e], group_scale(kp[2 * s + e / 4]));
+        for (int e = 0; e < 4; ++e) {
+          const uint4 y = unpack8(kc[4 * s + e], group_scale(kp[s]));
           x[4 * e] = __uint_as_float(y.x); x[4 * e + 1] = __uint_as_float(y.y); x[4 * e + 2] = __uint_as_float(y.z); x[4 * e + 3] = __uint_as_float(y.w);
         }
-        tmem_st32(k_col + lanes + 32 * s, x);
+        tmem_st16(k_col + lanes + 16 * s, x);
       }
       tmem_wait_st();
       tc_fence_before_sync();
