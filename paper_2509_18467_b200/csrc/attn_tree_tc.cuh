@@ -287,7 +287,7 @@ struct JoinTile {
 template <int D, bool QUANT, int TS, bool ROWS_INNER, int GROUPS>
 __global__ void __launch_bounds__(JoinTile<D, ROWS_INNER, GROUPS>::THREADS) attn_tree_join_tc_kernel(const __grid_constant__ TreeTcArgs f) {
   using J = JoinTile<D, ROWS_INNER, GROUPS>;
-  constexpr int U = GROUPS == 1 ? 2 : 4;
+  constexpr int U = GROUPS == 1 ? 3 : 4;
   const TreeArgs& a = f.a;
   const int G = a.H / a.H_kv, chunks = f.rows_pad / J::ROWS, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   const int group = threadIdx.x / J::PER, in = threadIdx.x % J::PER;
