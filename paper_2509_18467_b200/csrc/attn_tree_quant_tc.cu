@@ -99,7 +99,9 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
   const uint32_t tmem = (uint32_t)s_flags[0], k_col = tmem, s_col = tmem + L::K_COLS, o_col = s_col + NCOL, lanes = (uint32_t)(warp * 32) << 16;
 
   Walk<128> walk;
-  walk.start(f, (int)blockIdx.x, pos_lane);
+  const int share = share_of_block(f);
+  if (tid == 0 && !f.whole && !f.apart) f.told[share] = 0ull;   // (what a call that gave up may have left)
+  walk.start(f, share, pos_lane);
   Piece w;
   int count = 0;   // tiles so far
   bool fail = false;
@@ -394,28 +396,74 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
     if (!fail) fail = !wait_bar(bar_o, (count - 1) & 1, s_abort, f.limit);
     if (named_bar_or(3, 128, fail)) break;
     tc_fence_after_sync();
-    const bool direct = is_whole(w);
-    const size_t slot = piece_slot(w, (int)blockIdx.x);
+    const bool join = is_joined_here(f, w), direct = is_whole(w) || join;
+    const int others = join ? w.last - share : 0;
+    float sum = 0.f;
     if (tid < NCOL) {
-      float sum = (s_red[tid] + s_red[NCOL + tid]) + (s_red[2 * NCOL + tid] + s_red[3 * NCOL + tid]);
+      sum = (s_red[tid] + s_red[NCOL + tid]) + (s_red[2 * NCOL + tid] + s_red[3 * NCOL + tid]);
       if (s_depth[tid] < 0) sum = 0.f;
-      s_sum[tid] = direct ? sum == 0.f ? 0.f : 1.f / (sum * KV_FACTOR) : 1.f / KV_FACTOR;
       const float m = -s_ref[tid / 2 * 4 + 2 + (tid & 1)];
-      if (!direct && r0 + tid < R) f.part_ml[slot * f.rows_pad + tid] = make_float2(sum == 0.f ? -INFINITY : m, sum);
+      if (!direct && r0 + tid < R) f.part_ml[(size_t)share * f.rows_pad + tid] = make_float2(sum == 0.f ? -INFINITY : m, sum);
     }
     float o[NCOL];
 #pragma unroll
     for (int c = 0; c < NCOL; c += 16) tmem_ld16(o_col + lanes + c, o + c);
     tmem_wait_ld();
-    named_bar_sync(3, 128);
     const int ch = (tid & ~7) + ((tid & 7) >> 1) + 4 * (tid & 1);   // the lane's channel
+    if (join) {
+      // the other pieces of the segment: their maxima first, then their sums at the common one
+      bool told = true;
+      if (tid == 0)
+        for (int i = 0; i < others && told; ++i) told = wait_told(f.told + share + 1 + i, f.number, s_abort, item_limit(f.limit, w.tiles));
+      fail = named_bar_or(3, 128, !told);
+      if (fail) break;
+      float m = -INFINITY, top = -INFINITY;
+      const bool row = tid < NCOL && r0 + tid < R;
+      auto other = [&](int i) { return row ? __ldcg(f.part_ml + (size_t)(share + 1 + i) * f.rows_pad + tid) : make_float2(-INFINITY, 0.f); };
+      if (tid < NCOL) {
+        m = top = sum == 0.f ? -INFINITY : -s_ref[tid / 2 * 4 + 2 + (tid & 1)];
+        for (int i = 0; i < others; ++i) {
+          const float2 x = other(i);
+          if (x.y != 0.f) top = fmaxf(top, x.x);
+        }
+        s_factor[tid] = m == -INFINITY ? 0.f : ex2f(m - top);
+        sum *= s_factor[tid];
+      }
+      named_bar_sync(3, 128);
+#pragma unroll
+      for (int c = 0; c < NCOL; ++c) o[c] = s_factor[c] == 0.f ? 0.f : o[c] * s_factor[c];
+#pragma unroll 1
+      for (int i = 0; i < others; ++i) {
+        named_bar_sync(3, 128);   // (the factors have been read)
+        if (tid < NCOL) {
+          const float2 x = other(i);
+          s_factor[tid] = x.y == 0.f ? 0.f : ex2f(x.x - top) * KV_FACTOR;
+          sum += x.y == 0.f ? 0.f : x.y * ex2f(x.x - top);
+        }
+        named_bar_sync(3, 128);
+        const float* const from = f.part_o + (size_t)(share + 1 + i) * f.rows_pad * D + ch;
+        if (tid < D)
+#pragma unroll
+          for (int c = 0; c < NCOL; c += 8) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = r0 + c + e < R ? __ldcg(from + (c + e) * D) : 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[c + e] += s_factor[c + e] == 0.f ? 0.f : s_factor[c + e] * x[e];
+          }
+      }
+      if (tid < NCOL && s_depth[tid] < 0) sum = 0.f;
+    }
+    if (tid < NCOL) s_sum[tid] = direct ? sum == 0.f ? 0.f : 1.f / (sum * KV_FACTOR) : 1.f / KV_FACTOR;
+    named_bar_sync(3, 128);
     if (!direct) {
-      float* const dst = f.part_o + slot * f.rows_pad * D + ch;
+      float* const dst = f.part_o + (size_t)share * f.rows_pad * D + ch;
 #pragma unroll
       for (int c = 0; c < NCOL; ++c)
         if (r0 + c < R && tid < D) dst[c * D] = o[c] * s_sum[c];
       tc_fence_before_sync();
       named_bar_sync(3, 128);
+      if (!f.apart && tid == 0) tell(f.told + share, f.number);
     } else {
       bf16* const s_out = reinterpret_cast<bf16*>(smem);   // [NCOL][D] over V
 #pragma unroll

@@ -100,7 +100,9 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   // a warpgroup's steps of a piece: every tile, or every other one
   auto steps_of = [&](int u, int n) { return two ? n : (n + 1 - u) / 2; };
   Walk<64> walk;
-  walk.start(f, (int)blockIdx.x, pos_lane);
+  const int share = share_of_block(f);
+  if (tid == 0 && !f.whole && !f.apart) f.told[share] = 0ull;   // (what a call that gave up may have left)
+  walk.start(f, share, pos_lane);
   Piece w;
 
   if (warp < 8) {
@@ -284,7 +286,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       ok = ok && __all_sync(0xffffffffu, wait_bar(bar(L::B_DONE), seq & 1, s_abort, item_limit(f.limit, n)));
       tc_fence_after_sync();
       // with one tile of rows a warpgroup has half of the channels of both sums
-      const bool direct = is_whole(w);
+      const bool join = is_joined_here(f, w), direct = is_whole(w) || join;
       float f0 = 1.f, f1 = 0.f;
       if (!two) {
         s_ml[u * 128 + r128] = make_float2(m, l);
@@ -297,13 +299,37 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         m = top;
       }
       if (!there) l = 0.f;
-      const float inv = (!direct ? 1.f : l == 0.f ? 0.f : 1.f / l) * (QUANT ? 1.f / KV_FACTOR : 1.f);
-      f0 *= inv;
-      f1 *= inv;
+      // the other pieces of the segment, where this block joins them
+      const int others = join ? w.last - share : 0;
+      auto other_ml = [&](int i) { return __ldcg(f.part_ml + (size_t)(share + 1 + i) * f.rows_pad + rp); };
+      if (join) {
+        bool told = true;
+        if (tid == 0)
+          for (int i = 0; i < others && told; ++i) told = wait_told(f.told + share + 1 + i, f.number, s_abort, item_limit(f.limit, w.tiles));
+        ok = !named_bar_or(2, 256, !told || !ok);
+        float top = l == 0.f ? -INFINITY : m, sum = 0.f;
+        if (r < R)
+          for (int i = 0; i < others; ++i) {
+            const float2 x = other_ml(i);
+            const float was = top;
+            if (x.y == 0.f) continue;   // (a piece without keys has no weights)
+            top = fmaxf(top, x.x);
+            sum = sum * (was == -INFINITY ? 0.f : ex2f(was - top)) + x.y * ex2f(x.x - top);
+          }
+        const float own = m == -INFINITY || top == -INFINITY ? 0.f : ex2f(m - top);
+        f0 *= own;
+        f1 *= own;
+        l = there ? l * own + sum : 0.f;
+        m = top;
+      }
+      if (QUANT) {
+        f0 *= 1.f / KV_FACTOR;
+        f1 *= 1.f / KV_FACTOR;
+      }
+      const float inv = !direct ? 1.f : l == 0.f ? 0.f : 1.f / l;
       float test = l * 0.f, largest = 0.f;
-      const size_t slot = piece_slot(w, (int)blockIdx.x);
       bf16* const dst = (bf16*)a.o + (((size_t)b * a.N + node) * a.H + h) * D;
-      float* const pdst = f.part_o + slot * D * f.rows_pad + rp;
+      float* const pdst = f.part_o + (size_t)share * D * f.rows_pad + rp;
       const int c0 = two ? 0 : u * (D / 2), c1 = two ? D : c0 + D / 2;
       const uint32_t O0 = o_col(two ? u : 0) + lanes, O1 = o_col(1) + lanes;
       const bool both = !two && n > 1;
@@ -322,11 +348,6 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[e] *= f0;
         }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          test = fmaf(o[e], 0.f, test);
-          if constexpr (QUANT) largest = fmaxf(largest, fabsf(o[e]));
-        }
         if constexpr (QUANT) {   // channels of eight back into their order
 #pragma unroll
           for (int e = 0; e < 16; e += 8) {
@@ -337,6 +358,24 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
               o[e + 4 + k] = x[2 * k + 1];
             }
           }
+        }
+        if (r < R)
+#pragma unroll 1
+          for (int i = 0; i < others; ++i) {
+            const float2 y = other_ml(i);
+            const float* const from = f.part_o + ((size_t)(share + 1 + i) * D + c) * f.rows_pad + rp;
+            float x[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = __ldcg(from + e * f.rows_pad);
+            const float k = y.y == 0.f ? 0.f : ex2f(y.x - m);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] += k == 0.f ? 0.f : k * x[e];
+          }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          o[e] *= inv;
+          test = fmaf(o[e], 0.f, test);
+          if constexpr (QUANT) largest = fmaxf(largest, fabsf(o[e]));
         }
         if (r < R) {
           if (!direct) {
@@ -353,8 +392,8 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       }
       tc_fence_before_sync();
       mbar_arrive(bar(L::B_OE));
-      if (r < R && !direct && (two || u == 0)) f.part_ml[slot * f.rows_pad + rp] = make_float2(m, l);
-      // rows to be computed again (of a segment in pieces the join looks)
+      if (r < R && !direct && (two || u == 0)) f.part_ml[(size_t)share * f.rows_pad + rp] = make_float2(m, l);
+      // rows to be computed again (of a segment in pieces whoever joins them looks)
       const uint32_t bad = __ballot_sync(0xffffffffu, ok && there && direct && !(test == 0.f));
       const uint32_t large = QUANT ? __ballot_sync(0xffffffffu, !(ok && there && direct) || l == 0.f || !(largest < SMALL)) : 0xffffffffu;
       if (lane == 0) {
@@ -372,6 +411,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       at += n;
       if (named_bar_or(2, 256, !ok)) break;   // (s_ml, the paths and the flags have been read)
       if (tid < 16) s_bad[tid] = 0u;          // (written again behind other barriers)
+      if (!direct && !f.apart && tid == 0) tell(f.told + share, f.number);
     }
   } else if (warp != 9) {
     // ------------------------------------------------------------------------------------------------ copies
@@ -380,7 +420,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       // warp's time) does for four stores of 32 groups. Zeros where no row may see a slot.
       constexpr int NG = D / 32, SLOTS = 32 / NG, AHEAD = 6;   // AHEAD: tiles towards L2
       const int me = warp == 8 ? 0 : warp - 9, slot = lane / NG, grp = lane % NG;
-      int tile = 0;
+      int tile = 0, clear = 0;   // tiles of the pieces so far; those whose stages are known to be free
       bool ok = true;
       while (ok && walk.next(f, w)) {
         const Ring<64> ring = ring_of<64>(w.pos, a.C, a.W);
@@ -419,9 +459,14 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 #pragma unroll 1
         for (int x = me; x < all; x += L::LOADERS) {
           const int it = (uint32_t)x / L::ITEMS, p = (uint32_t)x % L::ITEMS, at = 2 * (tile + it), s = (uint32_t)at % ST;
-          if (at >= ST)
-            ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_EMPTY + s), ((uint32_t)at / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles)) &&
-                                             wait_bar(bar(L::B_EMPTY + s + 1), ((uint32_t)at / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles)));
+          // Tile by tile, those without a part for this warp too: it may have had none in many short pieces, and a barrier's phase bit tells
+          // a stage that is free from one that is still to be used twice only to those who have followed it.
+          for (; clear <= tile + it && ok; ++clear) {
+            const int c = 2 * clear, e = (uint32_t)c % ST;
+            if (c >= ST)
+              ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_EMPTY + e), ((uint32_t)c / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles)) &&
+                                               wait_bar(bar(L::B_EMPTY + e + 1), ((uint32_t)c / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles)));
+          }
           if (!ok) break;
           while (seen < it) to_l2(++seen + AHEAD);
           const uint32_t st = sb + L::OFF_RING + (uint32_t)s * L::KT;

@@ -2,11 +2,18 @@
 //
 // A segment is a block of rows of one (sequence, key-value head); its work is its key tiles, the nodes' own and the cached ones. Positions lie on
 // the device (a captured call is replayed at every length), so that blocks find their work there: all tiles of all segments in a row, cut
-// into as many equal shares as blocks run at once. A block walks its share, segment by segment; a segment that lies in one share is stored
-// by its block, the pieces of one that does not (at most two a block: the first of its share and the last) meet in a second kernel. Where
-// there are four blocks or more to a segment, no share reaches over a segment's end (a block's second segment costs it 4 us). Where the
-// capacity allows a segment a few tiles only, shares are whole segments, and there is no second kernel.
+// into as many equal shares as blocks run at once. A block walks its share, segment by segment; a segment that lies in one share is stored by
+// its block. Of one that does not, the block with its first piece waits for the others' sums and joins them: they are the first pieces of
+// their blocks' shares, and done long before as a rule (16 sequences of 6000 slots, 32 nodes: a second kernel that joined took 13 us of
+// 92). Shares are dealt out from the last to the first, so that a block waits only for blocks that started before it.
+// Where there are four blocks or more to a segment, no share reaches over a segment's end (a block's second segment costs it 4 us), and the
+// pieces, which end together, meet in a second kernel. Where the capacity allows a segment a few tiles only, shares are whole segments.
+//
+// That a block's sums are there is told by a number that is the call's own, in scratch that may hold anything: 64 bits that no other call
+// has; the block that waits for it puts a zero in its place, so that a replayed call finds none.
 #pragma once
+#include <chrono>
+
 #include "attn_tree.cuh"
 
 namespace lawcat {
@@ -76,8 +83,10 @@ struct TreeTcArgs {
   int node_tiles;     // key tiles of the nodes' own
   int shares;         // blocks
   int least;          // tiles that make a share
-  float2* part_ml;    // [2 shares, rows_pad] (maximum in log2 units, sum)
-  float* part_o;      // [2 shares, ...] weighted values: D x rows_pad, or rows_pad x D
+  float2* part_ml;    // [shares, rows_pad] (maximum in log2 units, sum)
+  float* part_o;      // [shares, ...] weighted values: D x rows_pad, or rows_pad x D
+  unsigned long long* told;   // [shares] `number` once the share's sums are there
+  unsigned long long number;
   long long limit;
   int* dev_status;
 };
@@ -145,6 +154,7 @@ struct Shares {
     more = n - one * count;
   }
   __device__ __forceinline__ int begin(int c) const { return min(c, count) * one + min(c, more); }
+  Shares() = default;
   __device__ __forceinline__ int of(int x) const { return x < more * (one + 1) ? x / (one + 1) : more + (x - more * (one + 1)) / one; }   // (x: one of the n)
 };
 
@@ -176,6 +186,7 @@ struct Apart {
 struct Piece {
   int b, segment, g, rb, pos;   // segment: of the sequence
   int t0, n, tiles;             // its tiles, of the segment's
+  int last;                     // the share that the segment's last tile lies in (not where shares are whole segments or end with them)
 };
 
 // A block's walk over its share.
@@ -183,6 +194,8 @@ template <int TS>
 struct Walk {
   int left;   // tiles (whole: segments) left
   int b, segment, t, tiles, pos;
+  int at;     // of all tiles
+  Shares shares;
 
   // By a whole warp; pos_lane: the position of sequence `lane`, which is asked for ahead of what comes before.
   __device__ __forceinline__ void start(const TreeTcArgs& f, int c, int pos_lane) {
@@ -216,9 +229,9 @@ struct Walk {
     }
     int n = __reduce_add_sync(0xffffffffu, first) * per;
     if (f.a.B > 32) n = tiles_up_to<TS>(f, f.a.B);
-    const Shares s(n, f.shares, f.least);
-    int x = s.begin(c);
-    left = s.begin(c + 1) - x;
+    shares = Shares(n, f.shares, f.least);
+    int x = at = shares.begin(c);
+    left = shares.begin(c + 1) - x;
     for (int b0 = 0; left > 0 && b0 < f.a.B; b0 += 32) {   // (32 sequences at a time: the one that x lies in)
       const int mine = (b0 == 0 ? first : b0 + lane < f.a.B ? segment_tiles<TS>(f, f.a.pos[b0 + lane]) : 0) * per;
       int upto = mine;
@@ -255,6 +268,8 @@ struct Walk {
     p.t0 = t;
     p.tiles = tiles;
     p.n = f.whole ? tiles : min(tiles - t, left);
+    p.last = f.whole || f.apart ? 0 : shares.of(at - t + tiles - 1);
+    at += p.n;
     left -= f.whole ? 1 : p.n;
     t += p.n;
     if (t == tiles) {
@@ -274,54 +289,57 @@ __device__ __forceinline__ int row_of_piece(const TreeTcArgs& f, int rb, int rp)
   return in < f.tile_rows ? rb * f.rows + tile * f.tile_rows + in : 0x7fffffff;
 }
 __device__ __forceinline__ bool is_whole(const Piece& p) { return p.n == p.tiles; }
-__device__ __forceinline__ int piece_slot(const Piece& p, int c) { return 2 * c + (p.t0 == 0); }
+// whether a piece's block joins the others, and the share that a block has
+__device__ __forceinline__ bool is_joined_here(const TreeTcArgs& f, const Piece& p) { return !f.apart && p.t0 == 0 && !is_whole(p); }
+__device__ __forceinline__ int share_of_block(const TreeTcArgs& f) { return f.whole || f.apart ? (int)blockIdx.x : f.shares - 1 - (int)blockIdx.x; }
 
-// The pieces of a segment's rows, eight channels to a thread. Of few pieces a block has 32 rows; of many it has 1024 values, 32 rows x 32 channels
-// where a piece's weighted values are D x rows_pad (ROWS_INNER), 1024 / D whole rows where they are rows_pad x D, and four groups of threads
-// share the pieces out, four pieces' loads in flight, and meet in shared memory.
-template <int D, bool ROWS_INNER, int GROUPS>
+// Bounded wait for a share's sums (by one thread, a barrier behind it); the number is taken away.
+__device__ __forceinline__ bool wait_told(unsigned long long* at, unsigned long long number, volatile int* abort_flag, long long limit) {
+  const long long t0 = clock64();
+  for (;;) {
+    unsigned long long x;
+    asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(x) : "l"(at) : "memory");
+    if (x == number) break;
+    if (*abort_flag) return false;
+    if (clock64() - t0 > limit) {
+      *abort_flag = 1;
+      return false;
+    }
+    __nanosleep(100);
+  }
+  asm volatile("st.relaxed.gpu.global.u64 [%0], %1;" ::"l"(at), "l"(0ull) : "memory");
+  return true;
+}
+__device__ __forceinline__ void tell(unsigned long long* at, unsigned long long number) {   // (behind a barrier behind the stores)
+  __threadfence();
+  asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(at), "l"(number) : "memory");
+}
+
+// The pieces of a segment's rows where shares end with segments. A block has 1024 values of a piece, eight to a thread: 32 rows x 32 channels
+// where a piece's weighted values are D x rows_pad (ROWS_INNER), 1024 / D whole rows where they are rows_pad x D; four groups of threads share
+// the pieces out, four pieces' loads in flight, and meet in shared memory.
+template <int D, bool ROWS_INNER>
 struct JoinTile {
-  static constexpr int ROWS = ROWS_INNER || GROUPS == 1 ? 32 : 1024 / D, CHANNELS = ROWS_INNER && GROUPS > 1 ? 32 : D, SPLIT = D / CHANNELS;   // SPLIT: blocks of the same rows
-  static constexpr int PER = ROWS * CHANNELS / 8, THREADS = GROUPS * PER;   // threads of a group
+  static constexpr int ROWS = ROWS_INNER ? 32 : 1024 / D, CHANNELS = ROWS_INNER ? 32 : D, SPLIT = D / CHANNELS;   // SPLIT: blocks of the same rows
 };
-template <int D, bool QUANT, int TS, bool ROWS_INNER, int GROUPS>
-__global__ void __launch_bounds__(JoinTile<D, ROWS_INNER, GROUPS>::THREADS) attn_tree_join_tc_kernel(const __grid_constant__ TreeTcArgs f) {
-  using J = JoinTile<D, ROWS_INNER, GROUPS>;
-  constexpr int U = GROUPS == 1 ? 3 : 4;
+template <int D, bool QUANT, int TS, bool ROWS_INNER>
+__global__ void __launch_bounds__(512) attn_tree_join_tc_kernel(const __grid_constant__ TreeTcArgs f) {
+  using J = JoinTile<D, ROWS_INNER>;
+  constexpr int GROUPS = 4, U = 4;
   const TreeArgs& a = f.a;
   const int G = a.H / a.H_kv, chunks = f.rows_pad / J::ROWS, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-  const int group = threadIdx.x / J::PER, in = threadIdx.x % J::PER;
+  const int group = threadIdx.x / 128, in = threadIdx.x % 128;
   const int per = segments_of_one(f), piece = blockIdx.x / J::SPLIT, seg = piece / chunks, b = seg / per, segment = seg % per, r_first = piece % chunks * J::ROWS;
   const int c_first = blockIdx.x % J::SPLIT * J::CHANNELS;
-  __shared__ float s_acc[GROUPS - 1 ? GROUPS : 1][GROUPS - 1 ? 8 : 1][GROUPS - 1 ? J::PER : 1];
-  __shared__ float2 s_ml[GROUPS - 1 ? GROUPS : 1][GROUPS - 1 ? J::PER : 1];
+  __shared__ float s_acc[GROUPS][8][128];
+  __shared__ float2 s_ml[GROUPS][128];
   __shared__ uint32_t s_bad, s_large;
   if (threadIdx.x == 0) s_bad = s_large = 0u;
   behind_last_kernel();
-  int c0, c1;   // the shares that its first and its last tile lie in
-  const int mine = lane < a.B ? segment_tiles<TS>(f, a.pos[lane]) : 0;   // (of the first 32 sequences)
-  if (f.apart) {
-    const Apart s(f, mine);
-    const int n = __shfl_sync(0xffffffffu, s.pieces, b);
-    c0 = __shfl_sync(0xffffffffu, s.before(s.pieces * per, lane), b) + segment * n;
-    c1 = c0 + n - 1;
-  } else {
-    int n, n0, tiles;   // all tiles, those in front of this sequence, and a segment's
-    if (a.B <= 32) {
-      n = __reduce_add_sync(0xffffffffu, mine) * per;
-      n0 = __reduce_add_sync(0xffffffffu, lane < b ? mine : 0) * per;
-      tiles = __shfl_sync(0xffffffffu, mine, b);
-    } else {
-      n = tiles_up_to<TS>(f, a.B);
-      n0 = tiles_up_to<TS>(f, b);
-      tiles = segment_tiles<TS>(f, a.pos[b]);
-    }
-    const Shares shares(n, f.shares, f.least);
-    const int x0 = n0 + segment * tiles;
-    c0 = shares.of(x0);
-    c1 = shares.of(x0 + tiles - 1);
-  }
-  if (c0 == c1) return;                              // (one piece, which its block has stored)
+  const Apart shares(f, lane < a.B ? segment_tiles<TS>(f, a.pos[lane]) : 0);
+  const int n = __shfl_sync(0xffffffffu, shares.pieces, b);
+  const int c0 = __shfl_sync(0xffffffffu, shares.before(shares.pieces * per, lane), b) + segment * n, c1 = c0 + n - 1;
+  if (n == 1) return;                                // (its block has stored it)
   const int ri = ROWS_INNER ? lane : in / (D / 8), ch = c_first + (ROWS_INNER ? in / 32 : in % (D / 8)) * 8;
   const int R = a.N * G, rp = r_first + ri, r = row_of_piece(f, segment % f.row_blocks, rp);
   const bool some = r < R;
@@ -340,8 +358,7 @@ __global__ void __launch_bounds__(JoinTile<D, ROWS_INNER, GROUPS>::THREADS) attn
       float x[U][8];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int c = min(i0 + u * GROUPS, c1);
-        const size_t slot = 2 * (size_t)c + (c == c0);
+        const size_t slot = min(i0 + u * GROUPS, c1);
         ml[u] = f.part_ml[slot * f.rows_pad + rp];
         if constexpr (ROWS_INNER) {
 #pragma unroll
@@ -357,12 +374,10 @@ __global__ void __launch_bounds__(JoinTile<D, ROWS_INNER, GROUPS>::THREADS) attn
       for (int u = 0; u < U; ++u)
         if (i0 + u * GROUPS <= c1) add(ml[u].x, ml[u].y, x[u]);
     }
-  if constexpr (GROUPS > 1) {
-    if (group > 0) {
+  if (group > 0) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s_acc[group][e][in] = acc[e];
-      s_ml[group][in] = make_float2(m, l);
-    }
+    for (int e = 0; e < 8; ++e) s_acc[group][e][in] = acc[e];
+    s_ml[group][in] = make_float2(m, l);
   }
   __syncthreads();
   if (group == 0) {
@@ -392,7 +407,7 @@ __global__ void __launch_bounds__(JoinTile<D, ROWS_INNER, GROUPS>::THREADS) attn
   __syncthreads();
   const uint32_t again = s_bad | (QUANT ? ~s_large : 0u);
   if (!again) return;
-  for (int i = warp; i < J::ROWS; i += J::THREADS / 32)           // (behind the barrier: nobody else writes these channels any more)
+  for (int i = warp; i < J::ROWS; i += 16)           // (behind the barrier: nobody else writes these channels any more)
     if (again >> i & 1u) {
       const int row = row_of_piece(f, segment % f.row_blocks, r_first + i), node = quot(row, f.group);
       tree_row_again<bf16, D, QUANT>(a, b, node, segment / f.row_blocks * G + rest(row, node, f.group), c_first, J::CHANNELS);
@@ -432,7 +447,18 @@ inline TreePlan tree_plan(int B, int N, int H, int H_kv, int C, int W, int rows,
 }
 inline size_t tree_plan_bytes(const TreePlan& p, int d) {
   if (p.whole) return 0;
-  return align_up(sizeof(float2) * 2 * (size_t)p.shares * p.rows_pad, 256) + align_up(sizeof(float) * 2 * (size_t)p.shares * p.rows_pad * d, 256);
+  return align_up(sizeof(float2) * (size_t)p.shares * p.rows_pad, 256) + align_up(sizeof(float) * (size_t)p.shares * p.rows_pad * d, 256) +
+         align_up(sizeof(unsigned long long) * (size_t)p.shares, 256);
+}
+// A number that no other call of this process has, and that nothing else is likely to be: the count of calls, its bits mixed (by a
+// bijection) with those of the process's start.
+inline unsigned long long call_number() {
+  static std::atomic<unsigned long long> count{0};
+  static const unsigned long long start = (unsigned long long)std::chrono::system_clock::now().time_since_epoch().count();
+  unsigned long long x = count.fetch_add(1, std::memory_order_relaxed) * 0x9E3779B97F4A7C15ull + start;
+  x = (x ^ (x >> 31)) * 0xD6E8FEB86659FD93ull;
+  x ^= x >> 32;
+  return x ? x : 1;
 }
 inline TreeTcArgs tree_tc_args(const AttnTree& c, const TreePlan& p) {
   TreeTcArgs f{};
@@ -441,25 +467,22 @@ inline TreeTcArgs tree_tc_args(const AttnTree& c, const TreePlan& p) {
   f.row_blocks = p.row_blocks; f.rows = p.rows; f.tile_rows = p.tile_rows; f.stride = p.stride; f.rows_pad = p.rows_pad; f.whole = p.whole; f.apart = p.apart; f.node_tiles = p.node_tiles;
   f.shares = p.shares; f.least = p.least;
   f.part_ml = (float2*)c.ws;
-  f.part_o = (float*)((char*)c.ws + align_up(sizeof(float2) * 2 * (size_t)p.shares * p.rows_pad, 256));
+  f.part_o = (float*)((char*)c.ws + align_up(sizeof(float2) * (size_t)p.shares * p.rows_pad, 256));
+  f.told = (unsigned long long*)((char*)f.part_o + align_up(sizeof(float) * (size_t)p.shares * p.rows_pad * c.d, 256));
+  f.number = call_number();
   f.limit = wait_limit();
   f.dev_status = c.dev_status;
   return f;
 }
-template <int D, bool QUANT, int TS, bool ROWS_INNER, int GROUPS>
+template <int D, bool QUANT, int TS, bool ROWS_INNER>
 int launch_tree_join(const AttnTree& c, const TreeTcArgs& f) {
-  using J = JoinTile<D, ROWS_INNER, GROUPS>;
+  if (!f.apart) return LAWCAT_OK;
+  using J = JoinTile<D, ROWS_INNER>;
   const long long blocks = (long long)f.a.B * f.a.H_kv * f.row_blocks * (f.rows_pad / J::ROWS) * J::SPLIT;
   if (blocks > 0x7fffffffLL) return LAWCAT_ERR_UNSUPPORTED;
-  LAWCAT_LAUNCH("attn_tree_join_tc", c.stream,
-                launch_behind(attn_tree_join_tc_kernel<D, QUANT, TS, ROWS_INNER, GROUPS>, dim3((unsigned)blocks), dim3(J::THREADS), 0, c.stream, f));
+  LAWCAT_LAUNCH("attn_tree_join_tc", c.stream, launch_behind(attn_tree_join_tc_kernel<D, QUANT, TS, ROWS_INNER>, dim3((unsigned)blocks), dim3(512), 0, c.stream, f));
   LAWCAT_CHECK_LAUNCH();
   return LAWCAT_OK;
-}
-template <int D, bool QUANT, int TS, bool ROWS_INNER>
-int launch_tree_join(const AttnTree& c, const TreeTcArgs& f) {   // (more than four shares to a segment are many pieces)
-  if (f.shares > 4LL * f.a.B * f.a.H_kv * f.row_blocks) return launch_tree_join<D, QUANT, TS, ROWS_INNER, 4>(c, f);
-  return launch_tree_join<D, QUANT, TS, ROWS_INNER, 1>(c, f);
 }
 
 }  // namespace attn
