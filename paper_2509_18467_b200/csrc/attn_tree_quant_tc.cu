@@ -55,6 +55,39 @@ __device__ __forceinline__ float across(float (&x)[N], int lane, F op) {
   return y[0];
 }
 
+// Eight channels of a row whose segment is cut: this block's piece (maximum m, sum l, weighted values at `own`) and those of shares first to
+// last.
+template <int D>
+__device__ __forceinline__ uint4 joined(const TreeTcArgs& f, float m, float l, uint32_t own, int first, int last, int row, int ch) {
+  float acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; e += 4) {
+    const uint4 x = lds128(own + 4 * e);
+    acc[e] = __uint_as_float(x.x); acc[e + 1] = __uint_as_float(x.y); acc[e + 2] = __uint_as_float(x.z); acc[e + 3] = __uint_as_float(x.w);
+  }
+  if (l == 0.f) {   // (a piece without keys has no weights)
+    m = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+  }
+#pragma unroll 2
+  for (int i = first; i <= last; ++i) {
+    const size_t at = (size_t)i * f.rows_pad + row;
+    const float2 ml = __ldcg(f.part_ml + at);
+    const float4 y = __ldcg(reinterpret_cast<const float4*>(f.part_o + at * D + ch)), z = __ldcg(reinterpret_cast<const float4*>(f.part_o + at * D + ch + 4));
+    if (ml.y == 0.f) continue;
+    const float top = fmaxf(m, ml.x), k = ex2f(m - top), w = ex2f(ml.x - top), x[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
+    m = top;
+    l = l * k + w * ml.y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = fmaf(w, x[e], acc[e] * k);
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] *= inv;
+  return make_uint4(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]), pack_bf16(acc[4], acc[5]), pack_bf16(acc[6], acc[7]));
+}
+
 // BIAS: distance biases
 template <int D, int NCOL, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quant_tc_kernel(const __grid_constant__ TreeTcArgs f) {
@@ -102,9 +135,39 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
   const int share = share_of_block(f);
   if (tid == 0 && !f.whole && !f.apart) f.told[share] = 0ull;   // (what a call that gave up may have left)
   walk.start(f, share, pos_lane);
-  Piece w;
+  Piece w{};
   int count = 0;   // tiles so far
   bool fail = false;
+  // The piece's rows to memory (value(x): eight channels of bf16, vector x of the rows), and those computed again that are not finite somewhere,
+  // or small everywhere.
+  auto rows_out = [&](auto value) {
+    const int r0 = w.rb * NCOL;
+#pragma unroll 1
+    for (int x = tid; x < NCOL * (D / 8); x += 128) {
+      const int c = x / (D / 8), r = r0 + c, node = quot(min(r, R - 1), f.group);
+      const uint4 y = value(x);
+      if (r < R) *reinterpret_cast<uint4*>((bf16*)a.o + (((size_t)w.b * a.N + node) * a.H + w.g * G + rest(r, node, f.group)) * D + x % (D / 8) * 8) = y;
+      const uint32_t u[4] = {y.x & 0x7fff7fffu, y.y & 0x7fff7fffu, y.z & 0x7fff7fffu, y.w & 0x7fff7fffu};
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = max(top, max(u[e] >> 16, u[e] & 0xffffu));
+#pragma unroll
+      for (int m = 1; m < D / 8; m <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, m));
+      if (x % (D / 8) == 0 && r < R && s_depth[c] >= 0 && (top >= 0x7f80u || __uint_as_float(top << 16) < SMALL)) atomicOr(s_bad + c / 32, 1u << (c & 31));
+    }
+    named_bar_sync(3, 128);
+    if (s_bad[0] | s_bad[1]) {
+#pragma unroll 1
+      for (int c = warp; c < NCOL && r0 + c < R; c += 4)
+        if (s_bad[c / 32] >> (c & 31) & 1u) {
+          const int node = quot(r0 + c, f.group);
+          tree_row_again<bf16, D, true>(a, w.b, node, w.g * G + rest(r0 + c, node, f.group));
+        }
+      named_bar_sync(3, 128);
+      if (tid < 2) s_bad[tid] = 0u;
+      named_bar_sync(3, 128);
+    }
+  };
   while (walk.next(f, w)) {
     const int b = w.b, pos = w.pos, r0 = w.rb * NCOL, n = w.n;
     const Ring<128> ring = ring_of<128>(pos, a.C, a.W);
@@ -396,107 +459,52 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
     if (!fail) fail = !wait_bar(bar_o, (count - 1) & 1, s_abort, f.limit);
     if (named_bar_or(3, 128, fail)) break;
     tc_fence_after_sync();
-    const bool join = is_joined_here(f, w), direct = is_whole(w) || join;
-    const int others = join ? w.last - share : 0;
+    const bool whole = is_whole(w), join = is_joined_here(f, w);
     float sum = 0.f;
     if (tid < NCOL) {
       sum = (s_red[tid] + s_red[NCOL + tid]) + (s_red[2 * NCOL + tid] + s_red[3 * NCOL + tid]);
       if (s_depth[tid] < 0) sum = 0.f;
       const float m = -s_ref[tid / 2 * 4 + 2 + (tid & 1)];
-      if (!direct && r0 + tid < R) f.part_ml[(size_t)share * f.rows_pad + tid] = make_float2(sum == 0.f ? -INFINITY : m, sum);
+      if (!whole && !join && r0 + tid < R) f.part_ml[(size_t)share * f.rows_pad + tid] = make_float2(sum == 0.f ? -INFINITY : m, sum);
     }
     float o[NCOL];
 #pragma unroll
     for (int c = 0; c < NCOL; c += 16) tmem_ld16(o_col + lanes + c, o + c);
     tmem_wait_ld();
     const int ch = (tid & ~7) + ((tid & 7) >> 1) + 4 * (tid & 1);   // the lane's channel
-    if (join) {
-      // the other pieces of the segment: their maxima first, then their sums at the common one
-      bool told = true;
-      if (tid == 0)
-        for (int i = 0; i < others && told; ++i) told = wait_told(f.told + share + 1 + i, f.number, s_abort, item_limit(f.limit, w.tiles));
-      fail = named_bar_or(3, 128, !told);
-      if (fail) break;
-      float m = -INFINITY, top = -INFINITY;
-      const bool row = tid < NCOL && r0 + tid < R;
-      auto other = [&](int i) { return row ? __ldcg(f.part_ml + (size_t)(share + 1 + i) * f.rows_pad + tid) : make_float2(-INFINITY, 0.f); };
-      if (tid < NCOL) {
-        m = top = sum == 0.f ? -INFINITY : -s_ref[tid / 2 * 4 + 2 + (tid & 1)];
-        for (int i = 0; i < others; ++i) {
-          const float2 x = other(i);
-          if (x.y != 0.f) top = fmaxf(top, x.x);
-        }
-        s_factor[tid] = m == -INFINITY ? 0.f : ex2f(m - top);
-        sum *= s_factor[tid];
-      }
-      named_bar_sync(3, 128);
-#pragma unroll
-      for (int c = 0; c < NCOL; ++c) o[c] = s_factor[c] == 0.f ? 0.f : o[c] * s_factor[c];
-#pragma unroll 1
-      for (int i = 0; i < others; ++i) {
-        named_bar_sync(3, 128);   // (the factors have been read)
-        if (tid < NCOL) {
-          const float2 x = other(i);
-          s_factor[tid] = x.y == 0.f ? 0.f : ex2f(x.x - top) * KV_FACTOR;
-          sum += x.y == 0.f ? 0.f : x.y * ex2f(x.x - top);
-        }
-        named_bar_sync(3, 128);
-        const float* const from = f.part_o + (size_t)(share + 1 + i) * f.rows_pad * D + ch;
-        if (tid < D)
-#pragma unroll
-          for (int c = 0; c < NCOL; c += 8) {
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = r0 + c + e < R ? __ldcg(from + (c + e) * D) : 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[c + e] += s_factor[c + e] == 0.f ? 0.f : s_factor[c + e] * x[e];
-          }
-      }
-      if (tid < NCOL && s_depth[tid] < 0) sum = 0.f;
-    }
-    if (tid < NCOL) s_sum[tid] = direct ? sum == 0.f ? 0.f : 1.f / (sum * KV_FACTOR) : 1.f / KV_FACTOR;
+    if (tid < NCOL) s_sum[tid] = whole ? sum == 0.f ? 0.f : 1.f / (sum * KV_FACTOR) : 1.f / KV_FACTOR;
     named_bar_sync(3, 128);
-    if (!direct) {
-      float* const dst = f.part_o + (size_t)share * f.rows_pad * D + ch;
+    if (!whole) {
+      float* const dst = (join ? reinterpret_cast<float*>(smem) : f.part_o + (size_t)share * f.rows_pad * D) + ch;   // [NCOL][D] over V, or scratch
 #pragma unroll
       for (int c = 0; c < NCOL; ++c)
         if (r0 + c < R && tid < D) dst[c * D] = o[c] * s_sum[c];
       tc_fence_before_sync();
       named_bar_sync(3, 128);
-      if (!f.apart && tid == 0) tell(f.told + share, f.number);
+      if (!join && !f.apart && tid == 0) tell(f.told + share, f.number);
     } else {
-      bf16* const s_out = reinterpret_cast<bf16*>(smem);   // [NCOL][D] over V
+      bf16* const s_out = reinterpret_cast<bf16*>(smem);   // [NCOL][D]
 #pragma unroll
       for (int c = 0; c < NCOL; ++c)
         if (tid < D) s_out[c * D + ch] = __float2bfloat16_rn(s_sum[c] == 0.f ? 0.f : o[c] * s_sum[c]);
       tc_fence_before_sync();
       named_bar_sync(3, 128);
-#pragma unroll 1
-      for (int x = tid; x < NCOL * (D / 8); x += 128) {
-        const int c = x / (D / 8), r = r0 + c, node = quot(min(r, R - 1), f.group);
-        const uint4 y = lds128(sb + x * 16);
-        if (r < R) *reinterpret_cast<uint4*>((bf16*)a.o + (((size_t)b * a.N + node) * a.H + w.g * G + rest(r, node, f.group)) * D + x % (D / 8) * 8) = y;
-        // rows to be computed again: not finite somewhere, or small everywhere
-        const uint32_t u[4] = {y.x & 0x7fff7fffu, y.y & 0x7fff7fffu, y.z & 0x7fff7fffu, y.w & 0x7fff7fffu};
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top = max(top, max(u[e] >> 16, u[e] & 0xffffu));
-#pragma unroll
-        for (int m = 1; m < D / 8; m <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, m));
-        if (x % (D / 8) == 0 && r < R && s_depth[c] >= 0 && (top >= 0x7f80u || __uint_as_float(top << 16) < SMALL)) atomicOr(s_bad + c / 32, 1u << (c & 31));
-      }
+      rows_out([&](int x) { return lds128(sb + x * 16); });
+    }
+  }
+  // a segment that others go on with is the block's last: its pieces meet here, where the tiles' registers are free
+  if (!named_bar_or(3, 128, *s_abort != 0) && is_joined_here(f, w)) {
+    bool told = true;
+    if (tid == 0)
+      for (int i = share + 1; i <= w.last && told; ++i) told = wait_told(f.told + i, f.number, s_abort, item_limit(f.limit, w.tiles));
+    if (!named_bar_or(3, 128, !told)) {
+      const int r0 = w.rb * NCOL;
+      if (tid < NCOL) s_sum[tid] = s_depth[tid] < 0 ? 0.f : (s_red[tid] + s_red[NCOL + tid]) + (s_red[2 * NCOL + tid] + s_red[3 * NCOL + tid]);
       named_bar_sync(3, 128);
-      if (s_bad[0] | s_bad[1]) {
-#pragma unroll 1
-        for (int c = warp; c < NCOL && r0 + c < R; c += 4)
-          if (s_bad[c / 32] >> (c & 31) & 1u) {
-            const int node = quot(r0 + c, f.group);
-            tree_row_again<bf16, D, true>(a, b, node, w.g * G + rest(r0 + c, node, f.group));
-          }
-        named_bar_sync(3, 128);
-        if (tid < 2) s_bad[tid] = 0u;
-        named_bar_sync(3, 128);
-      }
+      rows_out([&](int x) {
+        const int c = x / (D / 8);
+        return r0 + c < R ? joined<D>(f, -s_ref[c / 2 * 4 + 2 + (c & 1)], s_sum[c], sb + x * 32, share + 1, w.last, c, x % (D / 8) * 8) : make_uint4(0, 0, 0, 0);
+      });
     }
   }
   __syncthreads();
