@@ -506,15 +506,14 @@ def rope_frequencies(rot, base=10000.0, scaling="plain", factor=1.0, original=0.
     return freq
 
 
-def _rope(name, p, freq, q, k, positions, start, parent, q_out, k_out, stream):
+def _rope(name, p, freq, q, k, positions, start, parent, q_out, k_out, names, stream):
     B, T, dt, check = p.B, p.T, p.dtype, _checked()
     if len(freq) != p.rot // 2:
         raise ValueError(f"freq holds {len(freq)} angles, rot = {p.rot} takes {p.rot // 2}")
-    if not isinstance(freq, ctypes.Array):
+    if getattr(freq, "_type_", None) is not ctypes.c_double:
         freq = (ctypes.c_double * len(freq))(*[float(x) for x in freq])
-    for x, out, heads, what in ((q, q_out, p.H, "q"), (k, k_out, p.H_kv, "k")):
+    for x, heads, what in zip((q, k, q_out, k_out), (p.H, p.H_kv) * 2, names):
         check(what, x, dt, B, T, heads, p.d)
-        check(what + "_out", out, dt, B, T, heads, p.d)
     check("positions", positions, I32, B, T)
     check("start", start, I32, B)
     check("parent", parent, I32, B, T)
@@ -529,12 +528,12 @@ def _rope(name, p, freq, q, k, positions, start, parent, q_out, k_out, stream):
 def lawcat_rope_fwd(p: RopeParams, freq, q, k=None, positions=None, start=None, parent=None, q_out=None, k_out=None, stream=None):
     """Rotary positions: positions [B,T], or start [B] (plus t, or plus the depth of drafted node t given by parent [B,T]). The outputs may
     be q and k themselves. Returns (q, k) turned; either may be left out."""
-    return _rope("lawcat_rope_fwd", p, freq, q, k, positions, start, parent, q_out, k_out, stream)
+    return _rope("lawcat_rope_fwd", p, freq, q, k, positions, start, parent, q_out, k_out, ("q", "k", "q_out", "k_out"), stream)
 
 
 def lawcat_rope_bwd(p: RopeParams, freq, dq_out, dk_out=None, positions=None, start=None, parent=None, dq=None, dk=None, stream=None):
     """The gradients of the turned q and k -> those of q and k."""
-    return _rope("lawcat_rope_bwd", p, freq, dq_out, dk_out, positions, start, parent, dq, dk, stream)
+    return _rope("lawcat_rope_bwd", p, freq, dq_out, dk_out, positions, start, parent, dq, dk, ("dq_out", "dk_out", "dq", "dk"), stream)
 
 
 def _check_tree(p, q_t, k_t, v_t, pos, parent, slopes, o_t):
