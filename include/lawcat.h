@@ -481,8 +481,11 @@ int lawcat_rope_bwd(const lawcat_rope_params* p, const double* freq, const void*
  * A node of depth e (0 for parent -1) stands at position pos + e and sees, as the same tokens fed to lawcat_attn_decode one by one would,
  * the cached tokens and the nodes of its path, itself included, that lie less than W behind it: W = p->window, or C without one.
  * Distances (slopes) are those of the positions. Slots that hold no token yet may hold anything.
- * Rounding as in lawcat_attn_fwd; bf16 with d = 64 or 128 (and exact = 0) runs on the tensor cores. A key or value row that a node does not
- * see does not reach its result, not even as a NaN (a row that comes out not finite is computed again, which takes its time).
+ * Rounding as in lawcat_attn_fwd; bf16 with d = 64 or 128, exact = 0 and at most 128 query heads to a key-value head runs on the tensor
+ * cores. A key or value row that a node does not see does not reach its result, not even as a NaN (a row that comes out not finite is
+ * computed again, which takes its time).
+ *   ws: may hold anything; two calls that may overlap on the GPU need one each. Blocks that share a sequence's keys wait for one another's
+ *     sums: a wait that runs out ends the call, dev_status becomes LAWCAT_ERR_TIMEOUT and o_t is not to be used.
  */
 enum { LAWCAT_OP_ATTN_TREE = 10 }; /* for lawcat_attn_workspace_bytes; both caches share it */
 int lawcat_attn_tree(const lawcat_attn_params* p, const void* q_t, const void* k_t, const void* v_t, const void* K, const void* V,
@@ -490,7 +493,8 @@ int lawcat_attn_tree(const lawcat_attn_params* p, const void* q_t, const void* k
                      int* dev_status);
 
 /*
- * lawcat_attn_tree over a cache in 4 bits (read only); a node's key and value are what the cache would hold of k_t, v_t.
+ * lawcat_attn_tree over a cache in 4 bits (read only); a node's key and value are what the cache would hold of k_t, v_t. On the tensor cores
+ * keys, values and weights are rounded to fp16 as operands; weights are relative to a score of the row that is at most 2^8 below its largest.
  */
 int lawcat_attn_tree_quant(const lawcat_attn_params* p, const void* q_t, const void* k_t, const void* v_t, const void* kq, const void* kp,
                            const void* vq, const void* vp, const int32_t* pos, const int32_t* parent, const float* slopes, void* o_t, void* ws,
