@@ -27,7 +27,8 @@ struct ColLay {
   static constexpr uint32_t OFF_ON = OFF_COL + 8 * NCOL * 4, OFF_RED = OFF_ON + NCOL * (TREE_MAX / 32) * 4, OFF_BAR = OFF_RED + 6 * NCOL * 4, BYTES = OFF_BAR + 64;
   static constexpr uint32_t OFF_CODES = 0, OFF_PAIRS = 128 * WPR * 4, STAGED = OFF_PAIRS + 128 * NG * 4;   // a node tile's keys as the cache would hold them, then its values
   static constexpr uint32_t K_COLS = D / 2, COLS = K_COLS + 2 * NCOL <= 128 ? 128 : 256;
-  static constexpr int RESIDENT = COLS != 128 ? 2 : NCOL == 32 ? 3 : 4;
+  // blocks of an SM: as many as tensor memory holds (NCOL = 32, 64 sequences of 12000 slots, d = 128: 342 us; three with more registers 379)
+  static constexpr int RESIDENT = COLS == 128 ? 4 : 2;
   static_assert(K_COLS + 2 * NCOL <= COLS && OFF_P % 1024 == 0 && OFF_BAR % 16 == 0 && sizeof(Paths) <= OFF_Q && 2 * STAGED <= OFF_Q && RESIDENT * (BYTES + 1024) <= 233472, "layout");
 };
 
