@@ -10,6 +10,9 @@
 // The keys are walked from the newest to the oldest: the nodes' own first, quantized as the cache would hold them, then the cached ones.
 // Slots that no row sees, and nodes that are not there, are zeros, whatever they hold.
 //
+// Bound by instruction issue and the waits between a tile's phases: 64 sequences of 16384 slots, 32 rows, d = 128: 360 us (HBM alone 155), issue 53 %,
+// integer pipe 32 %, tensor pipe 12 %; of a warp's 1470 instructions a tile half unpack codes. One sequence of 32768 slots, 64 rows: 46 us.
+//
 // Rounding: keys, values and weights to fp16 as operands, o once; all else fp32.
 #include <algorithm>
 
@@ -539,7 +542,8 @@ static int tree_quant_tc(const AttnTree& c) {
 
 }  // namespace attn
 
-// Columns for the rows of a group: 16, 32 or 64; more go to the rows' kernel (0).
+// Columns for the rows of a group: 16, 32 or 64; more go to the rows' kernel (0). (Cycles of an SM for 64 slots at d = 128: 775, 815 and 1520 for
+// 16, 32 and 64 columns, 2200 for the rows' kernel up to 128 rows.)
 static int columns(const AttnTree& c) {
   const int R = c.a.N * (c.a.H / c.a.H_kv);
   return R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : 0;

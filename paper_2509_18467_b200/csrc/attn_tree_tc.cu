@@ -5,17 +5,21 @@
 //   two warpgroups    softmax, one thread per row: S from tensor memory, masks, running maximum and sum in registers, P = exp2(x - m) over S;
 //                     then the segment's outputs
 //   copy warp         queries, K and V tiles (through a ring of stages) by TMA, on into the next segment while this one ends;
-//                     over 4 bits seven warps in its place, which unpack codes into the stages (a warp at a time 32 groups of 32 channels), and the queries come by the softmax warps
+//                     over 4 bits seven warps in its place, which unpack codes into the stages (a warp at a time 32 groups of 32 channels), and
+//                     the queries come by the softmax warps
 //   product warp      S = Q K^T (shared memory), O += P V (P from tensor memory); fp32 accumulation
 // A tile of rows is as many whole nodes as 128 rows hold. Of two tiles each warpgroup has one, and both meet every key; of one, both have its
-// rows and take the key tiles in turn, each with sums of its own (in the same lanes of tensor memory) that meet at the segment's end. S has two places per warpgroup; O is rescaled only when a maximum grew by
-// more than 2^8.
+// rows and take the key tiles in turn, each with sums of its own (in the same lanes of tensor memory) that meet at the segment's end. S has two
+// places per warpgroup; O is rescaled only when a maximum grew by more than 2^8.
+//
+// Up to 128 rows HBM bounds it (16 sequences of 8192 slots, 32/8 heads of 128, 32 nodes: 84.5 us, HBM alone 63; 1300 cycles of an SM a tile of
+// keys), with 256 the softmax's chain of product, maximum, weights, product (1990 cycles, 1590 at d = 64).
 //
 // The keys are walked from the newest to the oldest: the nodes' own rows first (the values of nodes that are not there are set to zero), then
 // the cached ones, whose tiles end where the newest slot, or slot C - 1, does. What a tile holds below its oldest key are slots in front of
 // slot 0, which read as zeros, or older tokens: never a slot without a token. So a row sees a tile's columns from one limit on.
 //
-// Rounding: weights to bf16 as an operand, o once; all else fp32.
+// Rounding: weights to bf16 as an operand (over 4 bits they, keys, values and queries to fp16), o once; all else fp32.
 #include <algorithm>
 
 #include "attn_tree_tc.cuh"
