@@ -7,7 +7,8 @@
 // their blocks' shares, and done long before as a rule (16 sequences of 6000 slots, 32 nodes: a second kernel that joined took 13 us of
 // 92). Shares are dealt out from the last to the first, so that a block waits only for blocks that started before it.
 // Where there are four blocks or more to a segment, no share reaches over a segment's end (a block's second segment costs it 4 us), and the
-// pieces, which end together, meet in a second kernel. Where the capacity allows a segment a few tiles only, shares are whole segments.
+// pieces, which end together, meet in a second kernel. Where segments are too short to be worth a cut (CUT_COST), by the capacity or by the
+// lengths that are found, shares are whole segments.
 //
 // That a block's sums are there is told by a number that is the call's own, in scratch that may hold anything: 64 bits that no other call
 // has; the block that waits for it puts a zero in its place, so that a replayed call finds none.
@@ -138,13 +139,12 @@ template <int TS>
 __device__ __forceinline__ int segment_tiles(const TreeTcArgs& f, int pos) { return f.node_tiles + ring_of<TS>(pos, f.a.C, f.a.W).tiles; }
 __device__ __forceinline__ int segments_of_one(const TreeTcArgs& f) { return f.a.H_kv * f.row_blocks; }
 
-// all tiles of the first `end` sequences; by a whole warp
+// What it costs to cut segments, in tiles of a block: a second piece's set-up, its sums to scratch, the join. From times of whole and cut
+// segments at several lengths, in us: 8 sequences, 64 nodes, heads of 64, 500 / 1000 / 2000 tokens: 16.8 and 21.5 / 23.5 and 26.5 / 38 and 32.6; 16
+// sequences, 32 nodes, heads of 128, 6000 tokens: 76 and 82; over 4 bits 64 sequences, 8 nodes, 500 / 2000 / 8000 tokens: 39 and 49 / 88 and 98 /
+// 258 and 246.
 template <int TS>
-__device__ __forceinline__ int tiles_up_to(const TreeTcArgs& f, int end) {
-  int n = 0;
-  for (int b = threadIdx.x & 31; b < end; b += 32) n += segment_tiles<TS>(f, f.a.pos[b]);
-  return __reduce_add_sync(0xffffffffu, n) * segments_of_one(f);
-}
+constexpr int CUT_COST = TS == 64 ? 14 : 6;
 // Shares of n tiles: `more` of one + 1 tiles, then those of one.
 struct Shares {
   int count, one, more;
@@ -192,6 +192,7 @@ struct Piece {
 // A block's walk over its share.
 template <int TS>
 struct Walk {
+  bool whole; // shares are whole segments, by the capacity or by the lengths
   int left;   // tiles (whole: segments) left
   int b, segment, t, tiles, pos;
   int at;     // of all tiles
@@ -201,15 +202,7 @@ struct Walk {
   __device__ __forceinline__ void start(const TreeTcArgs& f, int c, int pos_lane) {
     const int per = segments_of_one(f), lane = threadIdx.x & 31;
     b = segment = t = 0;
-    if (f.whole) {
-      const Shares s(f.a.B * per, f.shares, 1);
-      const int x = s.begin(c);
-      left = s.begin(c + 1) - x;
-      b = x / per;
-      segment = x - b * per;
-      load(f);
-      return;
-    }
+    whole = f.whole;
     const int first = lane < f.a.B ? segment_tiles<TS>(f, pos_lane) : 0;   // (of the first 32 sequences)
     if (f.apart) {
       const Apart s(f, first);
@@ -227,8 +220,29 @@ struct Walk {
       }
       return;
     }
-    int n = __reduce_add_sync(0xffffffffu, first) * per;
-    if (f.a.B > 32) n = tiles_up_to<TS>(f, f.a.B);
+    int n = first;
+    if (!whole) {
+      int most = first;
+      for (int i = 32 + lane; i < f.a.B; i += 32) {
+        const int x = segment_tiles<TS>(f, f.a.pos[i]);
+        n += x;
+        most = max(most, x);
+      }
+      n = __reduce_add_sync(0xffffffffu, n) * per;
+      // whole segments, where the blocks with most of them (each the longest) are not that far behind the mean (with tiles of 64 they run a
+      // sixteenth faster by themselves: HBM is what they share)
+      const int longest = (int)__reduce_max_sync(0xffffffffu, most) * ((f.a.B * per + f.shares - 1) / f.shares);
+      whole = longest - (TS == 64 ? longest / 16 : 0) <= n / f.shares + CUT_COST<TS>;
+    }
+    if (whole) {
+      const Shares s(f.a.B * per, f.shares, 1);
+      const int x = s.begin(c);
+      left = s.begin(c + 1) - x;
+      b = x / per;
+      segment = x - b * per;
+      load(f);
+      return;
+    }
     shares = Shares(n, f.shares, f.least);
     int x = at = shares.begin(c);
     left = shares.begin(c + 1) - x;
@@ -267,10 +281,10 @@ struct Walk {
     p.pos = pos;
     p.t0 = t;
     p.tiles = tiles;
-    p.n = f.whole ? tiles : min(tiles - t, left);
-    p.last = f.whole || f.apart ? 0 : shares.of(at - t + tiles - 1);
+    p.n = whole ? tiles : min(tiles - t, left);
+    p.last = whole || f.apart ? 0 : shares.of(at - t + tiles - 1);
     at += p.n;
-    left -= f.whole ? 1 : p.n;
+    left -= whole ? 1 : p.n;
     t += p.n;
     if (t == tiles) {
       t = 0;
