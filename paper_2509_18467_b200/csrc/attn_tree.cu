@@ -4,7 +4,7 @@
 // widens to fp32 in shared memory, and keeps the running maximum and sum of each row (four rows to a warp: a key or value that is read from
 // shared memory serves four). The keys are cut into as many parts as fill the SMs, by the capacity alone, so that a captured step may be
 // replayed at every length; a second kernel joins them. For small calls latency is all of it (2 sequences of 500 tokens, 13 nodes, 4 heads of 64 in
-// fp32: 12 us, both launches).
+// fp32: 11 us, both launches).
 //
 // Rows of one tile see different keys of it, and a weight of zero times a value that is not finite is a NaN: a row that comes out not finite
 // is computed again by itself, from the keys that it sees and nothing else.
@@ -45,9 +45,13 @@ __global__ void __launch_bounds__(TREE_THREADS) attn_tree_kernel(const __grid_co
   const int nodes = pos < 0 ? 0 : min(a.N, (r0 + TREE_ROWS - 1) / G + 1), cached = cached_keys(pos, a.W);
   const int node_tiles = (nodes + TK - 1) / TK, tiles = node_tiles + (cached + TK - 1) / TK;
   const int per = (tiles + a.parts - 1) / a.parts, i0 = min(tiles, part * per), i1 = min(tiles, i0 + per);
-  for (int i = tid; i < TREE_ROWS * D; i += TREE_THREADS) {
-    const int r = r0 + i / D;
-    Q[i / D * LD + i % D] = r < R ? ldf<T>((const T*)a.q + row_at(r) * D + i % D) : 0.f;
+#pragma unroll 2
+  for (int i = tid; i < TREE_ROWS * V8; i += TREE_THREADS) {
+    const int r = i / V8, c0 = i % V8 * 8;
+    float x[8] = {};
+    if (r0 + r < R) load8((const T*)a.q + row_at(r0 + r) * D + c0, x);
+#pragma unroll
+    for (int j = 0; j < 8; j += 4) *reinterpret_cast<float4*>(Q + r * LD + c0 + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
   }
   int depth[RW];
   float slope[RW], m[RW], l[RW], acc[RW][NC];
@@ -63,6 +67,7 @@ __global__ void __launch_bounds__(TREE_THREADS) attn_tree_kernel(const __grid_co
     for (int c = 0; c < NC; ++c) acc[j][c] = 0.f;
   }
   const int ps = pos < 0 ? 0 : pos % a.C;
+  const bool none = r0 + warp * RW >= R;   // (a warp without rows leaves shared memory to the others)
 
   for (int t = i0; t < i1; ++t) {
     const bool fresh = t < node_tiles;
@@ -103,6 +108,7 @@ __global__ void __launch_bounds__(TREE_THREADS) attn_tree_kernel(const __grid_co
       }
     }
     __syncthreads();
+    if (none) continue;
     float s[RW][2] = {};
     const float* const Qw = Q + warp * RW * LD;
 #pragma unroll 4
@@ -245,11 +251,12 @@ __global__ void __launch_bounds__(32 * W) attn_tree_join_kernel(const __grid_con
   if (__syncthreads_or(!fine) && warp == 0) tree_row_again<T, D, QUANT>(a, (int)(row / ((size_t)a.N * a.H)), (int)(row / a.H % a.N), (int)(row % a.H));
 }
 
-// Parts of the keys: as many as give each SM two blocks, and no more than there are tiles.
+// Parts of the keys: as many as give each SM two blocks, and no more than there are tiles (one sequence, 1468 tokens, 1 node,
+// 4 heads of 128 in fp32: 20.4 us with one part less, whose blocks have two tiles, and no warp idle; 11.4).
 static int tree_parts(const AttnTree& c) {
   const attn::TreeArgs& a = c.a;
   const long long rows = (long long)a.N * (a.H / a.H_kv), n = (long long)a.B * a.H_kv * ((rows + TREE_ROWS - 1) / TREE_ROWS);
-  const int most = std::min(a.W, a.C) / TREE_KEYS + 1;
+  const int most = (a.N + TREE_KEYS - 1) / TREE_KEYS + (std::min(a.W, a.C) - 1 + TREE_KEYS - 1) / TREE_KEYS;
   const long long want = (2LL * sm_count() + n - 1) / (n > 0 ? n : 1);
   return (int)(want < 1 ? 1 : want < most ? want : most);
 }
