@@ -483,7 +483,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
               load8((const bf16*)(v ? a.v_t : a.k_t) + (((size_t)w.b * a.N + min(k, a.N - 1)) * a.H_kv + w.g) * D + j * 8, h);
               quantize8<D, true>(h, j * 8, nullptr, nullptr, false, 0xffffffffu);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) h[i] = k < a.N ? h[i] * KV_FACTOR : 0.f;
+              for (int i = 0; i < 8; ++i) h[i] = k < a.N ? held(h[i] * KV_FACTOR) : 0.f;
               sts128(st + (v ? L::KT : 0u) + (uint32_t)(j >> 3) * 8192 + sw128(r, j & 7), halves_in_order(h));
             }
           } else {

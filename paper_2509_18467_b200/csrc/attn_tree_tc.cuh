@@ -21,12 +21,15 @@ namespace lawcat {
 namespace attn {
 
 // Over 4 bits all operands are fp16: a code becomes 1024 + code by an OR into the mantissa, less 1024, times scale, plus minimum (both times
-// 16), one rounding of 2^-11; queries are scaled by a power of two per row. Values beyond 4094 leave fp16's range, and outputs below 2^-18 feel
-// the smallest numbers that it holds: such rows, like all that come out not finite, are computed again on the CUDA cores. Channels of eight
-// are held in the order 0 4 1 5 2 6 3 7, in which a word of codes unpacks two at a time.
+// 16), one rounding of 2^-11; queries are scaled by a power of two per row. Values beyond 4094 leave fp16's range: a group that holds one is
+// NaN in the operand, so that every row that sees its slot comes out not finite (an infinite key would be a score of -inf, a slot that is not
+// seen, or with a cap a finite one). Such rows, and those whose outputs lie below 2^-18 and feel the smallest numbers that fp16 holds, are
+// computed again on the CUDA cores. Channels of eight are held in the order 0 4 1 5 2 6 3 7, in which a word of codes unpacks two at a time.
 constexpr float KV_FACTOR = 16.f;
 constexpr float SMALL = 1.f / (1 << 18);   // (the least difference of fp16 numbers, 2^-24 / 16, is 2^-10 of it)
 
+// a value (times 16) that fp16 holds, or NaN
+__device__ __forceinline__ float held(float x) { return fabsf(x) <= 65504.f ? x : NAN; }
 // eight channels as halves in that order
 __device__ __forceinline__ uint4 halves_in_order(const float (&x)[8]) {
   return make_uint4(pack_f16(x[0], x[4]), pack_f16(x[1], x[5]), pack_f16(x[2], x[6]), pack_f16(x[3], x[7]));
@@ -56,8 +59,9 @@ struct GroupScale {
 };
 __device__ __forceinline__ GroupScale group_scale(uint32_t pair) {   // (scale, minimum) in bf16
   const float s = bf16_lo(pair) * KV_FACTOR, l = bf16_hi(pair) * KV_FACTOR;
-  const __half2 x = __floats2half2_rn(s, s * 0.0625f), y = __floats2half2_rn(l, l);
-  return GroupScale{__low2half2(x), __high2half2(x), y};
+  const __half2 x = __floats2half2_rn(s, s * 0.0625f), y = __floats2half2_rn(l, l), s1 = __low2half2(x);
+  const __half2 top = __hfma2(s1, __float2half2_rn(15.f), y);                                  // (not finite where a value may be)
+  return GroupScale{s1, __high2half2(x), __hfma2(top, __float2half2_rn(0.f), y)};
 }
 // (w & mask) | with, in one instruction (two constants would be two)
 __device__ __forceinline__ uint32_t mask_or(uint32_t w, uint32_t mask, uint32_t with) {

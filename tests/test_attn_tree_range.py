@@ -1,0 +1,84 @@
+"""Attention of drafted tokens over a 4-bit cache whose keys and values lie outside what the tensor cores' fp16 operands hold, against 64 bits.
+
+Keys and values are held times 16 in fp16. A group of 32 channels (minimum m, scale s) that holds values beyond 65504 / 16 does not fit: rows that
+see such a slot are computed in fp32, and so are their bounds here (no operand is rounded). The others round keys, values and weights by 2^-11 each.
+"""
+import pytest
+import torch
+
+from attn_reference import U16, check, quantized
+from paper_2509_18467_b200 import api
+from test_attn import draw
+from test_attn_decode import rows_of
+from test_attn_tree import some_tree
+from tree_reference import U11, sees, tree_attention
+
+pytestmark = pytest.mark.gpu
+
+FITS = 65504.0 / 16
+MIN_P = 2.0 ** -25
+# lengths that are whole segments, that are cut into pieces which the first one's block joins, and that a second kernel joins
+LENGTHS = {"whole": ([300, 11, 0], 400), "cut": ([1500] * 24, 1600), "few": ([3000], 4000)}
+
+
+def groups(x):
+    """Scale and minimum of each group of the rows x [n, H_kv, d] as the cache holds them."""
+    _, scale, low, _ = quantized(x)
+    return scale, low
+
+
+def cached_groups(cache, which, b, slots):
+    pr = cache[which][b][:, slots].double().transpose(0, 1)
+    return pr[..., 0], pr[..., 1]
+
+
+def too_wide(scale, low):
+    """[n, H_kv]: rows with a group that fp16 does not hold."""
+    return ((low.abs() > FITS) | ((low + 15 * scale).abs() > FITS)).any(-1)
+
+
+def verify(q, k, v, K, V, pos, parents, cap=0.0, scale=None, slopes=None):
+    """One call over the quantized K, V [B, C, H_kv, d]; every row within its bound."""
+    B, N, H, d = q.shape
+    C, H_kv = K.shape[1], K.shape[2]
+    p = api.attn_params(B, N, H, H_kv, d, T_k=C, cap=cap, scale=scale)
+    cache = api.quant_cache(p)
+    api.lawcat_cache_quantize(api.attn_params(B, C, H, H_kv, d, T_k=C), K, V, torch.zeros(B, dtype=torch.int32, device="cuda"), *cache)
+    at = torch.tensor(pos, dtype=torch.int32, device="cuda")
+    up = torch.tensor(parents, dtype=torch.int32, device="cuda")
+    o = api.lawcat_attn_tree_quant(p, q, k, v, *cache, at, parent=up, slopes=slopes)
+    s = float(torch.tensor(d ** -0.5 if scale is None else scale))
+    for b, x in enumerate(pos):
+        cached, see, dist = sees(parents[b], x, C, 0)
+        slots = torch.tensor(cached, dtype=torch.long, device="cuda") % C
+        Kd, Vd = rows_of(cache, b, slots)
+        keys, values = torch.cat([Kd, quantized(k[b])[3]]), torch.cat([Vd, quantized(v[b])[3]])
+        wide = torch.cat([too_wide(*cached_groups(cache, 1, b, slots)), too_wide(*groups(k[b]))])          # [n, H_kv]
+        exact = (see.to("cuda")[:, :, None] & wide[None]).any(1).repeat_interleave(H // H_kv, 1)[..., None]  # [N, H, 1]
+        want, fine = tree_attention(q[b], keys, values, see, dist, s, cap, slopes)
+        _, coarse = tree_attention(q[b], keys, values, see, dist, s, cap, slopes, eps_p=U11, eps_k=U11, eps_v=U11, min_p=MIN_P)
+        check(o[b], want, torch.where(exact, fine, coarse), U16, f"o of sequence {b} at {x}")
+    return o
+
+
+@pytest.mark.parametrize("lengths", list(LENGTHS))
+@pytest.mark.parametrize("N,d", [(5, 64), (5, 128), (40, 64), (40, 128)])
+@pytest.mark.parametrize("where", ["some", "all", "nodes"])
+@pytest.mark.parametrize("size", [4000.0, 5000.0, 60000.0])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_one_large_channel_of_the_keys(cap, size, where, N, d, lengths):
+    """A channel of some cached keys, of all of them, or of the nodes' alone is +-size, and the queries' +-0.001: ordinary scores."""
+    pos, C = LENGTHS[lengths]
+    B, H, H_kv, c = len(pos), 8, 2, 5
+    q, k, v = draw((B, N, H, d), N, "bf16", 1.5), draw((B, N, H_kv, d), N + 1, "bf16"), draw((B, N, H_kv, d), N + 2, "bf16")
+    K, V = draw((B, C, H_kv, d), N + 3, "bf16"), draw((B, C, H_kv, d), N + 4, "bf16")
+    sign = 1.0 - 2.0 * ((torch.arange(N)[:, None] + torch.arange(H)) % 2)
+    q[..., c] = (1e-3 * sign).to(q)
+    large = torch.tensor([size, -size]).to(K)
+    if where == "some":
+        K[:, ::7, :, c] = large
+    elif where == "all":
+        K[..., c] = large
+    else:
+        k[..., c] = large
+    verify(q, k, v, K, V, pos, [some_tree(N, b) for b in range(B)], cap)
