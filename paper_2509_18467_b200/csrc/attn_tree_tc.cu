@@ -63,7 +63,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 
   if (tid == 0) {
     for (int i = 0; i < ST; ++i) {
-      mbar_init(bar(L::B_FULL + i), QUANT ? L::ITEMS : 1);
+      mbar_init(bar(L::B_FULL + i), L::LOADERS);
       mbar_init(bar(L::B_EMPTY + i), 1);
     }
     for (int i = 0; i < 4; ++i) {
@@ -420,11 +420,11 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   } else if (warp != 9) {
     // ------------------------------------------------------------------------------------------------ copies
     if constexpr (QUANT) {
-      // Parts of tiles, taken by the warps in turn: the keys and the values of 2 x 32 / (D / 32) slots, so that one fence (some 700 cycles of a
+      // Parts of tiles, taken up by the warps in turn: the keys and the values of 2 x 32 / (D / 32) slots, so that one fence (some 700 cycles of a
       // warp's time) does for four stores of 32 groups. Zeros where no row may see a slot.
       constexpr int NG = D / 32, SLOTS = 32 / NG, AHEAD = 6;   // AHEAD: tiles towards L2
       const int me = warp == 8 ? 0 : warp - 9, slot = lane / NG, grp = lane % NG;
-      int tile = 0, clear = 0;   // tiles of the pieces so far; those whose stages are known to be free
+      int tile = 0;   // tiles of the pieces so far
       bool ok = true;
       while (ok && walk.next(f, w)) {
         const Ring<64> ring = ring_of<64>(w.pos, a.C, a.W);
@@ -458,49 +458,51 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
                          me < 2 ? (me ? a.vq : a.kq) + head * (D / 2) : (const uint8_t*)((me == 2 ? a.kp : a.vp) + head * (D / 16)), me < 2 ? D / 2 : D / 8);
         };
         for (int it = 0; it < AHEAD; ++it) to_l2(it);
-        int seen = -1;   // (the last tile that to_l2 has gone ahead of)
         fetch(me);
+        int x = me;   // this warp's next part
+        // Tile by tile, and each warp's arrival belongs to every tile, whether or not it has a part of it: a barrier's phase bit tells a stage that
+        // is free from one that is still to be used twice only while no stage is used again before all warps have seen it free. (With arrivals
+        // for parts alone a warp without one could find its bit a use too late, and both it and the products wait for good.)
 #pragma unroll 1
-        for (int x = me; x < all; x += L::LOADERS) {
-          const int it = (uint32_t)x / L::ITEMS, p = (uint32_t)x % L::ITEMS, at = 2 * (tile + it), s = (uint32_t)at % ST;
-          // Tile by tile, those without a part for this warp too: it may have had none in many short pieces, and a barrier's phase bit tells
-          // a stage that is free from one that is still to be used twice only to those who have followed it.
-          for (; clear <= tile + it && ok; ++clear) {
-            const int c = 2 * clear, e = (uint32_t)c % ST;
-            if (c >= ST)
-              ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_EMPTY + e), ((uint32_t)c / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles)) &&
-                                               wait_bar(bar(L::B_EMPTY + e + 1), ((uint32_t)c / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles)));
-          }
+        for (int it = 0; it < w.n; ++it) {
+          const int at = 2 * (tile + it), s = (uint32_t)at % ST;
+          if (at >= ST)
+            ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_EMPTY + s), ((uint32_t)at / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles)) &&
+                                             wait_bar(bar(L::B_EMPTY + s + 1), ((uint32_t)at / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles)));
           if (!ok) break;
-          while (seen < it) to_l2(++seen + AHEAD);
+          to_l2(it + AHEAD);
           const uint32_t st = sb + L::OFF_RING + (uint32_t)s * L::KT;
-          if (it < fresh) {   // nodes, as the cache would hold them
+          if (x < (it + 1) * L::ITEMS) {
+            const int p = (uint32_t)x % L::ITEMS;
+            if (it < fresh) {   // nodes, as the cache would hold them
 #pragma unroll 1
-            for (int y = lane; y < 2 * 2 * SLOTS * (D / 8); y += 32) {
-              const bool v = y >= 2 * SLOTS * (D / 8);
-              const int z = y % (2 * SLOTS * (D / 8)), r = p * 2 * SLOTS + z / (D / 8), j = z % (D / 8), k = (w.t0 + it) * 64 + r;
-              float h[8];
-              load8((const bf16*)(v ? a.v_t : a.k_t) + (((size_t)w.b * a.N + min(k, a.N - 1)) * a.H_kv + w.g) * D + j * 8, h);
-              quantize8<D, true>(h, j * 8, nullptr, nullptr, false, 0xffffffffu);
+              for (int y = lane; y < 2 * 2 * SLOTS * (D / 8); y += 32) {
+                const bool v = y >= 2 * SLOTS * (D / 8);
+                const int z = y % (2 * SLOTS * (D / 8)), r = p * 2 * SLOTS + z / (D / 8), j = z % (D / 8), k = (w.t0 + it) * 64 + r;
+                float h[8];
+                load8((const bf16*)(v ? a.v_t : a.k_t) + (((size_t)w.b * a.N + min(k, a.N - 1)) * a.H_kv + w.g) * D + j * 8, h);
+                quantize8<D, true>(h, j * 8, nullptr, nullptr, false, 0xffffffffu);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) h[i] = k < a.N ? held(h[i] * KV_FACTOR) : 0.f;
-              sts128(st + (v ? L::KT : 0u) + (uint32_t)(j >> 3) * 8192 + sw128(r, j & 7), halves_in_order(h));
+                for (int i = 0; i < 8; ++i) h[i] = k < a.N ? held(h[i] * KV_FACTOR) : 0.f;
+                sts128(st + (v ? L::KT : 0u) + (uint32_t)(j >> 3) * 8192 + sw128(r, j & 7), halves_in_order(h));
+              }
+            } else {
+              const bool turn = grp >= 2;   // (the second 64 channels: in another order, so that eight threads' stores take different banks)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const GroupScale gs = group_scale(pr[e]);
+                const uint32_t word[4] = {turn ? q[e].z : q[e].x, turn ? q[e].w : q[e].y, turn ? q[e].x : q[e].z, turn ? q[e].y : q[e].w};
+                const int r = (p * 2 + (e & 1)) * SLOTS + slot;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  sts128(st + (e >> 1) * L::KT + (uint32_t)(grp >> 1) * 8192 + sw128(r, (grp & 1) * 4 + (turn ? i ^ 2 : i)), unpack8(word[i], gs));
+              }
             }
-          } else {
-            const bool turn = grp >= 2;   // (the second 64 channels: in another order, so that eight threads' stores take different banks)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const GroupScale gs = group_scale(pr[e]);
-              const uint32_t word[4] = {turn ? q[e].z : q[e].x, turn ? q[e].w : q[e].y, turn ? q[e].x : q[e].z, turn ? q[e].y : q[e].w};
-              const int r = (p * 2 + (e & 1)) * SLOTS + slot;
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                sts128(st + (e >> 1) * L::KT + (uint32_t)(grp >> 1) * 8192 + sw128(r, (grp & 1) * 4 + (turn ? i ^ 2 : i)), unpack8(word[i], gs));
-            }
+            x += L::LOADERS;
+            fetch(x);
+            fence_proxy_async();
+            __syncwarp();
           }
-          fetch(x + L::LOADERS);
-          fence_proxy_async();
-          __syncwarp();
           if (lane == 0) {
             mbar_arrive(bar(L::B_FULL + s));
             mbar_arrive(bar(L::B_FULL + s + 1));
