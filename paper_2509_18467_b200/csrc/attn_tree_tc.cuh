@@ -20,13 +20,16 @@
 namespace lawcat {
 namespace attn {
 
-// Over 4 bits all operands are fp16: a code becomes 1024 + code by an OR into the mantissa, less 1024, times scale, plus minimum (both times
-// 16), one rounding of 2^-11; queries are scaled by a power of two per row. Values beyond 4094 leave fp16's range: a group that holds one is
-// NaN in the operand, so that every row that sees its slot comes out not finite (an infinite key would be a score of -inf, a slot that is not
-// seen, or with a cap a finite one). Such rows, and those whose outputs lie below 2^-18 and feel the smallest numbers that fp16 holds, are
-// computed again on the CUDA cores. Channels of eight are held in the order 0 4 1 5 2 6 3 7, in which a word of codes unpacks two at a time.
+// Over 4 bits all operands are fp16: an OR into the mantissa makes a code 1024 + code, or in the upper half of a byte 64 + code; less that, times
+// scale, plus minimum (both times 16), one rounding of 2^-11. Queries are scaled by a power of two per row. Channels of eight are held in the
+// order 0 4 1 5 2 6 3 7, in which a word of codes unpacks two at a time.
+//   Values beyond 4094 leave fp16's range: a group that holds one is NaN in the operand, so that every row that sees its slot comes out not finite
+// (an infinite key would be a score of -inf, a slot that is not seen, or with a cap a finite one).
+//   From 2^-21 on 16 scale and 16 minimum are, as 8-bit numbers, whole multiples of 2^-24, which fp16 holds. Of smaller ones it holds the nearest
+// multiple, and a value is off by up to 17 2^-29: 2^-9.9 of an output of 2^-15.
+//   Rows that come out not finite or below 2^-15 everywhere are computed again on the CUDA cores.
 constexpr float KV_FACTOR = 16.f;
-constexpr float SMALL = 1.f / (1 << 18);   // (the least difference of fp16 numbers, 2^-24 / 16, is 2^-10 of it)
+constexpr float SMALL = 1.f / (1 << 15);
 
 // a value (times 16) that fp16 holds, or NaN
 __device__ __forceinline__ float held(float x) { return fabsf(x) <= 65504.f ? x : NAN; }
@@ -55,13 +58,12 @@ __device__ __forceinline__ float scale_query(const uint4& q, uint4& halves) {
 __device__ __forceinline__ __half2 as_half2(uint32_t w) { return *reinterpret_cast<const __half2*>(&w); }
 __device__ __forceinline__ uint32_t as_word(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
 struct GroupScale {
-  __half2 s1, s16, low;   // scale, scale / 16, minimum
+  __half2 scale, low;
 };
 __device__ __forceinline__ GroupScale group_scale(uint32_t pair) {   // (scale, minimum) in bf16
-  const float s = bf16_lo(pair) * KV_FACTOR, l = bf16_hi(pair) * KV_FACTOR;
-  const __half2 x = __floats2half2_rn(s, s * 0.0625f), y = __floats2half2_rn(l, l), s1 = __low2half2(x);
-  const __half2 top = __hfma2(s1, __float2half2_rn(15.f), y);                                  // (not finite where a value may be)
-  return GroupScale{s1, __high2half2(x), __hfma2(top, __float2half2_rn(0.f), y)};
+  const __half2 x = __floats2half2_rn(bf16_lo(pair) * KV_FACTOR, bf16_hi(pair) * KV_FACTOR), scale = __low2half2(x), low = __high2half2(x);
+  const __half2 top = __hfma2(scale, __float2half2_rn(15.f), low);   // (not finite where a value may be)
+  return GroupScale{scale, __hfma2(top, __float2half2_rn(0.f), low)};
 }
 // (w & mask) | with, in one instruction (two constants would be two)
 __device__ __forceinline__ uint32_t mask_or(uint32_t w, uint32_t mask, uint32_t with) {
@@ -71,10 +73,10 @@ __device__ __forceinline__ uint32_t mask_or(uint32_t w, uint32_t mask, uint32_t 
 }
 // a word of eight codes -> eight values in the order above
 __device__ __forceinline__ uint4 unpack8(uint32_t w, const GroupScale& g) {
-  const uint32_t k = 0x64006400u, hi = w >> 8;   // 1024
-  auto val = [&](uint32_t bits, __half2 s) { return as_word(__hfma2(__hsub2(as_half2(bits), as_half2(k)), s, g.low)); };
-  return make_uint4(val(mask_or(w, 0x000F000Fu, k), g.s1), val(mask_or(w, 0x00F000F0u, k), g.s16), val(mask_or(hi, 0x000F000Fu, k), g.s1),
-                    val(mask_or(hi, 0x00F000F0u, k), g.s16));
+  const uint32_t k = 0x64006400u, k16 = 0x54005400u, hi = w >> 8;   // 1024, 64
+  auto val = [&](uint32_t bits, uint32_t less) { return as_word(__hfma2(__hsub2(as_half2(bits), as_half2(less)), g.scale, g.low)); };
+  return make_uint4(val(mask_or(w, 0x000F000Fu, k), k), val(mask_or(w, 0x00F000F0u, k16), k16), val(mask_or(hi, 0x000F000Fu, k), k),
+                    val(mask_or(hi, 0x00F000F0u, k16), k16));
 }
 
 struct TreeTcArgs {

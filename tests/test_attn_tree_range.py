@@ -2,6 +2,10 @@
 
 Keys and values are held times 16 in fp16. A group of 32 channels (minimum m, scale s) that holds values beyond 65504 / 16 does not fit: rows that
 see such a slot are computed in fp32, and so are their bounds here (no operand is rounded). The others round keys, values and weights by 2^-11 each.
+
+Below, 16 s and 16 m are whole multiples of 2^-24 as bf16 numbers from 2^-21 on, so that fp16 holds them and, but for 2^-11 of it, the value. Of a
+smaller one it holds the nearest such multiple: half a step for each of 15 scales, the minimum and the value, 17 2^-29 in all (ABS). For keys that is
+a score's error of |scale| sum|q| 17 2^-29. Rows whose outputs lie below 2^-15 are computed in fp32.
 """
 import pytest
 import torch
@@ -37,6 +41,14 @@ def too_wide(scale, low):
     return ((low.abs() > FITS) | ((low + 15 * scale).abs() > FITS)).any(-1)
 
 
+ABS = 17 * 2.0 ** -29
+
+
+def too_small(scale, low):
+    """[n, H_kv]: rows with a group whose scale or minimum fp16 may not hold."""
+    return (((scale != 0) & (scale < 2.0 ** -21)) | ((low != 0) & (low.abs() < 2.0 ** -21))).any(-1)
+
+
 def verify(q, k, v, K, V, pos, parents, cap=0.0, scale=None, slopes=None):
     """One call over the quantized K, V [B, C, H_kv, d]; every row within its bound."""
     B, N, H, d = q.shape
@@ -53,11 +65,15 @@ def verify(q, k, v, K, V, pos, parents, cap=0.0, scale=None, slopes=None):
         slots = torch.tensor(cached, dtype=torch.long, device="cuda") % C
         Kd, Vd = rows_of(cache, b, slots)
         keys, values = torch.cat([Kd, quantized(k[b])[3]]), torch.cat([Vd, quantized(v[b])[3]])
-        wide = torch.cat([too_wide(*cached_groups(cache, 1, b, slots)), too_wide(*groups(k[b]))])          # [n, H_kv]
-        exact = (see.to("cuda")[:, :, None] & wide[None]).any(1).repeat_interleave(H // H_kv, 1)[..., None]  # [N, H, 1]
+        seen = lambda x: (see.to("cuda")[:, :, None] & x[None]).any(1).repeat_interleave(H // H_kv, 1)[..., None]  # noqa: E731  [n, H_kv] -> [N, H, 1]
+        wide = seen(torch.cat([too_wide(*cached_groups(cache, 1, b, slots)), too_wide(*groups(k[b]))]))
+        fine_values = seen(torch.cat([too_small(*cached_groups(cache, 3, b, slots)), too_small(*groups(v[b]))]))
+        reach = abs(s) * torch.where(see.any(1).to("cuda")[:, None, None], q[b].double(), 0.0).abs().sum(-1, keepdim=True)
         want, fine = tree_attention(q[b], keys, values, see, dist, s, cap, slopes)
         _, coarse = tree_attention(q[b], keys, values, see, dist, s, cap, slopes, eps_p=U11, eps_k=U11, eps_v=U11, min_p=MIN_P)
-        check(o[b], want, torch.where(exact, fine, coarse), U16, f"o of sequence {b} at {x}")
+        size, _ = tree_attention(q[b], keys, values.abs(), see, dist, s, cap, slopes)
+        coarse = coarse + 2 * ABS * reach * size + torch.where(fine_values & (want.abs().amax(-1, keepdim=True) > 0.98 * 2.0 ** -15), ABS, 0.0)
+        check(o[b], want, torch.where(wide, fine, coarse), U16, f"o of sequence {b} at {x}")
     return o
 
 
@@ -82,3 +98,21 @@ def test_one_large_channel_of_the_keys(cap, size, where, N, d, lengths):
     else:
         k[..., c] = large
     verify(q, k, v, K, V, pos, [some_tree(N, b) for b in range(B)], cap)
+
+
+@pytest.mark.parametrize("lengths", list(LENGTHS))
+@pytest.mark.parametrize("N,d", [(5, 64), (5, 128), (21, 128), (40, 64), (40, 128)])
+@pytest.mark.parametrize("std", [1e-4, 3e-5, 1e-5, 4e-6, 1e-6, 1e-9, "some"])
+def test_small_values(std, N, d, lengths):
+    """All values small, or ("some") a group of each cached row and all of every third."""
+    pos, C = LENGTHS[lengths]
+    B, H, H_kv = len(pos), 8, 2
+    q, k, v = draw((B, N, H, d), N, "bf16", 1.5), draw((B, N, H_kv, d), N + 1, "bf16"), draw((B, N, H_kv, d), N + 2, "bf16")
+    K, V = draw((B, C, H_kv, d), N + 3, "bf16"), draw((B, C, H_kv, d), N + 4, "bf16")
+    if std == "some":
+        V[..., 32:] *= 1e-6
+        V[:, ::3] *= 1e-5
+    else:
+        v *= std
+        V *= std
+    verify(q, k, v, K, V, pos, [some_tree(N, b) for b in range(B)])
