@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
     for (int i = 0; i < QV; ++i) {
       const int at = tid + 128 * i, c = at / (D / 8), j = at % (D / 8);
       uint4 h;
-      const float up = (CAP ? 1.f : a.scale * LOG2E) * (scale_query<D>(q[i], h) / KV_FACTOR);
+      const float up = (CAP ? 1.f : a.scale * LOG2E) * (scale_query<D>(q[i], h, a.scale) / KV_FACTOR);
       sts128(sb + L::OFF_Q + (uint32_t)(j >> 3) * (NCOL * 128) + sw128(c, j & 7), h);
       if (j == 0) s_ref[c / 2 * 4 + (c & 1)] = s_raw[c / 2 * 4 + (c & 1)] = up;
     }

@@ -133,7 +133,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           const int p = i / (D / 8), j = i % (D / 8), row = min(row_of_piece(f, w.rb, p), R - 1), nd = quot(row, f.group);
           const uint4 x = *reinterpret_cast<const uint4*>((const bf16*)a.q + (((size_t)b * a.N + nd) * a.H + w.g * G + rest(row, nd, f.group)) * D + j * 8);
           uint4 y;
-          const float up = scale_query<D>(x, y);
+          const float up = scale_query<D>(x, y, a.scale);
           sts128(sb + (uint32_t)(p >> 7) * L::TILE + (uint32_t)(j >> 3) * 16384 + sw128(p & 127, j & 7), y);
           if (j == 0) s_scale[p] = up / KV_FACTOR;
         }

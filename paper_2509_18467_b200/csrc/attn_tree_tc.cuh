@@ -26,7 +26,8 @@ namespace attn {
 //   Values beyond 4094 leave fp16's range: a group that holds one is NaN in the operand, so that every row that sees its slot comes out not finite
 // (an infinite key would be a score of -inf, a slot that is not seen, or with a cap a finite one).
 //   From 2^-21 on 16 scale and 16 minimum are, as 8-bit numbers, whole multiples of 2^-24, which fp16 holds. Of smaller ones it holds the nearest
-// multiple, and a value is off by up to 17 2^-29: 2^-9.9 of an output of 2^-15.
+// multiple, and a value is off by up to 17 2^-29: 2^-9.9 of an output of 2^-15, and in a key |scale| sum|q| 17 2^-29 of a score. Queries for which
+// that would pass 2^-11 are scaled by NaN.
 //   Rows that come out not finite or below 2^-15 everywhere are computed again on the CUDA cores.
 constexpr float KV_FACTOR = 16.f;
 constexpr float SMALL = 1.f / (1 << 15);
@@ -38,9 +39,9 @@ __device__ __forceinline__ uint4 halves_in_order(const float (&x)[8]) {
   return make_uint4(pack_f16(x[0], x[4]), pack_f16(x[1], x[5]), pack_f16(x[2], x[6]), pack_f16(x[3], x[7]));
 }
 // Eight channels of a query row, whose D / 8 threads lie side by side in a warp, scaled so that the row's largest value lies in [1, 2);
-// returns what that took.
+// returns what that took (NaN where `scale` times the row's sum is too large for keys in fp16).
 template <int D>
-__device__ __forceinline__ float scale_query(const uint4& q, uint4& halves) {
+__device__ __forceinline__ float scale_query(const uint4& q, uint4& halves, float scale) {
   float x[8] = {bf16_lo(q.x), bf16_hi(q.x), bf16_lo(q.y), bf16_hi(q.y), bf16_lo(q.z), bf16_hi(q.z), bf16_lo(q.w), bf16_hi(q.w)};
   uint32_t top = 0;
 #pragma unroll
@@ -48,11 +49,17 @@ __device__ __forceinline__ float scale_query(const uint4& q, uint4& halves) {
 #pragma unroll
   for (int o = 1; o < D / 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
   const uint32_t e2 = min(max(top >> 23, 1u), 253u);
-  const float down = __uint_as_float((254u - e2) << 23);
+  const float down = __uint_as_float((254u - e2) << 23), up = __uint_as_float(e2 << 23);
+  float sum = 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] *= down;
+  for (int e = 0; e < 8; ++e) {
+    x[e] *= down;
+    sum += fabsf(x[e]);
+  }
+#pragma unroll
+  for (int o = 1; o < D / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   halves = halves_in_order(x);
-  return __uint_as_float(e2 << 23);
+  return fabsf(scale) * up * sum <= 16384.f ? up : NAN;
 }
 
 __device__ __forceinline__ __half2 as_half2(uint32_t w) { return *reinterpret_cast<const __half2*>(&w); }

@@ -5,7 +5,8 @@ see such a slot are computed in fp32, and so are their bounds here (no operand i
 
 Below, 16 s and 16 m are whole multiples of 2^-24 as bf16 numbers from 2^-21 on, so that fp16 holds them and, but for 2^-11 of it, the value. Of a
 smaller one it holds the nearest such multiple: half a step for each of 15 scales, the minimum and the value, 17 2^-29 in all (ABS). For keys that is
-a score's error of |scale| sum|q| 17 2^-29. Rows whose outputs lie below 2^-15 are computed in fp32.
+a score's error of |scale| sum|q| 17 2^-29, and rows with |scale| sum|q| above 2^14 are computed in fp32; so are those whose outputs lie
+below 2^-15.
 """
 import pytest
 import torch
@@ -73,7 +74,7 @@ def verify(q, k, v, K, V, pos, parents, cap=0.0, scale=None, slopes=None):
         _, coarse = tree_attention(q[b], keys, values, see, dist, s, cap, slopes, eps_p=U11, eps_k=U11, eps_v=U11, min_p=MIN_P)
         size, _ = tree_attention(q[b], keys, values.abs(), see, dist, s, cap, slopes)
         coarse = coarse + 2 * ABS * reach * size + torch.where(fine_values & (want.abs().amax(-1, keepdim=True) > 0.98 * 2.0 ** -15), ABS, 0.0)
-        check(o[b], want, torch.where(wide, fine, coarse), U16, f"o of sequence {b} at {x}")
+        check(o[b], want, torch.where(wide | (reach > 1.01 * 2.0 ** 14), fine, coarse), U16, f"o of sequence {b} at {x}")
     return o
 
 
@@ -116,3 +117,15 @@ def test_small_values(std, N, d, lengths):
         v *= std
         V *= std
     verify(q, k, v, K, V, pos, [some_tree(N, b) for b in range(B)])
+
+
+@pytest.mark.parametrize("lengths", list(LENGTHS))
+@pytest.mark.parametrize("N,d", [(5, 64), (5, 128), (21, 128), (40, 64), (40, 128)])
+@pytest.mark.parametrize("small,large", [(1e-5, 1e5), (1e-4, 1e4), (1e-7, 1e7), (1e-5, 300.0), (1e-4, 1e3)])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_small_keys_under_large_queries(cap, small, large, N, d, lengths):
+    pos, C = LENGTHS[lengths]
+    B, H, H_kv = len(pos), 8, 2
+    q, k, v = draw((B, N, H, d), N, "bf16", large), draw((B, N, H_kv, d), N + 1, "bf16", small), draw((B, N, H_kv, d), N + 2, "bf16")
+    K, V = draw((B, C, H_kv, d), N + 3, "bf16", small), draw((B, C, H_kv, d), N + 4, "bf16")
+    verify(q, k, v, K, V, pos, [some_tree(N, b) for b in range(B)], cap)
