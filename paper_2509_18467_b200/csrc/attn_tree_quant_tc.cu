@@ -101,7 +101,8 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
   const TreeArgs& a = f.a;
   const uint32_t sb = smem_u32(smem);
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  float* const s_ref = reinterpret_cast<float*>(smem + L::OFF_COL);  // [NCOL / 2] (scale, scale, -reference, -reference) of two columns (CAP: scale without the softmax's)
+  // [NCOL / 2] (scale, scale, s, s) of two columns with s = WEIGHT_SHIFT - reference (CAP: scale without the softmax's)
+  float* const s_ref = reinterpret_cast<float*>(smem + L::OFF_COL);
   float* const s_raw = s_ref + 2 * NCOL;                             // the same with references of zero
   float* const s_bias = s_raw + 2 * NCOL;                            // [NCOL / 2] (-slope, -slope, -slope depth, -slope depth)
   int* const s_far = reinterpret_cast<int*>(s_bias + 2 * NCOL);      // [NCOL] the farthest key that is seen
@@ -384,7 +385,7 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
             mx1 = fmaxf(fmaxf(mx1, z[c + 2]), z[c + 3]);
           }
           mx0 = fmaxf(fmaxf(mx0, z[NCOL - 2]), z[NCOL - 1]);
-          if (!named_bar_or(3, 128, fmaxf(mx0, mx1) > COL_RESCALE || fail)) break;
+          if (!named_bar_or(3, 128, fmaxf(mx0, mx1) > WEIGHT_SHIFT + COL_RESCALE || fail)) break;
           if (named_bar_or(3, 128, fail)) break;
           table = s_raw;
           continue;
@@ -401,10 +402,11 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
         named_bar_sync(3, 128);
         if (tid < NCOL) {
           const float x = fmaxf(fmaxf(s_red[tid], s_red[NCOL + tid]), fmaxf(s_red[2 * NCOL + tid], s_red[3 * NCOL + tid]));
-          float& neg = s_ref[tid / 2 * 4 + 2 + (tid & 1)];
-          const bool grow = x > -neg + COL_RESCALE;
-          s_factor[tid] = grow ? ex2f(-neg - x) : 1.f;
-          if (grow) neg = -x;
+          float& shift = s_ref[tid / 2 * 4 + 2 + (tid & 1)];
+          const float ref = WEIGHT_SHIFT - shift;
+          const bool grow = x > ref + COL_RESCALE;
+          s_factor[tid] = grow ? ex2f(ref - x) : 1.f;
+          if (grow) shift = WEIGHT_SHIFT - x;
         }
         named_bar_sync(3, 128);
         if (i > 0) {

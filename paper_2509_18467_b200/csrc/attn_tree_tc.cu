@@ -253,7 +253,8 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           m = base;
         }
         const float base = m == -INFINITY ? 0.f : m;
-        const uint64_t sc = f2_pack(by, by), nb = f2_pack(-base, -base);
+        const float less = QUANT ? WEIGHT_SHIFT - base : -base;
+        const uint64_t sc = f2_pack(by, by), nb = f2_pack(less, less);
         uint64_t sum0 = 0, sum1 = 0;
 #pragma unroll
         for (int q = 0; q < 32; q += 8) {   // (step by step over eight pairs: what one warp has in flight is all that hides latencies)

@@ -31,6 +31,9 @@ namespace attn {
 //   Rows that come out not finite or below 2^-15 everywhere are computed again on the CUDA cores.
 constexpr float KV_FACTOR = 16.f;
 constexpr float SMALL = 1.f / (1 << 15);
+// Weights are 2^7 times exp2(score - reference), 2^15 at most: fp16 holds them down to 2^-32 of the reference's (without the 2^7 it would be 2^-25,
+// and 16384 slots 2^-26 below a token without a value would be lost: 10 % of the output). Sums and outputs are scaled alike.
+constexpr float WEIGHT_SHIFT = 7.f;
 
 // a value (times 16) that fp16 holds, or NaN
 __device__ __forceinline__ float held(float x) { return fabsf(x) <= 65504.f ? x : NAN; }

@@ -7,6 +7,8 @@ Below, 16 s and 16 m are whole multiples of 2^-24 as bf16 numbers from 2^-21 on,
 smaller one it holds the nearest such multiple: half a step for each of 15 scales, the minimum and the value, 17 2^-29 in all (ABS). For keys that is
 a score's error of |scale| sum|q| 17 2^-29, and rows with |scale| sum|q| above 2^14 are computed in fp32; so are those whose outputs lie
 below 2^-15.
+
+Weights are 2^7 times what they are relative to a score of the row, and whole multiples of 2^-24 below 2^-14: off by 2^-32 at most (MIN_P).
 """
 import pytest
 import torch
@@ -21,7 +23,7 @@ from tree_reference import U11, sees, tree_attention
 pytestmark = pytest.mark.gpu
 
 FITS = 65504.0 / 16
-MIN_P = 2.0 ** -25
+MIN_P = 2.0 ** -32
 # lengths that are whole segments, that are cut into pieces which the first one's block joins, and that a second kernel joins
 LENGTHS = {"whole": ([300, 11, 0], 400), "cut": ([1500] * 24, 1600), "few": ([3000], 4000)}
 
@@ -129,3 +131,17 @@ def test_small_keys_under_large_queries(cap, small, large, N, d, lengths):
     q, k, v = draw((B, N, H, d), N, "bf16", large), draw((B, N, H_kv, d), N + 1, "bf16", small), draw((B, N, H_kv, d), N + 2, "bf16")
     K, V = draw((B, C, H_kv, d), N + 3, "bf16", small), draw((B, C, H_kv, d), N + 4, "bf16")
     verify(q, k, v, K, V, pos, [some_tree(N, b) for b in range(B)], cap)
+
+
+@pytest.mark.parametrize("N", [3, 12, 20, 40])
+@pytest.mark.parametrize("where", ["newest", "middle", "oldest"])
+@pytest.mark.parametrize("B,d", [(1, 128), (24, 64)])
+def test_a_sink(B, d, where, N):
+    """One token holds all but 2^-12 of the weight and has next to no value; the others' weights are e^-18 of its own each."""
+    n, C, H, H_kv = 16380, 16384, 8, 2
+    full = lambda x, *s: torch.full(s, x, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    q, k, v = full(1.5, B, N, H, d), full(0.0, B, N, H_kv, d), full(0.5, B, N, H_kv, d)
+    K, V = full(0.0, B, C, H_kv, d), full(0.5, B, C, H_kv, d)
+    at = dict(newest=n - 1, middle=n // 2, oldest=0)[where]
+    K[:, at], V[:, at] = 1.5, 1e-3
+    verify(q, k, v, K, V, [n] * B, [some_tree(N, b) for b in range(B)], scale=18.0 / (2.25 * d))
