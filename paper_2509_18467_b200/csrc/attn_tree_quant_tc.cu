@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
   Paths& paths = *reinterpret_cast<Paths*>(smem);                    // (over V, ahead of a segment's tiles)
   volatile int* const s_flags = reinterpret_cast<volatile int*>(smem + L::OFF_BAR + 16);   // tensor memory, abort
   volatile int* const s_abort = s_flags + 1;
-  uint32_t* const s_bad = reinterpret_cast<uint32_t*>(smem + L::OFF_BAR + 24);             // [2] rows to be computed again
+  uint32_t* const s_bad = reinterpret_cast<uint32_t*>(smem + L::OFF_BAR + 24);             // [2] rows to be computed again, [2] those that are small everywhere
   const uint32_t bar_s = sb + L::OFF_BAR, bar_o = bar_s + 8;
   const int G = a.H / a.H_kv, R = a.N * G;
 
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
     mbar_init(bar_s, 1);
     mbar_init(bar_o, 1);
     s_flags[1] = 0;
-    s_bad[0] = s_bad[1] = 0u;
+    s_bad[0] = s_bad[1] = s_bad[2] = s_bad[3] = 0u;
     mbar_fence_init();
   }
   behind_last_kernel();
@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
   int count = 0;   // tiles so far
   bool fail = false;
   // The piece's rows to memory (value(x): eight channels of bf16, vector x of the rows), and those computed again that are not finite somewhere,
-  // or small everywhere.
+  // or small everywhere for want of smaller numbers.
   auto rows_out = [&](auto value) {
     const int r0 = w.rb * NCOL;
 #pragma unroll 1
@@ -158,18 +158,20 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
       for (int e = 0; e < 4; ++e) top = max(top, max(u[e] >> 16, u[e] & 0xffffu));
 #pragma unroll
       for (int m = 1; m < D / 8; m <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, m));
-      if (x % (D / 8) == 0 && r < R && s_depth[c] >= 0 && (top >= 0x7f80u || __uint_as_float(top << 16) < SMALL)) atomicOr(s_bad + c / 32, 1u << (c & 31));
+      if (x % (D / 8) == 0 && r < R && s_depth[c] >= 0 && (top >= 0x7f80u || __uint_as_float(top << 16) < SMALL))
+        atomicOr(s_bad + c / 32 + (top < 0x7f80u ? 2 : 0), 1u << (c & 31));
     }
     named_bar_sync(3, 128);
-    if (s_bad[0] | s_bad[1]) {
+    if (s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3]) {
+      const bool small = s_bad[2] | s_bad[3] ? named_bar_or(3, 128, small_values<D, 128>(a, w.b, w.g, tid)) : false;
 #pragma unroll 1
       for (int c = warp; c < NCOL && r0 + c < R; c += 4)
-        if (s_bad[c / 32] >> (c & 31) & 1u) {
+        if ((s_bad[c / 32] | (small ? s_bad[2 + c / 32] : 0u)) >> (c & 31) & 1u) {
           const int node = quot(r0 + c, f.group);
           tree_row_again<bf16, D, true>(a, w.b, node, w.g * G + rest(r0 + c, node, f.group));
         }
       named_bar_sync(3, 128);
-      if (tid < 2) s_bad[tid] = 0u;
+      if (tid < 4) s_bad[tid] = 0u;
       named_bar_sync(3, 128);
     }
   };

@@ -406,8 +406,11 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         if (QUANT && large) atomicOr(s_large + (rp >> 5), large);
       }
       if (named_bar_or(2, 256, bad != 0u || large != 0xffffffffu)) {
+        bool small = false;
+        if constexpr (QUANT)
+          if (named_bar_or(2, 256, ~s_large[rp >> 5] != 0u)) small = named_bar_or(2, 256, small_values<D, 256>(a, b, w.g, tid));
         for (int i = warp; i < q_tiles * 128; i += 8)
-          if ((s_bad[i >> 5] | (QUANT ? ~s_large[i >> 5] : 0u)) >> (i & 31) & 1u) {
+          if ((s_bad[i >> 5] | (small ? ~s_large[i >> 5] : 0u)) >> (i & 31) & 1u) {
             const int row = row_of_piece(f, w.rb, i), again = quot(row, f.group);
             tree_row_again<bf16, D, QUANT>(a, b, again, w.g * G + rest(row, again, f.group));
           }

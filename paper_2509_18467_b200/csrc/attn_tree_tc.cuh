@@ -28,7 +28,8 @@ namespace attn {
 //   From 2^-21 on 16 scale and 16 minimum are, as 8-bit numbers, whole multiples of 2^-24, which fp16 holds. Of smaller ones it holds the nearest
 // multiple, and a value is off by up to 17 2^-29: 2^-9.9 of an output of 2^-15, and in a key |scale| sum|q| 17 2^-29 of a score. Queries for which
 // that would pass 2^-11 are scaled by NaN.
-//   Rows that come out not finite or below 2^-15 everywhere are computed again on the CUDA cores.
+//   Rows that come out not finite are computed again on the CUDA cores, and so are those below 2^-15 everywhere if the sequence holds such small
+// values at all (zeros are held: a head without values, or a cache that is not filled yet, costs a look at the scales).
 constexpr float KV_FACTOR = 16.f;
 constexpr float SMALL = 1.f / (1 << 15);
 // Weights are 2^7 times exp2(score - reference), 2^15 at most: fp16 holds them down to 2^-32 of the reference's (without the 2^7 it would be 2^-25,
@@ -74,6 +75,30 @@ __device__ __forceinline__ GroupScale group_scale(uint32_t pair) {   // (scale, 
   const __half2 x = __floats2half2_rn(bf16_lo(pair) * KV_FACTOR, bf16_hi(pair) * KV_FACTOR), scale = __low2half2(x), low = __high2half2(x);
   const __half2 top = __hfma2(scale, __float2half2_rn(15.f), low);   // (not finite where a value may be)
   return GroupScale{scale, __hfma2(top, __float2half2_rn(0.f), low)};
+}
+// Whether values of sequence b's key-value head g may be smaller than fp16 holds: a scale or minimum in the cache is not 0 and below 2^-21 (0x3500
+// in bf16), or a node's value not 0 and below 2^-15. Each of the threads looks at some of them.
+template <int D, int THREADS>
+__device__ __noinline__ bool small_values(const TreeArgs& a, int b, int g, int tid) {
+  constexpr int NG = D / 32;
+  const int pos = a.pos[b], cached = cached_keys(pos, a.W), ps = pos < 0 ? 0 : pos % a.C;
+  const uint32_t* const pairs = reinterpret_cast<const uint32_t*>(a.vp) + ((size_t)b * a.H_kv + g) * a.C * NG;
+  uint32_t found = 0u;
+  for (int k = tid; k < cached; k += THREADS) {
+    const size_t slot = k < ps ? ps - 1 - k : ps - 1 - k + a.C;
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const uint32_t x = pairs[slot * NG + i] & 0x7fff7fffu;
+      found |= (x + 0x7fff7fffu) & ~(x + 0x4B004B00u) & 0x80008000u;   // (no carries: above 0, not above 0x34ff)
+    }
+  }
+  for (int i = tid; i < a.N * (D / 8); i += THREADS) {
+    float x[8];
+    load8((const bf16*)a.v_t + (((size_t)b * a.N + i / (D / 8)) * a.H_kv + g) * D + i % (D / 8) * 8, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) found |= x[e] != 0.f && fabsf(x[e]) < SMALL;
+  }
+  return found != 0u;
 }
 // (w & mask) | with, in one instruction (two constants would be two)
 __device__ __forceinline__ uint32_t mask_or(uint32_t w, uint32_t mask, uint32_t with) {
@@ -435,7 +460,11 @@ __global__ void __launch_bounds__(512) attn_tree_join_tc_kernel(const __grid_con
     if (QUANT && (!some || l == 0.f || !(largest < SMALL))) atomicOr(&s_large, 1u << ri);
   }
   __syncthreads();
-  const uint32_t again = s_bad | (QUANT ? ~s_large : 0u);
+  uint32_t again = s_bad;
+  if constexpr (QUANT) {
+    const uint32_t low = ~s_large & 0xffffffffu >> (32 - J::ROWS);
+    if (low && __syncthreads_or(small_values<D, 512>(a, b, segment / f.row_blocks, threadIdx.x))) again |= low;
+  }
   if (!again) return;
   for (int i = warp; i < J::ROWS; i += 16)           // (behind the barrier: nobody else writes these channels any more)
     if (again >> i & 1u) {

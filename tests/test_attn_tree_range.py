@@ -6,7 +6,7 @@ see such a slot are computed in fp32, and so are their bounds here (no operand i
 Below, 16 s and 16 m are whole multiples of 2^-24 as bf16 numbers from 2^-21 on, so that fp16 holds them and, but for 2^-11 of it, the value. Of a
 smaller one it holds the nearest such multiple: half a step for each of 15 scales, the minimum and the value, 17 2^-29 in all (ABS). For keys that is
 a score's error of |scale| sum|q| 17 2^-29, and rows with |scale| sum|q| above 2^14 are computed in fp32; so are those whose outputs lie
-below 2^-15.
+below 2^-15 and that see values of the kind.
 
 Weights are 2^7 times what they are relative to a score of the row, and whole multiples of 2^-24 below 2^-14: off by 2^-32 at most (MIN_P).
 """
@@ -145,3 +145,28 @@ def test_a_sink(B, d, where, N):
     at = dict(newest=n - 1, middle=n // 2, oldest=0)[where]
     K[:, at], V[:, at] = 1.5, 1e-3
     verify(q, k, v, K, V, [n] * B, [some_tree(N, b) for b in range(B)], scale=18.0 / (2.25 * d))
+
+
+@pytest.mark.parametrize("N", [5, 40])
+def test_values_of_zero_take_no_longer(N):
+    """A cache whose values are all zero (a warm-up, a head that is off): nothing is computed twice."""
+    B, C, H, H_kv, d = 8, 8192, 8, 2, 128
+    p = api.attn_params(B, N, H, H_kv, d, T_k=C)
+    q, k, v = draw((B, N, H, d), 1, "bf16"), draw((B, N, H_kv, d), 2, "bf16"), draw((B, N, H_kv, d), 3, "bf16")
+    K, V = draw((B, C, H_kv, d), 4, "bf16"), draw((B, C, H_kv, d), 5, "bf16")
+    pos = torch.full((B,), 8000, dtype=torch.int32, device="cuda")
+    times = []
+    for f in (1.0, 0.0):
+        cache = api.quant_cache(p)
+        api.lawcat_cache_quantize(api.attn_params(B, C, H, H_kv, d, T_k=C), K, V * f, torch.zeros(B, dtype=torch.int32, device="cuda"), *cache)
+        once = []
+        for _ in range(5):
+            t = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+            t[0].record()
+            o = api.lawcat_attn_tree_quant(p, q, k, v * f, *cache, pos)
+            t[1].record()
+            torch.cuda.synchronize()
+            once.append(t[0].elapsed_time(t[1]))
+        times.append(min(once))
+        assert f or not o.any()
+    assert times[1] < 5 * times[0] + 0.1       # (computed again it takes some hundred times as long)
