@@ -103,6 +103,9 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
   auto o_col = [&](int u) { return tmem + (uint32_t)(256 + u * D); };
   // a warpgroup's steps of a piece: every tile, or every other one
   auto steps_of = [&](int u, int n) { return two ? n : (n + 1 - u) / 2; };
+  // What the copy and product warps wait for may come behind rows of the last piece that are computed again: as many keys as its segment has. So
+  // they wait as long as the longest segment so far allows.
+  long long patience = f.limit;
   Walk<64> walk;
   const int share = share_of_block(f);
   if (tid == 0 && !f.whole && !f.apart) f.told[share] = 0ull;   // (what a call that gave up may have left)
@@ -431,6 +434,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       int tile = 0;   // tiles of the pieces so far
       bool ok = true;
       while (ok && walk.next(f, w)) {
+        patience = max(patience, item_limit(f.limit, w.tiles));
         const Ring<64> ring = ring_of<64>(w.pos, a.C, a.W);
         const size_t head = ((size_t)w.b * a.H_kv + w.g) * a.C;
         const int fresh = max(0, min(f.node_tiles - w.t0, w.n)), all = w.n * L::ITEMS;
@@ -471,8 +475,8 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         for (int it = 0; it < w.n; ++it) {
           const int at = 2 * (tile + it), s = (uint32_t)at % ST;
           if (at >= ST)
-            ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_EMPTY + s), ((uint32_t)at / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles)) &&
-                                             wait_bar(bar(L::B_EMPTY + s + 1), ((uint32_t)at / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles)));
+            ok = __all_sync(0xffffffffu, wait_bar(bar(L::B_EMPTY + s), ((uint32_t)at / ST - 1) & 1, s_abort, patience) &&
+                                             wait_bar(bar(L::B_EMPTY + s + 1), ((uint32_t)at / ST - 1) & 1, s_abort, patience));
           if (!ok) break;
           to_l2(it + AHEAD);
           const uint32_t st = sb + L::OFF_RING + (uint32_t)s * L::KT;
@@ -518,9 +522,10 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       int at = 0, seq = 0;
       bool ok = true;
       while (ok && walk.next(f, w)) {
+        patience = max(patience, item_limit(f.limit, w.tiles));
         const Ring<64> ring = ring_of<64>(w.pos, a.C, a.W);
         const int qb = seq % q_places;
-        if (seq >= q_places) ok = wait_bar(bar(L::B_QE + qb), (seq / q_places - 1) & 1, s_abort, item_limit(f.limit, w.tiles));
+        if (seq >= q_places) ok = wait_bar(bar(L::B_QE + qb), (seq / q_places - 1) & 1, s_abort, patience);
         if (!ok) break;
         mbar_arrive_expect_tx(bar(L::B_Q + qb), (uint32_t)(q_tiles * (D / 64) * f.tile_rows * 128));
         for (int i = 0; i < q_tiles; ++i)
@@ -534,7 +539,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 #pragma unroll
           for (int v = 0; v < 2; ++v, ++at) {
             const int s = at % ST;
-            if (at >= ST) ok = ok && wait_bar(bar(L::B_EMPTY + s), (at / ST - 1) & 1, s_abort, item_limit(f.limit, w.tiles));
+            if (at >= ST) ok = ok && wait_bar(bar(L::B_EMPTY + s), (at / ST - 1) & 1, s_abort, patience);
             if (!ok) break;
             mbar_arrive_expect_tx(bar(L::B_FULL + s), L::KT);
             load_tile<D, 64>(sb + L::OFF_RING + s * L::KT, fresh ? v ? &tm_vt : &tm_kt : v ? &tm_v : &tm_k, bar(L::B_FULL + s), w.g, s0, w.b);
@@ -562,7 +567,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       };
       auto values = [&](int u, int it, int step, bool first, bool last, bool begin) {
         if (first && !full(2 * it + 1)) return false;
-        if (!wait_bar(bar(L::B_P + 2 * u + (step & 1)), (step >> 1) & 1, s_abort, f.limit)) return false;
+        if (!wait_bar(bar(L::B_P + 2 * u + (step & 1)), (step >> 1) & 1, s_abort, patience)) return false;
         tc_fence_after_sync();
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) mma_ts(o_col(u), s_col(u, step) + kk * 8, mdesc<64>(stage(2 * it + 1), kk), id_o, !begin || kk != 0);
@@ -572,13 +577,13 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       };
       bool ok = true;
       while (ok && walk.next(f, w)) {
+        patience = max(patience, item_limit(f.limit, w.tiles));
         const int n = w.n;
         bool fix = w.t0 < f.node_tiles;
         qb = seq % q_places;
-        ok = wait_bar(bar(L::B_Q + qb), (seq / q_places) & 1, s_abort, f.limit);
+        ok = wait_bar(bar(L::B_Q + qb), (seq / q_places) & 1, s_abort, patience);
         if (!ok) break;
-        // (the last piece's outputs may take as long as rows that are computed again do)
-        auto outputs_read = [&] { return seq == 0 || wait_bar(bar(L::B_OE), (seq - 1) & 1, s_abort, item_limit(f.limit, w.tiles)); };
+        auto outputs_read = [&] { return seq == 0 || wait_bar(bar(L::B_OE), (seq - 1) & 1, s_abort, patience); };
         if (two) {
           ok = scores(0, tile, steps[0], true, false) && scores(1, tile, steps[0], false, true);
           for (int it = 0; it < n && ok; ++it, ++tile, ++steps[0]) {
@@ -587,7 +592,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
               if (it + 1 < n) ok = scores(u, tile + 1, steps[0] + 1, u == 0, u == 1);
               if (ok && it == 0 && u == 0) ok = outputs_read();
               if (it + 1 == n && u == 1) mma_commit(bar(L::B_QE));   // (the queries' last product)
-              if (ok && fix) ok = wait_bar(bar(L::B_FIX), fixed++ & 1, s_abort, item_limit(f.limit, w.tiles));
+              if (ok && fix) ok = wait_bar(bar(L::B_FIX), fixed++ & 1, s_abort, patience);
               fix = false;
               if (ok) ok = values(u, tile, steps[0], u == 0, u == 1, it == 0);
             }
@@ -599,7 +604,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             if (it + 2 < n) ok = scores(u, tile + 2, steps[u] + 1, true, true);
             if (it + 1 == n) mma_commit(bar(L::B_QE + qb));   // (the queries' last product)
             if (ok && it == 0) ok = outputs_read();
-            if (ok && fix) ok = wait_bar(bar(L::B_FIX), fixed++ & 1, s_abort, item_limit(f.limit, w.tiles));
+            if (ok && fix) ok = wait_bar(bar(L::B_FIX), fixed++ & 1, s_abort, patience);
             fix = false;
             if (ok) ok = values(u, tile, steps[u], true, true, it < 2);
             ++steps[u];
