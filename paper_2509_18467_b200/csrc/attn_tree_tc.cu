@@ -296,13 +296,16 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       // with one tile of rows a warpgroup has half of the channels of both sums
       const bool join = is_joined_here(f, w), direct = is_whole(w) || join;
       float f0 = 1.f, f1 = 0.f;
+      bool none0 = false, none1 = false;   // (sums without keys: whatever stands there; a weight that underflows takes a NaN along)
       if (!two) {
         s_ml[u * 128 + r128] = make_float2(m, l);
         named_bar_sync(2, 256);
         const float2 x = s_ml[r128], y = s_ml[128 + r128];
         const float top = fmaxf(x.x, y.x), base = top == -INFINITY ? 0.f : top;
-        f0 = x.x == -INFINITY ? 0.f : ex2f(x.x - base);
-        f1 = y.x == -INFINITY ? 0.f : ex2f(y.x - base);
+        none0 = x.x == -INFINITY;
+        none1 = y.x == -INFINITY;
+        f0 = none0 ? 0.f : ex2f(x.x - base);
+        f1 = none1 ? 0.f : ex2f(y.x - base);
         l = x.y * f0 + y.y * f1;
         m = top;
       }
@@ -350,7 +353,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
           tmem_ld16(O1 + c, y);
           tmem_wait_ld();
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = (f0 == 0.f ? 0.f : o[e] * f0) + (f1 == 0.f ? 0.f : y[e] * f1);
+          for (int e = 0; e < 16; ++e) o[e] = (none0 ? 0.f : o[e] * f0) + (none1 ? 0.f : y[e] * f1);
         } else {
           tmem_wait_ld();
 #pragma unroll
@@ -375,9 +378,9 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             float x[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) x[e] = __ldcg(from + e * f.rows_pad);
-            const float k = y.y == 0.f ? 0.f : ex2f(y.x - m);
+            const float k = ex2f(y.x - m);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] += k == 0.f ? 0.f : k * x[e];
+            for (int e = 0; e < 16; ++e) o[e] += y.y == 0.f ? 0.f : k * x[e];
           }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
