@@ -135,15 +135,11 @@ __device__ __forceinline__ void cap_poly(float (&s)[N], float k, float c2, const
     f2_unpack(f2_mul(x, r), s[i], s[i + 1]);
   }
 }
+// what scores `top` and below are in caps, for the choice of the cap's form
+__device__ __forceinline__ float cap_reach(float top, float k) { return fabsf(k) < 1e4f ? top * fabsf(k) : 1.f; }
+// y: cap_reach of this thread's scores
 template <int N>
-__device__ __forceinline__ void cap_scores(float (&s)[N], float k, float c2) {
-  float b0 = 0.f, b1 = 0.f;
-#pragma unroll
-  for (int c = 0; c < N; c += 4) {
-    b0 = fmaxf(b0, fmaxf(fabsf(s[c]), fabsf(s[c + 1])));
-    b1 = fmaxf(b1, fmaxf(fabsf(s[c + 2]), fabsf(s[c + 3])));
-  }
-  const float y = fabsf(k) < 1e4f ? fmaxf(b0, b1) * fabsf(k) : 1.f;
+__device__ __forceinline__ void cap_scores(float (&s)[N], float k, float c2, float y) {
   if (__all_sync(0xffffffffu, y <= 0.4f)) {
     const float coef[4] = {0.9999998807907104f, -0.333313912153244f, 0.1327143758535385f, -0.04757280275225639f};
     cap_poly<N, 3>(s, k, c2, coef);
@@ -156,6 +152,18 @@ __device__ __forceinline__ void cap_scores(float (&s)[N], float k, float c2) {
     for (int c = 0; c < N; ++c) s[c] = c2 - 2.f * c2 * rcpf(1.f + ex2f(s[c] * k1));
   }
 }
+template <int N>
+__device__ __forceinline__ float top_score(const float (&s)[N]) {
+  float b0 = 0.f, b1 = 0.f;
+#pragma unroll
+  for (int c = 0; c < N; c += 4) {
+    b0 = fmaxf(b0, fmaxf(fabsf(s[c]), fabsf(s[c + 1])));
+    b1 = fmaxf(b1, fmaxf(fabsf(s[c + 2]), fabsf(s[c + 3])));
+  }
+  return fmaxf(b0, b1);
+}
+template <int N>
+__device__ __forceinline__ void cap_scores(float (&s)[N], float k, float c2) { cap_scores(s, k, c2, cap_reach(top_score(s), k)); }
 
 }  // namespace attn
 }  // namespace lawcat

@@ -248,9 +248,10 @@ __global__ void __launch_bounds__(128, ColLay<D, NCOL>::RESIDENT) attn_tree_quan
     }
 #pragma unroll
     for (int i = 0; i < QV; ++i) {
-      const int at = tid + 128 * i, c = at / (D / 8), j = at % (D / 8);
+      const int at = tid + 128 * i, c = at / (D / 8), j = at % (D / 8), node = quot(min(r0 + c, R - 1), f.group);
       uint4 h;
-      const float up = (CAP ? 1.f : a.scale * LOG2E) * (scale_query<D>(q[i], h, a.scale) / KV_FACTOR);
+      float up = (CAP ? 1.f : a.scale * LOG2E) * (scale_query<D>(q[i], h, a.scale) / KV_FACTOR);
+      if (pos < 0 || paths.on[node][node / 32] == 0u) up = 0.f;   // (a node that is not there: its scores, whatever it holds, choose nothing for the others)
       sts128(sb + L::OFF_Q + (uint32_t)(j >> 3) * (NCOL * 128) + sw128(c, j & 7), h);
       if (j == 0) s_ref[c / 2 * 4 + (c & 1)] = s_raw[c / 2 * 4 + (c & 1)] = up;
     }

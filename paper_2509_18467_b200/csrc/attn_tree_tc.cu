@@ -144,15 +144,20 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         mbar_arrive(bar(L::B_Q));
         named_bar_sync(2, 256);   // (s_scale)
       }
-      // the values of nodes that are not there: zeros (their weights are, and whatever they hold must not meet those)
+      // the values of nodes that are not there: zeros (their weights are, and whatever they hold must not meet those); with a cap their keys too,
+      // whose scores would help to choose its form
       for (int it = 0; it < node_tiles; ++it) {
         const int st = 2 * (at + it) + 1, k = (w.t0 + it) * 64 + (tid >> 2);
         if (k < a.N && s_depth[k] < 0) {
-          ok = ok && wait_bar(bar(L::B_FULL + st % ST), (st / ST) & 1, s_abort, f.limit);
+          ok = ok && wait_bar(bar(L::B_FULL + st % ST), (st / ST) & 1, s_abort, f.limit) &&
+               (!CAP || wait_bar(bar(L::B_FULL + st % ST - 1), (st / ST) & 1, s_abort, f.limit));
           if (ok)
 #pragma unroll
-            for (int j = tid & 3; j < D / 8; j += 4)
-              sts128(sb + L::OFF_RING + (uint32_t)(st % ST) * L::KT + (uint32_t)(j >> 3) * 8192 + sw128(tid >> 2, j & 7), make_uint4(0u, 0u, 0u, 0u));
+            for (int j = tid & 3; j < D / 8; j += 4) {
+              const uint32_t at = sb + L::OFF_RING + (uint32_t)(st % ST) * L::KT + (uint32_t)(j >> 3) * 8192 + sw128(tid >> 2, j & 7);
+              sts128(at, make_uint4(0u, 0u, 0u, 0u));
+              if (CAP) sts128(at - L::KT, make_uint4(0u, 0u, 0u, 0u));
+            }
           fence_proxy_async();
         }
       }
@@ -165,6 +170,7 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       const int depth = s_depth[node];
       const bool there = r < R && depth >= 0;
       const float unit = QUANT ? s_scale[rp] : 1.f;   // of a product in tensor memory
+      const float cap_scale = CAP ? a.scale * unit / a.cap : 0.f;
       const float scale2 = a.scale * LOG2E * unit, slope2 = BIAS && a.slopes ? a.slopes[h] * LOG2E : 0.f;
       const Ring<64> ring = ring_of<64>(pos, a.C, a.W);
       // the farthest key that the row sees, and the least of the warp's (of rows that are not there nothing is stored but zeros)
@@ -187,7 +193,8 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 #pragma unroll
         for (int c = 0; c < 64; c += 32) tmem_ld32(S + c, s + c);
         tmem_wait_ld();
-        if constexpr (CAP) cap_scores(s, a.scale * unit / a.cap, a.cap * LOG2E);
+        // (the cap's form is chosen by the warp's scores: none of rows that are not there, whatever they hold)
+        if constexpr (CAP) cap_scores(s, cap_scale, a.cap * LOG2E, there ? cap_reach(top_score(s), cap_scale) : 0.f);
         float by = CAP ? 1.f : scale2;
         if (it < f.node_tiles) {
           // the nodes' own: those of the path, by their distance
@@ -585,6 +592,10 @@ attn_tree_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         bool fix = w.t0 < f.node_tiles;
         qb = seq % q_places;
         ok = wait_bar(bar(L::B_Q + qb), (seq / q_places) & 1, s_abort, patience);
+        if (CAP && ok && fix) {
+          ok = wait_bar(bar(L::B_FIX), fixed++ & 1, s_abort, patience);
+          fix = false;
+        }
         if (!ok) break;
         auto outputs_read = [&] { return seq == 0 || wait_bar(bar(L::B_OE), (seq - 1) & 1, s_abort, patience); };
         if (two) {
