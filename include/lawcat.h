@@ -429,7 +429,8 @@ int lawcat_attn_decode_quant(const lawcat_attn_params* p, const void* q_t, const
  * it is distilled from and the softmax layers of a hybrid do). The leading `rot` channels of a head form rot / 2 pairs; pair i of a token at
  * position n is turned by the angle n freq[i] and multiplied by `scale`:
  *   (x, y) -> scale (x cos a - y sin a, x sin a + y cos a),  a = n freq[i]
- * The other channels are copied. All in fp32 but the angle, which is exact to 2^-32 of a turn at every 32-bit position; one rounding.
+ * The other channels are copied. All in fp32 but the angle, whose product with the position is exact modulo a turn at every 32-bit position and then
+ * rounded to 2^-26 of a turn; one rounding of the result.
  */
 typedef struct {
   int32_t B, T;
@@ -483,7 +484,8 @@ int lawcat_rope_bwd(const lawcat_rope_params* p, const double* freq, const void*
  * Distances (slopes) are those of the positions. Slots that hold no token yet may hold anything.
  * Rounding as in lawcat_attn_fwd; bf16 with d = 64 or 128, exact = 0 and at most 128 query heads to a key-value head runs on the tensor
  * cores. A key or value row that a node does not see does not reach its result, not even as a NaN (a row that comes out not finite is
- * computed again, which takes its time).
+ * computed again by itself, in fp32; that takes some 1 ms for each 8000 keys, beside calls of 50 us).
+ * Trees are for softmax layers: the linearized layers of a hybrid verify a chain (lawcat_layer_fwd with S0 and S_T apart), of which they keep one state.
  *   ws: may hold anything; two calls that may overlap on the GPU need one each. Blocks that share a sequence's keys wait for one another's
  *     sums: a wait that runs out ends the call, dev_status becomes LAWCAT_ERR_TIMEOUT and o_t is not to be used.
  */
@@ -494,7 +496,11 @@ int lawcat_attn_tree(const lawcat_attn_params* p, const void* q_t, const void* k
 
 /*
  * lawcat_attn_tree over a cache in 4 bits (read only); a node's key and value are what the cache would hold of k_t, v_t. On the tensor cores
- * keys, values and weights are rounded to fp16 as operands; weights are relative to a score of the row that is at most 2^8 below its largest.
+ * queries, keys, values and weights are rounded to fp16 as operands: by 2^-11 of themselves, but at least by
+ *   queries: 2^-25 of the row's largest; weights: 2^-32 of a score's of the row that is at most 2^8 below its largest;
+ *   keys, values: 17 2^-29 where a group's scale or minimum lies below 2^-21 (and is not 0).
+ * Rows that fp16 would not serve are computed again by themselves in fp32, in the time above: those that see a group of keys or values beyond
+ * +-4094, those with |scale| sum|q| above 2^14, and those whose outputs all lie below 2^-15 where the sequence has such small scales.
  */
 int lawcat_attn_tree_quant(const lawcat_attn_params* p, const void* q_t, const void* k_t, const void* v_t, const void* kq, const void* kp,
                            const void* vq, const void* vp, const int32_t* pos, const int32_t* parent, const float* slopes, void* o_t, void* ws,

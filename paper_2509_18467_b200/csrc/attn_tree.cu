@@ -4,7 +4,8 @@
 // widens to fp32 in shared memory, and keeps the running maximum and sum of each row (four rows to a warp: a key or value that is read from
 // shared memory serves four). The keys are cut into as many parts as fill the SMs, by the capacity alone, so that a captured step may be
 // replayed at every length; a second kernel joins them. For small calls latency is all of it (2 sequences of 500 tokens, 13 nodes, 4 heads of 64 in
-// fp32: 11 us, both launches).
+// fp32: 10.7 us, both launches); over long caches fp32 products from shared memory (16 sequences of 8190 tokens, 20 rows, 8/2 heads of 128, exact: 262 us,
+// over 4 bits 217; the tensor cores take 40 and 32).
 //
 // Rows of one tile see different keys of it, and a weight of zero times a value that is not finite is a NaN: a row that comes out not finite
 // is computed again by itself, from the keys that it sees and nothing else.

@@ -10,10 +10,11 @@
 // The keys are walked from the newest to the oldest: the nodes' own first, quantized as the cache would hold them, then the cached ones.
 // Slots that no row sees, and nodes that are not there, are zeros, whatever they hold.
 //
-// Bound by instruction issue and the waits between a tile's phases: 64 sequences of 16384 slots, 32 rows, d = 128: 360 us (HBM alone 155), issue 53 %,
-// integer pipe 32 %, tensor pipe 12 %; of a warp's 1470 instructions a tile half unpack codes. One sequence of 32768 slots, 64 rows: 46 us.
+// A tile's phases one after the other, with three barriers and two waits, are what it takes; no unit is at its limit: 64 sequences of 8192 to 16383
+// tokens, 32 rows, d = 128: 340 us (HBM alone 155), issue 53 %, integer pipe 32 %, tensor pipe 12 %; of a warp's 1470 instructions a tile half unpack
+// codes. One sequence of 32700 tokens, 64 rows: 41 us.
 //
-// Rounding: keys, values and weights to fp16 as operands, o once; all else fp32.
+// Rounding: queries, keys, values and weights to fp16 as operands (attn_tree_tc.cuh), o once; all else fp32.
 #include <algorithm>
 
 #include "attn_tree_tc.cuh"

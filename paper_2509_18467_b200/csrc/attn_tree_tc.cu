@@ -12,14 +12,15 @@
 // rows and take the key tiles in turn, each with sums of its own (in the same lanes of tensor memory) that meet at the segment's end. S has two
 // places per warpgroup; O is rescaled only when a maximum grew by more than 2^8.
 //
-// Up to 128 rows HBM bounds it (16 sequences of 8192 slots, 32/8 heads of 128, 32 nodes: 84.5 us, HBM alone 63; 1300 cycles of an SM a tile of
-// keys), with 256 the softmax's chain of product, maximum, weights, product (1990 cycles, 1590 at d = 64).
+// Cycles of an SM a tile of keys: 1300 up to 128 rows at d = 128, with 256 rows 1990 (1590 at d = 64), where the softmax's chain of product, maximum,
+// weights, product bounds it. 16 sequences of 4095 to 8190 tokens, 32/8 heads of 128, 32 nodes: 85 us, of which HBM alone would take 63 and the tiles take
+// 56; what is over is set-up and the join of cut segments. The same over 4 bits 125 us, with 64 nodes 171 (the warps that unpack).
 //
 // The keys are walked from the newest to the oldest: the nodes' own rows first (the values of nodes that are not there are set to zero), then
 // the cached ones, whose tiles end where the newest slot, or slot C - 1, does. What a tile holds below its oldest key are slots in front of
 // slot 0, which read as zeros, or older tokens: never a slot without a token. So a row sees a tile's columns from one limit on.
 //
-// Rounding: weights to bf16 as an operand (over 4 bits they, keys, values and queries to fp16), o once; all else fp32.
+// Rounding: weights to bf16 as an operand (over 4 bits they, keys, values and queries to fp16, attn_tree_tc.cuh), o once; all else fp32.
 #include <algorithm>
 
 #include "attn_tree_tc.cuh"

@@ -3,7 +3,7 @@
 //
 // The angle in units of a full turn is n f_i / (2 pi), and only its fraction matters. f_i / (2 pi) is held as a whole number of 2^-64 turns, so
 // that n times it, modulo 2^64, is the fraction exactly (one 64-bit product; an fp32 angle would be 0.004 off at position 131072). Its
-// leading 32 bits go through sincospi, whose argument needs no reduction.
+// leading 32 bits go through sincospi as an fp32 number (good to 2^-26 of a turn), whose argument needs no reduction.
 //
 // Memory-bound: every value is read once and written once. A block takes a few tokens; their cosines and sines are computed once, into
 // shared memory, for all heads. A thread has V pairs of a head (two loads of 16 bytes where the sizes allow it) and takes head after head, the
